@@ -543,6 +543,171 @@ size_t tg_mask_rois_workspace_bytes(int32_t n_frames, int32_t width, int32_t hei
  */
 int tg_mask_rois(const tg_mask_rois_args *args, void *stream);
 
+/* ---- Token operators: a transformer over stitched canvases ---- */
+
+/*
+ * When the model behind the canvases is a transformer, a canvas becomes a sequence of
+ * tokens, one per cell of pixels, and the patches that share it (Sec. III-C) share the
+ * sequence. Three calls make its attention layer aware of that: tg_project multiplies by a
+ * weight all cameras share and adds each camera's low-rank adapter, tg_rotate normalises
+ * queries and keys and rotates them by their position in the frame, and tg_attend lets a
+ * token see the tokens of its own patch only. With a cache they serve single tokens too.
+ * They compute forward results; nothing in this library trains.
+ *
+ * Values are binary16 or bfloat16, sums, norms and softmax statistics binary32, and each
+ * result is rounded once to nearest-even. Strides are in elements, the last dimension is
+ * contiguous.
+ */
+enum tg_type {
+  TG_F16 = 0, /* binary16 */
+  TG_BF16 = 1 /* bfloat16 */
+};
+
+/* Largest rank of an adapter. */
+#define TG_PROJECT_MAX_RANK 64
+
+typedef struct {
+  const void *x;          /* device: token t's row is x + t * x_stride, k values */
+  int64_t x_stride;       /* >= k */
+  const void *w;          /* device: output j's row is w + j * w_stride, k values */
+  int64_t w_stride;       /* >= k */
+  const int32_t *adapter; /* device [n_tokens]: adapter of each token; outside
+                             [0, n_adapters) the token has none. NULL: no token has one */
+  const void *a;          /* device [n_adapters][rank][k] */
+  const void *b;          /* device [n_adapters][n][rank] */
+  const float *scale;     /* device [n_adapters] */
+  void *y;                /* device out: token t's row is y + t * y_stride, n values */
+  int64_t y_stride;       /* >= n */
+  int32_t n_tokens, k, n, n_adapters, rank;
+  int32_t type;           /* enum tg_type of x, w, a, b and y */
+  void *workspace;        /* device scratch, 16-byte aligned, >=
+                             tg_project_workspace_bytes(...); unused without adapters */
+  size_t workspace_bytes;
+} tg_project_args;
+
+/* Device scratch tg_project needs (0 when n_tokens, k, n, n_adapters or rank is <= 0). */
+size_t tg_project_workspace_bytes(int32_t n_tokens, int32_t k, int32_t n, int32_t n_adapters,
+                                  int32_t rank);
+
+/*
+ * A shared projection with the low-rank adapters of many cameras at once: with
+ * g = adapter[t],
+ *   y[t][j] = sum_i x[t][i] w[j][i]  +  scale[g] * sum_r b[g][j][r] * h[t][r],
+ *   h[t][r] = sum_i x[t][i] a[g][r][i],
+ * the second term only for tokens that have an adapter; an adapter's values reach no token
+ * but its own, whatever they are (infinities and NaN included). Tokens may come in any order
+ * of adapters; runs of one adapter are the fastest. y must not overlap an input. h is kept to
+ * 16 bits or more (two values of the type each); everything else is summed in binary32.
+ * Enqueued on `stream`; the library allocates nothing. Returns TG_E_INVAL (null pointer,
+ * negative count, k < 1 or not a multiple of 8, n < 1, rank outside [1, TG_PROJECT_MAX_RANK]
+ * with adapters, a bad type or stride, x, w or a not 16-byte aligned or with a stride that is
+ * not a multiple of 8), TG_E_WORKSPACE, TG_E_HIP. n_tokens == 0 enqueues nothing.
+ */
+int tg_project(const tg_project_args *args, void *stream);
+
+typedef struct {
+  /* Queries and keys (and values, or NULL): value c of head h of token t is
+   * q[t * q_stride + h * q_head_stride + c], c < d. */
+  const void *q, *k, *v;
+  int64_t q_stride, q_head_stride, k_stride, k_head_stride, v_stride, v_head_stride;
+  const void *q_weight, *k_weight; /* device [d], of `type`; NULL: all ones */
+  const float *table;   /* device [n_positions][rot / 2][2]: cosine and sine of pair i at a
+                           position */
+  const int32_t *pos;   /* device [n_tokens][axes]: position of each token on each axis; a
+                           position outside [0, n_positions) counts as the nearest inside */
+  /* Results, laid out like the inputs; rows of k_out and v_out are tokens, or with `slot`
+   * rows of a cache. */
+  void *q_out, *k_out, *v_out;
+  int64_t q_out_stride, q_out_head_stride, k_out_stride, k_out_head_stride, v_out_stride,
+      v_out_head_stride;
+  const int64_t *slot;  /* device [n_tokens] or NULL: the cache row of each token's key and
+                           value; outside [0, n_rows) they are not written */
+  int64_t n_rows;       /* rows of k_out and v_out, with slot */
+  float eps;            /* >= 0, finite */
+  int32_t n_tokens, n_heads, n_kv_heads, d;
+  int32_t rot;          /* leading values of a head that are rotated: even, 0 .. d */
+  int32_t axes;         /* 1, or 2 (x, y of a token on its frame or canvas) */
+  int32_t interleaved;  /* 0: pair i is (i, i + rot / 2); 1: (2 i, 2 i + 1) */
+  int32_t n_positions;
+  int32_t type;         /* enum tg_type of everything but table */
+} tg_rotate_args;
+
+/*
+ * Norm and position rotation of queries and keys, per head, in one pass: with
+ * u = v * weight / sqrt(mean(v^2) + eps) over the d values of a head, pair i of the leading
+ * `rot` values turns by the angle whose cosine and sine are table[p][i],
+ *   (u_a, u_b) -> (u_a cos - u_b sin, u_a sin + u_b cos),
+ * p = pos[t][0], or with two axes p = pos[t][floor(2 i / (rot / 2))]: the first half of the
+ * pairs turns with the first axis, the rest with the second. The other d - rot values are
+ * normalised only. Keys, and with v_out the values (copied as they are), can go to rows of a
+ * cache instead; two tokens with the same row leave one or the other's whole value row and
+ * key row, in no set order. An output may be its own input (same pointer and strides, no
+ * slot) and must not overlap another. Enqueued on `stream`; allocates nothing. Returns
+ * TG_E_INVAL (null pointer, negative count, d outside [2, 512] or odd, bad rot, axes, type,
+ * eps, or n_positions < 1 while rot > 0), TG_E_HIP. n_tokens == 0 enqueues nothing.
+ */
+int tg_rotate(const tg_rotate_args *args, void *stream);
+
+/* Largest head size of tg_attend. */
+#define TG_ATTEND_MAX_D 128
+
+typedef struct {
+  /* Value c of head h in row r is q[r * q_stride + h * q_head_stride + c], c < d; k and v
+   * alike, with n_kv_heads heads: query head h reads key head h / (n_heads / n_kv_heads). */
+  const void *q, *k, *v;
+  int64_t q_stride, q_head_stride, k_stride, k_head_stride, v_stride, v_head_stride;
+  void *out;                 /* device out, rows and heads of q */
+  int64_t out_stride, out_head_stride;
+  const int32_t *q_begin;    /* device [n_seqs + 1]: sequence s has query rows
+                                [q_begin[s], q_begin[s + 1]), in order */
+  const int64_t *kv_begin;   /* device [n_seqs]: first key row of each sequence */
+  const int32_t *kv_len;     /* device [n_seqs]: its keys, in order; its last query stands at
+                                its last key */
+  const int32_t *prefix;     /* device [n_seqs] or NULL: every query sees the first prefix[s]
+                                keys of its sequence (with causal) */
+  const int32_t *q_doc;      /* device [n_q_rows] and [n_k_rows], both or neither: a query sees */
+  const int32_t *k_doc;      /* keys of its own document only; documents < 0 see nothing */
+  const int32_t *q_pos;      /* device [n_q_rows][2] and [n_k_rows][2], both or neither: */
+  const int32_t *k_pos;      /* positions the distance is taken from */
+  const float *slope;        /* device [n_heads] or NULL: bias per unit of distance */
+  float scale;               /* finite */
+  float cap;                 /* > 0: scores are capped; 0: not */
+  int32_t causal;            /* nonzero: a query sees keys up to its own place */
+  int32_t n_seqs, n_q_rows;
+  int64_t n_k_rows;
+  int32_t max_q_len, max_kv_len; /* bounds on the lengths; what a longer sequence has beyond
+                                    them is left out (queries unwritten, keys unread) */
+  int32_t n_heads, n_kv_heads, d;
+  int32_t type;              /* enum tg_type of q, k, v and out */
+  void *workspace;           /* device scratch, 16-byte aligned, >=
+                                tg_attend_workspace_bytes(...) */
+  size_t workspace_bytes;
+} tg_attend_args;
+
+/* Device scratch tg_attend needs (0 when it needs none, or for bad arguments). */
+size_t tg_attend_workspace_bytes(int32_t n_seqs, int32_t n_q_rows, int32_t max_q_len,
+                                 int32_t max_kv_len, int32_t n_heads, int32_t n_kv_heads,
+                                 int32_t d);
+
+/*
+ * Attention over a ragged batch. Query i of sequence s stands at place
+ * p = kv_len[s] - queries + i. Its score with key j is
+ *   z = scale * (q . k_j);  with cap z = cap * tanh(z / cap);
+ *   with slope z -= slope[h] * distance, |p - j|, or |xq - xk| + |yq - yk| of the positions;
+ * it sees key j when j <= p or j < prefix[s] or not causal, and its document is the key's
+ * (and >= 0). The output is the softmax-weighted sum of the visible v_j, 0 for a query that
+ * sees no key; keys and values it does not see do not reach it, whatever they hold. Weights
+ * are rounded to the type before the product with v, their sum is not.
+ * Rows outside [0, n_q_rows) and [0, n_k_rows) are not read or written, whatever q_begin,
+ * kv_begin and kv_len say. out must not overlap an input. Enqueued on `stream`; allocates
+ * nothing. Returns TG_E_INVAL (null pointer, negative count, d outside [8, TG_ATTEND_MAX_D]
+ * or not a multiple of 8, heads that n_kv_heads does not divide, a bad type, scale or cap,
+ * one of a pair missing, prefix without causal, q, k, v or out not 16-byte aligned or with a
+ * stride that is not a multiple of 8), TG_E_WORKSPACE, TG_E_HIP. n_seqs == 0 or
+ * n_q_rows == 0 enqueues nothing.
+ */
+int tg_attend(const tg_attend_args *args, void *stream);
+
 /* Static description of a status code. */
 const char *tg_strerror(int code);
 

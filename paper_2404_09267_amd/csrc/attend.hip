@@ -1,0 +1,883 @@
+// tg_attend: attention over a ragged batch, with capped scores, a bias by distance, a document
+// mask and a prefix mask.
+//
+// Softmax in one pass over the keys (Milakov and Gimelshein 2018; tiled as by Dao et al. 2022):
+// a running maximum m, the sum l of 2^(z - m) and the weighted sum of values, the latter two
+// multiplied by 2^(m_old - m_new) when m grows. Scores are kept in units of log2, so that a
+// weight is one exponential. m is only moved when a score passes it by more than kSlack: weights
+// then reach 2^kSlack instead of 1, which neither binary16 nor the sums mind, and the
+// accumulators are seldom touched.
+//
+// Scores are computed transposed, S^T = K Q^T: a lane holds scores of ONE query, so that m, l
+// and the correction are plain registers, and the weights come out where the second product,
+// O^T = V^T P^T, takes them as an operand. That operand's key slots are then not in key order
+// (a lane has the keys 4 h + 0..3 of every 8, h its half of the wave); the sum over keys does
+// not care, as long as V is taken in the same order, which the transposing LDS reads do.
+//
+// Two kernels: attend_tile_kernel takes 128 queries of a head at a time, attend_few_kernel the
+// few queries of all heads that share keys, with long key ranges cut over workgroups and joined
+// by join_kernel.
+//
+// A key that a query does not see has weight 0, and 0 times infinity or NaN would still reach
+// the query's sum. Such sums stay NaN, so each result is looked at once, at the end; a row that
+// is not finite is computed again by strict_row, which leaves unseen keys out one by one.
+#include <hip/hip_runtime.h>
+
+#include <climits>
+#include <cmath>
+#include <cstdint>
+
+#include "tg.h"
+#include "token_math.h"
+
+namespace {
+
+using namespace tok;
+
+constexpr int kMaxStride = 1 << 22;
+constexpr float kSlack = 8.0f;
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr int kThreads = 256;
+constexpr int kWaves = kThreads / 64;
+// Caps up to here use 1 - 2 / (1 + 2^x) for tanh, whose error of a few 2^-24 times the cap stays
+// below 1e-4 in the exponent; larger ones the function of the math library.
+constexpr float kFastCap = 256.0f;
+
+struct AttendParams {
+  const void *q, *k, *v;
+  void *out;
+  int64_t q_stride, q_head, k_stride, k_head, v_stride, v_head, out_stride, out_head;
+  const int32_t *q_begin, *kv_len, *prefix, *q_doc, *k_doc, *q_pos, *k_pos;
+  const int64_t *kv_begin;
+  const float *slope;
+  float to_log2;    // scale * log2(e): a raw score's factor
+  float cap_in;     // raw score -> exponent of 2 inside tanh: 2 log2(e) scale / cap
+  float cap_out;    // cap * log2(e)
+  float cap_arg;    // scale / cap
+  int32_t capped;   // 0 none, 1 fast, 2 exact
+  int32_t shaped;   // scores are brought to log2 units before the softmax (cap, bias, scale <= 0)
+  int32_t causal, n_seqs, n_q_rows;
+  int64_t n_k_rows;
+  int32_t max_q, max_kv, n_heads, n_kv_heads, group, d;
+  // attend_few_kernel
+  int32_t row_tiles, splits, chunk;
+  float *part;      // [splits][n_q_rows * n_heads][d] weighted sums, then
+  float *part_ml;   // [splits][n_q_rows * n_heads][2] maximum (log2 units) and sum
+};
+
+struct Seq {
+  int q0, nq;       // first query row, queries
+  int64_t k0;       // first key row
+  int nk, place0;   // keys, place of the first query
+  int prefix;
+};
+
+// A sequence, clamped to the tensors and to the caller's bounds.
+__device__ __forceinline__ Seq sequence(const AttendParams &P, int s) {
+  Seq r;
+  const int a = min(max(P.q_begin[s], 0), P.n_q_rows);
+  const int b = min(max(P.q_begin[s + 1], a), P.n_q_rows);
+  r.q0 = a;
+  r.k0 = P.kv_begin[s];
+  int64_t nk = P.kv_len[s];
+  if (r.k0 < 0 || r.k0 >= P.n_k_rows) {
+    r.k0 = 0;
+    nk = 0;
+  }
+  nk = min(max(nk, int64_t(0)), P.n_k_rows - r.k0);
+  r.place0 = static_cast<int>(nk) - (b - a);
+  r.nk = min(static_cast<int>(nk), P.max_kv);
+  r.nq = min(b - a, P.max_q);
+  r.prefix = P.prefix ? P.prefix[s] : 0;
+  return r;
+}
+
+// Keys before this one are the ones that query i may see, documents aside.
+__device__ __forceinline__ int key_limit(const AttendParams &P, const Seq &s, int i) {
+  if (!P.causal) return s.nk;
+  return min(s.nk, max(s.place0 + i + 1, s.prefix));
+}
+
+// A raw score in log2 units; `far` is the distance. (The tile kernels do the same steps.)
+__device__ __forceinline__ float shape(const AttendParams &P, float s, float slope2, float far) {
+  float z = s * P.to_log2;
+  if (P.capped == 1) {
+    z = P.cap_out - 2.0f * P.cap_out * __builtin_amdgcn_rcpf(
+                        1.0f + __builtin_amdgcn_exp2f(s * P.cap_in));
+  } else if (P.capped == 2) {
+    z = P.cap_out * tanhf(s * P.cap_arg);
+  }
+  return z - slope2 * far;
+}
+
+__device__ __forceinline__ int abs_diff(int a, int b) { return a > b ? a - b : b - a; }
+
+// One query row of one head, by one wave, unseen keys left out one by one.
+template <int kType>
+__device__ __attribute__((noinline)) void strict_row(const AttendParams &P, const Seq &s, int i,
+                                                     int head) {
+  typedef typename Num<kType>::E E;
+  const int lane = threadIdx.x & 63;
+  const int64_t row = int64_t(s.q0) + i;
+  const E *q = static_cast<const E *>(P.q) + row * P.q_stride + head * P.q_head;
+  const E *k = static_cast<const E *>(P.k) + (head / P.group) * P.k_head;
+  const E *v = static_cast<const E *>(P.v) + (head / P.group) * P.v_head;
+  const int limit = key_limit(P, s, i), place = s.place0 + i;
+  const int doc = P.q_doc ? P.q_doc[row] : 0;
+  const float slope2 = P.slope ? P.slope[head] * kLog2e : 0.0f;
+  auto score = [&](int j, bool &seen) {
+    seen = j < limit && doc >= 0 && (!P.k_doc || P.k_doc[s.k0 + j] == doc);
+    if (!seen) return -INFINITY;
+    const E *kr = k + (s.k0 + j) * P.k_stride;
+    float z = 0.0f;
+    for (int c = 0; c < P.d; ++c) z += static_cast<float>(q[c]) * static_cast<float>(kr[c]);
+    int far = abs_diff(place, j);
+    if (P.k_pos)
+      far = abs_diff(P.q_pos[2 * row], P.k_pos[2 * (s.k0 + j)]) +
+            abs_diff(P.q_pos[2 * row + 1], P.k_pos[2 * (s.k0 + j) + 1]);
+    return shape(P, z, slope2, P.slope ? static_cast<float>(far) : 0.0f);
+  };
+  float m = -INFINITY;
+  for (int j = lane; j < limit; j += 64) {
+    bool seen;
+    m = fmaxf(m, score(j, seen));
+  }
+  m = wave_max(m);
+  if (m == -INFINITY) m = 0.0f;
+  float l = 0.0f, sum[TG_ATTEND_MAX_D / 64] = {};
+  for (int j0 = 0; j0 < limit; j0 += 64) {
+    bool seen = false;
+    const float z = score(j0 + lane, seen);
+    const float p = seen ? __builtin_amdgcn_exp2f(z - m) : 0.0f;
+    l += p;
+    for (uint64_t left = __ballot(seen); left; left &= left - 1) {
+      const int at = __builtin_ctzll(left);
+      const float w = __shfl(p, at);
+      const E *vr = v + (s.k0 + j0 + at) * P.v_stride;
+#pragma unroll
+      for (int c = 0; c < TG_ATTEND_MAX_D / 64; ++c)
+        if (lane + 64 * c < P.d) sum[c] += w * static_cast<float>(vr[lane + 64 * c]);
+    }
+  }
+  l = wave_sum(l);
+  E *o = static_cast<E *>(P.out) + row * P.out_stride + head * P.out_head;
+#pragma unroll
+  for (int c = 0; c < TG_ATTEND_MAX_D / 64; ++c)
+    if (lane + 64 * c < P.d)
+      o[lane + 64 * c] = static_cast<E>(l == 0.0f ? 0.0f : sum[c] / l);
+}
+
+// Place of 16-byte chunk c of row r in a tile of rows of kChunks chunks (8 or 16). Matrix
+// operands take one chunk of 16 rows at once, transposing reads 4 chunks of 4 rows (the tile
+// kernel) or 2 chunks of 8 rows (kPairs, the kernel for few rows): all fall on 16 different
+// places of the 256 bytes that LDS serves at once.
+template <int kChunks, bool kPairs>
+__device__ __forceinline__ int place_of(int r, int c) {
+  if (kChunks == 16) {
+    const int g = kPairs ? ((r & 7) << 1) | ((r >> 3) & 1) : ((r & 3) << 2) | ((r >> 2) & 3);
+    return c ^ g;
+  }
+  const int g = kPairs ? (((r >> 1) & 3) << 1) | ((r >> 3) & 1)
+                       : (((r >> 1) & 1) << 2) | ((r >> 2) & 3);
+  return c ^ g;
+}
+
+// Loads `kRows` rows from row j0 of a head's keys or values into an LDS tile; rows past the last
+// repeat it, values past d are 0. `first`, `count`: the waves that share the work.
+template <int kRows, int kChunks, bool kPairs>
+__device__ __forceinline__ void load_rows(const void *base, int64_t stride, int64_t row, int rows,
+                                          int d, void *tile, int wave, int waves) {
+  constexpr int kPer = 64 / kChunks;  // rows of one load
+  const int lane = threadIdx.x & 63;
+  const auto b = buffer(static_cast<const char *>(base) + row * stride * 2,
+                        static_cast<uint32_t>(((min(rows, kRows) - 1) * stride + d) * 2));
+#pragma unroll
+  for (int i = 0; i < kRows / kPer; ++i) {
+    if (i % waves != wave) continue;
+    const int r = i * kPer + lane / kChunks;
+    const int c = place_of<kChunks, kPairs>(r, lane & (kChunks - 1));
+    const uint32_t off = c * 8 < d ? static_cast<uint32_t>((min(r, rows - 1) * stride + c * 8) * 2)
+                                   : kNowhere;
+    load_lds(b, static_cast<char *>(tile) + i * 1024, off, 0);
+  }
+}
+
+template <int kType>
+__device__ __forceinline__ typename Num<kType>::V4 read_transposed(const void *p) {
+  typedef __attribute__((address_space(3))) s16x4 *P3;
+  return __builtin_bit_cast(
+      typename Num<kType>::V4,
+      __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<P3>(
+          reinterpret_cast<uintptr_t>(p))));
+}
+
+// ------------------------------------------------------------------- 128 queries of a head
+
+constexpr int kBM = 128, kBN = 64;
+constexpr int kMaskTiles = 4096;  // key tiles whose documents are looked through at once
+
+template <int kType, int kD>
+__global__ __launch_bounds__(kThreads, 2) void attend_tile_kernel(const AttendParams P) {
+  typedef Num<kType> N;
+  typedef typename N::E E;
+  typedef typename N::V4 V4;
+  typedef typename N::V8 V8;
+  constexpr int kChunks = kD / 8, kSteps = kD / 16, kBlocks = kD / 32;
+  __shared__ __attribute__((aligned(16))) E tk[2][kBN * kD];
+  __shared__ __attribute__((aligned(16))) E tv[2][kBN * kD];
+  __shared__ int s_doc[2][kBN];
+  __shared__ int s_pos[2][kBN][2];
+  __shared__ uint64_t s_use[kMaskTiles / 64];
+  __shared__ int s_range[kWaves][2];
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int col = lane & 31, half = lane >> 5;
+  const int head = blockIdx.x % P.n_heads;
+  const int tile = gridDim.x / P.n_heads - 1 - blockIdx.x / P.n_heads;  // long rows first
+  // sequence b owns the tiles from q_begin[b] / kBM + b on: room for all of its queries
+  int lo = 0, hi = P.n_seqs - 1;
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (min(max(P.q_begin[mid], 0), P.n_q_rows) / kBM + mid <= tile) lo = mid; else hi = mid - 1;
+  }
+  const Seq s = sequence(P, lo);
+  const int first = (tile - (s.q0 / kBM + lo)) * kBM;
+  if (first < 0 || first >= s.nq) return;
+  const int i = first + wave * 32 + col;       // this lane's query
+  const bool live = i < s.nq;
+  const int64_t row = int64_t(s.q0) + min(i, s.nq - 1);
+  const E *qr = static_cast<const E *>(P.q) + row * P.q_stride + head * P.q_head;
+  V8 qf[kSteps];
+#pragma unroll
+  for (int k = 0; k < kSteps; ++k) {
+    qf[k] = V8{};
+    if (k * 16 + half * 8 < P.d) qf[k] = *reinterpret_cast<const V8 *>(qr + k * 16 + half * 8);
+  }
+  const void *kb = static_cast<const E *>(P.k) + (head / P.group) * P.k_head;
+  const void *vb = static_cast<const E *>(P.v) + (head / P.group) * P.v_head;
+  const int limit = live ? key_limit(P, s, i) : 0;
+  const int wave_first = first + wave * 32;
+  // every key before `all` is seen by all of the wave's queries, none from `end` on by any of
+  // the workgroup's (limits do not fall with i)
+  const int all = key_limit(P, s, min(wave_first, s.nq - 1));
+  const int end = key_limit(P, s, min(first + kBM, s.nq) - 1);
+  const int wave_end = wave_first < s.nq ? key_limit(P, s, min(wave_first + 32, s.nq) - 1) : 0;
+  int doc = P.q_doc && live ? P.q_doc[row] : -1;
+  const float slope2 = P.slope ? P.slope[head] * kLog2e : 0.0f;
+  const int place = s.place0 + i;
+  int px = 0, py = 0;
+  if (P.q_pos) {
+    px = P.q_pos[2 * row];
+    py = P.q_pos[2 * row + 1];
+  }
+  int wave_lo = INT_MAX, wave_hi = -1;  // the documents of the wave's queries
+  int block_lo = INT_MAX, block_hi = -1;
+  if (P.q_doc) {
+    int a = doc >= 0 ? doc : INT_MAX, b = doc;
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) {
+      a = min(a, __shfl_xor(a, o));
+      b = max(b, __shfl_xor(b, o));
+    }
+    wave_lo = a;
+    wave_hi = b;
+    if (lane == 0) {
+      s_range[wave][0] = a;
+      s_range[wave][1] = b;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      block_lo = min(block_lo, s_range[w][0]);
+      block_hi = max(block_hi, s_range[w][1]);
+    }
+    if (doc < 0) doc = INT_MIN;  // equal to no key's
+  }
+  f32x16 acc[kBlocks] = {};
+  float m = -INFINITY, l = 0.0f;
+  const float unit = P.shaped ? 1.0f : P.to_log2;
+  const int tiles = (end + kBN - 1) / kBN;
+
+  for (int seg = 0; seg < tiles; seg += kMaskTiles) {
+    const int seg_end = min(tiles, seg + kMaskTiles);
+    if (P.k_doc) {  // which tiles hold a key whose document is in the queries' range
+      __syncthreads();
+      for (int t = threadIdx.x; t < kMaskTiles / 64; t += kThreads) s_use[t] = 0;
+      __syncthreads();
+      for (int t = seg + wave; t < seg_end; t += kWaves) {
+        const int j = t * kBN + lane;
+        const int kd = j < end ? P.k_doc[s.k0 + j] : -1;
+        if (__ballot(kd >= block_lo && kd <= block_hi) && lane == 0)
+          atomicOr(reinterpret_cast<unsigned long long *>(&s_use[(t - seg) >> 6]),
+                   1ull << ((t - seg) & 63));
+      }
+      __syncthreads();
+    }
+    auto next = [&](int t) {  // the first tile to visit from t on
+      if (!P.k_doc) return t;
+      while (t < seg_end) {
+        const uint64_t w = s_use[(t - seg) >> 6] >> ((t - seg) & 63);
+        if (w) {
+          t += __builtin_ctzll(w);
+          break;
+        }
+        t = seg + (((t - seg) >> 6) + 1) * 64;
+      }
+      return __builtin_amdgcn_readfirstlane(t);
+    };
+    auto fetch = [&](int t, int to) {
+      const int j0 = t * kBN;
+      load_rows<kBN, kChunks, false>(kb, P.k_stride, s.k0 + j0, s.nk - j0, P.d, tk[to], wave,
+                                     kWaves);
+      load_rows<kBN, kChunks, false>(vb, P.v_stride, s.k0 + j0, s.nk - j0, P.d, tv[to], wave,
+                                     kWaves);
+      if (wave == 0 && (P.k_doc || P.k_pos)) {
+        const int64_t r = s.k0 + min(j0 + lane, s.nk - 1);
+        if (P.k_doc) s_doc[to][lane] = P.k_doc[r];
+        if (P.k_pos) {
+          s_pos[to][lane][0] = P.k_pos[2 * r];
+          s_pos[to][lane][1] = P.k_pos[2 * r + 1];
+        }
+      }
+    };
+    int t = next(seg), buf = 0;
+    if (t < seg_end) fetch(t, 0);
+    while (t < seg_end) {
+      const int j0 = t * kBN;
+      const int after = next(t + 1);
+      wait_loads();
+      __syncthreads();
+      if (after < seg_end) fetch(after, buf ^ 1);
+      bool skip = j0 >= wave_end, docs = false;
+      if (P.k_doc && !skip) {
+        const int kd = s_doc[buf][lane];
+        skip = __ballot(kd >= wave_lo && kd <= wave_hi) == 0;
+        docs = !(wave_lo == wave_hi && __ballot(kd == wave_lo) == ~0ull &&
+                 __ballot(doc == wave_lo) == ~0ull);
+      }
+      if (!skip) {
+        f32x16 z[2] = {};
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+          for (int k = 0; k < kSteps; ++k) {
+            const int r = b * 32 + col;
+            const V8 kf = *reinterpret_cast<const V8 *>(
+                tk[buf] + r * kD + place_of<kChunks, false>(r, 2 * k + half) * 8);
+            z[b] = N::mfma32(kf, qf[k], z[b]);
+          }
+        if (P.shaped) {
+          if (P.capped == 1) {
+#pragma unroll
+            for (int e = 0; e < 32; ++e)
+              z[e >> 4][e & 15] =
+                  P.cap_out - 2.0f * P.cap_out *
+                                  __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(
+                                                                   z[e >> 4][e & 15] * P.cap_in));
+          } else if (P.capped == 2) {
+            for (int b = 0; b < 2; ++b)
+#pragma unroll
+              for (int e = 0; e < 16; ++e) z[b][e] = P.cap_out * tanhf(z[b][e] * P.cap_arg);
+          } else {
+#pragma unroll
+            for (int e = 0; e < 32; ++e) z[e >> 4][e & 15] *= P.to_log2;
+          }
+          if (P.slope && !P.k_pos) {
+            const float here = static_cast<float>(place - j0 - 4 * half);
+#pragma unroll
+            for (int e = 0; e < 32; ++e)
+              z[e >> 4][e & 15] -=
+                  slope2 * fabsf(here - static_cast<float>((e >> 2) * 8 + (e & 3)));
+          } else if (P.slope) {
+#pragma unroll
+            for (int e = 0; e < 32; ++e) {
+              const int j = (e >> 2) * 8 + 4 * half + (e & 3);
+              const int far = abs_diff(px, s_pos[buf][j][0]) + abs_diff(py, s_pos[buf][j][1]);
+              z[e >> 4][e & 15] -= slope2 * static_cast<float>(far);
+            }
+          }
+        }
+        if (j0 + kBN > all) {
+          const int last = limit - j0 - 4 * half;
+#pragma unroll
+          for (int e = 0; e < 32; ++e)
+            if ((e >> 2) * 8 + (e & 3) >= last) z[e >> 4][e & 15] = -INFINITY;
+        }
+        if (docs) {
+#pragma unroll
+          for (int e = 0; e < 32; ++e)
+            if (s_doc[buf][(e >> 2) * 8 + 4 * half + (e & 3)] != doc)
+              z[e >> 4][e & 15] = -INFINITY;
+        }
+        float big = -INFINITY;
+#pragma unroll
+        for (int e = 0; e < 32; ++e) big = fmaxf(big, z[e >> 4][e & 15]);
+        big *= unit;
+        {
+          const auto r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(unsigned, big),
+                                                          __builtin_bit_cast(unsigned, big), false,
+                                                          false);
+          big = fmaxf(__builtin_bit_cast(float, static_cast<unsigned>(r[0])),
+                      __builtin_bit_cast(float, static_cast<unsigned>(r[1])));
+        }
+        if (__ballot(big > m + kSlack)) {
+          const float to = fmaxf(m, big);
+          const float fix = to == m ? 1.0f : __builtin_amdgcn_exp2f(m - to);
+          m = to;
+          l *= fix;
+#pragma unroll
+          for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) acc[b][r] *= fix;
+        }
+        const float base = m == -INFINITY ? 0.0f : m;
+#pragma unroll
+        for (int e = 0; e < 32; ++e) {
+          const float p =
+              __builtin_amdgcn_exp2f(__builtin_fmaf(z[e >> 4][e & 15], unit, -base));
+          z[e >> 4][e & 15] = p;
+          l += p;
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {  // 16 keys
+          V8 pf;
+#pragma unroll
+          for (int e = 0; e < 8; e += 2) {
+            const auto two =
+                pack2<kType>(z[k >> 1][(k & 1) * 8 + e], z[k >> 1][(k & 1) * 8 + e + 1]);
+            pf[e] = two[0];
+            pf[e + 1] = two[1];
+          }
+          const int i16 = lane & 15, g = (lane >> 4) & 1;
+#pragma unroll
+          for (int b = 0; b < kBlocks; ++b) {
+            const int r0 = k * 16 + 4 * half + (i16 >> 2);
+            const int c = 4 * b + 2 * g + ((i16 & 3) >> 1);
+            const V4 v0 = read_transposed<kType>(
+                tv[buf] + r0 * kD + place_of<kChunks, false>(r0, c) * 8 + (i16 & 1) * 4);
+            const V4 v1 = read_transposed<kType>(
+                tv[buf] + (r0 + 8) * kD + place_of<kChunks, false>(r0 + 8, c) * 8 +
+                (i16 & 1) * 4);
+            const V8 vf = __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7);
+            acc[b] = N::mfma32(vf, pf, acc[b]);
+          }
+        }
+      }
+      t = after;
+      buf ^= 1;
+    }
+  }
+
+  l += __shfl_xor(l, 32);
+  const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+  bool fine = true;
+  E *o = static_cast<E *>(P.out) + row * P.out_stride + head * P.out_head;
+#pragma unroll
+  for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+    for (int r4 = 0; r4 < 4; ++r4) {
+      const int c = b * 32 + r4 * 8 + 4 * half;
+      f32x4 v;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        v[r] = l == 0.0f ? 0.0f : acc[b][r4 * 4 + r] * inv;
+        fine = fine && fabsf(v[r]) < INFINITY;
+      }
+      if (live && c < P.d) *reinterpret_cast<V4 *>(o + c) = __builtin_convertvector(v, V4);
+    }
+  uint64_t bad = __ballot(!fine && live);
+  bad = (bad | (bad >> 32)) & 0xFFFFFFFFull;
+  for (; bad; bad &= bad - 1)
+    strict_row<kType>(P, s, wave_first + __builtin_ctzll(bad), head);
+}
+
+// ------------------------------------------------------------------------ few queries
+
+// Rows of a workgroup: 16 (query, head) pairs that share a key head, query-major. Each wave
+// takes every kWaves'th 32 keys of the workgroup's range through LDS of its own.
+template <int kType, int kD>
+__global__ __launch_bounds__(kThreads) void attend_few_kernel(const AttendParams P) {
+  typedef Num<kType> N;
+  typedef typename N::E E;
+  typedef typename N::V4 V4;
+  typedef typename N::V8 V8;
+  constexpr int kChunks = kD / 8, kSteps = kD / 32, kBlocks = kD / 16, kKeys = 32;
+  __shared__ __attribute__((aligned(16))) E tile[kWaves][2][2][kKeys * kD];
+  __shared__ float s_m[kWaves][16], s_l[kWaves][16];
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int col = lane & 15, quad = lane >> 4;
+  int id = blockIdx.x;
+  const int kvh = id % P.n_kv_heads;
+  id /= P.n_kv_heads;
+  const int rt = id % P.row_tiles;
+  id /= P.row_tiles;
+  const int split = id % P.splits, si = id / P.splits;
+  const Seq s = sequence(P, si);
+  const int rows = s.nq * P.group;
+  if (rt * 16 >= rows) return;
+  const int from = split * P.chunk;
+  const int my = rt * 16 + col;  // this lane's row
+  const bool live = my < rows;
+  const int i = (live ? my : rows - 1) / P.group;
+  const int head = kvh * P.group + (live ? my : rows - 1) % P.group;
+  const int end = min(from + P.chunk, key_limit(P, s, (min(rt * 16 + 16, rows) - 1) / P.group));
+  const int all = key_limit(P, s, rt * 16 / P.group);
+  const int64_t row = int64_t(s.q0) + i;
+  if (split > 0 && from >= end) return;  // join_kernel knows
+  const E *qr = static_cast<const E *>(P.q) + row * P.q_stride + head * P.q_head;
+  V8 qf[kSteps];
+#pragma unroll
+  for (int k = 0; k < kSteps; ++k) {
+    qf[k] = V8{};
+    if (k * 32 + quad * 8 < P.d) qf[k] = *reinterpret_cast<const V8 *>(qr + k * 32 + quad * 8);
+  }
+  const void *kb = static_cast<const E *>(P.k) + kvh * P.k_head;
+  const void *vb = static_cast<const E *>(P.v) + kvh * P.v_head;
+  const int limit = live ? key_limit(P, s, i) : 0;
+  int doc = P.q_doc ? P.q_doc[row] : 0;
+  if (doc < 0) doc = INT_MIN;
+  const float slope2 = P.slope ? P.slope[head] * kLog2e : 0.0f;
+  const int place = s.place0 + i;
+  int px = 0, py = 0;
+  if (P.q_pos) {
+    px = P.q_pos[2 * row];
+    py = P.q_pos[2 * row + 1];
+  }
+  f32x4 acc[kBlocks] = {};
+  float m = -INFINITY, l = 0.0f;
+  const float unit = P.shaped ? 1.0f : P.to_log2;
+  auto fetch = [&](int j0, int to) {
+    load_rows<kKeys, kChunks, true>(kb, P.k_stride, s.k0 + j0, s.nk - j0, P.d, tile[wave][to][0],
+                                    0, 1);
+    load_rows<kKeys, kChunks, true>(vb, P.v_stride, s.k0 + j0, s.nk - j0, P.d, tile[wave][to][1],
+                                    0, 1);
+  };
+  int j0 = from + wave * kKeys, buf = 0;
+  if (j0 < end) fetch(j0, 0);
+  for (; j0 < end; j0 += kWaves * kKeys) {
+    wait_loads();
+    const E *tk = tile[wave][buf][0], *tv = tile[wave][buf][1];
+    if (j0 + kWaves * kKeys < end) fetch(j0 + kWaves * kKeys, buf ^ 1);
+    f32x4 z[2] = {};
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+      for (int k = 0; k < kSteps; ++k) {
+        const int r = b * 16 + col;
+        const V8 kf = *reinterpret_cast<const V8 *>(
+            tk + r * kD + place_of<kChunks, true>(r, 4 * k + quad) * 8);
+        z[b] = N::mfma16(kf, qf[k], z[b]);
+      }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const int j = j0 + (e >> 2) * 16 + 4 * quad + (e & 3);
+      float ze = z[e >> 2][e & 3];
+      if (P.shaped) {
+        float far = 0.0f;
+        if (P.slope) {
+          int f = abs_diff(place, j);
+          if (P.k_pos) {
+            const int64_t r = s.k0 + min(j, s.nk - 1);
+            f = abs_diff(px, P.k_pos[2 * r]) + abs_diff(py, P.k_pos[2 * r + 1]);
+          }
+          far = static_cast<float>(f);
+        }
+        ze = shape(P, ze, slope2, far);
+      }
+      if (j0 + kKeys > all && j >= limit) ze = -INFINITY;
+      if (P.k_doc && P.k_doc[s.k0 + min(j, s.nk - 1)] != doc) ze = -INFINITY;
+      z[e >> 2][e & 3] = ze;
+    }
+    float big = -INFINITY;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) big = fmaxf(big, z[e >> 2][e & 3]);
+    big *= unit;
+    if (__ballot(big > m + kSlack)) {
+      big = fmaxf(big, __shfl_xor(big, 16));
+      big = fmaxf(big, __shfl_xor(big, 32));
+      const float to = fmaxf(m, big);
+      const float fix = to == m ? 1.0f : __builtin_amdgcn_exp2f(m - to);
+      m = to;
+      l *= fix;
+#pragma unroll
+      for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) acc[b][r] *= fix;
+    }
+    const float base = m == -INFINITY ? 0.0f : m;
+    V8 pf;
+#pragma unroll
+    for (int e = 0; e < 8; e += 2) {
+      const float p0 =
+          __builtin_amdgcn_exp2f(__builtin_fmaf(z[e >> 2][e & 3], unit, -base));
+      const float p1 =
+          __builtin_amdgcn_exp2f(__builtin_fmaf(z[e >> 2][(e & 3) + 1], unit, -base));
+      l += p0 + p1;
+      const auto two = pack2<kType>(p0, p1);
+      pf[e] = two[0];
+      pf[e + 1] = two[1];
+    }
+#pragma unroll
+    for (int b = 0; b < kBlocks; ++b) {
+      const int r0 = 4 * quad + (col >> 2), c = 2 * b + ((col & 3) >> 1);
+      const V4 v0 = read_transposed<kType>(
+          tv + r0 * kD + place_of<kChunks, true>(r0, c) * 8 + (col & 1) * 4);
+      const V4 v1 = read_transposed<kType>(
+          tv + (r0 + 16) * kD + place_of<kChunks, true>(r0 + 16, c) * 8 + (col & 1) * 4);
+      const V8 vf = __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7);
+      acc[b] = N::mfma16(vf, pf, acc[b]);
+    }
+    buf ^= 1;
+  }
+  // the waves' ranges are joined through LDS
+  l += __shfl_xor(l, 16);
+  l += __shfl_xor(l, 32);
+  __syncthreads();  // the tiles are done with
+  float *sums = reinterpret_cast<float *>(&tile[0][0][0][0]);  // [kWaves][16][kD]
+  if (quad == 0) {
+    s_m[wave][col] = m;
+    s_l[wave][col] = l;
+  }
+#pragma unroll
+  for (int b = 0; b < kBlocks; ++b)
+    *reinterpret_cast<f32x4 *>(sums + (wave * 16 + col) * kD + b * 16 + quad * 4) = acc[b];
+  __syncthreads();
+  const int r = threadIdx.x >> 4, c0 = threadIdx.x & 15;  // 16 threads a row
+  const int mine = rt * 16 + r;
+  float top = -INFINITY;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) top = fmaxf(top, s_m[w][r]);
+  float f[kWaves], total = 0.0f;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) {
+    f[w] = s_m[w][r] == top ? 1.0f : __builtin_amdgcn_exp2f(s_m[w][r] - top);
+    total += f[w] * s_l[w][r];
+  }
+  const int64_t orow = int64_t(s.q0) + min(mine, rows - 1) / P.group;
+  const int ohead = kvh * P.group + min(mine, rows - 1) % P.group;
+  const int64_t flat = orow * P.n_heads + ohead;
+  const int64_t all_rows = int64_t(P.n_q_rows) * P.n_heads;
+  float *part = P.part + (split * all_rows + flat) * P.d;
+  E *o = static_cast<E *>(P.out) + orow * P.out_stride + ohead * P.out_head;
+  bool fine = true;
+#pragma unroll
+  for (int b = 0; b < kD / 16; ++b) {
+    const int c = b * 16 + c0;
+    float v = 0.0f;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) v += f[w] * sums[(w * 16 + r) * kD + c];
+    if (mine < rows && c < P.d) {
+      if (P.splits == 1) {
+        v = total == 0.0f ? 0.0f : v / total;
+        fine = fine && fabsf(v) < INFINITY;
+        o[c] = static_cast<E>(v);
+      } else {
+        part[c] = v;
+      }
+    }
+  }
+  if (P.splits > 1) {
+    if (mine < rows && c0 == 0) {
+      P.part_ml[(split * all_rows + flat) * 2] = top;
+      P.part_ml[(split * all_rows + flat) * 2 + 1] = total;
+    }
+    return;
+  }
+  for (uint64_t bad = __ballot(!fine); bad;) {
+    const int w = __builtin_ctzll(bad) >> 4;  // row of the wave
+    bad &= ~(0xFFFFull << (16 * w));
+    const int rr = rt * 16 + wave * 4 + w;
+    strict_row<kType>(P, s, rr / P.group, kvh * P.group + rr % P.group);
+  }
+}
+
+// Joins the parts of a row: one wave a row.
+template <int kType>
+__global__ __launch_bounds__(kThreads) void join_kernel(const AttendParams P) {
+  typedef typename Num<kType>::E E;
+  const int lane = threadIdx.x & 63;
+  const int per = P.row_tiles * 16;  // rows of a sequence and key head
+  int64_t id = int64_t(blockIdx.x) * kWaves + (threadIdx.x >> 6);
+  const int my = static_cast<int>(id % per);
+  id /= per;
+  const int kvh = static_cast<int>(id % P.n_kv_heads);
+  const int si = static_cast<int>(id / P.n_kv_heads);
+  if (si >= P.n_seqs) return;
+  const Seq s = sequence(P, si);
+  const int rows = s.nq * P.group;
+  if (my >= rows) return;
+  const int i = my / P.group, head = kvh * P.group + my % P.group;
+  // the splits that attend_few_kernel ran for this row's tile
+  const int rt = my / 16;
+  const int end = key_limit(P, s, (min(rt * 16 + 16, rows) - 1) / P.group);
+  const int n = min(max((end + P.chunk - 1) / P.chunk, 1), P.splits);
+  const int64_t flat = (int64_t(s.q0) + i) * P.n_heads + head;
+  const int64_t all_rows = int64_t(P.n_q_rows) * P.n_heads;
+  float top = -INFINITY;
+  for (int k = lane; k < n; k += 64) top = fmaxf(top, P.part_ml[(k * all_rows + flat) * 2]);
+  top = wave_max(top);
+  float total = 0.0f, sum[TG_ATTEND_MAX_D / 64] = {};
+  for (int k = 0; k < n; ++k) {
+    const float pm = P.part_ml[(k * all_rows + flat) * 2];
+    const float f = pm == top ? 1.0f : __builtin_amdgcn_exp2f(pm - top);
+    total += f * P.part_ml[(k * all_rows + flat) * 2 + 1];
+#pragma unroll
+    for (int c = 0; c < TG_ATTEND_MAX_D / 64; ++c)
+      if (lane + 64 * c < P.d) sum[c] += f * P.part[(k * all_rows + flat) * P.d + lane + 64 * c];
+  }
+  E *o = static_cast<E *>(P.out) + (int64_t(s.q0) + i) * P.out_stride + head * P.out_head;
+  bool fine = true;
+#pragma unroll
+  for (int c = 0; c < TG_ATTEND_MAX_D / 64; ++c)
+    if (lane + 64 * c < P.d) {
+      const float v = total == 0.0f ? 0.0f : sum[c] / total;
+      fine = fine && fabsf(v) < INFINITY;
+      o[lane + 64 * c] = static_cast<E>(v);
+    }
+  if (__ballot(!fine)) strict_row<kType>(P, s, i, head);
+}
+
+// ------------------------------------------------------------------------------- the host
+
+// How few queries are split: `few` when a key head's rows fit a few 16-row tiles.
+struct Split {
+  bool few;
+  int row_tiles, splits, chunk;
+};
+
+Split split_of(int n_seqs, int max_q, int max_kv, int n_heads, int n_kv_heads) {
+  Split r = {};
+  const int64_t rows = int64_t(max_q) * (n_heads / n_kv_heads);
+  r.few = rows <= 64;
+  if (!r.few) return r;
+  r.row_tiles = static_cast<int>((rows + 15) / 16);
+  const int64_t blocks = int64_t(n_seqs) * n_kv_heads * r.row_tiles;
+  const int64_t want = (1024 + blocks - 1) / blocks;
+  const int64_t most = (int64_t(max_kv) + 255) / 256;
+  r.splits = static_cast<int>(want < most ? want : most);
+  if (r.splits < 1) r.splits = 1;
+  r.chunk = static_cast<int>(((int64_t(max_kv) + r.splits - 1) / r.splits + 127) / 128 * 128);
+  if (r.chunk < 128) r.chunk = 128;
+  r.splits = static_cast<int>((int64_t(max_kv) + r.chunk - 1) / r.chunk);
+  if (r.splits < 1) r.splits = 1;
+  return r;
+}
+
+template <int kType, int kD>
+int launch(const AttendParams &P, const Split &sp, hipStream_t s) {
+  if (sp.few) {
+    const int64_t blocks = int64_t(P.n_seqs) * P.n_kv_heads * sp.row_tiles * sp.splits;
+    if (blocks > INT32_MAX) return TG_E_INVAL;
+    hipLaunchKernelGGL((attend_few_kernel<kType, kD>), dim3(static_cast<uint32_t>(blocks)),
+                       dim3(kThreads), 0, s, P);
+    if (sp.splits > 1) {
+      const int64_t waves = int64_t(P.n_seqs) * P.n_kv_heads * sp.row_tiles * 16;
+      hipLaunchKernelGGL(join_kernel<kType>, dim3(static_cast<uint32_t>((waves + 3) / 4)),
+                         dim3(kThreads), 0, s, P);
+    }
+  } else {
+    const int64_t blocks = (int64_t(P.n_q_rows) / kBM + P.n_seqs) * P.n_heads;
+    if (blocks > INT32_MAX) return TG_E_INVAL;
+    hipLaunchKernelGGL((attend_tile_kernel<kType, kD>), dim3(static_cast<uint32_t>(blocks)),
+                       dim3(kThreads), 0, s, P);
+  }
+  return hipGetLastError() == hipSuccess ? TG_OK : TG_E_HIP;
+}
+
+bool layout_ok(const void *p, int64_t stride, int64_t head) {
+  return p && aligned16(p) && stride >= 0 && stride <= kMaxStride && stride % 8 == 0 &&
+         head >= 0 && head % 8 == 0;
+}
+
+bool sizes_ok(int n_seqs, int n_q_rows, int max_q, int max_kv, int n_heads, int n_kv_heads,
+              int d) {
+  return n_seqs >= 0 && n_q_rows >= 0 && max_q >= 0 && max_kv >= 0 && n_heads >= 1 &&
+         n_kv_heads >= 1 && n_heads % n_kv_heads == 0 && d >= 8 && d <= TG_ATTEND_MAX_D &&
+         d % 8 == 0;
+}
+
+}  // namespace
+
+extern "C" size_t tg_attend_workspace_bytes(int32_t n_seqs, int32_t n_q_rows, int32_t max_q_len,
+                                            int32_t max_kv_len, int32_t n_heads,
+                                            int32_t n_kv_heads, int32_t d) {
+  if (!sizes_ok(n_seqs, n_q_rows, max_q_len, max_kv_len, n_heads, n_kv_heads, d)) return 0;
+  if (n_seqs == 0 || n_q_rows == 0 || max_q_len == 0) return 0;
+  const Split sp = split_of(n_seqs, max_q_len, max_kv_len, n_heads, n_kv_heads);
+  if (!sp.few || sp.splits == 1) return 0;
+  return static_cast<size_t>(sp.splits) * n_q_rows * n_heads * (d + 2) * sizeof(float);
+}
+
+extern "C" int tg_attend(const tg_attend_args *a, void *stream) {
+  if (!a || !type_ok(a->type) ||
+      !sizes_ok(a->n_seqs, a->n_q_rows, a->max_q_len, a->max_kv_len, a->n_heads, a->n_kv_heads,
+                a->d) ||
+      a->n_k_rows < 0 || !std::isfinite(a->scale) || !std::isfinite(a->cap) || a->cap < 0.0f)
+    return TG_E_INVAL;
+  if ((a->q_doc == nullptr) != (a->k_doc == nullptr) ||
+      (a->q_pos == nullptr) != (a->k_pos == nullptr) || (a->prefix && !a->causal))
+    return TG_E_INVAL;
+  if (a->n_seqs == 0 || a->n_q_rows == 0 || a->max_q_len == 0) return TG_OK;
+  if (!a->q_begin || !a->kv_begin || !a->kv_len || !layout_ok(a->q, a->q_stride, a->q_head_stride) ||
+      !layout_ok(a->out, a->out_stride, a->out_head_stride))
+    return TG_E_INVAL;
+  if (a->n_k_rows > 0 && (!layout_ok(a->k, a->k_stride, a->k_head_stride) ||
+                          !layout_ok(a->v, a->v_stride, a->v_head_stride)))
+    return TG_E_INVAL;
+  const Split sp = split_of(a->n_seqs, a->max_q_len, a->max_kv_len, a->n_heads, a->n_kv_heads);
+  const size_t need = tg_attend_workspace_bytes(a->n_seqs, a->n_q_rows, a->max_q_len,
+                                                a->max_kv_len, a->n_heads, a->n_kv_heads, a->d);
+  if (need > 0 && (!a->workspace || a->workspace_bytes < need || !aligned16(a->workspace)))
+    return TG_E_WORKSPACE;
+
+  AttendParams P = {};
+  P.q = a->q;
+  P.k = a->k;
+  P.v = a->v;
+  P.out = a->out;
+  P.q_stride = a->q_stride;
+  P.q_head = a->q_head_stride;
+  P.k_stride = a->k_stride;
+  P.k_head = a->k_head_stride;
+  P.v_stride = a->v_stride;
+  P.v_head = a->v_head_stride;
+  P.out_stride = a->out_stride;
+  P.out_head = a->out_head_stride;
+  P.q_begin = a->q_begin;
+  P.kv_begin = a->kv_begin;
+  P.kv_len = a->kv_len;
+  P.prefix = a->prefix;
+  P.q_doc = a->q_doc;
+  P.k_doc = a->k_doc;
+  P.q_pos = a->q_pos;
+  P.k_pos = a->k_pos;
+  P.slope = a->slope;
+  P.to_log2 = a->scale * kLog2e;
+  if (a->cap > 0.0f) {
+    P.capped = a->cap <= kFastCap ? 1 : 2;
+    P.cap_arg = a->scale / a->cap;
+    P.cap_in = 2.0f * kLog2e * P.cap_arg;
+    P.cap_out = a->cap * kLog2e;
+  }
+  P.shaped = P.capped || a->slope || !(P.to_log2 > 0.0f);
+  P.causal = a->causal != 0;
+  P.n_seqs = a->n_seqs;
+  P.n_q_rows = a->n_q_rows;
+  P.n_k_rows = a->n_k_rows;
+  P.max_q = a->max_q_len;
+  P.max_kv = a->max_kv_len;
+  P.n_heads = a->n_heads;
+  P.n_kv_heads = a->n_kv_heads;
+  P.group = a->n_heads / a->n_kv_heads;
+  P.d = a->d;
+  P.row_tiles = sp.row_tiles;
+  P.splits = sp.splits;
+  P.chunk = sp.chunk;
+  P.part = static_cast<float *>(a->workspace);
+  P.part_ml = P.part + static_cast<size_t>(sp.splits) * a->n_q_rows * a->n_heads * a->d;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  if (a->d <= 64)
+    return a->type == TG_F16 ? launch<TG_F16, 64>(P, sp, s) : launch<TG_BF16, 64>(P, sp, s);
+  return a->type == TG_F16 ? launch<TG_F16, 128>(P, sp, s) : launch<TG_BF16, 128>(P, sp, s);
+}

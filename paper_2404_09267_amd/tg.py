@@ -94,7 +94,42 @@ class MaskRoisArgs(ctypes.Structure):
                 ("workspace_bytes", ctypes.c_size_t)]
 
 
+class ProjectArgs(ctypes.Structure):
+    _fields_ = [("x", _vp), ("x_stride", _i64), ("w", _vp), ("w_stride", _i64), ("adapter", _vp),
+                ("a", _vp), ("b", _vp), ("scale", _vp), ("y", _vp), ("y_stride", _i64),
+                ("n_tokens", _i32), ("k", _i32), ("n", _i32), ("n_adapters", _i32),
+                ("rank", _i32), ("type", _i32), ("workspace", _vp),
+                ("workspace_bytes", ctypes.c_size_t)]
+
+
+class RotateArgs(ctypes.Structure):
+    _fields_ = [("q", _vp), ("k", _vp), ("v", _vp), ("q_stride", _i64), ("q_head_stride", _i64),
+                ("k_stride", _i64), ("k_head_stride", _i64), ("v_stride", _i64),
+                ("v_head_stride", _i64), ("q_weight", _vp), ("k_weight", _vp), ("table", _vp),
+                ("pos", _vp), ("q_out", _vp), ("k_out", _vp), ("v_out", _vp),
+                ("q_out_stride", _i64), ("q_out_head_stride", _i64), ("k_out_stride", _i64),
+                ("k_out_head_stride", _i64), ("v_out_stride", _i64), ("v_out_head_stride", _i64),
+                ("slot", _vp), ("n_rows", _i64), ("eps", _f32), ("n_tokens", _i32),
+                ("n_heads", _i32), ("n_kv_heads", _i32), ("d", _i32), ("rot", _i32),
+                ("axes", _i32), ("interleaved", _i32), ("n_positions", _i32), ("type", _i32)]
+
+
+class AttendArgs(ctypes.Structure):
+    _fields_ = [("q", _vp), ("k", _vp), ("v", _vp), ("q_stride", _i64), ("q_head_stride", _i64),
+                ("k_stride", _i64), ("k_head_stride", _i64), ("v_stride", _i64),
+                ("v_head_stride", _i64), ("out", _vp), ("out_stride", _i64),
+                ("out_head_stride", _i64), ("q_begin", _vp), ("kv_begin", _vp), ("kv_len", _vp),
+                ("prefix", _vp), ("q_doc", _vp), ("k_doc", _vp), ("q_pos", _vp), ("k_pos", _vp),
+                ("slope", _vp), ("scale", _f32), ("cap", _f32), ("causal", _i32),
+                ("n_seqs", _i32), ("n_q_rows", _i32), ("n_k_rows", _i64), ("max_q_len", _i32),
+                ("max_kv_len", _i32), ("n_heads", _i32), ("n_kv_heads", _i32), ("d", _i32),
+                ("type", _i32), ("workspace", _vp), ("workspace_bytes", ctypes.c_size_t)]
+
+
 GMM_MAX_MIX = 5
+F16, BF16 = 0, 1  # enum tg_type
+PROJECT_MAX_RANK = 64
+ATTEND_MAX_D = 128
 
 EXPORTS = ["tg_gmm_plane_stride", "tg_gmm_state_bytes", "tg_gmm_update",
            "tg_mask_rois_workspace_bytes", "tg_mask_rois", "tg_partition_workspace_bytes", "tg_partition", "tg_plan_pack", "tg_batch_count",
@@ -102,6 +137,8 @@ EXPORTS = ["tg_gmm_plane_stride", "tg_gmm_state_bytes", "tg_gmm_update",
            "tg_stitch_units", "tg_stitch_norm_uses_table",
            "tg_unstitch_workspace_bytes", "tg_unstitch", "tg_unstitch_noalloc",
            "tg_merge_workspace_bytes", "tg_merge",
+           "tg_project_workspace_bytes", "tg_project", "tg_rotate",
+           "tg_attend_workspace_bytes", "tg_attend",
            "tg_strerror", "tg_abi_version"]
 
 _lib = None
@@ -174,6 +211,16 @@ def lib() -> ctypes.CDLL:
         L.tg_mask_rois_workspace_bytes.restype = ctypes.c_size_t
         L.tg_mask_rois.argtypes = [ctypes.POINTER(MaskRoisArgs), _vp]
         L.tg_mask_rois.restype = ctypes.c_int
+        L.tg_project_workspace_bytes.argtypes = [_i32] * 5
+        L.tg_project_workspace_bytes.restype = ctypes.c_size_t
+        L.tg_project.argtypes = [ctypes.POINTER(ProjectArgs), _vp]
+        L.tg_project.restype = ctypes.c_int
+        L.tg_rotate.argtypes = [ctypes.POINTER(RotateArgs), _vp]
+        L.tg_rotate.restype = ctypes.c_int
+        L.tg_attend_workspace_bytes.argtypes = [_i32] * 7
+        L.tg_attend_workspace_bytes.restype = ctypes.c_size_t
+        L.tg_attend.argtypes = [ctypes.POINTER(AttendArgs), _vp]
+        L.tg_attend.restype = ctypes.c_int
         L.tg_strerror.argtypes = [ctypes.c_int]
         L.tg_strerror.restype = ctypes.c_char_p
         L.tg_abi_version.argtypes = []
@@ -694,3 +741,272 @@ def mask_rois(mask, bufs: MaskRoisBuffers, min_area: int = 1, stream=None) -> No
     rc = lib().tg_mask_rois(ctypes.byref(a), _stream_handle(stream))
     if rc != OK:
         raise TgError("tg_mask_rois", rc)
+
+
+# ---- token operators: a transformer over stitched canvases --------------------------
+
+def _type_of(dtype) -> int:
+    import torch
+
+    if dtype == torch.float16:
+        return F16
+    if dtype == torch.bfloat16:
+        return BF16
+    raise ValueError(f"float16 or bfloat16, got {dtype}")
+
+
+def _values(t, dtype, dims, name, shape=None):
+    """Checks a tensor of values: on the device, of `dtype`, last dimension contiguous."""
+    import torch
+
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise ValueError(f"{name} must be a device tensor")
+    if t.dtype != dtype:
+        raise ValueError(f"{name} must be {dtype}, got {t.dtype}")
+    if t.dim() != dims or (t.numel() > 0 and t.shape[-1] > 1 and t.stride(-1) != 1):
+        raise ValueError(f"{name} must have {dims} dimensions, the last one contiguous")
+    if shape is not None and tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
+
+
+class Adapters:
+    """Low-rank adapters on the device: a [n, rank, k], b [n, outputs, rank], scale [n]."""
+
+    def __init__(self, a, b, scale):
+        import torch
+
+        _check(a, a.dtype, None, "a")
+        if a.dim() != 3:
+            raise ValueError("a must be [adapters, rank, k]")
+        _type_of(a.dtype)
+        self.n, self.rank, self.k = a.shape
+        if b.dim() != 3 or b.shape[0] != self.n or b.shape[2] != self.rank:
+            raise ValueError("b must be [adapters, outputs, rank]")
+        _check(b, a.dtype, None, "b")
+        _check(scale, torch.float32, (self.n,), "scale")
+        self.a, self.b, self.scale = a, b, scale
+        self.outputs = b.shape[1]
+
+
+class ProjectBuffers:
+    """Caller-owned result and scratch of tg_project for n_tokens tokens."""
+
+    def __init__(self, n_tokens: int, k: int, n: int, dtype, adapters: Adapters | None = None,
+                 device="cuda"):
+        import torch
+
+        self.n_tokens = n_tokens
+        self.y = torch.empty((n_tokens, n), dtype=dtype, device=device)
+        ws = 0
+        if adapters is not None:
+            ws = int(lib().tg_project_workspace_bytes(n_tokens, k, n, adapters.n, adapters.rank))
+        self.workspace = torch.empty(max(ws, 16), dtype=torch.uint8, device=device)
+        self.workspace_bytes = ws
+
+
+def project_args(x, w, bufs: ProjectBuffers, adapters: Adapters | None = None,
+                 token_adapter=None) -> ProjectArgs:
+    """x [tokens, k], w [outputs, k], rows of any stride; token_adapter: device int32
+    [tokens], outside [0, adapters.n) a token has none."""
+    import torch
+
+    dt = x.dtype
+    type_ = _type_of(dt)
+    _values(x, dt, 2, "x")
+    n_tokens, k = x.shape
+    _values(w, dt, 2, "w")
+    n = w.shape[0]
+    if w.shape[1] != k:
+        raise ValueError(f"w must have {k} columns")
+    _values(bufs.y, dt, 2, "y", (n_tokens, n))
+    if (adapters is None) != (token_adapter is None):
+        raise ValueError("adapters and token_adapter: both or neither")
+    a = ProjectArgs()
+    a.x, a.x_stride = x.data_ptr(), x.stride(0) if n_tokens > 1 else k
+    a.w, a.w_stride = w.data_ptr(), w.stride(0) if n > 1 else k
+    a.y, a.y_stride = bufs.y.data_ptr(), bufs.y.stride(0) if n_tokens > 1 else n
+    a.n_tokens, a.k, a.n, a.type = n_tokens, k, n, type_
+    if adapters is not None:
+        _check(token_adapter, torch.int32, (n_tokens,), "token_adapter")
+        if adapters.a.dtype != dt or adapters.k != k or adapters.outputs != n:
+            raise ValueError("the adapters' type or sizes differ from the projection's")
+        a.adapter, a.a, a.b = (token_adapter.data_ptr(), adapters.a.data_ptr(),
+                               adapters.b.data_ptr())
+        a.scale, a.n_adapters, a.rank = adapters.scale.data_ptr(), adapters.n, adapters.rank
+        a.workspace, a.workspace_bytes = bufs.workspace.data_ptr(), bufs.workspace_bytes
+    a._keep = (x, w, bufs, adapters, token_adapter)  # the struct holds raw pointers: keep their owners alive
+    return a
+
+
+def project_raw(args: ProjectArgs, stream=None) -> int:
+    return int(lib().tg_project(ctypes.byref(args), _stream_handle(stream)))
+
+
+def project(x, w, bufs: ProjectBuffers, adapters: Adapters | None = None, token_adapter=None,
+            stream=None) -> None:
+    """Enqueue tg_project: x w^T plus each token's adapter, into bufs.y."""
+    rc = project_raw(project_args(x, w, bufs, adapters, token_adapter), stream)
+    if rc != OK:
+        raise TgError("tg_project", rc)
+
+
+def rotate_args(q, k, q_weight, k_weight, table, pos, q_out, k_out, v=None, v_out=None, slot=None,
+                eps: float = 1e-6, interleaved: bool = False) -> RotateArgs:
+    """q [tokens, heads, d], k and v [tokens, kv heads, d], any strides; weights [d] or None;
+    table float32 [positions, rot / 2, 2] of cosines and sines; pos int32 [tokens, axes];
+    slot: int64 [tokens], rows of k_out and v_out."""
+    import torch
+
+    dt = q.dtype
+    type_ = _type_of(dt)
+    _values(q, dt, 3, "q")
+    n_tokens, n_heads, d = q.shape
+    _values(k, dt, 3, "k")
+    n_kv = k.shape[1]
+    if k.shape[0] != n_tokens or k.shape[2] != d:
+        raise ValueError(f"k must have shape ({n_tokens}, kv heads, {d})")
+    _values(q_out, dt, 3, "q_out", q.shape)
+    _values(k_out, dt, 3, "k_out", None if slot is not None else k.shape)
+    if tuple(k_out.shape[1:]) != (n_kv, d):
+        raise ValueError("k_out must have the heads of k")
+    if (v is None) != (v_out is None):
+        raise ValueError("v and v_out: both or neither")
+    if v is not None:
+        _values(v, dt, 3, "v", k.shape)
+        _values(v_out, dt, 3, "v_out", k_out.shape)
+    for w, name in ((q_weight, "q_weight"), (k_weight, "k_weight")):
+        if w is not None:
+            _check(w, dt, (d,), name)
+    _check(table, torch.float32, None, "table")
+    if table.dim() != 3 or table.shape[2] != 2:
+        raise ValueError("table must be [positions, rot / 2, 2]")
+    _check(pos, torch.int32, None, "pos")
+    if pos.dim() != 2 or pos.shape[0] != n_tokens:
+        raise ValueError("pos must be [tokens, axes]")
+    a = RotateArgs()
+    a.q, a.q_stride, a.q_head_stride = q.data_ptr(), q.stride(0), q.stride(1)
+    a.k, a.k_stride, a.k_head_stride = k.data_ptr(), k.stride(0), k.stride(1)
+    a.q_out, a.q_out_stride, a.q_out_head_stride = (q_out.data_ptr(), q_out.stride(0),
+                                                    q_out.stride(1))
+    a.k_out, a.k_out_stride, a.k_out_head_stride = (k_out.data_ptr(), k_out.stride(0),
+                                                    k_out.stride(1))
+    if v is not None:
+        a.v, a.v_stride, a.v_head_stride = v.data_ptr(), v.stride(0), v.stride(1)
+        a.v_out, a.v_out_stride, a.v_out_head_stride = (v_out.data_ptr(), v_out.stride(0),
+                                                        v_out.stride(1))
+    a.q_weight = q_weight.data_ptr() if q_weight is not None else None
+    a.k_weight = k_weight.data_ptr() if k_weight is not None else None
+    a.table, a.pos = table.data_ptr(), pos.data_ptr()
+    if slot is not None:
+        _check(slot, torch.int64, (n_tokens,), "slot")
+        a.slot, a.n_rows = slot.data_ptr(), k_out.shape[0]
+    a.eps, a.n_tokens, a.n_heads, a.n_kv_heads, a.d = float(eps), n_tokens, n_heads, n_kv, d
+    a.rot, a.axes, a.interleaved = 2 * table.shape[1], pos.shape[1], int(bool(interleaved))
+    a.n_positions, a.type = table.shape[0], type_
+    a._keep = (q, k, v, q_weight, k_weight, table, pos, q_out, k_out, v_out, slot)  # the struct holds raw pointers: keep their owners alive
+    return a
+
+
+def rotate_raw(args: RotateArgs, stream=None) -> int:
+    return int(lib().tg_rotate(ctypes.byref(args), _stream_handle(stream)))
+
+
+def rotate(q, k, q_weight, k_weight, table, pos, q_out, k_out, v=None, v_out=None, slot=None,
+           eps: float = 1e-6, interleaved: bool = False, stream=None) -> None:
+    """Enqueue tg_rotate: norm and rotation of q and k (and a copy of v) into the outputs."""
+    rc = rotate_raw(rotate_args(q, k, q_weight, k_weight, table, pos, q_out, k_out, v, v_out, slot,
+                                eps, interleaved), stream)
+    if rc != OK:
+        raise TgError("tg_rotate", rc)
+
+
+class Sequences:
+    """A ragged batch on the device: queries of sequence s are rows q_begin[s] ..
+    q_begin[s + 1], its keys kv_len[s] rows from kv_begin[s] on; max_q and max_kv bound the
+    lengths. prefix: int32 [n] or None."""
+
+    def __init__(self, q_begin, kv_begin, kv_len, max_q: int, max_kv: int, prefix=None):
+        import torch
+
+        self.n = int(kv_len.shape[0])
+        _check(q_begin, torch.int32, (self.n + 1,), "q_begin")
+        _check(kv_begin, torch.int64, (self.n,), "kv_begin")
+        _check(kv_len, torch.int32, (self.n,), "kv_len")
+        if prefix is not None:
+            _check(prefix, torch.int32, (self.n,), "prefix")
+        self.q_begin, self.kv_begin, self.kv_len, self.prefix = q_begin, kv_begin, kv_len, prefix
+        self.max_q, self.max_kv = int(max_q), int(max_kv)
+
+
+class AttendBuffers:
+    """Caller-owned scratch of tg_attend for queries like q [rows, heads, d] and keys like k
+    [rows, kv heads, d]."""
+
+    def __init__(self, seqs: Sequences, q, k, device="cuda"):
+        import torch
+
+        ws = int(lib().tg_attend_workspace_bytes(seqs.n, q.shape[0], seqs.max_q, seqs.max_kv,
+                                                 q.shape[1], k.shape[1], q.shape[2]))
+        self.workspace = torch.empty(max(ws, 16), dtype=torch.uint8, device=device)
+        self.workspace_bytes = ws
+
+
+def attend_args(q, k, v, seqs: Sequences, out, bufs: AttendBuffers, scale: float,
+                cap: float = 0.0, causal: bool = False, q_doc=None, k_doc=None, q_pos=None,
+                k_pos=None, slope=None) -> AttendArgs:
+    """q and out [rows, heads, d], k and v [key rows, kv heads, d], any strides; q_doc and
+    k_doc int32 per row, q_pos and k_pos int32 [rows, 2], slope float32 [heads]."""
+    import torch
+
+    dt = q.dtype
+    type_ = _type_of(dt)
+    _values(q, dt, 3, "q")
+    n_q, n_heads, d = q.shape
+    _values(k, dt, 3, "k")
+    n_k, n_kv, _ = k.shape
+    if k.shape[2] != d:
+        raise ValueError(f"k must have heads of {d}")
+    _values(v, dt, 3, "v", k.shape)
+    _values(out, dt, 3, "out", q.shape)
+    if (q_doc is None) != (k_doc is None) or (q_pos is None) != (k_pos is None):
+        raise ValueError("documents and positions: of queries and keys, or of neither")
+    a = AttendArgs()
+    a.q, a.q_stride, a.q_head_stride = q.data_ptr(), q.stride(0), q.stride(1)
+    a.k, a.k_stride, a.k_head_stride = k.data_ptr(), k.stride(0), k.stride(1)
+    a.v, a.v_stride, a.v_head_stride = v.data_ptr(), v.stride(0), v.stride(1)
+    a.out, a.out_stride, a.out_head_stride = out.data_ptr(), out.stride(0), out.stride(1)
+    a.q_begin, a.kv_begin, a.kv_len = (seqs.q_begin.data_ptr(), seqs.kv_begin.data_ptr(),
+                                       seqs.kv_len.data_ptr())
+    a.prefix = seqs.prefix.data_ptr() if seqs.prefix is not None else None
+    if q_doc is not None:
+        _check(q_doc, torch.int32, (n_q,), "q_doc")
+        _check(k_doc, torch.int32, (n_k,), "k_doc")
+        a.q_doc, a.k_doc = q_doc.data_ptr(), k_doc.data_ptr()
+    if q_pos is not None:
+        _check(q_pos, torch.int32, (n_q, 2), "q_pos")
+        _check(k_pos, torch.int32, (n_k, 2), "k_pos")
+        a.q_pos, a.k_pos = q_pos.data_ptr(), k_pos.data_ptr()
+    if slope is not None:
+        _check(slope, torch.float32, (n_heads,), "slope")
+        a.slope = slope.data_ptr()
+    a.scale, a.cap, a.causal = float(scale), float(cap), int(bool(causal))
+    a.n_seqs, a.n_q_rows, a.n_k_rows = seqs.n, n_q, n_k
+    a.max_q_len, a.max_kv_len = seqs.max_q, seqs.max_kv
+    a.n_heads, a.n_kv_heads, a.d, a.type = n_heads, n_kv, d, type_
+    a.workspace, a.workspace_bytes = bufs.workspace.data_ptr(), bufs.workspace_bytes
+    a._keep = (q, k, v, seqs, out, bufs, q_doc, k_doc, q_pos, k_pos, slope)  # the struct holds raw pointers: keep their owners alive
+    return a
+
+
+def attend_raw(args: AttendArgs, stream=None) -> int:
+    return int(lib().tg_attend(ctypes.byref(args), _stream_handle(stream)))
+
+
+def attend(q, k, v, seqs: Sequences, out, bufs: AttendBuffers, scale: float, cap: float = 0.0,
+           causal: bool = False, q_doc=None, k_doc=None, q_pos=None, k_pos=None, slope=None,
+           stream=None) -> None:
+    """Enqueue tg_attend: attention of q over k and v, into out."""
+    rc = attend_raw(attend_args(q, k, v, seqs, out, bufs, scale, cap, causal, q_doc, k_doc, q_pos,
+                                k_pos, slope), stream)
+    if rc != OK:
+        raise TgError("tg_attend", rc)
