@@ -86,6 +86,17 @@ __device__ __forceinline__ void wait_loads() {
   __builtin_amdgcn_s_waitcnt((left & 15) | ((left >> 4) << 14) | 0x0F70);
 }
 
+// The same, and for the wave's LDS accesses; then the workgroup's barrier. Nothing moves across.
+template <int left>
+__device__ __forceinline__ void wait_and_meet() {
+  __builtin_amdgcn_sched_barrier(0);
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt((left & 15) | ((left >> 4) << 14) | 0x0070);
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_sched_barrier(0);
+}
+
 __device__ __forceinline__ float wave_max(float v) {
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o));
