@@ -581,11 +581,12 @@ typedef struct {
   int32_t n_tokens, k, n, n_adapters, rank;
   int32_t type;           /* enum tg_type of x, w, a, b and y */
   void *workspace;        /* device scratch, 16-byte aligned, >=
-                             tg_project_workspace_bytes(...); unused without adapters */
+                             tg_project_workspace_bytes(...) */
   size_t workspace_bytes;
 } tg_project_args;
 
-/* Device scratch tg_project needs (0 when n_tokens, k, n, n_adapters or rank is <= 0). */
+/* Device scratch tg_project needs (0 when it needs none, or for bad arguments); n_adapters and
+ * rank 0 when no token has an adapter. */
 size_t tg_project_workspace_bytes(int32_t n_tokens, int32_t k, int32_t n, int32_t n_adapters,
                                   int32_t rank);
 
@@ -596,8 +597,9 @@ size_t tg_project_workspace_bytes(int32_t n_tokens, int32_t k, int32_t n, int32_
  *   h[t][r] = sum_i x[t][i] a[g][r][i],
  * the second term only for tokens that have an adapter; an adapter's values reach no token
  * but its own, whatever they are (infinities and NaN included). Tokens may come in any order
- * of adapters; runs of one adapter are the fastest. y must not overlap an input. h is kept to
- * 16 bits or more (two values of the type each); everything else is summed in binary32.
+ * of adapters; runs of one adapter are the fastest. y must not overlap an input. h is kept as
+ * two values of the type each, the rounded one and what that left, or in binary32; everything
+ * else is summed in binary32.
  * Enqueued on `stream`; the library allocates nothing. Returns TG_E_INVAL (null pointer,
  * negative count, k < 1 or not a multiple of 8, n < 1, rank outside [1, TG_PROJECT_MAX_RANK]
  * with adapters, a bad type or stride, x, w or a not 16-byte aligned or with a stride that is

@@ -1,16 +1,23 @@
 // tg_project: a shared projection and the low-rank adapters of many cameras, y = x w^T + the
 // adapter's scale_g (x a_g^T) b_g^T (low-rank adaptation, Hu et al. 2021, one adapter a token).
 //
-// Two launches:
-//  1. shrink: h[t] = scale_g x[t] a_g^T for the tokens that have an adapter. Kept as two values
-//     of the type whose sum is h (the first rounded, the second what that rounding left): 22
-//     bits of binary16, 16 of bfloat16. A binary16 row whose largest value is far from 1 is
-//     divided by a power of two first, which is kept with it.
-//  2. the product: tiles of x and w go through LDS to the matrix instructions; each tile then
-//     adds b_g h[t] for its tokens, adapter by adapter, as a few more matrix instructions in
-//     which h is 0 for the tokens of other adapters.
-// Results lie transposed in the registers (a lane holds 4 outputs of one token), so that a
-// token's adapter and power of two belong to the lane, and stores are contiguous.
+// Two launches. With many tokens:
+//  1. shrink: h[t] = scale_g x[t] a_g^T for the tokens that have an adapter, in binary32, and as
+//     two values of the type whose sum is h (the first rounded, the second what that rounding
+//     left): 22 bits of binary16, 16 of bfloat16.
+//  2. the product: tiles of x and w go through LDS to the matrix instructions. An adapter of the
+//     tile's tokens is some more steps of the same loop, with the two values of h in the place of
+//     x, 0 for tokens of other adapters, and b_g in the place of w: the joint takes no work of
+//     its own, and no further registers.
+// With few tokens, where launches and loads are what takes the time:
+//  1. tiles of x and w with k cut over workgroups, so that every CU has a share of w to read,
+//     and beside them one workgroup a token for its row of h;
+//  2. finish: the cuts are added up, and each token's adapter to them.
+// 0 times an infinite b_g, or a row of h past binary16's range, would leave NaN at tokens it does
+// not belong to, or in the place of a number. Sums that are not finite at the end of a tile with
+// adapters are therefore formed again one by one, from binary32 h and the token's own adapter.
+// Results lie transposed in the registers (a lane holds 4 outputs of one token), so that stores
+// are contiguous and a token's adapter belongs to the lane.
 #include <hip/hip_runtime.h>
 
 #include <climits>
@@ -33,8 +40,12 @@ struct ProjectParams {
   int64_t x_stride, w_stride, y_stride;
   int32_t n_tokens, k, n, n_adapters, rank;
   int32_t pad_rank;  // 16, 32 or 64
+  int32_t b_step;    // values of b that one load can take: 8, 2 or 1
   void *h;           // [n_tokens][2][pad_rank] of the type
-  float *power;      // [n_tokens]
+  float *h32;        // [n_tokens][pad_rank]
+  int32_t gather;    // adapters are added by add_gathered
+  float *part;       // [splits][n_tokens][part_stride]: sums over a cut of k
+  int32_t part_stride, splits, low_blocks;
   int32_t tiles_t, tiles_n;
   int32_t vec_y;     // 4 outputs of a token can be stored at once
 };
@@ -55,26 +66,14 @@ constexpr int kShrinkWaves = kShrinkThreads / 64;
 template <int kType, int kFrags>
 __device__ __forceinline__ void keep_h(const ProjectParams &P, int t, float (&v)[kFrags], int r0) {
   typedef typename Num<kType>::E E;
-  int e = 0;
-  if (kType == TG_F16) {  // bfloat16 has the range of the sums
-    float big = 0.0f;
-#pragma unroll
-    for (int f = 0; f < kFrags; ++f) big = fmaxf(big, fabsf(v[f]));
-#pragma unroll
-    for (int o = 8; o > 0; o >>= 1) big = fmaxf(big, __shfl_xor(big, o, 16));
-    // in between, the second value's last bit is 2^-19 of the largest or less
-    if ((big >= 32768.0f || big < 0.015625f) && big > 0.0f && big < INFINITY) frexpf(big, &e);
-    e = min(max(e, -126), 127);  // the power itself stays a normal number
-  }
-  if (r0 == 0) P.power[t] = ldexpf(1.0f, e);
   E *h = static_cast<E *>(P.h) + int64_t(t) * 2 * P.pad_rank;
+  float *h32 = P.h32 + int64_t(t) * P.pad_rank;
 #pragma unroll
   for (int f = 0; f < kFrags; ++f) {
-    const float s = ldexpf(v[f], -e);
-    const E hi = static_cast<E>(s);
-    const float rest = s - static_cast<float>(hi);
+    const E hi = static_cast<E>(v[f]);
+    h32[f * 16 + r0] = v[f];
     h[f * 16 + r0] = hi;
-    h[P.pad_rank + f * 16 + r0] = static_cast<E>(fabsf(s) < INFINITY ? rest : 0.0f);
+    h[P.pad_rank + f * 16 + r0] = static_cast<E>(v[f] - static_cast<float>(hi));
   }
 }
 
@@ -182,60 +181,54 @@ __global__ __launch_bounds__(kShrinkThreads) void shrink_kernel(const ProjectPar
   }
 }
 
-// Few tokens: a workgroup a token, whose row of x and rows of a are read as they lie.
-template <int kType, int kFrags>
-__global__ __launch_bounds__(kShrinkThreads) void shrink_few_kernel(const ProjectParams P) {
+// One token's row of h, by a workgroup of kWaves: rows of x and a are read as they lie, 4 ranks a
+// wave at a time.
+template <int kType, int kWaves>
+__device__ __forceinline__ void shrink_token(const ProjectParams &P, int t) {
   typedef typename Num<kType>::E E;
   typedef typename Num<kType>::V8 V8;
-  constexpr int kEach = kFrags * 16 / kShrinkWaves;  // ranks of a wave
-  __shared__ float part[kFrags * 16];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int t = blockIdx.x;
   const int g = adapter_of(P, t);
-  if (g < 0) return;
+  if (g < 0) return;  // nothing reads h of a token without an adapter
   const E *x = static_cast<const E *>(P.x) + t * P.x_stride;
   const E *a = static_cast<const E *>(P.a) + int64_t(g) * P.rank * P.k;
-  float sum[kEach] = {};
-  for (int k = lane * 8; k < P.k; k += 1024) {
+  const float scale = P.scale[g];
+  for (int r0 = wave * 4; r0 < P.pad_rank; r0 += kWaves * 4) {
+    float sum[4] = {};
+    for (int k = lane * 8; k < P.k; k += 1024) {
+      V8 xv[2] = {}, av[2][4] = {};
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      if (k + u * 512 >= P.k) continue;
-      const V8 xv = *reinterpret_cast<const V8 *>(x + k + u * 512);
+      for (int u = 0; u < 2; ++u)
+        if (k + u * 512 < P.k) {
+          xv[u] = *reinterpret_cast<const V8 *>(x + k + u * 512);
 #pragma unroll
-      for (int e = 0; e < kEach; ++e) {
-        const int r = min(e * kShrinkWaves + wave, P.rank - 1);
-        const V8 av = *reinterpret_cast<const V8 *>(a + int64_t(r) * P.k + k + u * 512);
+          for (int r = 0; r < 4; ++r)
+            av[u][r] = *reinterpret_cast<const V8 *>(a + int64_t(min(r0 + r, P.rank - 1)) * P.k +
+                                                     k + u * 512);
+        }
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-          sum[e] = __builtin_fmaf(static_cast<float>(av[i]), static_cast<float>(xv[i]), sum[e]);
-      }
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            sum[r] = __builtin_fmaf(static_cast<float>(av[u][r][i]), static_cast<float>(xv[u][i]),
+                                    sum[r]);
+    }
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      sum[r] = wave_sum(sum[r]);
+      if (lane == 0)
+        P.h32[int64_t(t) * P.pad_rank + r0 + r] = r0 + r < P.rank ? sum[r] * scale : 0.0f;
     }
   }
-#pragma unroll
-  for (int e = 0; e < kEach; ++e) {
-    sum[e] = wave_sum(sum[e]);
-    if (lane == 0) part[e * kShrinkWaves + wave] = sum[e];
-  }
-  __syncthreads();
-  if (threadIdx.x >= 16) return;
-  const float scale = P.scale[g];
-  float v[kFrags];
-#pragma unroll
-  for (int f = 0; f < kFrags; ++f) {
-    const int r = f * 16 + threadIdx.x;
-    v[f] = r < P.rank ? part[r] * scale : 0.0f;
-  }
-  keep_h<kType, kFrags>(P, t, v, threadIdx.x);
 }
 
 template <int kType, int kFrags>
 void launch_shrink_rank(const ProjectParams &P, hipStream_t s) {
   const int most = P.n_adapters < 16 ? P.n_adapters : 16;
-  if (P.n_tokens <= 64)
-    hipLaunchKernelGGL((shrink_few_kernel<kType, kFrags>), dim3(P.n_tokens), dim3(kShrinkThreads),
-                       0, s, P);
-  else if (P.n_tokens < 8192)
+  if (P.n_tokens < 8192)
     hipLaunchKernelGGL((shrink_kernel<kType, kFrags, 1>),
                        dim3((P.n_tokens + 15) / 16, P.n_tokens < 1024 ? most : (most + 3) / 4),
                        dim3(kShrinkThreads), 0, s, P);
@@ -261,12 +254,21 @@ template <int kType>
 __device__ __forceinline__ typename Num<kType>::V8 b_chunk(const ProjectParams &P, int g, int j,
                                                             int r) {
   typedef typename Num<kType>::E E;
+  typedef typename Num<kType>::V2 V2;
   typedef typename Num<kType>::V8 V8;
   V8 v = {};
   if (j >= P.n || r >= P.rank) return v;
   const E *b = static_cast<const E *>(P.b) + (int64_t(g) * P.n + j) * P.rank + r;
-  if (P.rank % 8 == 0 && (reinterpret_cast<uintptr_t>(P.b) & 15) == 0) {
+  if (P.b_step == 8) {
     v = *reinterpret_cast<const V8 *>(b);
+  } else if (P.b_step == 2) {
+#pragma unroll
+    for (int i = 0; i < 8; i += 2)
+      if (r + i < P.rank) {
+        const V2 two = *reinterpret_cast<const V2 *>(b + i);
+        v[i] = two[0];
+        v[i + 1] = two[1];
+      }
   } else {
 #pragma unroll
     for (int i = 0; i < 8; ++i)
@@ -275,105 +277,119 @@ __device__ __forceinline__ typename Num<kType>::V8 b_chunk(const ProjectParams &
   return v;
 }
 
-// Whether one of 8 values is an infinity or NaN.
-template <int kType>
-__device__ __forceinline__ bool wild(typename Num<kType>::V8 v) {
-  const i32x4 d = __builtin_bit_cast(i32x4, v);
-  const uint32_t mask = kType == TG_F16 ? 0x7C007C00u : 0x7F807F80u;
-  const uint32_t one = kType == TG_F16 ? 0x04000400u : 0x00800080u;  // an exponent's last bit
-  uint32_t any = 0;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) any |= (static_cast<uint32_t>(d[i]) & mask) + one;
-  return any & 0x80008000u;
-}
-
 // Adds b_g h[t] to a wave's results: acc[j][i] holds outputs n0 + 16 j + 4 (lane / 16) .. of
-// token t0 + 16 i + lane % 16. Tokens of other adapters have h = 0 in the product, which adds
-// nothing as long as b_g is finite; otherwise, and where h carries a power of two, the product
-// is formed by itself and taken by the adapter's own tokens.
+// token t0 + 16 i + lane % 16. Each lane takes its own token's adapter: the time does not hang on
+// how many there are, and all loads are independent.
 template <int kType, int kFn, int kFt>
-__device__ __forceinline__ void add_adapters(const ProjectParams &P, int t0, int n0,
+__device__ __forceinline__ void add_gathered(const ProjectParams &P, int t0, int n0,
                                              f32x4 (&acc)[kFn][kFt]) {
-  typedef Num<kType> N;
-  typedef typename N::E E;
-  typedef typename N::V8 V8;
+  typedef typename Num<kType>::V8 V8;
   const int lane = threadIdx.x & 63, col = lane & 15, quad = lane >> 4;
-  int mine[kFt];
-  float power[kFt];
-  uint64_t left[kFt];
-  bool plain = true;
-#pragma unroll
-  for (int i = 0; i < kFt; ++i) mine[i] = adapter_of(P, t0 + 16 * i + col);
 #pragma unroll
   for (int i = 0; i < kFt; ++i) {
-    left[i] = __ballot(mine[i] >= 0) & 0xFFFF;
-    power[i] = 1.0f;
-    if (kType == TG_F16 && mine[i] >= 0) power[i] = P.power[t0 + 16 * i + col];
-    plain = plain && power[i] == 1.0f;
-  }
-  if (kType == TG_F16) plain = __ballot(!plain) == 0;
-  const E *h = static_cast<const E *>(P.h) + int64_t(t0 + col) * 2 * P.pad_rank;
-  // with 16 ranks one step of 32 holds both values of h, otherwise a step holds one of them
-  const int narrow = P.pad_rank == 16;
-  for (;;) {
-    int g = -1;
+    const int t = t0 + 16 * i + col;
+    const int g = adapter_of(P, t);
+    if (g < 0) continue;
+    const f32x4 *h = reinterpret_cast<const f32x4 *>(P.h32 + int64_t(t) * P.pad_rank);
+    for (int r0 = 0; r0 < P.rank; r0 += 16) {
 #pragma unroll
-    for (int i = kFt - 1; i >= 0; --i)
-      if (left[i]) g = __builtin_amdgcn_readlane(mine[i], __builtin_ctzll(left[i]));
-    if (g < 0) break;
-    uint64_t has[kFt];
+      for (int r = r0; r < r0 + 16; r += 8) {
+        const f32x4 h0 = h[r / 4], h1 = h[r / 4 + 1];
 #pragma unroll
-    for (int i = 0; i < kFt; ++i) {
-      has[i] = __ballot(mine[i] == g) & 0xFFFF;
-      left[i] &= ~has[i];
-    }
-    for (int r0 = 0; r0 < P.pad_rank; r0 += 32) {
-      const int r = r0 + (narrow ? (quad & 1) * 8 : quad * 8);
-      V8 bf[kFn];
-      bool odd = false;
+        for (int j = 0; j < kFn; ++j)
 #pragma unroll
-      for (int j = 0; j < kFn; ++j) bf[j] = b_chunk<kType>(P, g, n0 + 16 * j + col, r);
+          for (int q = 0; q < 4; ++q) {
+            const V8 b = b_chunk<kType>(P, g, n0 + 16 * j + 4 * quad + q, r);
 #pragma unroll
-      for (int j = 0; j < kFn; ++j) odd = odd || wild<kType>(bf[j]);
-      const bool direct = plain && __ballot(odd) == 0;
-      constexpr int kAt = kFt < 4 ? kFt : 4;  // token blocks whose h is loaded at once
-#pragma unroll
-      for (int i0 = 0; i0 < kFt; i0 += kAt) {
-        V8 hv[kAt][2];
-#pragma unroll
-        for (int i = 0; i < kAt; ++i) {
-          hv[i][0] = hv[i][1] = V8{};
-          if (mine[i0 + i] == g) {
-            const E *from = h + int64_t(16 * (i0 + i)) * 2 * P.pad_rank;
-            hv[i][0] = *reinterpret_cast<const V8 *>(from + (narrow ? quad * 8 : r));
-            if (!narrow) hv[i][1] = *reinterpret_cast<const V8 *>(from + P.pad_rank + r);
+            for (int e = 0; e < 8; ++e)
+              acc[j][i][q] = __builtin_fmaf(static_cast<float>(b[e]), e < 4 ? h0[e & 3] : h1[e & 3],
+                                            acc[j][i][q]);
           }
-        }
-#pragma unroll
-        for (int i = 0; i < kAt; ++i) {
-          if (!has[i0 + i]) continue;
-          if (direct) {
-#pragma unroll
-            for (int j = 0; j < kFn; ++j) {
-              acc[j][i0 + i] = N::mfma16(bf[j], hv[i][0], acc[j][i0 + i]);
-              if (!narrow) acc[j][i0 + i] = N::mfma16(bf[j], hv[i][1], acc[j][i0 + i]);
-            }
-          } else {
-#pragma unroll
-            for (int j = 0; j < kFn; ++j) {
-              f32x4 low = {};
-              low = N::mfma16(bf[j], hv[i][0], low);
-              if (!narrow) low = N::mfma16(bf[j], hv[i][1], low);
-              if (mine[i0 + i] == g) {
-#pragma unroll
-                for (int q = 0; q < 4; ++q) acc[j][i0 + i][q] += power[i0 + i] * low[q];
-              }
-            }
-          }
-        }
       }
     }
   }
+}
+
+// One result from the formula.
+template <int kType>
+__device__ __attribute__((noinline)) float strict_value(const void *x, const void *w, int k,
+                                                        const float *h, const void *b, int rank) {
+  typedef typename Num<kType>::E E;
+  float sum = 0.0f;
+  for (int i = 0; i < k; ++i)
+    sum = __builtin_fmaf(static_cast<float>(static_cast<const E *>(x)[i]),
+                         static_cast<float>(static_cast<const E *>(w)[i]), sum);
+  for (int r = 0; r < rank; ++r)
+    sum = __builtin_fmaf(h[r], static_cast<float>(static_cast<const E *>(b)[r]), sum);
+  return sum;
+}
+
+// Forms those of a wave's results again that are not finite (they have been stored).
+template <int kType, int kFn, int kFt>
+__device__ __forceinline__ void mend(const ProjectParams &P, int t0, int n0,
+                                     const f32x4 (&acc)[kFn][kFt]) {
+  typedef typename Num<kType>::E E;
+  const int lane = threadIdx.x & 63, col = lane & 15, quad = lane >> 4;
+  bool fine = true;
+  uint32_t bad[(kFn * kFt * 4 + 31) / 32] = {};
+#pragma unroll
+  for (int j = 0; j < kFn; ++j)
+#pragma unroll
+    for (int i = 0; i < kFt; ++i)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) fine = fine && fabsf(acc[j][i][q]) < INFINITY;
+  if (__ballot(!fine) == 0) return;
+#pragma unroll
+  for (int j = 0; j < kFn; ++j)
+#pragma unroll
+    for (int i = 0; i < kFt; ++i)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int at = (j * kFt + i) * 4 + q;
+        bad[at / 32] |= fabsf(acc[j][i][q]) < INFINITY ? 0u : 1u << (at % 32);
+      }
+#pragma unroll
+  for (int word = 0; word < (kFn * kFt * 4 + 31) / 32; ++word)
+    for (uint32_t left = bad[word]; left; left &= left - 1) {
+      const int at = word * 32 + __builtin_ctz(left);
+      const int t = t0 + 16 * (at / 4 % kFt) + col;
+      const int n = n0 + 16 * (at / 4 / kFt) + 4 * quad + at % 4;
+      if (t >= P.n_tokens || n >= P.n) continue;
+      const int g = adapter_of(P, t);
+      const float v = strict_value<kType>(
+          static_cast<const E *>(P.x) + t * P.x_stride, static_cast<const E *>(P.w) + n * P.w_stride,
+          P.k, P.h32 + int64_t(t) * P.pad_rank,
+          static_cast<const E *>(P.b) + (int64_t(max(g, 0)) * P.n + n) * P.rank,
+          g < 0 ? 0 : P.rank);
+      static_cast<E *>(P.y)[t * P.y_stride + n] = static_cast<E>(v);
+    }
+}
+
+// The distinct adapters among ids[0 .. kT), as list; returns how many. One id a thread, the whole
+// workgroup takes part. Neighbours of one adapter are folded first.
+template <int kT, int kWaves>
+__device__ __forceinline__ int distinct(const int *ids, int *heads, int *list, int *counts) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  auto compact = [&](bool keep, int value, int *to) {
+    const uint64_t all = __ballot(keep);
+    if (lane == 0) counts[wave] = __popcll(all);
+    __syncthreads();
+    int before = 0, total = 0;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      if (w < wave) before += counts[w];
+      total += counts[w];
+    }
+    if (keep) to[before + __popcll(all & ((1ull << lane) - 1))] = value;
+    __syncthreads();
+    return total;
+  };
+  const int mine = tid < kT ? ids[tid] : -1;
+  const int n = compact(mine >= 0 && (tid == 0 || ids[tid - 1] != mine), mine, heads);
+  const int head = tid < n ? heads[tid] : -1;
+  bool first = tid < n;
+  for (int i = 0; i < n - 1; ++i) first = first && (i >= tid || heads[i] != head);
+  return __builtin_amdgcn_readfirstlane(compact(first, head, list));
 }
 
 template <int kType, int kFn, int kFt>
@@ -426,7 +442,7 @@ __device__ __forceinline__ void tile_of(int id, int tiles_t, int tiles_n, int &t
   tn = in / rows;
 }
 
-template <int kType, int kT, int kN, int kWt, int kWn, int kBK, int kStages>
+template <int kType, int kT, int kN, int kWt, int kWn, int kBK, int kStages, bool kCut>
 __global__ __launch_bounds__(kWt *kWn * 64, 2) void project_kernel(const ProjectParams P) {
   typedef Num<kType> N;
   typedef typename N::E E;
@@ -436,31 +452,53 @@ __global__ __launch_bounds__(kWt *kWn * 64, 2) void project_kernel(const Project
   constexpr int kLoads = kRows / kPer / kWaves, kSub = kBK / 32;
   static_assert(kLoads * kPer * kWaves == kRows && kT % kPer == 0, "whole loads");
   __shared__ __attribute__((aligned(16))) E tile[kStages][kRows * kBK];
+  __shared__ int s_id[kT], s_heads[kT], s_list[kT], s_counts[kWaves];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int col = lane & 15, quad = lane >> 4;
-  int tt, tn;
-  tile_of(blockIdx.x, P.tiles_t, P.tiles_n, tt, tn);
+  int tt, tn, cut = 0;
+  if constexpr (kCut) {
+    int id = blockIdx.x;
+    if (id < P.low_blocks) return shrink_token<kType, kWaves>(P, id);
+    id -= P.low_blocks;
+    cut = id % P.splits;
+    id /= P.splits;
+    tt = id % P.tiles_t;
+    tn = id / P.tiles_t;
+  } else {
+    tile_of(blockIdx.x, P.tiles_t, P.tiles_n, tt, tn);
+  }
   const int t0 = tt * kT, n0 = tn * kN;
   const int xr = min(kT, P.n_tokens - t0), wr = min(kN, P.n - n0);
   const auto xb = buffer(static_cast<const E *>(P.x) + t0 * P.x_stride,
                          static_cast<uint32_t>(((xr - 1) * P.x_stride + P.k) * 2));
   const auto wb = buffer(static_cast<const E *>(P.w) + n0 * P.w_stride,
                          static_cast<uint32_t>(((wr - 1) * P.w_stride + P.k) * 2));
-  // load i of a wave covers kPer rows; rows past the tensor repeat its last one. A lane's chunk
-  // is the same in all loads, since their rows are 4 kPer apart or more.
+  // load i of a wave covers kPer rows; rows past the tensor are not read. A lane's chunk is the
+  // same in all loads, since their rows are 4 kPer apart or more.
   static_assert(kWaves * kPer % 16 == 0, "rows of one lane");
   const int chunk = place_of<kBK>(wave * kPer + lane / kChunks, lane % kChunks);
   uint32_t at[kLoads];
 #pragma unroll
   for (int i = 0; i < kLoads; ++i) {
     const int row = (i * kWaves + wave) * kPer + lane / kChunks;
-    at[i] = row < kT ? static_cast<uint32_t>((min(row, xr - 1) * P.x_stride + chunk * 8) * 2)
-                     : static_cast<uint32_t>((min(row - kT, wr - 1) * P.w_stride + chunk * 8) * 2);
+    at[i] = row < kT ? static_cast<uint32_t>((row * P.x_stride + chunk * 8) * 2)
+                     : static_cast<uint32_t>(((row - kT) * P.w_stride + chunk * 8) * 2);
+    if (row < kT ? row >= xr : row - kT >= wr) at[i] = kNowhere;
   }
-  auto fetch = [&](int s) {  // every step's loads are issued, so that they can be counted
-    const int k0 = s * kBK;
-    const bool past = k0 + chunk * 8 >= P.k;
+  const int all_steps = (P.k + kBK - 1) / kBK;
+  int s0 = 0, main_steps = all_steps;
+  if constexpr (kCut) {
+    const int each = (all_steps + P.splits - 1) / P.splits;
+    s0 = cut * each;
+    main_steps = min(each, all_steps - s0);  // the host leaves no cut empty
+  }
+  const int k_end = min(P.k, (s0 + main_steps) * kBK);
+  int steps = main_steps;  // and then the adapters' steps
+  // every step's loads are issued, past the last one too, so that they can be counted
+  auto fetch = [&](int s) {
+    const int k0 = (s0 + s) * kBK;
+    const bool past = k0 + chunk * 8 >= k_end;
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
       const int first = (i * kWaves + wave) * kPer;
@@ -468,9 +506,30 @@ __global__ __launch_bounds__(kWt *kWn * 64, 2) void project_kernel(const Project
                static_cast<uint32_t>(k0) * 2);
     }
   };
+  const int per = (2 * P.pad_rank + kBK - 1) / kBK;  // steps of an adapter
+  auto fetch_low = [&](int s) {
+    const int a = (s - main_steps) / per, part = (s - main_steps) - a * per;
+    const int g = s < steps ? __builtin_amdgcn_readfirstlane(s_list[a]) : 0;
+    const int e = part * kBK + chunk * 8, r = e & (P.pad_rank - 1);
+    const auto hb = buffer(static_cast<const E *>(P.h) + int64_t(t0) * 2 * P.pad_rank,
+                           static_cast<uint32_t>(xr) * 4 * P.pad_rank);
+    const auto bb = buffer(static_cast<const E *>(P.b) + int64_t(g) * P.n * P.rank,
+                           static_cast<uint32_t>(P.n) * P.rank * 2);
+    const bool in = s < steps && e < 2 * P.pad_rank;
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const int first = (i * kWaves + wave) * kPer, row = first + lane / kChunks;
+      uint32_t off = kNowhere;
+      if (first < kT) {
+        if (in && s_id[row] == g) off = static_cast<uint32_t>((row * 2 * P.pad_rank + e) * 2);
+      } else if (in && r < P.rank && n0 + row - kT < P.n) {
+        off = (static_cast<uint32_t>(n0 + row - kT) * P.rank + r) * 2;
+      }
+      load_lds(first < kT ? hb : bb, &tile[s % kStages][first * kBK], off, 0);
+    }
+  };
   f32x4 acc[kFn][kFt] = {};
   const int wt = (wave % kWt) * (kT / kWt), wn = (wave / kWt) * (kN / kWn);
-  const int steps = (P.k + kBK - 1) / kBK;
   struct Operands {
     V8 x[kSub][kFt], w[kSub][kFn];
   };
@@ -500,9 +559,10 @@ __global__ __launch_bounds__(kWt *kWn * 64, 2) void project_kernel(const Project
 #pragma unroll
         for (int i = 0; i < kFt; ++i) acc[j][i] = N::mfma16(o.w[ks][j], o.x[ks][i], acc[j][i]);
   };
-  auto step = [&](int s, Operands &now, Operands &then) {
+  auto step = [&](int s, Operands &now, Operands &then, bool low) {
     wait_and_meet<(kStages - 2) * kLoads>();  // step s + 1 is here, step s in registers
-    fetch(s + kStages);
+    if (low && s + kStages >= main_steps) fetch_low(s + kStages);
+    else fetch(s + kStages);
     read(then, s + 1);
     multiply(now);
     // the scheduler would put the reads at the end, where the next step waits for them
@@ -514,106 +574,159 @@ __global__ __launch_bounds__(kWt *kWn * 64, 2) void project_kernel(const Project
       if (i < kLoads) __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);
     }
   };
-#pragma unroll
-  for (int s = 0; s < kStages; ++s) fetch(s);
+  // steps of a small tile are short, so that they wait for their loads: from a few adapters on
+  // they are gathered
+  constexpr int kMany = 3;
+  bool gather = P.adapter && P.gather;
+  const bool steps_low = !kCut && P.adapter && !P.gather;
+  int id = -1;
+  if (steps_low && threadIdx.x < kT) id = adapter_of(P, t0 + threadIdx.x);
+  const int begun = steps_low ? min(main_steps, kStages) : kStages;
+  for (int s = 0; s < begun; ++s) fetch(s);
+  if (steps_low) {
+    if (threadIdx.x < kT) s_id[threadIdx.x] = id;
+    __syncthreads();
+    const int n = distinct<kT, kWaves>(s_id, s_heads, s_list, s_counts);
+    gather = kFt * kFn <= 4 && n > kMany;
+    if (!gather) steps += per * n;
+    for (int s = begun; s < kStages; ++s) fetch_low(s);
+  }
   wait_and_meet<(kStages - 1) * kLoads>();
   Operands a, b;
   read(a, 0);
-  for (int s = 0; s < steps; s += 2) {  // a step past the last one multiplies zeros
-    step(s, a, b);
-    step(s + 1, b, a);
+  int s = 0;
+  for (; s + 1 + kStages < main_steps; s += 2) {
+    step(s, a, b, false);
+    step(s + 1, b, a, false);
+  }
+  for (; s < steps; s += 2) {  // a step past the last one multiplies zeros
+    step(s, a, b, steps_low);
+    step(s + 1, b, a, steps_low);
   }
   wait_loads();  // LDS belongs to the next workgroup from here on
-  if (P.adapter) add_adapters<kType, kFn, kFt>(P, t0 + wt, n0 + wn, acc);
+  if constexpr (kCut) {
+    float *to = P.part + int64_t(cut) * P.n_tokens * P.part_stride;
+#pragma unroll
+    for (int i = 0; i < kFt; ++i) {
+      const int t = t0 + wt + 16 * i + col;
+      if (t >= P.n_tokens) continue;
+#pragma unroll
+      for (int j = 0; j < kFn; ++j) {
+        const int n = n0 + wn + 16 * j + 4 * quad;
+        if (n < P.part_stride)
+          *reinterpret_cast<f32x4 *>(to + int64_t(t) * P.part_stride + n) = acc[j][i];
+      }
+    }
+    return;
+  }
+  if constexpr (kFt * kFn <= 4) {
+    if (gather) add_gathered<kType, kFn, kFt>(P, t0 + wt, n0 + wn, acc);
+  }
   store<kType, kFn, kFt>(P, t0 + wt, n0 + wn, acc);
+  if (steps > main_steps) mend<kType, kFn, kFt>(P, t0 + wt, n0 + wn, acc);
 }
 
-// Few tokens (kFt x 16 of them): 16 outputs a workgroup, k cut over its waves, operands straight
-// from memory; the waves' sums are joined in LDS. A lane takes 32 bytes of a row at a time, so
-// that 4 lanes cover a line; x is read in the same order of k.
-constexpr int kFewWaves = 8;
+// Adds the cuts of k, and each token's adapter: a thread has 4 outputs of a token.
+constexpr int kFinishThreads = 256;
 
-template <int kType, int kFt>
-__global__ __launch_bounds__(kFewWaves * 64) void project_few_kernel(const ProjectParams P) {
-  typedef Num<kType> N;
-  typedef typename N::E E;
-  typedef typename N::V8 V8;
-  __shared__ f32x4 part[kFewWaves][kFt][64];
-  const int lane = threadIdx.x & 63;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int col = lane & 15, quad = lane >> 4;
-  const int n0 = blockIdx.x * 16;
-  const E *w = static_cast<const E *>(P.w) + min(n0 + col, P.n - 1) * P.w_stride;
-  const E *x[kFt];
+template <int kType>
+__global__ __launch_bounds__(kFinishThreads) void finish_kernel(const ProjectParams P) {
+  typedef typename Num<kType>::E E;
+  typedef typename Num<kType>::V4 V4;
+  typedef typename Num<kType>::V8 V8;
+  const int t = blockIdx.y, n = (blockIdx.x * kFinishThreads + threadIdx.x) * 4;
+  if (n >= P.n) return;
+  const float *from = P.part + int64_t(t) * P.part_stride + n;
+  const int64_t cut = int64_t(P.n_tokens) * P.part_stride;
+  const int g = adapter_of(P, t);
+  f32x4 sum = {};
+#pragma unroll 8
+  for (int s = 0; s < P.splits; ++s) sum += *reinterpret_cast<const f32x4 *>(from + s * cut);
+  if (g >= 0) {
+    const f32x4 *h = reinterpret_cast<const f32x4 *>(P.h32 + int64_t(t) * P.pad_rank);
+    for (int r0 = 0; r0 < P.rank; r0 += 16) {
 #pragma unroll
-  for (int i = 0; i < kFt; ++i)
-    x[i] = static_cast<const E *>(P.x) + min(16 * i + col, P.n_tokens - 1) * P.x_stride;
-  f32x4 acc[kFt] = {};
-  // a wave takes 64 values of k at a time, two such at once
-  auto take = [&](int k) {
-    V8 wf[2][2], xf[2][2][kFt];
+      for (int r = r0; r < r0 + 16; r += 8) {
+        const f32x4 h0 = h[r / 4], h1 = h[r / 4 + 1];
 #pragma unroll
-    for (int u = 0; u < 2; ++u)
+        for (int q = 0; q < 4; ++q) {
+          const V8 b = b_chunk<kType>(P, g, n + q, r);
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const int at = k + u * kFewWaves * 64 + 8 * h;
-        wf[u][h] = V8{};
-        if (at < P.k) wf[u][h] = *reinterpret_cast<const V8 *>(w + at);
-#pragma unroll
-        for (int i = 0; i < kFt; ++i) {
-          xf[u][h][i] = V8{};
-          if (at < P.k) xf[u][h][i] = *reinterpret_cast<const V8 *>(x[i] + at);
+          for (int e = 0; e < 8; ++e)
+            sum[q] = __builtin_fmaf(static_cast<float>(b[e]), e < 4 ? h0[e & 3] : h1[e & 3], sum[q]);
         }
       }
+    }
+  }
+  E *y = static_cast<E *>(P.y) + t * P.y_stride + n;
+  const V4 v = __builtin_convertvector(sum, V4);
+  if (P.vec_y && n + 3 < P.n) {
+    *reinterpret_cast<V4 *>(y) = v;
+  } else {
 #pragma unroll
-    for (int u = 0; u < 2; ++u)
-#pragma unroll
-      for (int h = 0; h < 2; ++h)
-#pragma unroll
-        for (int i = 0; i < kFt; ++i) acc[i] = N::mfma16(wf[u][h], xf[u][h][i], acc[i]);
-  };
-  for (int k = wave * 64; k < P.k; k += 2 * kFewWaves * 64) take(k + quad * 16);
-#pragma unroll
-  for (int i = 0; i < kFt; ++i) part[wave][i][lane] = acc[i];
-  __syncthreads();
-  if (wave >= kFt) return;
-  f32x4 sum[1][1] = {};
-#pragma unroll
-  for (int v = 0; v < kFewWaves; ++v) sum[0][0] += part[v][wave][lane];
-  if (P.adapter) add_adapters<kType, 1, 1>(P, 16 * wave, n0, sum);
-  store<kType, 1, 1>(P, 16 * wave, n0, sum);
+    for (int q = 0; q < 4; ++q)
+      if (n + q < P.n) y[q] = v[q];
+  }
 }
 
-template <int kType, int kT, int kN, int kWt, int kWn, int kBK, int kStages>
+template <int kType, int kT, int kN, int kWt, int kWn, int kBK, int kStages, bool kCut = false>
 int launch_tiles(ProjectParams P, hipStream_t s) {
   const int64_t tiles_t = (int64_t(P.n_tokens) + kT - 1) / kT;
   const int64_t tiles_n = (int64_t(P.n) + kN - 1) / kN;
-  if (tiles_t * tiles_n > INT32_MAX / kGroup) return TG_E_INVAL;
+  if (tiles_t * tiles_n > INT32_MAX / (kCut ? 64 : kGroup)) return TG_E_INVAL;
   P.tiles_t = static_cast<int32_t>(tiles_t);
   P.tiles_n = static_cast<int32_t>(tiles_n);
-  hipLaunchKernelGGL((project_kernel<kType, kT, kN, kWt, kWn, kBK, kStages>),
-                     dim3(static_cast<uint32_t>(tiles_t * tiles_n)), dim3(kWt * kWn * 64), 0, s,
-                     P);
+  const int64_t blocks = tiles_t * tiles_n * (kCut ? P.splits : 1) + (kCut ? P.low_blocks : 0);
+  hipLaunchKernelGGL((project_kernel<kType, kT, kN, kWt, kWn, kBK, kStages, kCut>),
+                     dim3(static_cast<uint32_t>(blocks)), dim3(kWt * kWn * 64), 0, s, P);
   return TG_OK;
 }
 
-template <int kType, int kFt>
-int launch_few(const ProjectParams &P, hipStream_t s) {
-  hipLaunchKernelGGL((project_few_kernel<kType, kFt>), dim3((P.n + 15) / 16),
-                     dim3(kFewWaves * 64), 0, s, P);
-  return TG_OK;
+// The few-token form: tiles of 32 or 64 tokens x 64 outputs, k in `splits` cuts.
+constexpr int kFewTokens = 256;
+struct Few {
+  bool use, alone;  // for adapters, and without any
+  int tile, splits;
+};
+
+Few few_of(int n_tokens, int k, int n) {
+  Few f = {n_tokens <= kFewTokens, false, n_tokens <= 32 ? 32 : 64, 1};
+  if (!f.use) return f;
+  const int64_t tiles = int64_t((n_tokens + f.tile - 1) / f.tile) * ((int64_t(n) + 63) / 64);
+  const int steps = (k + 63) / 64;
+  // two workgroups a CU, and 4 steps at least for a cut
+  int64_t want = (512 + tiles - 1) / tiles;
+  if (want > steps / 4) want = steps / 4;
+  if (want > 16) want = 16;
+  if (want < 1) want = 1;
+  const int each = (steps + static_cast<int>(want) - 1) / static_cast<int>(want);
+  f.splits = (steps + each - 1) / each;
+  f.alone = tiles <= 64 && steps >= 32;  // else the second launch costs more than it brings
+  return f;
 }
+
+int part_stride(int n) { return (n + 3) / 4 * 4; }
 
 template <int kType>
-int launch(const ProjectParams &P, hipStream_t s) {
-  if (P.adapter) launch_shrink<kType>(P, s);
+int launch(ProjectParams P, const Few &few, hipStream_t s) {
   int rc;
+  if (few.use && (P.adapter || few.alone)) {
+    P.splits = few.splits;
+    P.low_blocks = P.adapter ? P.n_tokens : 0;
+    rc = few.tile == 32 ? launch_tiles<kType, 32, 64, 1, 4, 64, 4, true>(P, s)
+                        : launch_tiles<kType, 64, 64, 2, 2, 64, 4, true>(P, s);
+    if (rc != TG_OK) return rc;
+    hipLaunchKernelGGL(finish_kernel<kType>,
+                       dim3((P.part_stride / 4 + kFinishThreads - 1) / kFinishThreads, P.n_tokens),
+                       dim3(kFinishThreads), 0, s, P);
+    return hipGetLastError() == hipSuccess ? TG_OK : TG_E_HIP;
+  }
+  if (P.adapter) launch_shrink<kType>(P, s);
   const int64_t big = ((int64_t(P.n_tokens) + 255) / 256) * ((P.n + 255) / 256);
   const int64_t mid = ((int64_t(P.n_tokens) + 127) / 128) * ((P.n + 127) / 128);
-  if (P.n_tokens <= 16) rc = launch_few<kType, 1>(P, s);
-  else if (P.n_tokens <= 32) rc = launch_few<kType, 2>(P, s);
-  else if (P.n_tokens <= 64) rc = launch_few<kType, 4>(P, s);
-  else if (big >= 256) rc = launch_tiles<kType, 256, 256, 2, 4, 32, 4>(P, s);
+  P.gather = P.adapter && P.b_step == 1;  // rows of b that a load to LDS cannot take
+  if (P.gather) rc = launch_tiles<kType, 64, 64, 2, 2, 64, 4>(P, s);
+  else if (big >= 1024) rc = launch_tiles<kType, 256, 256, 2, 4, 32, 4>(P, s);
   else if (mid >= 256) rc = launch_tiles<kType, 128, 128, 2, 2, 64, 2>(P, s);
   else rc = launch_tiles<kType, 64, 64, 2, 2, 64, 4>(P, s);
   if (rc != TG_OK) return rc;
@@ -626,9 +739,14 @@ int pad_rank(int rank) { return rank <= 16 ? 16 : rank <= 32 ? 32 : 64; }
 
 extern "C" size_t tg_project_workspace_bytes(int32_t n_tokens, int32_t k, int32_t n,
                                              int32_t n_adapters, int32_t rank) {
-  if (n_tokens <= 0 || k <= 0 || n <= 0 || n_adapters <= 0 || rank <= 0) return 0;
+  if (n_tokens <= 0 || k <= 0 || n <= 0 || n_adapters < 0 || rank < 0) return 0;
+  const bool low = n_adapters > 0 && rank > 0;
+  if (n_adapters > 0 && !low) return 0;
   const size_t t = static_cast<size_t>(n_tokens);
-  return (t * 4 + 15) / 16 * 16 + t * 2 * pad_rank(rank) * 2;
+  const Few few = few_of(n_tokens, k, n);
+  size_t bytes = low ? t * pad_rank(rank) * (2 * 2 + sizeof(float)) : 0;
+  if (few.use && (low || few.alone)) bytes += few.splits * t * part_stride(n) * sizeof(float);
+  return bytes;
 }
 
 extern "C" int tg_project(const tg_project_args *a, void *stream) {
@@ -639,7 +757,7 @@ extern "C" int tg_project(const tg_project_args *a, void *stream) {
       a->w_stride % 8 || a->x_stride > kMaxStride || a->w_stride > kMaxStride)
     return TG_E_INVAL;
   const bool low = a->adapter && a->n_adapters > 0;
-  if (low && (a->rank < 1 || a->rank > TG_PROJECT_MAX_RANK)) return TG_E_INVAL;
+  if (low && (a->rank < 1 || a->rank > TG_PROJECT_MAX_RANK || a->n > (1 << 23))) return TG_E_INVAL;
   if (a->n_tokens == 0) return TG_OK;
   if (!a->x || !a->w || !a->y || !aligned16(a->x) || !aligned16(a->w)) return TG_E_INVAL;
   if (low && (!a->a || !a->b || !a->scale || !aligned16(a->a))) return TG_E_INVAL;
@@ -654,11 +772,14 @@ extern "C" int tg_project(const tg_project_args *a, void *stream) {
   P.k = a->k;
   P.n = a->n;
   P.vec_y = reinterpret_cast<uintptr_t>(a->y) % 8 == 0 && a->y_stride % 4 == 0;
+  const Few few = few_of(a->n_tokens, a->k, a->n);
+  const size_t need = tg_project_workspace_bytes(a->n_tokens, a->k, a->n,
+                                                 low ? a->n_adapters : 0, low ? a->rank : 0);
+  if (need > 0 && (!a->workspace || a->workspace_bytes < need || !aligned16(a->workspace)))
+    return TG_E_WORKSPACE;
+  P.part = static_cast<float *>(a->workspace);
+  P.part_stride = part_stride(a->n);
   if (low) {
-    const size_t need =
-        tg_project_workspace_bytes(a->n_tokens, a->k, a->n, a->n_adapters, a->rank);
-    if (!a->workspace || a->workspace_bytes < need || !aligned16(a->workspace))
-      return TG_E_WORKSPACE;
     P.a = a->a;
     P.b = a->b;
     P.adapter = a->adapter;
@@ -666,9 +787,12 @@ extern "C" int tg_project(const tg_project_args *a, void *stream) {
     P.n_adapters = a->n_adapters;
     P.rank = a->rank;
     P.pad_rank = pad_rank(a->rank);
-    P.power = static_cast<float *>(a->workspace);
-    P.h = static_cast<char *>(a->workspace) + (size_t(a->n_tokens) * 4 + 15) / 16 * 16;
+    const uintptr_t at = reinterpret_cast<uintptr_t>(a->b);
+    P.b_step = a->rank % 8 == 0 && at % 16 == 0 ? 8 : a->rank % 2 == 0 && at % 4 == 0 ? 2 : 1;
+    P.h32 = static_cast<float *>(a->workspace);
+    P.h = P.h32 + size_t(a->n_tokens) * P.pad_rank;
+    P.part = P.h32 + size_t(a->n_tokens) * P.pad_rank * 2;
   }
   hipStream_t s = static_cast<hipStream_t>(stream);
-  return a->type == TG_F16 ? launch<TG_F16>(P, s) : launch<TG_BF16>(P, s);
+  return a->type == TG_F16 ? launch<TG_F16>(P, few, s) : launch<TG_BF16>(P, few, s);
 }

@@ -797,9 +797,8 @@ class ProjectBuffers:
 
         self.n_tokens = n_tokens
         self.y = torch.empty((n_tokens, n), dtype=dtype, device=device)
-        ws = 0
-        if adapters is not None:
-            ws = int(lib().tg_project_workspace_bytes(n_tokens, k, n, adapters.n, adapters.rank))
+        low = (adapters.n, adapters.rank) if adapters is not None else (0, 0)
+        ws = int(lib().tg_project_workspace_bytes(n_tokens, k, n, *low))
         self.workspace = torch.empty(max(ws, 16), dtype=torch.uint8, device=device)
         self.workspace_bytes = ws
 
@@ -833,7 +832,7 @@ def project_args(x, w, bufs: ProjectBuffers, adapters: Adapters | None = None,
         a.adapter, a.a, a.b = (token_adapter.data_ptr(), adapters.a.data_ptr(),
                                adapters.b.data_ptr())
         a.scale, a.n_adapters, a.rank = adapters.scale.data_ptr(), adapters.n, adapters.rank
-        a.workspace, a.workspace_bytes = bufs.workspace.data_ptr(), bufs.workspace_bytes
+    a.workspace, a.workspace_bytes = bufs.workspace.data_ptr(), bufs.workspace_bytes
     a._keep = (x, w, bufs, adapters, token_adapter)  # the struct holds raw pointers: keep their owners alive
     return a
 
