@@ -40,7 +40,8 @@ constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / 64;
 // Caps up to here use 1 - 2 / (1 + 2^x) for tanh, whose error of a few 2^-24 times the cap stays
-// below 1e-4 in the exponent; larger ones the function of the math library.
+// below 1e-4 in the exponent; with larger ones small arguments, where 1 and the quotient cancel,
+// take the series.
 constexpr float kFastCap = 256.0f;
 
 struct AttendParams {
@@ -54,7 +55,7 @@ struct AttendParams {
   float cap_in;     // raw score -> exponent of 2 inside tanh: 2 log2(e) scale / cap
   float cap_out;    // cap * log2(e)
   float cap_arg;    // scale / cap
-  int32_t capped;   // 0 none, 1 fast, 2 exact
+  int32_t capped;   // 0 none, 1 up to kFastCap, 2 above
   int32_t shaped;   // scores are brought to log2 units before the softmax (cap, bias, scale <= 0)
   int32_t causal, n_seqs, n_q_rows;
   int64_t n_k_rows;
@@ -98,16 +99,60 @@ __device__ __forceinline__ int key_limit(const AttendParams &P, const Seq &s, in
   return min(s.nk, max(s.place0 + i + 1, s.prefix));
 }
 
-// A raw score in log2 units; `far` is the distance. (The tile kernels do the same steps.)
+// 1 / (1 + 2^x), which is (1 - tanh) / 2 of the argument that x stands for.
+__device__ __forceinline__ float fall(float x) {
+  return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(x));
+}
+
+// A raw score capped, in log2 units.
+__device__ __forceinline__ float cap_score(const AttendParams &P, float s) {
+  const float z = __builtin_fmaf(-2.0f * P.cap_out, fall(s * P.cap_in), P.cap_out);
+  if (P.capped == 1) return z;
+  // x - x^3 / 3 + 2 x^5 / 15 - 17 x^7 / 315: to 2e-9 below 1 / 8
+  const float x = s * P.cap_arg, x2 = x * x;
+  const float p = __builtin_fmaf(
+      x2, __builtin_fmaf(x2, __builtin_fmaf(x2, -17.0f / 315, 2.0f / 15), -1.0f / 3), 1.0f);
+  return fabsf(x) < 0.125f ? P.cap_out * (x * p) : z;
+}
+
+// A raw score in log2 units; `far` is the distance. (The tile kernel does the same steps.)
 __device__ __forceinline__ float shape(const AttendParams &P, float s, float slope2, float far) {
-  float z = s * P.to_log2;
-  if (P.capped == 1) {
-    z = P.cap_out - 2.0f * P.cap_out * __builtin_amdgcn_rcpf(
-                        1.0f + __builtin_amdgcn_exp2f(s * P.cap_in));
-  } else if (P.capped == 2) {
-    z = P.cap_out * tanhf(s * P.cap_arg);
-  }
+  const float z = P.capped ? cap_score(P, s) : s * P.to_log2;
   return z - slope2 * far;
+}
+
+// The largest, or smallest, of three in one instruction; NaN is left out where there is another.
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+  return r;
+}
+__device__ __forceinline__ float min3(float a, float b, float c) {
+  float r;
+  asm("v_min3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+  return r;
+}
+
+// a[0] + a[1] + c of two values of the type.
+template <int kType>
+__device__ __forceinline__ float add2(typename Num<kType>::V2 a, float c);
+template <>
+__device__ __forceinline__ float add2<TG_F16>(Num<TG_F16>::V2 a, float c) {
+  const Num<TG_F16>::V2 one = {static_cast<_Float16>(1.0f), static_cast<_Float16>(1.0f)};
+  return __builtin_amdgcn_fdot2(a, one, c, false);
+}
+template <>
+__device__ __forceinline__ float add2<TG_BF16>(Num<TG_BF16>::V2 a, float c) {
+  const Num<TG_BF16>::V2 one = {static_cast<__bf16>(1.0f), static_cast<__bf16>(1.0f)};
+  return __builtin_amdgcn_fdot2_f32_bf16(a, one, c, false);
+}
+
+// The larger of a lane's value and that of its partner in the other half of the wave.
+__device__ __forceinline__ float both_halves(float v) {
+  const unsigned u = __builtin_bit_cast(unsigned, v);
+  const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+  return fmaxf(__builtin_bit_cast(float, static_cast<unsigned>(r[0])),
+               __builtin_bit_cast(float, static_cast<unsigned>(r[1])));
 }
 
 __device__ __forceinline__ int abs_diff(int a, int b) { return a > b ? a - b : b - a; }
@@ -216,7 +261,15 @@ __device__ __forceinline__ typename Num<kType>::V4 read_transposed(const void *p
 constexpr int kBM = 128, kBN = 64;
 constexpr int kMaskTiles = 4096;  // key tiles whose documents are looked through at once
 
-template <int kType, int kD>
+// What is done to a score between the products, decided when compiled where it is common.
+enum Mode {
+  kPlain = 0,  // the factor only
+  kCapped = 1, // a cap up to kFastCap
+  kSloped = 2, // a bias by the distance of indexes
+  kAny = 3     // any of the above at once, positions, documents, a factor <= 0
+};
+
+template <int kType, int kD, int kMode>
 __global__ __launch_bounds__(kThreads, 2) void attend_tile_kernel(const AttendParams P) {
   typedef Num<kType> N;
   typedef typename N::E E;
@@ -225,10 +278,12 @@ __global__ __launch_bounds__(kThreads, 2) void attend_tile_kernel(const AttendPa
   constexpr int kChunks = kD / 8, kSteps = kD / 16, kBlocks = kD / 32;
   __shared__ __attribute__((aligned(16))) E tk[2][kBN * kD];
   __shared__ __attribute__((aligned(16))) E tv[2][kBN * kD];
-  __shared__ int s_doc[2][kBN];
-  __shared__ int s_pos[2][kBN][2];
-  __shared__ uint64_t s_use[kMaskTiles / 64];
+  constexpr bool kAnyMode = kMode == kAny;
+  __shared__ int s_doc[2][kAnyMode ? kBN : 1];
+  __shared__ int s_pos[2][kAnyMode ? kBN : 1][2];
+  __shared__ uint64_t s_use[kAnyMode ? kMaskTiles / 64 : 1];
   __shared__ int s_range[kWaves][2];
+  const bool with_docs = kAnyMode && P.k_doc, with_pos = kAnyMode && P.k_pos;
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int col = lane & 31, half = lane >> 5;
@@ -262,17 +317,17 @@ __global__ __launch_bounds__(kThreads, 2) void attend_tile_kernel(const AttendPa
   const int all = key_limit(P, s, min(wave_first, s.nq - 1));
   const int end = key_limit(P, s, min(first + kBM, s.nq) - 1);
   const int wave_end = wave_first < s.nq ? key_limit(P, s, min(wave_first + 32, s.nq) - 1) : 0;
-  int doc = P.q_doc && live ? P.q_doc[row] : -1;
-  const float slope2 = P.slope ? P.slope[head] * kLog2e : 0.0f;
+  int doc = with_docs && live ? P.q_doc[row] : -1;
+  const float slope2 = kMode >= kSloped && P.slope ? P.slope[head] * kLog2e : 0.0f;
   const int place = s.place0 + i;
   int px = 0, py = 0;
-  if (P.q_pos) {
+  if (with_pos) {
     px = P.q_pos[2 * row];
     py = P.q_pos[2 * row + 1];
   }
   int wave_lo = INT_MAX, wave_hi = -1;  // the documents of the wave's queries
   int block_lo = INT_MAX, block_hi = -1;
-  if (P.q_doc) {
+  if (with_docs) {
     int a = doc >= 0 ? doc : INT_MAX, b = doc;
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) {
@@ -295,12 +350,11 @@ __global__ __launch_bounds__(kThreads, 2) void attend_tile_kernel(const AttendPa
   }
   f32x16 acc[kBlocks] = {};
   float m = -INFINITY, l = 0.0f;
-  const float unit = P.shaped ? 1.0f : P.to_log2;
   const int tiles = (end + kBN - 1) / kBN;
 
   for (int seg = 0; seg < tiles; seg += kMaskTiles) {
     const int seg_end = min(tiles, seg + kMaskTiles);
-    if (P.k_doc) {  // which tiles hold a key whose document is in the queries' range
+    if (with_docs) {  // which tiles hold a key whose document is in the queries' range
       __syncthreads();
       for (int t = threadIdx.x; t < kMaskTiles / 64; t += kThreads) s_use[t] = 0;
       __syncthreads();
@@ -314,7 +368,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_tile_kernel(const AttendPa
       __syncthreads();
     }
     auto next = [&](int t) {  // the first tile to visit from t on
-      if (!P.k_doc) return t;
+      if (!with_docs) return t;
       while (t < seg_end) {
         const uint64_t w = s_use[(t - seg) >> 6] >> ((t - seg) & 63);
         if (w) {
@@ -331,10 +385,10 @@ __global__ __launch_bounds__(kThreads, 2) void attend_tile_kernel(const AttendPa
                                      kWaves);
       load_rows<kBN, kChunks, false>(vb, P.v_stride, s.k0 + j0, s.nk - j0, P.d, tv[to], wave,
                                      kWaves);
-      if (wave == 0 && (P.k_doc || P.k_pos)) {
+      if (wave == 0 && (with_docs || with_pos)) {
         const int64_t r = s.k0 + min(j0 + lane, s.nk - 1);
-        if (P.k_doc) s_doc[to][lane] = P.k_doc[r];
-        if (P.k_pos) {
+        if (with_docs) s_doc[to][lane] = P.k_doc[r];
+        if (with_pos) {
           s_pos[to][lane][0] = P.k_pos[2 * r];
           s_pos[to][lane][1] = P.k_pos[2 * r + 1];
         }
@@ -349,7 +403,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_tile_kernel(const AttendPa
       __syncthreads();
       if (after < seg_end) fetch(after, buf ^ 1);
       bool skip = j0 >= wave_end, docs = false;
-      if (P.k_doc && !skip) {
+      if (with_docs && !skip) {
         const int kd = s_doc[buf][lane];
         skip = __ballot(kd >= wave_lo && kd <= wave_hi) == 0;
         docs = !(wave_lo == wave_hi && __ballot(kd == wave_lo) == ~0ull &&
@@ -366,60 +420,80 @@ __global__ __launch_bounds__(kThreads, 2) void attend_tile_kernel(const AttendPa
                 tk[buf] + r * kD + place_of<kChunks, false>(r, 2 * k + half) * 8);
             z[b] = N::mfma32(kf, qf[k], z[b]);
           }
-        if (P.shaped) {
-          if (P.capped == 1) {
+        const bool edge = j0 + kBN > all;  // some query does not see some key, documents aside
+        // A weight is 2^(z factor - (m - shift)): what is left of a score's way to log2 units,
+        // and what all of a lane's scores of the tile have in common.
+        float factor = 1.0f, shift = 0.0f;
+        if constexpr (kMode == kPlain) {
+          factor = P.to_log2;
+        } else if constexpr (kMode == kCapped) {
+          // cap (1 - 2 f): with f in the place of the score the cap is one more factor
+#pragma unroll
+          for (int e = 0; e < 32; ++e) z[e >> 4][e & 15] = fall(z[e >> 4][e & 15] * P.cap_in);
+          factor = -2.0f * P.cap_out;
+          shift = P.cap_out;
+        } else if constexpr (kMode == kSloped) {
+          const float here = static_cast<float>(place - j0 - 4 * half);
+          if (!edge && j0 + kBN <= s.place0 + wave_first + 1) {  // all keys at or before all queries
+            shift = -slope2 * here;
 #pragma unroll
             for (int e = 0; e < 32; ++e)
-              z[e >> 4][e & 15] =
-                  P.cap_out - 2.0f * P.cap_out *
-                                  __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(
-                                                                   z[e >> 4][e & 15] * P.cap_in));
-          } else if (P.capped == 2) {
-            for (int b = 0; b < 2; ++b)
-#pragma unroll
-              for (int e = 0; e < 16; ++e) z[b][e] = P.cap_out * tanhf(z[b][e] * P.cap_arg);
+              z[e >> 4][e & 15] = __builtin_fmaf(
+                  z[e >> 4][e & 15], P.to_log2,
+                  slope2 * static_cast<float>((e >> 2) * 8 + (e & 3)));
           } else {
 #pragma unroll
-            for (int e = 0; e < 32; ++e) z[e >> 4][e & 15] *= P.to_log2;
+            for (int e = 0; e < 32; ++e)
+              z[e >> 4][e & 15] = __builtin_fmaf(
+                  z[e >> 4][e & 15], P.to_log2,
+                  -slope2 * fabsf(here - static_cast<float>((e >> 2) * 8 + (e & 3))));
           }
-          if (P.slope && !P.k_pos) {
+        } else {
+          if (P.capped) {
+#pragma unroll
+            for (int e = 0; e < 32; ++e) z[e >> 4][e & 15] = cap_score(P, z[e >> 4][e & 15]);
+          } else if (P.shaped) {
+#pragma unroll
+            for (int e = 0; e < 32; ++e) z[e >> 4][e & 15] *= P.to_log2;
+          } else {
+            factor = P.to_log2;
+          }
+          if (P.slope && !with_pos) {
             const float here = static_cast<float>(place - j0 - 4 * half);
 #pragma unroll
             for (int e = 0; e < 32; ++e)
-              z[e >> 4][e & 15] -=
-                  slope2 * fabsf(here - static_cast<float>((e >> 2) * 8 + (e & 3)));
+              z[e >> 4][e & 15] = __builtin_fmaf(
+                  -slope2, fabsf(here - static_cast<float>((e >> 2) * 8 + (e & 3))),
+                  z[e >> 4][e & 15]);
           } else if (P.slope) {
 #pragma unroll
             for (int e = 0; e < 32; ++e) {
               const int j = (e >> 2) * 8 + 4 * half + (e & 3);
               const int far = abs_diff(px, s_pos[buf][j][0]) + abs_diff(py, s_pos[buf][j][1]);
-              z[e >> 4][e & 15] -= slope2 * static_cast<float>(far);
+              z[e >> 4][e & 15] =
+                  __builtin_fmaf(-slope2, static_cast<float>(far), z[e >> 4][e & 15]);
             }
           }
         }
-        if (j0 + kBN > all) {
+        // a factor < 0 turns the order round
+        constexpr float kNone = kMode == kCapped ? INFINITY : -INFINITY;
+        if (edge) {
           const int last = limit - j0 - 4 * half;
 #pragma unroll
           for (int e = 0; e < 32; ++e)
-            if ((e >> 2) * 8 + (e & 3) >= last) z[e >> 4][e & 15] = -INFINITY;
+            if ((e >> 2) * 8 + (e & 3) >= last) z[e >> 4][e & 15] = kNone;
         }
         if (docs) {
 #pragma unroll
           for (int e = 0; e < 32; ++e)
-            if (s_doc[buf][(e >> 2) * 8 + 4 * half + (e & 3)] != doc)
-              z[e >> 4][e & 15] = -INFINITY;
+            if (s_doc[buf][(e >> 2) * 8 + 4 * half + (e & 3)] != doc) z[e >> 4][e & 15] = kNone;
         }
-        float big = -INFINITY;
+        float big = kNone;
 #pragma unroll
-        for (int e = 0; e < 32; ++e) big = fmaxf(big, z[e >> 4][e & 15]);
-        big *= unit;
-        {
-          const auto r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(unsigned, big),
-                                                          __builtin_bit_cast(unsigned, big), false,
-                                                          false);
-          big = fmaxf(__builtin_bit_cast(float, static_cast<unsigned>(r[0])),
-                      __builtin_bit_cast(float, static_cast<unsigned>(r[1])));
-        }
+        for (int e = 0; e < 32; e += 2)
+          big = kMode == kCapped ? min3(big, z[e >> 4][e & 15], z[e >> 4][(e & 15) + 1])
+                                 : max3(big, z[e >> 4][e & 15], z[e >> 4][(e & 15) + 1]);
+        big = both_halves(__builtin_fmaf(big, factor, shift));
         if (__ballot(big > m + kSlack)) {
           const float to = fmaxf(m, big);
           const float fix = to == m ? 1.0f : __builtin_amdgcn_exp2f(m - to);
@@ -430,21 +504,18 @@ __global__ __launch_bounds__(kThreads, 2) void attend_tile_kernel(const AttendPa
 #pragma unroll
             for (int r = 0; r < 16; ++r) acc[b][r] *= fix;
         }
-        const float base = m == -INFINITY ? 0.0f : m;
-#pragma unroll
-        for (int e = 0; e < 32; ++e) {
-          const float p =
-              __builtin_amdgcn_exp2f(__builtin_fmaf(z[e >> 4][e & 15], unit, -base));
-          z[e >> 4][e & 15] = p;
-          l += p;
-        }
+        const float base = shift - (m == -INFINITY ? 0.0f : m);
 #pragma unroll
         for (int k = 0; k < 4; ++k) {  // 16 keys
           V8 pf;
 #pragma unroll
           for (int e = 0; e < 8; e += 2) {
-            const auto two =
-                pack2<kType>(z[k >> 1][(k & 1) * 8 + e], z[k >> 1][(k & 1) * 8 + e + 1]);
+            const float p0 = __builtin_amdgcn_exp2f(
+                __builtin_fmaf(z[k >> 1][(k & 1) * 8 + e], factor, base));
+            const float p1 = __builtin_amdgcn_exp2f(
+                __builtin_fmaf(z[k >> 1][(k & 1) * 8 + e + 1], factor, base));
+            const auto two = pack2<kType>(p0, p1);
+            l = add2<kType>(two, l);
             pf[e] = two[0];
             pf[e + 1] = two[1];
           }
@@ -779,8 +850,16 @@ int launch(const AttendParams &P, const Split &sp, hipStream_t s) {
   } else {
     const int64_t blocks = (int64_t(P.n_q_rows) / kBM + P.n_seqs) * P.n_heads;
     if (blocks > INT32_MAX) return TG_E_INVAL;
-    hipLaunchKernelGGL((attend_tile_kernel<kType, kD>), dim3(static_cast<uint32_t>(blocks)),
-                       dim3(kThreads), 0, s, P);
+    const dim3 grid(static_cast<uint32_t>(blocks)), threads(kThreads);
+    const bool any = P.k_doc || P.k_pos || P.capped == 2 || !(P.to_log2 > 0.0f);
+    if (any || (P.capped && P.slope))
+      hipLaunchKernelGGL((attend_tile_kernel<kType, kD, kAny>), grid, threads, 0, s, P);
+    else if (P.capped)
+      hipLaunchKernelGGL((attend_tile_kernel<kType, kD, kCapped>), grid, threads, 0, s, P);
+    else if (P.slope)
+      hipLaunchKernelGGL((attend_tile_kernel<kType, kD, kSloped>), grid, threads, 0, s, P);
+    else
+      hipLaunchKernelGGL((attend_tile_kernel<kType, kD, kPlain>), grid, threads, 0, s, P);
   }
   return hipGetLastError() == hipSuccess ? TG_OK : TG_E_HIP;
 }
