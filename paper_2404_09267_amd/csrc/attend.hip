@@ -227,23 +227,28 @@ __device__ __forceinline__ int place_of(int r, int c) {
   return c ^ g;
 }
 
-// Loads `kRows` rows from row j0 of a head's keys or values into an LDS tile; rows past the last
-// repeat it, values past d are 0. `first`, `count`: the waves that share the work.
-template <int kRows, int kChunks, bool kPairs>
+// Loads kRows rows of a head's keys or values, from `row` on, into an LDS tile, shared by kShare
+// waves; rows from `rows` on and values past d are 0. `offset` is that of the wave's first load,
+// which row_offset gives: rows of later loads lie kShare * 64 / kChunks further, and take their
+// chunks from the same places where that is a multiple of 16.
+template <int kChunks, bool kPairs>
+__device__ __forceinline__ uint32_t row_offset(int64_t stride, int d, int r) {
+  const int c = place_of<kChunks, kPairs>(r, (threadIdx.x & 63) & (kChunks - 1));
+  return c * 8 < d ? static_cast<uint32_t>((r * stride + c * 8) * 2) : kNowhere;
+}
+
+template <int kRows, int kChunks, bool kPairs, int kShare>
 __device__ __forceinline__ void load_rows(const void *base, int64_t stride, int64_t row, int rows,
-                                          int d, void *tile, int wave, int waves) {
-  constexpr int kPer = 64 / kChunks;  // rows of one load
-  const int lane = threadIdx.x & 63;
+                                          int d, void *tile, int wave, uint32_t offset) {
+  constexpr int kPer = 64 / kChunks, kStep = kPer * kShare;  // rows of one load, of one turn
   const auto b = buffer(static_cast<const char *>(base) + row * stride * 2,
                         static_cast<uint32_t>(((min(rows, kRows) - 1) * stride + d) * 2));
 #pragma unroll
-  for (int i = 0; i < kRows / kPer; ++i) {
-    if (i % waves != wave) continue;
-    const int r = i * kPer + lane / kChunks;
-    const int c = place_of<kChunks, kPairs>(r, lane & (kChunks - 1));
-    const uint32_t off = c * 8 < d ? static_cast<uint32_t>((min(r, rows - 1) * stride + c * 8) * 2)
-                                   : kNowhere;
-    load_lds(b, static_cast<char *>(tile) + i * 1024, off, 0);
+  for (int i = 0; i < kRows / kStep; ++i) {
+    uint32_t off = offset + static_cast<uint32_t>(i * kStep * stride * 2);
+    if (kStep % 16)
+      off = row_offset<kChunks, kPairs>(stride, d, i * kStep + (threadIdx.x & 63) / kChunks);
+    load_lds(b, static_cast<char *>(tile) + (i * kShare + wave) * 1024, off, 0);
   }
 }
 
@@ -348,6 +353,9 @@ __global__ __launch_bounds__(kThreads, 2) void attend_tile_kernel(const AttendPa
     }
     if (doc < 0) doc = INT_MIN;  // equal to no key's
   }
+  const int first_row = wave * (64 / kChunks) + lane / kChunks;
+  const uint32_t k_off = row_offset<kChunks, false>(P.k_stride, P.d, first_row);
+  const uint32_t v_off = row_offset<kChunks, false>(P.v_stride, P.d, first_row);
   f32x16 acc[kBlocks] = {};
   float m = -INFINITY, l = 0.0f;
   const int tiles = (end + kBN - 1) / kBN;
@@ -381,10 +389,10 @@ __global__ __launch_bounds__(kThreads, 2) void attend_tile_kernel(const AttendPa
     };
     auto fetch = [&](int t, int to) {
       const int j0 = t * kBN;
-      load_rows<kBN, kChunks, false>(kb, P.k_stride, s.k0 + j0, s.nk - j0, P.d, tk[to], wave,
-                                     kWaves);
-      load_rows<kBN, kChunks, false>(vb, P.v_stride, s.k0 + j0, s.nk - j0, P.d, tv[to], wave,
-                                     kWaves);
+      load_rows<kBN, kChunks, false, kWaves>(kb, P.k_stride, s.k0 + j0, s.nk - j0, P.d, tk[to],
+                                             wave, k_off);
+      load_rows<kBN, kChunks, false, kWaves>(vb, P.v_stride, s.k0 + j0, s.nk - j0, P.d, tv[to],
+                                             wave, v_off);
       if (wave == 0 && (with_docs || with_pos)) {
         const int64_t r = s.k0 + min(j0 + lane, s.nk - 1);
         if (with_docs) s_doc[to][lane] = P.k_doc[r];
@@ -619,10 +627,10 @@ __global__ __launch_bounds__(kThreads) void attend_few_kernel(const AttendParams
   float m = -INFINITY, l = 0.0f;
   const float unit = P.shaped ? 1.0f : P.to_log2;
   auto fetch = [&](int j0, int to) {
-    load_rows<kKeys, kChunks, true>(kb, P.k_stride, s.k0 + j0, s.nk - j0, P.d, tile[wave][to][0],
-                                    0, 1);
-    load_rows<kKeys, kChunks, true>(vb, P.v_stride, s.k0 + j0, s.nk - j0, P.d, tile[wave][to][1],
-                                    0, 1);
+    load_rows<kKeys, kChunks, true, 1>(kb, P.k_stride, s.k0 + j0, s.nk - j0, P.d,
+                                       tile[wave][to][0], 0, 0);
+    load_rows<kKeys, kChunks, true, 1>(vb, P.v_stride, s.k0 + j0, s.nk - j0, P.d,
+                                       tile[wave][to][1], 0, 0);
   };
   int j0 = from + wave * kKeys, buf = 0;
   if (j0 < end) fetch(j0, 0);
