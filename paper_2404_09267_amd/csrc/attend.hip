@@ -252,6 +252,16 @@ __device__ __forceinline__ void load_rows(const void *base, int64_t stride, int6
   }
 }
 
+// A key's document, or a coordinate (`part`) of its position, of up to kRows keys from `row` on:
+// one lane a key.
+template <int kRows>
+__device__ __forceinline__ void load_marks(const int32_t *base, int64_t row, int rows, int width,
+                                           int part, int *to) {
+  const int lane = threadIdx.x & 63;
+  const auto b = buffer(base + row * width, static_cast<uint32_t>(min(rows, kRows) * width * 4));
+  load_lds4(b, to, lane < kRows ? static_cast<uint32_t>((lane * width + part) * 4) : kNowhere);
+}
+
 template <int kType>
 __device__ __forceinline__ typename Num<kType>::V4 read_transposed(const void *p) {
   typedef __attribute__((address_space(3))) s16x4 *P3;
@@ -285,7 +295,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_tile_kernel(const AttendPa
   __shared__ __attribute__((aligned(16))) E tv[2][kBN * kD];
   constexpr bool kAnyMode = kMode == kAny;
   __shared__ int s_doc[2][kAnyMode ? kBN : 1];
-  __shared__ int s_pos[2][kAnyMode ? kBN : 1][2];
+  __shared__ int s_pos[2][2][kAnyMode ? kBN : 1];
   __shared__ uint64_t s_use[kAnyMode ? kMaskTiles / 64 : 1];
   __shared__ int s_range[kWaves][2];
   const bool with_docs = kAnyMode && P.k_doc, with_pos = kAnyMode && P.k_pos;
@@ -366,12 +376,21 @@ __global__ __launch_bounds__(kThreads, 2) void attend_tile_kernel(const AttendPa
       __syncthreads();
       for (int t = threadIdx.x; t < kMaskTiles / 64; t += kThreads) s_use[t] = 0;
       __syncthreads();
-      for (int t = seg + wave; t < seg_end; t += kWaves) {
-        const int j = t * kBN + lane;
-        const int kd = j < end ? P.k_doc[s.k0 + j] : -1;
-        if (__ballot(kd >= block_lo && kd <= block_hi) && lane == 0)
-          atomicOr(reinterpret_cast<unsigned long long *>(&s_use[(t - seg) >> 6]),
-                   1ull << ((t - seg) & 63));
+      constexpr int kAhead = 8;  // tiles of a wave whose documents are under way
+      for (int t0 = seg + wave * kAhead; t0 < seg_end; t0 += kWaves * kAhead) {
+        int kd[kAhead];
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+          const int j = (t0 + u) * kBN + lane;
+          kd[u] = t0 + u < seg_end && j < end ? P.k_doc[s.k0 + j] : -1;
+        }
+        uint32_t used = 0;
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u)
+          used |= (__ballot(kd[u] >= block_lo && kd[u] <= block_hi) ? 1u : 0u) << u;
+        if (used && lane == 0)  // 8 tiles from a multiple of 8 on: within one word
+          atomicOr(reinterpret_cast<unsigned long long *>(&s_use[(t0 - seg) >> 6]),
+                   static_cast<unsigned long long>(used) << ((t0 - seg) & 63));
       }
       __syncthreads();
     }
@@ -393,14 +412,10 @@ __global__ __launch_bounds__(kThreads, 2) void attend_tile_kernel(const AttendPa
                                              wave, k_off);
       load_rows<kBN, kChunks, false, kWaves>(vb, P.v_stride, s.k0 + j0, s.nk - j0, P.d, tv[to],
                                              wave, v_off);
-      if (wave == 0 && (with_docs || with_pos)) {
-        const int64_t r = s.k0 + min(j0 + lane, s.nk - 1);
-        if (with_docs) s_doc[to][lane] = P.k_doc[r];
-        if (with_pos) {
-          s_pos[to][lane][0] = P.k_pos[2 * r];
-          s_pos[to][lane][1] = P.k_pos[2 * r + 1];
-        }
-      }
+      if (with_docs && wave == 0)
+        load_marks<kBN>(P.k_doc, s.k0 + j0, s.nk - j0, 1, 0, s_doc[to]);
+      if (with_pos && (wave == 1 || wave == 2))
+        load_marks<kBN>(P.k_pos, s.k0 + j0, s.nk - j0, 2, wave - 1, s_pos[to][wave - 1]);
     };
     int t = next(seg), buf = 0;
     if (t < seg_end) fetch(t, 0);
@@ -477,7 +492,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_tile_kernel(const AttendPa
 #pragma unroll
             for (int e = 0; e < 32; ++e) {
               const int j = (e >> 2) * 8 + 4 * half + (e & 3);
-              const int far = abs_diff(px, s_pos[buf][j][0]) + abs_diff(py, s_pos[buf][j][1]);
+              const int far = abs_diff(px, s_pos[buf][0][j]) + abs_diff(py, s_pos[buf][1][j]);
               z[e >> 4][e & 15] =
                   __builtin_fmaf(-slope2, static_cast<float>(far), z[e >> 4][e & 15]);
             }
@@ -572,17 +587,21 @@ __global__ __launch_bounds__(kThreads, 2) void attend_tile_kernel(const AttendPa
 
 // ------------------------------------------------------------------------ few queries
 
-// Rows of a workgroup: 16 (query, head) pairs that share a key head, query-major. Each wave
-// takes every kWaves'th 32 keys of the workgroup's range through LDS of its own.
+// Rows of a workgroup: 16 (query, head) pairs that share a key head, query-major. Each of its two
+// waves takes every second 32 keys of the workgroup's range through LDS of its own; two waves, so
+// that several workgroups fit a CU and one's start and end fall into another's loads.
+constexpr int kFewWaves = 2;
+
 template <int kType, int kD>
-__global__ __launch_bounds__(kThreads) void attend_few_kernel(const AttendParams P) {
+__global__ __launch_bounds__(kFewWaves * 64) void attend_few_kernel(const AttendParams P) {
   typedef Num<kType> N;
   typedef typename N::E E;
   typedef typename N::V4 V4;
   typedef typename N::V8 V8;
   constexpr int kChunks = kD / 8, kSteps = kD / 32, kBlocks = kD / 16, kKeys = 32;
-  __shared__ __attribute__((aligned(16))) E tile[kWaves][2][2][kKeys * kD];
-  __shared__ float s_m[kWaves][16], s_l[kWaves][16];
+  __shared__ __attribute__((aligned(16))) E tile[kFewWaves][2][2][kKeys * kD];
+  __shared__ int s_marks[kFewWaves][2][3][64];  // documents and positions of a step's keys
+  __shared__ float s_m[kFewWaves][16], s_l[kFewWaves][16];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int col = lane & 15, quad = lane >> 4;
@@ -604,6 +623,21 @@ __global__ __launch_bounds__(kThreads) void attend_few_kernel(const AttendParams
   const int all = key_limit(P, s, rt * 16 / P.group);
   const int64_t row = int64_t(s.q0) + i;
   if (split > 0 && from >= end) return;  // join_kernel knows
+  const void *kb = static_cast<const E *>(P.k) + kvh * P.k_head;
+  const void *vb = static_cast<const E *>(P.v) + kvh * P.v_head;
+  auto fetch = [&](int j0, int to) {
+    load_rows<kKeys, kChunks, true, 1>(kb, P.k_stride, s.k0 + j0, s.nk - j0, P.d,
+                                       tile[wave][to][0], 0, 0);
+    load_rows<kKeys, kChunks, true, 1>(vb, P.v_stride, s.k0 + j0, s.nk - j0, P.d,
+                                       tile[wave][to][1], 0, 0);
+    if (P.k_doc) load_marks<kKeys>(P.k_doc, s.k0 + j0, s.nk - j0, 1, 0, s_marks[wave][to][0]);
+    if (P.k_pos) {
+      load_marks<kKeys>(P.k_pos, s.k0 + j0, s.nk - j0, 2, 0, s_marks[wave][to][1]);
+      load_marks<kKeys>(P.k_pos, s.k0 + j0, s.nk - j0, 2, 1, s_marks[wave][to][2]);
+    }
+  };
+  int j0 = from + wave * kKeys, buf = 0;
+  if (j0 < end) fetch(j0, 0);
   const E *qr = static_cast<const E *>(P.q) + row * P.q_stride + head * P.q_head;
   V8 qf[kSteps];
 #pragma unroll
@@ -611,8 +645,6 @@ __global__ __launch_bounds__(kThreads) void attend_few_kernel(const AttendParams
     qf[k] = V8{};
     if (k * 32 + quad * 8 < P.d) qf[k] = *reinterpret_cast<const V8 *>(qr + k * 32 + quad * 8);
   }
-  const void *kb = static_cast<const E *>(P.k) + kvh * P.k_head;
-  const void *vb = static_cast<const E *>(P.v) + kvh * P.v_head;
   const int limit = live ? key_limit(P, s, i) : 0;
   int doc = P.q_doc ? P.q_doc[row] : 0;
   if (doc < 0) doc = INT_MIN;
@@ -626,18 +658,11 @@ __global__ __launch_bounds__(kThreads) void attend_few_kernel(const AttendParams
   f32x4 acc[kBlocks] = {};
   float m = -INFINITY, l = 0.0f;
   const float unit = P.shaped ? 1.0f : P.to_log2;
-  auto fetch = [&](int j0, int to) {
-    load_rows<kKeys, kChunks, true, 1>(kb, P.k_stride, s.k0 + j0, s.nk - j0, P.d,
-                                       tile[wave][to][0], 0, 0);
-    load_rows<kKeys, kChunks, true, 1>(vb, P.v_stride, s.k0 + j0, s.nk - j0, P.d,
-                                       tile[wave][to][1], 0, 0);
-  };
-  int j0 = from + wave * kKeys, buf = 0;
-  if (j0 < end) fetch(j0, 0);
-  for (; j0 < end; j0 += kWaves * kKeys) {
+  for (; j0 < end; j0 += kFewWaves * kKeys) {
     wait_loads();
     const E *tk = tile[wave][buf][0], *tv = tile[wave][buf][1];
-    if (j0 + kWaves * kKeys < end) fetch(j0 + kWaves * kKeys, buf ^ 1);
+    const int(*marks)[64] = s_marks[wave][buf];
+    if (j0 + kFewWaves * kKeys < end) fetch(j0 + kFewWaves * kKeys, buf ^ 1);
     f32x4 z[2] = {};
 #pragma unroll
     for (int b = 0; b < 2; ++b)
@@ -648,29 +673,30 @@ __global__ __launch_bounds__(kThreads) void attend_few_kernel(const AttendParams
             tk + r * kD + place_of<kChunks, true>(r, 4 * k + quad) * 8);
         z[b] = N::mfma16(kf, qf[k], z[b]);
       }
+    if (P.shaped) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const int j = j0 + (e >> 2) * 16 + 4 * quad + (e & 3);
-      float ze = z[e >> 2][e & 3];
-      if (P.shaped) {
+      for (int e = 0; e < 8; ++e) {
+        const int at = (e >> 2) * 16 + 4 * quad + (e & 3);
         float far = 0.0f;
-        if (P.slope) {
-          int f = abs_diff(place, j);
-          if (P.k_pos) {
-            const int64_t r = s.k0 + min(j, s.nk - 1);
-            f = abs_diff(px, P.k_pos[2 * r]) + abs_diff(py, P.k_pos[2 * r + 1]);
-          }
-          far = static_cast<float>(f);
-        }
-        ze = shape(P, ze, slope2, far);
+        if (P.slope)
+          far = static_cast<float>(P.k_pos ? abs_diff(px, marks[1][at]) + abs_diff(py, marks[2][at])
+                                           : abs_diff(place, j0 + at));
+        z[e >> 2][e & 3] = shape(P, z[e >> 2][e & 3], slope2, far);
       }
-      if (j0 + kKeys > all && j >= limit) ze = -INFINITY;
-      if (P.k_doc && P.k_doc[s.k0 + min(j, s.nk - 1)] != doc) ze = -INFINITY;
-      z[e >> 2][e & 3] = ze;
+    }
+    if (j0 + kKeys > all) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (j0 + (e >> 2) * 16 + 4 * quad + (e & 3) >= limit) z[e >> 2][e & 3] = -INFINITY;
+    }
+    if (P.k_doc) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (marks[0][(e >> 2) * 16 + 4 * quad + (e & 3)] != doc) z[e >> 2][e & 3] = -INFINITY;
     }
     float big = -INFINITY;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) big = fmaxf(big, z[e >> 2][e & 3]);
+    for (int e = 0; e < 8; e += 2) big = max3(big, z[e >> 2][e & 3], z[e >> 2][(e & 3) + 1]);
     big *= unit;
     if (__ballot(big > m + kSlack)) {
       big = fmaxf(big, __shfl_xor(big, 16));
@@ -692,8 +718,8 @@ __global__ __launch_bounds__(kThreads) void attend_few_kernel(const AttendParams
           __builtin_amdgcn_exp2f(__builtin_fmaf(z[e >> 2][e & 3], unit, -base));
       const float p1 =
           __builtin_amdgcn_exp2f(__builtin_fmaf(z[e >> 2][(e & 3) + 1], unit, -base));
-      l += p0 + p1;
       const auto two = pack2<kType>(p0, p1);
+      l = add2<kType>(two, l);
       pf[e] = two[0];
       pf[e + 1] = two[1];
     }
@@ -713,7 +739,7 @@ __global__ __launch_bounds__(kThreads) void attend_few_kernel(const AttendParams
   l += __shfl_xor(l, 16);
   l += __shfl_xor(l, 32);
   __syncthreads();  // the tiles are done with
-  float *sums = reinterpret_cast<float *>(&tile[0][0][0][0]);  // [kWaves][16][kD]
+  float *sums = reinterpret_cast<float *>(&tile[0][0][0][0]);  // [kFewWaves][16][kD]
   if (quad == 0) {
     s_m[wave][col] = m;
     s_l[wave][col] = l;
@@ -722,14 +748,15 @@ __global__ __launch_bounds__(kThreads) void attend_few_kernel(const AttendParams
   for (int b = 0; b < kBlocks; ++b)
     *reinterpret_cast<f32x4 *>(sums + (wave * 16 + col) * kD + b * 16 + quad * 4) = acc[b];
   __syncthreads();
-  const int r = threadIdx.x >> 4, c0 = threadIdx.x & 15;  // 16 threads a row
+  constexpr int kLanes = kFewWaves * 4;  // threads of a row
+  const int r = threadIdx.x / kLanes, c0 = threadIdx.x % kLanes;
   const int mine = rt * 16 + r;
   float top = -INFINITY;
 #pragma unroll
-  for (int w = 0; w < kWaves; ++w) top = fmaxf(top, s_m[w][r]);
-  float f[kWaves], total = 0.0f;
+  for (int w = 0; w < kFewWaves; ++w) top = fmaxf(top, s_m[w][r]);
+  float f[kFewWaves], total = 0.0f;
 #pragma unroll
-  for (int w = 0; w < kWaves; ++w) {
+  for (int w = 0; w < kFewWaves; ++w) {
     f[w] = s_m[w][r] == top ? 1.0f : __builtin_amdgcn_exp2f(s_m[w][r] - top);
     total += f[w] * s_l[w][r];
   }
@@ -741,18 +768,22 @@ __global__ __launch_bounds__(kThreads) void attend_few_kernel(const AttendParams
   E *o = static_cast<E *>(P.out) + orow * P.out_stride + ohead * P.out_head;
   bool fine = true;
 #pragma unroll
-  for (int b = 0; b < kD / 16; ++b) {
-    const int c = b * 16 + c0;
-    float v = 0.0f;
+  for (int b = 0; b < kD / 4 / kLanes; ++b) {
+    const int c = (b * kLanes + c0) * 4;
+    f32x4 v = {};
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) v += f[w] * sums[(w * 16 + r) * kD + c];
+    for (int w = 0; w < kFewWaves; ++w)
+      v += f[w] * *reinterpret_cast<const f32x4 *>(sums + (w * 16 + r) * kD + c);
     if (mine < rows && c < P.d) {
       if (P.splits == 1) {
-        v = total == 0.0f ? 0.0f : v / total;
-        fine = fine && fabsf(v) < INFINITY;
-        o[c] = static_cast<E>(v);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          v[q] = total == 0.0f ? 0.0f : v[q] / total;
+          fine = fine && fabsf(v[q]) < INFINITY;
+        }
+        *reinterpret_cast<V4 *>(o + c) = __builtin_convertvector(v, V4);
       } else {
-        part[c] = v;
+        *reinterpret_cast<f32x4 *>(part + c) = v;
       }
     }
   }
@@ -764,9 +795,9 @@ __global__ __launch_bounds__(kThreads) void attend_few_kernel(const AttendParams
     return;
   }
   for (uint64_t bad = __ballot(!fine); bad;) {
-    const int w = __builtin_ctzll(bad) >> 4;  // row of the wave
-    bad &= ~(0xFFFFull << (16 * w));
-    const int rr = rt * 16 + wave * 4 + w;
+    const int w = __builtin_ctzll(bad) / kLanes;  // row of the wave
+    bad &= ~(((1ull << kLanes) - 1) << (kLanes * w));
+    const int rr = rt * 16 + wave * (64 / kLanes) + w;
     strict_row<kType>(P, s, rr / P.group, kvh * P.group + rr % P.group);
   }
 }
@@ -793,17 +824,40 @@ __global__ __launch_bounds__(kThreads) void join_kernel(const AttendParams P) {
   const int n = min(max((end + P.chunk - 1) / P.chunk, 1), P.splits);
   const int64_t flat = (int64_t(s.q0) + i) * P.n_heads + head;
   const int64_t all_rows = int64_t(P.n_q_rows) * P.n_heads;
-  float top = -INFINITY;
-  for (int k = lane; k < n; k += 64) top = fmaxf(top, P.part_ml[(k * all_rows + flat) * 2]);
-  top = wave_max(top);
-  float total = 0.0f, sum[TG_ATTEND_MAX_D / 64] = {};
-  for (int k = 0; k < n; ++k) {
-    const float pm = P.part_ml[(k * all_rows + flat) * 2];
-    const float f = pm == top ? 1.0f : __builtin_amdgcn_exp2f(pm - top);
-    total += f * P.part_ml[(k * all_rows + flat) * 2 + 1];
+  // lane k has part k, 64 parts at a time; their sums are taken 8 at a time
+  float top = -INFINITY, total = 0.0f, sum[TG_ATTEND_MAX_D / 64] = {};
+  for (int k0 = 0; k0 < n; k0 += 64) {
+    float pm = -INFINITY, pl = 0.0f;
+    if (k0 + lane < n) {
+      pm = P.part_ml[((k0 + lane) * all_rows + flat) * 2];
+      pl = P.part_ml[((k0 + lane) * all_rows + flat) * 2 + 1];
+    }
+    const float to = fmaxf(top, wave_max(pm));
+    const float fix = top == to ? 1.0f : __builtin_amdgcn_exp2f(top - to);
+    const float f = pm == to ? 1.0f : __builtin_amdgcn_exp2f(pm - to);
+    top = to;
+    total = total * fix + wave_sum(f * pl);
 #pragma unroll
-    for (int c = 0; c < TG_ATTEND_MAX_D / 64; ++c)
-      if (lane + 64 * c < P.d) sum[c] += f * P.part[(k * all_rows + flat) * P.d + lane + 64 * c];
+    for (int c = 0; c < TG_ATTEND_MAX_D / 64; ++c) sum[c] *= fix;
+    const int here = min(64, n - k0);
+    for (int k = 0; k < here; k += 8) {
+      float v[8][TG_ATTEND_MAX_D / 64];
+#pragma unroll
+      for (int u = 0; u < 8; ++u)
+#pragma unroll
+        for (int c = 0; c < TG_ATTEND_MAX_D / 64; ++c) {
+          v[u][c] = 0.0f;
+          if (k + u < here && lane + 64 * c < P.d)
+            v[u][c] = P.part[((k0 + k + u) * all_rows + flat) * P.d + lane + 64 * c];
+        }
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        const float w = __shfl(f, (k + u) & 63);
+#pragma unroll
+        for (int c = 0; c < TG_ATTEND_MAX_D / 64; ++c)
+          if (k + u < here) sum[c] += w * v[u][c];
+      }
+    }
   }
   E *o = static_cast<E *>(P.out) + (int64_t(s.q0) + i) * P.out_stride + head * P.out_head;
   bool fine = true;
@@ -849,7 +903,7 @@ int launch(const AttendParams &P, const Split &sp, hipStream_t s) {
     const int64_t blocks = int64_t(P.n_seqs) * P.n_kv_heads * sp.row_tiles * sp.splits;
     if (blocks > INT32_MAX) return TG_E_INVAL;
     hipLaunchKernelGGL((attend_few_kernel<kType, kD>), dim3(static_cast<uint32_t>(blocks)),
-                       dim3(kThreads), 0, s, P);
+                       dim3(kFewWaves * 64), 0, s, P);
     if (sp.splits > 1) {
       const int64_t waves = int64_t(P.n_seqs) * P.n_kv_heads * sp.row_tiles * 16;
       hipLaunchKernelGGL(join_kernel<kType>, dim3(static_cast<uint32_t>((waves + 3) / 4)),

@@ -79,6 +79,14 @@ __device__ __forceinline__ void load_lds(__amdgpu_buffer_rsrc_t r, void *to, uin
       16, offset, base, 0, 0);
 }
 
+// The same with 4 bytes per lane, to `to` + 4 * lane.
+__device__ __forceinline__ void load_lds4(__amdgpu_buffer_rsrc_t r, void *to, uint32_t offset) {
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(
+      r, reinterpret_cast<__attribute__((address_space(3))) void *>(
+             reinterpret_cast<uintptr_t>(to)),
+      4, offset, 0, 0, 0);
+}
+
 // Waits until at most `left` of the wave's loads are under way.
 template <int left = 0>
 __device__ __forceinline__ void wait_loads() {
