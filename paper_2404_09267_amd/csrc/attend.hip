@@ -61,9 +61,10 @@ struct AttendParams {
   int64_t n_k_rows;
   int32_t max_q, max_kv, n_heads, n_kv_heads, group, d;
   // attend_few_kernel
-  int32_t row_tiles, splits, chunk;
-  float *part;      // [splits][n_q_rows * n_heads][d] weighted sums, then
-  float *part_ml;   // [splits][n_q_rows * n_heads][2] maximum (log2 units) and sum
+  int32_t row_tiles;
+  int32_t width;    // parts that all keys are cut into, 0: no sequence is cut
+  float *part;      // [width + n_seqs][n_kv_heads][16 row_tiles][d] weighted sums, and
+  float *part_ml;   // [..][..][..][2] maximum (log2 units) and sum of weights
 };
 
 struct Seq {
@@ -159,7 +160,7 @@ __device__ __forceinline__ int abs_diff(int a, int b) { return a > b ? a - b : b
 
 // One query row of one head, by one wave, unseen keys left out one by one.
 template <int kType>
-__device__ __attribute__((noinline)) void strict_row(const AttendParams &P, const Seq &s, int i,
+__device__ __forceinline__ void strict_row(const AttendParams &P, const Seq &s, int i,
                                                      int head) {
   typedef typename Num<kType>::E E;
   const int lane = threadIdx.x & 63;
@@ -587,10 +588,70 @@ __global__ __launch_bounds__(kThreads, 2) void attend_tile_kernel(const AttendPa
 
 // ------------------------------------------------------------------------ few queries
 
+// How the keys of all sequences are cut: parts of one length, so that every workgroup has as much
+// to read, whatever the lengths are. A wave works it out; the host knows bounds only.
+constexpr int kMaxCut = 256;   // sequences, where any is cut
+constexpr int kMinPart = 128;  // keys of a part
+
+struct Parts {
+  int chunk;   // keys of a part
+  int seq;     // the sequence asked for, -1: there is none
+  int first;   // its first part
+  int count;   // its parts
+};
+
+// `part` >= 0: the sequence that has it; otherwise sequence `seq`.
+__device__ __forceinline__ Parts find_parts(const AttendParams &P, int part, int seq) {
+  const int lane = threadIdx.x & 63;
+  constexpr int kEach = kMaxCut / 64;
+  int nk[kEach];
+  int64_t total = 0;
+#pragma unroll
+  for (int u = 0; u < kEach; ++u) {
+    nk[u] = -1;  // no queries: no part
+    if (u * 64 + lane < P.n_seqs) {
+      const Seq s = sequence(P, u * 64 + lane);
+      if (s.nq > 0) nk[u] = s.nk;
+    }
+    total += max(nk[u], 0);
+  }
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) total += __shfl_xor(total, o);
+  Parts r = {kMinPart, -1, 0, 0};
+  const int64_t even = ((total + P.width - 1) / P.width + 63) / 64 * 64;
+  if (even > r.chunk) r.chunk = static_cast<int>(even);
+  int before = 0;
+#pragma unroll
+  for (int u = 0; u < kEach; ++u) {
+    const int mine = nk[u] < 0 ? 0 : max((nk[u] + r.chunk - 1) / r.chunk, 1);
+    int upto = mine;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int v = __shfl_up(upto, o);
+      if (lane >= o) upto += v;
+    }
+    const uint64_t at = part >= 0 ? __ballot(before + upto > part)
+                                  : (seq >= u * 64 && seq < u * 64 + 64 ? 1ull << (seq & 63) : 0);
+    if (at && r.seq < 0) {
+      const int l = __builtin_ctzll(at);
+      r.seq = u * 64 + l;
+      r.count = __shfl(mine, l);
+      r.first = before + __shfl(upto, l) - r.count;
+    }
+    before += __shfl(upto, 63);
+  }
+  r.seq = __builtin_amdgcn_readfirstlane(r.seq);
+  r.first = __builtin_amdgcn_readfirstlane(r.first);
+  r.count = __builtin_amdgcn_readfirstlane(r.count);
+  r.chunk = __builtin_amdgcn_readfirstlane(r.chunk);
+  return r;
+}
+
 // Rows of a workgroup: 16 (query, head) pairs that share a key head, query-major. Each of its two
 // waves takes every second 32 keys of the workgroup's range through LDS of its own; two waves, so
 // that several workgroups fit a CU and one's start and end fall into another's loads.
 constexpr int kFewWaves = 2;
+constexpr int kFewWorkgroups = 1024;  // that the keys are cut for
 
 template <int kType, int kD>
 __global__ __launch_bounds__(kFewWaves * 64) void attend_few_kernel(const AttendParams P) {
@@ -610,19 +671,23 @@ __global__ __launch_bounds__(kFewWaves * 64) void attend_few_kernel(const Attend
   id /= P.n_kv_heads;
   const int rt = id % P.row_tiles;
   id /= P.row_tiles;
-  const int split = id % P.splits, si = id / P.splits;
-  const Seq s = sequence(P, si);
+  Parts parts = {0, id, id, 1};
+  if (P.width > 0) {
+    parts = find_parts(P, id, -1);
+    if (parts.seq < 0) return;
+  }
+  const Seq s = sequence(P, parts.seq);
   const int rows = s.nq * P.group;
   if (rt * 16 >= rows) return;
-  const int from = split * P.chunk;
+  const int from = (id - parts.first) * parts.chunk;
   const int my = rt * 16 + col;  // this lane's row
   const bool live = my < rows;
   const int i = (live ? my : rows - 1) / P.group;
   const int head = kvh * P.group + (live ? my : rows - 1) % P.group;
-  const int end = min(from + P.chunk, key_limit(P, s, (min(rt * 16 + 16, rows) - 1) / P.group));
+  int end = key_limit(P, s, (min(rt * 16 + 16, rows) - 1) / P.group);
+  if (parts.count > 1) end = min(end, from + parts.chunk);
   const int all = key_limit(P, s, rt * 16 / P.group);
   const int64_t row = int64_t(s.q0) + i;
-  if (split > 0 && from >= end) return;  // join_kernel knows
   const void *kb = static_cast<const E *>(P.k) + kvh * P.k_head;
   const void *vb = static_cast<const E *>(P.v) + kvh * P.v_head;
   auto fetch = [&](int j0, int to) {
@@ -762,9 +827,8 @@ __global__ __launch_bounds__(kFewWaves * 64) void attend_few_kernel(const Attend
   }
   const int64_t orow = int64_t(s.q0) + min(mine, rows - 1) / P.group;
   const int ohead = kvh * P.group + min(mine, rows - 1) % P.group;
-  const int64_t flat = orow * P.n_heads + ohead;
-  const int64_t all_rows = int64_t(P.n_q_rows) * P.n_heads;
-  float *part = P.part + (split * all_rows + flat) * P.d;
+  const int64_t flat = (int64_t(id) * P.n_kv_heads + kvh) * P.row_tiles * 16 + mine;
+  float *part = P.part + flat * P.d;
   E *o = static_cast<E *>(P.out) + orow * P.out_stride + ohead * P.out_head;
   bool fine = true;
 #pragma unroll
@@ -775,7 +839,7 @@ __global__ __launch_bounds__(kFewWaves * 64) void attend_few_kernel(const Attend
     for (int w = 0; w < kFewWaves; ++w)
       v += f[w] * *reinterpret_cast<const f32x4 *>(sums + (w * 16 + r) * kD + c);
     if (mine < rows && c < P.d) {
-      if (P.splits == 1) {
+      if (parts.count == 1) {
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
           v[q] = total == 0.0f ? 0.0f : v[q] / total;
@@ -787,10 +851,10 @@ __global__ __launch_bounds__(kFewWaves * 64) void attend_few_kernel(const Attend
       }
     }
   }
-  if (P.splits > 1) {
+  if (parts.count > 1) {
     if (mine < rows && c0 == 0) {
-      P.part_ml[(split * all_rows + flat) * 2] = top;
-      P.part_ml[(split * all_rows + flat) * 2 + 1] = total;
+      P.part_ml[flat * 2] = top;
+      P.part_ml[flat * 2 + 1] = total;
     }
     return;
   }
@@ -814,23 +878,21 @@ __global__ __launch_bounds__(kThreads) void join_kernel(const AttendParams P) {
   const int kvh = static_cast<int>(id % P.n_kv_heads);
   const int si = static_cast<int>(id / P.n_kv_heads);
   if (si >= P.n_seqs) return;
+  const Parts parts = find_parts(P, -1, si);
   const Seq s = sequence(P, si);
   const int rows = s.nq * P.group;
-  if (my >= rows) return;
+  if (my >= rows || parts.count <= 1) return;
   const int i = my / P.group, head = kvh * P.group + my % P.group;
-  // the splits that attend_few_kernel ran for this row's tile
-  const int rt = my / 16;
-  const int end = key_limit(P, s, (min(rt * 16 + 16, rows) - 1) / P.group);
-  const int n = min(max((end + P.chunk - 1) / P.chunk, 1), P.splits);
-  const int64_t flat = (int64_t(s.q0) + i) * P.n_heads + head;
-  const int64_t all_rows = int64_t(P.n_q_rows) * P.n_heads;
+  const int n = parts.count;
+  const int64_t step = int64_t(P.n_kv_heads) * per;  // rows of a part
+  const int64_t flat = (int64_t(parts.first) * P.n_kv_heads + kvh) * per + my;
   // lane k has part k, 64 parts at a time; their sums are taken 8 at a time
   float top = -INFINITY, total = 0.0f, sum[TG_ATTEND_MAX_D / 64] = {};
   for (int k0 = 0; k0 < n; k0 += 64) {
     float pm = -INFINITY, pl = 0.0f;
     if (k0 + lane < n) {
-      pm = P.part_ml[((k0 + lane) * all_rows + flat) * 2];
-      pl = P.part_ml[((k0 + lane) * all_rows + flat) * 2 + 1];
+      pm = P.part_ml[((k0 + lane) * step + flat) * 2];
+      pl = P.part_ml[((k0 + lane) * step + flat) * 2 + 1];
     }
     const float to = fmaxf(top, wave_max(pm));
     const float fix = top == to ? 1.0f : __builtin_amdgcn_exp2f(top - to);
@@ -848,7 +910,7 @@ __global__ __launch_bounds__(kThreads) void join_kernel(const AttendParams P) {
         for (int c = 0; c < TG_ATTEND_MAX_D / 64; ++c) {
           v[u][c] = 0.0f;
           if (k + u < here && lane + 64 * c < P.d)
-            v[u][c] = P.part[((k0 + k + u) * all_rows + flat) * P.d + lane + 64 * c];
+            v[u][c] = P.part[((k0 + k + u) * step + flat) * P.d + lane + 64 * c];
         }
 #pragma unroll
       for (int u = 0; u < 8; ++u) {
@@ -873,42 +935,37 @@ __global__ __launch_bounds__(kThreads) void join_kernel(const AttendParams P) {
 
 // ------------------------------------------------------------------------------- the host
 
-// How few queries are split: `few` when a key head's rows fit a few 16-row tiles.
-struct Split {
-  bool few;
-  int row_tiles, splits, chunk;
+// The form for few queries: 16-row tiles of a key head's rows, and into how many parts the keys
+// of all sequences are cut.
+struct Few {
+  bool use;
+  int row_tiles, width;
 };
 
-Split split_of(int n_seqs, int max_q, int max_kv, int n_heads, int n_kv_heads) {
-  Split r = {};
+Few few_of(int n_seqs, int max_q, int max_kv, int n_heads, int n_kv_heads) {
+  Few r = {};
   const int64_t rows = int64_t(max_q) * (n_heads / n_kv_heads);
-  r.few = rows <= 64;
-  if (!r.few) return r;
+  r.use = rows <= 64;
+  if (!r.use) return r;
   r.row_tiles = static_cast<int>((rows + 15) / 16);
-  const int64_t blocks = int64_t(n_seqs) * n_kv_heads * r.row_tiles;
-  const int64_t want = (1024 + blocks - 1) / blocks;
-  const int64_t most = (int64_t(max_kv) + 255) / 256;
-  r.splits = static_cast<int>(want < most ? want : most);
-  if (r.splits < 1) r.splits = 1;
-  r.chunk = static_cast<int>(((int64_t(max_kv) + r.splits - 1) / r.splits + 127) / 128 * 128);
-  if (r.chunk < 128) r.chunk = 128;
-  r.splits = static_cast<int>((int64_t(max_kv) + r.chunk - 1) / r.chunk);
-  if (r.splits < 1) r.splits = 1;
+  const int64_t each = int64_t(n_kv_heads) * r.row_tiles;
+  const int64_t want = kFewWorkgroups;
+  if (n_seqs <= kMaxCut && n_seqs * each < want && max_kv > 2 * kMinPart)
+    r.width = static_cast<int>((want + each - 1) / each);
   return r;
 }
 
 template <int kType, int kD>
-int launch(const AttendParams &P, const Split &sp, hipStream_t s) {
-  if (sp.few) {
-    const int64_t blocks = int64_t(P.n_seqs) * P.n_kv_heads * sp.row_tiles * sp.splits;
-    if (blocks > INT32_MAX) return TG_E_INVAL;
+int launch(const AttendParams &P, const Few &few, hipStream_t s) {
+  if (few.use) {
+    const int64_t blocks = (int64_t(P.n_seqs) + P.width) * P.n_kv_heads * P.row_tiles;
+    const int64_t waves = int64_t(P.n_seqs) * P.n_kv_heads * P.row_tiles * 16;
+    if (blocks > INT32_MAX || waves > INT32_MAX) return TG_E_INVAL;
     hipLaunchKernelGGL((attend_few_kernel<kType, kD>), dim3(static_cast<uint32_t>(blocks)),
                        dim3(kFewWaves * 64), 0, s, P);
-    if (sp.splits > 1) {
-      const int64_t waves = int64_t(P.n_seqs) * P.n_kv_heads * sp.row_tiles * 16;
+    if (P.width > 0)
       hipLaunchKernelGGL(join_kernel<kType>, dim3(static_cast<uint32_t>((waves + 3) / 4)),
                          dim3(kThreads), 0, s, P);
-    }
   } else {
     const int64_t blocks = (int64_t(P.n_q_rows) / kBM + P.n_seqs) * P.n_heads;
     if (blocks > INT32_MAX) return TG_E_INVAL;
@@ -945,9 +1002,10 @@ extern "C" size_t tg_attend_workspace_bytes(int32_t n_seqs, int32_t n_q_rows, in
                                             int32_t n_kv_heads, int32_t d) {
   if (!sizes_ok(n_seqs, n_q_rows, max_q_len, max_kv_len, n_heads, n_kv_heads, d)) return 0;
   if (n_seqs == 0 || n_q_rows == 0 || max_q_len == 0) return 0;
-  const Split sp = split_of(n_seqs, max_q_len, max_kv_len, n_heads, n_kv_heads);
-  if (!sp.few || sp.splits == 1) return 0;
-  return static_cast<size_t>(sp.splits) * n_q_rows * n_heads * (d + 2) * sizeof(float);
+  const Few few = few_of(n_seqs, max_q_len, max_kv_len, n_heads, n_kv_heads);
+  if (!few.use || few.width == 0) return 0;
+  return (static_cast<size_t>(few.width) + n_seqs) * n_kv_heads * few.row_tiles * 16 * (d + 2) *
+         sizeof(float);
 }
 
 extern "C" int tg_attend(const tg_attend_args *a, void *stream) {
@@ -966,7 +1024,7 @@ extern "C" int tg_attend(const tg_attend_args *a, void *stream) {
   if (a->n_k_rows > 0 && (!layout_ok(a->k, a->k_stride, a->k_head_stride) ||
                           !layout_ok(a->v, a->v_stride, a->v_head_stride)))
     return TG_E_INVAL;
-  const Split sp = split_of(a->n_seqs, a->max_q_len, a->max_kv_len, a->n_heads, a->n_kv_heads);
+  const Few few = few_of(a->n_seqs, a->max_q_len, a->max_kv_len, a->n_heads, a->n_kv_heads);
   const size_t need = tg_attend_workspace_bytes(a->n_seqs, a->n_q_rows, a->max_q_len,
                                                 a->max_kv_len, a->n_heads, a->n_kv_heads, a->d);
   if (need > 0 && (!a->workspace || a->workspace_bytes < need || !aligned16(a->workspace)))
@@ -1012,13 +1070,13 @@ extern "C" int tg_attend(const tg_attend_args *a, void *stream) {
   P.n_kv_heads = a->n_kv_heads;
   P.group = a->n_heads / a->n_kv_heads;
   P.d = a->d;
-  P.row_tiles = sp.row_tiles;
-  P.splits = sp.splits;
-  P.chunk = sp.chunk;
+  P.row_tiles = few.row_tiles;
+  P.width = few.width;
   P.part = static_cast<float *>(a->workspace);
-  P.part_ml = P.part + static_cast<size_t>(sp.splits) * a->n_q_rows * a->n_heads * a->d;
+  P.part_ml = P.part + (static_cast<size_t>(few.width) + a->n_seqs) * a->n_kv_heads *
+                           few.row_tiles * 16 * a->d;
   hipStream_t s = static_cast<hipStream_t>(stream);
   if (a->d <= 64)
-    return a->type == TG_F16 ? launch<TG_F16, 64>(P, sp, s) : launch<TG_BF16, 64>(P, sp, s);
-  return a->type == TG_F16 ? launch<TG_F16, 128>(P, sp, s) : launch<TG_BF16, 128>(P, sp, s);
+    return a->type == TG_F16 ? launch<TG_F16, 64>(P, few, s) : launch<TG_BF16, 64>(P, few, s);
+  return a->type == TG_F16 ? launch<TG_F16, 128>(P, few, s) : launch<TG_BF16, 128>(P, few, s);
 }
