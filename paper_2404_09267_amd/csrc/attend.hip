@@ -444,6 +444,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_tile_kernel(const AttendPa
                 tk[buf] + r * kD + place_of<kChunks, false>(r, 2 * k + half) * 8);
             z[b] = N::mfma32(kf, qf[k], z[b]);
           }
+        __builtin_amdgcn_s_setprio(1);  // a wave that is at its exponentials goes first
         const bool edge = j0 + kBN > all;  // some query does not see some key, documents aside
         // A weight is 2^(z factor - (m - shift)): what is left of a score's way to log2 units,
         // and what all of a lane's scores of the tile have in common.
@@ -529,6 +530,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_tile_kernel(const AttendPa
             for (int r = 0; r < 16; ++r) acc[b][r] *= fix;
         }
         const float base = shift - (m == -INFINITY ? 0.0f : m);
+        __builtin_amdgcn_s_setprio(0);
 #pragma unroll
         for (int k = 0; k < 4; ++k) {  // 16 keys
           V8 pf;

@@ -312,7 +312,7 @@ __device__ __forceinline__ void add_gathered(const ProjectParams &P, int t0, int
 
 // One result from the formula.
 template <int kType>
-__device__ __attribute__((noinline)) float strict_value(const void *x, const void *w, int k,
+__device__ __forceinline__ float strict_value(const void *x, const void *w, int k,
                                                         const float *h, const void *b, int rank) {
   typedef typename Num<kType>::E E;
   float sum = 0.0f;
@@ -422,11 +422,12 @@ __device__ __forceinline__ void store(const ProjectParams &P, int t0, int n0,
 // loads under way. Step s + 1's operands are read from LDS while step s's are multiplied, so
 // that the matrix units have work across the barrier; the buffer of step s is free for step
 // s + kStages behind that barrier, since its operands are in registers by then.
-// Rows of a tile lie in LDS as kBK / 8 chunks of 16 bytes, and the 16 rows that an operand takes
-// one chunk of fall on 16 different places of the 256 bytes that LDS serves at once.
+// Rows of a tile lie in LDS as kBK / 8 chunks of 16 bytes, in an order that serves the operands'
+// reads (one chunk of 16 rows) best: 156 bytes a cycle and CU measured with rows of 64 and 146
+// with rows of 32, where (row / 4) in the place of (row / 2) gives 116 and no change of order 123.
 template <int kBK>
 __device__ __forceinline__ int place_of(int row, int c) {
-  return kBK == 64 ? c ^ ((row >> 1) & 7) : c ^ ((row >> 2) & 3);
+  return c ^ ((row >> 1) & (kBK / 8 - 1));
 }
 
 // Which tile a workgroup takes: workgroups go round the 8 XCDs, so each XCD gets a run of tiles
@@ -722,12 +723,22 @@ int launch(ProjectParams P, const Few &few, hipStream_t s) {
     return hipGetLastError() == hipSuccess ? TG_OK : TG_E_HIP;
   }
   if (P.adapter) launch_shrink<kType>(P, s);
-  const int64_t big = ((int64_t(P.n_tokens) + 255) / 256) * ((P.n + 255) / 256);
-  const int64_t mid = ((int64_t(P.n_tokens) + 127) / 128) * ((P.n + 127) / 128);
+  // The largest tile of which there are enough: it reads the least for its products. Measured
+  // (bfloat16, no adapters), as tiles x tiles of 256, 128, 128 with 8 waves, 128 x 64 and 64:
+  //   25,600 x 4,096, k 4,096: 742, 759, 870, 996, 1247 us
+  //    2,048 x 4,096, k 4,096:  87,  61,  69,  77,   96
+  //    1,777 x 2,048, k 1,160:  41,  21,  18,  21,   25
+  //      512 x 4,096, k 4,096:  84,  43,  32,  25,   27
+  //      256 x 2,048, k 2,048:  46,  20,  19,  14,   11
+  const auto tiles = [&](int t, int n) {
+    return ((int64_t(P.n_tokens) + t - 1) / t) * ((int64_t(P.n) + n - 1) / n);
+  };
   P.gather = P.adapter && P.b_step == 1;  // rows of b that a load to LDS cannot take
   if (P.gather) rc = launch_tiles<kType, 64, 64, 2, 2, 64, 4>(P, s);
-  else if (big >= 1024) rc = launch_tiles<kType, 256, 256, 2, 4, 32, 4>(P, s);
-  else if (mid >= 256) rc = launch_tiles<kType, 128, 128, 2, 2, 64, 2>(P, s);
+  else if (tiles(256, 256) >= 1024) rc = launch_tiles<kType, 256, 256, 4, 2, 32, 4>(P, s);
+  else if (tiles(128, 128) >= 256) rc = launch_tiles<kType, 128, 128, 2, 2, 64, 2>(P, s);
+  else if (tiles(128, 128) >= 192) rc = launch_tiles<kType, 128, 128, 2, 4, 64, 4>(P, s);
+  else if (tiles(128, 64) >= 256) rc = launch_tiles<kType, 128, 64, 2, 2, 64, 3>(P, s);
   else rc = launch_tiles<kType, 64, 64, 2, 2, 64, 4>(P, s);
   if (rc != TG_OK) return rc;
   return hipGetLastError() == hipSuccess ? TG_OK : TG_E_HIP;
