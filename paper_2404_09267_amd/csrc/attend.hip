@@ -286,7 +286,7 @@ enum Mode {
 };
 
 template <int kType, int kD, int kMode>
-__global__ __launch_bounds__(kThreads, 2) void attend_tile_kernel(const AttendParams P) {
+__global__ __launch_bounds__(kThreads, kD == 64 ? 3 : 2) void attend_tile_kernel(const AttendParams P) {
   typedef Num<kType> N;
   typedef typename N::E E;
   typedef typename N::V4 V4;
@@ -297,6 +297,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_tile_kernel(const AttendPa
   constexpr bool kAnyMode = kMode == kAny;
   __shared__ int s_doc[2][kAnyMode ? kBN : 1];
   __shared__ int s_pos[2][2][kAnyMode ? kBN : 1];
+  __shared__ float s_far[kWaves][2][kAnyMode ? kBN : 1];  // a wave's keys' places, times the slope
   __shared__ uint64_t s_use[kAnyMode ? kMaskTiles / 64 : 1];
   __shared__ int s_range[kWaves][2];
   const bool with_docs = kAnyMode && P.k_doc, with_pos = kAnyMode && P.k_pos;
@@ -341,6 +342,9 @@ __global__ __launch_bounds__(kThreads, 2) void attend_tile_kernel(const AttendPa
     px = P.q_pos[2 * row];
     py = P.q_pos[2 * row + 1];
   }
+  const int x0 = __builtin_amdgcn_readfirstlane(px), y0 = __builtin_amdgcn_readfirstlane(py);
+  const float steep = fabsf(slope2);
+  const float fx = static_cast<float>(px - x0) * steep, fy = static_cast<float>(py - y0) * steep;
   int wave_lo = INT_MAX, wave_hi = -1;  // the documents of the wave's queries
   int block_lo = INT_MAX, block_hi = -1;
   if (with_docs) {
@@ -474,9 +478,13 @@ __global__ __launch_bounds__(kThreads, 2) void attend_tile_kernel(const AttendPa
                   -slope2 * fabsf(here - static_cast<float>((e >> 2) * 8 + (e & 3))));
           }
         } else {
+          // what brings a score to log2 units: here, with the bias, or with the weight
+          float scale = 1.0f;
           if (P.capped) {
 #pragma unroll
             for (int e = 0; e < 32; ++e) z[e >> 4][e & 15] = cap_score(P, z[e >> 4][e & 15]);
+          } else if (P.slope) {
+            scale = P.to_log2;
           } else if (P.shaped) {
 #pragma unroll
             for (int e = 0; e < 32; ++e) z[e >> 4][e & 15] *= P.to_log2;
@@ -488,16 +496,32 @@ __global__ __launch_bounds__(kThreads, 2) void attend_tile_kernel(const AttendPa
 #pragma unroll
             for (int e = 0; e < 32; ++e)
               z[e >> 4][e & 15] = __builtin_fmaf(
-                  -slope2, fabsf(here - static_cast<float>((e >> 2) * 8 + (e & 3))),
-                  z[e >> 4][e & 15]);
+                  z[e >> 4][e & 15], scale,
+                  -slope2 * fabsf(here - static_cast<float>((e >> 2) * 8 + (e & 3))));
           } else if (P.slope) {
+            float tmp[32];
+            // both places from the wave's first query on, times |slope|: two subtractions and two
+            // additions a score
+            s_far[wave][0][lane] = static_cast<float>(s_pos[buf][0][lane] - x0) * steep;
+            s_far[wave][1][lane] = static_cast<float>(s_pos[buf][1][lane] - y0) * steep;
+            __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+            __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+            const float sign = slope2 < 0.0f ? 1.0f : -1.0f;
 #pragma unroll
-            for (int e = 0; e < 32; ++e) {
-              const int j = (e >> 2) * 8 + 4 * half + (e & 3);
-              const int far = abs_diff(px, s_pos[buf][0][j]) + abs_diff(py, s_pos[buf][1][j]);
-              z[e >> 4][e & 15] =
-                  __builtin_fmaf(-slope2, static_cast<float>(far), z[e >> 4][e & 15]);
+            for (int e = 0; e < 32; e += 4) {
+              const int j = (e >> 2) * 8 + 4 * half;
+              const f32x4 kx = *reinterpret_cast<const f32x4 *>(&s_far[wave][0][j]);
+              const f32x4 ky = *reinterpret_cast<const f32x4 *>(&s_far[wave][1][j]);
+#pragma unroll
+              for (int r = 0; r < 4; ++r) {
+                float &ze = tmp[e + r];
+                ze = __builtin_fmaf(z[e >> 4][(e & 15) + r], scale, sign * fabsf(kx[r] - fx));
+                ze = __builtin_fmaf(sign, fabsf(ky[r] - fy), ze);
+              }
             }
+#pragma unroll
+            for (int e = 0; e < 32; ++e) z[e >> 4][e & 15] = tmp[e];
           }
         }
         // a factor < 0 turns the order round
@@ -600,6 +624,7 @@ struct Parts {
   int seq;     // the sequence asked for, -1: there is none
   int first;   // its first part
   int count;   // its parts
+  Seq s;       // what else is known of it
 };
 
 // `part` >= 0: the sequence that has it; otherwise sequence `seq`.
@@ -607,24 +632,27 @@ __device__ __forceinline__ Parts find_parts(const AttendParams &P, int part, int
   const int lane = threadIdx.x & 63;
   constexpr int kEach = kMaxCut / 64;
   int nk[kEach];
+  Seq all[kEach];
   int64_t total = 0;
 #pragma unroll
   for (int u = 0; u < kEach; ++u) {
     nk[u] = -1;  // no queries: no part
+    if (u * 64 >= P.n_seqs) continue;
     if (u * 64 + lane < P.n_seqs) {
-      const Seq s = sequence(P, u * 64 + lane);
-      if (s.nq > 0) nk[u] = s.nk;
+      all[u] = sequence(P, u * 64 + lane);
+      if (all[u].nq > 0) nk[u] = all[u].nk;
     }
     total += max(nk[u], 0);
   }
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) total += __shfl_xor(total, o);
-  Parts r = {kMinPart, -1, 0, 0};
+  Parts r = {kMinPart, -1, 0, 0, {}};
   const int64_t even = ((total + P.width - 1) / P.width + 63) / 64 * 64;
   if (even > r.chunk) r.chunk = static_cast<int>(even);
   int before = 0;
 #pragma unroll
   for (int u = 0; u < kEach; ++u) {
+    if (u * 64 >= P.n_seqs) continue;
     const int mine = nk[u] < 0 ? 0 : max((nk[u] + r.chunk - 1) / r.chunk, 1);
     int upto = mine;
 #pragma unroll
@@ -635,10 +663,19 @@ __device__ __forceinline__ Parts find_parts(const AttendParams &P, int part, int
     const uint64_t at = part >= 0 ? __ballot(before + upto > part)
                                   : (seq >= u * 64 && seq < u * 64 + 64 ? 1ull << (seq & 63) : 0);
     if (at && r.seq < 0) {
-      const int l = __builtin_ctzll(at);
+      const int l = __builtin_amdgcn_readfirstlane(__builtin_ctzll(at));
       r.seq = u * 64 + l;
       r.count = __shfl(mine, l);
       r.first = before + __shfl(upto, l) - r.count;
+      const auto take = [&](int v) { return __builtin_amdgcn_readlane(v, l); };
+      r.s.q0 = take(all[u].q0);
+      r.s.nq = take(all[u].nq);
+      r.s.k0 = static_cast<int64_t>(
+          static_cast<uint64_t>(static_cast<uint32_t>(take(static_cast<int>(all[u].k0 >> 32)))) << 32 |
+          static_cast<uint32_t>(take(static_cast<int>(all[u].k0))));
+      r.s.nk = take(all[u].nk);
+      r.s.place0 = take(all[u].place0);
+      r.s.prefix = take(all[u].prefix);
     }
     before += __shfl(upto, 63);
   }
@@ -673,12 +710,14 @@ __global__ __launch_bounds__(kFewWaves * 64) void attend_few_kernel(const Attend
   id /= P.n_kv_heads;
   const int rt = id % P.row_tiles;
   id /= P.row_tiles;
-  Parts parts = {0, id, id, 1};
+  Parts parts = {0, id, id, 1, {}};
   if (P.width > 0) {
     parts = find_parts(P, id, -1);
     if (parts.seq < 0) return;
+  } else {
+    parts.s = sequence(P, id);
   }
-  const Seq s = sequence(P, parts.seq);
+  const Seq s = parts.s;
   const int rows = s.nq * P.group;
   if (rt * 16 >= rows) return;
   const int from = (id - parts.first) * parts.chunk;
@@ -868,71 +907,79 @@ __global__ __launch_bounds__(kFewWaves * 64) void attend_few_kernel(const Attend
   }
 }
 
-// Joins the parts of a row: one wave a row.
+// Joins the parts of a row: a workgroup a row, 32 lanes a part with 4 values each.
 template <int kType>
-__global__ __launch_bounds__(kThreads) void join_kernel(const AttendParams P) {
+__global__ __launch_bounds__(kThreads, 4) void join_kernel(const AttendParams P) {
   typedef typename Num<kType>::E E;
-  const int lane = threadIdx.x & 63;
-  const int per = P.row_tiles * 16;  // rows of a sequence and key head
-  int64_t id = int64_t(blockIdx.x) * kWaves + (threadIdx.x >> 6);
-  const int my = static_cast<int>(id % per);
-  id /= per;
-  const int kvh = static_cast<int>(id % P.n_kv_heads);
-  const int si = static_cast<int>(id / P.n_kv_heads);
-  if (si >= P.n_seqs) return;
+  typedef typename Num<kType>::V4 V4;
+  constexpr int kAtOnce = kThreads / 32;
+  __shared__ f32x4 s_sum[kAtOnce][32];
+  __shared__ float s_w[64];
+  __shared__ int s_bad;
+  const int tid = threadIdx.x, lane = tid & 63, group = tid >> 5, c = (tid & 31) * 4;
+  const int per = P.row_tiles * 16;       // rows of a sequence and key head in the parts
+  const int most = P.max_q * P.group;     // and those that may be in use
+  int id = blockIdx.x;
+  const int my = id % most;
+  id /= most;
+  const int kvh = id % P.n_kv_heads, si = id / P.n_kv_heads;
   const Parts parts = find_parts(P, -1, si);
-  const Seq s = sequence(P, si);
+  const Seq s = parts.s;
   const int rows = s.nq * P.group;
   if (my >= rows || parts.count <= 1) return;
   const int i = my / P.group, head = kvh * P.group + my % P.group;
   const int n = parts.count;
   const int64_t step = int64_t(P.n_kv_heads) * per;  // rows of a part
   const int64_t flat = (int64_t(parts.first) * P.n_kv_heads + kvh) * per + my;
-  // lane k has part k, 64 parts at a time; their sums are taken 8 at a time
-  float top = -INFINITY, total = 0.0f, sum[TG_ATTEND_MAX_D / 64] = {};
-  for (int k0 = 0; k0 < n; k0 += 64) {
+  float top = -INFINITY, total = 0.0f;
+  f32x4 sum = {};
+  for (int k0 = 0; k0 < n; k0 += 64) {  // lane k of every wave has part k's maximum and sum
     float pm = -INFINITY, pl = 0.0f;
     if (k0 + lane < n) {
       pm = P.part_ml[((k0 + lane) * step + flat) * 2];
       pl = P.part_ml[((k0 + lane) * step + flat) * 2 + 1];
+    }
+    f32x4 v[64 / kAtOnce];
+#pragma unroll
+    for (int u = 0; u < 64 / kAtOnce; ++u) {
+      const int k = k0 + u * kAtOnce + group;
+      v[u] = f32x4{};
+      if (k < n && c < P.d)
+        v[u] = *reinterpret_cast<const f32x4 *>(P.part + (k * step + flat) * P.d + c);
     }
     const float to = fmaxf(top, wave_max(pm));
     const float fix = top == to ? 1.0f : __builtin_amdgcn_exp2f(top - to);
     const float f = pm == to ? 1.0f : __builtin_amdgcn_exp2f(pm - to);
     top = to;
     total = total * fix + wave_sum(f * pl);
+    sum *= fix;
+    if (k0 > 0) __syncthreads();
+    if (tid < 64) s_w[lane] = f;
+    __syncthreads();
 #pragma unroll
-    for (int c = 0; c < TG_ATTEND_MAX_D / 64; ++c) sum[c] *= fix;
-    const int here = min(64, n - k0);
-    for (int k = 0; k < here; k += 8) {
-      float v[8][TG_ATTEND_MAX_D / 64];
-#pragma unroll
-      for (int u = 0; u < 8; ++u)
-#pragma unroll
-        for (int c = 0; c < TG_ATTEND_MAX_D / 64; ++c) {
-          v[u][c] = 0.0f;
-          if (k + u < here && lane + 64 * c < P.d)
-            v[u][c] = P.part[((k0 + k + u) * step + flat) * P.d + lane + 64 * c];
-        }
-#pragma unroll
-      for (int u = 0; u < 8; ++u) {
-        const float w = __shfl(f, (k + u) & 63);
-#pragma unroll
-        for (int c = 0; c < TG_ATTEND_MAX_D / 64; ++c)
-          if (k + u < here) sum[c] += w * v[u][c];
-      }
+    for (int u = 0; u < 64 / kAtOnce; ++u) {
+      const int k = u * kAtOnce + group;
+      if (k0 + k < n) sum += s_w[k] * v[u];
     }
   }
-  E *o = static_cast<E *>(P.out) + (int64_t(s.q0) + i) * P.out_stride + head * P.out_head;
-  bool fine = true;
+  s_sum[group][tid & 31] = sum;
+  if (tid == 0) s_bad = 0;
+  __syncthreads();
+  if (group == 0 && c < P.d) {
 #pragma unroll
-  for (int c = 0; c < TG_ATTEND_MAX_D / 64; ++c)
-    if (lane + 64 * c < P.d) {
-      const float v = total == 0.0f ? 0.0f : sum[c] / total;
-      fine = fine && fabsf(v) < INFINITY;
-      o[lane + 64 * c] = static_cast<E>(v);
+    for (int g = 1; g < kAtOnce; ++g) sum += s_sum[g][tid];
+    bool fine = true;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      sum[q] = total == 0.0f ? 0.0f : sum[q] / total;
+      fine = fine && fabsf(sum[q]) < INFINITY;
     }
-  if (__ballot(!fine)) strict_row<kType>(P, s, i, head);
+    E *o = static_cast<E *>(P.out) + (int64_t(s.q0) + i) * P.out_stride + head * P.out_head;
+    *reinterpret_cast<V4 *>(o + c) = __builtin_convertvector(sum, V4);
+    if (!fine) s_bad = 1;
+  }
+  __syncthreads();
+  if (s_bad && tid < 64) strict_row<kType>(P, s, i, head);
 }
 
 // ------------------------------------------------------------------------------- the host
@@ -961,13 +1008,13 @@ template <int kType, int kD>
 int launch(const AttendParams &P, const Few &few, hipStream_t s) {
   if (few.use) {
     const int64_t blocks = (int64_t(P.n_seqs) + P.width) * P.n_kv_heads * P.row_tiles;
-    const int64_t waves = int64_t(P.n_seqs) * P.n_kv_heads * P.row_tiles * 16;
-    if (blocks > INT32_MAX || waves > INT32_MAX) return TG_E_INVAL;
+    const int64_t joined = int64_t(P.n_seqs) * P.n_heads * P.max_q;
+    if (blocks > INT32_MAX || joined > INT32_MAX) return TG_E_INVAL;
     hipLaunchKernelGGL((attend_few_kernel<kType, kD>), dim3(static_cast<uint32_t>(blocks)),
                        dim3(kFewWaves * 64), 0, s, P);
     if (P.width > 0)
-      hipLaunchKernelGGL(join_kernel<kType>, dim3(static_cast<uint32_t>((waves + 3) / 4)),
-                         dim3(kThreads), 0, s, P);
+      hipLaunchKernelGGL(join_kernel<kType>, dim3(static_cast<uint32_t>(joined)), dim3(kThreads), 0,
+                         s, P);
   } else {
     const int64_t blocks = (int64_t(P.n_q_rows) / kBM + P.n_seqs) * P.n_heads;
     if (blocks > INT32_MAX) return TG_E_INVAL;

@@ -65,8 +65,9 @@ __device__ __forceinline__ int64_t out_row(const RotateParams &P, int which, int
   return r >= 0 && r < P.n_rows ? r : -1;
 }
 
-// d and rot multiples of 16, rows and heads on 16-byte boundaries. Lane c of a head holds
-// values 8 c .. and their partners rot / 2 later (half pairs) or the next chunk.
+// d a multiple of 16, rows and heads on 16-byte boundaries. Lane c of a head holds values 8 c ..
+// and their partners rot / 2 later (half pairs, rot a multiple of 16), or values 16 c .. where
+// pairs are neighbours.
 template <int kType, bool kInterleaved>
 __global__ __launch_bounds__(kThreads) void rotate_kernel(const RotateParams P) {
   typedef Num<kType> N;
@@ -79,8 +80,7 @@ __global__ __launch_bounds__(kThreads) void rotate_kernel(const RotateParams P) 
   const int lane = threadIdx.x & 63, sub = lane & (P.lanes - 1);
   const int step = 64 / P.lanes;
   const bool has = sub < P.d / 16;
-  const int turned = P.rot / 16;  // lanes whose chunks turn
-  const bool turns = sub < turned;
+  const bool turns = sub * 16 < P.rot;
   int c0, c1;  // first values of the two chunks
   if (kInterleaved || !turns) {
     c0 = 16 * sub;
@@ -92,7 +92,8 @@ __global__ __launch_bounds__(kThreads) void rotate_kernel(const RotateParams P) 
   float cs[8][2];
   if (turns) {
     const int pair = kInterleaved ? c0 / 2 : c0;
-    if (P.axes == 1 || (P.rot / 2) % 16 == 0) {  // the lane's 8 pairs are on one axis
+    // the lane's 8 pairs are all turned, and on one axis
+    if (P.rot % 16 == 0 && (P.axes == 1 || P.rot % 32 == 0)) {
       const f32x4 *row = reinterpret_cast<const f32x4 *>(table_row(P, t, pair));
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
@@ -102,8 +103,11 @@ __global__ __launch_bounds__(kThreads) void rotate_kernel(const RotateParams P) 
     } else {
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const float *row = table_row(P, t, pair + i);
-        cs[i][0] = row[0], cs[i][1] = row[1];
+        cs[i][0] = 1.0f, cs[i][1] = 0.0f;
+        if (2 * (pair + i) < P.rot) {
+          const float *row = table_row(P, t, pair + i);
+          cs[i][0] = row[0], cs[i][1] = row[1];
+        }
       }
     }
   } else {
@@ -256,7 +260,7 @@ extern "C" int tg_rotate(const tg_rotate_args *a, void *stream) {
   const int64_t ih[3] = {a->q_head_stride, a->k_head_stride, a->v_head_stride};
   const int64_t os[3] = {a->q_out_stride, a->k_out_stride, a->v_out_stride};
   const int64_t oh[3] = {a->q_out_head_stride, a->k_out_head_stride, a->v_out_head_stride};
-  bool vec = a->d % 16 == 0 && a->rot % 16 == 0 && aligned16(a->table) &&
+  bool vec = a->d % 16 == 0 && (a->rot % 16 == 0 || a->interleaved) && aligned16(a->table) &&
              aligned16(a->q_weight) && aligned16(a->k_weight);
   for (int i = 0; i < 3; ++i) {
     P.in[i] = in[i];
