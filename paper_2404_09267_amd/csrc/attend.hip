@@ -690,7 +690,7 @@ __device__ __forceinline__ Parts find_parts(const AttendParams &P, int part, int
 // waves takes every second 32 keys of the workgroup's range through LDS of its own; two waves, so
 // that several workgroups fit a CU and one's start and end fall into another's loads.
 constexpr int kFewWaves = 2;
-constexpr int kFewWorkgroups = 1024;  // that the keys are cut for
+constexpr int kFewWorkgroups = 1536;  // that the keys are cut for: 3 for each of the 512 places
 
 template <int kType, int kD>
 __global__ __launch_bounds__(kFewWaves * 64) void attend_few_kernel(const AttendParams P) {
