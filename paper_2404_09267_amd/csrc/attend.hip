@@ -994,10 +994,15 @@ struct Few {
 Few few_of(int n_seqs, int max_q, int max_kv, int n_heads, int n_kv_heads) {
   Few r = {};
   const int64_t rows = int64_t(max_q) * (n_heads / n_kv_heads);
-  r.use = rows <= 64;
+  const int64_t each = n_kv_heads * ((rows + 15) / 16);
+  // Up to 64 rows always; more where the keys are long and the tiles of the other form would be
+  // few, since its workgroups go over all keys one after the other. 16 heads of 128 over 4, this
+  // form against the other: 1 sequence, 32,768 keys, 64 queries 86 : 590 us, 256 queries 255 :
+  // 607; 4 sequences, 64 queries 280 : 598; 16 sequences, 64 queries 1199 : 906. 1,024 keys,
+  // 1 sequence, 64 queries 21 : 24, 128 queries 31 : 25.
+  r.use = rows <= 64 || (max_kv >= 4096 && n_seqs * each <= 256);
   if (!r.use) return r;
   r.row_tiles = static_cast<int>((rows + 15) / 16);
-  const int64_t each = int64_t(n_kv_heads) * r.row_tiles;
   const int64_t want = kFewWorkgroups;
   if (n_seqs <= kMaxCut && n_seqs * each < want && max_kv > 2 * kMinPart)
     r.width = static_cast<int>((want + each - 1) / each);

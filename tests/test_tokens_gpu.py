@@ -408,6 +408,17 @@ def test_attend_long_cache(n, q_len):
     assert torch.equal(got, run_attend(q, k, v, qb, kb, lens, 0.125, **f))
 
 
+@pytest.mark.parametrize("q_lens,kv_lens", [([40, 7, 33], [5000, 4097, 40]), ([120], [6000])])
+@pytest.mark.parametrize("kind", ["causal", "causal prefix cap slope", "docs slope pos"])
+def test_attend_tens_of_queries_over_long_keys(q_lens, kv_lens, kind):
+    """Several 16-row tiles of queries against keys that are cut into parts."""
+    say("attend tens", q_lens, kind)
+    g, q, k, v, qb, kb = make(20, q_lens, kv_lens, 4, 2, 64, "bf16")
+    f = features(kind, g, q.shape[0], k.shape[0], 4, len(q_lens), kv_lens)
+    want, bound = R.attend(q, k, v, qb, kb, kv_lens, 0.125, **f)
+    R.assert_within(run_attend(q, k, v, qb, kb, kv_lens, 0.125, **f), want, bound, "attend")
+
+
 def test_attend_many_documents():
     """More key tiles than are looked through at once, few of them seen."""
     n, d = 300000, 64
