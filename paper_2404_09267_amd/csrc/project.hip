@@ -723,20 +723,31 @@ int launch(ProjectParams P, const Few &few, hipStream_t s) {
     return hipGetLastError() == hipSuccess ? TG_OK : TG_E_HIP;
   }
   if (P.adapter) launch_shrink<kType>(P, s);
-  // The largest tile of which there are enough: it reads the least for its products. Measured
-  // (bfloat16, no adapters), as tiles x tiles of 256, 128, 128 with 8 waves, 128 x 64 and 64:
-  //   25,600 x 4,096, k 4,096: 742, 759, 870, 996, 1247 us
-  //    2,048 x 4,096, k 4,096:  87,  61,  69,  77,   96
-  //    1,777 x 2,048, k 1,160:  41,  21,  18,  21,   25
-  //      512 x 4,096, k 4,096:  84,  43,  32,  25,   27
-  //      256 x 2,048, k 2,048:  46,  20,  19,  14,   11
+  // Large problems take the tile with the least time for its rounds: 512 workgroups at once, two
+  // a CU (256 with tiles of 256 x 256), a round of 160 x 128 takes 1.25 times one of 128 x 128
+  // and one of 256 x 256 1.8 times. Fewer tiles than half a round: smaller ones. Measured
+  // (bfloat16, no adapters) with tiles of 256 x 256, 160 x 128, 128 x 128, the latter with 8 waves,
+  // 128 x 64, 64 x 64:
+  //   25,600 x 4,096, k 4,096: 760, 754, 781, 905, 1026, 1282 us
+  //    8,192 x 8,192, k 8,192: 822,  - , 933, 1049, 1200, 1476
+  //    6,400 x 1,536, k 1,024:  35,  27,  32,  37,  33,  42
+  //    2,048 x 4,096, k 4,096:  95,  76,  62,  74,  83, 103
+  //    1,777 x 2,048, k 1,160:  41,  24,  21,  17,  21,  25
+  //      512 x 4,096, k 4,096:  87,  45,  42,  33,  26,  28
+  //    1,000 x 1,024, k 2,048:  46,  26,  20,  18,  14,  11
   const auto tiles = [&](int t, int n) {
     return ((int64_t(P.n_tokens) + t - 1) / t) * ((int64_t(P.n) + n - 1) / n);
   };
   P.gather = P.adapter && P.b_step == 1;  // rows of b that a load to LDS cannot take
   if (P.gather) rc = launch_tiles<kType, 64, 64, 2, 2, 64, 4>(P, s);
-  else if (tiles(256, 256) >= 1024) rc = launch_tiles<kType, 256, 256, 4, 2, 32, 4>(P, s);
-  else if (tiles(128, 128) >= 256) rc = launch_tiles<kType, 128, 128, 2, 2, 64, 2>(P, s);
+  else if (tiles(128, 128) >= 256) {
+    const auto rounds = [&](int t, int n, int at_once) { return (tiles(t, n) + at_once - 1) / at_once; };
+    const int64_t c256 = 36 * rounds(256, 256, 256), c160 = 25 * rounds(160, 128, 512);
+    const int64_t c128 = 20 * rounds(128, 128, 512);
+    if (c256 <= c160 && c256 <= c128) rc = launch_tiles<kType, 256, 256, 4, 2, 32, 4>(P, s);
+    else if (c160 < c128) rc = launch_tiles<kType, 160, 128, 2, 2, 64, 2>(P, s);
+    else rc = launch_tiles<kType, 128, 128, 2, 2, 64, 2>(P, s);
+  }
   else if (tiles(128, 128) >= 192) rc = launch_tiles<kType, 128, 128, 2, 4, 64, 4>(P, s);
   else if (tiles(128, 64) >= 256) rc = launch_tiles<kType, 128, 64, 2, 2, 64, 3>(P, s);
   else rc = launch_tiles<kType, 64, 64, 2, 2, 64, 4>(P, s);

@@ -119,6 +119,35 @@ def test_project_keeps_adapters_apart(tokens):
     assert bool(torch.isnan(got[~rest]).any(1).all())
 
 
+# enough tiles of each size that the projection chooses from: 64 x 64, 128 x 64, 128 x 128 by 8
+# waves and by 4, 160 x 128, 256 x 256; each with k that ends inside a step
+TILES = [(300, 1000, 200), (520, 4100, 72), (1777, 2051, 136), (2050, 2100, 72), (4000, 2100, 104),
+         (8192, 4096, 40)]
+
+
+@pytest.mark.parametrize("dtype,adapters,rank", [("bf16", 6, 16), ("f16", 40, 12), ("f16", 3, 64),
+                                                 ("bf16", 4, 7)])
+@pytest.mark.parametrize("tokens,n,k", TILES)
+def test_project_tiles(tokens, n, k, dtype, adapters, rank):
+    say("project tiles", tokens, n, k, dtype, adapters, rank)
+    g, dt = gen(tokens + rank), DT[dtype]
+    x, w = normal(g, tokens, k, dtype=dt).cuda(), normal(g, n, k, dtype=dt, gain=k ** -0.5).cuda()
+    a = normal(g, adapters, rank, k, dtype=dt, gain=k ** -0.5).cuda()
+    b, scale = normal(g, adapters, n, rank, dtype=dt).cuda(), 0.5 + torch.rand(adapters, generator=g)
+    runs = torch.randint(-1, adapters, (tokens // 17 + 1,), generator=g, dtype=torch.int32)
+    ids = runs.repeat_interleave(17)[:tokens].contiguous()
+    want, bound = R.project(x, w, a, b, scale, ids.cuda())
+    got = run_project(x, w, (a, b, scale), ids).cuda()
+    R.assert_within(got, want, bound, "project")
+    # one adapter and two tokens gone bad change no other token
+    sick = [tokens // 2, tokens - 1]
+    b[1, n // 2:, 0], a[1, 0, 0], x[sick, 0] = NAN, INF, INF
+    rest = ids != 1
+    rest[sick] = False
+    got = run_project(x, w, (a, b, scale), ids)
+    R.assert_within(got[rest].cuda(), want[rest.cuda()], bound[rest.cuda()], "project")
+
+
 def test_project_large_and_small_rows():
     """Rows of h far from 1 in binary16: neither overflow nor lose their small values."""
     say("project range")

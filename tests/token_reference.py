@@ -19,17 +19,16 @@ def project(x, w, a, b, scale, adapter):
     xd, wd = x.double(), w.double()
     y = xd @ wd.t()
     err = x.shape[1] * E32 * (xd.abs() @ wd.abs().t())
-    if a is not None:
-        for t in range(x.shape[0]):
-            g = int(adapter[t])
-            if not 0 <= g < a.shape[0]:
-                continue
-            s, ad, bd = float(scale[g]), a[g].double(), b[g].double()
-            h = ad @ xd[t]
-            y[t] += s * (bd @ h)
-            mag = ad.abs() @ xd[t].abs()
-            err[t] += abs(s) * (bd.abs() @ ((x.shape[1] + 2 * a.shape[1] + 4) * E32 * mag
-                                            + 2 * u * u * h.abs().max()))
+    for g in range(a.shape[0] if a is not None else 0):
+        t = (adapter == g).nonzero()[:, 0]
+        if len(t) == 0:
+            continue
+        s, ad, bd = float(scale[g]), a[g].double(), b[g].double()
+        h = xd[t] @ ad.t()
+        y[t] += s * (h @ bd.t())
+        mag = xd[t].abs() @ ad.abs().t()
+        err[t] += abs(s) * (((x.shape[1] + 2 * a.shape[1] + 4) * E32 * mag
+                             + 2 * u * u * h.abs().amax(1, keepdim=True)) @ bd.abs().t())
     return y, err + u * y.abs() + TINY[x.dtype] + E32 * y.abs()
 
 
@@ -104,7 +103,7 @@ def attend(q, k, v, q_begin, kv_begin, kv_len, scale, cap=0.0, causal=False, pre
 
 
 def assert_within(got, want, bound, name):
-    got = got.double().cpu()
+    got = got.double().to(want.device)
     assert got.shape == want.shape
     assert torch.isfinite(got).all(), f"{name}: not finite"
     over = (got - want).abs() - bound
