@@ -41,6 +41,7 @@ struct ProjectParams {
   int32_t n_tokens, k, n, n_adapters, rank;
   int32_t pad_rank;  // 16, 32 or 64
   int32_t b_step;    // values of b that one load can take: 8, 2 or 1
+  int32_t b_rank;    // values of a row of b: rank, or pad_rank when it has been laid out anew
   void *h;           // [n_tokens][2][pad_rank] of the type
   float *h32;        // [n_tokens][pad_rank]
   int32_t gather;    // adapters are added by add_gathered
@@ -181,12 +182,15 @@ __global__ __launch_bounds__(kShrinkThreads) void shrink_kernel(const ProjectPar
   }
 }
 
-// One token's row of h, by a workgroup of kWaves: rows of x and a are read as they lie, 4 ranks a
-// wave at a time.
+// 4 ranks a wave of one token's row of h, from rank r0 on, by a workgroup of 4 waves: rows of x
+// and a are read as they lie.
+constexpr int kTokenRanks = 16;
 template <int kType, int kWaves>
-__device__ __forceinline__ void shrink_token(const ProjectParams &P, int t) {
+__device__ __forceinline__ void shrink_token(const ProjectParams &P, int t, int r0) {
   typedef typename Num<kType>::E E;
   typedef typename Num<kType>::V8 V8;
+  static_assert(kWaves * 4 == kTokenRanks, "4 ranks a wave");
+  constexpr int kAhead = 4;  // loads of a row under way
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int g = adapter_of(P, t);
@@ -194,34 +198,33 @@ __device__ __forceinline__ void shrink_token(const ProjectParams &P, int t) {
   const E *x = static_cast<const E *>(P.x) + t * P.x_stride;
   const E *a = static_cast<const E *>(P.a) + int64_t(g) * P.rank * P.k;
   const float scale = P.scale[g];
-  for (int r0 = wave * 4; r0 < P.pad_rank; r0 += kWaves * 4) {
-    float sum[4] = {};
-    for (int k = lane * 8; k < P.k; k += 1024) {
-      V8 xv[2] = {}, av[2][4] = {};
+  r0 += wave * 4;
+  float sum[4] = {};
+  for (int k = lane * 8; k < P.k; k += kAhead * 512) {
+    V8 xv[kAhead] = {}, av[kAhead][4] = {};
 #pragma unroll
-      for (int u = 0; u < 2; ++u)
-        if (k + u * 512 < P.k) {
-          xv[u] = *reinterpret_cast<const V8 *>(x + k + u * 512);
-#pragma unroll
-          for (int r = 0; r < 4; ++r)
-            av[u][r] = *reinterpret_cast<const V8 *>(a + int64_t(min(r0 + r, P.rank - 1)) * P.k +
-                                                     k + u * 512);
-        }
-#pragma unroll
-      for (int u = 0; u < 2; ++u)
+    for (int u = 0; u < kAhead; ++u)
+      if (k + u * 512 < P.k) {
+        xv[u] = *reinterpret_cast<const V8 *>(x + k + u * 512);
 #pragma unroll
         for (int r = 0; r < 4; ++r)
+          av[u][r] = *reinterpret_cast<const V8 *>(a + int64_t(min(r0 + r, P.rank - 1)) * P.k + k +
+                                                   u * 512);
+      }
 #pragma unroll
-          for (int i = 0; i < 8; ++i)
-            sum[r] = __builtin_fmaf(static_cast<float>(av[u][r][i]), static_cast<float>(xv[u][i]),
-                                    sum[r]);
-    }
+    for (int u = 0; u < kAhead; ++u)
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      sum[r] = wave_sum(sum[r]);
-      if (lane == 0)
-        P.h32[int64_t(t) * P.pad_rank + r0 + r] = r0 + r < P.rank ? sum[r] * scale : 0.0f;
-    }
+      for (int r = 0; r < 4; ++r)
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          sum[r] = __builtin_fmaf(static_cast<float>(av[u][r][i]), static_cast<float>(xv[u][i]),
+                                  sum[r]);
+  }
+#pragma unroll
+  for (int r = 0; r < 4; ++r) {
+    sum[r] = wave_sum(sum[r]);
+    if (lane == 0)
+      P.h32[int64_t(t) * P.pad_rank + r0 + r] = r0 + r < P.rank ? sum[r] * scale : 0.0f;
   }
 }
 
@@ -257,14 +260,14 @@ __device__ __forceinline__ typename Num<kType>::V8 b_chunk(const ProjectParams &
   typedef typename Num<kType>::V2 V2;
   typedef typename Num<kType>::V8 V8;
   V8 v = {};
-  if (j >= P.n || r >= P.rank) return v;
-  const E *b = static_cast<const E *>(P.b) + (int64_t(g) * P.n + j) * P.rank + r;
+  if (j >= P.n || r >= P.b_rank) return v;
+  const E *b = static_cast<const E *>(P.b) + (int64_t(g) * P.n + j) * P.b_rank + r;
   if (P.b_step == 8) {
     v = *reinterpret_cast<const V8 *>(b);
   } else if (P.b_step == 2) {
 #pragma unroll
     for (int i = 0; i < 8; i += 2)
-      if (r + i < P.rank) {
+      if (r + i < P.b_rank) {
         const V2 two = *reinterpret_cast<const V2 *>(b + i);
         v[i] = two[0];
         v[i + 1] = two[1];
@@ -272,7 +275,7 @@ __device__ __forceinline__ typename Num<kType>::V8 b_chunk(const ProjectParams &
   } else {
 #pragma unroll
     for (int i = 0; i < 8; ++i)
-      if (r + i < P.rank) v[i] = b[i];
+      if (r + i < P.b_rank) v[i] = b[i];
   }
   return v;
 }
@@ -359,7 +362,7 @@ __device__ __forceinline__ void mend(const ProjectParams &P, int t0, int n0,
       const float v = strict_value<kType>(
           static_cast<const E *>(P.x) + t * P.x_stride, static_cast<const E *>(P.w) + n * P.w_stride,
           P.k, P.h32 + int64_t(t) * P.pad_rank,
-          static_cast<const E *>(P.b) + (int64_t(max(g, 0)) * P.n + n) * P.rank,
+          static_cast<const E *>(P.b) + (int64_t(max(g, 0)) * P.n + n) * P.b_rank,
           g < 0 ? 0 : P.rank);
       static_cast<E *>(P.y)[t * P.y_stride + n] = static_cast<E>(v);
     }
@@ -460,7 +463,8 @@ __global__ __launch_bounds__(kWt *kWn * 64, 2) void project_kernel(const Project
   int tt, tn, cut = 0;
   if constexpr (kCut) {
     int id = blockIdx.x;
-    if (id < P.low_blocks) return shrink_token<kType, kWaves>(P, id);
+    if (id < P.low_blocks)
+      return shrink_token<kType, kWaves>(P, id % P.n_tokens, id / P.n_tokens * kTokenRanks);
     id -= P.low_blocks;
     cut = id % P.splits;
     id /= P.splits;
@@ -514,8 +518,8 @@ __global__ __launch_bounds__(kWt *kWn * 64, 2) void project_kernel(const Project
     const int e = part * kBK + chunk * 8, r = e & (P.pad_rank - 1);
     const auto hb = buffer(static_cast<const E *>(P.h) + int64_t(t0) * 2 * P.pad_rank,
                            static_cast<uint32_t>(xr) * 4 * P.pad_rank);
-    const auto bb = buffer(static_cast<const E *>(P.b) + int64_t(g) * P.n * P.rank,
-                           static_cast<uint32_t>(P.n) * P.rank * 2);
+    const auto bb = buffer(static_cast<const E *>(P.b) + int64_t(g) * P.n * P.b_rank,
+                           static_cast<uint32_t>(P.n) * P.b_rank * 2);
     const bool in = s < steps && e < 2 * P.pad_rank;
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
@@ -524,7 +528,7 @@ __global__ __launch_bounds__(kWt *kWn * 64, 2) void project_kernel(const Project
       if (first < kT) {
         if (in && s_id[row] == g) off = static_cast<uint32_t>((row * 2 * P.pad_rank + e) * 2);
       } else if (in && r < P.rank && n0 + row - kT < P.n) {
-        off = (static_cast<uint32_t>(n0 + row - kT) * P.rank + r) * 2;
+        off = (static_cast<uint32_t>(n0 + row - kT) * P.b_rank + r) * 2;
       }
       load_lds(first < kT ? hb : bb, &tile[s % kStages][first * kBK], off, 0);
     }
@@ -575,9 +579,8 @@ __global__ __launch_bounds__(kWt *kWn * 64, 2) void project_kernel(const Project
       if (i < kLoads) __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);
     }
   };
-  // steps of a small tile are short, so that they wait for their loads: from a few adapters on
-  // they are gathered
-  constexpr int kMany = 3;
+  // steps of a small tile are short, so that they wait for their loads: where there are many they
+  // are gathered, which takes about as long as pad_rank / 4 of them (more in narrow loads)
   bool gather = P.adapter && P.gather;
   const bool steps_low = !kCut && P.adapter && !P.gather;
   int id = -1;
@@ -588,7 +591,7 @@ __global__ __launch_bounds__(kWt *kWn * 64, 2) void project_kernel(const Project
     if (threadIdx.x < kT) s_id[threadIdx.x] = id;
     __syncthreads();
     const int n = distinct<kT, kWaves>(s_id, s_heads, s_list, s_counts);
-    gather = kFt * kFn <= 4 && n > kMany;
+    gather = kFt * kFn <= 4 && n * per * 4 > P.pad_rank * (P.b_step == 8 ? 1 : 3);
     if (!gather) steps += per * n;
     for (int s = begun; s < kStages; ++s) fetch_low(s);
   }
@@ -625,6 +628,27 @@ __global__ __launch_bounds__(kWt *kWn * 64, 2) void project_kernel(const Project
   }
   store<kType, kFn, kFt>(P, t0 + wt, n0 + wn, acc);
   if (steps > main_steps) mend<kType, kFn, kFt>(P, t0 + wt, n0 + wn, acc);
+}
+
+// Rows of b of an odd rank, laid out anew in rows of pad_rank that loads to LDS can take; 8 values
+// a thread.
+constexpr int kPackThreads = 256;
+template <int kType>
+__global__ __launch_bounds__(kPackThreads) void pack_kernel(const ProjectParams P, void *to,
+                                                            int64_t rows) {
+  typedef typename Num<kType>::E E;
+  typedef typename Num<kType>::V8 V8;
+  const int64_t id = int64_t(blockIdx.x) * kPackThreads + threadIdx.x;
+  const int chunks = P.pad_rank / 8;
+  const int64_t row = id / chunks;
+  if (row >= rows) return;
+  const int r = static_cast<int>(id - row * chunks) * 8;
+  const E *from = static_cast<const E *>(P.b) + row * P.rank;
+  V8 v = {};
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+    if (r + i < P.rank) v[i] = from[r + i];
+  *reinterpret_cast<V8 *>(static_cast<E *>(to) + row * P.pad_rank + r) = v;
 }
 
 // Adds the cuts of k, and each token's adapter: a thread has 4 outputs of a token.
@@ -709,11 +733,11 @@ Few few_of(int n_tokens, int k, int n) {
 int part_stride(int n) { return (n + 3) / 4 * 4; }
 
 template <int kType>
-int launch(ProjectParams P, const Few &few, hipStream_t s) {
+int launch(ProjectParams P, const Few &few, void *packed, hipStream_t s) {
   int rc;
   if (few.use && (P.adapter || few.alone)) {
     P.splits = few.splits;
-    P.low_blocks = P.adapter ? P.n_tokens : 0;
+    P.low_blocks = P.adapter ? P.n_tokens * (P.pad_rank / kTokenRanks) : 0;
     rc = few.tile == 32 ? launch_tiles<kType, 32, 64, 1, 4, 64, 4, true>(P, s)
                         : launch_tiles<kType, 64, 64, 2, 2, 64, 4, true>(P, s);
     if (rc != TG_OK) return rc;
@@ -723,6 +747,16 @@ int launch(ProjectParams P, const Few &few, hipStream_t s) {
     return hipGetLastError() == hipSuccess ? TG_OK : TG_E_HIP;
   }
   if (P.adapter) launch_shrink<kType>(P, s);
+  if (packed) {
+    const int64_t rows = int64_t(P.n_adapters) * P.n;
+    const int64_t threads = rows * (P.pad_rank / 8);
+    hipLaunchKernelGGL(pack_kernel<kType>,
+                       dim3(static_cast<uint32_t>((threads + kPackThreads - 1) / kPackThreads)),
+                       dim3(kPackThreads), 0, s, P, packed, rows);
+    P.b = packed;
+    P.b_rank = P.pad_rank;
+    P.b_step = 8;
+  }
   // Large problems take the tile with the least time for its rounds: 512 workgroups at once, two
   // a CU (256 with tiles of 256 x 256), a round of 160 x 128 takes 1.25 times one of 128 x 128
   // and one of 256 x 256 1.8 times. Fewer tiles than half a round: smaller ones. Measured
@@ -757,6 +791,14 @@ int launch(ProjectParams P, const Few &few, hipStream_t s) {
 
 int pad_rank(int rank) { return rank <= 16 ? 16 : rank <= 32 ? 32 : 64; }
 
+// Bytes for b laid out anew: an odd rank, and not the few-token form, which reads it as it is.
+// What would take more than a few microseconds to lay out is gathered.
+size_t pack_bytes(int n_tokens, int n, int n_adapters, int rank) {
+  if (rank % 2 == 0 || n_tokens <= kFewTokens) return 0;
+  const size_t bytes = size_t(n_adapters) * n * pad_rank(rank) * 2;
+  return bytes <= (size_t(64) << 20) ? bytes : 0;
+}
+
 }  // namespace
 
 extern "C" size_t tg_project_workspace_bytes(int32_t n_tokens, int32_t k, int32_t n,
@@ -767,6 +809,7 @@ extern "C" size_t tg_project_workspace_bytes(int32_t n_tokens, int32_t k, int32_
   const size_t t = static_cast<size_t>(n_tokens);
   const Few few = few_of(n_tokens, k, n);
   size_t bytes = low ? t * pad_rank(rank) * (2 * 2 + sizeof(float)) : 0;
+  if (low) bytes += pack_bytes(n_tokens, n, n_adapters, rank);
   if (few.use && (low || few.alone)) bytes += few.splits * t * part_stride(n) * sizeof(float);
   return bytes;
 }
@@ -801,6 +844,7 @@ extern "C" int tg_project(const tg_project_args *a, void *stream) {
     return TG_E_WORKSPACE;
   P.part = static_cast<float *>(a->workspace);
   P.part_stride = part_stride(a->n);
+  void *packed = nullptr;
   if (low) {
     P.a = a->a;
     P.b = a->b;
@@ -814,7 +858,10 @@ extern "C" int tg_project(const tg_project_args *a, void *stream) {
     P.h32 = static_cast<float *>(a->workspace);
     P.h = P.h32 + size_t(a->n_tokens) * P.pad_rank;
     P.part = P.h32 + size_t(a->n_tokens) * P.pad_rank * 2;
+    if (pack_bytes(a->n_tokens, a->n, a->n_adapters, a->rank) > 0) packed = P.part;
+    P.b_rank = a->rank;
   }
   hipStream_t s = static_cast<hipStream_t>(stream);
-  return a->type == TG_F16 ? launch<TG_F16>(P, few, s) : launch<TG_BF16>(P, few, s);
+  return a->type == TG_F16 ? launch<TG_F16>(P, few, packed, s)
+                           : launch<TG_BF16>(P, few, packed, s);
 }
