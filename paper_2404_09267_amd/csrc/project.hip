@@ -40,7 +40,7 @@ struct ProjectParams {
   int64_t x_stride, w_stride, y_stride;
   int32_t n_tokens, k, n, n_adapters, rank;
   int32_t pad_rank;  // 16, 32 or 64
-  int32_t b_step;    // values of b that one load can take: 8, 2 or 1
+  int32_t b_apart;   // rows of b lie on 4-byte boundaries, which loads to LDS ask for: 0, else 1
   int32_t b_rank;    // values of a row of b: rank, or pad_rank when it has been laid out anew
   void *h;           // [n_tokens][2][pad_rank] of the type
   float *h32;        // [n_tokens][pad_rank]
@@ -252,26 +252,23 @@ void launch_shrink(const ProjectParams &P, hipStream_t s) {
 
 // ---------------------------------------------------------------------------- the product
 
-// 8 values of b_g's row j from rank r on, zero past the rank and past the last output.
+// 8 values of b_g's row j from rank r on, zero past the rank and past the last output. Rows may
+// start anywhere: the 16 bytes are loaded as they lie, into the next row where the rank ends
+// inside, and one by one where that would be past the last row.
 template <int kType>
 __device__ __forceinline__ typename Num<kType>::V8 b_chunk(const ProjectParams &P, int g, int j,
                                                             int r) {
   typedef typename Num<kType>::E E;
-  typedef typename Num<kType>::V2 V2;
   typedef typename Num<kType>::V8 V8;
   V8 v = {};
   if (j >= P.n || r >= P.b_rank) return v;
-  const E *b = static_cast<const E *>(P.b) + (int64_t(g) * P.n + j) * P.b_rank + r;
-  if (P.b_step == 8) {
-    v = *reinterpret_cast<const V8 *>(b);
-  } else if (P.b_step == 2) {
+  const int64_t at = (int64_t(g) * P.n + j) * P.b_rank + r;
+  const E *b = static_cast<const E *>(P.b) + at;
+  if (at + 8 <= int64_t(P.n_adapters) * P.n * P.b_rank) {
+    __builtin_memcpy(&v, b, sizeof(v));
 #pragma unroll
-    for (int i = 0; i < 8; i += 2)
-      if (r + i < P.b_rank) {
-        const V2 two = *reinterpret_cast<const V2 *>(b + i);
-        v[i] = two[0];
-        v[i + 1] = two[1];
-      }
+    for (int i = 1; i < 8; ++i)
+      if (r + i >= P.b_rank) v[i] = static_cast<E>(0.0f);
   } else {
 #pragma unroll
     for (int i = 0; i < 8; ++i)
@@ -580,7 +577,7 @@ __global__ __launch_bounds__(kWt *kWn * 64, 2) void project_kernel(const Project
     }
   };
   // steps of a small tile are short, so that they wait for their loads: where there are many they
-  // are gathered, which takes about as long as pad_rank / 4 of them (more in narrow loads)
+  // are gathered, which takes about as long as pad_rank / 4 of them
   bool gather = P.adapter && P.gather;
   const bool steps_low = !kCut && P.adapter && !P.gather;
   int id = -1;
@@ -591,7 +588,7 @@ __global__ __launch_bounds__(kWt *kWn * 64, 2) void project_kernel(const Project
     if (threadIdx.x < kT) s_id[threadIdx.x] = id;
     __syncthreads();
     const int n = distinct<kT, kWaves>(s_id, s_heads, s_list, s_counts);
-    gather = kFt * kFn <= 4 && n * per * 4 > P.pad_rank * (P.b_step == 8 ? 1 : 3);
+    gather = kFt * kFn <= 4 && n * per * 4 > P.pad_rank;
     if (!gather) steps += per * n;
     for (int s = begun; s < kStages; ++s) fetch_low(s);
   }
@@ -755,7 +752,7 @@ int launch(ProjectParams P, const Few &few, void *packed, hipStream_t s) {
                        dim3(kPackThreads), 0, s, P, packed, rows);
     P.b = packed;
     P.b_rank = P.pad_rank;
-    P.b_step = 8;
+    P.b_apart = 0;
   }
   // Large problems take the tile with the least time for its rounds: 512 workgroups at once, two
   // a CU (256 with tiles of 256 x 256), a round of 160 x 128 takes 1.25 times one of 128 x 128
@@ -772,7 +769,7 @@ int launch(ProjectParams P, const Few &few, void *packed, hipStream_t s) {
   const auto tiles = [&](int t, int n) {
     return ((int64_t(P.n_tokens) + t - 1) / t) * ((int64_t(P.n) + n - 1) / n);
   };
-  P.gather = P.adapter && P.b_step == 1;  // rows of b that a load to LDS cannot take
+  P.gather = P.adapter && P.b_apart;  // rows of b that a load to LDS cannot take
   if (P.gather) rc = launch_tiles<kType, 64, 64, 2, 2, 64, 4>(P, s);
   else if (tiles(128, 128) >= 256) {
     const auto rounds = [&](int t, int n, int at_once) { return (tiles(t, n) + at_once - 1) / at_once; };
@@ -854,7 +851,7 @@ extern "C" int tg_project(const tg_project_args *a, void *stream) {
     P.rank = a->rank;
     P.pad_rank = pad_rank(a->rank);
     const uintptr_t at = reinterpret_cast<uintptr_t>(a->b);
-    P.b_step = a->rank % 8 == 0 && at % 16 == 0 ? 8 : a->rank % 2 == 0 && at % 4 == 0 ? 2 : 1;
+    P.b_apart = a->rank % 2 != 0 || at % 4 != 0;
     P.h32 = static_cast<float *>(a->workspace);
     P.h = P.h32 + size_t(a->n_tokens) * P.pad_rank;
     P.part = P.h32 + size_t(a->n_tokens) * P.pad_rank * 2;
