@@ -41,6 +41,7 @@ struct RotateParams {
   int32_t rows;             // heads of a token, over q, k and v
   int32_t passes;           // waves of a token, each takes rows / passes heads in turn
   int32_t lanes;            // lanes of a head, a power of two
+  int32_t at_once;          // heads of a token that a wave takes at once, a power of two
 };
 
 // Which tensor (0 q, 1 k, 2 v) head row `r` of a token is in; r becomes the head there.
@@ -75,11 +76,13 @@ __global__ __launch_bounds__(kThreads) void rotate_kernel(const RotateParams P) 
   typedef typename N::E E;
   typedef typename N::V8 V8;
   const int64_t unit = int64_t(blockIdx.x) * (kThreads / 64) + (threadIdx.x >> 6);
-  const int64_t t = unit / P.passes;
-  if (t >= P.n_tokens) return;
-  const int pass = static_cast<int>(unit - t * P.passes);
   const int lane = threadIdx.x & 63, sub = lane & (P.lanes - 1);
-  const int step = 64 / P.lanes;
+  const int slot = lane / P.lanes, step = P.at_once;
+  // a wave has several tokens where one has fewer heads than the wave has room for
+  const int64_t several = unit / P.passes;
+  const int pass = static_cast<int>(unit - several * P.passes);
+  const int64_t t = several * (64 / P.lanes / step) + slot / step;
+  if (t >= P.n_tokens) return;
   const bool has = sub < P.d / 16;
   const bool turns = sub * 16 < P.rot;
   int c0, c1;  // first values of the two chunks
@@ -116,7 +119,7 @@ __global__ __launch_bounds__(kThreads) void rotate_kernel(const RotateParams P) 
     for (int i = 0; i < 8; ++i) cs[i][0] = 1.0f, cs[i][1] = 0.0f;
   }
   for (int first = pass * step; first < P.rows; first += P.passes * step) {
-    int h = first + lane / P.lanes;
+    int h = first + (slot & (step - 1));
     const bool use = has && h < P.rows;
     const int which = use ? tensor_of(P, h) : 0;
     V8 a = {}, b = {};
@@ -316,10 +319,14 @@ extern "C" int tg_rotate(const tg_rotate_args *a, void *stream) {
   if (vec) {
     P.lanes = 1;
     while (P.lanes < a->d / 16) P.lanes *= 2;
-    const int step = 64 / P.lanes;
-    const int most = (P.rows + step - 1) / step;
+    const int room = 64 / P.lanes;
+    P.at_once = 1;
+    while (P.at_once < room && P.at_once < P.rows) P.at_once *= 2;
+    const int most = (P.rows + P.at_once - 1) / P.at_once;
     P.passes = a->n_tokens < 4096 ? most : 1;
-    const int64_t blocks = (int64_t(a->n_tokens) * P.passes + kWaves - 1) / kWaves;
+    const int per = room / P.at_once;  // tokens of a wave
+    const int64_t waves = (int64_t(a->n_tokens) + per - 1) / per * P.passes;
+    const int64_t blocks = (waves + kWaves - 1) / kWaves;
     if (blocks > INT32_MAX) return TG_E_INVAL;
     const dim3 grid(static_cast<uint32_t>(blocks));
     if (a->type == TG_F16)
