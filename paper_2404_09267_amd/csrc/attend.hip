@@ -1103,8 +1103,8 @@ extern "C" int tg_attend(const tg_attend_args *a, void *stream) {
   P.prefix = a->prefix;
   P.q_doc = a->q_doc;
   P.k_doc = a->k_doc;
-  P.q_pos = a->q_pos;
-  P.k_pos = a->k_pos;
+  P.q_pos = a->slope ? a->q_pos : nullptr;  // nothing else asks for places
+  P.k_pos = a->slope ? a->k_pos : nullptr;
   P.slope = a->slope;
   P.to_log2 = a->scale * kLog2e;
   if (a->cap > 0.0f) {

@@ -20,6 +20,7 @@
 // are contiguous and a token's adapter belongs to the lane.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <climits>
 #include <cstdint>
 
@@ -419,9 +420,9 @@ __device__ __forceinline__ void store(const ProjectParams &P, int t0, int n0,
 }
 
 // A tile of kT tokens x kN outputs, kWt x kWn waves, kBK values of k a step, kStages steps of
-// loads under way. Step s + 1's operands are read from LDS while step s's are multiplied, so
+// loads under way. The next 32 values' operands are read from LDS while these are multiplied, so
 // that the matrix units have work across the barrier; the buffer of step s is free for step
-// s + kStages behind that barrier, since its operands are in registers by then.
+// s + kStages behind the barrier at the end of it, since its operands are in registers by then.
 // Rows of a tile lie in LDS as kBK / 8 chunks of 16 bytes, in an order that serves the operands'
 // reads (one chunk of 16 rows) best: 156 bytes a cycle and CU measured with rows of 64 and 146
 // with rows of 32, where (row / 4) in the place of (row / 2) gives 116 and no change of order 123.
@@ -532,49 +533,52 @@ __global__ __launch_bounds__(kWt *kWn * 64, 2) void project_kernel(const Project
   };
   f32x4 acc[kFn][kFt] = {};
   const int wt = (wave % kWt) * (kT / kWt), wn = (wave / kWt) * (kN / kWn);
-  struct Operands {
-    V8 x[kSub][kFt], w[kSub][kFn];
+  struct Operands {  // of 32 values of k
+    V8 x[kFt], w[kFn];
   };
-  auto read = [&](Operands &o, int s) {
+  auto read = [&](Operands &o, int s, int ks) {
     const E *m = tile[s % kStages];
 #pragma unroll
-    for (int ks = 0; ks < kSub; ++ks) {
+    for (int i = 0; i < kFt; ++i) {
+      const int row = wt + 16 * i + col;
+      o.x[i] = *reinterpret_cast<const V8 *>(m + row * kBK + place_of<kBK>(row, ks * 4 + quad) * 8);
+    }
 #pragma unroll
-      for (int i = 0; i < kFt; ++i) {
-        const int row = wt + 16 * i + col;
-        o.x[ks][i] =
-            *reinterpret_cast<const V8 *>(m + row * kBK + place_of<kBK>(row, ks * 4 + quad) * 8);
-      }
-#pragma unroll
-      for (int j = 0; j < kFn; ++j) {
-        const int row = kT + wn + 16 * j + col;
-        o.w[ks][j] =
-            *reinterpret_cast<const V8 *>(m + row * kBK + place_of<kBK>(row, ks * 4 + quad) * 8);
-      }
+    for (int j = 0; j < kFn; ++j) {
+      const int row = kT + wn + 16 * j + col;
+      o.w[j] = *reinterpret_cast<const V8 *>(m + row * kBK + place_of<kBK>(row, ks * 4 + quad) * 8);
     }
   };
   auto multiply = [&](const Operands &o) {
 #pragma unroll
-    for (int ks = 0; ks < kSub; ++ks)
+    for (int j = 0; j < kFn; ++j)
 #pragma unroll
-      for (int j = 0; j < kFn; ++j)
-#pragma unroll
-        for (int i = 0; i < kFt; ++i) acc[j][i] = N::mfma16(o.w[ks][j], o.x[ks][i], acc[j][i]);
+      for (int i = 0; i < kFt; ++i) acc[j][i] = N::mfma16(o.w[j], o.x[i], acc[j][i]);
   };
-  auto step = [&](int s, Operands &now, Operands &then, bool low) {
-    wait_and_meet<(kStages - 2) * kLoads>();  // step s + 1 is here, step s in registers
-    if (low && s + kStages >= main_steps) fetch_low(s + kStages);
-    else fetch(s + kStages);
-    read(then, s + 1);
-    multiply(now);
-    // the scheduler would put the reads at the end, where the next step waits for them
-    constexpr int kReads = kSub * (kFt + kFn), kMul = kSub * kFt * kFn;
+  // the scheduler would put the reads at the end, where the products after them wait for them
+  auto interleave = [&](bool loads) {
+    constexpr int kReads = kFt + kFn, kMul = kFt * kFn;
 #pragma unroll
     for (int i = 0; i < kReads; ++i) {
       __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
       __builtin_amdgcn_sched_group_barrier(0x008, kMul / kReads, 0);
-      if (i < kLoads) __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);
+      if (loads && i < kLoads) __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);
     }
+  };
+  // `now` has the first 32 values of step s; it, or `then`, is left with those of step s + 1
+  auto step = [&](int s, Operands &now, Operands &then, bool low) {
+    if constexpr (kSub == 2) {
+      read(then, s, 1);
+      multiply(now);
+      interleave(false);
+    }
+    Operands &last = kSub == 2 ? then : now, &next = kSub == 2 ? now : then;
+    wait_and_meet<(kStages - 2) * kLoads>();  // step s + 1 is here, step s in registers
+    if (low && s + kStages >= main_steps) fetch_low(s + kStages);
+    else fetch(s + kStages);
+    read(next, s + 1, 0);
+    multiply(last);
+    interleave(true);
   };
   // steps of a small tile are short, so that they wait for their loads: where there are many they
   // are gathered, which takes about as long as pad_rank / 4 of them
@@ -594,15 +598,16 @@ __global__ __launch_bounds__(kWt *kWn * 64, 2) void project_kernel(const Project
   }
   wait_and_meet<(kStages - 1) * kLoads>();
   Operands a, b;
-  read(a, 0);
+  read(a, 0, 0);
   int s = 0;
-  for (; s + 1 + kStages < main_steps; s += 2) {
+  constexpr int kTurn = kSub == 2 ? 1 : 2;  // steps after which a and b are back in their places
+  for (; s + kTurn - 1 + kStages < main_steps; s += kTurn) {
     step(s, a, b, false);
-    step(s + 1, b, a, false);
+    if constexpr (kTurn == 2) step(s + 1, b, a, false);
   }
-  for (; s < steps; s += 2) {  // a step past the last one multiplies zeros
+  for (; s < steps; s += kTurn) {  // a step past the last one multiplies zeros
     step(s, a, b, steps_low);
-    step(s + 1, b, a, steps_low);
+    if constexpr (kTurn == 2) step(s + 1, b, a, steps_low);
   }
   wait_loads();  // LDS belongs to the next workgroup from here on
   if constexpr (kCut) {
@@ -755,17 +760,19 @@ int launch(ProjectParams P, const Few &few, void *packed, hipStream_t s) {
     P.b_apart = 0;
   }
   // Large problems take the tile with the least time for its rounds: 512 workgroups at once, two
-  // a CU (256 with tiles of 256 x 256), a round of 160 x 128 takes 1.25 times one of 128 x 128
-  // and one of 256 x 256 1.8 times. Fewer tiles than half a round: smaller ones. Measured
-  // (bfloat16, no adapters) with tiles of 256 x 256, 160 x 128, 128 x 128, the latter with 8 waves,
-  // 128 x 64, 64 x 64:
-  //   25,600 x 4,096, k 4,096: 760, 754, 781, 905, 1026, 1282 us
-  //    8,192 x 8,192, k 8,192: 822,  - , 933, 1049, 1200, 1476
-  //    6,400 x 1,536, k 1,024:  35,  27,  32,  37,  33,  42
-  //    2,048 x 4,096, k 4,096:  95,  76,  62,  74,  83, 103
-  //    1,777 x 2,048, k 1,160:  41,  24,  21,  17,  21,  25
-  //      512 x 4,096, k 4,096:  87,  45,  42,  33,  26,  28
-  //    1,000 x 1,024, k 2,048:  46,  26,  20,  18,  14,  11
+  // a CU (256 with tiles of 256 values of n), and a round of 160 x 128, 192 x 256 and 256 x 256
+  // takes 1.18, 1.37 and 1.64 times one of 128 x 128. Fewer tiles than half a round: smaller ones.
+  // Measured (bfloat16, no adapters, us) with tiles of 256 x 256, 192 x 256, 160 x 128, 128 x 128,
+  // the latter with 8 waves, 128 x 64, 64 x 64:
+  //   25,600 x 4,096, k 4,096: 700, 753, 721, 795, 851, 974, 1238
+  //    8,192 x 8,192, k 8,192: 773, 936, 888, 948, 999, 1143, 1473
+  //   12,000 x 1,024, k 1,024:  34,  28,  36,  33,  35,   36,   45
+  //    6,400 x 1,536, k 1,024:  33,  28,  25,  32,  33,   31,   39
+  //    2,048 x 4,096, k 4,096:  88,  71,  69,  63,  65,   75,   97
+  //    1,777 x 2,048, k 1,160:  37,  32,  23,  20,  17,   20,   25
+  //   11,019 x   233, k 2,464:  58,  48,  35,  33,  25,   31,   31
+  //      512 x 4,096, k 4,096:  86,  68,  45,  43,  30,   25,   28
+  //    1,000 x 1,024, k 2,048:  47,  39,  26,  21,  17,   14,   12
   const auto tiles = [&](int t, int n) {
     return ((int64_t(P.n_tokens) + t - 1) / t) * ((int64_t(P.n) + n - 1) / n);
   };
@@ -773,13 +780,15 @@ int launch(ProjectParams P, const Few &few, void *packed, hipStream_t s) {
   if (P.gather) rc = launch_tiles<kType, 64, 64, 2, 2, 64, 4>(P, s);
   else if (tiles(128, 128) >= 256) {
     const auto rounds = [&](int t, int n, int at_once) { return (tiles(t, n) + at_once - 1) / at_once; };
-    const int64_t c256 = 36 * rounds(256, 256, 256), c160 = 25 * rounds(160, 128, 512);
-    const int64_t c128 = 20 * rounds(128, 128, 512);
-    if (c256 <= c160 && c256 <= c128) rc = launch_tiles<kType, 256, 256, 4, 2, 32, 4>(P, s);
-    else if (c160 < c128) rc = launch_tiles<kType, 160, 128, 2, 2, 64, 2>(P, s);
+    const int64_t c256 = 164 * rounds(256, 256, 256), c192 = 137 * rounds(192, 256, 256);
+    const int64_t c160 = 118 * rounds(160, 128, 512), c128 = 100 * rounds(128, 128, 512);
+    const int64_t least = std::min(std::min(c256, c192), std::min(c160, c128));
+    if (c256 == least) rc = launch_tiles<kType, 256, 256, 2, 4, 64, 2>(P, s);
+    else if (c192 == least) rc = launch_tiles<kType, 192, 256, 4, 2, 64, 2>(P, s);
+    else if (c160 == least) rc = launch_tiles<kType, 160, 128, 2, 2, 64, 2>(P, s);
     else rc = launch_tiles<kType, 128, 128, 2, 2, 64, 2>(P, s);
   }
-  else if (tiles(128, 128) >= 192) rc = launch_tiles<kType, 128, 128, 2, 4, 64, 4>(P, s);
+  else if (tiles(128, 128) >= 160) rc = launch_tiles<kType, 128, 128, 2, 4, 64, 4>(P, s);
   else if (tiles(128, 64) >= 256) rc = launch_tiles<kType, 128, 64, 2, 2, 64, 3>(P, s);
   else rc = launch_tiles<kType, 64, 64, 2, 2, 64, 4>(P, s);
   if (rc != TG_OK) return rc;
