@@ -49,7 +49,6 @@ struct ProjectParams {
   float *part;       // [splits][n_tokens][part_stride]: sums over a cut of k
   int32_t part_stride, splits, low_blocks;
   int32_t tiles_t, tiles_n;
-  int32_t vec_y;     // 4 outputs of a token can be stored at once
 };
 
 __device__ __forceinline__ int adapter_of(const ProjectParams &P, int t) {
@@ -408,8 +407,8 @@ __device__ __forceinline__ void store(const ProjectParams &P, int t0, int n0,
     for (int j = 0; j < kFn; ++j) {
       const int n = n0 + 16 * j + 4 * quad;
       const V4 v = __builtin_convertvector(acc[j][i], V4);
-      if (P.vec_y && n + 3 < P.n) {
-        *reinterpret_cast<V4 *>(row + n) = v;
+      if (n + 3 < P.n) {  // as they lie: rows may start anywhere
+        __builtin_memcpy(row + n, &v, sizeof(v));
       } else {
 #pragma unroll
         for (int r = 0; r < 4; ++r)
@@ -687,8 +686,8 @@ __global__ __launch_bounds__(kFinishThreads) void finish_kernel(const ProjectPar
   }
   E *y = static_cast<E *>(P.y) + t * P.y_stride + n;
   const V4 v = __builtin_convertvector(sum, V4);
-  if (P.vec_y && n + 3 < P.n) {
-    *reinterpret_cast<V4 *>(y) = v;
+  if (n + 3 < P.n) {
+    __builtin_memcpy(y, &v, sizeof(v));
   } else {
 #pragma unroll
     for (int q = 0; q < 4; ++q)
@@ -842,7 +841,6 @@ extern "C" int tg_project(const tg_project_args *a, void *stream) {
   P.n_tokens = a->n_tokens;
   P.k = a->k;
   P.n = a->n;
-  P.vec_y = reinterpret_cast<uintptr_t>(a->y) % 8 == 0 && a->y_stride % 4 == 0;
   const Few few = few_of(a->n_tokens, a->k, a->n);
   const size_t need = tg_project_workspace_bytes(a->n_tokens, a->k, a->n,
                                                  low ? a->n_adapters : 0, low ? a->rank : 0);
