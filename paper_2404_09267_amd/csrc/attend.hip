@@ -94,6 +94,44 @@ __device__ __forceinline__ Seq sequence(const AttendParams &P, int s) {
   return r;
 }
 
+// Lane `l`'s sequence, for every lane.
+__device__ __forceinline__ Seq broadcast(const Seq &s, int l) {
+  const auto take = [&](int v) { return __builtin_amdgcn_readlane(v, l); };
+  Seq r;
+  r.q0 = take(s.q0);
+  r.nq = take(s.nq);
+  const uint32_t hi = static_cast<uint32_t>(take(static_cast<int>(s.k0 >> 32)));
+  const uint32_t lo = static_cast<uint32_t>(take(static_cast<int>(s.k0)));
+  r.k0 = static_cast<int64_t>(static_cast<uint64_t>(hi) << 32 | lo);
+  r.nk = take(s.nk);
+  r.place0 = take(s.place0);
+  r.prefix = take(s.prefix);
+  return r;
+}
+
+// The sequence that has a tile of `rows` queries, and the tile's first query in it (none of its
+// own where that is outside). Sequence b owns the tiles from q_begin[b] / rows + b on, room for
+// all of its queries. Up to 64 sequences are looked at at once, one a lane.
+__device__ __forceinline__ Seq sequence_of(const AttendParams &P, int tile, int rows, int &first) {
+  if (P.n_seqs <= 64) {
+    const int lane = threadIdx.x & 63;
+    const Seq mine = sequence(P, min(lane, P.n_seqs - 1));
+    const uint64_t before = __ballot(lane < P.n_seqs && mine.q0 / rows + lane <= tile);
+    const int at = before ? 63 - __builtin_clzll(before) : 0;
+    const Seq s = broadcast(mine, __builtin_amdgcn_readfirstlane(at));
+    first = (tile - (s.q0 / rows + at)) * rows;
+    return s;
+  }
+  int lo = 0, hi = P.n_seqs - 1;
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (min(max(P.q_begin[mid], 0), P.n_q_rows) / rows + mid <= tile) lo = mid; else hi = mid - 1;
+  }
+  const Seq s = sequence(P, lo);
+  first = (tile - (s.q0 / rows + lo)) * rows;
+  return s;
+}
+
 // Keys before this one are the ones that query i may see, documents aside.
 __device__ __forceinline__ int key_limit(const AttendParams &P, const Seq &s, int i) {
   if (!P.causal) return s.nk;
@@ -103,6 +141,12 @@ __device__ __forceinline__ int key_limit(const AttendParams &P, const Seq &s, in
 // 1 / (1 + 2^x), which is (1 - tanh) / 2 of the argument that x stands for.
 __device__ __forceinline__ float fall(float x) {
   return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(x));
+}
+
+// a - b of any two, rounded once: by halves, as the difference can pass 32 bits.
+__device__ __forceinline__ float apart(int a, int b) {
+  return __builtin_fmaf(static_cast<float>((a >> 16) - (b >> 16)), 65536.0f,
+                        static_cast<float>((a & 0xFFFF) - (b & 0xFFFF)));
 }
 
 // A raw score capped, in log2 units.
@@ -156,12 +200,15 @@ __device__ __forceinline__ float both_halves(float v) {
                __builtin_bit_cast(float, static_cast<unsigned>(r[1])));
 }
 
-__device__ __forceinline__ int abs_diff(int a, int b) { return a > b ? a - b : b - a; }
+__device__ __forceinline__ float abs_diff(int a, int b) {  // of any two
+  const uint32_t d = static_cast<uint32_t>(a) - static_cast<uint32_t>(b);
+  return static_cast<float>(a > b ? d : 0u - d);
+}
 
 // One query row of one head, by one wave, unseen keys left out one by one.
 template <int kType>
 __device__ __forceinline__ void strict_row(const AttendParams &P, const Seq &s, int i,
-                                                     int head) {
+                                           int head) {
   typedef typename Num<kType>::E E;
   const int lane = threadIdx.x & 63;
   const int64_t row = int64_t(s.q0) + i;
@@ -177,11 +224,11 @@ __device__ __forceinline__ void strict_row(const AttendParams &P, const Seq &s, 
     const E *kr = k + (s.k0 + j) * P.k_stride;
     float z = 0.0f;
     for (int c = 0; c < P.d; ++c) z += static_cast<float>(q[c]) * static_cast<float>(kr[c]);
-    int far = abs_diff(place, j);
+    float far = abs_diff(place, j);
     if (P.k_pos)
       far = abs_diff(P.q_pos[2 * row], P.k_pos[2 * (s.k0 + j)]) +
             abs_diff(P.q_pos[2 * row + 1], P.k_pos[2 * (s.k0 + j) + 1]);
-    return shape(P, z, slope2, P.slope ? static_cast<float>(far) : 0.0f);
+    return shape(P, z, slope2, P.slope ? far : 0.0f);
   };
   float m = -INFINITY;
   for (int j = lane; j < limit; j += 64) {
@@ -297,7 +344,7 @@ __global__ __launch_bounds__(kThreads, kD == 64 ? 3 : 2) void attend_tile_kernel
   constexpr bool kAnyMode = kMode == kAny;
   __shared__ int s_doc[2][kAnyMode ? kBN : 1];
   __shared__ int s_pos[2][2][kAnyMode ? kBN : 1];
-  __shared__ float s_far[kWaves][2][kAnyMode ? kBN : 1];  // a wave's keys' places, times the slope
+  __shared__ float s_far[kWaves][2][kAnyMode ? kBN : 1];  // the keys' places from the wave's first
   __shared__ uint64_t s_use[kAnyMode ? kMaskTiles / 64 : 1];
   __shared__ int s_range[kWaves][2];
   const bool with_docs = kAnyMode && P.k_doc, with_pos = kAnyMode && P.k_pos;
@@ -306,14 +353,8 @@ __global__ __launch_bounds__(kThreads, kD == 64 ? 3 : 2) void attend_tile_kernel
   const int col = lane & 31, half = lane >> 5;
   const int head = blockIdx.x % P.n_heads;
   const int tile = gridDim.x / P.n_heads - 1 - blockIdx.x / P.n_heads;  // long rows first
-  // sequence b owns the tiles from q_begin[b] / kBM + b on: room for all of its queries
-  int lo = 0, hi = P.n_seqs - 1;
-  while (lo < hi) {
-    const int mid = (lo + hi + 1) >> 1;
-    if (min(max(P.q_begin[mid], 0), P.n_q_rows) / kBM + mid <= tile) lo = mid; else hi = mid - 1;
-  }
-  const Seq s = sequence(P, lo);
-  const int first = (tile - (s.q0 / kBM + lo)) * kBM;
+  int first;
+  const Seq s = sequence_of(P, tile, kBM, first);
   if (first < 0 || first >= s.nq) return;
   const int i = first + wave * 32 + col;       // this lane's query
   const bool live = i < s.nq;
@@ -343,8 +384,9 @@ __global__ __launch_bounds__(kThreads, kD == 64 ? 3 : 2) void attend_tile_kernel
     py = P.q_pos[2 * row + 1];
   }
   const int x0 = __builtin_amdgcn_readfirstlane(px), y0 = __builtin_amdgcn_readfirstlane(py);
-  const float steep = fabsf(slope2);
-  const float fx = static_cast<float>(px - x0) * steep, fy = static_cast<float>(py - y0) * steep;
+  const float fx = apart(px, x0), fy = apart(py, y0);
+  const bool late = !P.capped && P.to_log2 >= 0x1p-20f;
+  const float rate = late ? slope2 / P.to_log2 : slope2;
   int wave_lo = INT_MAX, wave_hi = -1;  // the documents of the wave's queries
   int block_lo = INT_MAX, block_hi = -1;
   if (with_docs) {
@@ -381,19 +423,36 @@ __global__ __launch_bounds__(kThreads, kD == 64 ? 3 : 2) void attend_tile_kernel
       __syncthreads();
       for (int t = threadIdx.x; t < kMaskTiles / 64; t += kThreads) s_use[t] = 0;
       __syncthreads();
-      constexpr int kAhead = 8;  // tiles of a wave whose documents are under way
-      for (int t0 = seg + wave * kAhead; t0 < seg_end; t0 += kWaves * kAhead) {
-        int kd[kAhead];
+      // 4 keys a lane and 4 tiles a load, 8 loads under way
+      constexpr int kAhead = 8, kTurn = 4 * kAhead;
+      for (int t0 = seg + wave * kTurn; t0 < seg_end; t0 += kWaves * kTurn) {
+        i32x4 kd[kAhead];
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
-          const int j = (t0 + u) * kBN + lane;
-          kd[u] = t0 + u < seg_end && j < end ? P.k_doc[s.k0 + j] : -1;
+          const int j = (t0 + 4 * u) * kBN + 4 * lane;
+          kd[u] = i32x4{-1, -1, -1, -1};
+          if (t0 + 4 * u < seg_end) {
+            if (j + 3 < end) {
+              __builtin_memcpy(&kd[u], P.k_doc + s.k0 + j, 16);
+            } else {
+#pragma unroll
+              for (int e = 0; e < 3; ++e)
+                if (j + e < end) kd[u][e] = P.k_doc[s.k0 + j + e];
+            }
+          }
         }
         uint32_t used = 0;
 #pragma unroll
-        for (int u = 0; u < kAhead; ++u)
-          used |= (__ballot(kd[u] >= block_lo && kd[u] <= block_hi) ? 1u : 0u) << u;
-        if (used && lane == 0)  // 8 tiles from a multiple of 8 on: within one word
+        for (int u = 0; u < kAhead; ++u) {
+          bool in = false;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) in = in || (kd[u][e] >= block_lo && kd[u][e] <= block_hi);
+          const uint64_t lanes = __ballot(in);
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            used |= ((lanes >> (16 * e)) & 0xFFFF ? 1u : 0u) << (4 * u + e);
+        }
+        if (used && lane == 0)  // 32 tiles from a multiple of 32 on: within one word
           atomicOr(reinterpret_cast<unsigned long long *>(&s_use[(t0 - seg) >> 6]),
                    static_cast<unsigned long long>(used) << ((t0 - seg) & 63));
       }
@@ -478,50 +537,40 @@ __global__ __launch_bounds__(kThreads, kD == 64 ? 3 : 2) void attend_tile_kernel
                   -slope2 * fabsf(here - static_cast<float>((e >> 2) * 8 + (e & 3))));
           }
         } else {
-          // what brings a score to log2 units: here, with the bias, or with the weight
-          float scale = 1.0f;
+          // what brings a score to log2 units comes with the weight, if it can be undone in the bias
           if (P.capped) {
 #pragma unroll
             for (int e = 0; e < 32; ++e) z[e >> 4][e & 15] = cap_score(P, z[e >> 4][e & 15]);
-          } else if (P.slope) {
-            scale = P.to_log2;
-          } else if (P.shaped) {
+          } else if (late) {
+            factor = P.to_log2;
+          } else {
 #pragma unroll
             for (int e = 0; e < 32; ++e) z[e >> 4][e & 15] *= P.to_log2;
-          } else {
-            factor = P.to_log2;
           }
           if (P.slope && !with_pos) {
             const float here = static_cast<float>(place - j0 - 4 * half);
 #pragma unroll
             for (int e = 0; e < 32; ++e)
               z[e >> 4][e & 15] = __builtin_fmaf(
-                  z[e >> 4][e & 15], scale,
-                  -slope2 * fabsf(here - static_cast<float>((e >> 2) * 8 + (e & 3))));
+                  -rate, fabsf(here - static_cast<float>((e >> 2) * 8 + (e & 3))),
+                  z[e >> 4][e & 15]);
           } else if (P.slope) {
-            float tmp[32];
-            // both places from the wave's first query on, times |slope|: two subtractions and two
-            // additions a score
-            s_far[wave][0][lane] = static_cast<float>(s_pos[buf][0][lane] - x0) * steep;
-            s_far[wave][1][lane] = static_cast<float>(s_pos[buf][1][lane] - y0) * steep;
+            s_far[wave][0][lane] = apart(s_pos[buf][0][lane], x0);
+            s_far[wave][1][lane] = apart(s_pos[buf][1][lane], y0);
             __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
             __builtin_amdgcn_wave_barrier();
             __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-            const float sign = slope2 < 0.0f ? 1.0f : -1.0f;
 #pragma unroll
             for (int e = 0; e < 32; e += 4) {
               const int j = (e >> 2) * 8 + 4 * half;
               const f32x4 kx = *reinterpret_cast<const f32x4 *>(&s_far[wave][0][j]);
               const f32x4 ky = *reinterpret_cast<const f32x4 *>(&s_far[wave][1][j]);
 #pragma unroll
-              for (int r = 0; r < 4; ++r) {
-                float &ze = tmp[e + r];
-                ze = __builtin_fmaf(z[e >> 4][(e & 15) + r], scale, sign * fabsf(kx[r] - fx));
-                ze = __builtin_fmaf(sign, fabsf(ky[r] - fy), ze);
-              }
+              for (int r = 0; r < 4; ++r)
+                z[e >> 4][(e & 15) + r] =
+                    __builtin_fmaf(-rate, fabsf(kx[r] - fx) + fabsf(ky[r] - fy),
+                                   z[e >> 4][(e & 15) + r]);
             }
-#pragma unroll
-            for (int e = 0; e < 32; ++e) z[e >> 4][e & 15] = tmp[e];
           }
         }
         // a factor < 0 turns the order round
@@ -667,15 +716,7 @@ __device__ __forceinline__ Parts find_parts(const AttendParams &P, int part, int
       r.seq = u * 64 + l;
       r.count = __shfl(mine, l);
       r.first = before + __shfl(upto, l) - r.count;
-      const auto take = [&](int v) { return __builtin_amdgcn_readlane(v, l); };
-      r.s.q0 = take(all[u].q0);
-      r.s.nq = take(all[u].nq);
-      r.s.k0 = static_cast<int64_t>(
-          static_cast<uint64_t>(static_cast<uint32_t>(take(static_cast<int>(all[u].k0 >> 32)))) << 32 |
-          static_cast<uint32_t>(take(static_cast<int>(all[u].k0))));
-      r.s.nk = take(all[u].nk);
-      r.s.place0 = take(all[u].place0);
-      r.s.prefix = take(all[u].prefix);
+      r.s = broadcast(all[u], l);
     }
     before += __shfl(upto, 63);
   }
@@ -785,8 +826,8 @@ __global__ __launch_bounds__(kFewWaves * 64) void attend_few_kernel(const Attend
         const int at = (e >> 2) * 16 + 4 * quad + (e & 3);
         float far = 0.0f;
         if (P.slope)
-          far = static_cast<float>(P.k_pos ? abs_diff(px, marks[1][at]) + abs_diff(py, marks[2][at])
-                                           : abs_diff(place, j0 + at));
+          far = P.k_pos ? abs_diff(px, marks[1][at]) + abs_diff(py, marks[2][at])
+                        : abs_diff(place, j0 + at);
         z[e >> 2][e & 3] = shape(P, z[e >> 2][e & 3], slope2, far);
       }
     }

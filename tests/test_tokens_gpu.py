@@ -339,6 +339,22 @@ def test_attend(shape, kind, dtype):
     R.assert_within(got, want, bound, "attend")
 
 
+@pytest.mark.parametrize("places", ["index", "pos"])
+@pytest.mark.parametrize("q_len", [1, 90])
+def test_attend_slopes_of_any_sign(q_len, places):
+    """Nearer keys less, and heads without a bias, beside the usual ones; far and negative places."""
+    say("attend slopes", q_len, places)
+    g, q, k, v, qb, kb = make(21, [q_len], [150], 4, 2, 64, "bf16")
+    f = dict(slope=torch.tensor([-0.05, 0.0, 0.3, -0.2]))
+    if places == "pos":
+        f["q_pos"] = torch.randint(-30, 30, (q_len, 2), generator=g, dtype=torch.int32) + 100000
+        f["k_pos"] = torch.randint(-30, 30, (150, 2), generator=g, dtype=torch.int32) + 100000
+        f["k_pos"][::7] -= 50
+        f["k_pos"][3] = -(1 << 31)
+    want, bound = R.attend(q, k, v, qb, kb, [150], 0.125, **f)
+    R.assert_within(run_attend(q, k, v, qb, kb, [150], 0.125, **f), want, bound, "attend")
+
+
 @pytest.mark.parametrize("scale", [-0.2, 0.0, 3.0])
 @pytest.mark.parametrize("q_len", [1, 90])
 def test_attend_scales(q_len, scale):

@@ -2,8 +2,7 @@
 bounds on what 32-bit sums and one rounding may differ from them (test infrastructure)."""
 from __future__ import annotations
 
-import math
-
+import numpy as np
 import torch
 
 UNIT = {torch.float16: 2.0 ** -11, torch.bfloat16: 2.0 ** -8}  # half an ulp, relative
@@ -77,7 +76,7 @@ def attend(q, k, v, q_begin, kv_begin, kv_len, scale, cap=0.0, causal=False, pre
             js = j[see]
             far = (js - place).abs().double()
             if k_pos is not None:
-                far = (k_pos[k0 + js] - q_pos[i]).abs().sum(-1).double()
+                far = (k_pos[k0 + js].double() - q_pos[i].double()).abs().sum(-1)
             for h in range(q.shape[1]):
                 kr, vr = k[k0 + js, h // group].double(), v[k0 + js, h // group].double()
                 qi = q[i, h].double()
@@ -97,7 +96,7 @@ def attend(q, k, v, q_begin, kv_begin, kv_len, scale, cap=0.0, causal=False, pre
                     (torch.where(p > 1e-12, ez, torch.zeros_like(ez))).max())
                 mag = p @ vr.abs()
                 out[i, h] = p @ vr
-                bound[i, h] += u * out[i, h].abs() + (u + 2 * math.expm1(2 * e)
+                bound[i, h] += u * out[i, h].abs() + (u + 2 * np.expm1(2 * e)
                                                       + (n + 8) * E32) * mag
     return out, bound
 
