@@ -46,6 +46,7 @@ struct ProjectParams {
   void *h;           // [n_tokens][2][pad_rank] of the type
   float *h32;        // [n_tokens][pad_rank]
   int32_t gather;    // adapters are added by add_gathered
+  int32_t b_whole;   // all of b is within the reach of one buffer
   float *part;       // [splits][n_tokens][part_stride]: sums over a cut of k
   int32_t part_stride, splits, low_blocks;
   int32_t tiles_t, tiles_n;
@@ -508,16 +509,24 @@ __global__ __launch_bounds__(kWt *kWn * 64, 2) void project_kernel(const Project
                static_cast<uint32_t>(k0) * 2);
     }
   };
-  const int per = (2 * P.pad_rank + kBK - 1) / kBK;  // steps of an adapter
+  // values of k that an adapter has of the steps: whole steps, or part of one that others share,
+  // where one buffer holds all of b
+  const int wide = 2 * P.pad_rank;
+  const int slot = P.b_whole ? wide : (wide + kBK - 1) / kBK * kBK;
+  const int slot_log2 = 31 - __builtin_clz(slot);
+  int n_low = 0;  // adapters in this tile
   auto fetch_low = [&](int s) {
-    const int a = (s - main_steps) / per, part = (s - main_steps) - a * per;
-    const int g = s < steps ? __builtin_amdgcn_readfirstlane(s_list[a]) : 0;
-    const int e = part * kBK + chunk * 8, r = e & (P.pad_rank - 1);
+    const int at_k = (s - main_steps) * kBK + chunk * 8;
+    const int a = at_k >> slot_log2, e = at_k & (slot - 1), r = e & (P.pad_rank - 1);
+    const bool in = a < n_low && e < wide;
+    const int g = in ? s_list[a] : 0;
+    const int g0 = P.b_whole ? 0 : __builtin_amdgcn_readfirstlane(g);
     const auto hb = buffer(static_cast<const E *>(P.h) + int64_t(t0) * 2 * P.pad_rank,
                            static_cast<uint32_t>(xr) * 4 * P.pad_rank);
-    const auto bb = buffer(static_cast<const E *>(P.b) + int64_t(g) * P.n * P.b_rank,
-                           static_cast<uint32_t>(P.n) * P.b_rank * 2);
-    const bool in = s < steps && e < 2 * P.pad_rank;
+    const auto bb =
+        buffer(static_cast<const E *>(P.b) + int64_t(g0) * P.n * P.b_rank,
+               static_cast<uint32_t>(P.b_whole ? P.n_adapters : 1) * P.n * P.b_rank * 2);
+    const uint32_t from = static_cast<uint32_t>(g - g0) * P.n + n0 - kT;
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
       const int first = (i * kWaves + wave) * kPer, row = first + lane / kChunks;
@@ -525,7 +534,7 @@ __global__ __launch_bounds__(kWt *kWn * 64, 2) void project_kernel(const Project
       if (first < kT) {
         if (in && s_id[row] == g) off = static_cast<uint32_t>((row * 2 * P.pad_rank + e) * 2);
       } else if (in && r < P.rank && n0 + row - kT < P.n) {
-        off = (static_cast<uint32_t>(n0 + row - kT) * P.b_rank + r) * 2;
+        off = ((from + row) * P.b_rank + r) * 2;
       }
       load_lds(first < kT ? hb : bb, &tile[s % kStages][first * kBK], off, 0);
     }
@@ -590,9 +599,10 @@ __global__ __launch_bounds__(kWt *kWn * 64, 2) void project_kernel(const Project
   if (steps_low) {
     if (threadIdx.x < kT) s_id[threadIdx.x] = id;
     __syncthreads();
-    const int n = distinct<kT, kWaves>(s_id, s_heads, s_list, s_counts);
-    gather = kFt * kFn <= 4 && n * per * 4 > P.pad_rank;
-    if (!gather) steps += per * n;
+    n_low = distinct<kT, kWaves>(s_id, s_heads, s_list, s_counts);
+    const int more = (n_low * slot + kBK - 1) / kBK;
+    gather = kFt * kFn <= 4 && more * 4 > P.pad_rank;
+    if (!gather) steps += more;
     for (int s = begun; s < kStages; ++s) fetch_low(s);
   }
   wait_and_meet<(kStages - 1) * kLoads>();
@@ -775,6 +785,7 @@ int launch(ProjectParams P, const Few &few, void *packed, hipStream_t s) {
   const auto tiles = [&](int t, int n) {
     return ((int64_t(P.n_tokens) + t - 1) / t) * ((int64_t(P.n) + n - 1) / n);
   };
+  P.b_whole = int64_t(P.n_adapters) * P.n * P.b_rank * 2 < (int64_t(1) << 31);
   P.gather = P.adapter && P.b_apart;  // rows of b that a load to LDS cannot take
   if (P.gather) rc = launch_tiles<kType, 64, 64, 2, 2, 64, 4>(P, s);
   else if (tiles(128, 128) >= 256) {
