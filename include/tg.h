@@ -25,7 +25,8 @@
  *    has enqueued nothing.
  *  - Device buffers need only their natural alignment (4 bytes for int32/float, 2 for
  *    fp16); tg_stitch takes a faster path when `out` is 16-byte aligned and
- *    canvas_w * canvas_h is a multiple of 8.
+ *    canvas_w * canvas_h is a multiple of 8. The token operators ask for more where they
+ *    say so.
  */
 #ifndef TG_H
 #define TG_H
@@ -556,7 +557,7 @@ int tg_mask_rois(const tg_mask_rois_args *args, void *stream);
  *
  * Values are binary16 or bfloat16, sums, norms and softmax statistics binary32, and each
  * result is rounded once to nearest-even. Strides are in elements, the last dimension is
- * contiguous.
+ * contiguous. A call whose workgroups one launch cannot hold (2^31) returns TG_E_INVAL.
  */
 enum tg_type {
   TG_F16 = 0, /* binary16 */
@@ -568,9 +569,9 @@ enum tg_type {
 
 typedef struct {
   const void *x;          /* device: token t's row is x + t * x_stride, k values */
-  int64_t x_stride;       /* >= k */
+  int64_t x_stride;       /* k .. 2^22, a multiple of 8 */
   const void *w;          /* device: output j's row is w + j * w_stride, k values */
-  int64_t w_stride;       /* >= k */
+  int64_t w_stride;       /* k .. 2^22, a multiple of 8 */
   const int32_t *adapter; /* device [n_tokens]: adapter of each token; outside
                              [0, n_adapters) the token has none. NULL: no token has one */
   const void *a;          /* device [n_adapters][rank][k] */
@@ -601,9 +602,9 @@ size_t tg_project_workspace_bytes(int32_t n_tokens, int32_t k, int32_t n, int32_
  * two values of the type each, the rounded one and what that left, or in binary32; everything
  * else is summed in binary32.
  * Enqueued on `stream`; the library allocates nothing. Returns TG_E_INVAL (null pointer,
- * negative count, k < 1 or not a multiple of 8, n < 1, rank outside [1, TG_PROJECT_MAX_RANK]
- * with adapters, a bad type or stride, x, w or a not 16-byte aligned or with a stride that is
- * not a multiple of 8), TG_E_WORKSPACE, TG_E_HIP. n_tokens == 0 enqueues nothing.
+ * negative count, k < 1 or not a multiple of 8, n < 1, with adapters n > 2^23 or a rank outside
+ * [1, TG_PROJECT_MAX_RANK], a bad type or stride, x, w or a not 16-byte aligned),
+ * TG_E_WORKSPACE, TG_E_HIP. n_tokens == 0 enqueues nothing.
  */
 int tg_project(const tg_project_args *args, void *stream);
 
@@ -642,11 +643,10 @@ typedef struct {
  * p = pos[t][0], or with two axes p = pos[t][floor(2 i / (rot / 2))]: the first half of the
  * pairs turns with the first axis, the rest with the second. The other d - rot values are
  * normalised only. Keys, and with v_out the values (copied as they are), can go to rows of a
- * cache instead; two tokens with the same row leave one or the other's whole value row and
- * key row, in no set order. An output may be its own input (same pointer and strides, no
+ * cache instead; two tokens with the same row leave a mix of both there. An output may be its own input (same pointer and strides, no
  * slot) and must not overlap another. Enqueued on `stream`; allocates nothing. Returns
  * TG_E_INVAL (null pointer, negative count, d outside [2, 512] or odd, bad rot, axes, type,
- * eps, or n_positions < 1 while rot > 0), TG_E_HIP. n_tokens == 0 enqueues nothing.
+ * eps, more than 2^20 heads, or n_positions < 1 while rot > 0), TG_E_HIP. n_tokens == 0 enqueues nothing.
  */
 int tg_rotate(const tg_rotate_args *args, void *stream);
 
@@ -670,8 +670,9 @@ typedef struct {
   const int32_t *q_doc;      /* device [n_q_rows] and [n_k_rows], both or neither: a query sees */
   const int32_t *k_doc;      /* keys of its own document only; documents < 0 see nothing */
   const int32_t *q_pos;      /* device [n_q_rows][2] and [n_k_rows][2], both or neither: */
-  const int32_t *k_pos;      /* positions the distance is taken from */
-  const float *slope;        /* device [n_heads] or NULL: bias per unit of distance */
+  const int32_t *k_pos;      /* positions the distance is taken from; not read without slope */
+  const float *slope;        /* device [n_heads] or NULL: bias per unit of distance, of any sign;
+                                distances up to 2^24 are exact */
   float scale;               /* finite */
   float cap;                 /* > 0: scores are capped; 0: not */
   int32_t causal;            /* nonzero: a query sees keys up to its own place */
@@ -699,13 +700,14 @@ size_t tg_attend_workspace_bytes(int32_t n_seqs, int32_t n_q_rows, int32_t max_q
  * it sees key j when j <= p or j < prefix[s] or not causal, and its document is the key's
  * (and >= 0). The output is the softmax-weighted sum of the visible v_j, 0 for a query that
  * sees no key; keys and values it does not see do not reach it, whatever they hold. Weights
- * are rounded to the type before the product with v, their sum is not.
+ * are rounded to the type before the product with v, and their sum, in binary32, is of the
+ * rounded ones, so that the weights of a row make 1.
  * Rows outside [0, n_q_rows) and [0, n_k_rows) are not read or written, whatever q_begin,
  * kv_begin and kv_len say. out must not overlap an input. Enqueued on `stream`; allocates
  * nothing. Returns TG_E_INVAL (null pointer, negative count, d outside [8, TG_ATTEND_MAX_D]
  * or not a multiple of 8, heads that n_kv_heads does not divide, a bad type, scale or cap,
- * one of a pair missing, prefix without causal, q, k, v or out not 16-byte aligned or with a
- * stride that is not a multiple of 8), TG_E_WORKSPACE, TG_E_HIP. n_seqs == 0 or
+ * one of a pair missing, prefix without causal, q, k, v or out not 16-byte aligned, a stride that
+ * is negative, not a multiple of 8 or, of rows, over 2^22), TG_E_WORKSPACE, TG_E_HIP. n_seqs == 0 or
  * n_q_rows == 0 enqueues nothing.
  */
 int tg_attend(const tg_attend_args *args, void *stream);

@@ -8,10 +8,12 @@
 //
 // Nothing is reused but the table's row, so memory bounds it: a head is read once into
 // registers, and written once, past the caches where they could not keep it (131,072 tokens, 18
-// heads of 128, 1.2 GB in and out: 290 us, 4.4 TB/s; through the caches 313). Lanes hold 2 x 8 values, the two chunks whose values are each
-// other's partners, so that a turn needs no exchange between lanes; the sum of squares is the
-// only one. A wave takes a token and goes over its heads, which share the table's row; with
-// few tokens the heads of a token are spread over waves instead.
+// heads of 128, 1.2 GB in and out: 291 us, 4.2 TB/s where a large copy reaches 4.85; through the
+// caches 313). Lanes hold 2 x 8 values, the two chunks whose values are each other's partners, so
+// that a turn needs no exchange between lanes; the sum of squares is the only one. A wave takes a
+// token and goes over its heads, which share the table's row; where a token's heads do not fill a
+// wave it takes several tokens, and with few tokens the heads are spread over waves instead (20
+// tokens, 24 heads: 4 us, a launch).
 #include <hip/hip_runtime.h>
 
 #include <cmath>
