@@ -636,17 +636,18 @@ typedef struct {
 } tg_rotate_args;
 
 /*
- * Norm and position rotation of queries and keys, per head, in one pass: with
- * u = v * weight / sqrt(mean(v^2) + eps) over the d values of a head, pair i of the leading
- * `rot` values turns by the angle whose cosine and sine are table[p][i],
+ * Norm and position rotation of queries and keys, per head, in one pass: with u = v * weight /
+ * sqrt(mean(v^2) + eps) over the d values of a head, pair i of the leading `rot` values turns
+ * by the angle whose cosine and sine are table[p][i],
  *   (u_a, u_b) -> (u_a cos - u_b sin, u_a sin + u_b cos),
  * p = pos[t][0], or with two axes p = pos[t][floor(2 i / (rot / 2))]: the first half of the
  * pairs turns with the first axis, the rest with the second. The other d - rot values are
  * normalised only. Keys, and with v_out the values (copied as they are), can go to rows of a
- * cache instead; two tokens with the same row leave a mix of both there. An output may be its own input (same pointer and strides, no
- * slot) and must not overlap another. Enqueued on `stream`; allocates nothing. Returns
- * TG_E_INVAL (null pointer, negative count, d outside [2, 512] or odd, bad rot, axes, type,
- * eps, more than 2^20 heads, or n_positions < 1 while rot > 0), TG_E_HIP. n_tokens == 0 enqueues nothing.
+ * cache instead; two tokens with the same row leave a mix of both there. An output may be its
+ * own input (same pointer and strides, no slot) and must not overlap another. Enqueued on
+ * `stream`; allocates nothing. Returns TG_E_INVAL (null pointer, negative count, d outside [2,
+ * 512] or odd, bad rot, axes, type, eps, more than 2^20 heads, or n_positions < 1 while rot >
+ * 0), TG_E_HIP. n_tokens == 0 enqueues nothing.
  */
 int tg_rotate(const tg_rotate_args *args, void *stream);
 
@@ -693,22 +694,21 @@ size_t tg_attend_workspace_bytes(int32_t n_seqs, int32_t n_q_rows, int32_t max_q
                                  int32_t d);
 
 /*
- * Attention over a ragged batch. Query i of sequence s stands at place
- * p = kv_len[s] - queries + i. Its score with key j is
+ * Attention over a ragged batch. Query i of sequence s stands at place p = kv_len[s] - queries
+ * + i. Its score with key j is
  *   z = scale * (q . k_j);  with cap z = cap * tanh(z / cap);
  *   with slope z -= slope[h] * distance, |p - j|, or |xq - xk| + |yq - yk| of the positions;
- * it sees key j when j <= p or j < prefix[s] or not causal, and its document is the key's
- * (and >= 0). The output is the softmax-weighted sum of the visible v_j, 0 for a query that
- * sees no key; keys and values it does not see do not reach it, whatever they hold. Weights
- * are rounded to the type before the product with v, and their sum, in binary32, is of the
- * rounded ones, so that the weights of a row make 1.
- * Rows outside [0, n_q_rows) and [0, n_k_rows) are not read or written, whatever q_begin,
- * kv_begin and kv_len say. out must not overlap an input. Enqueued on `stream`; allocates
- * nothing. Returns TG_E_INVAL (null pointer, negative count, d outside [8, TG_ATTEND_MAX_D]
- * or not a multiple of 8, heads that n_kv_heads does not divide, a bad type, scale or cap,
- * one of a pair missing, prefix without causal, q, k, v or out not 16-byte aligned, a stride that
- * is negative, not a multiple of 8 or, of rows, over 2^22), TG_E_WORKSPACE, TG_E_HIP. n_seqs == 0 or
- * n_q_rows == 0 enqueues nothing.
+ * it sees key j when j <= p or j < prefix[s] or not causal, and its document is the key's (and
+ * >= 0). The output is the softmax-weighted sum of the visible v_j, 0 for a query that sees no
+ * key; keys and values it does not see do not reach it, whatever they hold. Weights are
+ * rounded to the type before the product with v, and their sum, in binary32, is of the rounded
+ * ones, so that the weights of a row make 1. Rows outside [0, n_q_rows) and [0, n_k_rows) are
+ * not read or written, whatever q_begin, kv_begin and kv_len say. out must not overlap an
+ * input. Enqueued on `stream`; allocates nothing. Returns TG_E_INVAL (null pointer, negative
+ * count, d outside [8, TG_ATTEND_MAX_D] or not a multiple of 8, heads that n_kv_heads does not
+ * divide, a bad type, scale or cap, one of a pair missing, prefix without causal, q, k, v or
+ * out not 16-byte aligned, a stride that is negative, not a multiple of 8 or, of rows, over
+ * 2^22), TG_E_WORKSPACE, TG_E_HIP. n_seqs == 0 or n_q_rows == 0 enqueues nothing.
  */
 int tg_attend(const tg_attend_args *args, void *stream);
 
