@@ -22,6 +22,7 @@
 // is not finite is computed again by strict_row, which leaves unseen keys out one by one.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <climits>
 #include <cmath>
 #include <cstdint>
@@ -59,6 +60,9 @@ struct AttendParams {
   int32_t causal, n_seqs, n_q_rows;
   int64_t n_k_rows;
   int32_t max_q, max_kv, n_heads, n_kv_heads, group, d;
+  // attend_tile_kernel
+  int32_t splits;   // workgroups that share a tile's keys; with more than one, parts are laid out
+                    // as [splits][n_q_rows][n_heads][d], and [..][..][..][2]
   // attend_few_kernel
   int32_t row_tiles;
   int32_t width;    // parts that all keys are cut into, 0: no sequence is cut
@@ -321,6 +325,7 @@ __device__ __forceinline__ typename Num<kType>::V4 read_transposed(const void *p
 // ------------------------------------------------------------------- 128 queries of a head
 
 constexpr int kBM = 128, kBN = 64;
+constexpr int kCus = 256;
 constexpr int kMaskTiles = 4096;  // key tiles whose documents are looked through at once
 
 // What is done to a score between the products, decided when compiled where it is common.
@@ -364,7 +369,12 @@ __global__ __launch_bounds__(kThreads, kD == 64 ? 3 : 2) void attend_tile_kernel
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int col = lane & 31, half = lane >> 5;
   const int head = blockIdx.x % P.n_heads;
-  const int tile = gridDim.x / P.n_heads - 1 - blockIdx.x / P.n_heads;  // long rows first
+  // Long rows first; workgroups 256 to 511 the other way round, as they share a CU with those 256
+  // before them
+  const int turns = gridDim.x / P.n_heads, round = kCus / P.n_heads;
+  int turn = blockIdx.x / P.n_heads;
+  if (turn >= round && turn < 2 * round) turn = round + min(2 * round, turns) - 1 - turn;
+  const int split = turn % P.splits, tile = (turns - 1 - turn) / P.splits;
   int first;
   const Seq s = sequence_of(P, tile, kBM, first);
   if (first < 0 || first >= s.nq) return;
@@ -427,9 +437,13 @@ __global__ __launch_bounds__(kThreads, kD == 64 ? 3 : 2) void attend_tile_kernel
   const uint32_t v_off = row_offset<kChunks, false>(P.v_stride, P.d, first_row);
   f32x16 acc[kBlocks] = {};
   float m = -INFINITY, l = 0.0f;
-  const int tiles = (end + kBN - 1) / kBN;
+  int tiles = (end + kBN - 1) / kBN, from = 0;
+  if (P.splits > 1) {
+    from = static_cast<int>(int64_t(tiles) * split / P.splits);
+    tiles = static_cast<int>(int64_t(tiles) * (split + 1) / P.splits);
+  }
 
-  for (int seg = 0; seg < tiles; seg += kMaskTiles) {
+  for (int seg = from; seg < tiles; seg += kMaskTiles) {
     const int seg_end = min(tiles, seg + kMaskTiles);
     if (with_docs) {  // which tiles hold a key whose document is in the queries' range
       __syncthreads();
@@ -651,6 +665,25 @@ __global__ __launch_bounds__(kThreads, kD == 64 ? 3 : 2) void attend_tile_kernel
   }
 
   l += __shfl_xor(l, 32);
+  if (P.splits > 1) {
+    const int64_t to = (int64_t(split) * P.n_q_rows + row) * P.n_heads + head;
+    if (!live) return;
+    if (half == 0) {
+      P.part_ml[to * 2] = m;
+      P.part_ml[to * 2 + 1] = l;
+    }
+    if (m == -INFINITY) return;  // the sums are not looked at
+#pragma unroll
+    for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+      for (int r4 = 0; r4 < 4; ++r4) {
+        const int c = b * 32 + r4 * 8 + 4 * half;
+        if (c < P.d)
+          *reinterpret_cast<f32x4 *>(P.part + to * P.d + c) =
+              f32x4{acc[b][r4 * 4], acc[b][r4 * 4 + 1], acc[b][r4 * 4 + 2], acc[b][r4 * 4 + 3]};
+      }
+    return;
+  }
   const float inv = l == 0.0f ? 0.0f : 1.0f / l;
   bool fine = true;
   E *o = static_cast<E *>(P.out) + row * P.out_stride + head * P.out_head;
@@ -671,6 +704,74 @@ __global__ __launch_bounds__(kThreads, kD == 64 ? 3 : 2) void attend_tile_kernel
   bad = (bad | (bad >> 32)) & 0xFFFFFFFFull;
   for (; bad; bad &= bad - 1)
     strict_row<kType>(P, s, wave_first + __builtin_ctzll(bad), head);
+}
+
+// Joins the parts of a tile's rows, 32 rows of a head a workgroup, 32 lanes a row with 4 values
+// each.
+constexpr int kMaxSplits = 16, kJoinRows = 32;
+template <int kType>
+__global__ __launch_bounds__(kThreads) void join_tile_kernel(const AttendParams P) {
+  typedef typename Num<kType>::E E;
+  typedef typename Num<kType>::V4 V4;
+  constexpr int kEach = kJoinRows * 32 / kThreads, kStep = kThreads / 32;
+  const int c = (threadIdx.x & 31) * 4, group = threadIdx.x >> 5;
+  const int head = blockIdx.x % P.n_heads, id = blockIdx.x / P.n_heads;
+  int first;
+  const Seq s = sequence_of(P, id / (kBM / kJoinRows), kBM, first);
+  if (first < 0) return;
+  first += id % (kBM / kJoinRows) * kJoinRows;
+  if (first >= s.nq) return;
+  float pm[kEach][kMaxSplits], pl[kEach][kMaxSplits];
+  f32x4 sum[kEach];
+  uint32_t bad = 0;
+#pragma unroll
+  for (int u = 0; u < kEach; ++u) {
+    const int i = min(first + u * kStep + group, s.nq - 1);
+    const int64_t at = (int64_t(s.q0) + i) * P.n_heads + head;
+    const int64_t step = int64_t(P.n_q_rows) * P.n_heads;
+#pragma unroll
+    for (int k = 0; k < kMaxSplits; ++k) {
+      pm[u][k] = -INFINITY;
+      pl[u][k] = 0.0f;
+      if (k < P.splits) {
+        pm[u][k] = P.part_ml[(k * step + at) * 2];
+        pl[u][k] = P.part_ml[(k * step + at) * 2 + 1];
+      }
+    }
+  }
+#pragma unroll
+  for (int u = 0; u < kEach; ++u) {
+    const int i = first + u * kStep + group;
+    const int64_t at = (int64_t(s.q0) + min(i, s.nq - 1)) * P.n_heads + head;
+    const int64_t step = int64_t(P.n_q_rows) * P.n_heads;
+    float top = -INFINITY, total = 0.0f;
+#pragma unroll
+    for (int k = 0; k < kMaxSplits; ++k) top = fmaxf(top, pm[u][k]);
+    sum[u] = f32x4{};
+#pragma unroll
+    for (int k = 0; k < kMaxSplits; ++k)
+      if (pm[u][k] != -INFINITY) {
+        const float f = __builtin_amdgcn_exp2f(pm[u][k] - top);
+        total += f * pl[u][k];
+        if (c < P.d)
+          sum[u] += f * *reinterpret_cast<const f32x4 *>(P.part + (k * step + at) * P.d + c);
+      }
+    bool fine = true;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      sum[u][q] = total == 0.0f ? 0.0f : sum[u][q] / total;
+      fine = fine && fabsf(sum[u][q]) < INFINITY;
+    }
+    E *o = static_cast<E *>(P.out) + (int64_t(s.q0) + i) * P.out_stride + head * P.out_head;
+    if (i < s.nq && c < P.d) *reinterpret_cast<V4 *>(o + c) = __builtin_convertvector(sum[u], V4);
+    const uint64_t worse = __ballot(!fine && i < s.nq && c < P.d);
+    bad |= ((worse & 0xFFFFFFFFull ? 1u : 0u) | (worse >> 32 ? 2u : 0u)) << (2 * u);
+  }
+  const int low = __builtin_amdgcn_readfirstlane(group);  // the row of the wave's first half
+  for (; bad; bad &= bad - 1) {
+    const int at = __builtin_ctz(bad);
+    strict_row<kType>(P, s, first + (at >> 1) * kStep + low + (at & 1), head);
+  }
 }
 
 // ------------------------------------------------------------------------ few queries
@@ -1042,23 +1143,41 @@ __global__ __launch_bounds__(kThreads, 4) void join_kernel(const AttendParams P)
 // ------------------------------------------------------------------------------- the host
 
 // The form for few queries: 16-row tiles of a key head's rows, and into how many parts the keys
-// of all sequences are cut.
+// of all sequences are cut; or into how many those of a tile of the other form are.
 struct Few {
   bool use;
   int row_tiles, width;
+  int splits;  // of the other form
 };
 
-Few few_of(int n_seqs, int max_q, int max_kv, int n_heads, int n_kv_heads) {
+Few few_of(int n_seqs, int n_q_rows, int max_q, int max_kv, int n_heads, int n_kv_heads, int d,
+            bool causal, bool docs) {
   Few r = {};
   const int64_t rows = int64_t(max_q) * (n_heads / n_kv_heads);
   const int64_t each = n_kv_heads * ((rows + 15) / 16);
-  // Up to 64 rows always; more where the keys are long and the tiles of the other form would be
-  // few, since its workgroups go over all keys one after the other. 16 heads of 128 over 4, this
-  // form against the other: 1 sequence, 32,768 keys, 64 queries 86 : 590 us, 256 queries 255 :
-  // 607; 4 sequences, 64 queries 280 : 598; 16 sequences, 64 queries 1199 : 906. 1,024 keys,
-  // 1 sequence, 64 queries 21 : 24, 128 queries 31 : 25.
-  r.use = rows <= 64 || (max_kv >= 4096 && n_seqs * each <= 256);
-  if (!r.use) return r;
+  r.use = rows <= 64;
+  if (!r.use) {
+    // Tiles' keys are cut where the tiles alone would leave CUs idle: for 768 workgroups, or for 512
+    // where most rows see about half of the keys, of 12 key tiles or more each, since the join
+    // and the parts' way through memory cost about as much as 7. Not with documents, which leave
+    // most tiles out. bfloat16, causal, heads of 128 over a quarter as many, us with 1, 2, 4, 8
+    // and 16 parts:
+    //    16 tiles, 64 queries, 32,768 keys: 591, 310, 166, 100, 77
+    //    96 tiles, 4 times the same:        602, 332, 231, 179, 198
+    //   384 tiles, 16 times the same:       909, 629, 639, 673, 716
+    //    72 tiles, 1,024 queries of 16,384: 303, 169, 101,  92, 113
+    //   132 tiles, 4,096 queries and keys:   79,  54,  43,  52
+    //   272 tiles, 2,048:                    45,  40,  49,  71
+    //   144 tiles, 1,024:                    25,  24,  28,  42
+    //   528 tiles, 4,096:                    92,  97, 115, 182
+    const int64_t blocks = (int64_t(n_q_rows) / kBM + n_seqs) * n_heads;
+    const int64_t key_tiles = (int64_t(max_kv) + kBN - 1) / kBN;
+    const int64_t want = causal && max_q > max_kv / 2 ? 512 : 768;
+    const int64_t splits =
+        std::min({(want + blocks / 2) / blocks, key_tiles / 12, int64_t(kMaxSplits)});
+    r.splits = docs || splits < 1 ? 1 : static_cast<int>(splits);
+    return r;
+  }
   r.row_tiles = static_cast<int>((rows + 15) / 16);
   const int64_t want = kFewWorkgroups;
   if (n_seqs <= kMaxCut && n_seqs * each < want && max_kv > 2 * kMinPart)
@@ -1078,9 +1197,9 @@ int launch(const AttendParams &P, const Few &few, hipStream_t s) {
       hipLaunchKernelGGL(join_kernel<kType>, dim3(static_cast<uint32_t>(joined)), dim3(kThreads), 0,
                          s, P);
   } else {
-    const int64_t blocks = (int64_t(P.n_q_rows) / kBM + P.n_seqs) * P.n_heads;
-    if (blocks > INT32_MAX) return TG_E_INVAL;
-    const dim3 grid(static_cast<uint32_t>(blocks)), threads(kThreads);
+    const int64_t tiles = (int64_t(P.n_q_rows) / kBM + P.n_seqs) * P.n_heads;
+    if (tiles * P.splits > INT32_MAX) return TG_E_INVAL;
+    const dim3 grid(static_cast<uint32_t>(tiles * P.splits)), threads(kThreads);
     const bool any = P.k_doc || P.k_pos || P.capped == 2 || !(P.to_log2 > 0.0f);
     if (any || (P.capped && P.slope))
       hipLaunchKernelGGL((attend_tile_kernel<kType, kD, kAny>), grid, threads, 0, s, P);
@@ -1090,6 +1209,9 @@ int launch(const AttendParams &P, const Few &few, hipStream_t s) {
       hipLaunchKernelGGL((attend_tile_kernel<kType, kD, kSloped>), grid, threads, 0, s, P);
     else
       hipLaunchKernelGGL((attend_tile_kernel<kType, kD, kPlain>), grid, threads, 0, s, P);
+    if (P.splits > 1)
+      hipLaunchKernelGGL(join_tile_kernel<kType>,
+                         dim3(static_cast<uint32_t>(tiles * (kBM / kJoinRows))), threads, 0, s, P);
   }
   return hipGetLastError() == hipSuccess ? TG_OK : TG_E_HIP;
 }
@@ -1113,8 +1235,13 @@ extern "C" size_t tg_attend_workspace_bytes(int32_t n_seqs, int32_t n_q_rows, in
                                             int32_t n_kv_heads, int32_t d) {
   if (!sizes_ok(n_seqs, n_q_rows, max_q_len, max_kv_len, n_heads, n_kv_heads, d)) return 0;
   if (n_seqs == 0 || n_q_rows == 0 || max_q_len == 0) return 0;
-  const Few few = few_of(n_seqs, max_q_len, max_kv_len, n_heads, n_kv_heads);
-  if (!few.use || few.width == 0) return 0;
+  const Few few = few_of(n_seqs, n_q_rows, max_q_len, max_kv_len, n_heads, n_kv_heads, d,
+                         false, false);
+  if (!few.use)
+    return few.splits > 1 ? static_cast<size_t>(few.splits) * n_q_rows * n_heads * (d + 2) *
+                                sizeof(float)
+                          : 0;
+  if (few.width == 0) return 0;
   return (static_cast<size_t>(few.width) + n_seqs) * n_kv_heads * few.row_tiles * 16 * (d + 2) *
          sizeof(float);
 }
@@ -1135,7 +1262,8 @@ extern "C" int tg_attend(const tg_attend_args *a, void *stream) {
   if (a->n_k_rows > 0 && (!layout_ok(a->k, a->k_stride, a->k_head_stride) ||
                           !layout_ok(a->v, a->v_stride, a->v_head_stride)))
     return TG_E_INVAL;
-  const Few few = few_of(a->n_seqs, a->max_q_len, a->max_kv_len, a->n_heads, a->n_kv_heads);
+  const Few few = few_of(a->n_seqs, a->n_q_rows, a->max_q_len, a->max_kv_len, a->n_heads,
+                         a->n_kv_heads, a->d, a->causal != 0, a->q_doc != nullptr);
   const size_t need = tg_attend_workspace_bytes(a->n_seqs, a->n_q_rows, a->max_q_len,
                                                 a->max_kv_len, a->n_heads, a->n_kv_heads, a->d);
   if (need > 0 && (!a->workspace || a->workspace_bytes < need || !aligned16(a->workspace)))
@@ -1184,8 +1312,11 @@ extern "C" int tg_attend(const tg_attend_args *a, void *stream) {
   P.row_tiles = few.row_tiles;
   P.width = few.width;
   P.part = static_cast<float *>(a->workspace);
-  P.part_ml = P.part + (static_cast<size_t>(few.width) + a->n_seqs) * a->n_kv_heads *
-                           few.row_tiles * 16 * a->d;
+  P.splits = few.splits;
+  P.part_ml =
+      P.part + (few.use ? (static_cast<size_t>(few.width) + a->n_seqs) * a->n_kv_heads *
+                              few.row_tiles * 16 * a->d
+                        : static_cast<size_t>(few.splits) * a->n_q_rows * a->n_heads * a->d);
   hipStream_t s = static_cast<hipStream_t>(stream);
   if (a->d <= 64)
     return a->type == TG_F16 ? launch<TG_F16, 64>(P, few, s) : launch<TG_BF16, 64>(P, few, s);

@@ -464,6 +464,41 @@ def test_attend_tens_of_queries_over_long_keys(q_lens, kv_lens, kind):
     R.assert_within(run_attend(q, k, v, qb, kb, kv_lens, 0.125, **f), want, bound, "attend")
 
 
+CUT = [
+    # few tiles and long keys: the keys of a tile are cut over workgroups
+    ([100, 3, 0, 130], [4000, 3, 900, 2500], 4, 2, 64), ([300], [1600], 2, 1, 128),
+    ([65, 70], [10, 3000], 2, 2, 72), ([129], [900], 1, 1, 40), ([900], [900], 2, 1, 128),
+]
+
+
+@pytest.mark.parametrize("kind", ["plain", "causal", "causal prefix", "cap", "causal bigcap",
+                                  "causal slope", "slope pos", "docs",
+                                  "cap causal slope pos prefix"])
+@pytest.mark.parametrize("shape", range(len(CUT)))
+def test_attend_tiles_whose_keys_are_cut(shape, kind):
+    q_lens, kv_lens, heads, kv, d = CUT[shape]
+    say("attend cut", CUT[shape], kind)
+    dtype = ["f16", "bf16"][shape % 2]
+    g, q, k, v, qb, kb = make(shape, q_lens, kv_lens, heads, kv, d, dtype, gap=shape % 3)
+    f = features(kind, g, q.shape[0], k.shape[0], heads, len(q_lens), kv_lens)
+    want, bound = R.attend(q, k, v, qb, kb, kv_lens, d ** -0.5, **f)
+    got = run_attend(q, k, v, qb, kb, kv_lens, d ** -0.5, **f)
+    R.assert_within(got, want, bound, "attend")
+
+
+@pytest.mark.parametrize("what", ["k", "v"])
+@pytest.mark.parametrize("bad", [NAN, float("inf"), -float("inf")])
+def test_attend_hidden_values_where_keys_are_cut(bad, what):
+    say("attend cut hidden", bad, what)
+    n, n_q, seen = 1700, 140, 1610  # the first 50 queries do not see key 1610
+    g, q, k, v, qb, kb = make(7, [n_q], [n], 4, 2, 64, "bf16", gap=60)
+    want, bound = R.attend(q, k, v, qb, kb, [n], 0.125, causal=True)
+    (k if what == "k" else v)[[seen, seen + 1, n, n + 40]] = bad
+    got = run_attend(q, k, v, qb, kb, [n], 0.125, causal=True)
+    first = n_q - (n - seen)
+    R.assert_within(got[:first], want[:first], bound[:first], "attend")
+
+
 def test_attend_many_documents():
     """More key tiles than are looked through at once, few of them seen."""
     n, d = 300000, 64
