@@ -776,7 +776,9 @@ int launch(ProjectParams P, const Few &few, void *packed, hipStream_t s) {
   }
   // Large problems take the tile with the least time for its rounds: 512 workgroups at once, two
   // a CU (256 with tiles of 256 values of n), and a round of 160 x 128, 192 x 256 and 256 x 256
-  // takes 1.18, 1.37 and 1.64 times one of 128 x 128. Fewer tiles than half a round: smaller ones.
+  // takes 1.18, 1.37 and 1.64 times one of 128 x 128. Up to half a round of those: one a
+  // CU, by 8 waves and with more steps under way; far fewer tiles than CUs: smaller ones, the
+  // smallest where each has a CU.
   // Measured (bfloat16, no adapters, us) with tiles of 256 x 256, 192 x 256, 160 x 128, 128 x 128,
   // the latter with 8 waves, 128 x 64, 64 x 64:
   //   25,600 x 4,096, k 4,096: 700, 753, 721, 795, 851, 974, 1238
@@ -784,17 +786,20 @@ int launch(ProjectParams P, const Few &few, void *packed, hipStream_t s) {
   //   12,000 x 1,024, k 1,024:  34,  28,  36,  33,  35,   36,   45
   //    6,400 x 1,536, k 1,024:  33,  28,  25,  32,  33,   31,   39
   //    2,048 x 4,096, k 4,096:  88,  71,  69,  63,  65,   75,   97
+  //    2,048 x 2,048, k 4,096:                 45,  34,   41,   51
+  //    4,000 x 1,000, k 1,000:                 16,  14,   18,   20
   //    1,777 x 2,048, k 1,160:  37,  32,  23,  20,  17,   20,   25
   //   11,019 x   233, k 2,464:  58,  48,  35,  33,  25,   31,   31
+  //    2,314 x   721, k 3,632:                 45,  36,   27,   33
   //      512 x 4,096, k 4,096:  86,  68,  45,  43,  30,   25,   28
-  //    1,000 x 1,024, k 2,048:  47,  39,  26,  21,  17,   14,   12
+  //    1,000 x 1,024, k 2,048:  47,  39,  26,  21,  17,   13,   10
   const auto tiles = [&](int t, int n) {
     return ((int64_t(P.n_tokens) + t - 1) / t) * ((int64_t(P.n) + n - 1) / n);
   };
   P.b_whole = int64_t(P.n_adapters) * P.n * P.b_rank * 2 < (int64_t(1) << 31);
   P.gather = P.adapter && P.b_apart;  // rows of b that a load to LDS cannot take
   if (P.gather) rc = launch_tiles<kType, 64, 64, 2, 2, 64, 4>(P, s);
-  else if (tiles(128, 128) >= 256) {
+  else if (tiles(128, 128) > 256) {
     const auto rounds = [&](int t, int n, int at_once) { return (tiles(t, n) + at_once - 1) / at_once; };
     const int64_t c256 = 164 * rounds(256, 256, 256), c192 = 137 * rounds(192, 256, 256);
     const int64_t c160 = 118 * rounds(160, 128, 512), c128 = 100 * rounds(128, 128, 512);
@@ -805,7 +810,7 @@ int launch(ProjectParams P, const Few &few, void *packed, hipStream_t s) {
     else rc = launch_tiles<kType, 128, 128, 2, 2, 64, 2>(P, s);
   }
   else if (tiles(128, 128) >= 160) rc = launch_tiles<kType, 128, 128, 2, 4, 64, 4>(P, s);
-  else if (tiles(128, 64) >= 256) rc = launch_tiles<kType, 128, 64, 2, 2, 64, 3>(P, s);
+  else if (tiles(64, 64) > 256) rc = launch_tiles<kType, 128, 64, 2, 2, 64, 3>(P, s);
   else rc = launch_tiles<kType, 64, 64, 2, 2, 64, 4>(P, s);
   if (rc != TG_OK) return rc;
   return hipGetLastError() == hipSuccess ? TG_OK : TG_E_HIP;

@@ -122,7 +122,7 @@ def test_project_keeps_adapters_apart(tokens):
 # enough tiles of each size that the projection chooses from: 64 x 64, 128 x 64, 128 x 128 by 8
 # waves and by 4, 160 x 128, 192 x 256, 256 x 256; each with k that ends inside a step
 TILES = [(300, 1000, 200), (520, 4100, 72), (1777, 2051, 136), (2050, 2100, 72), (4000, 2100, 104),
-         (12000, 1000, 136), (8192, 4096, 40)]
+         (12000, 1000, 136), (8192, 4096, 40), (862, 1317, 504), (2048, 2048, 136)]
 
 
 @pytest.mark.parametrize("dtype,adapters,rank", [("bf16", 6, 16), ("f16", 40, 12), ("f16", 3, 64),
