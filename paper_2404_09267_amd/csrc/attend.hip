@@ -15,7 +15,8 @@
 // not care, as long as V is taken in the same order, which the transposing LDS reads do.
 //
 // attend_tile_kernel takes 128 queries of a head at a time, attend_few_kernel the few queries of
-// all heads that share keys, with long key ranges cut over workgroups and joined by join_kernel.
+// all heads that share keys. Both cut long key ranges over workgroups where there are few, joined
+// by join_tile_kernel and join_kernel.
 //
 // A key that a query does not see has weight 0, and 0 times infinity or NaN would still reach
 // the query's sum. Such sums stay NaN, so each result is looked at once, at the end; a row that
@@ -370,7 +371,8 @@ __global__ __launch_bounds__(kThreads, kD == 64 ? 3 : 2) void attend_tile_kernel
   const int col = lane & 31, half = lane >> 5;
   const int head = blockIdx.x % P.n_heads;
   // Long rows first; workgroups 256 to 511 the other way round, as they share a CU with those 256
-  // before them
+  // before them (4 causal prompts of 2,048, 8 heads of 128: 57 us for 63; 1 of 4,096, 16 heads:
+  // 101 for 104)
   const int turns = gridDim.x / P.n_heads, round = kCus / P.n_heads;
   int turn = blockIdx.x / P.n_heads;
   if (turn >= round && turn < 2 * round) turn = round + min(2 * round, turns) - 1 - turn;
