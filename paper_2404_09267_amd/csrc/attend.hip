@@ -781,7 +781,11 @@ __global__ __launch_bounds__(kThreads) void join_tile_kernel(const AttendParams 
 // How the keys of all sequences are cut: parts of one length, so that every workgroup has as much
 // to read, whatever the lengths are. A wave works it out; the host knows bounds only.
 constexpr int kMaxCut = 256;   // sequences, where any is cut
-constexpr int kMinPart = 128;  // keys of a part
+// Parts have 128 keys at least; where that makes more than one workgroup a place, up to 512, for
+// one workgroup a place; beyond, for three (20 queries, 16 heads of 64 over 4, 1,600 keys each, 256
+// keys a part and not 128: 15.0 us for 17.5; 64 queries, 8 heads of 128 over 2, 1,200 keys each:
+// 27 for 33; 64 queries, 16 heads of 128 over 4, 2,200 keys each, 512 and not 384: 63 for 62).
+constexpr int kMinPart = 128, kOneRound = 512;
 
 struct Parts {
   int chunk;   // keys of a part
@@ -811,8 +815,12 @@ __device__ __forceinline__ Parts find_parts(const AttendParams &P, int part, int
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) total += __shfl_xor(total, o);
   Parts r = {kMinPart, -1, 0, 0, {}};
-  const int64_t even = ((total + P.width - 1) / P.width + 63) / 64 * 64;
-  if (even > r.chunk) r.chunk = static_cast<int>(even);
+  const auto even = [&](int parts) {
+    return static_cast<int>(((total + parts - 1) / parts + 63) / 64 * 64);
+  };
+  const int one = even((P.width + 2) / 3);
+  if (one >= 2 * kMinPart) r.chunk = min(one, kOneRound);
+  r.chunk = max(r.chunk, even(P.width));
   int before = 0;
 #pragma unroll
   for (int u = 0; u < kEach; ++u) {
@@ -1181,8 +1189,13 @@ Few few_of(int n_seqs, int n_q_rows, int max_q, int max_kv, int n_heads, int n_k
     return r;
   }
   r.row_tiles = static_cast<int>((rows + 15) / 16);
+  // Few keys are not cut, as the join's launch costs more: up to 512, or 1,024 where the
+  // sequences alone make 64 workgroups. 16 heads, us cut and not: 20 queries of heads of 64 over 4,
+  // 500 keys 12.4, 8.8, 1,000 keys 13.0, 13.1; of heads of 128, 700 keys 17.7, 15.0; 64 queries, 8
+  // heads of 128 over 2, 1,000 keys 28, 20; but 1 query, 32 heads over 8, 1,000 keys 12.7, 18.6.
   const int64_t want = kFewWorkgroups;
-  if (n_seqs <= kMaxCut && n_seqs * each < want && max_kv > 2 * kMinPart)
+  const int whole = n_seqs * each >= 64 ? 1024 : 512;
+  if (n_seqs <= kMaxCut && n_seqs * each < want && max_kv > whole)
     r.width = static_cast<int>((want + each - 1) / each);
   return r;
 }
