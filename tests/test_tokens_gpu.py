@@ -499,6 +499,18 @@ def test_attend_hidden_values_where_keys_are_cut(bad, what):
     R.assert_within(got[:first], want[:first], bound[:first], "attend")
 
 
+@pytest.mark.parametrize("n_seqs,longest,heads,kv,d", [(33, 1000, 4, 2, 64), (40, 1500, 16, 4, 40),
+                                                      (20, 512, 4, 1, 128), (20, 513, 4, 1, 128)])
+def test_attend_single_tokens_of_many_caches(n_seqs, longest, heads, kv, d):
+    """Keys that are not cut, and parts of more keys than the fewest, with caches of every length."""
+    say("attend many caches", n_seqs, longest)
+    lens = [longest - (longest * i // n_seqs if i % 3 else i % 2) for i in range(n_seqs)]
+    g, q, k, v, qb, kb = make(n_seqs, [1] * n_seqs, lens, heads, kv, d, "bf16", gap=3)
+    f = features("cap causal slope", g, q.shape[0], k.shape[0], heads, n_seqs, lens)
+    want, bound = R.attend(q, k, v, qb, kb, lens, d ** -0.5, **f)
+    R.assert_within(run_attend(q, k, v, qb, kb, lens, d ** -0.5, **f), want, bound, "attend")
+
+
 def test_attend_many_documents():
     """More key tiles than are looked through at once, few of them seen."""
     n, d = 300000, 64
