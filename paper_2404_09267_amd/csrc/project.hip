@@ -526,7 +526,9 @@ __global__ __launch_bounds__(kWt *kWn * 64, 2) void project_kernel(const Project
     const int a = at_k >> slot_log2, e = at_k & (slot - 1), r = e & (P.pad_rank - 1);
     const bool in = a < n_low && e < wide;
     const int g = in ? s_list[a] : 0;
-    const int g0 = P.b_whole ? 0 : __builtin_amdgcn_readfirstlane(g);
+    // the adapter whose b the buffer starts at: with whole steps each, all lanes' of the step
+    const int a0 = (s - main_steps) * kBK >> slot_log2;
+    const int g0 = P.b_whole || a0 >= n_low ? 0 : __builtin_amdgcn_readfirstlane(s_list[a0]);
     const auto hb = buffer(static_cast<const E *>(P.h) + int64_t(t0) * 2 * P.pad_rank,
                            static_cast<uint32_t>(xr) * 4 * P.pad_rank);
     const auto bb =
