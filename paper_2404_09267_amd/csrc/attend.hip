@@ -757,6 +757,8 @@ __global__ __launch_bounds__(kThreads) void join_tile_kernel(const AttendParams 
         total += f * pl[u][k];
         if (c < P.d)
           sum[u] += f * *reinterpret_cast<const f32x4 *>(P.part + (k * step + at) * P.d + c);
+      } else {
+        total += pl[u][k];  // 0, or NaN where NaN is all that was seen of the part
       }
     bool fine = true;
 #pragma unroll

@@ -5,7 +5,7 @@ import torch
 
 from gpu_helpers import say
 from paper_2404_09267_amd import tg
-from test_tokens_gpu import NAN, gen, normal
+from test_tokens_gpu import NAN, gen, make, normal, run_attend
 import token_reference as R
 
 pytestmark = pytest.mark.gpu
@@ -40,3 +40,44 @@ def test_project_adapters_past_one_buffer(rank):
     tg.project(x, w, bufs, tg.Adapters(a, b, scale.cuda()), ids.cuda())
     torch.cuda.synchronize()
     R.assert_within(bufs.y, want, bound, "project")
+
+
+# -------------------------------------------------------------------------------- attend
+
+CUT_KEYS = [(300, 1600, 2, 1, 128, "bf16"), (140, 4000, 4, 2, 64, "f16")]
+
+
+def finite_rest(got, want, bound, lost):
+    """The rows `lost` are NaN throughout, all others within their bounds."""
+    got = got.cpu()
+    assert bool(torch.isnan(got[lost]).all())
+    R.assert_within(got[~lost], want[~lost], bound[~lost], "attend")
+
+
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("n_q,n,heads,kv,d,dtype", CUT_KEYS + [(1, 3000, 4, 2, 64, "bf16"),
+                                                              (100, 300, 2, 1, 64, "f16"),
+                                                              (1, 200, 4, 1, 40, "f16")])
+def test_attend_seen_nan(n_q, n, heads, kv, d, dtype, causal):
+    """A NaN in a query, or in keys it sees, is its result, however the keys are cut."""
+    say("attend seen nan", n_q, n, dtype, causal)
+    _, q, k, v, qb, kb = make(34, [n_q], [n], heads, kv, d, dtype)
+    f = dict(causal=causal)
+    want, bound = R.attend(q, k, v, qb, kb, [n], d ** -0.5, **f)
+    place = torch.arange(n_q) + n - n_q
+    bad = q.clone()
+    bad[n_q // 2, :, 3] = NAN
+    got = run_attend(bad, k, v, qb, kb, [n], d ** -0.5, **f)
+    finite_rest(got, want, bound, torch.arange(n_q) == n_q // 2)
+    # whole parts of the keys, and the first key of a tile as all that some queries see of it
+    for keys in (slice(0, n // 2), slice(n // 2, n), slice(n - n_q // 2 & ~63, None)):
+        bad = k.clone()
+        bad[keys] = NAN
+        first = torch.arange(n)[keys][0]
+        lost = place >= first if causal else torch.ones(n_q, dtype=torch.bool)
+        finite_rest(run_attend(q, bad, v, qb, kb, [n], d ** -0.5, **f), want, bound, lost)
+    for j in range(n - n_q & ~63, n, 64):
+        bad = k.clone()
+        bad[max(j, 0)] = NAN
+        lost = place >= j if causal else torch.ones(n_q, dtype=torch.bool)
+        finite_rest(run_attend(q, bad, v, qb, kb, [n], d ** -0.5, **f), want, bound, lost)
