@@ -432,7 +432,7 @@ __global__ __launch_bounds__(kThreads, kD == 64 ? 3 : 2) void attend_tile_kernel
       block_lo = min(block_lo, s_range[w][0]);
       block_hi = max(block_hi, s_range[w][1]);
     }
-    if (doc < 0) doc = INT_MIN;  // equal to no key's
+    if (doc < 0) doc = INT_MIN;  // hardly any key's
   }
   const int first_row = wave * (64 / kChunks) + lane / kChunks;
   const uint32_t k_off = row_offset<kChunks, false>(P.k_stride, P.d, first_row);
@@ -667,6 +667,10 @@ __global__ __launch_bounds__(kThreads, kD == 64 ? 3 : 2) void attend_tile_kernel
   }
 
   l += __shfl_xor(l, 32);
+  if (with_docs && doc < 0) {  // keys of document INT_MIN are not seen either
+    m = -INFINITY;
+    l = 0.0f;
+  }
   if (P.splits > 1) {
     const int64_t to = (int64_t(split) * P.n_q_rows + row) * P.n_heads + head;
     if (!live) return;
@@ -1014,6 +1018,10 @@ __global__ __launch_bounds__(kFewWaves * 64) void attend_few_kernel(const Attend
   // the waves' ranges are joined through LDS
   l += __shfl_xor(l, 16);
   l += __shfl_xor(l, 32);
+  if (doc < 0) {  // sees nothing, nor keys of document INT_MIN
+    m = -INFINITY;
+    l = 0.0f;
+  }
   __syncthreads();  // the tiles are done with
   float *sums = reinterpret_cast<float *>(&tile[0][0][0][0]);  // [kFewWaves][16][kD]
   if (quad == 0) {

@@ -81,3 +81,15 @@ def test_attend_seen_nan(n_q, n, heads, kv, d, dtype, causal):
         bad[max(j, 0)] = NAN
         lost = place >= j if causal else torch.ones(n_q, dtype=torch.bool)
         finite_rest(run_attend(q, bad, v, qb, kb, [n], d ** -0.5, **f), want, bound, lost)
+
+
+@pytest.mark.parametrize("q_len", [3, 100])
+def test_attend_documents_of_every_sign(q_len):
+    """Documents below 0 see nothing, the lowest number among them; the highest is one like others."""
+    say("attend documents", q_len)
+    g, q, k, v, qb, kb = make(35, [q_len], [170], 4, 2, 64, "bf16")
+    names = torch.tensor([-(1 << 31), -1, 0, (1 << 31) - 1, -(1 << 31) + 1], dtype=torch.int32)
+    f = dict(q_doc=names[torch.arange(q_len) % 5], k_doc=names[torch.arange(170) * 7 // 3 % 5])
+    want, bound = R.attend(q, k, v, qb, kb, [170], 0.125, **f)
+    assert bool((want[0] == 0).all())
+    R.assert_within(run_attend(q, k, v, qb, kb, [170], 0.125, **f), want, bound, "attend")
