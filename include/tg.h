@@ -701,8 +701,9 @@ size_t tg_attend_workspace_bytes(int32_t n_seqs, int32_t n_q_rows, int32_t max_q
  * it sees key j when j <= p or j < prefix[s] or not causal, and its document is the key's (and
  * >= 0). The output is the softmax-weighted sum of the visible v_j, 0 for a query that sees no
  * key; keys and values it does not see do not reach it, whatever they hold. Weights are
- * rounded to the type before the product with v, and their sum, in binary32, is of the rounded
- * ones, so that the weights of a row make 1. Rows outside [0, n_q_rows) and [0, n_k_rows) are
+ * rounded to the type before the product with v (in binary16 as 2^7 times their share of the
+ * largest or more, so that they count down to 2^-32 of it), and their sum, in binary32, is of the
+ * rounded ones, so that the weights of a row make 1. Rows outside [0, n_q_rows) and [0, n_k_rows) are
  * not read or written, whatever q_begin, kv_begin and kv_len say. out must not overlap an
  * input. Enqueued on `stream`; allocates nothing. Returns TG_E_INVAL (null pointer, negative
  * count, d outside [8, TG_ATTEND_MAX_D] or not a multiple of 8, heads that n_kv_heads does not

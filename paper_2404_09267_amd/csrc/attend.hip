@@ -5,7 +5,7 @@
 // a running maximum m, the sum l of 2^(z - m) and the weighted sum of values, the latter two
 // multiplied by 2^(m_old - m_new) when m grows. Scores are kept in units of log2, so that a
 // weight is one exponential. m is only moved when a score passes it by more than kSlack: weights
-// then reach 2^kSlack instead of 1, which neither binary16 nor the sums mind, and the
+// then reach 2^kSlack times what they would, which neither binary16 nor the sums mind, and the
 // accumulators are seldom touched.
 //
 // Scores are computed transposed, S^T = K Q^T: a lane holds scores of ONE query, so that m, l
@@ -37,6 +37,11 @@ using namespace tok;
 
 constexpr int kMaxStride = 1 << 22;
 constexpr float kSlack = 8.0f;
+// Weights are kept times 2^kLift: binary16's smallest number is 2^-24, and without it what lies
+// below 2^-25 of the largest weight would be lost, however many such keys there are. With kSlack
+// they reach 2^15, which binary16 holds.
+template <int kType>
+constexpr float kLift = kType == TG_F16 ? 7.0f : 0.0f;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / 64;
@@ -630,7 +635,7 @@ __global__ __launch_bounds__(kThreads, kD == 64 ? 3 : 2) void attend_tile_kernel
 #pragma unroll
             for (int r = 0; r < 16; ++r) acc[b][r] *= fix;
         }
-        const float base = shift - (m == -INFINITY ? 0.0f : m);
+        const float base = shift - (m == -INFINITY ? 0.0f : m) + kLift<kType>;
         __builtin_amdgcn_s_setprio(0);
 #pragma unroll
         for (int k = 0; k < 4; ++k) {  // 16 keys
@@ -990,7 +995,7 @@ __global__ __launch_bounds__(kFewWaves * 64) void attend_few_kernel(const Attend
 #pragma unroll
         for (int r = 0; r < 4; ++r) acc[b][r] *= fix;
     }
-    const float base = m == -INFINITY ? 0.0f : m;
+    const float base = (m == -INFINITY ? 0.0f : m) - kLift<kType>;
     V8 pf;
 #pragma unroll
     for (int e = 0; e < 8; e += 2) {

@@ -1,5 +1,7 @@
 """The token operators where sizes, masks and values are at their ends, against plain 64-bit
 implementations: what the tests of single operators do not reach."""
+import math
+
 import pytest
 import torch
 
@@ -93,3 +95,24 @@ def test_attend_documents_of_every_sign(q_len):
     want, bound = R.attend(q, k, v, qb, kb, [170], 0.125, **f)
     assert bool((want[0] == 0).all())
     R.assert_within(run_attend(q, k, v, qb, kb, [170], 0.125, **f), want, bound, "attend")
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("q_len,n", [(1, 500), (70, 500), (1, 100003), (70, 100003)])
+def test_attend_many_small_weights(q_len, n, dtype):
+    """A key of weight 1 in every 64, whose value is 0, and many of weight e^-17.5, 0.84 of half
+    binary16's smallest number, whose values add up. A weight is off by its rounding to the type;
+    in binary16, with the largest weight at 2^7, by no less than 2^-32 of it."""
+    say("attend small weights", q_len, n, dtype)
+    _, q, k, v, qb, kb = make(36, [q_len], [n], 1, 1, 8, dtype)
+    q[:], k[:] = 0, 0
+    q[:, :, 0], k[:, :, 0] = 1.0, -17.5
+    v = (v.abs() * 60).clamp(1.0, 200.0)
+    k[::64], v[::64] = 0, 0
+    want, _ = R.attend(q, k, v, qb, kb, [n], 1.0)
+    small, u = math.exp(-17.5), R.UNIT[q.dtype]
+    each = max(u * small, 2.0 ** -32) if dtype == "f16" else u * small
+    # 64 keys' errors against a sum of 1, those of the exponent (26 in binary32) and of the sum
+    bound = (u * want + R.TINY[q.dtype] + 64 * float(v.max()) * (each + 40 * R.E32 * small)
+             + 2 * u * want + (n + 8) * R.E32 * want)
+    R.assert_within(run_attend(q, k, v, qb, kb, [n], 1.0), want, bound, "attend")
