@@ -20,7 +20,9 @@
 //
 // A key that a query does not see has weight 0, and 0 times infinity or NaN would still reach
 // the query's sum. Such sums stay NaN, so each result is looked at once, at the end; a row that
-// is not finite is computed again by strict_row, which leaves unseen keys out one by one.
+// is not finite is computed again by strict_row, which leaves unseen keys out one by one. So is a
+// row whose scores are so large (2^24 and more) that the maximum, which is rounded, lies so far
+// from the score that it comes from that the largest weight is lost (full_sum).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -213,6 +215,9 @@ __device__ __forceinline__ float abs_diff(int a, int b) {  // of any two
   const uint32_t d = static_cast<uint32_t>(a) - static_cast<uint32_t>(b);
   return static_cast<float>(a > b ? d : 0u - d);
 }
+
+// Whether a row's sum holds its largest weight, which is 1 at least if it was not rounded away.
+__device__ __forceinline__ bool full_sum(float m, float l) { return l >= 0.5f || m == -INFINITY; }
 
 // One query row of one head, by one wave, unseen keys left out one by one.
 template <int kType>
@@ -696,7 +701,7 @@ __global__ __launch_bounds__(kThreads, kD == 64 ? 3 : 2) void attend_tile_kernel
     return;
   }
   const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-  bool fine = true;
+  bool fine = full_sum(m, l);
   E *o = static_cast<E *>(P.out) + row * P.out_stride + head * P.out_head;
 #pragma unroll
   for (int b = 0; b < kBlocks; ++b)
@@ -769,7 +774,7 @@ __global__ __launch_bounds__(kThreads) void join_tile_kernel(const AttendParams 
       } else {
         total += pl[u][k];  // 0, or NaN where NaN is all that was seen of the part
       }
-    bool fine = true;
+    bool fine = full_sum(top, total);
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
       sum[u][q] = total == 0.0f ? 0.0f : sum[u][q] / total;
@@ -1054,7 +1059,7 @@ __global__ __launch_bounds__(kFewWaves * 64) void attend_few_kernel(const Attend
   const int64_t flat = (int64_t(id) * P.n_kv_heads + kvh) * P.row_tiles * 16 + mine;
   float *part = P.part + flat * P.d;
   E *o = static_cast<E *>(P.out) + orow * P.out_stride + ohead * P.out_head;
-  bool fine = true;
+  bool fine = full_sum(top, total) || mine >= rows;
 #pragma unroll
   for (int b = 0; b < kD / 4 / kLanes; ++b) {
     const int c = (b * kLanes + c0) * 4;
@@ -1151,7 +1156,7 @@ __global__ __launch_bounds__(kThreads, 4) void join_kernel(const AttendParams P)
   if (group == 0 && c < P.d) {
 #pragma unroll
     for (int g = 1; g < kAtOnce; ++g) sum += s_sum[g][tid];
-    bool fine = true;
+    bool fine = full_sum(top, total);
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
       sum[q] = total == 0.0f ? 0.0f : sum[q] / total;

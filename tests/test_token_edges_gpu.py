@@ -116,3 +116,34 @@ def test_attend_many_small_weights(q_len, n, dtype):
     bound = (u * want + R.TINY[q.dtype] + 64 * float(v.max()) * (each + 40 * R.E32 * small)
              + 2 * u * want + (n + 8) * R.E32 * want)
     R.assert_within(run_attend(q, k, v, qb, kb, [n], 1.0), want, bound, "attend")
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("q_len,n", [(1, 150), (1, 3000), (90, 150), (140, 3000)])
+def test_attend_scores_of_any_size(q_len, n, dtype):
+    """Scores so large that their rounding alone is many units of the exponent: the largest has
+    all of the weight. They are whole multiples of the scale, so it is the same in any order."""
+    say("attend large scores", q_len, n, dtype)
+    g, q, k, v, qb, kb = make(38, [q_len], [n], 4, 2, 64, dtype)
+    q[:], k[:] = 0, 0
+    q[..., 0], q[..., 5] = 2.0, 1.0
+    top = torch.randint(0, n, (2,), generator=g)
+    k[..., 0] = -torch.randint(1, 9, (n, 2), generator=g).to(k.dtype)
+    k[..., 5] = torch.randint(0, 2, (n, 2), generator=g).to(k.dtype)
+    for h in range(2):
+        k[top[h], h, 0], k[top[h], h, 5] = 50.0, 1.0
+    want = torch.stack([v[top[h // 2], h // 2] for h in range(4)]).expand(q.shape)
+    for scale in (1e6, 1.1e7, 3e8, 7.7e8, 1e9, 3.3e9, 1.7e10, 6e12, 1e20):
+        got = run_attend(q, k, v, qb, kb, [n], scale).cpu()
+        assert bool((got == want).all()), scale
+    # the same by a bias that favours distance
+    f = dict(slope=-torch.tensor([0.7, 1.25, 2.5, 5.0]),
+             q_pos=torch.randint(0, 30, (q_len, 2), generator=g, dtype=torch.int32),
+             k_pos=torch.randint(0, 30, (n, 2), generator=g, dtype=torch.int32))
+    for far in (2 ** 31 - 1, 2 ** 31 - 12345, 2 ** 28 + 99):
+        f["k_pos"][top] = -far
+        both = v[top].float().mean(0) if top[0] != top[1] else v[top[0]].float()
+        got = run_attend(q, k * 0, v, qb, kb, [n], 0.125, **f).cpu()
+        bound = 4 * R.UNIT[q.dtype] * v[top].double().abs().amax(0)
+        for h in range(4):
+            R.assert_within(got[:, h], both[h // 2].double().expand(q_len, -1), bound[h // 2], "attend")
