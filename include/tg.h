@@ -673,7 +673,8 @@ typedef struct {
   const int32_t *q_pos;      /* device [n_q_rows][2] and [n_k_rows][2], both or neither: */
   const int32_t *k_pos;      /* positions the distance is taken from; not read without slope */
   const float *slope;        /* device [n_heads] or NULL: bias per unit of distance, of any sign;
-                                distances up to 2^24 are exact */
+                                distances up to 2^23 are exact (slow where queries that follow
+                                each other are further apart than that) */
   float scale;               /* finite */
   float cap;                 /* > 0: scores are capped; 0: not */
   int32_t causal;            /* nonzero: a query sees keys up to its own place */

@@ -419,6 +419,8 @@ __global__ __launch_bounds__(kThreads, kD == 64 ? 3 : 2) void attend_tile_kernel
   }
   const int x0 = __builtin_amdgcn_readfirstlane(px), y0 = __builtin_amdgcn_readfirstlane(py);
   const float fx = apart(px, x0), fy = apart(py, y0);
+  // queries so far apart that the wave's first is no origin for exact differences
+  const bool scattered = with_pos && __ballot(fmaxf(fabsf(fx), fabsf(fy)) > 0x1p23f) != 0;
   const bool late = !P.capped && P.to_log2 >= 0x1p-20f;
   const float rate = late ? slope2 / P.to_log2 : slope2;
   int wave_lo = INT_MAX, wave_hi = -1;  // the documents of the wave's queries
@@ -681,6 +683,7 @@ __global__ __launch_bounds__(kThreads, kD == 64 ? 3 : 2) void attend_tile_kernel
     m = -INFINITY;
     l = 0.0f;
   }
+  if (scattered) l = NAN;  // for strict_row: a second formula in the loop spilled registers
   if (P.splits > 1) {
     const int64_t to = (int64_t(split) * P.n_q_rows + row) * P.n_heads + head;
     if (!live) return;

@@ -118,6 +118,25 @@ def test_attend_many_small_weights(q_len, n, dtype):
     R.assert_within(run_attend(q, k, v, qb, kb, [n], 1.0), want, bound, "attend")
 
 
+@pytest.mark.parametrize("q_len", [1, 90, 300])
+def test_attend_far_positions_are_exact(q_len):
+    """Queries of one batch at places 2^30 apart: the distance to a key beside each is whole. Keys
+    of the other places are too far to weigh anything."""
+    say("attend far positions", q_len)
+    n, heads = 400, 2
+    g, q, k, v, qb, kb = make(37, [q_len], [n], heads, 1, 64, "bf16", gain=0.5)
+    bases = torch.tensor([0, 1 << 30, -(1 << 30) - 77, (1 << 31) - 100, 1 << 25, -(1 << 31) + 9])
+    qc, kc = torch.arange(q_len) % 6, torch.randint(0, 6, (n,), generator=g)
+    if q_len == 1:
+        qc[:] = 1
+    f = dict(slope=torch.tensor([0.25, 1.0]))
+    place = lambda c, rows: (bases[c][:, None] + torch.randint(0, 5, (rows, 2), generator=g)).int()
+    f["q_pos"], f["k_pos"] = place(qc, q_len), place(kc, n)
+    want, bound = R.attend(q, k, v, qb, kb, [n], 0.125, q_doc=qc.int(), k_doc=kc.int(), **f)
+    got = run_attend(q, k, v, qb, kb, [n], 0.125, **f)
+    R.assert_within(got, want, bound, "attend")
+
+
 @pytest.mark.parametrize("dtype", ["f16", "bf16"])
 @pytest.mark.parametrize("q_len,n", [(1, 150), (1, 3000), (90, 150), (140, 3000)])
 def test_attend_scores_of_any_size(q_len, n, dtype):
