@@ -26,6 +26,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <cfloat>
 #include <climits>
 #include <cmath>
 #include <cstdint>
@@ -1329,12 +1330,20 @@ extern "C" int tg_attend(const tg_attend_args *a, void *stream) {
   P.q_pos = a->slope ? a->q_pos : nullptr;  // nothing else asks for places
   P.k_pos = a->slope ? a->k_pos : nullptr;
   P.slope = a->slope;
-  P.to_log2 = a->scale * kLog2e;
+  // Scales and caps at the ends of binary32: a factor past it is its largest number (a score that
+  // is not 0 is past tanh's range with either, and 0 stays 0). Of a cap so large that no score
+  // reaches tanh's bend, any other such will do.
+  const auto factor = [](double v) {
+    return static_cast<float>(std::min(std::max(v, -double(FLT_MAX)), double(FLT_MAX)));
+  };
+  P.to_log2 = factor(double(a->scale) * kLog2e);
   if (a->cap > 0.0f) {
-    P.capped = a->cap <= kFastCap ? 1 : 2;
-    P.cap_arg = a->scale / a->cap;
-    P.cap_in = 2.0f * kLog2e * P.cap_arg;
-    P.cap_out = a->cap * kLog2e;
+    const double cap = std::min<double>(
+        a->cap, 0x1p100 * std::min(std::max(std::fabs(double(a->scale)), 1.0), 0x1p26));
+    P.capped = cap <= kFastCap ? 1 : 2;
+    P.cap_arg = factor(a->scale / cap);
+    P.cap_in = factor(2.0 * kLog2e * a->scale / cap);
+    P.cap_out = static_cast<float>(cap * kLog2e);
   }
   P.shaped = P.capped || a->slope || !(P.to_log2 > 0.0f);
   P.causal = a->causal != 0;

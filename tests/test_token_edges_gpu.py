@@ -166,3 +166,19 @@ def test_attend_scores_of_any_size(q_len, n, dtype):
         bound = 4 * R.UNIT[q.dtype] * v[top].double().abs().amax(0)
         for h in range(4):
             R.assert_within(got[:, h], both[h // 2].double().expand(q_len, -1), bound[h // 2], "attend")
+
+
+@pytest.mark.parametrize("cap", [1e-40, 1e-30, 1e-6, 3e38])
+@pytest.mark.parametrize("q_len,more", [(1, {}), (90, {}), (90, {"slope": True}), (1, {"slope": True})])
+def test_attend_caps_of_every_size(q_len, more, cap):
+    """Caps whose quotient with the scale leaves binary32, scores of 0 among them."""
+    say("attend caps", q_len, cap)
+    _, q, k, v, qb, kb = make(39, [q_len], [150], 2, 1, 64, "bf16")
+    k[::9], q[::5] = 0, 0
+    f = dict(cap=cap)
+    if more:
+        f["slope"] = torch.tensor([0.5, 0.01])
+    # the bound has a share of the cap in it: tanh of next to nothing is straight
+    straight = {n: t for n, t in f.items() if n != "cap"}
+    want, bound = R.attend(q, k, v, qb, kb, [150], 0.125, **(straight if cap > 1e30 else f))
+    R.assert_within(run_attend(q, k, v, qb, kb, [150], 0.125, **f), want, bound, "attend")
