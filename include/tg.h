@@ -557,7 +557,8 @@ int tg_mask_rois(const tg_mask_rois_args *args, void *stream);
  *
  * Values are binary16 or bfloat16, sums, norms and softmax statistics binary32, and each
  * result is rounded once to nearest-even. Strides are in elements, the last dimension is
- * contiguous. A call whose workgroups one launch cannot hold (2^31) returns TG_E_INVAL.
+ * contiguous. A call that one launch cannot hold (2^31 workgroups or so, of tg_project 2^32 threads)
+ * returns TG_E_INVAL.
  */
 enum tg_type {
   TG_F16 = 0, /* binary16 */
@@ -602,8 +603,8 @@ size_t tg_project_workspace_bytes(int32_t n_tokens, int32_t k, int32_t n, int32_
  * two values of the type each, the rounded one and what that left, or in binary32; everything
  * else is summed in binary32.
  * Enqueued on `stream`; the library allocates nothing. Returns TG_E_INVAL (null pointer,
- * negative count, k < 1 or not a multiple of 8, n < 1, with adapters n > 2^23 or a rank outside
- * [1, TG_PROJECT_MAX_RANK], a bad type or stride, x, w or a not 16-byte aligned),
+ * negative count, k < 1 or not a multiple of 8, n < 1, with adapters n > 2^23, n_tokens > 2^28 or
+ * a rank outside [1, TG_PROJECT_MAX_RANK], a bad type or stride, x, w or a not 16-byte aligned),
  * TG_E_WORKSPACE, TG_E_HIP. n_tokens == 0 enqueues nothing.
  */
 int tg_project(const tg_project_args *args, void *stream);

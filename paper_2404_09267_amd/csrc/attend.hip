@@ -70,6 +70,7 @@ struct AttendParams {
   int64_t n_k_rows;
   int32_t max_q, max_kv, n_heads, n_kv_heads, group, d;
   // attend_tile_kernel
+  int32_t turns;    // workgroups of a head
   int32_t splits;   // workgroups that share a tile's keys; with more than one, parts are laid out
                     // as [splits][n_q_rows][n_heads][d], and [..][..][..][2]
   // attend_few_kernel
@@ -380,12 +381,13 @@ __global__ __launch_bounds__(kThreads, kD == 64 ? 3 : 2) void attend_tile_kernel
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int col = lane & 31, half = lane >> 5;
-  const int head = blockIdx.x % P.n_heads;
+  const int id = static_cast<int>(workgroup()), head = id % P.n_heads;
   // Long rows first; workgroups 256 to 511 the other way round, as they share a CU with those 256
   // before them (4 causal prompts of 2,048, 8 heads of 128: 57 us for 63; 1 of 4,096, 16 heads:
   // 101 for 104)
-  const int turns = gridDim.x / P.n_heads, round = kCus / P.n_heads;
-  int turn = blockIdx.x / P.n_heads;
+  const int turns = P.turns, round = kCus / P.n_heads;
+  int turn = id / P.n_heads;
+  if (turn >= turns) return;
   if (turn >= round && turn < 2 * round) turn = round + min(2 * round, turns) - 1 - turn;
   const int split = turn % P.splits, tile = (turns - 1 - turn) / P.splits;
   int first;
@@ -893,7 +895,7 @@ __global__ __launch_bounds__(kFewWaves * 64) void attend_few_kernel(const Attend
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int col = lane & 15, quad = lane >> 4;
-  int id = blockIdx.x;
+  int id = static_cast<int>(workgroup());
   const int kvh = id % P.n_kv_heads;
   id /= P.n_kv_heads;
   const int rt = id % P.row_tiles;
@@ -903,6 +905,7 @@ __global__ __launch_bounds__(kFewWaves * 64) void attend_few_kernel(const Attend
     parts = find_parts(P, id, -1);
     if (parts.seq < 0) return;
   } else {
+    if (id >= P.n_seqs) return;
     parts.s = sequence(P, id);
   }
   const Seq s = parts.s;
@@ -1225,20 +1228,21 @@ Few few_of(int n_seqs, int n_q_rows, int max_q, int max_kv, int n_heads, int n_k
 }
 
 template <int kType, int kD>
-int launch(const AttendParams &P, const Few &few, hipStream_t s) {
+int launch(AttendParams P, const Few &few, hipStream_t s) {
   if (few.use) {
     const int64_t blocks = (int64_t(P.n_seqs) + P.width) * P.n_kv_heads * P.row_tiles;
     const int64_t joined = int64_t(P.n_seqs) * P.n_heads * P.max_q;
-    if (blocks > INT32_MAX || joined > INT32_MAX) return TG_E_INVAL;
-    hipLaunchKernelGGL((attend_few_kernel<kType, kD>), dim3(static_cast<uint32_t>(blocks)),
+    if (blocks > kMaxWorkgroups || joined > INT32_MAX) return TG_E_INVAL;
+    hipLaunchKernelGGL((attend_few_kernel<kType, kD>), grid_of(blocks, kFewWaves * 64),
                        dim3(kFewWaves * 64), 0, s, P);
     if (P.width > 0)
       hipLaunchKernelGGL(join_kernel<kType>, dim3(static_cast<uint32_t>(joined)), dim3(kThreads), 0,
                          s, P);
   } else {
     const int64_t tiles = (int64_t(P.n_q_rows) / kBM + P.n_seqs) * P.n_heads;
-    if (tiles * P.splits > INT32_MAX) return TG_E_INVAL;
-    const dim3 grid(static_cast<uint32_t>(tiles * P.splits)), threads(kThreads);
+    if (tiles * P.splits > kMaxWorkgroups) return TG_E_INVAL;
+    P.turns = static_cast<int32_t>(tiles / P.n_heads * P.splits);
+    const dim3 grid = grid_of(tiles * P.splits, kThreads), threads(kThreads);
     const bool any = P.k_doc || P.k_pos || P.capped == 2 || !(P.to_log2 > 0.0f);
     if (any || (P.capped && P.slope))
       hipLaunchKernelGGL((attend_tile_kernel<kType, kD, kAny>), grid, threads, 0, s, P);

@@ -713,14 +713,18 @@ __global__ __launch_bounds__(kFinishThreads) void finish_kernel(const ProjectPar
   }
 }
 
-template <int kType, int kT, int kN, int kWt, int kWn, int kBK, int kStages, bool kCut = false>
-int launch_tiles(ProjectParams P, hipStream_t s) {
+// `first` enqueues what the tiles wait for, if they can be launched.
+template <int kType, int kT, int kN, int kWt, int kWn, int kBK, int kStages, bool kCut = false,
+          class First>
+int launch_tiles(ProjectParams P, hipStream_t s, const First &first) {
   const int64_t tiles_t = (int64_t(P.n_tokens) + kT - 1) / kT;
   const int64_t tiles_n = (int64_t(P.n) + kN - 1) / kN;
-  if (tiles_t * tiles_n > INT32_MAX / (kCut ? 64 : kGroup)) return TG_E_INVAL;
+  const int64_t blocks = tiles_t * tiles_n * (kCut ? P.splits : 1) + (kCut ? P.low_blocks : 0);
+  // threads that a launch takes in one direction
+  if (blocks * (kWt * kWn * 64) >= int64_t(1) << 32) return TG_E_INVAL;
   P.tiles_t = static_cast<int32_t>(tiles_t);
   P.tiles_n = static_cast<int32_t>(tiles_n);
-  const int64_t blocks = tiles_t * tiles_n * (kCut ? P.splits : 1) + (kCut ? P.low_blocks : 0);
+  first();
   hipLaunchKernelGGL((project_kernel<kType, kT, kN, kWt, kWn, kBK, kStages, kCut>),
                      dim3(static_cast<uint32_t>(blocks)), dim3(kWt * kWn * 64), 0, s, P);
   return TG_OK;
@@ -757,21 +761,27 @@ int launch(ProjectParams P, const Few &few, void *packed, hipStream_t s) {
   if (few.use && (P.adapter || few.alone)) {
     P.splits = few.splits;
     P.low_blocks = P.adapter ? P.n_tokens * (P.pad_rank / kTokenRanks) : 0;
-    rc = few.tile == 32 ? launch_tiles<kType, 32, 64, 1, 4, 64, 4, true>(P, s)
-                        : launch_tiles<kType, 64, 64, 2, 2, 64, 4, true>(P, s);
+    const auto none = [] {};
+    rc = few.tile == 32 ? launch_tiles<kType, 32, 64, 1, 4, 64, 4, true>(P, s, none)
+                        : launch_tiles<kType, 64, 64, 2, 2, 64, 4, true>(P, s, none);
     if (rc != TG_OK) return rc;
     hipLaunchKernelGGL(finish_kernel<kType>,
                        dim3((P.part_stride / 4 + kFinishThreads - 1) / kFinishThreads, P.n_tokens),
                        dim3(kFinishThreads), 0, s, P);
     return hipGetLastError() == hipSuccess ? TG_OK : TG_E_HIP;
   }
-  if (P.adapter) launch_shrink<kType>(P, s);
-  if (packed) {
-    const int64_t rows = int64_t(P.n_adapters) * P.n;
-    const int64_t threads = rows * (P.pad_rank / 8);
+  const ProjectParams given = P;
+  const auto first = [&] {
+    if (!given.adapter) return;
+    launch_shrink<kType>(given, s);
+    if (!packed) return;
+    const int64_t rows = int64_t(given.n_adapters) * given.n;
+    const int64_t threads = rows * (given.pad_rank / 8);
     hipLaunchKernelGGL(pack_kernel<kType>,
                        dim3(static_cast<uint32_t>((threads + kPackThreads - 1) / kPackThreads)),
-                       dim3(kPackThreads), 0, s, P, packed, rows);
+                       dim3(kPackThreads), 0, s, given, packed, rows);
+  };
+  if (packed) {
     P.b = packed;
     P.b_rank = P.pad_rank;
     P.b_apart = 0;
@@ -800,20 +810,20 @@ int launch(ProjectParams P, const Few &few, void *packed, hipStream_t s) {
   };
   P.b_whole = int64_t(P.n_adapters) * P.n * P.b_rank * 2 < (int64_t(1) << 31);
   P.gather = P.adapter && P.b_apart;  // rows of b that a load to LDS cannot take
-  if (P.gather) rc = launch_tiles<kType, 64, 64, 2, 2, 64, 4>(P, s);
+  if (P.gather) rc = launch_tiles<kType, 64, 64, 2, 2, 64, 4>(P, s, first);
   else if (tiles(128, 128) > 256) {
     const auto rounds = [&](int t, int n, int at_once) { return (tiles(t, n) + at_once - 1) / at_once; };
     const int64_t c256 = 164 * rounds(256, 256, 256), c192 = 137 * rounds(192, 256, 256);
     const int64_t c160 = 118 * rounds(160, 128, 512), c128 = 100 * rounds(128, 128, 512);
     const int64_t least = std::min(std::min(c256, c192), std::min(c160, c128));
-    if (c256 == least) rc = launch_tiles<kType, 256, 256, 2, 4, 64, 2>(P, s);
-    else if (c192 == least) rc = launch_tiles<kType, 192, 256, 4, 2, 64, 2>(P, s);
-    else if (c160 == least) rc = launch_tiles<kType, 160, 128, 2, 2, 64, 2>(P, s);
-    else rc = launch_tiles<kType, 128, 128, 2, 2, 64, 2>(P, s);
+    if (c256 == least) rc = launch_tiles<kType, 256, 256, 2, 4, 64, 2>(P, s, first);
+    else if (c192 == least) rc = launch_tiles<kType, 192, 256, 4, 2, 64, 2>(P, s, first);
+    else if (c160 == least) rc = launch_tiles<kType, 160, 128, 2, 2, 64, 2>(P, s, first);
+    else rc = launch_tiles<kType, 128, 128, 2, 2, 64, 2>(P, s, first);
   }
-  else if (tiles(128, 128) >= 160) rc = launch_tiles<kType, 128, 128, 2, 4, 64, 4>(P, s);
-  else if (tiles(64, 64) > 256) rc = launch_tiles<kType, 128, 64, 2, 2, 64, 3>(P, s);
-  else rc = launch_tiles<kType, 64, 64, 2, 2, 64, 4>(P, s);
+  else if (tiles(128, 128) >= 160) rc = launch_tiles<kType, 128, 128, 2, 4, 64, 4>(P, s, first);
+  else if (tiles(64, 64) > 256) rc = launch_tiles<kType, 128, 64, 2, 2, 64, 3>(P, s, first);
+  else rc = launch_tiles<kType, 64, 64, 2, 2, 64, 4>(P, s, first);
   if (rc != TG_OK) return rc;
   return hipGetLastError() == hipSuccess ? TG_OK : TG_E_HIP;
 }
@@ -851,7 +861,9 @@ extern "C" int tg_project(const tg_project_args *a, void *stream) {
       a->w_stride % 8 || a->x_stride > kMaxStride || a->w_stride > kMaxStride)
     return TG_E_INVAL;
   const bool low = a->adapter && a->n_adapters > 0;
-  if (low && (a->rank < 1 || a->rank > TG_PROJECT_MAX_RANK || a->n > (1 << 23))) return TG_E_INVAL;
+  if (low && (a->rank < 1 || a->rank > TG_PROJECT_MAX_RANK || a->n > (1 << 23) ||
+              a->n_tokens > (1 << 28)))
+    return TG_E_INVAL;
   if (a->n_tokens == 0) return TG_OK;
   if (!a->x || !a->w || !a->y || !aligned16(a->x) || !aligned16(a->w)) return TG_E_INVAL;
   if (low && (!a->a || !a->b || !a->scale || !aligned16(a->a))) return TG_E_INVAL;

@@ -77,7 +77,7 @@ __global__ __launch_bounds__(kThreads) void rotate_kernel(const RotateParams P) 
   typedef Num<kType> N;
   typedef typename N::E E;
   typedef typename N::V8 V8;
-  const int64_t unit = int64_t(blockIdx.x) * (kThreads / 64) + (threadIdx.x >> 6);
+  const int64_t unit = workgroup() * (kThreads / 64) + (threadIdx.x >> 6);
   const int lane = threadIdx.x & 63, sub = lane & (P.lanes - 1);
   const int slot = lane / P.lanes, step = P.at_once;
   // a wave has several tokens where one has fewer heads than the wave has room for
@@ -192,7 +192,7 @@ template <int kType>
 __global__ __launch_bounds__(kThreads) void rotate_any_kernel(const RotateParams P,
                                                               int interleaved) {
   typedef typename Num<kType>::E E;
-  const int64_t unit = int64_t(blockIdx.x) * (kThreads / 64) + (threadIdx.x >> 6);
+  const int64_t unit = workgroup() * (kThreads / 64) + (threadIdx.x >> 6);
   const int64_t t = unit / P.rows;
   if (t >= P.n_tokens) return;
   int h = static_cast<int>(unit - t * P.rows);
@@ -329,16 +329,16 @@ extern "C" int tg_rotate(const tg_rotate_args *a, void *stream) {
     const int per = room / P.at_once;  // tokens of a wave
     const int64_t waves = (int64_t(a->n_tokens) + per - 1) / per * P.passes;
     const int64_t blocks = (waves + kWaves - 1) / kWaves;
-    if (blocks > INT32_MAX) return TG_E_INVAL;
-    const dim3 grid(static_cast<uint32_t>(blocks));
+    if (blocks > kMaxWorkgroups) return TG_E_INVAL;
+    const dim3 grid = grid_of(blocks, kThreads);
     if (a->type == TG_F16)
       launch_vec<TG_F16>(P, a->interleaved != 0, grid, s);
     else
       launch_vec<TG_BF16>(P, a->interleaved != 0, grid, s);
   } else {
     const int64_t blocks = (int64_t(a->n_tokens) * P.rows + kWaves - 1) / kWaves;
-    if (blocks > INT32_MAX) return TG_E_INVAL;
-    const dim3 grid(static_cast<uint32_t>(blocks));
+    if (blocks > kMaxWorkgroups) return TG_E_INVAL;
+    const dim3 grid = grid_of(blocks, kThreads);
     const int inter = a->interleaved != 0;
     if (a->type == TG_F16)
       hipLaunchKernelGGL(rotate_any_kernel<TG_F16>, grid, dim3(kThreads), 0, s, P, inter);
