@@ -44,7 +44,49 @@ def test_project_adapters_past_one_buffer(rank):
     R.assert_within(bufs.y, want, bound, "project")
 
 
+# -------------------------------------------------------------------------------- rotate
+
+def test_rotate_more_heads_than_a_row_of_workgroups():
+    """So many heads that their threads pass 2^32."""
+    say("rotate many")
+    room(24)
+    tokens, d = 2 ** 26 + 5, 2
+    q = torch.empty((tokens, 1, d), dtype=torch.bfloat16, device="cuda").normal_()
+    pos = (torch.arange(tokens, device="cuda") % 3).int()[:, None].contiguous()
+    table = torch.tensor([[[1.0, 0.0]], [[0.0, 1.0]], [[0.6, -0.8]]]).cuda()
+    out = torch.full_like(q, NAN)
+    none = q[:, :0]
+    tg.rotate(q, none, None, None, table, pos, out, none)
+    torch.cuda.synchronize()
+    for t in (slice(0, 10000), slice(tokens // 2, tokens // 2 + 10000), slice(tokens - 10000, None)):
+        want, bound = R.rotate(q[t].cpu(), None, table.cpu(), pos[t].cpu(), 1e-6, False)
+        R.assert_within(out[t].cpu(), want, bound, "rotate")
+    assert bool(torch.isfinite(out).all())
+
+
 # -------------------------------------------------------------------------------- attend
+
+@pytest.mark.parametrize("n_seqs,heads,kv,queries", [(2 ** 20 + 3, 32, 32, 1),
+                                                     (2 ** 18 + 1, 64, 1, 2)])
+def test_attend_more_rows_than_a_row_of_workgroups(n_seqs, heads, kv, queries):
+    """So many sequences that the threads of both forms pass 2^32; each sees one key, or none."""
+    say("attend many", n_seqs, heads, kv, queries)
+    room(24)
+    d, dt, keys = 8, torch.float16, 1000
+    g = gen(33)
+    k, v = normal(g, keys, kv, d, dtype=dt).cuda(), normal(g, keys, kv, d, dtype=dt).cuda()
+    q = torch.empty((n_seqs * queries, heads, d), dtype=dt, device="cuda").normal_()
+    at = torch.arange(n_seqs, device="cuda")
+    seqs = tg.Sequences((torch.arange(n_seqs + 1, device="cuda") * queries).int(), at % keys,
+                        (at % 7 > 0).int(), queries, 1)
+    out = torch.full_like(q, NAN)
+    tg.attend(q, k, v, seqs, out, tg.AttendBuffers(seqs, q, k), 0.5)
+    torch.cuda.synchronize()
+    want = v[at % keys].repeat_interleave(heads // kv, 1) * (at % 7 > 0)[:, None, None]
+    out = out.view(n_seqs, queries, heads, d)
+    for i in range(queries):
+        assert bool((out[:, i] == want).all())
+
 
 CUT_KEYS = [(300, 1600, 2, 1, 128, "bf16"), (140, 4000, 4, 2, 64, "f16")]
 
