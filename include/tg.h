@@ -709,9 +709,9 @@ size_t tg_attend_workspace_bytes(int32_t n_seqs, int32_t n_q_rows, int32_t max_q
  * not read or written, whatever q_begin, kv_begin and kv_len say. out must not overlap an
  * input. Enqueued on `stream`; allocates nothing. Returns TG_E_INVAL (null pointer, negative
  * count, d outside [8, TG_ATTEND_MAX_D] or not a multiple of 8, heads that n_kv_heads does not
- * divide, a bad type, scale or cap, one of a pair missing, prefix without causal, q, k, v or
- * out not 16-byte aligned, a stride that is negative, not a multiple of 8 or, of rows, over
- * 2^22), TG_E_WORKSPACE, TG_E_HIP. n_seqs == 0 or n_q_rows == 0 enqueues nothing.
+ * divide, a bad type, scale or cap, one of a pair missing where there are keys, prefix without
+ * causal, q, k, v or out not 16-byte aligned, a stride that is negative, not a multiple of 8 or,
+ * of rows, over 2^22), TG_E_WORKSPACE, TG_E_HIP. n_seqs == 0 or n_q_rows == 0 enqueues nothing.
  */
 int tg_attend(const tg_attend_args *args, void *stream);
 

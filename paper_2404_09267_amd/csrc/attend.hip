@@ -1295,15 +1295,18 @@ extern "C" int tg_attend(const tg_attend_args *a, void *stream) {
                 a->d) ||
       a->n_k_rows < 0 || !std::isfinite(a->scale) || !std::isfinite(a->cap) || a->cap < 0.0f)
     return TG_E_INVAL;
-  if ((a->q_doc == nullptr) != (a->k_doc == nullptr) ||
-      (a->q_pos == nullptr) != (a->k_pos == nullptr) || (a->prefix && !a->causal))
-    return TG_E_INVAL;
+  if (a->prefix && !a->causal) return TG_E_INVAL;
   if (a->n_seqs == 0 || a->n_q_rows == 0 || a->max_q_len == 0) return TG_OK;
+  // arrays of no rows may be null; where there is no key, nothing asks for the queries' either
+  const bool keys = a->n_k_rows > 0;
+  if (keys && ((a->q_doc == nullptr) != (a->k_doc == nullptr) ||
+               (a->q_pos == nullptr) != (a->k_pos == nullptr)))
+    return TG_E_INVAL;
   if (!a->q_begin || !a->kv_begin || !a->kv_len || !layout_ok(a->q, a->q_stride, a->q_head_stride) ||
       !layout_ok(a->out, a->out_stride, a->out_head_stride))
     return TG_E_INVAL;
-  if (a->n_k_rows > 0 && (!layout_ok(a->k, a->k_stride, a->k_head_stride) ||
-                          !layout_ok(a->v, a->v_stride, a->v_head_stride)))
+  if (keys && (!layout_ok(a->k, a->k_stride, a->k_head_stride) ||
+               !layout_ok(a->v, a->v_stride, a->v_head_stride)))
     return TG_E_INVAL;
   const Few few = few_of(a->n_seqs, a->n_q_rows, a->max_q_len, a->max_kv_len, a->n_heads,
                          a->n_kv_heads, a->d, a->causal != 0, a->q_doc != nullptr);
@@ -1329,10 +1332,10 @@ extern "C" int tg_attend(const tg_attend_args *a, void *stream) {
   P.kv_begin = a->kv_begin;
   P.kv_len = a->kv_len;
   P.prefix = a->prefix;
-  P.q_doc = a->q_doc;
-  P.k_doc = a->k_doc;
-  P.q_pos = a->slope ? a->q_pos : nullptr;  // nothing else asks for places
-  P.k_pos = a->slope ? a->k_pos : nullptr;
+  P.q_doc = keys ? a->q_doc : nullptr;
+  P.k_doc = keys ? a->k_doc : nullptr;
+  P.q_pos = keys && a->slope ? a->q_pos : nullptr;  // nothing else asks for places
+  P.k_pos = keys && a->slope ? a->k_pos : nullptr;
   P.slope = a->slope;
   // Scales and caps at the ends of binary32: a factor past it is its largest number (a score that
   // is not 0 is past tanh's range with either, and 0 stays 0). Of a cap so large that no score

@@ -224,3 +224,17 @@ def test_attend_caps_of_every_size(q_len, more, cap):
     straight = {n: t for n, t in f.items() if n != "cap"}
     want, bound = R.attend(q, k, v, qb, kb, [150], 0.125, **(straight if cap > 1e30 else f))
     R.assert_within(run_attend(q, k, v, qb, kb, [150], 0.125, **f), want, bound, "attend")
+
+
+@pytest.mark.parametrize("q_len,n", [(0, 40), (3, 0), (80, 0)])
+def test_attend_nothing_to_see_with_documents(q_len, n):
+    """No queries, or no keys at all, beside documents and positions."""
+    say("attend nothing", q_len, n)
+    dt = torch.float16
+    q = torch.ones((q_len, 2, 64), dtype=dt, device="cuda")
+    k = torch.ones((n, 1, 64), dtype=dt, device="cuda")
+    ints = lambda *shape: torch.zeros(shape, dtype=torch.int32, device="cuda")
+    f = dict(q_doc=ints(q_len), k_doc=ints(n), q_pos=ints(q_len, 2), k_pos=ints(n, 2),
+             slope=torch.ones(2))
+    out = run_attend(q, k, k, [0, q_len], [0], [n], 0.125, **f)
+    assert out.shape == q.shape and bool((out == 0).all())

@@ -20,3 +20,10 @@ def test_rotate_more_than_one_launch():
 def test_attend_more_than_one_launch(queries):
     assert attend(n_seqs=(1 << 31) - 1, max_q_len=queries, max_kv_len=1,
                   n_q_rows=(1 << 31) - 1) == tg.E_INVAL
+
+
+@pytest.mark.parametrize("none", [dict(q_doc=None), dict(k_doc=None), dict(q_pos=None)])
+def test_attend_arrays_of_no_rows(none):
+    """An array of no rows is null as often as not: there is nothing to do."""
+    assert attend(n_q_rows=0, **none) == tg.OK
+    assert attend(n_seqs=0, **none) == tg.OK
