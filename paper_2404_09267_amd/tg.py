@@ -782,6 +782,11 @@ def _values(t, dtype, dims, name, shape=None):
         raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
 
 
+def _rows(t):
+    """Pointer and strides of rows and heads; 0 for one row or head, whose stride may be anything."""
+    return (t.data_ptr(), *(t.stride(i) if t.shape[i] > 1 else 0 for i in (0, 1)))
+
+
 class Adapters:
     """Low-rank adapters on the device: a [n, rank, k], b [n, outputs, rank], scale [n]."""
 
@@ -896,16 +901,13 @@ def rotate_args(q, k, q_weight, k_weight, table, pos, q_out, k_out, v=None, v_ou
     if pos.dim() != 2 or pos.shape[0] != n_tokens:
         raise ValueError("pos must be [tokens, axes]")
     a = RotateArgs()
-    a.q, a.q_stride, a.q_head_stride = q.data_ptr(), q.stride(0), q.stride(1)
-    a.k, a.k_stride, a.k_head_stride = k.data_ptr(), k.stride(0), k.stride(1)
-    a.q_out, a.q_out_stride, a.q_out_head_stride = (q_out.data_ptr(), q_out.stride(0),
-                                                    q_out.stride(1))
-    a.k_out, a.k_out_stride, a.k_out_head_stride = (k_out.data_ptr(), k_out.stride(0),
-                                                    k_out.stride(1))
+    a.q, a.q_stride, a.q_head_stride = _rows(q)
+    a.k, a.k_stride, a.k_head_stride = _rows(k)
+    a.q_out, a.q_out_stride, a.q_out_head_stride = _rows(q_out)
+    a.k_out, a.k_out_stride, a.k_out_head_stride = _rows(k_out)
     if v is not None:
-        a.v, a.v_stride, a.v_head_stride = v.data_ptr(), v.stride(0), v.stride(1)
-        a.v_out, a.v_out_stride, a.v_out_head_stride = (v_out.data_ptr(), v_out.stride(0),
-                                                        v_out.stride(1))
+        a.v, a.v_stride, a.v_head_stride = _rows(v)
+        a.v_out, a.v_out_stride, a.v_out_head_stride = _rows(v_out)
     a.q_weight = q_weight.data_ptr() if q_weight is not None else None
     a.k_weight = k_weight.data_ptr() if k_weight is not None else None
     a.table, a.pos = table.data_ptr(), pos.data_ptr()
@@ -983,10 +985,10 @@ def attend_args(q, k, v, seqs: Sequences, out, bufs: AttendBuffers, scale: float
     if (q_doc is None) != (k_doc is None) or (q_pos is None) != (k_pos is None):
         raise ValueError("documents and positions: of queries and keys, or of neither")
     a = AttendArgs()
-    a.q, a.q_stride, a.q_head_stride = q.data_ptr(), q.stride(0), q.stride(1)
-    a.k, a.k_stride, a.k_head_stride = k.data_ptr(), k.stride(0), k.stride(1)
-    a.v, a.v_stride, a.v_head_stride = v.data_ptr(), v.stride(0), v.stride(1)
-    a.out, a.out_stride, a.out_head_stride = out.data_ptr(), out.stride(0), out.stride(1)
+    a.q, a.q_stride, a.q_head_stride = _rows(q)
+    a.k, a.k_stride, a.k_head_stride = _rows(k)
+    a.v, a.v_stride, a.v_head_stride = _rows(v)
+    a.out, a.out_stride, a.out_head_stride = _rows(out)
     a.q_begin, a.kv_begin, a.kv_len = (seqs.q_begin.data_ptr(), seqs.kv_begin.data_ptr(),
                                        seqs.kv_len.data_ptr())
     a.prefix = seqs.prefix.data_ptr() if seqs.prefix is not None else None

@@ -238,3 +238,18 @@ def test_attend_nothing_to_see_with_documents(q_len, n):
              slope=torch.ones(2))
     out = run_attend(q, k, k, [0, q_len], [0], [n], 0.125, **f)
     assert out.shape == q.shape and bool((out == 0).all())
+
+
+def test_one_row_or_head_of_any_stride():
+    """A dimension of one element has a stride that nothing is reached by."""
+    say("one row")
+    g, dt, d, rows = gen(40), torch.bfloat16, 64, 90
+    odd = lambda t, s: t.as_strided(t.shape, s)
+    q, k, v = (normal(g, n, 1, d, dtype=dt).cuda() for n in (1, rows, rows))
+    want, bound = R.attend(q.cpu(), k.cpu(), v.cpu(), [0, 1], [0], [rows], 0.125)
+    out = odd(torch.empty_like(q), (1 << 40, 3, 1))
+    run_attend(odd(q, (12345, 1 << 33, 1)), odd(k, (d, 7, 1)), v, [0, 1], [0], [rows], 0.125, out=out)
+    R.assert_within(out, want, bound, "attend")
+    one = odd(k[:1], (1 << 30, 1, 1))
+    run_attend(q, one, one, [0, 1], [0], [1], 0.125, out=out)
+    assert bool((out == one).all())
