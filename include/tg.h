@@ -690,7 +690,9 @@ typedef struct {
   size_t workspace_bytes;
 } tg_attend_args;
 
-/* Device scratch tg_attend needs (0 when it needs none, or for bad arguments). */
+/* Device scratch tg_attend needs (0 when it needs none, or for bad arguments). With the same heads
+ * and d it does not shrink as the other sizes grow: what does for the largest batch does for any
+ * smaller one. */
 size_t tg_attend_workspace_bytes(int32_t n_seqs, int32_t n_q_rows, int32_t max_q_len,
                                  int32_t max_kv_len, int32_t n_heads, int32_t n_kv_heads,
                                  int32_t d);

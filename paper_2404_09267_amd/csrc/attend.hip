@@ -1187,12 +1187,26 @@ struct Few {
   int splits;  // of the other form
 };
 
-Few few_of(int n_seqs, int n_q_rows, int max_q, int max_kv, int n_heads, int n_kv_heads, int d,
+constexpr int kFewRows = 64;
+// Of the form for few queries, keys that are not cut, as the join's launch costs more: up to 512,
+// or 1,024 where the sequences alone make 64 workgroups. 16 heads, us cut and not: 20 queries of
+// heads of 64 over 4, 500 keys 12.4, 8.8, 1,000 keys 13.0, 13.1; of heads of 128, 700 keys 17.7,
+// 15.0; 64 queries, 8 heads of 128 over 2, 1,000 keys 28, 20; but 1 query, 32 heads over 8, 1,000
+// keys 12.7, 18.6.
+constexpr int kWhole = 512, kWholeOfMany = 1024, kManyWorkgroups = 64;
+int whole_keys(int64_t workgroups) {
+  return workgroups >= kManyWorkgroups ? kWholeOfMany : kWhole;
+}
+// Of the other form, the workgroups that tiles' keys are cut for, and the key tiles of a part.
+constexpr int kTileWorkgroups = 768, kTilesOfPart = 12;
+int64_t key_tiles(int max_kv) { return (int64_t(max_kv) + kBN - 1) / kBN; }
+
+Few few_of(int n_seqs, int n_q_rows, int max_q, int max_kv, int n_heads, int n_kv_heads,
             bool causal, bool docs) {
   Few r = {};
   const int64_t rows = int64_t(max_q) * (n_heads / n_kv_heads);
   const int64_t each = n_kv_heads * ((rows + 15) / 16);
-  r.use = rows <= 64;
+  r.use = rows <= kFewRows;
   if (!r.use) {
     // Tiles' keys are cut where the tiles alone would leave CUs idle: for 768 workgroups, or for 512
     // where most rows see about half of the keys, of 12 key tiles or more each, since the join
@@ -1208,21 +1222,15 @@ Few few_of(int n_seqs, int n_q_rows, int max_q, int max_kv, int n_heads, int n_k
     //   144 tiles, 1,024:                    25,  24,  28,  42
     //   528 tiles, 4,096:                    92,  97, 115, 182
     const int64_t blocks = (int64_t(n_q_rows) / kBM + n_seqs) * n_heads;
-    const int64_t key_tiles = (int64_t(max_kv) + kBN - 1) / kBN;
-    const int64_t want = causal && max_q > max_kv / 2 ? 512 : 768;
-    const int64_t splits =
-        std::min({(want + blocks / 2) / blocks, key_tiles / 12, int64_t(kMaxSplits)});
+    const int64_t want = causal && max_q > max_kv / 2 ? 512 : kTileWorkgroups;
+    const int64_t splits = std::min(
+        {(want + blocks / 2) / blocks, key_tiles(max_kv) / kTilesOfPart, int64_t(kMaxSplits)});
     r.splits = docs || splits < 1 ? 1 : static_cast<int>(splits);
     return r;
   }
   r.row_tiles = static_cast<int>((rows + 15) / 16);
-  // Few keys are not cut, as the join's launch costs more: up to 512, or 1,024 where the
-  // sequences alone make 64 workgroups. 16 heads, us cut and not: 20 queries of heads of 64 over 4,
-  // 500 keys 12.4, 8.8, 1,000 keys 13.0, 13.1; of heads of 128, 700 keys 17.7, 15.0; 64 queries, 8
-  // heads of 128 over 2, 1,000 keys 28, 20; but 1 query, 32 heads over 8, 1,000 keys 12.7, 18.6.
   const int64_t want = kFewWorkgroups;
-  const int whole = n_seqs * each >= 64 ? 1024 : 512;
-  if (n_seqs <= kMaxCut && n_seqs * each < want && max_kv > whole)
+  if (n_seqs <= kMaxCut && n_seqs * each < want && max_kv > whole_keys(n_seqs * each))
     r.width = static_cast<int>((want + each - 1) / each);
   return r;
 }
@@ -1273,20 +1281,34 @@ bool sizes_ok(int n_seqs, int n_q_rows, int max_q, int max_kv, int n_heads, int 
 
 }  // namespace
 
+// What a call needs, and every call of fewer sequences, rows or shorter ones with it: those have
+// more parts, or take the other form. The largest product of parts and rows is looked for per rows
+// of 16 in the form for few queries, and per number of parts in the other.
 extern "C" size_t tg_attend_workspace_bytes(int32_t n_seqs, int32_t n_q_rows, int32_t max_q_len,
                                             int32_t max_kv_len, int32_t n_heads,
                                             int32_t n_kv_heads, int32_t d) {
   if (!sizes_ok(n_seqs, n_q_rows, max_q_len, max_kv_len, n_heads, n_kv_heads, d)) return 0;
   if (n_seqs == 0 || n_q_rows == 0 || max_q_len == 0) return 0;
-  const Few few = few_of(n_seqs, n_q_rows, max_q_len, max_kv_len, n_heads, n_kv_heads, d,
-                         false, false);
-  if (!few.use)
-    return few.splits > 1 ? static_cast<size_t>(few.splits) * n_q_rows * n_heads * (d + 2) *
-                                sizeof(float)
-                          : 0;
-  if (few.width == 0) return 0;
-  return (static_cast<size_t>(few.width) + n_seqs) * n_kv_heads * few.row_tiles * 16 * (d + 2) *
-         sizeof(float);
+  const int64_t group = n_heads / n_kv_heads;
+  int64_t rows = 0;  // rows of d sums, a maximum and a sum of weights
+  const int64_t few_q = std::min<int64_t>(max_q_len, kFewRows / group);
+  for (int64_t row_tiles = 1; row_tiles <= (few_q * group + 15) / 16; ++row_tiles) {
+    const int64_t each = n_kv_heads * row_tiles;
+    if (max_kv_len <= whole_keys(each)) continue;
+    const int64_t most = max_kv_len <= kWholeOfMany ? kManyWorkgroups : kFewWorkgroups;
+    const int64_t seqs = std::min<int64_t>({n_seqs, kMaxCut, (most - 1) / each});
+    if (seqs > 0) rows = std::max(rows, ((kFewWorkgroups + each - 1) / each + seqs) * each * 16);
+  }
+  if (max_q_len * group > kFewRows) {
+    const int64_t most = std::min<int64_t>(key_tiles(max_kv_len) / kTilesOfPart, kMaxSplits);
+    for (int64_t splits = 2; splits <= most; ++splits) {
+      // the most tiles that are cut into so many, and the most rows that these can have
+      const int64_t tiles = 2 * kTileWorkgroups / (2 * splits - 1) / n_heads;
+      if (tiles > 0)
+        rows = std::max(rows, splits * std::min<int64_t>(n_q_rows, tiles * kBM - 1) * n_heads);
+    }
+  }
+  return static_cast<size_t>(rows) * (d + 2) * sizeof(float);
 }
 
 extern "C" int tg_attend(const tg_attend_args *a, void *stream) {
@@ -1309,10 +1331,18 @@ extern "C" int tg_attend(const tg_attend_args *a, void *stream) {
                !layout_ok(a->v, a->v_stride, a->v_head_stride)))
     return TG_E_INVAL;
   const Few few = few_of(a->n_seqs, a->n_q_rows, a->max_q_len, a->max_kv_len, a->n_heads,
-                         a->n_kv_heads, a->d, a->causal != 0, a->q_doc != nullptr);
+                         a->n_kv_heads, a->causal != 0, a->q_doc != nullptr);
+  // rows of the parts that this call writes
+  const size_t parts =
+      few.use ? few.width == 0 ? 0
+                               : (static_cast<size_t>(few.width) + a->n_seqs) * a->n_kv_heads *
+                                     few.row_tiles * 16
+              : few.splits == 1 ? 0 : static_cast<size_t>(few.splits) * a->n_q_rows * a->n_heads;
+  const size_t written = parts * (a->d + 2) * sizeof(float);
   const size_t need = tg_attend_workspace_bytes(a->n_seqs, a->n_q_rows, a->max_q_len,
                                                 a->max_kv_len, a->n_heads, a->n_kv_heads, a->d);
-  if (need > 0 && (!a->workspace || a->workspace_bytes < need || !aligned16(a->workspace)))
+  if (need > 0 && (!a->workspace || a->workspace_bytes < std::max(need, written) ||
+                   !aligned16(a->workspace)))
     return TG_E_WORKSPACE;
 
   AttendParams P = {};
@@ -1367,10 +1397,7 @@ extern "C" int tg_attend(const tg_attend_args *a, void *stream) {
   P.width = few.width;
   P.part = static_cast<float *>(a->workspace);
   P.splits = few.splits;
-  P.part_ml =
-      P.part + (few.use ? (static_cast<size_t>(few.width) + a->n_seqs) * a->n_kv_heads *
-                              few.row_tiles * 16 * a->d
-                        : static_cast<size_t>(few.splits) * a->n_q_rows * a->n_heads * a->d);
+  P.part_ml = P.part + parts * a->d;
   hipStream_t s = static_cast<hipStream_t>(stream);
   if (a->d <= 64)
     return a->type == TG_F16 ? launch<TG_F16, 64>(P, few, s) : launch<TG_BF16, 64>(P, few, s);

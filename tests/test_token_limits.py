@@ -1,4 +1,5 @@
 """Limits of the token operators that the host checks before any HIP work (no GPU)."""
+import numpy as np
 import pytest
 
 from paper_2404_09267_amd import tg
@@ -27,3 +28,22 @@ def test_attend_arrays_of_no_rows(none):
     """An array of no rows is null as often as not: there is nothing to do."""
     assert attend(n_q_rows=0, **none) == tg.OK
     assert attend(n_seqs=0, **none) == tg.OK
+
+
+def less(rng, sizes):
+    """Sizes of which none is larger."""
+    return [int(rng.integers(1, n + 1)) if rng.random() < 0.7 else n for n in sizes]
+
+
+def test_attend_workspace_of_the_largest_batch_does_for_smaller_ones():
+    """Scratch is made once, for the largest batch; fewer sequences or queries may be cut into more
+    parts, and take another form."""
+    need = lambda sizes, heads: int(tg.lib().tg_attend_workspace_bytes(*sizes, *heads))
+    assert need((191, 191, 1, 4000), (32, 8, 128)) <= need((192, 192, 1, 4000), (32, 8, 128))
+    assert need((4, 64, 16, 4000), (32, 8, 128)) <= need((4, 68, 17, 4000), (32, 8, 128))
+    rng = np.random.default_rng(0)
+    for _ in range(20000):
+        kv = int(rng.choice([1, 2, 3, 4, 8, 16, 71, 1600]))
+        heads = (kv * int(rng.choice([1, 2, 4, 7, 8, 16, 71])), kv, int(rng.choice([8, 64, 72, 128])))
+        most = [int(2 ** rng.uniform(0, top)) for top in (10, 16, 13, 18)]
+        assert need(less(rng, most), heads) <= need(most, heads), (most, heads)
