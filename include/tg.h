@@ -588,7 +588,8 @@ typedef struct {
 } tg_project_args;
 
 /* Device scratch tg_project needs (0 when it needs none, or for bad arguments); n_adapters and
- * rank 0 when no token has an adapter. */
+ * rank 0 when no token has an adapter. With the same k, n and rank it does not shrink as the others
+ * grow: what does for the most tokens and adapters does for any fewer, and for none. */
 size_t tg_project_workspace_bytes(int32_t n_tokens, int32_t k, int32_t n, int32_t n_adapters,
                                   int32_t rank);
 

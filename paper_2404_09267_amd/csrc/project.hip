@@ -830,12 +830,23 @@ int launch(ProjectParams P, const Few &few, void *packed, hipStream_t s) {
 
 int pad_rank(int rank) { return rank <= 16 ? 16 : rank <= 32 ? 32 : 64; }
 
-// Bytes for b laid out anew: an odd rank, and not the few-token form, which reads it as it is.
-// What would take more than a few microseconds to lay out is gathered.
-size_t pack_bytes(int n_tokens, int n, int n_adapters, int rank) {
+// Adapters whose b may be laid out anew: with an odd rank, and not in the few-token form, which
+// reads it as it is. What would take more than a few microseconds to lay out is gathered.
+size_t pack_row_bytes(int n, int rank) { return size_t(n) * pad_rank(rank) * 2; }
+size_t most_packed(int n_tokens, int n, int rank) {
   if (rank % 2 == 0 || n_tokens <= kFewTokens) return 0;
-  const size_t bytes = size_t(n_adapters) * n * pad_rank(rank) * 2;
-  return bytes <= (size_t(64) << 20) ? bytes : 0;
+  return (size_t(64) << 20) / pack_row_bytes(n, rank);
+}
+
+// Sums over cuts of k, of any number of tokens up to this one: fewer may have more cuts.
+size_t part_bytes(int n_tokens, int k, int n, bool low) {
+  int64_t rows = 0;
+  for (int tokens : {32, 64, 128, 192, 256}) {  // the most of a number of tiles
+    const int t = std::min(tokens, n_tokens);
+    const Few few = few_of(t, k, n);
+    if (low || few.alone) rows = std::max<int64_t>(rows, int64_t(few.splits) * t);
+  }
+  return static_cast<size_t>(rows) * part_stride(n) * sizeof(float);
 }
 
 }  // namespace
@@ -846,10 +857,11 @@ extern "C" size_t tg_project_workspace_bytes(int32_t n_tokens, int32_t k, int32_
   const bool low = n_adapters > 0 && rank > 0;
   if (n_adapters > 0 && !low) return 0;
   const size_t t = static_cast<size_t>(n_tokens);
-  const Few few = few_of(n_tokens, k, n);
-  size_t bytes = low ? t * pad_rank(rank) * (2 * 2 + sizeof(float)) : 0;
-  if (low) bytes += pack_bytes(n_tokens, n, n_adapters, rank);
-  if (few.use && (low || few.alone)) bytes += few.splits * t * part_stride(n) * sizeof(float);
+  size_t bytes = part_bytes(n_tokens, k, n, low);
+  if (low) {
+    bytes += t * pad_rank(rank) * (2 * 2 + sizeof(float));
+    bytes += std::min<size_t>(n_adapters, most_packed(n_tokens, n, rank)) * pack_row_bytes(n, rank);
+  }
   return bytes;
 }
 
@@ -898,7 +910,7 @@ extern "C" int tg_project(const tg_project_args *a, void *stream) {
     P.h32 = static_cast<float *>(a->workspace);
     P.h = P.h32 + size_t(a->n_tokens) * P.pad_rank;
     P.part = P.h32 + size_t(a->n_tokens) * P.pad_rank * 2;
-    if (pack_bytes(a->n_tokens, a->n, a->n_adapters, a->rank) > 0) packed = P.part;
+    if (size_t(a->n_adapters) <= most_packed(a->n_tokens, a->n, a->rank)) packed = P.part;
     P.b_rank = a->rank;
   }
   hipStream_t s = static_cast<hipStream_t>(stream);
