@@ -425,17 +425,15 @@ __device__ __forceinline__ void store(const ProjectParams &P, int t0, int n0,
   }
 }
 
-// A tile of kT tokens x kN outputs, kWt x kWn waves, kBK values of k a step, kStages steps of
+// A tile of kT tokens x kN outputs, kWt x kWn waves, 64 values of k a step, kStages steps of
 // loads under way. The next 32 values' operands are read from LDS while these are multiplied, so
 // that the matrix units have work across the barrier; the buffer of step s is free for step
 // s + kStages behind the barrier at the end of it, since its operands are in registers by then.
-// Rows of a tile lie in LDS as kBK / 8 chunks of 16 bytes, in an order that serves the operands'
-// reads (one chunk of 16 rows) best: 156 bytes a cycle and CU measured with rows of 64 and 146
-// with rows of 32, where (row / 4) in the place of (row / 2) gives 116 and no change of order 123.
-template <int kBK>
-__device__ __forceinline__ int place_of(int row, int c) {
-  return c ^ ((row >> 1) & (kBK / 8 - 1));
-}
+// Rows of a tile lie in LDS as 8 chunks of 16 bytes, in an order that serves the operands' reads
+// (one chunk of 16 rows) best: 156 bytes a cycle and CU measured, where (row / 4) in the place of
+// (row / 2) gives 116 and no change of order 123.
+constexpr int kBK = 64;
+__device__ __forceinline__ int place_of(int row, int c) { return c ^ ((row >> 1) & 7); }
 
 // Which tile a workgroup takes: workgroups go round the 8 XCDs, so each XCD gets a run of tiles
 // of its own, in blocks of kGroup token tiles by all output tiles, whose operands its L2 shares.
@@ -450,14 +448,14 @@ __device__ __forceinline__ void tile_of(int id, int tiles_t, int tiles_n, int &t
   tn = in / rows;
 }
 
-template <int kType, int kT, int kN, int kWt, int kWn, int kBK, int kStages, bool kCut>
+template <int kType, int kT, int kN, int kWt, int kWn, int kStages, bool kCut>
 __global__ __launch_bounds__(kWt *kWn * 64, 2) void project_kernel(const ProjectParams P) {
   typedef Num<kType> N;
   typedef typename N::E E;
   typedef typename N::V8 V8;
   constexpr int kWaves = kWt * kWn, kFt = kT / kWt / 16, kFn = kN / kWn / 16;
   constexpr int kChunks = kBK / 8, kRows = kT + kN, kPer = 64 / kChunks;  // rows of one load
-  constexpr int kLoads = kRows / kPer / kWaves, kSub = kBK / 32;
+  constexpr int kLoads = kRows / kPer / kWaves;
   static_assert(kLoads * kPer * kWaves == kRows && kT % kPer == 0, "whole loads");
   __shared__ __attribute__((aligned(16))) E tile[kStages][kRows * kBK];
   __shared__ int s_id[kT], s_heads[kT], s_list[kT], s_counts[kWaves];
@@ -486,7 +484,7 @@ __global__ __launch_bounds__(kWt *kWn * 64, 2) void project_kernel(const Project
   // load i of a wave covers kPer rows; rows past the tensor are not read. A lane's chunk is the
   // same in all loads, since their rows are 4 kPer apart or more.
   static_assert(kWaves * kPer % 16 == 0, "rows of one lane");
-  const int chunk = place_of<kBK>(wave * kPer + lane / kChunks, lane % kChunks);
+  const int chunk = place_of(wave * kPer + lane / kChunks, lane % kChunks);
   uint32_t at[kLoads];
 #pragma unroll
   for (int i = 0; i < kLoads; ++i) {
@@ -557,12 +555,12 @@ __global__ __launch_bounds__(kWt *kWn * 64, 2) void project_kernel(const Project
 #pragma unroll
     for (int i = 0; i < kFt; ++i) {
       const int row = wt + 16 * i + col;
-      o.x[i] = *reinterpret_cast<const V8 *>(m + row * kBK + place_of<kBK>(row, ks * 4 + quad) * 8);
+      o.x[i] = *reinterpret_cast<const V8 *>(m + row * kBK + place_of(row, ks * 4 + quad) * 8);
     }
 #pragma unroll
     for (int j = 0; j < kFn; ++j) {
       const int row = kT + wn + 16 * j + col;
-      o.w[j] = *reinterpret_cast<const V8 *>(m + row * kBK + place_of<kBK>(row, ks * 4 + quad) * 8);
+      o.w[j] = *reinterpret_cast<const V8 *>(m + row * kBK + place_of(row, ks * 4 + quad) * 8);
     }
   };
   auto multiply = [&](const Operands &o) {
@@ -581,19 +579,17 @@ __global__ __launch_bounds__(kWt *kWn * 64, 2) void project_kernel(const Project
       if (loads && i < kLoads) __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);
     }
   };
-  // `now` has the first 32 values of step s; it, or `then`, is left with those of step s + 1
-  auto step = [&](int s, Operands &now, Operands &then, bool low) {
-    if constexpr (kSub == 2) {
-      read(then, s, 1);
-      multiply(now);
-      interleave(false);
-    }
-    Operands &last = kSub == 2 ? then : now, &next = kSub == 2 ? now : then;
+  // `now` has the first 32 values of step s, and is left with those of step s + 1
+  Operands now, then;
+  auto step = [&](int s, bool low) {
+    read(then, s, 1);
+    multiply(now);
+    interleave(false);
     wait_and_meet<(kStages - 2) * kLoads>();  // step s + 1 is here, step s in registers
     if (low && s + kStages >= main_steps) fetch_low(s + kStages);
     else fetch(s + kStages);
-    read(next, s + 1, 0);
-    multiply(last);
+    read(now, s + 1, 0);
+    multiply(then);
     interleave(true);
   };
   // steps of a small tile are short, so that they wait for their loads: where there are many they
@@ -614,18 +610,10 @@ __global__ __launch_bounds__(kWt *kWn * 64, 2) void project_kernel(const Project
     for (int s = begun; s < kStages; ++s) fetch_low(s);
   }
   wait_and_meet<(kStages - 1) * kLoads>();
-  Operands a, b;
-  read(a, 0, 0);
+  read(now, 0, 0);
   int s = 0;
-  constexpr int kTurn = kSub == 2 ? 1 : 2;  // steps after which a and b are back in their places
-  for (; s + kTurn - 1 + kStages < main_steps; s += kTurn) {
-    step(s, a, b, false);
-    if constexpr (kTurn == 2) step(s + 1, b, a, false);
-  }
-  for (; s < steps; s += kTurn) {  // a step past the last one multiplies zeros
-    step(s, a, b, steps_low);
-    if constexpr (kTurn == 2) step(s + 1, b, a, steps_low);
-  }
+  for (; s + kStages < main_steps; ++s) step(s, false);
+  for (; s < steps; ++s) step(s, steps_low);
   wait_loads();  // LDS belongs to the next workgroup from here on
   if constexpr (kCut) {
     float *to = P.part + int64_t(cut) * P.n_tokens * P.part_stride;
@@ -714,8 +702,7 @@ __global__ __launch_bounds__(kFinishThreads) void finish_kernel(const ProjectPar
 }
 
 // `first` enqueues what the tiles wait for, if they can be launched.
-template <int kType, int kT, int kN, int kWt, int kWn, int kBK, int kStages, bool kCut = false,
-          class First>
+template <int kType, int kT, int kN, int kWt, int kWn, int kStages, bool kCut = false, class First>
 int launch_tiles(ProjectParams P, hipStream_t s, const First &first) {
   const int64_t tiles_t = (int64_t(P.n_tokens) + kT - 1) / kT;
   const int64_t tiles_n = (int64_t(P.n) + kN - 1) / kN;
@@ -725,7 +712,7 @@ int launch_tiles(ProjectParams P, hipStream_t s, const First &first) {
   P.tiles_t = static_cast<int32_t>(tiles_t);
   P.tiles_n = static_cast<int32_t>(tiles_n);
   first();
-  hipLaunchKernelGGL((project_kernel<kType, kT, kN, kWt, kWn, kBK, kStages, kCut>),
+  hipLaunchKernelGGL((project_kernel<kType, kT, kN, kWt, kWn, kStages, kCut>),
                      dim3(static_cast<uint32_t>(blocks)), dim3(kWt * kWn * 64), 0, s, P);
   return TG_OK;
 }
@@ -762,8 +749,8 @@ int launch(ProjectParams P, const Few &few, void *packed, hipStream_t s) {
     P.splits = few.splits;
     P.low_blocks = P.adapter ? P.n_tokens * (P.pad_rank / kTokenRanks) : 0;
     const auto none = [] {};
-    rc = few.tile == 32 ? launch_tiles<kType, 32, 64, 1, 4, 64, 4, true>(P, s, none)
-                        : launch_tiles<kType, 64, 64, 2, 2, 64, 4, true>(P, s, none);
+    rc = few.tile == 32 ? launch_tiles<kType, 32, 64, 1, 4, 4, true>(P, s, none)
+                        : launch_tiles<kType, 64, 64, 2, 2, 4, true>(P, s, none);
     if (rc != TG_OK) return rc;
     hipLaunchKernelGGL(finish_kernel<kType>,
                        dim3((P.part_stride / 4 + kFinishThreads - 1) / kFinishThreads, P.n_tokens),
@@ -810,20 +797,20 @@ int launch(ProjectParams P, const Few &few, void *packed, hipStream_t s) {
   };
   P.b_whole = int64_t(P.n_adapters) * P.n * P.b_rank * 2 < (int64_t(1) << 31);
   P.gather = P.adapter && P.b_apart;  // rows of b that a load to LDS cannot take
-  if (P.gather) rc = launch_tiles<kType, 64, 64, 2, 2, 64, 4>(P, s, first);
+  if (P.gather) rc = launch_tiles<kType, 64, 64, 2, 2, 4>(P, s, first);
   else if (tiles(128, 128) > 256) {
     const auto rounds = [&](int t, int n, int at_once) { return (tiles(t, n) + at_once - 1) / at_once; };
     const int64_t c256 = 164 * rounds(256, 256, 256), c192 = 137 * rounds(192, 256, 256);
     const int64_t c160 = 118 * rounds(160, 128, 512), c128 = 100 * rounds(128, 128, 512);
     const int64_t least = std::min(std::min(c256, c192), std::min(c160, c128));
-    if (c256 == least) rc = launch_tiles<kType, 256, 256, 2, 4, 64, 2>(P, s, first);
-    else if (c192 == least) rc = launch_tiles<kType, 192, 256, 4, 2, 64, 2>(P, s, first);
-    else if (c160 == least) rc = launch_tiles<kType, 160, 128, 2, 2, 64, 2>(P, s, first);
-    else rc = launch_tiles<kType, 128, 128, 2, 2, 64, 2>(P, s, first);
+    if (c256 == least) rc = launch_tiles<kType, 256, 256, 2, 4, 2>(P, s, first);
+    else if (c192 == least) rc = launch_tiles<kType, 192, 256, 4, 2, 2>(P, s, first);
+    else if (c160 == least) rc = launch_tiles<kType, 160, 128, 2, 2, 2>(P, s, first);
+    else rc = launch_tiles<kType, 128, 128, 2, 2, 2>(P, s, first);
   }
-  else if (tiles(128, 128) >= 160) rc = launch_tiles<kType, 128, 128, 2, 4, 64, 4>(P, s, first);
-  else if (tiles(64, 64) > 256) rc = launch_tiles<kType, 128, 64, 2, 2, 64, 3>(P, s, first);
-  else rc = launch_tiles<kType, 64, 64, 2, 2, 64, 4>(P, s, first);
+  else if (tiles(128, 128) >= 160) rc = launch_tiles<kType, 128, 128, 2, 4, 4>(P, s, first);
+  else if (tiles(64, 64) > 256) rc = launch_tiles<kType, 128, 64, 2, 2, 3>(P, s, first);
+  else rc = launch_tiles<kType, 64, 64, 2, 2, 4>(P, s, first);
   if (rc != TG_OK) return rc;
   return hipGetLastError() == hipSuccess ? TG_OK : TG_E_HIP;
 }
