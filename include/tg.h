@@ -601,8 +601,9 @@ size_t tg_project_workspace_bytes(int32_t n_tokens, int32_t k, int32_t n, int32_
  * the second term only for tokens that have an adapter; an adapter's values reach no token
  * but its own, whatever they are (infinities and NaN included). Tokens may come in any order
  * of adapters; runs of one adapter are the fastest. y must not overlap an input. h is kept as
- * two values of the type each, the rounded one and what that left, or in binary32; everything
- * else is summed in binary32.
+ * two values of the type each, the rounded one and what that left (in binary16 times a power of
+ * two, so that they hold 22 bits of a row's largest), or in binary32; everything else is summed
+ * in binary32.
  * Enqueued on `stream`; the library allocates nothing. Returns TG_E_INVAL (null pointer,
  * negative count, k < 1 or not a multiple of 8, n < 1, with adapters n > 2^23, n_tokens > 2^28 or
  * a rank outside [1, TG_PROJECT_MAX_RANK], a bad type or stride, x, w or a not 16-byte aligned),

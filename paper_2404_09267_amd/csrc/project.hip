@@ -4,11 +4,14 @@
 // Two launches. With many tokens:
 //  1. shrink: h[t] = scale_g x[t] a_g^T for the tokens that have an adapter, in binary32, and as
 //     two values of the type whose sum is h (the first rounded, the second what that rounding
-//     left): 22 bits of binary16, 16 of bfloat16.
+//     left): 22 bits of binary16, 16 of bfloat16. In binary16 a row of smaller or larger numbers
+//     is first brought near 2^13 by a power of two: below 2^-14 bits would be lost, and above 2^16
+//     all.
 //  2. the product: tiles of x and w go through LDS to the matrix instructions. An adapter of the
 //     tile's tokens is some more steps of the same loop, with the two values of h in the place of
-//     x, 0 for tokens of other adapters, and b_g in the place of w: the joint takes no work of
-//     its own, and no further registers.
+//     x, 0 for tokens of other adapters, and b_g in the place of w: the joint takes no further
+//     registers and no work of its own, but that in binary16 a token's sums take on the power of
+//     two of its row of h before, and lose it after.
 // With few tokens, where launches and loads are what takes the time:
 //  1. tiles of x and w with k cut over workgroups, so that every CU has a share of w to read,
 //     and beside them one workgroup a token for its row of h;
@@ -51,6 +54,7 @@ struct ProjectParams {
   int32_t b_rank;    // values of a row of b: rank, or pad_rank when it has been laid out anew
   void *h;           // [n_tokens][2][pad_rank] of the type
   float *h32;        // [n_tokens][pad_rank]
+  float *h_up;       // [n_tokens]: the power of two that h has been multiplied by, in binary16
   int32_t gather;    // adapters are added by add_gathered
   int32_t b_whole;   // all of b is within the reach of one buffer
   float *part;       // [splits][n_tokens][part_stride]: sums over a cut of k
@@ -76,12 +80,28 @@ __device__ __forceinline__ void keep_h(const ProjectParams &P, int t, float (&v)
   typedef typename Num<kType>::E E;
   E *h = static_cast<E *>(P.h) + int64_t(t) * 2 * P.pad_rank;
   float *h32 = P.h32 + int64_t(t) * P.pad_rank;
+  float up = 1.0f;
+  if constexpr (kType == TG_F16) {
+    float most = 0.0f;
+#pragma unroll
+    for (int f = 0; f < kFrags; ++f) most = fmaxf(most, fabsf(v[f]));
+#pragma unroll
+    for (int o = 8; o > 0; o >>= 1) most = fmaxf(most, __shfl_xor(most, o));
+    // Rows with a largest from 2^-3 to 2^15 have their 22 bits as they are. Up to 2^60 either way:
+    // sums of binary16 products stay far from binary32's ends, and h below 2^-47 adds less than
+    // half of binary16's smallest number to any result.
+    const int e = static_cast<int>(__builtin_bit_cast(uint32_t, most) >> 23) - 127;
+    if (e < -3 || e >= 15)
+      up = __builtin_bit_cast(float, (min(max(13 - e, -60), 60) + 127) << 23);
+    if (r0 == 0) P.h_up[t] = up;
+  }
 #pragma unroll
   for (int f = 0; f < kFrags; ++f) {
-    const E hi = static_cast<E>(v[f]);
+    const float w = v[f] * up;
+    const E hi = static_cast<E>(w);
     h32[f * 16 + r0] = v[f];
     h[f * 16 + r0] = hi;
-    h[P.pad_rank + f * 16 + r0] = static_cast<E>(v[f] - static_cast<float>(hi));
+    h[P.pad_rank + f * 16 + r0] = static_cast<E>(w - static_cast<float>(hi));
   }
 }
 
@@ -459,6 +479,7 @@ __global__ __launch_bounds__(kWt *kWn * 64, 2) void project_kernel(const Project
   static_assert(kLoads * kPer * kWaves == kRows && kT % kPer == 0, "whole loads");
   __shared__ __attribute__((aligned(16))) E tile[kStages][kRows * kBK];
   __shared__ int s_id[kT], s_heads[kT], s_list[kT], s_counts[kWaves];
+  __shared__ float s_up[kType == TG_F16 && !kCut ? kT : 1];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int col = lane & 15, quad = lane >> 4;
@@ -580,8 +601,7 @@ __global__ __launch_bounds__(kWt *kWn * 64, 2) void project_kernel(const Project
     }
   };
   // `now` has the first 32 values of step s, and is left with those of step s + 1
-  Operands now, then;
-  auto step = [&](int s, bool low) {
+  auto step = [&](int s, Operands &now, Operands &then, bool low) {
     read(then, s, 1);
     multiply(now);
     interleave(false);
@@ -597,11 +617,18 @@ __global__ __launch_bounds__(kWt *kWn * 64, 2) void project_kernel(const Project
   bool gather = P.adapter && P.gather;
   const bool steps_low = !kCut && P.adapter && !P.gather;
   int id = -1;
-  if (steps_low && threadIdx.x < kT) id = adapter_of(P, t0 + threadIdx.x);
+  float up = 1.0f;
+  if (steps_low && threadIdx.x < kT) {
+    id = adapter_of(P, t0 + threadIdx.x);
+    if (kType == TG_F16 && t0 + threadIdx.x < P.n_tokens) up = P.h_up[t0 + threadIdx.x];
+  }
   const int begun = steps_low ? min(main_steps, kStages) : kStages;
   for (int s = 0; s < begun; ++s) fetch(s);
   if (steps_low) {
-    if (threadIdx.x < kT) s_id[threadIdx.x] = id;
+    if (threadIdx.x < kT) {
+      s_id[threadIdx.x] = id;
+      if (kType == TG_F16) s_up[threadIdx.x] = id < 0 ? 1.0f : up;
+    }
     __syncthreads();
     n_low = distinct<kT, kWaves>(s_id, s_heads, s_list, s_counts);
     const int more = (n_low * slot + kBK - 1) / kBK;
@@ -610,10 +637,31 @@ __global__ __launch_bounds__(kWt *kWn * 64, 2) void project_kernel(const Project
     for (int s = begun; s < kStages; ++s) fetch_low(s);
   }
   wait_and_meet<(kStages - 1) * kLoads>();
-  read(now, 0, 0);
+  Operands a, b;
+  read(a, 0, 0);
   int s = 0;
-  for (; s + kStages < main_steps; ++s) step(s, false);
-  for (; s < steps; ++s) step(s, steps_low);
+  for (; s + kStages < main_steps; ++s) step(s, a, b, false);
+  // a token's sums times the power of two of its row of h, and back (the exponent negated)
+  auto scale = [&](bool back) {
+#pragma unroll
+    for (int i = 0; i < kFt; ++i) {
+      const float up = s_up[wt + 16 * i + col];
+      if (!__ballot(up != 1.0f)) continue;
+      const uint32_t f = __builtin_bit_cast(uint32_t, up);
+      const float by = __builtin_bit_cast(float, back ? 0x7F000000u - f : f);
+#pragma unroll
+      for (int j = 0; j < kFn; ++j) acc[j][i] *= by;
+    }
+  };
+  for (; s < steps; ++s) {
+    if constexpr (kType == TG_F16 && !kCut) {
+      if (s == main_steps) scale(false);
+    }
+    step(s, a, b, steps_low);
+  }
+  if constexpr (kType == TG_F16 && !kCut) {
+    if (steps > main_steps) scale(true);
+  }
   wait_loads();  // LDS belongs to the next workgroup from here on
   if constexpr (kCut) {
     float *to = P.part + int64_t(cut) * P.n_tokens * P.part_stride;
@@ -817,6 +865,12 @@ int launch(ProjectParams P, const Few &few, void *packed, hipStream_t s) {
 
 int pad_rank(int rank) { return rank <= 16 ? 16 : rank <= 32 ? 32 : 64; }
 
+// Bytes of h: two values of the type and one of binary32 a rank, and a power of two a token.
+size_t h_bytes(size_t n_tokens, int rank) {
+  return n_tokens * pad_rank(rank) * (2 * 2 + sizeof(float)) +
+         (n_tokens + 3) / 4 * 4 * sizeof(float);
+}
+
 // Adapters whose b may be laid out anew: with an odd rank, and not in the few-token form, which
 // reads it as it is. What would take more than a few microseconds to lay out is gathered.
 size_t pack_row_bytes(int n, int rank) { return size_t(n) * pad_rank(rank) * 2; }
@@ -843,10 +897,9 @@ extern "C" size_t tg_project_workspace_bytes(int32_t n_tokens, int32_t k, int32_
   if (n_tokens <= 0 || k <= 0 || n <= 0 || n_adapters < 0 || rank < 0) return 0;
   const bool low = n_adapters > 0 && rank > 0;
   if (n_adapters > 0 && !low) return 0;
-  const size_t t = static_cast<size_t>(n_tokens);
   size_t bytes = part_bytes(n_tokens, k, n, low);
   if (low) {
-    bytes += t * pad_rank(rank) * (2 * 2 + sizeof(float));
+    bytes += h_bytes(n_tokens, rank);
     bytes += std::min<size_t>(n_adapters, most_packed(n_tokens, n, rank)) * pack_row_bytes(n, rank);
   }
   return bytes;
@@ -896,7 +949,8 @@ extern "C" int tg_project(const tg_project_args *a, void *stream) {
     P.b_apart = a->rank % 2 != 0 || at % 4 != 0;
     P.h32 = static_cast<float *>(a->workspace);
     P.h = P.h32 + size_t(a->n_tokens) * P.pad_rank;
-    P.part = P.h32 + size_t(a->n_tokens) * P.pad_rank * 2;
+    P.h_up = P.h32 + size_t(a->n_tokens) * P.pad_rank * 2;
+    P.part = P.h32 + h_bytes(a->n_tokens, a->rank) / sizeof(float);
     if (size_t(a->n_adapters) <= most_packed(a->n_tokens, a->n, a->rank)) packed = P.part;
     P.b_rank = a->rank;
   }

@@ -7,7 +7,7 @@ import torch
 
 from gpu_helpers import say
 from paper_2404_09267_amd import tg
-from test_tokens_gpu import NAN, gen, make, normal, run_attend
+from test_tokens_gpu import NAN, gen, make, normal, run_attend, run_project
 import token_reference as R
 
 pytestmark = pytest.mark.gpu
@@ -42,6 +42,24 @@ def test_project_adapters_past_one_buffer(rank):
     tg.project(x, w, bufs, tg.Adapters(a, b, scale.cuda()), ids.cuda())
     torch.cuda.synchronize()
     R.assert_within(bufs.y, want, bound, "project")
+
+
+@pytest.mark.parametrize("tokens", [200, 300, 2100])
+def test_project_small_rows_of_h(tokens):
+    """Rows of h far below binary16's smallest normal number, and b large: as exact as others."""
+    say("project small h", tokens)
+    g, k, n, dt = gen(31), 64, 160, torch.float16
+    x, w = normal(g, tokens, k, dtype=dt), normal(g, n, k, dtype=dt) * 0
+    a = normal(g, 3, 8, k, dtype=dt, gain=2.0 ** -6)
+    x[::3] *= 2.0 ** -9
+    b = normal(g, 3, n, 8, dtype=dt, gain=1024.0)
+    scale = torch.tensor([2.0 ** -18, 1.0, 2.0 ** 9])
+    a[2] *= 2.0 ** 9  # and rows of h past its largest, with a b to match
+    b[2] *= 2.0 ** -20
+    ids = (torch.arange(tokens) // 7 % 4).int() - 1
+    w[::5] = normal(g, len(range(0, n, 5)), k, dtype=dt, gain=0.1)
+    want, bound = R.project(x, w, a, b, scale, ids)
+    R.assert_within(run_project(x, w, (a, b, scale), ids), want, bound, "project")
 
 
 # -------------------------------------------------------------------------------- rotate
