@@ -221,59 +221,72 @@ __device__ __forceinline__ float abs_diff(int a, int b) {  // of any two
 // Whether a row's sum holds its largest weight, which is 1 at least if it was not rounded away.
 __device__ __forceinline__ bool full_sum(float m, float l) { return l >= 0.5f || m == -INFINITY; }
 
-// One query row of one head, by one wave, unseen keys left out one by one.
+// One query row of one head, by one wave, unseen keys left out one by one: a lane a key's score,
+// then 8 or 16 lanes a key's values. A NaN that is seen in the query or a key is all of the result,
+// so that the rest is not looked at. bfloat16, the 7 prompts of up to 2,077 with a cap below, all of
+// whose rows come here: 17 ms for 0.15 with a NaN in every value, 1.3 in every query.
 template <int kType>
 __device__ __forceinline__ void strict_row(const AttendParams &P, const Seq &s, int i,
                                            int head) {
   typedef typename Num<kType>::E E;
+  typedef typename Num<kType>::V8 V8;
   const int lane = threadIdx.x & 63;
   const int64_t row = int64_t(s.q0) + i;
   const E *q = static_cast<const E *>(P.q) + row * P.q_stride + head * P.q_head;
-  const E *k = static_cast<const E *>(P.k) + (head / P.group) * P.k_head;
-  const E *v = static_cast<const E *>(P.v) + (head / P.group) * P.v_head;
+  const E *k = static_cast<const E *>(P.k) + (head / P.group) * P.k_head + s.k0 * P.k_stride;
   const int limit = key_limit(P, s, i), place = s.place0 + i;
   const int doc = P.q_doc ? P.q_doc[row] : 0;
   const float slope2 = P.slope ? P.slope[head] * kLog2e : 0.0f;
-  auto score = [&](int j, bool &seen) {
-    seen = j < limit && doc >= 0 && (!P.k_doc || P.k_doc[s.k0 + j] == doc);
-    if (!seen) return -INFINITY;
-    const E *kr = k + (s.k0 + j) * P.k_stride;
-    float z = 0.0f;
-    for (int c = 0; c < P.d; ++c) z += static_cast<float>(q[c]) * static_cast<float>(kr[c]);
-    float far = abs_diff(place, j);
-    if (P.k_pos)
-      far = abs_diff(P.q_pos[2 * row], P.k_pos[2 * (s.k0 + j)]) +
-            abs_diff(P.q_pos[2 * row + 1], P.k_pos[2 * (s.k0 + j) + 1]);
-    return shape(P, z, slope2, P.slope ? far : 0.0f);
-  };
-  float m = -INFINITY;
-  for (int j = lane; j < limit; j += 64) {
-    bool seen;
-    m = fmaxf(m, score(j, seen));
-  }
-  m = wave_max(m);
-  if (m == -INFINITY) m = 0.0f;
-  float l = 0.0f, sum[TG_ATTEND_MAX_D / 64] = {};
-  for (int j0 = 0; j0 < limit; j0 += 64) {
-    bool seen = false;
-    const float z = score(j0 + lane, seen);
-    const float p = seen ? __builtin_amdgcn_exp2f(z - m) : 0.0f;
-    l += p;
-    for (uint64_t left = __ballot(seen); left; left &= left - 1) {
-      const int at = __builtin_ctzll(left);
-      const float w = __shfl(p, at);
-      const E *vr = v + (s.k0 + j0 + at) * P.v_stride;
+  const int wide = P.d <= 64 ? 8 : 16, c = lane % wide * 8, own = lane / wide;
+  const E *v = static_cast<const E *>(P.v) + (head / P.group) * P.v_head + s.k0 * P.v_stride + c;
+  float m = -INFINITY, l = 0.0f, sum[8] = {};
+  bool lost = false;
+  for (int j0 = 0; j0 < limit && !lost; j0 += 64) {
+    const int j = j0 + lane;
+    const bool seen = j < limit && doc >= 0 && (!P.k_doc || P.k_doc[s.k0 + j] == doc);
+    const uint64_t all = __ballot(seen);
+    if (!all) continue;
+    float z = -INFINITY;
+    if (seen) {
+      const E *kr = k + j * P.k_stride;
+      float dot = 0.0f;
+      for (int e0 = 0; e0 < P.d; e0 += 8) {
+        const V8 a = *reinterpret_cast<const V8 *>(q + e0);
+        const V8 b = *reinterpret_cast<const V8 *>(kr + e0);
 #pragma unroll
-      for (int c = 0; c < TG_ATTEND_MAX_D / 64; ++c)
-        if (lane + 64 * c < P.d) sum[c] += w * static_cast<float>(vr[lane + 64 * c]);
+        for (int e = 0; e < 8; ++e) dot += static_cast<float>(a[e]) * static_cast<float>(b[e]);
+      }
+      float far = abs_diff(place, j);
+      if (P.k_pos)
+        far = abs_diff(P.q_pos[2 * row], P.k_pos[2 * (s.k0 + j)]) +
+              abs_diff(P.q_pos[2 * row + 1], P.k_pos[2 * (s.k0 + j) + 1]);
+      z = shape(P, dot, slope2, P.slope ? far : 0.0f);
+    }
+    lost = __ballot(z != z) != 0;
+    const float to = fmaxf(m, wave_max(z));
+    const float fix = to == m ? 1.0f : __builtin_amdgcn_exp2f(m - to);
+    m = to;
+    const float p = seen ? __builtin_amdgcn_exp2f(z - (m == -INFINITY ? 0.0f : m)) : 0.0f;
+    l = l * fix + p;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) sum[e] *= fix;
+    for (int u = own; u < 64; u += 64 / wide) {
+      const float w = __shfl(p, u);
+      if (!(all >> u & 1) || c >= P.d) continue;
+      const V8 x = *reinterpret_cast<const V8 *>(v + int64_t(j0 + u) * P.v_stride);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) sum[e] += w * static_cast<float>(x[e]);
     }
   }
   l = wave_sum(l);
-  E *o = static_cast<E *>(P.out) + row * P.out_stride + head * P.out_head;
+  V8 out;
 #pragma unroll
-  for (int c = 0; c < TG_ATTEND_MAX_D / 64; ++c)
-    if (lane + 64 * c < P.d)
-      o[lane + 64 * c] = static_cast<E>(l == 0.0f ? 0.0f : sum[c] / l);
+  for (int e = 0; e < 8; ++e) {
+    for (int o = wide; o < 64; o <<= 1) sum[e] += __shfl_xor(sum[e], o);
+    out[e] = static_cast<E>(lost ? NAN : l == 0.0f ? 0.0f : sum[e] / l);
+  }
+  E *o = static_cast<E *>(P.out) + row * P.out_stride + head * P.out_head;
+  if (own == 0 && c < P.d) *reinterpret_cast<V8 *>(o + c) = out;
 }
 
 // Place of 16-byte chunk c of row r in a tile of rows of kChunks chunks (8 or 16). Matrix

@@ -271,3 +271,38 @@ def test_one_row_or_head_of_any_stride():
     one = odd(k[:1], (1 << 30, 1, 1))
     run_attend(q, one, one, [0, 1], [0], [1], 0.125, out=out)
     assert bool((out == one).all())
+
+
+def test_broken_values_do_not_stall():
+    """All results NaN: formed again one by one, which must not take hundreds of times as long."""
+    say("broken values")
+    g, dt, n = gen(44), torch.bfloat16, 4096
+
+    def took(call):
+        call()
+        best = math.inf
+        for _ in range(3):
+            a, b = (torch.cuda.Event(enable_timing=True) for _ in range(2))
+            a.record()
+            call()
+            b.record()
+            torch.cuda.synchronize()
+            best = min(best, a.elapsed_time(b))
+        return best
+
+    q, k, v = (normal(g, n, h, 128, dtype=dt).cuda() for h in (8, 2, 2))
+    seqs = tg.Sequences(*(torch.tensor(t, dtype=i).cuda() for t, i in (
+        ([0, n], torch.int32), ([0], torch.int64), ([n], torch.int32))), n, n)
+    out, bufs = torch.empty_like(q), tg.AttendBuffers(seqs, q, k)
+    call = lambda: tg.attend(q, k, v, seqs, out, bufs, 0.1, causal=True)
+    well = took(call)
+    q[:, :, 7] = NAN
+    assert took(call) < 60 * well and bool(torch.isnan(out).all())
+    x, w = normal(g, n, 1024, dtype=dt).cuda(), normal(g, 1024, 1024, dtype=dt).cuda()
+    low = tg.Adapters(normal(g, 2, 16, 1024, dtype=dt).cuda(), normal(g, 2, 1024, 16, dtype=dt).cuda(),
+                      torch.ones(2, device="cuda"))
+    ids, pb = (torch.arange(n, device="cuda") // 100 % 2).int(), tg.ProjectBuffers(n, 1024, 1024, dt, low)
+    call = lambda: tg.project(x, w, pb, low, ids)
+    well = took(call)
+    x[:, 7] = NAN
+    assert took(call) < 60 * well and bool(torch.isnan(pb.y).all())
