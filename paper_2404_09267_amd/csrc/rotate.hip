@@ -69,6 +69,15 @@ __device__ __forceinline__ int64_t out_row(const RotateParams &P, int which, int
   return r >= 0 && r < P.n_rows ? r : -1;
 }
 
+// 1 / sqrt(mean square + eps) of a head. Where the sum of squares has left binary32 it is formed
+// from `small`, that of the values times kDown, as ordinary bfloat16 can be so large.
+constexpr float kDown = 0x1p-70f;
+__device__ __forceinline__ float inverse_norm(const RotateParams &P, float sum, float small) {
+  const float d = static_cast<float>(P.d);
+  if (sum < INFINITY) return rsqrtf(sum / d + P.eps);
+  return rsqrtf(small / d + P.eps * kDown * kDown) * kDown;
+}
+
 // d a multiple of 16, rows and heads on 16-byte boundaries. Lane c of a head holds values 8 c ..
 // and their partners rot / 2 later (half pairs, rot a multiple of 16), or values 16 c .. where
 // pairs are neighbours.
@@ -142,12 +151,19 @@ __global__ __launch_bounds__(kThreads) void rotate_kernel(const RotateParams P) 
 #pragma unroll
     for (int i = 0; i < 16; ++i) sum += u[i] * u[i];
     for (int o = P.lanes >> 1; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
+    float small = sum;
+    if (kType == TG_BF16 && __ballot(!(sum < INFINITY))) {
+      small = 0.0f;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) small += (u[i] * kDown) * (u[i] * kDown);
+      for (int o = P.lanes >> 1; o > 0; o >>= 1) small += __shfl_xor(small, o);
+    }
     if (!use) continue;
     const int64_t row = out_row(P, which, t);
     if (row < 0) continue;
     E *to = static_cast<E *>(P.out[which]) + row * P.out_stride[which] + h * P.out_head[which];
     if (which < 2) {
-      const float inv = rsqrtf(sum / static_cast<float>(P.d) + P.eps);
+      const float inv = inverse_norm(P, sum, small);
       V8 wa, wb;
       const E *w = static_cast<const E *>(P.weight[which]);
       if (w) {
@@ -202,7 +218,7 @@ __global__ __launch_bounds__(kThreads) void rotate_any_kernel(const RotateParams
                h * P.in_head[which];
   constexpr int kMost = kMaxD / 128;  // pairs a lane may hold
   E va[kMost], vb[kMost];
-  float sum = 0.0f;
+  float sum = 0.0f, small = 0.0f;
 #pragma unroll
   for (int k = 0; k < kMost; ++k) {
     const int i = lane + 64 * k;
@@ -213,13 +229,15 @@ __global__ __launch_bounds__(kThreads) void rotate_any_kernel(const RotateParams
       vb[k] = p[y];
       const float fa = static_cast<float>(va[k]), fb = static_cast<float>(vb[k]);
       sum += fa * fa + fb * fb;
+      small += (fa * kDown) * (fa * kDown) + (fb * kDown) * (fb * kDown);
     }
   }
   sum = wave_sum(sum);
+  if (!(sum < INFINITY)) small = kType == TG_BF16 ? wave_sum(small) : sum;  // in every lane
   const int64_t row = out_row(P, which, t);
   if (row < 0) return;
   E *to = static_cast<E *>(P.out[which]) + row * P.out_stride[which] + h * P.out_head[which];
-  const float inv = rsqrtf(sum / static_cast<float>(P.d) + P.eps);
+  const float inv = inverse_norm(P, sum, small);
   const E *w = which < 2 ? static_cast<const E *>(P.weight[which]) : nullptr;
 #pragma unroll
   for (int k = 0; k < kMost; ++k) {

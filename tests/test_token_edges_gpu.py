@@ -7,7 +7,7 @@ import torch
 
 from gpu_helpers import say
 from paper_2404_09267_amd import tg
-from test_tokens_gpu import NAN, gen, make, normal, run_attend, run_project
+from test_tokens_gpu import NAN, gen, make, make_table, normal, run_attend, run_project
 import token_reference as R
 
 pytestmark = pytest.mark.gpu
@@ -80,6 +80,27 @@ def test_rotate_more_heads_than_a_row_of_workgroups():
         want, bound = R.rotate(q[t].cpu(), None, table.cpu(), pos[t].cpu(), 1e-6, False)
         R.assert_within(out[t].cpu(), want, bound, "rotate")
     assert bool(torch.isfinite(out).all())
+
+
+@pytest.mark.parametrize("tokens,heads,d,rot", [(5, 3, 64, 64), (7, 2, 34, 20), (3, 1, 512, 512),
+                                                (40, 8, 16, 0)])
+def test_rotate_values_whose_squares_overflow(tokens, heads, d, rot):
+    """bfloat16 reaches 3 * 10^38, squares of 2 * 10^19 pass it: the norm is that of the values."""
+    say("rotate huge", tokens, heads, d, rot)
+    g, dt = gen(45), torch.bfloat16
+    q, k = normal(g, tokens, heads, d, dtype=dt), normal(g, tokens, 1, d, dtype=dt)
+    q[1::2] *= 2.0 ** 70
+    q[2] *= 2.0 ** 50
+    k[::2] *= 2.0 ** 120
+    k[1, 0, :5] = 2.0 ** 100  # and next to ordinary ones
+    w, pos = normal(g, d, dtype=dt), torch.randint(0, 9, (tokens, 1), generator=g, dtype=torch.int32)
+    table = make_table(g, 9, rot // 2)
+    out, k_out = (torch.full(t.shape, NAN, dtype=dt, device="cuda") for t in (q, k))
+    tg.rotate(q.cuda(), k.cuda(), w.cuda(), None, table.cuda(), pos.cuda(), out, k_out)
+    torch.cuda.synchronize()
+    for got, x, by in ((out, q, w), (k_out, k, None)):
+        want, bound = R.rotate(x, by, table, pos, 1e-6, False)
+        R.assert_within(got, want, bound, "rotate")
 
 
 # -------------------------------------------------------------------------------- attend
