@@ -96,6 +96,7 @@ __global__ __launch_bounds__(kThreads) void rotate_kernel(const RotateParams P) 
   if (t >= P.n_tokens) return;
   const bool has = sub < P.d / 16;
   const bool turns = sub * 16 < P.rot;
+  const bool part = P.rot % 16 != 0;  // a lane may hold pairs that turn and others
   int c0, c1;  // first values of the two chunks
   if (kInterleaved || !turns) {
     c0 = 16 * sub;
@@ -104,7 +105,7 @@ __global__ __launch_bounds__(kThreads) void rotate_kernel(const RotateParams P) 
     c0 = 8 * sub;
     c1 = c0 + P.rot / 2;
   }
-  float cs[8][2];
+  float cs[8][2] = {};
   if (turns) {
     const int pair = kInterleaved ? c0 / 2 : c0;
     // the lane's 8 pairs are all turned, and on one axis
@@ -118,16 +119,12 @@ __global__ __launch_bounds__(kThreads) void rotate_kernel(const RotateParams P) 
     } else {
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        cs[i][0] = 1.0f, cs[i][1] = 0.0f;
         if (2 * (pair + i) < P.rot) {
           const float *row = table_row(P, t, pair + i);
           cs[i][0] = row[0], cs[i][1] = row[1];
         }
       }
     }
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) cs[i][0] = 1.0f, cs[i][1] = 0.0f;
   }
   for (int first = pass * step; first < P.rows; first += P.passes * step) {
     int h = first + (slot & (step - 1));
@@ -178,13 +175,17 @@ __global__ __launch_bounds__(kThreads) void rotate_kernel(const RotateParams P) 
         u[i] *= inv * static_cast<float>(wa[i]);
         u[8 + i] *= inv * static_cast<float>(wb[i]);
       }
+      // a pair that does not turn stays as it is: 0 times its partner would not, if that is infinite
+      if (turns) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const int x = kInterleaved ? 2 * i : i, y = kInterleaved ? 2 * i + 1 : 8 + i;
-        const float p = u[x] * cs[i][0] - u[y] * cs[i][1];
-        const float q = u[x] * cs[i][1] + u[y] * cs[i][0];
-        u[x] = p;
-        u[y] = q;
+        for (int i = 0; i < 8; ++i) {
+          const int x = kInterleaved ? 2 * i : i, y = kInterleaved ? 2 * i + 1 : 8 + i;
+          const float p = u[x] * cs[i][0] - u[y] * cs[i][1];
+          const float q = u[x] * cs[i][1] + u[y] * cs[i][0];
+          if (kInterleaved && part && 2 * (8 * sub + i) >= P.rot) continue;
+          u[x] = p;
+          u[y] = q;
+        }
       }
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
@@ -252,14 +253,14 @@ __global__ __launch_bounds__(kThreads) void rotate_any_kernel(const RotateParams
       }
       const float fa = static_cast<float>(va[k]) * inv * (w ? static_cast<float>(w[x]) : 1.0f);
       const float fb = static_cast<float>(vb[k]) * inv * (w ? static_cast<float>(w[y]) : 1.0f);
-      float c = 1.0f, s = 0.0f;
-      if (i < half) {
-        const float *r = table_row(P, t, i);
-        c = r[0];
-        s = r[1];
+      if (i >= half) {
+        to[x] = static_cast<E>(fa);
+        to[y] = static_cast<E>(fb);
+        continue;
       }
-      to[x] = static_cast<E>(fa * c - fb * s);
-      to[y] = static_cast<E>(fa * s + fb * c);
+      const float *r = table_row(P, t, i);
+      to[x] = static_cast<E>(fa * r[0] - fb * r[1]);
+      to[y] = static_cast<E>(fa * r[1] + fb * r[0]);
     }
   }
 }

@@ -7,7 +7,7 @@ import torch
 
 from gpu_helpers import say
 from paper_2404_09267_amd import tg
-from test_tokens_gpu import NAN, gen, make, make_table, normal, run_attend, run_project
+from test_tokens_gpu import DT, NAN, gen, make, make_table, normal, run_attend, run_project
 import token_reference as R
 
 pytestmark = pytest.mark.gpu
@@ -100,6 +100,28 @@ def test_rotate_values_whose_squares_overflow(tokens, heads, d, rot):
     torch.cuda.synchronize()
     for got, x, by in ((out, q, w), (k_out, k, None)):
         want, bound = R.rotate(x, by, table, pos, 1e-6, False)
+        R.assert_within(got, want, bound, "rotate")
+
+
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("d,rot", [(64, 0), (64, 32), (64, 36), (34, 0), (34, 10)])
+def test_rotate_infinite_and_nan_heads(d, rot, dtype, interleaved):
+    """An infinity leaves the rest of its head 0, NaN takes its head, and neither another one; a
+    value that does not turn does not see those beside it."""
+    say("rotate inf nan", d, rot, dtype, interleaved)
+    g, dt = gen(46), DT[dtype]
+    q, k = normal(g, 4, 2, d, dtype=dt), normal(g, 4, 1, d, dtype=dt)
+    q[0, 0, d - 1], k[0, 0, 1] = math.inf, NAN  # the last value turns in no case
+    table, pos = make_table(g, 3, rot // 2), torch.zeros((4, 1), dtype=torch.int32)
+    out, k_out = (torch.full(t.shape, NAN, dtype=dt, device="cuda") for t in (q, k))
+    tg.rotate(q.cuda(), k.cuda(), None, None, table.cuda(), pos.cuda(), out, k_out,
+              interleaved=interleaved)
+    torch.cuda.synchronize()
+    assert bool(torch.isnan(out[0, 0, d - 1])) and bool((out[0, 0, :d - 1] == 0).all())
+    assert bool(torch.isnan(k_out[0, 0]).all())
+    for got, x in ((out[1:], q[1:]), (out[:1, 1:], q[:1, 1:]), (k_out[1:], k[1:])):
+        want, bound = R.rotate(x, None, table, pos[:len(x)], 1e-6, interleaved)
         R.assert_within(got, want, bound, "rotate")
 
 
