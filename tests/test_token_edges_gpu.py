@@ -7,7 +7,8 @@ import torch
 
 from gpu_helpers import say
 from paper_2404_09267_amd import tg
-from test_tokens_gpu import DT, NAN, gen, make, make_table, normal, run_attend, run_project
+from test_tokens_gpu import DT, NAN, dev, features, gen, make, make_table, \
+    normal, run_attend, run_project
 import token_reference as R
 
 pytestmark = pytest.mark.gpu
@@ -60,6 +61,26 @@ def test_project_small_rows_of_h(tokens):
     w[::5] = normal(g, len(range(0, n, 5)), k, dtype=dt, gain=0.1)
     want, bound = R.project(x, w, a, b, scale, ids)
     R.assert_within(run_project(x, w, (a, b, scale), ids), want, bound, "project")
+
+
+@pytest.mark.parametrize("case", ["odd rank, 70 MB of b", "b between boundaries"])
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+def test_project_gathered_adapters(case, dtype):
+    """Rows of b that loads to LDS cannot take and that are not laid out anew."""
+    say("project gathered", case, dtype)
+    room(8)
+    g, dt = gen(32), DT[dtype]
+    tokens, k, n, adapters, rank = ((300, 72, 28001, 40, 17) if "odd" in case else
+                                    (333, 136, 515, 5, 12))
+    x, w = normal(g, tokens, k, dtype=dt).cuda(), normal(g, n, k, dtype=dt, gain=k ** -0.5).cuda()
+    a = normal(g, adapters, rank, k, dtype=dt, gain=k ** -0.5).cuda()
+    b = torch.empty(1 + adapters * n * rank, dtype=dt, device="cuda").normal_()
+    b = b[0 if "odd" in case else 1:][:adapters * n * rank].view(adapters, n, rank)
+    scale = 0.5 + torch.rand(adapters, generator=g)
+    ids = torch.randint(-1, adapters + 1, (tokens,), generator=g, dtype=torch.int32)
+    want, bound = R.project(x, w, a, b, scale, ids.cuda())
+    got = run_project(x, w, (a, b, scale), ids)
+    R.assert_within(got.cuda(), want, bound, "project")
 
 
 # -------------------------------------------------------------------------------- rotate
@@ -314,6 +335,136 @@ def test_one_row_or_head_of_any_stride():
     one = odd(k[:1], (1 << 30, 1, 1))
     run_attend(q, one, one, [0, 1], [0], [1], 0.125, out=out)
     assert bool((out == one).all())
+
+
+def clamped(q, k, v, qb, kb, kl, max_q, max_kv, scale):
+    """What the operator documents for tables that leave the tensors or the bounds: results, their
+    bounds, and which rows are written."""
+    n_q, n_k = q.shape[0], k.shape[0]
+    want = torch.zeros(q.shape, dtype=torch.float64)
+    bound = torch.full(q.shape, R.TINY[q.dtype], dtype=torch.float64)
+    written = torch.zeros(n_q, dtype=torch.bool)
+    for s in range(len(kb)):
+        a = min(max(qb[s], 0), n_q)
+        b = min(max(qb[s + 1], a), n_q)
+        k0 = kb[s] if 0 <= kb[s] < n_k else 0
+        n = min(max(kl[s], 0), n_k - k0, max_kv) if 0 <= kb[s] < n_k else 0
+        b = min(b, a + max_q)
+        written[a:b] = True
+        if n > 0 and b > a:
+            want[a:b], bound[a:b] = R.attend(q[a:b], k[k0:k0 + n], v[k0:k0 + n], [0, b - a], [0],
+                                             [n], scale)
+    return want, bound, written
+
+
+BROKEN = [  # queries and keys there are; q_begin, kv_begin, kv_len, max_q, max_kv
+    (7, 160, [0, 4, 7], [0, 100], [100, 1000], 4, 1000), (7, 160, [0, 4, 9999], [0, 100], [100, 60], 30, 100),
+    (7, 160, [-5, 4, 2], [-3, 10 ** 12], [100, 60], 30, 100), (7, 160, [0, 4, 7], [0, 100], [-1, -7], 4, 100),
+    (7, 160, [0, 4, 7], [0, 159], [100, 60], 2, 50), (300, 500, [0, 130, 9999], [0, 400], [400, 1000], 400, 1000),
+    (300, 500, [-70, 100, 290], [-3, 499], [100, 60], 250, 100), (300, 500, [10, 200, 250], [0, 10 ** 12], [500, 9], 90, 130),
+    (300, 4000, [0, 150, 9999], [0, 2000], [4000, 4000], 300, 4000), (300, 4000, [5, 150, 300], [100, 3990], [2500, 10 ** 9], 129, 2400),
+    (40, 3000, [0, 20, 9999], [500, 0], [9999, 3000], 25, 2900),
+]
+
+
+@pytest.mark.parametrize("case", range(len(BROKEN)))
+def test_attend_broken_tables_reach_nothing_else(case):
+    """Lengths and rows outside the tensors or the bounds count as documented; the rows of no
+    sequence, and what lies around the result, stay as they were."""
+    n_q, n_k, qb, kb, kl, max_q, max_kv = BROKEN[case]
+    say("attend broken", BROKEN[case])
+    g, dt, heads, d = gen(41), torch.float16, 2, 64
+    q, k, v = normal(g, n_q, heads, d, dtype=dt), normal(g, n_k, 1, d, dtype=dt), normal(g, n_k, 1, d, dtype=dt)
+    wide = torch.full((n_q + 64, heads, d + 16), 7.0, dtype=dt, device="cuda")
+    out = wide[32:-32, :, 8:8 + d]
+    run_attend(q, k, v, qb, kb, kl, 0.125, out=out, max_q=max_q, max_kv=max_kv)
+    want, bound, written = clamped(q, k, v, qb, kb, kl, max_q, max_kv, 0.125)
+    R.assert_within(out.cpu()[written], want[written], bound[written], "attend")
+    out[written.cuda()] = 7.0
+    assert bool((wide == 7.0).all())
+
+
+@pytest.mark.parametrize("kind", ["causal", "causal docs prefix", "slope pos"])
+@pytest.mark.parametrize("n_seqs,q_most,kv_most,heads,kv", [(150, 1, 1500, 4, 2), (250, 2, 2000, 2, 2),
+                                                           (300, 3, 90, 4, 1), (100, 80, 60, 2, 1),
+                                                           (70, 40, 200, 4, 2), (65, 1, 3000, 8, 1)])
+def test_attend_more_sequences_than_lanes(n_seqs, q_most, kv_most, heads, kv, kind):
+    """More than 64 sequences, up to and past those whose keys are cut."""
+    say("attend many sequences", n_seqs, q_most, kv_most, kind)
+    g = gen(n_seqs)
+    q_lens = [int(torch.randint(0, q_most + 1, (1,), generator=g)) for _ in range(n_seqs)]
+    kv_lens = [int(torch.randint(0, kv_most + 1, (1,), generator=g)) for _ in range(n_seqs)]
+    q_lens[3], kv_lens[5] = q_most, kv_most
+    g, q, k, v, qb, kb = make(n_seqs, q_lens, kv_lens, heads, kv, 32, "bf16", gap=2)
+    f = features(kind, g, q.shape[0], k.shape[0], heads, n_seqs, kv_lens)
+    want, bound = R.attend(q, k, v, qb, kb, kv_lens, 0.2, **f)
+    R.assert_within(run_attend(q, k, v, qb, kb, kv_lens, 0.2, **f), want, bound, "attend")
+
+
+@pytest.mark.parametrize("lens,heads,kv,d", [([20011, 2858, 4], 4, 2, 64), ([9000], 8, 1, 128),
+                                             ([1500 - 37 * i for i in range(40)], 4, 2, 40)])
+@pytest.mark.parametrize("q_len", [1, 4])
+def test_attend_long_caches_in_binary16(lens, heads, kv, d, q_len):
+    say("attend long f16", len(lens), q_len)
+    g, q, k, v, qb, kb = make(42, [q_len] * len(lens), lens, heads, kv, d, "f16")
+    f = features("cap causal slope", g, q.shape[0], k.shape[0], heads, len(lens), lens)
+    want, bound = R.attend(q, k, v, qb, kb, lens, d ** -0.5, **f)
+    R.assert_within(run_attend(q, k, v, qb, kb, lens, d ** -0.5, **f), want, bound, "attend")
+
+
+def test_operators_in_a_graph_are_right():
+    """Each call's results in every replay of a captured graph against the formulas, with other
+    work and synchronisations between the replays."""
+    say("graph and formulas")
+    g, dt, tokens, heads, kv, d, k = gen(43), torch.float16, 6, 4, 2, 64, 128
+    width, rows, keys = (heads + 2 * kv) * d, 6 * 700, 700
+    w = normal(g, width, k, dtype=dt, gain=k ** -0.5)
+    ad = (normal(g, 3, 8, k, dtype=dt, gain=k ** -0.5), normal(g, 3, width, 8, dtype=dt), torch.ones(3))
+    dad, dw = tg.Adapters(*(dev(t) for t in ad)), w.cuda()
+    x = torch.empty((tokens, k), dtype=dt, device="cuda")
+    ids = torch.arange(tokens, dtype=torch.int32) % 4
+    pb = tg.ProjectBuffers(tokens, k, width, dt, dad)
+    table, pos = make_table(g, 32, d // 2), torch.arange(tokens, dtype=torch.int32)[:, None].contiguous()
+    kc, vc = (normal(g, rows, kv, d, dtype=dt).cuda() for _ in range(2))
+    slot = torch.arange(tokens) * keys + keys - 1
+    seqs = tg.Sequences(torch.arange(tokens + 1, dtype=torch.int32, device="cuda"),
+                        torch.arange(tokens, dtype=torch.int64, device="cuda") * keys,
+                        torch.full((tokens,), keys, dtype=torch.int32, device="cuda"), 1, keys)
+    qkv = pb.y.view(tokens, heads + 2 * kv, d)
+    q_out, out = (torch.empty((tokens, heads, d), dtype=dt, device="cuda") for _ in range(2))
+    ab, dids, dtable, dpos, dslot = (tg.AttendBuffers(seqs, q_out, kc), ids.cuda(), table.cuda(),
+                                     pos.cuda(), slot.cuda())
+
+    def step():
+        tg.project(x, dw, pb, dad, dids)
+        tg.rotate(qkv[:, :heads], qkv[:, heads:heads + kv], None, None, dtable, dpos, q_out, kc,
+                  qkv[:, heads + kv:], vc, dslot)
+        tg.attend(q_out, kc, vc, seqs, out, ab, d ** -0.5, causal=True)
+
+    x.zero_()
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for _ in range(3):
+        hx = normal(g, tokens, k, dtype=dt)
+        x.copy_(hx)
+        for t in (pb.y, q_out, out, pb.workspace.view(torch.float32), ab.workspace.view(torch.float32)):
+            t.fill_(NAN)
+        graph.replay()
+        torch.cuda.synchronize()
+        want, bound = R.project(hx, w, *ad, ids)
+        R.assert_within(pb.y, want, bound, "project")
+        h = qkv.cpu()
+        want, bound = R.rotate(h[:, :heads], None, table, pos, 1e-6, False)
+        R.assert_within(q_out, want, bound, "queries")
+        want, bound = R.rotate(h[:, heads:heads + kv], None, table, pos, 1e-6, False)
+        R.assert_within(kc[dslot], want, bound, "keys")
+        assert torch.equal(vc[dslot].cpu(), h[:, heads + kv:])
+        want, bound = R.attend(q_out.cpu(), kc.cpu(), vc.cpu(), list(range(tokens + 1)),
+                               [i * keys for i in range(tokens)], [keys] * tokens, d ** -0.5, causal=True)
+        R.assert_within(out, want, bound, "attend")
 
 
 def test_broken_values_do_not_stall():
