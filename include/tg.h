@@ -708,16 +708,17 @@ size_t tg_attend_workspace_bytes(int32_t n_seqs, int32_t n_q_rows, int32_t max_q
  *   with slope z -= slope[h] * distance, |p - j|, or |xq - xk| + |yq - yk| of the positions;
  * it sees key j when j <= p or j < prefix[s] or not causal, and its document is the key's (and
  * >= 0). The output is the softmax-weighted sum of the visible v_j, 0 for a query that sees no
- * key; keys and values it does not see do not reach it, whatever they hold. Weights are
- * rounded to the type before the product with v (in binary16 as 2^7 times their share of the
- * largest or more, so that they count down to 2^-32 of it), and their sum, in binary32, is of the
- * rounded ones, so that the weights of a row make 1. Rows outside [0, n_q_rows) and [0, n_k_rows) are
- * not read or written, whatever q_begin, kv_begin and kv_len say. out must not overlap an
- * input. Enqueued on `stream`; allocates nothing. Returns TG_E_INVAL (null pointer, negative
- * count, d outside [8, TG_ATTEND_MAX_D] or not a multiple of 8, heads that n_kv_heads does not
- * divide, a bad type, scale or cap, one of a pair missing where there are keys, prefix without
- * causal, q, k, v or out not 16-byte aligned, a stride that is negative, not a multiple of 8 or,
- * of rows, over 2^22), TG_E_WORKSPACE, TG_E_HIP. n_seqs == 0 or n_q_rows == 0 enqueues nothing.
+ * key (with documents also where all scores are minus infinity); keys and values it does not
+ * see do not reach it, whatever they hold. Weights are rounded to the type before the product
+ * with v (in binary16 as 2^7 times their share of the largest or more, so that they count down
+ * to 2^-32 of it), and their sum, in binary32, is of the rounded ones, so that the weights of a
+ * row make 1. Rows outside [0, n_q_rows) and [0, n_k_rows) are not read or written, whatever
+ * q_begin, kv_begin and kv_len say. out must not overlap an input. Enqueued on `stream`;
+ * allocates nothing. Returns TG_E_INVAL (null pointer, negative count, d outside [8,
+ * TG_ATTEND_MAX_D] or not a multiple of 8, heads that n_kv_heads does not divide, a bad type,
+ * scale or cap, one of a pair missing where there are keys, prefix without causal, q, k, v or
+ * out not 16-byte aligned, a stride that is negative, not a multiple of 8 or, of rows, over
+ * 2^22), TG_E_WORKSPACE, TG_E_HIP. n_seqs == 0 or n_q_rows == 0 enqueues nothing.
  */
 int tg_attend(const tg_attend_args *args, void *stream);
 

@@ -21,8 +21,9 @@
 // A key that a query does not see has weight 0, and 0 times infinity or NaN would still reach
 // the query's sum. Such sums stay NaN, so each result is looked at once, at the end; a row that
 // is not finite is computed again by strict_row, which leaves unseen keys out one by one. So is a
-// row whose scores are so large (2^24 and more) that the maximum, which is rounded, lies so far
-// from the score that it comes from that the largest weight is lost (full_sum).
+// row that has no maximum though it sees keys, and one whose scores are so large (2^24 and more)
+// that the maximum, which is rounded, lies so far from the score that it comes from that the
+// largest weight is lost (full_sum).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -218,8 +219,11 @@ __device__ __forceinline__ float abs_diff(int a, int b) {  // of any two
   return static_cast<float>(a > b ? d : 0u - d);
 }
 
-// Whether a row's sum holds its largest weight, which is 1 at least if it was not rounded away.
-__device__ __forceinline__ bool full_sum(float m, float l) { return l >= 0.5f || m == -INFINITY; }
+// Whether a row's sum holds its largest weight, which is 1 at least if it was not rounded away;
+// without a maximum, whether the row sees no key (`limit`: that of key_limit) or may not (documents).
+__device__ __forceinline__ bool full_sum(const AttendParams &P, int limit, float m, float l) {
+  return l >= 0.5f || (m == -INFINITY && (limit <= 0 || P.k_doc));
+}
 
 // One query row of one head, by one wave, unseen keys left out one by one: a lane a key's score,
 // then 8 or 16 lanes a key's values. A NaN that is seen in the query or a key is all of the result,
@@ -240,12 +244,13 @@ __device__ __forceinline__ void strict_row(const AttendParams &P, const Seq &s, 
   const int wide = P.d <= 64 ? 8 : 16, c = lane % wide * 8, own = lane / wide;
   const E *v = static_cast<const E *>(P.v) + (head / P.group) * P.v_head + s.k0 * P.v_stride + c;
   float m = -INFINITY, l = 0.0f, sum[8] = {};
-  bool lost = false;
+  bool lost = false, any = false;
   for (int j0 = 0; j0 < limit && !lost; j0 += 64) {
     const int j = j0 + lane;
     const bool seen = j < limit && doc >= 0 && (!P.k_doc || P.k_doc[s.k0 + j] == doc);
     const uint64_t all = __ballot(seen);
     if (!all) continue;
+    any = true;
     float z = -INFINITY;
     if (seen) {
       const E *kr = k + j * P.k_stride;
@@ -278,6 +283,7 @@ __device__ __forceinline__ void strict_row(const AttendParams &P, const Seq &s, 
       for (int e = 0; e < 8; ++e) sum[e] += w * static_cast<float>(x[e]);
     }
   }
+  lost = lost || (any && m == -INFINITY);  // all scores minus infinity: no weights
   l = wave_sum(l);
   V8 out;
 #pragma unroll
@@ -720,7 +726,7 @@ __global__ __launch_bounds__(kThreads, kD == 64 ? 3 : 2) void attend_tile_kernel
     return;
   }
   const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-  bool fine = full_sum(m, l);
+  bool fine = full_sum(P, limit, m, l);
   E *o = static_cast<E *>(P.out) + row * P.out_stride + head * P.out_head;
 #pragma unroll
   for (int b = 0; b < kBlocks; ++b)
@@ -793,7 +799,7 @@ __global__ __launch_bounds__(kThreads) void join_tile_kernel(const AttendParams 
       } else {
         total += pl[u][k];  // 0, or NaN where NaN is all that was seen of the part
       }
-    bool fine = full_sum(top, total);
+    bool fine = full_sum(P, key_limit(P, s, i), top, total);
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
       sum[u][q] = total == 0.0f ? 0.0f : sum[u][q] / total;
@@ -1079,7 +1085,7 @@ __global__ __launch_bounds__(kFewWaves * 64) void attend_few_kernel(const Attend
   const int64_t flat = (int64_t(id) * P.n_kv_heads + kvh) * P.row_tiles * 16 + mine;
   float *part = P.part + flat * P.d;
   E *o = static_cast<E *>(P.out) + orow * P.out_stride + ohead * P.out_head;
-  bool fine = full_sum(top, total) || mine >= rows;
+  bool fine = mine >= rows || full_sum(P, key_limit(P, s, mine / P.group), top, total);
 #pragma unroll
   for (int b = 0; b < kD / 4 / kLanes; ++b) {
     const int c = (b * kLanes + c0) * 4;
@@ -1176,7 +1182,7 @@ __global__ __launch_bounds__(kThreads, 4) void join_kernel(const AttendParams P)
   if (group == 0 && c < P.d) {
 #pragma unroll
     for (int g = 1; g < kAtOnce; ++g) sum += s_sum[g][tid];
-    bool fine = full_sum(top, total);
+    bool fine = full_sum(P, key_limit(P, s, i), top, total);
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
       sum[q] = total == 0.0f ? 0.0f : sum[q] / total;

@@ -500,3 +500,17 @@ def test_broken_values_do_not_stall():
     well = took(call)
     x[:, 7] = NAN
     assert took(call) < 60 * well and bool(torch.isnan(pb.y).all())
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("q_len,n", [(1, 1), (1, 3000), (5, 90), (90, 1), (90, 150), (140, 3000)])
+def test_attend_scores_of_minus_infinity(q_len, n, dtype):
+    """A query whose every score is minus infinity has no weights: NaN, and not 0 as for no key."""
+    say("attend minus infinity", q_len, n, dtype)
+    _, q, k, v, qb, kb = make(47, [q_len], [n], 4, 2, 64, dtype)
+    k[..., 0] = k[..., 0].abs() + 0.5
+    f = dict(causal=True)
+    want, bound = R.attend(q, k, v, qb, kb, [n], 0.125, **f)
+    sick = torch.arange(q_len) == q_len - 1 if n < q_len else torch.arange(q_len) % 3 == 0
+    q[sick, :, 0] = -math.inf
+    finite_rest(run_attend(q, k, v, qb, kb, [n], 0.125, **f), want, bound, sick)
