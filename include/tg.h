@@ -559,8 +559,8 @@ int tg_mask_rois(const tg_mask_rois_args *args, void *stream);
  * result is rounded once to nearest-even. Results that are not finite, or that infinities or NaN
  * which do not belong to them have touched, are formed again one by one: where they are most of a
  * call it takes some ten, and up to about 150, times as long. Strides are in elements, the last
- * dimension is contiguous. A call that one launch cannot hold (2^31 workgroups or so, of tg_project 2^32 threads)
- * returns TG_E_INVAL.
+ * dimension is contiguous. A call that one launch cannot hold (2^31 workgroups or so, of
+ * tg_project 2^32 threads) returns TG_E_INVAL.
  */
 enum tg_type {
   TG_F16 = 0, /* binary16 */

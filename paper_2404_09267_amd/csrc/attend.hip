@@ -220,15 +220,16 @@ __device__ __forceinline__ float abs_diff(int a, int b) {  // of any two
 }
 
 // Whether a row's sum holds its largest weight, which is 1 at least if it was not rounded away;
-// without a maximum, whether the row sees no key (`limit`: that of key_limit) or may not (documents).
+// without a maximum, whether the row sees no key (`limit`: that of key_limit) or may not see one
+// (documents).
 __device__ __forceinline__ bool full_sum(const AttendParams &P, int limit, float m, float l) {
   return l >= 0.5f || (m == -INFINITY && (limit <= 0 || P.k_doc));
 }
 
 // One query row of one head, by one wave, unseen keys left out one by one: a lane a key's score,
 // then 8 or 16 lanes a key's values. A NaN that is seen in the query or a key is all of the result,
-// so that the rest is not looked at. bfloat16, the 7 prompts of up to 2,077 with a cap below, all of
-// whose rows come here: 17 ms for 0.15 with a NaN in every value, 1.3 in every query.
+// so that the rest is not looked at. bfloat16, the 7 prompts of up to 2,077 with a cap below, all
+// of whose rows come here: 17 ms for 0.15 with a NaN in every value, 1.3 in every query.
 template <int kType>
 __device__ __forceinline__ void strict_row(const AttendParams &P, const Seq &s, int i,
                                            int head) {
@@ -371,14 +372,15 @@ enum Mode {
 // A wave takes 32 queries and a workgroup's 4 waves share tiles of 64 keys and values, two of them
 // in LDS by turns, so that a tile's loads run while the one before it is worked on: 69 KB with
 // heads of 128 and 2 workgroups a CU, 3 with heads of 64. The weights never leave the registers.
-// Matrix and vector instructions share the issue slots, and a tile has about as many cycles of
-// one as of the other: that, and not memory, bounds it, so the vector work a score costs is what
-// the modes are for. bfloat16, one sequence of 16,384 tokens, 16 heads of 128 over 4, causal, a
-// bias: 1.16 ms, 950 TFLOP/s of the products that are seen, matrix units 46 % of the time at
-// work, vector units 54 %; 7 of up to 2,077 with a cap and prefixes 0.15 ms, 620 (33 %, 59 %).
+// A tile has about as many cycles of matrix as of vector instructions, and they hardly overlap:
+// that, and not memory, bounds it, so the vector work a score costs is what the modes are for.
+// bfloat16, one sequence of 16,384 tokens, 16 heads of 128 over 4, causal, a bias: 1.12 to 1.21 ms
+// by card, 910 to 980 TFLOP/s of the products that are seen, matrix units 48 % of the time at
+// work, vector units 57 %; 7 of up to 2,077 with a cap and prefixes 0.15 ms, 620 (33 %, 58 %).
 // binary16, 4 canvases of up to 6,400 tokens, 16 heads of 64, 32 documents each and a bias by
-// position: 0.11 ms (11 %, 60 %; 0.26 with the tokens in raster order, where few keys of a tile
-// are of a query's document).
+// position: 0.11 ms (12 %, 59 %, and waves that wait 47 % of their time, as a workgroup has about 7
+// tiles and looks through all documents first; 0.26 with the tokens in raster order, where few
+// keys of a tile are of a query's document).
 // 64 queries a wave (half the LDS reads) spilled registers and took three times as long; one
 // tile's products between the other's exponentials, by half tiles, 1.30 ms for 1.20.
 template <int kType, int kD, int kMode>

@@ -16,9 +16,10 @@
 //  1. tiles of x and w with k cut over workgroups, so that every CU has a share of w to read,
 //     and beside them one workgroup a token for its row of h;
 //  2. finish: the cuts are added up, and each token's adapter to them.
-// 0 times an infinite b_g, or a row of h past binary16's range, would leave NaN at tokens it does
-// not belong to, or in the place of a number. Sums that are not finite at the end of a tile with
-// adapters are therefore formed again one by one, from binary32 h and the token's own adapter.
+// 0 times an infinite b_g, or a row of h past what its power of two can bring back, would leave NaN
+// at tokens it does not belong to, or in the place of a number. Sums that are not finite at the
+// end of a tile with adapters are therefore formed again one by one, from binary32 h and the
+// token's own adapter.
 // Results lie transposed in the registers (a lane holds 4 outputs of one token), so that stores
 // are contiguous and a token's adapter belongs to the lane.
 // The product is bound by how fast tiles reach LDS (about 20 bytes a cycle and CU in every shape,

@@ -175,7 +175,7 @@ __global__ __launch_bounds__(kThreads) void rotate_kernel(const RotateParams P) 
         u[i] *= inv * static_cast<float>(wa[i]);
         u[8 + i] *= inv * static_cast<float>(wb[i]);
       }
-      // a pair that does not turn stays as it is: 0 times its partner would not, if that is infinite
+      // a pair that does not turn stays as it is: 0 times an infinite partner would be NaN
       if (turns) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {

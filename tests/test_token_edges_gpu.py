@@ -97,7 +97,8 @@ def test_rotate_more_heads_than_a_row_of_workgroups():
     none = q[:, :0]
     tg.rotate(q, none, None, None, table, pos, out, none)
     torch.cuda.synchronize()
-    for t in (slice(0, 10000), slice(tokens // 2, tokens // 2 + 10000), slice(tokens - 10000, None)):
+    for first in (0, tokens // 2, tokens - 10000):
+        t = slice(first, first + 10000)
         want, bound = R.rotate(q[t].cpu(), None, table.cpu(), pos[t].cpu(), 1e-6, False)
         R.assert_within(out[t].cpu(), want, bound, "rotate")
     assert bool(torch.isfinite(out).all())
@@ -114,7 +115,8 @@ def test_rotate_values_whose_squares_overflow(tokens, heads, d, rot):
     q[2] *= 2.0 ** 50
     k[::2] *= 2.0 ** 120
     k[1, 0, :5] = 2.0 ** 100  # and next to ordinary ones
-    w, pos = normal(g, d, dtype=dt), torch.randint(0, 9, (tokens, 1), generator=g, dtype=torch.int32)
+    w = normal(g, d, dtype=dt)
+    pos = torch.randint(0, 9, (tokens, 1), generator=g, dtype=torch.int32)
     table = make_table(g, 9, rot // 2)
     out, k_out = (torch.full(t.shape, NAN, dtype=dt, device="cuda") for t in (q, k))
     tg.rotate(q.cuda(), k.cuda(), w.cuda(), None, table.cuda(), pos.cuda(), out, k_out)
@@ -211,7 +213,7 @@ def test_attend_seen_nan(n_q, n, heads, kv, d, dtype, causal):
 
 @pytest.mark.parametrize("q_len", [3, 100])
 def test_attend_documents_of_every_sign(q_len):
-    """Documents below 0 see nothing, the lowest number among them; the highest is one like others."""
+    """Documents below 0 see nothing, the lowest number among them; the highest sees its own."""
     say("attend documents", q_len)
     g, q, k, v, qb, kb = make(35, [q_len], [170], 4, 2, 64, "bf16")
     names = torch.tensor([-(1 << 31), -1, 0, (1 << 31) - 1, -(1 << 31) + 1], dtype=torch.int32)
@@ -289,11 +291,13 @@ def test_attend_scores_of_any_size(q_len, n, dtype):
         got = run_attend(q, k * 0, v, qb, kb, [n], 0.125, **f).cpu()
         bound = 4 * R.UNIT[q.dtype] * v[top].double().abs().amax(0)
         for h in range(4):
-            R.assert_within(got[:, h], both[h // 2].double().expand(q_len, -1), bound[h // 2], "attend")
+            R.assert_within(got[:, h], both[h // 2].double().expand(q_len, -1), bound[h // 2],
+                            "attend")
 
 
 @pytest.mark.parametrize("cap", [1e-40, 1e-30, 1e-6, 3e38])
-@pytest.mark.parametrize("q_len,more", [(1, {}), (90, {}), (90, {"slope": True}), (1, {"slope": True})])
+@pytest.mark.parametrize("q_len,more", [(1, {}), (90, {}), (90, {"slope": True}),
+                                        (1, {"slope": True})])
 def test_attend_caps_of_every_size(q_len, more, cap):
     """Caps whose quotient with the scale leaves binary32, scores of 0 among them."""
     say("attend caps", q_len, cap)
@@ -330,7 +334,8 @@ def test_one_row_or_head_of_any_stride():
     q, k, v = (normal(g, n, 1, d, dtype=dt).cuda() for n in (1, rows, rows))
     want, bound = R.attend(q.cpu(), k.cpu(), v.cpu(), [0, 1], [0], [rows], 0.125)
     out = odd(torch.empty_like(q), (1 << 40, 3, 1))
-    run_attend(odd(q, (12345, 1 << 33, 1)), odd(k, (d, 7, 1)), v, [0, 1], [0], [rows], 0.125, out=out)
+    run_attend(odd(q, (12345, 1 << 33, 1)), odd(k, (d, 7, 1)), v, [0, 1], [0], [rows], 0.125,
+               out=out)
     R.assert_within(out, want, bound, "attend")
     one = odd(k[:1], (1 << 30, 1, 1))
     run_attend(q, one, one, [0, 1], [0], [1], 0.125, out=out)
@@ -358,11 +363,16 @@ def clamped(q, k, v, qb, kb, kl, max_q, max_kv, scale):
 
 
 BROKEN = [  # queries and keys there are; q_begin, kv_begin, kv_len, max_q, max_kv
-    (7, 160, [0, 4, 7], [0, 100], [100, 1000], 4, 1000), (7, 160, [0, 4, 9999], [0, 100], [100, 60], 30, 100),
-    (7, 160, [-5, 4, 2], [-3, 10 ** 12], [100, 60], 30, 100), (7, 160, [0, 4, 7], [0, 100], [-1, -7], 4, 100),
-    (7, 160, [0, 4, 7], [0, 159], [100, 60], 2, 50), (300, 500, [0, 130, 9999], [0, 400], [400, 1000], 400, 1000),
-    (300, 500, [-70, 100, 290], [-3, 499], [100, 60], 250, 100), (300, 500, [10, 200, 250], [0, 10 ** 12], [500, 9], 90, 130),
-    (300, 4000, [0, 150, 9999], [0, 2000], [4000, 4000], 300, 4000), (300, 4000, [5, 150, 300], [100, 3990], [2500, 10 ** 9], 129, 2400),
+    (7, 160, [0, 4, 7], [0, 100], [100, 1000], 4, 1000),
+    (7, 160, [0, 4, 9999], [0, 100], [100, 60], 30, 100),
+    (7, 160, [-5, 4, 2], [-3, 10 ** 12], [100, 60], 30, 100),
+    (7, 160, [0, 4, 7], [0, 100], [-1, -7], 4, 100),
+    (7, 160, [0, 4, 7], [0, 159], [100, 60], 2, 50),
+    (300, 500, [0, 130, 9999], [0, 400], [400, 1000], 400, 1000),
+    (300, 500, [-70, 100, 290], [-3, 499], [100, 60], 250, 100),
+    (300, 500, [10, 200, 250], [0, 10 ** 12], [500, 9], 90, 130),
+    (300, 4000, [0, 150, 9999], [0, 2000], [4000, 4000], 300, 4000),
+    (300, 4000, [5, 150, 300], [100, 3990], [2500, 10 ** 9], 129, 2400),
     (40, 3000, [0, 20, 9999], [500, 0], [9999, 3000], 25, 2900),
 ]
 
@@ -374,7 +384,7 @@ def test_attend_broken_tables_reach_nothing_else(case):
     n_q, n_k, qb, kb, kl, max_q, max_kv = BROKEN[case]
     say("attend broken", BROKEN[case])
     g, dt, heads, d = gen(41), torch.float16, 2, 64
-    q, k, v = normal(g, n_q, heads, d, dtype=dt), normal(g, n_k, 1, d, dtype=dt), normal(g, n_k, 1, d, dtype=dt)
+    q, k, v = (normal(g, n, h, d, dtype=dt) for n, h in ((n_q, heads), (n_k, 1), (n_k, 1)))
     wide = torch.full((n_q + 64, heads, d + 16), 7.0, dtype=dt, device="cuda")
     out = wide[32:-32, :, 8:8 + d]
     run_attend(q, k, v, qb, kb, kl, 0.125, out=out, max_q=max_q, max_kv=max_kv)
@@ -385,9 +395,9 @@ def test_attend_broken_tables_reach_nothing_else(case):
 
 
 @pytest.mark.parametrize("kind", ["causal", "causal docs prefix", "slope pos"])
-@pytest.mark.parametrize("n_seqs,q_most,kv_most,heads,kv", [(150, 1, 1500, 4, 2), (250, 2, 2000, 2, 2),
-                                                           (300, 3, 90, 4, 1), (100, 80, 60, 2, 1),
-                                                           (70, 40, 200, 4, 2), (65, 1, 3000, 8, 1)])
+@pytest.mark.parametrize("n_seqs,q_most,kv_most,heads,kv", [
+    (150, 1, 1500, 4, 2), (250, 2, 2000, 2, 2), (300, 3, 90, 4, 1), (100, 80, 60, 2, 1),
+    (70, 40, 200, 4, 2), (65, 1, 3000, 8, 1)])
 def test_attend_more_sequences_than_lanes(n_seqs, q_most, kv_most, heads, kv, kind):
     """More than 64 sequences, up to and past those whose keys are cut."""
     say("attend many sequences", n_seqs, q_most, kv_most, kind)
@@ -419,12 +429,14 @@ def test_operators_in_a_graph_are_right():
     g, dt, tokens, heads, kv, d, k = gen(43), torch.float16, 6, 4, 2, 64, 128
     width, rows, keys = (heads + 2 * kv) * d, 6 * 700, 700
     w = normal(g, width, k, dtype=dt, gain=k ** -0.5)
-    ad = (normal(g, 3, 8, k, dtype=dt, gain=k ** -0.5), normal(g, 3, width, 8, dtype=dt), torch.ones(3))
+    ad = (normal(g, 3, 8, k, dtype=dt, gain=k ** -0.5), normal(g, 3, width, 8, dtype=dt),
+          torch.ones(3))
     dad, dw = tg.Adapters(*(dev(t) for t in ad)), w.cuda()
     x = torch.empty((tokens, k), dtype=dt, device="cuda")
     ids = torch.arange(tokens, dtype=torch.int32) % 4
     pb = tg.ProjectBuffers(tokens, k, width, dt, dad)
-    table, pos = make_table(g, 32, d // 2), torch.arange(tokens, dtype=torch.int32)[:, None].contiguous()
+    table = make_table(g, 32, d // 2)
+    pos = torch.arange(tokens, dtype=torch.int32)[:, None].contiguous()
     kc, vc = (normal(g, rows, kv, d, dtype=dt).cuda() for _ in range(2))
     slot = torch.arange(tokens) * keys + keys - 1
     seqs = tg.Sequences(torch.arange(tokens + 1, dtype=torch.int32, device="cuda"),
@@ -450,7 +462,8 @@ def test_operators_in_a_graph_are_right():
     for _ in range(3):
         hx = normal(g, tokens, k, dtype=dt)
         x.copy_(hx)
-        for t in (pb.y, q_out, out, pb.workspace.view(torch.float32), ab.workspace.view(torch.float32)):
+        scratch = (b.workspace.view(torch.float32) for b in (pb, ab))
+        for t in (pb.y, q_out, out, *scratch):
             t.fill_(NAN)
         graph.replay()
         torch.cuda.synchronize()
@@ -463,7 +476,8 @@ def test_operators_in_a_graph_are_right():
         R.assert_within(kc[dslot], want, bound, "keys")
         assert torch.equal(vc[dslot].cpu(), h[:, heads + kv:])
         want, bound = R.attend(q_out.cpu(), kc.cpu(), vc.cpu(), list(range(tokens + 1)),
-                               [i * keys for i in range(tokens)], [keys] * tokens, d ** -0.5, causal=True)
+                               [i * keys for i in range(tokens)], [keys] * tokens, d ** -0.5,
+                               causal=True)
         R.assert_within(out, want, bound, "attend")
 
 
@@ -493,9 +507,10 @@ def test_broken_values_do_not_stall():
     q[:, :, 7] = NAN
     assert took(call) < 60 * well and bool(torch.isnan(out).all())
     x, w = normal(g, n, 1024, dtype=dt).cuda(), normal(g, 1024, 1024, dtype=dt).cuda()
-    low = tg.Adapters(normal(g, 2, 16, 1024, dtype=dt).cuda(), normal(g, 2, 1024, 16, dtype=dt).cuda(),
-                      torch.ones(2, device="cuda"))
-    ids, pb = (torch.arange(n, device="cuda") // 100 % 2).int(), tg.ProjectBuffers(n, 1024, 1024, dt, low)
+    low = tg.Adapters(normal(g, 2, 16, 1024, dtype=dt).cuda(),
+                      normal(g, 2, 1024, 16, dtype=dt).cuda(), torch.ones(2, device="cuda"))
+    ids = (torch.arange(n, device="cuda") // 100 % 2).int()
+    pb = tg.ProjectBuffers(n, 1024, 1024, dt, low)
     call = lambda: tg.project(x, w, pb, low, ids)
     well = took(call)
     x[:, 7] = NAN

@@ -44,7 +44,8 @@ def test_attend_workspace_of_the_largest_batch_does_for_smaller_ones():
     rng = np.random.default_rng(0)
     for _ in range(20000):
         kv = int(rng.choice([1, 2, 3, 4, 8, 16, 71, 1600]))
-        heads = (kv * int(rng.choice([1, 2, 4, 7, 8, 16, 71])), kv, int(rng.choice([8, 64, 72, 128])))
+        group, d = int(rng.choice([1, 2, 4, 7, 8, 16, 71])), int(rng.choice([8, 64, 72, 128]))
+        heads = (kv * group, kv, d)
         most = [int(2 ** rng.uniform(0, top)) for top in (10, 16, 13, 18)]
         assert need(less(rng, most), heads) <= need(most, heads), (most, heads)
 
@@ -56,7 +57,8 @@ def test_project_workspace_of_the_most_tokens_does_for_fewer():
     assert need(300, 64, 28001, 30, 17) <= need(300, 64, 28001, 40, 17)
     rng = np.random.default_rng(0)
     for _ in range(20000):
-        k, n, rank = 8 * int(2 ** rng.uniform(0, 10)), int(2 ** rng.uniform(0, 17)), int(rng.integers(1, 65))
+        k, n = 8 * int(2 ** rng.uniform(0, 10)), int(2 ** rng.uniform(0, 17))
+        rank = int(rng.integers(1, 65))
         tokens, adapters = int(2 ** rng.uniform(0, 16)), int(2 ** rng.uniform(0, 7))
         t, g = less(rng, (tokens, adapters))
         assert need(t, k, n, g, rank) <= need(tokens, k, n, adapters, rank)
