@@ -86,7 +86,7 @@ __global__ __launch_bounds__(kThreads) void rotate_kernel(const RotateParams P) 
   typedef Num<kType> N;
   typedef typename N::E E;
   typedef typename N::V8 V8;
-  const int64_t unit = workgroup() * (kThreads / 64) + (threadIdx.x >> 6);
+  const int64_t unit = int64_t(workgroup()) * (kThreads / 64) + (threadIdx.x >> 6);
   const int lane = threadIdx.x & 63, sub = lane & (P.lanes - 1);
   const int slot = lane / P.lanes, step = P.at_once;
   // a wave has several tokens where one has fewer heads than the wave has room for
@@ -209,7 +209,7 @@ template <int kType>
 __global__ __launch_bounds__(kThreads) void rotate_any_kernel(const RotateParams P,
                                                               int interleaved) {
   typedef typename Num<kType>::E E;
-  const int64_t unit = workgroup() * (kThreads / 64) + (threadIdx.x >> 6);
+  const int64_t unit = int64_t(workgroup()) * (kThreads / 64) + (threadIdx.x >> 6);
   const int64_t t = unit / P.rows;
   if (t >= P.n_tokens) return;
   int h = static_cast<int>(unit - t * P.rows);

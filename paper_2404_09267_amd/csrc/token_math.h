@@ -116,17 +116,18 @@ __device__ __forceinline__ float wave_sum(float v) {
   return v;
 }
 
-// `blocks` workgroups: in one row, or in several where their threads would pass the 2^32 that a
-// launch takes in one direction. A kernel's own place is workgroup(); the last row may have some
-// more than asked for, and even those are numbered in 31 bits.
-constexpr int64_t kMaxWorkgroups = INT32_MAX - 256;
+// `blocks` workgroups: in one row, or in several of kRow where their threads would pass the 2^32
+// that a launch takes in one direction. A kernel's own place is workgroup(), which asks for no
+// size of the grid (its load adds 0.1 us to a call); the last row may have more than asked for, and
+// even those are numbered in 31 bits.
+constexpr int kRow = 1 << 20;
+constexpr int64_t kMaxWorkgroups = INT32_MAX - kRow;
 inline dim3 grid_of(int64_t blocks, int threads) {
-  const int64_t most = ((int64_t(1) << 32) - 1) / threads;
-  const int64_t rows = (blocks + most - 1) / most;
-  return dim3(static_cast<uint32_t>((blocks + rows - 1) / rows), static_cast<uint32_t>(rows));
+  if (blocks * threads < int64_t(1) << 32) return dim3(static_cast<uint32_t>(blocks));
+  return dim3(kRow, static_cast<uint32_t>((blocks + kRow - 1) / kRow));
 }
-__device__ __forceinline__ int64_t workgroup() {
-  return int64_t(blockIdx.y) * gridDim.x + blockIdx.x;
+__device__ __forceinline__ int workgroup() {
+  return static_cast<int>(blockIdx.y * kRow + blockIdx.x);
 }
 
 inline bool aligned16(const void *p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
