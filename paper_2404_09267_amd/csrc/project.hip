@@ -626,8 +626,8 @@ __global__ __launch_bounds__(kWt *kWn * 64, 2) void project_kernel(const Project
   int id = -1;
   float up = 1.0f;
   if (steps_low && threadIdx.x < kT) {
-    id = adapter_of(P, t0 + threadIdx.x);
     if (kType == TG_F16 && t0 + threadIdx.x < P.n_tokens) up = P.h_up[t0 + threadIdx.x];
+    id = adapter_of(P, t0 + threadIdx.x);
   }
   const int begun = steps_low ? min(main_steps, kStages) : kStages;
   for (int s = 0; s < begun; ++s) fetch(s);
@@ -650,12 +650,17 @@ __global__ __launch_bounds__(kWt *kWn * 64, 2) void project_kernel(const Project
   for (; s + kStages < main_steps; ++s) step(s, a, b, false);
   // a token's sums times the power of two of its row of h, and back (the exponent negated)
   auto scale = [&](bool back) {
+    uint32_t up[kFt];
+    bool any = false;
 #pragma unroll
     for (int i = 0; i < kFt; ++i) {
-      const float up = s_up[wt + 16 * i + col];
-      if (!__ballot(up != 1.0f)) continue;
-      const uint32_t f = __builtin_bit_cast(uint32_t, up);
-      const float by = __builtin_bit_cast(float, back ? 0x7F000000u - f : f);
+      up[i] = __builtin_bit_cast(uint32_t, s_up[wt + 16 * i + col]);
+      any = any || up[i] != 0x3F800000u;
+    }
+    if (!__ballot(any)) return;
+#pragma unroll
+    for (int i = 0; i < kFt; ++i) {
+      const float by = __builtin_bit_cast(float, back ? 0x7F000000u - up[i] : up[i]);
 #pragma unroll
       for (int j = 0; j < kFn; ++j) acc[j][i] *= by;
     }
