@@ -380,8 +380,8 @@ enum Mode {
 // heads of 128 and 2 workgroups a CU, 3 with heads of 64. The weights never leave the registers.
 // A tile has about as many cycles of matrix as of vector instructions, and they hardly overlap:
 // that, and not memory, bounds it, so the vector work a score costs is what the modes are for.
-// bfloat16, one sequence of 16,384 tokens, 16 heads of 128 over 4, causal, a bias: 1.12 to 1.21 ms
-// by card, 910 to 980 TFLOP/s of the products that are seen, matrix units 48 % of the time at
+// bfloat16, one sequence of 16,384 tokens, 16 heads of 128 over 4, causal, a bias: 1.12 to 1.22 ms
+// by card, 900 to 980 TFLOP/s of the products that are seen, matrix units 48 % of the time at
 // work, vector units 57 %; 7 of up to 2,077 with a cap and prefixes 0.15 ms, 620 (33 %, 58 %).
 // binary16, 4 canvases of up to 6,400 tokens, 16 heads of 64, 32 documents each and a bias by
 // position: 0.11 ms (12 %, 59 %, and waves that wait 47 % of their time, as a workgroup has about 7
