@@ -722,6 +722,217 @@ size_t tg_attend_workspace_bytes(int32_t n_seqs, int32_t n_q_rows, int32_t max_q
  */
 int tg_attend(const tg_attend_args *args, void *stream);
 
+/* ---- Serving operators: a step of many requests over one paged cache ---- */
+
+/*
+ * Requests that come and go share one cache of keys and values, whose rows are dealt out in
+ * pages of page_size rows: key j of sequence s is cache row
+ *   table[s][j / page_size] * page_size + j % page_size.
+ * A step is tg_pages, which gives every new token a row (the `slot` that tg_rotate writes to),
+ * then per layer tg_norm, tg_quantize, tg_project_i8, tg_rotate and tg_attend_pages. All of it
+ * runs on the device from lengths that stay there, so that a step can be captured once and
+ * replayed. Values, sums and strides are as with the token operators above; only forward results.
+ */
+
+/* Most sequences of tg_pages and tg_attend_pages. */
+#define TG_PAGES_MAX_SEQS (1 << 20)
+
+typedef struct {
+  const int32_t *q_begin;  /* device [n_seqs + 1]: sequence s brings tokens [q_begin[s],
+                              q_begin[s + 1]), none to many, in order */
+  const int32_t *kv_len;   /* device [n_seqs]: rows that each sequence holds before the call */
+  int32_t *kv_len_out;     /* device out [n_seqs]: and after it; may be kv_len */
+  const int32_t *release;  /* device [n_seqs] or NULL: nonzero: the sequence has ended, its pages go
+                              back before any are taken, and it starts anew with no rows */
+  int32_t *table;          /* device in/out: pages of sequence s are table[s * table_stride + i],
+                              i < max_pages; entries that get no page are left as they are */
+  int64_t table_stride;    /* >= max_pages */
+  int32_t *free_pages;     /* device in/out [n_pages]: a stack, the pages that nobody holds are
+                              its first *n_free entries; what lies above is not kept */
+  const int32_t *n_free;   /* device [1] */
+  int32_t *n_free_out;     /* device out [1]; may be n_free */
+  int64_t *slot;           /* device out [n_tokens]: the cache row of each token, -1: none */
+  int32_t *pos;            /* device out [n_tokens] or NULL: its place in its sequence, 0 where it
+                              has no row */
+  int32_t *refused;        /* device out [1]: sequences whose tokens got no rows */
+  int32_t n_seqs, n_tokens, n_pages;
+  int32_t page_size;       /* >= 1; n_pages * page_size < 2^31 */
+  int32_t max_pages;       /* pages that a sequence may hold, >= 1 */
+  void *workspace;         /* device scratch, 16-byte aligned, >= tg_pages_workspace_bytes(...) */
+  size_t workspace_bytes;
+} tg_pages_args;
+
+/* Device scratch tg_pages needs (0 when it needs none, or for bad arguments); it does not shrink as
+ * the sizes grow. */
+size_t tg_pages_workspace_bytes(int32_t n_seqs, int32_t n_tokens);
+
+/*
+ * Page tables and cache rows of a step, from lengths. In this order: every sequence with `release`
+ * pushes its pages on the stack (sequences in order, their pages in order) and holds no rows; a
+ * sequence whose new tokens end inside its pages takes none; the others ask for pages, and as long
+ * as the sum of what has been asked for, up to and with the sequence, does not pass the stack, it
+ * gets them, from the top. A sequence that does not, or would pass max_pages or 2^31 - 1 rows, is
+ * refused: its tokens get no rows, and it keeps what it holds. Tokens before q_begin[0] and
+ * from q_begin[n_seqs] on belong to nobody and get no rows, so that a batch can be padded.
+ * Nothing but the order of sequences decides, so two runs give the same. With kv_len_out and
+ * n_free_out apart from the inputs, and no sequence that is both released and given tokens, the
+ * call can be repeated. Lengths outside [0, max_pages * page_size] count as the nearest inside,
+ * n_free outside [0, n_pages] alike; q_begin outside [0, n_tokens] alike, and a sequence that ends
+ * before it begins has no tokens. A table entry outside [0, n_pages) gives its tokens no row. A
+ * page belongs to one sequence: nothing counts who shares it.
+ * Enqueued on `stream`; the library allocates nothing. Returns TG_E_INVAL (null pointer, negative
+ * count, n_seqs > TG_PAGES_MAX_SEQS, page_size or max_pages < 1, n_pages * page_size >= 2^31, a
+ * stride below max_pages), TG_E_WORKSPACE, TG_E_HIP. n_seqs == 0 and n_tokens == 0 enqueues
+ * nothing, n_seqs == 0 alone gives slot, pos, n_free_out and refused.
+ */
+int tg_pages(const tg_pages_args *args, void *stream);
+
+typedef struct {
+  /* Value c of head h of sequence s's query is q[s * q_stride + h * q_head_stride + c], c < d;
+   * k and v alike by cache row, with n_kv_heads heads: query head h reads key head
+   * h / (n_heads / n_kv_heads). */
+  const void *q, *k, *v;
+  int64_t q_stride, q_head_stride, k_stride, k_head_stride, v_stride, v_head_stride;
+  void *out;                 /* device out, rows and heads of q */
+  int64_t out_stride, out_head_stride;
+  const int32_t *table;      /* device: as tg_pages leaves it */
+  int64_t table_stride;      /* >= max_pages */
+  const int32_t *kv_len;     /* device [n_seqs]: keys of each sequence; its query stands at the
+                                last */
+  const float *slope;        /* device [n_heads] or NULL: bias per unit of distance, of any sign */
+  float scale;               /* finite */
+  float cap;                 /* > 0: scores are capped; 0: not */
+  int32_t window;            /* > 0: a query sees that many of the last keys; 0: all */
+  int32_t n_seqs, n_pages, page_size, max_pages;
+  int32_t max_kv_len;        /* bound on kv_len; keys from there on are left out */
+  int32_t n_heads, n_kv_heads, d;
+  int32_t type;              /* enum tg_type of q, k, v and out */
+  void *workspace;           /* device scratch, 16-byte aligned, >=
+                                tg_attend_pages_workspace_bytes(...) */
+  size_t workspace_bytes;
+} tg_attend_pages_args;
+
+/* Device scratch tg_attend_pages needs (0 when it needs none, or for bad arguments). With the same
+ * heads and d it does not shrink as the other sizes grow. */
+size_t tg_attend_pages_workspace_bytes(int32_t n_seqs, int32_t max_kv_len, int32_t n_heads,
+                                       int32_t n_kv_heads, int32_t d);
+
+/*
+ * Attention of one new token a sequence over its pages. With n = kv_len[s], the score with key j is
+ *   z = scale * (q . k_j);  with cap z = cap * tanh(z / cap);
+ *   with slope z -= slope[h] * (n - 1 - j);
+ * and the query sees keys j < min(n, max_kv_len, max_pages * page_size) with window == 0 or
+ * j >= n - window, but none on a page outside [0, n_pages). The output is the softmax-weighted sum
+ * of the v_j it sees, 0 if it sees none (kv_len <= 0 among them; such rows are written), NaN if all
+ * its scores are minus infinity. Rows that it does not see are not read. Weights are rounded to
+ * the type before the product with v, in binary16 as 2^7 times their share of the largest or more;
+ * their sum is of the rounded ones. An infinite value whose weight rounds to 0 makes NaN. Distances
+ * up to 2^24 are exact.
+ * out must not overlap an input. Enqueued on `stream`; allocates nothing. Returns TG_E_INVAL (null
+ * pointer, negative count, n_seqs > TG_PAGES_MAX_SEQS, max_kv_len > 2^30, d outside [8,
+ * TG_ATTEND_MAX_D] or not a multiple of 8, heads that n_kv_heads does not divide, a negative
+ * window, page_size or max_pages < 1, n_pages * page_size >= 2^31, a bad type, scale or cap, a table_stride below max_pages, q, k, v or out not
+ * 16-byte aligned, another stride that is negative, not a multiple of 8 or, of rows, over 2^22),
+ * TG_E_WORKSPACE, TG_E_HIP. n_seqs == 0 enqueues nothing.
+ */
+int tg_attend_pages(const tg_attend_pages_args *args, void *stream);
+
+enum tg_norm_kind {
+  TG_NORM_NONE = 0,
+  TG_NORM_RMS = 1,  /* u / sqrt(mean(u^2) + eps) */
+  TG_NORM_LAYER = 2 /* the same of u - mean(u) */
+};
+
+/* Longest row of tg_norm. */
+#define TG_NORM_MAX_N 32768
+
+typedef struct {
+  const void *x;           /* device: token t's row is x + t * x_stride, n values */
+  int64_t x_stride;        /* all strides >= n */
+  const void *y;           /* device or NULL: what a block has made of it */
+  int64_t y_stride;
+  int32_t y_norm;          /* enum tg_norm_kind of y */
+  const void *y_weight, *y_bias; /* device [n] or NULL (ones, zeros) */
+  const void *gate;        /* device or NULL (ones): gate g's row is gate + g * gate_stride */
+  int64_t gate_stride;
+  const int32_t *gate_row; /* device [n_tokens] or NULL: each token's gate; outside [0, n_gates) y
+                              is not added. NULL: gate 0 for all */
+  float x_scale, y_scale;  /* finite */
+  void *x_out;             /* device out or NULL: the new residual; may be x or y (same pointer and
+                              stride) */
+  int64_t x_out_stride;
+  void *h;                 /* device out or NULL: its norm; may be x or y where x_out is not */
+  int64_t h_stride;
+  int32_t norm;            /* enum tg_norm_kind of h */
+  const void *weight, *bias; /* device [n] or NULL */
+  float eps;               /* >= 0, finite */
+  int32_t n_tokens, n, n_gates;
+  int32_t type;            /* enum tg_type of everything but gate_row */
+} tg_norm_args;
+
+/*
+ * The norm after a block, its gate and the residual, and the norm before the next block, in one
+ * pass: with N(u) = weight * (u [- mean(u)]) / sqrt(mean((u [- mean(u)])^2) + eps) + bias,
+ *   r[t] = x_scale * x[t] + y_scale * gate[gate_row[t]] * N_y(y[t]),
+ *   x_out[t] = r[t],  h[t] = N(r[t]).
+ * r is kept in binary32 between the two, and each output rounded once. Sums of squares that leave
+ * binary32 are formed again from scaled values. A weight or bias without its norm is applied all the
+ * same.
+ * x_out and h must not overlap each other, nor an input but as above. Enqueued on `stream`;
+ * allocates nothing. Returns TG_E_INVAL (x NULL, x_out and h both NULL, negative count, n outside
+ * [1, TG_NORM_MAX_N], a bad kind, type, eps, scale or stride, y NULL with a gate, gate_row without
+ * gate, gate with n_gates < 1), TG_E_HIP. n_tokens == 0 enqueues nothing.
+ */
+int tg_norm(const tg_norm_args *args, void *stream);
+
+typedef struct {
+  const void *x;    /* device: row t is x + t * x_stride, k values */
+  int64_t x_stride; /* >= k */
+  int8_t *q;        /* device out: row t is q + t * q_stride, k integers */
+  int64_t q_stride; /* >= k */
+  float *scale;     /* device out [n_rows] */
+  int32_t n_rows, k;
+  int32_t type;     /* enum tg_type of x */
+} tg_quantize_args;
+
+/*
+ * Rows (tokens, or a weight's outputs) to 8-bit integers with a scale each:
+ *   scale[t] = max_i |x[t][i]| / 127, rounded to binary32;  q[t][i] = x[t][i] / scale[t], the
+ * exact quotient rounded to the nearest integer, ties to even, at most 127 either way. A row of zeros
+ * has scale 0 and integers 0. A row with an infinity or NaN has no such integers: its scale is NaN
+ * and they are 0, so that its products are NaN, and those of no other row.
+ * q must not overlap x. Enqueued on `stream`; allocates nothing. Returns TG_E_INVAL (null pointer,
+ * negative count, k < 1, a bad type or stride), TG_E_HIP. n_rows == 0 enqueues nothing.
+ */
+int tg_quantize(const tg_quantize_args *args, void *stream);
+
+/* Longest row of tg_project_i8: sums of products of 8-bit integers up to here hold in 32 bits. */
+#define TG_PROJECT_I8_MAX_K 131056
+
+typedef struct {
+  const int8_t *x;      /* device: token t's row is x + t * x_stride, k integers */
+  int64_t x_stride;     /* k .. 2^22, a multiple of 16 */
+  const float *x_scale; /* device [n_tokens] */
+  const int8_t *w;      /* device: output j's row is w + j * w_stride, k integers */
+  int64_t w_stride;     /* k .. 2^22, a multiple of 16 */
+  const float *w_scale; /* device [n] */
+  void *y;              /* device out: token t's row is y + t * y_stride, n values */
+  int64_t y_stride;     /* >= n */
+  int32_t n_tokens, k, n;
+  int32_t type;         /* enum tg_type of y */
+} tg_project_i8_args;
+
+/*
+ * A projection in 8-bit integers with a scale for each token and output:
+ *   y[t][j] = (x_scale[t] * w_scale[j]) * sum_i x[t][i] w[j][i].
+ * The sum is exact, in 32 bits; it, the scales' product and the result are rounded once each in
+ * binary32, and the result once to the type. All 256 integers may occur. y must not overlap an
+ * input. Enqueued on `stream`; allocates nothing and needs no workspace. Returns TG_E_INVAL (null
+ * pointer, negative count, k outside [16, TG_PROJECT_I8_MAX_K] or not a multiple of 16, n < 1,
+ * n_tokens or n over 2^30, a bad type or stride, x or w not 16-byte aligned), TG_E_HIP. n_tokens == 0 enqueues nothing.
+ */
+int tg_project_i8(const tg_project_i8_args *args, void *stream);
+
 /* Static description of a status code. */
 const char *tg_strerror(int code);
 

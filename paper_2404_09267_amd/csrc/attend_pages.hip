@@ -1,0 +1,622 @@
+// tg_attend_pages: attention of one new token a sequence over the pages of a cache.
+//
+// The query heads that share a key head are rows of one matrix tile, so that keys and values are
+// read once, and reading them bounds it: each wave has tiles of 32 keys and their values under way
+// to LDS while it works on the one before. A key's row in the cache is looked up by a lane, a
+// tile ahead of its loads; rows that are not seen (past the end, before the window, on a page
+// that is none) are loaded from 16 zeros instead, so that whatever lies there stays out, and
+// have no weight.
+//
+// Softmax in one pass over the keys (Milakov and Gimelshein 2018): a running maximum m in units of
+// log2, the sum l of 2^(z - m) and the weighted sum of values, the latter two multiplied by
+// 2^(m_old - m_new) when a score passes m by kSlack. Scores are computed transposed, S^T = K Q^T,
+// so that a lane's scores are of one query and the weights come out where the second product,
+// O^T = V^T P^T, takes them as an operand.
+//
+// All sequences' keys are cut into parts of one length, found on the device, so that every
+// workgroup has as much to read whatever the lengths are; join_kernel joins them in a set order.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cfloat>
+#include <climits>
+#include <cmath>
+#include <cstdint>
+
+#include "tg.h"
+#include "token_math.h"
+
+namespace {
+
+using namespace tok;
+
+constexpr int kMaxStride = 1 << 22, kMaxKeys = 1 << 30;
+constexpr float kSlack = 8.0f;
+// Weights are kept times 2^kLift: binary16's smallest number is 2^-24, and what lies below 2^-25 of
+// the largest weight would be lost, however many such keys there are. With kSlack they reach
+// 2^15, which binary16 holds.
+template <int kType>
+constexpr float kLift = kType == TG_F16 ? 7.0f : 0.0f;
+constexpr float kLog2e = 1.4426950408889634f;
+
+struct AttendParams {
+  const void *q, *k, *v;
+  void *out;
+  int64_t q_stride, q_head, k_stride, k_head, v_stride, v_head, out_stride, out_head;
+  int64_t table_stride;
+  const int32_t *table, *kv_len;
+  const float *slope;
+  float to_log2;   // scale * log2(e): a raw score's factor
+  float cap_arg;   // scale / cap
+  float cap_out;   // cap * log2(e), 0: no cap
+  int32_t window, n_seqs, n_pages, page_size;
+  int32_t page_log2;  // of page_size, -1: it is no power of two
+  int32_t most;    // keys of a sequence at most
+  int32_t n_heads, n_kv_heads, group, d;
+  int32_t row_tiles;
+  int32_t width;   // parts that all keys are cut into, 0: no sequence is cut
+  float *part;     // [width + n_seqs][n_heads][d] weighted sums, and
+  float *part_ml;  // [..][..][2] maximum (log2 units) and sum of weights
+};
+
+// Keys [lo, hi) of a sequence are seen by its query.
+struct Span {
+  int lo, hi;
+};
+
+__device__ __forceinline__ Span span_of(const AttendParams &P, int len) {
+  Span r;
+  r.hi = min(max(len, 0), P.most);
+  // the query stands at the last key there is, whatever of them is left out at the end
+  r.lo = P.window > 0 && len > P.window ? min(len - P.window, r.hi) : 0;
+  return r;
+}
+
+// tanh(x) in binary32, to 3e-7 of it: the quotient where 1 and 2 / (1 + e^2x) do not cancel, else
+// the series x - x^3 / 3 + 2 x^5 / 15 - 17 x^7 / 315 (to 2e-9 below 1 / 8).
+__device__ __forceinline__ float bend(float x) {
+  const float e = __builtin_amdgcn_exp2f(x * (2.0f * kLog2e));
+  const float z = __builtin_fmaf(-2.0f, __builtin_amdgcn_rcpf(1.0f + e), 1.0f);
+  const float x2 = x * x;
+  const float p = __builtin_fmaf(
+      x2, __builtin_fmaf(x2, __builtin_fmaf(x2, -17.0f / 315, 2.0f / 15), -1.0f / 3), 1.0f);
+  return fabsf(x) < 0.125f ? x * p : z;
+}
+
+// a[0] + a[1] + c of two values of the type.
+template <int kType>
+__device__ __forceinline__ float add2(typename Num<kType>::V2 a, float c);
+template <>
+__device__ __forceinline__ float add2<TG_F16>(Num<TG_F16>::V2 a, float c) {
+  const Num<TG_F16>::V2 one = {static_cast<_Float16>(1.0f), static_cast<_Float16>(1.0f)};
+  return __builtin_amdgcn_fdot2(a, one, c, false);
+}
+template <>
+__device__ __forceinline__ float add2<TG_BF16>(Num<TG_BF16>::V2 a, float c) {
+  const Num<TG_BF16>::V2 one = {static_cast<__bf16>(1.0f), static_cast<__bf16>(1.0f)};
+  return __builtin_amdgcn_fdot2_f32_bf16(a, one, c, false);
+}
+
+template <int kType>
+__device__ __forceinline__ typename Num<kType>::V4 read_transposed(const void *p) {
+  typedef __attribute__((address_space(3))) s16x4 *P3;
+  return __builtin_bit_cast(
+      typename Num<kType>::V4,
+      __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<P3>(
+          reinterpret_cast<uintptr_t>(p))));
+}
+
+// 16 bytes per lane, each from its own address, into LDS at `to` + 16 * lane. The caller waits.
+__device__ __forceinline__ void gather_lds(const void *from, void *to) {
+  __builtin_amdgcn_global_load_lds(
+      reinterpret_cast<const __attribute__((address_space(1))) void *>(
+          reinterpret_cast<uintptr_t>(from)),
+      reinterpret_cast<__attribute__((address_space(3))) void *>(reinterpret_cast<uintptr_t>(to)),
+      16, 0, 0);
+}
+
+// What rows that are not seen are read from.
+__device__ const uint32_t kZeros[4] __attribute__((aligned(16))) = {0, 0, 0, 0};
+
+// Place of 16-byte chunk c of row r in a tile of rows of kChunks chunks (8 or 16). Matrix
+// operands take one chunk of 16 rows at once, transposing reads 2 chunks of 8 rows: both fall on
+// 16 different places of the 256 bytes that LDS serves at once.
+template <int kChunks>
+__device__ __forceinline__ int place_of(int r, int c) {
+  if (kChunks == 16) return c ^ (((r & 7) << 1) | ((r >> 3) & 1));
+  return c ^ ((((r >> 1) & 3) << 1) | ((r >> 3) & 1));
+}
+
+// ------------------------------------------------------------------------ the parts of all keys
+
+constexpr int kMaxCut = 1024;  // sequences, where any is cut
+// Parts have 128 keys at least; where that makes more than one workgroup a place, up to 512, for
+// one workgroup a place; beyond, for three.
+constexpr int kMinPart = 128, kOneRound = 512;
+
+struct Parts {
+  int chunk;   // keys of a part
+  int seq;     // the sequence asked for, -1: there is none
+  int first;   // its first part
+  int count;   // its parts
+  Span s;
+};
+
+// `part` >= 0: the sequence that has it; otherwise sequence `seq`. A wave works it out.
+__device__ __forceinline__ Parts find_parts(const AttendParams &P, int part, int seq) {
+  const int lane = threadIdx.x & 63;
+  constexpr int kEach = kMaxCut / 64, kAtOnce = 4;
+  int keys[kEach];
+  int64_t total = 0;
+#pragma unroll
+  for (int u0 = 0; u0 < kEach; u0 += kAtOnce) {
+    if (u0 * 64 < P.n_seqs) {  // loads of one turn without a branch between them
+      int len[kAtOnce];
+#pragma unroll
+      for (int u = 0; u < kAtOnce; ++u)
+        len[u] = P.kv_len[min((u0 + u) * 64 + lane, P.n_seqs - 1)];
+#pragma unroll
+      for (int u = 0; u < kAtOnce; ++u) {
+        const Span s = span_of(P, len[u]);
+        keys[u0 + u] = (u0 + u) * 64 + lane < P.n_seqs ? s.hi - s.lo : -1;
+        total += max(keys[u0 + u], 0);
+      }
+    } else {
+#pragma unroll
+      for (int u = 0; u < kAtOnce; ++u) keys[u0 + u] = -1;
+    }
+  }
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) total += __shfl_xor(total, o);
+  const auto even = [&](int parts) {
+    return static_cast<int>(((total + parts - 1) / parts + 63) / 64 * 64);
+  };
+  Parts r = {kMinPart, -1, 0, 0, {0, 0}};
+  const int one = even((P.width + 2) / 3);
+  if (one >= 2 * kMinPart) r.chunk = min(one, kOneRound);
+  r.chunk = max(r.chunk, even(P.width));
+  int before = 0;
+#pragma unroll
+  for (int u = 0; u < kEach; ++u) {
+    if (u * 64 >= P.n_seqs) continue;
+    const int mine = keys[u] < 0 ? 0 : max((keys[u] + r.chunk - 1) / r.chunk, 1);
+    int upto = mine;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int v = __shfl_up(upto, o);
+      if (lane >= o) upto += v;
+    }
+    const uint64_t at = part >= 0 ? __ballot(before + upto > part)
+                                  : (seq >= u * 64 && seq < u * 64 + 64 ? 1ull << (seq & 63) : 0);
+    if (at && r.seq < 0) {
+      const int l = __builtin_amdgcn_readfirstlane(__builtin_ctzll(at));
+      r.seq = u * 64 + l;
+      r.count = __builtin_amdgcn_readlane(mine, l);
+      r.first = before + __builtin_amdgcn_readlane(upto, l) - r.count;
+    }
+    before += __builtin_amdgcn_readlane(upto, 63);
+  }
+  r.seq = __builtin_amdgcn_readfirstlane(r.seq);
+  r.first = __builtin_amdgcn_readfirstlane(r.first);
+  r.count = __builtin_amdgcn_readfirstlane(r.count);
+  r.chunk = __builtin_amdgcn_readfirstlane(r.chunk);
+  if (r.seq >= 0) r.s = span_of(P, P.kv_len[r.seq]);
+  return r;
+}
+
+// A result from its sum of weights: a query that sees no key has no maximum, one whose scores are
+// all minus infinity the least number as one.
+__device__ __forceinline__ float weighted(float sum, float m, float l) {
+  return l == 0.0f ? (m == -INFINITY ? 0.0f : NAN) : sum / l;
+}
+
+// Rows of a workgroup: 16 query heads that share a key head. Each of its two waves takes every
+// second 32 keys of the workgroup's range through LDS of its own; two waves, so that several
+// workgroups fit a CU and one's start and end fall into another's loads.
+constexpr int kWaves = 2, kKeys = 32;
+constexpr int kWorkgroups = 1536;  // that the keys are cut for
+
+template <int kType, int kD>
+__global__ __launch_bounds__(kWaves * 64) void attend_pages_kernel(const AttendParams P) {
+  typedef Num<kType> N;
+  typedef typename N::E E;
+  typedef typename N::V4 V4;
+  typedef typename N::V8 V8;
+  constexpr int kChunks = kD / 8, kSteps = kD / 32, kBlocks = kD / 16;
+  constexpr int kPer = 64 / kChunks, kLoads = kKeys / kPer;  // rows of one load, loads of a tile
+  __shared__ __attribute__((aligned(16))) E tile[kWaves][2][2][kKeys * kD];
+  __shared__ float s_m[kWaves][16], s_l[kWaves][16];
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int col = lane & 15, quad = lane >> 4;
+  int id = workgroup();
+  const int kvh = id % P.n_kv_heads;
+  id /= P.n_kv_heads;
+  const int rt = id % P.row_tiles;
+  id /= P.row_tiles;
+  Parts parts = {0, id, id, 1, {0, 0}};
+  if (P.width > 0) {
+    parts = find_parts(P, id, -1);
+    if (parts.seq < 0) return;
+  } else {
+    if (id >= P.n_seqs) return;
+    parts.s = span_of(P, P.kv_len[id]);
+  }
+  const int seq = parts.seq;
+  const int from = parts.s.lo + (id - parts.first) * parts.chunk;
+  const int end = parts.count > 1 ? from + min(parts.s.hi - from, parts.chunk) : parts.s.hi;
+  const int32_t *table = P.table + seq * P.table_stride;
+  const E *kb = static_cast<const E *>(P.k) + kvh * P.k_head;
+  const E *vb = static_cast<const E *>(P.v) + kvh * P.v_head;
+  // Lane r of each half of the wave looks after key r of a tile: its page, and its row there.
+  auto page_at = [&](int j0) {
+    const uint32_t j = j0 + (lane & 31);
+    const uint32_t at = P.page_log2 >= 0 ? j >> P.page_log2 : j / P.page_size;
+    return static_cast<int>(j) < end ? table[at] : -1;
+  };
+  auto row_at = [&](int j0, int page) {
+    const uint32_t j = j0 + (lane & 31);
+    const uint32_t in = P.page_log2 >= 0 ? j & (P.page_size - 1) : j % P.page_size;
+    return static_cast<uint32_t>(page) < static_cast<uint32_t>(P.n_pages)
+               ? page * P.page_size + static_cast<int>(in)
+               : -1;
+  };
+  // The loads of a tile, and which of its keys are seen.
+  auto fetch = [&](int row, int to) {
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const int r = i * kPer + lane / kChunks;
+      const int c = place_of<kChunks>(r, lane & (kChunks - 1)) * 8;
+      const int64_t at = __shfl(row, r);
+      const bool use = at >= 0 && c < P.d;
+      const void *pk = use ? static_cast<const void *>(kb + at * P.k_stride + c) : kZeros;
+      const void *pv = use ? static_cast<const void *>(vb + at * P.v_stride + c) : kZeros;
+      gather_lds(pk, &tile[wave][to][0][i * kPer * kD]);
+      gather_lds(pv, &tile[wave][to][1][i * kPer * kD]);
+    }
+    return static_cast<uint32_t>(__ballot(row >= 0));
+  };
+  constexpr int kStep = kWaves * kKeys;
+  int j0 = from + wave * kKeys, buf = 0;
+  const int page0 = page_at(j0);
+  int page = page_at(j0 + kStep);
+  const int my = rt * 16 + col;  // this lane's row
+  const bool live = my < P.group;
+  const int head = kvh * P.group + min(my, P.group - 1);
+  const E *qr = static_cast<const E *>(P.q) + seq * P.q_stride + head * P.q_head;
+  V8 qf[kSteps];
+#pragma unroll
+  for (int k = 0; k < kSteps; ++k) {
+    qf[k] = V8{};
+    if (live && k * 32 + quad * 8 < P.d)
+      qf[k] = *reinterpret_cast<const V8 *>(qr + k * 32 + quad * 8);
+  }
+  const float slope2 = P.slope ? P.slope[head] * kLog2e : 0.0f;
+  const int last = P.kv_len[seq] - 1;
+  uint32_t seen = 0;
+  if (j0 < end) seen = fetch(row_at(j0, page0), 0);
+  f32x4 acc[kBlocks] = {};
+  float m = -INFINITY, l = 0.0f;
+  bool any = false;
+  for (; j0 < end; j0 += kStep) {
+    wait_loads();
+    const E *tk = tile[wave][buf][0], *tv = tile[wave][buf][1];
+    const uint32_t now = seen;
+    if (j0 + kStep < end) {
+      // nothing may ask for the page before the wait: the tile's loads are older
+      asm volatile("" : "+v"(page));
+      const int row = row_at(j0 + kStep, page);
+      page = page_at(j0 + 2 * kStep);
+      seen = fetch(row, buf ^ 1);
+    }
+    f32x4 z[2] = {};
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+      for (int k = 0; k < kSteps; ++k) {
+        const int r = b * 16 + col;
+        const V8 kf = *reinterpret_cast<const V8 *>(
+            tk + r * kD + place_of<kChunks>(r, 4 * k + quad) * 8);
+        z[b] = N::mfma16(kf, qf[k], z[b]);
+      }
+    if (P.cap_out > 0.0f) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        z[e >> 2][e & 3] = P.cap_out * bend(z[e >> 2][e & 3] * P.cap_arg);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) z[e >> 2][e & 3] *= P.to_log2;
+    }
+    if (P.slope) {
+      const int far = last - j0 - 4 * quad;
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        z[e >> 2][e & 3] -= slope2 * static_cast<float>(far - ((e >> 2) * 16 + (e & 3)));
+    }
+    if (now != 0xFFFFFFFFu) {
+      const uint32_t mine = now >> (4 * quad);
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (!(mine >> ((e >> 2) * 16 + (e & 3)) & 1)) z[e >> 2][e & 3] = -INFINITY;
+    }
+    any = any || now != 0;
+    float big = -INFINITY;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) big = fmaxf(big, z[e >> 2][e & 3]);
+    if (__ballot(big > m + kSlack)) {
+      big = fmaxf(big, __shfl_xor(big, 16));
+      big = fmaxf(big, __shfl_xor(big, 32));
+      const float to = fmaxf(m, big);
+      const float fix = to == m ? 1.0f : __builtin_amdgcn_exp2f(m - to);
+      m = to;
+      l *= fix;
+#pragma unroll
+      for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) acc[b][r] *= fix;
+    }
+    // the difference first: with scores of 2^24 and more the sum of m and kLift would be off
+    const float base = m == -INFINITY ? 0.0f : m;
+    V8 pf;
+#pragma unroll
+    for (int e = 0; e < 8; e += 2) {
+      const float p0 = __builtin_amdgcn_exp2f((z[e >> 2][e & 3] - base) + kLift<kType>);
+      const float p1 = __builtin_amdgcn_exp2f((z[e >> 2][(e & 3) + 1] - base) + kLift<kType>);
+      const auto two = pack2<kType>(p0, p1);
+      l = add2<kType>(two, l);
+      pf[e] = two[0];
+      pf[e + 1] = two[1];
+    }
+#pragma unroll
+    for (int b = 0; b < kBlocks; ++b) {
+      const int r0 = 4 * quad + (col >> 2), c = 2 * b + ((col & 3) >> 1);
+      const V4 v0 = read_transposed<kType>(
+          tv + r0 * kD + place_of<kChunks>(r0, c) * 8 + (col & 1) * 4);
+      const V4 v1 = read_transposed<kType>(
+          tv + (r0 + 16) * kD + place_of<kChunks>(r0 + 16, c) * 8 + (col & 1) * 4);
+      const V8 vf = __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7);
+      acc[b] = N::mfma16(vf, pf, acc[b]);
+    }
+    buf ^= 1;
+  }
+  // the waves' ranges are joined through LDS
+  l += __shfl_xor(l, 16);
+  l += __shfl_xor(l, 32);
+  if (any && m == -INFINITY) m = -FLT_MAX;
+  wait_loads();
+  __syncthreads();  // the tiles are done with
+  float *sums = reinterpret_cast<float *>(&tile[0][0][0][0]);  // [kWaves][16][kD]
+  if (quad == 0) {
+    s_m[wave][col] = m;
+    s_l[wave][col] = l;
+  }
+#pragma unroll
+  for (int b = 0; b < kBlocks; ++b)
+    *reinterpret_cast<f32x4 *>(sums + (wave * 16 + col) * kD + b * 16 + quad * 4) = acc[b];
+  __syncthreads();
+  constexpr int kLanes = kWaves * 4;  // threads of a row
+  const int r = threadIdx.x / kLanes, c0 = threadIdx.x % kLanes;
+  const int mine = rt * 16 + r;
+  if (mine >= P.group) return;
+  float top = -INFINITY;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) top = fmaxf(top, s_m[w][r]);
+  float f[kWaves], sum = 0.0f;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) {
+    f[w] = s_m[w][r] == top ? 1.0f : __builtin_amdgcn_exp2f(s_m[w][r] - top);
+    sum += f[w] * s_l[w][r];
+  }
+  const int ohead = kvh * P.group + mine;
+  const int64_t flat = int64_t(id) * P.n_heads + ohead;
+  E *o = static_cast<E *>(P.out) + seq * P.out_stride + ohead * P.out_head;
+#pragma unroll
+  for (int b = 0; b < kD / 4 / kLanes; ++b) {
+    const int c = (b * kLanes + c0) * 4;
+    if (c >= P.d) continue;
+    f32x4 v = {};
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w)
+      v += f[w] * *reinterpret_cast<const f32x4 *>(sums + (w * 16 + r) * kD + c);
+    if (parts.count == 1) {
+#pragma unroll
+      for (int q = 0; q < 4; ++q) v[q] = weighted(v[q], top, sum);
+      *reinterpret_cast<V4 *>(o + c) = __builtin_convertvector(v, V4);
+    } else {
+      *reinterpret_cast<f32x4 *>(P.part + flat * P.d + c) = v;
+    }
+  }
+  if (parts.count > 1 && c0 == 0) {
+    P.part_ml[flat * 2] = top;
+    P.part_ml[flat * 2 + 1] = sum;
+  }
+}
+
+// Joins the parts of a query head: a workgroup each, 32 lanes a part with 4 values each.
+constexpr int kJoinThreads = 256;
+
+template <int kType>
+__global__ __launch_bounds__(kJoinThreads, 4) void join_kernel(const AttendParams P) {
+  typedef typename Num<kType>::E E;
+  typedef typename Num<kType>::V4 V4;
+  constexpr int kAtOnce = kJoinThreads / 32;
+  __shared__ f32x4 s_sum[kAtOnce][32];
+  __shared__ float s_w[64];
+  const int tid = threadIdx.x, lane = tid & 63, group = tid >> 5, c = (tid & 31) * 4;
+  const int id = workgroup(), head = id % P.n_heads, seq = id / P.n_heads;
+  if (seq >= P.n_seqs) return;
+  const Parts parts = find_parts(P, -1, seq);
+  if (parts.count <= 1) return;
+  const int n = parts.count;
+  const int64_t flat = int64_t(parts.first) * P.n_heads + head;
+  float top = -INFINITY, total = 0.0f;
+  f32x4 sum = {};
+  for (int k0 = 0; k0 < n; k0 += 64) {  // lane k of every wave has part k's maximum and sum
+    float pm = -INFINITY, pl = 0.0f;
+    if (k0 + lane < n) {
+      const float *ml = P.part_ml + (int64_t(k0 + lane) * P.n_heads + flat) * 2;
+      pm = ml[0];
+      pl = ml[1];
+    }
+    f32x4 v[64 / kAtOnce];
+#pragma unroll
+    for (int u = 0; u < 64 / kAtOnce; ++u) {
+      const int k = k0 + u * kAtOnce + group;
+      v[u] = f32x4{};
+      if (k < n && c < P.d)
+        v[u] = *reinterpret_cast<const f32x4 *>(P.part + (int64_t(k) * P.n_heads + flat) * P.d + c);
+    }
+    const float to = fmaxf(top, wave_max(pm));
+    const float fix = top == to ? 1.0f : __builtin_amdgcn_exp2f(top - to);
+    const float f = pm == to ? 1.0f : __builtin_amdgcn_exp2f(pm - to);
+    top = to;
+    total = total * fix + wave_sum(f * pl);
+    sum *= fix;
+    if (k0 > 0) __syncthreads();
+    if (tid < 64) s_w[lane] = f;
+    __syncthreads();
+#pragma unroll
+    for (int u = 0; u < 64 / kAtOnce; ++u) {
+      const int k = u * kAtOnce + group;
+      if (k0 + k < n) sum += s_w[k] * v[u];
+    }
+  }
+  s_sum[group][tid & 31] = sum;
+  __syncthreads();
+  if (group == 0 && c < P.d) {
+#pragma unroll
+    for (int g = 1; g < kAtOnce; ++g) sum += s_sum[g][tid];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) sum[q] = weighted(sum[q], top, total);
+    E *o = static_cast<E *>(P.out) + seq * P.out_stride + head * P.out_head;
+    *reinterpret_cast<V4 *>(o + c) = __builtin_convertvector(sum, V4);
+  }
+}
+
+// ------------------------------------------------------------------------------- the host
+
+// Keys that are not cut, as the join's launch costs more: up to 512, or 1,024 where the sequences
+// alone make 64 workgroups, or 4,096 where they make all that the cut would be for.
+constexpr int kWhole = 512, kWholeOfMany = 1024, kWholeOfAll = 4096, kManyWorkgroups = 64;
+
+int64_t each_of(int n_heads, int n_kv_heads) {  // workgroups of a part
+  return int64_t(n_kv_heads) * ((n_heads / n_kv_heads + 15) / 16);
+}
+
+// Parts that the keys are cut into, 0 for no cut.
+int width_of(int n_seqs, int max_kv, int64_t each) {
+  const int64_t alone = n_seqs * each;
+  const int whole = alone >= kWorkgroups ? kWholeOfAll : alone >= kManyWorkgroups ? kWholeOfMany
+                                                                                  : kWhole;
+  if (n_seqs > kMaxCut || max_kv <= whole) return 0;
+  return static_cast<int>(std::max<int64_t>((kWorkgroups + each - 1) / each, n_seqs));
+}
+
+template <int kType, int kD>
+int launch(const AttendParams &P, hipStream_t s) {
+  const int64_t blocks = (int64_t(P.n_seqs) + P.width) * P.n_kv_heads * P.row_tiles;
+  const int64_t joined = P.width > 0 ? int64_t(P.n_seqs) * P.n_heads : 0;
+  if (blocks > kMaxWorkgroups || joined > kMaxWorkgroups) return TG_E_INVAL;
+  hipLaunchKernelGGL((attend_pages_kernel<kType, kD>), grid_of(blocks, kWaves * 64),
+                     dim3(kWaves * 64), 0, s, P);
+  if (joined > 0)
+    hipLaunchKernelGGL(join_kernel<kType>, grid_of(joined, kJoinThreads), dim3(kJoinThreads), 0, s,
+                       P);
+  return hipGetLastError() == hipSuccess ? TG_OK : TG_E_HIP;
+}
+
+bool layout_ok(const void *p, int64_t stride, int64_t head) {
+  return p && aligned16(p) && stride >= 0 && stride <= kMaxStride && stride % 8 == 0 &&
+         head >= 0 && head % 8 == 0;
+}
+
+bool sizes_ok(int n_seqs, int max_kv, int n_heads, int n_kv_heads, int d) {
+  return n_seqs >= 0 && n_seqs <= TG_PAGES_MAX_SEQS && max_kv >= 0 &&
+         max_kv <= kMaxKeys && n_heads >= 1 &&
+         n_kv_heads >= 1 && n_heads % n_kv_heads == 0 && d >= 8 && d <= TG_ATTEND_MAX_D &&
+         d % 8 == 0;
+}
+
+}  // namespace
+
+// Parts of a call, and of every call of fewer sequences or shorter ones with it: those may have more
+// parts than this one, which may have none.
+extern "C" size_t tg_attend_pages_workspace_bytes(int32_t n_seqs, int32_t max_kv_len,
+                                                  int32_t n_heads, int32_t n_kv_heads,
+                                                  int32_t d) {
+  if (!sizes_ok(n_seqs, max_kv_len, n_heads, n_kv_heads, d) || n_seqs == 0) return 0;
+  const int64_t each = each_of(n_heads, n_kv_heads);
+  if (max_kv_len <= kWhole) return 0;
+  const int64_t cut = std::min<int64_t>(n_seqs, kMaxCut);
+  const int64_t parts = std::max<int64_t>((kWorkgroups + each - 1) / each, cut) + cut;
+  return static_cast<size_t>(parts) * n_heads * (d + 2) * sizeof(float);
+}
+
+extern "C" int tg_attend_pages(const tg_attend_pages_args *a, void *stream) {
+  if (!a || !type_ok(a->type) ||
+      !sizes_ok(a->n_seqs, a->max_kv_len, a->n_heads, a->n_kv_heads, a->d) || a->n_pages < 0 ||
+      a->page_size < 1 || a->max_pages < 1 || a->window < 0 ||
+      int64_t(a->n_pages) * a->page_size > INT32_MAX || a->table_stride < a->max_pages ||
+      !std::isfinite(a->scale) || !std::isfinite(a->cap) || a->cap < 0.0f)
+    return TG_E_INVAL;
+  if (a->n_seqs == 0) return TG_OK;
+  if (!a->table || !a->kv_len || !layout_ok(a->q, a->q_stride, a->q_head_stride) ||
+      !layout_ok(a->out, a->out_stride, a->out_head_stride))
+    return TG_E_INVAL;
+  if (a->n_pages > 0 && (!layout_ok(a->k, a->k_stride, a->k_head_stride) ||
+                         !layout_ok(a->v, a->v_stride, a->v_head_stride)))
+    return TG_E_INVAL;
+  const size_t need = tg_attend_pages_workspace_bytes(a->n_seqs, a->max_kv_len, a->n_heads,
+                                                      a->n_kv_heads, a->d);
+  if (need > 0 && (!a->workspace || a->workspace_bytes < need || !aligned16(a->workspace)))
+    return TG_E_WORKSPACE;
+  AttendParams P = {};
+  P.q = a->q;
+  P.k = a->k;
+  P.v = a->v;
+  P.out = a->out;
+  P.q_stride = a->q_stride;
+  P.q_head = a->q_head_stride;
+  P.k_stride = a->k_stride;
+  P.k_head = a->k_head_stride;
+  P.v_stride = a->v_stride;
+  P.v_head = a->v_head_stride;
+  P.out_stride = a->out_stride;
+  P.out_head = a->out_head_stride;
+  P.table = a->table;
+  P.table_stride = a->table_stride;
+  P.kv_len = a->kv_len;
+  P.slope = a->slope;
+  // factors at the ends of binary32 are its largest numbers
+  const auto factor = [](double v) {
+    return static_cast<float>(std::min(std::max(v, -double(FLT_MAX)), double(FLT_MAX)));
+  };
+  P.to_log2 = factor(double(a->scale) * kLog2e);
+  if (a->cap > 0.0f) {
+    // of a cap so large that no score reaches tanh's bend, any other such will do
+    const double cap = std::min<double>(
+        a->cap, 0x1p100 * std::min(std::max(std::fabs(double(a->scale)), 1.0), 0x1p26));
+    P.cap_arg = factor(a->scale / cap);
+    P.cap_out = static_cast<float>(cap * kLog2e);
+  }
+  P.window = a->window;
+  P.n_seqs = a->n_seqs;
+  P.n_pages = a->n_pages;
+  P.page_size = a->page_size;
+  P.page_log2 = -1;
+  if ((a->page_size & (a->page_size - 1)) == 0) P.page_log2 = __builtin_ctz(a->page_size);
+  P.most = static_cast<int32_t>(
+      std::min<int64_t>(int64_t(a->max_pages) * a->page_size, a->max_kv_len));
+  P.n_heads = a->n_heads;
+  P.n_kv_heads = a->n_kv_heads;
+  P.group = a->n_heads / a->n_kv_heads;
+  P.d = a->d;
+  const int64_t each = each_of(a->n_heads, a->n_kv_heads);
+  P.row_tiles = static_cast<int32_t>(each / a->n_kv_heads);
+  P.width = width_of(a->n_seqs, P.most, each);
+  P.part = static_cast<float *>(a->workspace);
+  P.part_ml = P.part + (static_cast<size_t>(P.width) + a->n_seqs) * a->n_heads * a->d;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  if (a->d <= 64) return a->type == TG_F16 ? launch<TG_F16, 64>(P, s) : launch<TG_BF16, 64>(P, s);
+  return a->type == TG_F16 ? launch<TG_F16, 128>(P, s) : launch<TG_BF16, 128>(P, s);
+}

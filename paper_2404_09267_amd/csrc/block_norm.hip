@@ -1,0 +1,236 @@
+// tg_norm: the norm after a block, its gate and the residual, and the norm before the next block.
+//
+// x and y are read once and the residual and its norm written once, 8 bytes a value, and everything
+// between is kept in registers: that is what bounds it. A row is a wave's, a workgroup's of 256 or
+// one of 1,024 threads, so that a thread has 8 to 32 values. Mean and variance are taken one after
+// the other (of the differences from the mean), which costs a second sum over the row but no
+// digits, where sum and sum of squares at once would cancel.
+#include <hip/hip_runtime.h>
+
+#include <cmath>
+#include <cstdint>
+
+#include "rows.h"
+#include "tg.h"
+
+namespace {
+
+using namespace tok;
+
+struct NormParams {
+  const void *x, *y, *y_weight, *y_bias, *gate, *weight, *bias;
+  void *x_out, *h;
+  const int32_t *gate_row;
+  int64_t x_stride, y_stride, gate_stride, x_out_stride, h_stride;
+  float x_scale, y_scale, eps;
+  int32_t y_norm, norm, n_tokens, n, n_gates;
+  int32_t stream;  // past the caches
+};
+
+// Squares pass binary32 at both ends; such a row is brought near 1 by kFar or 1 / kFar first. Below
+// kTiny, what the smallest squares have lost counts where eps does not hide it.
+constexpr float kFar = 0x1p80f, kTiny = 0x1p-80f, kHides = 0x1p-60f;
+
+// u of a row to weight * (u [- mean]) / sqrt(mean square + eps) + bias. `turns`: LDS of 6 sums.
+template <int kType, int R, int kV, bool kVec>
+__device__ __forceinline__ void normalise(const NormParams &P, float (&u)[kV * 8], int kind,
+                                          const void *weight, const void *bias, int first,
+                                          float (*turns)[16]) {
+  typedef typename Num<kType>::E E;
+  const int n = P.n;
+  const float share = 1.0f / static_cast<float>(n);
+  if (kind != TG_NORM_NONE) {
+    const bool layer = kind == TG_NORM_LAYER;
+    const auto mean_of = [&](float up, float *turn) {
+      float v = 0.0f;
+#pragma unroll
+      for (int i = 0; i < kV; ++i)
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (first + i * R * 8 + e < n) v += u[i * 8 + e] * up;
+      return row_sum<R>(v, turn) * share;
+    };
+    // Of the differences from a mean, which is rounded: their mean (what that rounding left), and
+    // their mean square less its square.
+    const auto spread = [&](auto &&from, float &left, float *turn) {
+      float v = 0.0f, w = 0.0f;
+#pragma unroll
+      for (int i = 0; i < kV; ++i)
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (first + i * R * 8 + e < n) {
+            const float d = from(u[i * 8 + e]);
+            v += d;
+            w += d * d;
+          }
+      w = row_sum<R>(w, turn) * share;
+      left = layer ? row_sum<R>(v, turn + 16) * share : 0.0f;
+      return layer ? fmaxf(w - left * left, 0.0f) : w;  // of NaN, `left` is NaN
+    };
+    float left, mean = layer ? mean_of(1.0f, turns[0]) : 0.0f;
+    float square = spread([&](float v) { return v - mean; }, left, turns[1]);
+    const bool large = !(square < INFINITY) || !(fabsf(left) < INFINITY);
+    if (large || (square < kTiny && P.eps < kHides)) {  // the same in the row's threads
+      const float up = large ? 1.0f / kFar : kFar, before = large ? up : 1.0f;
+      const float after = large ? 1.0f : up;
+      if (large) mean = layer ? mean_of(up, turns[3]) : 0.0f;
+      square = spread([&](float v) { return (v * before - mean) * after; }, left, turns[4]);
+      const float inverse = rsqrtf(square + P.eps * up * up);
+#pragma unroll
+      for (int i = 0; i < kV * 8; ++i)
+        u[i] = ((u[i] * before - mean) * after - left) * inverse;
+    } else {
+      const float inverse = rsqrtf(square + P.eps), shift = -left * inverse;
+#pragma unroll
+      for (int i = 0; i < kV * 8; ++i) u[i] = __builtin_fmaf(u[i] - mean, inverse, shift);
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < kV; ++i) {
+    const int c = first + i * R * 8;
+    if (weight) {
+      const Chunk<kType> w = load_chunk<kType, kVec>(static_cast<const E *>(weight), c, n, false);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) u[i * 8 + e] *= static_cast<float>(w[e]);
+    }
+    if (bias) {
+      const Chunk<kType> b = load_chunk<kType, kVec>(static_cast<const E *>(bias), c, n, false);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) u[i * 8 + e] += static_cast<float>(b[e]);
+    }
+  }
+}
+
+template <int kType, int R, int kV, bool kVec>
+__global__ __launch_bounds__(kGroupThreads<R>) void norm_kernel(const NormParams P) {
+  typedef typename Num<kType>::E E;
+  constexpr int kRows = kGroupThreads<R> / R;
+  __shared__ float s_turns[R > 64 ? 12 : 1][16];
+  const int64_t t = int64_t(workgroup()) * kRows + threadIdx.x / R;
+  if (t >= P.n_tokens) return;  // a whole wave, or the workgroup
+  const int first = threadIdx.x % R * 8, n = P.n;
+  const bool stream = P.stream != 0;
+  Chunk<kType> xv[kV];
+  const E *x = static_cast<const E *>(P.x) + t * P.x_stride;
+#pragma unroll
+  for (int i = 0; i < kV; ++i) xv[i] = load_chunk<kType, kVec>(x, first + i * R * 8, n, stream);
+  int g = P.y ? 0 : -1;
+  if (P.gate_row) g = P.gate_row[t];
+  if (P.gate && (g < 0 || g >= P.n_gates)) g = -1;
+  float u[kV * 8];
+  if (P.y && g >= 0) {
+    const E *y = static_cast<const E *>(P.y) + t * P.y_stride;
+#pragma unroll
+    for (int i = 0; i < kV; ++i) {
+      const Chunk<kType> v = load_chunk<kType, kVec>(y, first + i * R * 8, n, stream);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) u[i * 8 + e] = static_cast<float>(v[e]);
+    }
+    normalise<kType, R, kV, kVec>(P, u, P.y_norm, P.y_weight, P.y_bias, first, s_turns);
+    const E *gate = P.gate ? static_cast<const E *>(P.gate) + g * P.gate_stride : nullptr;
+#pragma unroll
+    for (int i = 0; i < kV; ++i) {
+      if (gate) {
+        const Chunk<kType> v = load_chunk<kType, kVec>(gate, first + i * R * 8, n, false);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) u[i * 8 + e] *= static_cast<float>(v[e]);
+      }
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        u[i * 8 + e] = P.x_scale * static_cast<float>(xv[i][e]) + P.y_scale * u[i * 8 + e];
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < kV * 8; ++i) u[i] = P.x_scale * static_cast<float>(xv[i / 8][i % 8]);
+  }
+  const auto put = [&](void *to, int64_t stride) {
+    E *row = static_cast<E *>(to) + t * stride;
+#pragma unroll
+    for (int i = 0; i < kV; ++i) {
+      Chunk<kType> v;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = static_cast<E>(u[i * 8 + e]);
+      store_chunk<kType, kVec>(row, first + i * R * 8, n, v, stream);
+    }
+  };
+  if (P.x_out) put(P.x_out, P.x_out_stride);
+  if (!P.h) return;
+  normalise<kType, R, kV, kVec>(P, u, P.norm, P.weight, P.bias, first, s_turns + (R > 64 ? 6 : 0));
+  put(P.h, P.h_stride);
+}
+
+template <int kType, int R, int kV>
+int launch_rows(const NormParams &P, bool vec, hipStream_t s) {
+  constexpr int kThreads = kGroupThreads<R>, kRows = kThreads / R;
+  const int64_t blocks = (int64_t(P.n_tokens) + kRows - 1) / kRows;
+  if (blocks > kMaxWorkgroups) return TG_E_INVAL;
+  const dim3 grid = grid_of(blocks, kThreads), threads(kThreads);
+  if (vec) hipLaunchKernelGGL((norm_kernel<kType, R, kV, true>), grid, threads, 0, s, P);
+  else hipLaunchKernelGGL((norm_kernel<kType, R, kV, false>), grid, threads, 0, s, P);
+  return hipGetLastError() == hipSuccess ? TG_OK : TG_E_HIP;
+}
+
+template <int kType>
+int launch(const NormParams &P, bool vec, hipStream_t s) {
+  if (P.n <= 512) return launch_rows<kType, 64, 1>(P, vec, s);
+  if (P.n <= 1024) return launch_rows<kType, 64, 2>(P, vec, s);
+  if (P.n <= 2048) return launch_rows<kType, 256, 1>(P, vec, s);
+  if (P.n <= 4096) return launch_rows<kType, 256, 2>(P, vec, s);
+  if (P.n <= 8192) return launch_rows<kType, 256, 4>(P, vec, s);
+  if (P.n <= 16384) return launch_rows<kType, 1024, 2>(P, vec, s);
+  return launch_rows<kType, 1024, 4>(P, vec, s);
+}
+
+bool kind_ok(int32_t k) { return k >= TG_NORM_NONE && k <= TG_NORM_LAYER; }
+
+}  // namespace
+
+extern "C" int tg_norm(const tg_norm_args *a, void *stream) {
+  if (!a || a->n_tokens < 0 || a->n < 1 || a->n > TG_NORM_MAX_N || a->n_gates < 0 ||
+      !type_ok(a->type) || !kind_ok(a->y_norm) || !kind_ok(a->norm) || !(a->eps >= 0.0f) ||
+      !std::isfinite(a->eps) || !std::isfinite(a->x_scale) || !std::isfinite(a->y_scale))
+    return TG_E_INVAL;
+  if ((a->gate && (!a->y || a->n_gates < 1)) || (a->gate_row && !a->gate)) return TG_E_INVAL;
+  if (a->n_tokens == 0) return TG_OK;
+  if (!a->x || (!a->x_out && !a->h)) return TG_E_INVAL;
+  bool vec = a->n % 8 == 0 && aligned16(a->y_weight) && aligned16(a->y_bias) &&
+             aligned16(a->weight) && aligned16(a->bias);
+  const void *rows[5] = {a->x, a->y, a->gate, a->x_out, a->h};
+  const int64_t strides[5] = {a->x_stride, a->y_stride, a->gate_stride, a->x_out_stride,
+                              a->h_stride};
+  int64_t arrays = 0;  // of n_tokens rows
+  for (int i = 0; i < 5; ++i) {
+    if (!rows[i]) continue;
+    if (strides[i] < a->n) return TG_E_INVAL;
+    vec = vec && aligned16(rows[i]) && strides[i] % 8 == 0;
+    arrays += i != 2;
+  }
+  NormParams P = {};
+  P.x = a->x;
+  P.y = a->y;
+  P.y_weight = a->y_weight;
+  P.y_bias = a->y_bias;
+  P.gate = a->gate;
+  P.weight = a->weight;
+  P.bias = a->bias;
+  P.x_out = a->x_out;
+  P.h = a->h;
+  P.gate_row = a->gate_row;
+  P.x_stride = a->x_stride;
+  P.y_stride = a->y_stride;
+  P.gate_stride = a->gate_stride;
+  P.x_out_stride = a->x_out_stride;
+  P.h_stride = a->h_stride;
+  P.x_scale = a->x_scale;
+  P.y_scale = a->y_scale;
+  P.eps = a->eps;
+  P.y_norm = a->y_norm;
+  P.norm = a->norm;
+  P.n_tokens = a->n_tokens;
+  P.n = a->n;
+  P.n_gates = a->n_gates;
+  // against the 256 MB that the last cache holds
+  P.stream = arrays * a->n_tokens * a->n * 2 > (int64_t(256) << 20);
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  return a->type == TG_F16 ? launch<TG_F16>(P, vec, s) : launch<TG_BF16>(P, vec, s);
+}

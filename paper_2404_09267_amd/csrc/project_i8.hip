@@ -1,0 +1,309 @@
+// tg_project_i8: a projection in 8-bit integers, y = (x_scale w_scale) (x w^T), sums exact in 32 bits.
+//
+// Few tokens: reading w bounds it. A workgroup takes 16 outputs and up to 64 tokens, its waves
+// parts of k in turn, straight from memory to the matrix instructions' registers, and the waves'
+// sums are joined through LDS: one launch, no workspace.
+// Many tokens: tiles of x and w go through LDS to the matrix instructions, several steps of 128
+// values of k under way.
+// Results lie transposed in the registers (a lane holds 4 outputs of one token), so that stores are
+// contiguous and a token's scale belongs to the lane. Both operands take the same values of k in
+// the same places, so that the order within an instruction does not matter.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <climits>
+#include <cstdint>
+
+#include "tg.h"
+#include "token_math.h"
+
+namespace {
+
+using namespace tok;
+
+constexpr int kMaxStride = 1 << 22, kMaxRows = 1 << 30;
+
+struct ProjectParams {
+  const int8_t *x, *w;
+  const float *x_scale, *w_scale;
+  void *y;
+  int64_t x_stride, w_stride, y_stride;
+  int32_t n_tokens, k, n;
+  int32_t tiles_t, tiles_n;
+};
+
+__device__ __forceinline__ i32x4 mfma(i32x4 a, i32x4 b, i32x4 c) {
+  return __builtin_amdgcn_mfma_i32_16x16x64_i8(a, b, c, 0, 0, 0);
+}
+
+// 4 outputs of one token, from n on.
+template <int kType>
+__device__ __forceinline__ void put(const ProjectParams &P, int t, int n, i32x4 sum) {
+  typedef typename Num<kType>::E E;
+  typedef typename Num<kType>::V4 V4;
+  if (t >= P.n_tokens || n >= P.n) return;
+  const float xs = P.x_scale[t];
+  E *to = static_cast<E *>(P.y) + int64_t(t) * P.y_stride + n;
+  f32x4 v;
+#pragma unroll
+  for (int r = 0; r < 4; ++r)
+    v[r] = static_cast<float>(sum[r]) * (xs * P.w_scale[min(n + r, P.n - 1)]);
+  const V4 out = __builtin_convertvector(v, V4);
+  if (n + 3 < P.n) {  // as they lie: rows may start anywhere
+    __builtin_memcpy(to, &out, sizeof(out));
+  } else {
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+      if (n + r < P.n) to[r] = out[r];
+  }
+}
+
+// ------------------------------------------------------------------------------ few tokens
+
+constexpr int kFewWaves = 8;
+
+// 16 kTt tokens x 16 outputs a workgroup; a wave takes every kFewWaves-th 256 values of k.
+template <int kType, int kTt>
+__global__ __launch_bounds__(kFewWaves * 64) void few_kernel(const ProjectParams P) {
+  constexpr int kAhead = 4;  // instructions' values of k that are loaded at once
+  __shared__ i32x4 s_sum[kFewWaves][kTt][64];
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int col = lane & 15, quad = lane >> 4;
+  const int id = workgroup();
+  const int n0 = id % P.tiles_n * 16, t0 = id / P.tiles_n * 16 * kTt;
+  const int8_t *w = P.w + int64_t(min(n0 + col, P.n - 1)) * P.w_stride;
+  const int8_t *x[kTt];
+#pragma unroll
+  for (int i = 0; i < kTt; ++i) x[i] = P.x + int64_t(min(t0 + 16 * i + col, P.n_tokens - 1)) * P.x_stride;
+  i32x4 acc[kTt] = {};
+  for (int k0 = wave * 64 * kAhead; k0 < P.k; k0 += kFewWaves * 64 * kAhead) {
+    i32x4 wv[kAhead], xv[kAhead][kTt];
+#pragma unroll
+    for (int a = 0; a < kAhead; ++a) {
+      const int c = k0 + a * 64 + quad * 16;
+      const bool in = c < P.k;
+      wv[a] = in ? *reinterpret_cast<const i32x4 *>(w + c) : i32x4{};
+#pragma unroll
+      for (int i = 0; i < kTt; ++i)
+        xv[a][i] = in ? *reinterpret_cast<const i32x4 *>(x[i] + c) : i32x4{};
+    }
+#pragma unroll
+    for (int a = 0; a < kAhead; ++a)
+#pragma unroll
+      for (int i = 0; i < kTt; ++i) acc[i] = mfma(wv[a], xv[a][i], acc[i]);
+  }
+#pragma unroll
+  for (int i = 0; i < kTt; ++i) s_sum[wave][i][lane] = acc[i];
+  __syncthreads();
+  for (int i = wave; i < kTt; i += kFewWaves) {
+    i32x4 sum = {};
+#pragma unroll
+    for (int v = 0; v < kFewWaves; ++v) sum += s_sum[v][i][lane];
+    put<kType>(P, t0 + 16 * i + col, n0 + 4 * quad, sum);
+  }
+}
+
+// ----------------------------------------------------------------------------- many tokens
+
+// A tile of kT tokens x kN outputs, kWt x kWn waves, 128 values of k a step, kStages steps of loads
+// under way. The next 64 values' operands are read from LDS while these are multiplied, so that the
+// matrix units have work across the barrier; the buffer of step s is free for step s + kStages
+// behind the barrier at the end of it, since its operands are in registers by then. Rows of a
+// tile lie in LDS as 8 chunks of 16 bytes, in an order in which one chunk of 16 rows, which is
+// what the operands' reads ask for, falls on all banks.
+constexpr int kBK = 128;
+__device__ __forceinline__ int place_of(int row, int c) { return c ^ ((row >> 1) & 7); }
+
+// Which tile a workgroup takes: workgroups go round the 8 XCDs, so each XCD gets a run of tiles of
+// its own, in blocks of kGroup token tiles by all output tiles, whose operands its L2 shares.
+constexpr int kXcds = 8, kGroup = 4;
+__device__ __forceinline__ void tile_of(int id, int tiles_t, int tiles_n, int &tt, int &tn) {
+  const int total = tiles_t * tiles_n;
+  const int each = total / kXcds, more = total % kXcds, x = id % kXcds;
+  const int k = x * each + min(x, more) + id / kXcds;
+  const int per = kGroup * tiles_n, g = k / per, in = k - g * per;
+  const int rows = min(kGroup, tiles_t - g * kGroup);
+  tt = g * kGroup + in % rows;
+  tn = in / rows;
+}
+
+template <int kType, int kT, int kN, int kWt, int kWn, int kStages>
+__global__ __launch_bounds__(kWt *kWn * 64, 2) void tile_kernel(const ProjectParams P) {
+  constexpr int kWaves = kWt * kWn, kFt = kT / kWt / 16, kFn = kN / kWn / 16;
+  constexpr int kChunks = kBK / 16, kRows = kT + kN, kPer = 64 / kChunks;  // rows of one load
+  constexpr int kLoads = kRows / kPer / kWaves;
+  static_assert(kLoads * kPer * kWaves == kRows && kT % kPer == 0, "whole loads");
+  static_assert(kWaves * kPer % 16 == 0, "rows of one lane");
+  __shared__ __attribute__((aligned(16))) int8_t tile[kStages][kRows * kBK];
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int col = lane & 15, quad = lane >> 4;
+  int tt, tn;
+  tile_of(blockIdx.x, P.tiles_t, P.tiles_n, tt, tn);
+  const int t0 = tt * kT, n0 = tn * kN;
+  const int xr = min(kT, P.n_tokens - t0), wr = min(kN, P.n - n0);
+  const auto xb =
+      buffer(P.x + t0 * P.x_stride, static_cast<uint32_t>((xr - 1) * P.x_stride + P.k));
+  const auto wb =
+      buffer(P.w + n0 * P.w_stride, static_cast<uint32_t>((wr - 1) * P.w_stride + P.k));
+  // load i of a wave covers kPer rows; rows past the tensor are not read. A lane's chunk is the
+  // same in all loads, since their rows are 4 kPer apart or more.
+  const int chunk = place_of(wave * kPer + lane / kChunks, lane % kChunks);
+  uint32_t at[kLoads];
+#pragma unroll
+  for (int i = 0; i < kLoads; ++i) {
+    const int row = (i * kWaves + wave) * kPer + lane / kChunks;
+    at[i] = row < kT ? static_cast<uint32_t>(row * P.x_stride + chunk * 16)
+                     : static_cast<uint32_t>((row - kT) * P.w_stride + chunk * 16);
+    if (row < kT ? row >= xr : row - kT >= wr) at[i] = kNowhere;
+  }
+  const int steps = (P.k + kBK - 1) / kBK;
+  // every step's loads are issued, past the last one too, so that they can be counted
+  auto fetch = [&](int s) {
+    const int k0 = s * kBK;
+    const bool past = k0 + chunk * 16 >= P.k;
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const int first = (i * kWaves + wave) * kPer;
+      load_lds(first < kT ? xb : wb, &tile[s % kStages][first * kBK], past ? kNowhere : at[i],
+               static_cast<uint32_t>(k0));
+    }
+  };
+  i32x4 acc[kFn][kFt] = {};
+  const int wt = (wave % kWt) * (kT / kWt), wn = (wave / kWt) * (kN / kWn);
+  struct Operands {  // of 64 values of k
+    i32x4 x[kFt], w[kFn];
+  };
+  auto read = [&](Operands &o, int s, int ks) {
+    const int8_t *m = tile[s % kStages];
+#pragma unroll
+    for (int i = 0; i < kFt; ++i) {
+      const int row = wt + 16 * i + col;
+      o.x[i] = *reinterpret_cast<const i32x4 *>(m + row * kBK + place_of(row, ks * 4 + quad) * 16);
+    }
+#pragma unroll
+    for (int j = 0; j < kFn; ++j) {
+      const int row = kT + wn + 16 * j + col;
+      o.w[j] = *reinterpret_cast<const i32x4 *>(m + row * kBK + place_of(row, ks * 4 + quad) * 16);
+    }
+  };
+  auto multiply = [&](const Operands &o) {
+#pragma unroll
+    for (int j = 0; j < kFn; ++j)
+#pragma unroll
+      for (int i = 0; i < kFt; ++i) acc[j][i] = mfma(o.w[j], o.x[i], acc[j][i]);
+  };
+  // the scheduler would put the reads at the end, where the products after them wait for them
+  auto interleave = [&](bool loads) {
+    constexpr int kReads = kFt + kFn, kMul = kFt * kFn;
+#pragma unroll
+    for (int i = 0; i < kReads; ++i) {
+      __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x008, kMul / kReads, 0);
+      if (loads && i < kLoads) __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);
+    }
+  };
+#pragma unroll
+  for (int s = 0; s < kStages; ++s) fetch(s);
+  wait_and_meet<(kStages - 1) * kLoads>();
+  Operands now, then;
+  read(now, 0, 0);
+  for (int s = 0; s < steps; ++s) {
+    // `now` has the first 64 values of step s, and is left with those of step s + 1
+    read(then, s, 1);
+    multiply(now);
+    interleave(false);
+    wait_and_meet<(kStages - 2) * kLoads>();  // step s + 1 is here, step s in registers
+    fetch(s + kStages);
+    read(now, s + 1, 0);
+    multiply(then);
+    interleave(true);
+  }
+  wait_loads();  // LDS belongs to the next workgroup from here on
+#pragma unroll
+  for (int i = 0; i < kFt; ++i)
+#pragma unroll
+    for (int j = 0; j < kFn; ++j)
+      put<kType>(P, t0 + wt + 16 * i + col, n0 + wn + 16 * j + 4 * quad, acc[j][i]);
+}
+
+// ------------------------------------------------------------------------------- the host
+
+template <int kType, int kT, int kN, int kWt, int kWn, int kStages>
+int launch_tiles(ProjectParams P, hipStream_t s) {
+  const int64_t tiles_t = (int64_t(P.n_tokens) + kT - 1) / kT;
+  const int64_t tiles_n = (int64_t(P.n) + kN - 1) / kN;
+  const int64_t blocks = tiles_t * tiles_n;
+  // threads that a launch takes in one direction
+  if (blocks * (kWt * kWn * 64) >= int64_t(1) << 32) return TG_E_INVAL;
+  P.tiles_t = static_cast<int32_t>(tiles_t);
+  P.tiles_n = static_cast<int32_t>(tiles_n);
+  hipLaunchKernelGGL((tile_kernel<kType, kT, kN, kWt, kWn, kStages>),
+                     dim3(static_cast<uint32_t>(blocks)), dim3(kWt * kWn * 64), 0, s, P);
+  return hipGetLastError() == hipSuccess ? TG_OK : TG_E_HIP;
+}
+
+template <int kType, int kTt>
+int launch_few(ProjectParams P, hipStream_t s) {
+  const int64_t tiles_t = (int64_t(P.n_tokens) + 16 * kTt - 1) / (16 * kTt);
+  P.tiles_n = static_cast<int32_t>((int64_t(P.n) + 15) / 16);
+  if (tiles_t * P.tiles_n > kMaxWorkgroups) return TG_E_INVAL;
+  hipLaunchKernelGGL((few_kernel<kType, kTt>), grid_of(tiles_t * P.tiles_n, kFewWaves * 64),
+                     dim3(kFewWaves * 64), 0, s, P);
+  return hipGetLastError() == hipSuccess ? TG_OK : TG_E_HIP;
+}
+
+constexpr int kFewTokens = 64;
+
+template <int kType>
+int launch(const ProjectParams &P, hipStream_t s) {
+  if (P.n_tokens <= 16) return launch_few<kType, 1>(P, s);
+  if (P.n_tokens <= 32) return launch_few<kType, 2>(P, s);
+  if (P.n_tokens <= kFewTokens) return launch_few<kType, 4>(P, s);
+  const auto tiles = [&](int t, int n) {
+    return ((int64_t(P.n_tokens) + t - 1) / t) * ((int64_t(P.n) + n - 1) / n);
+  };
+  if (tiles(128, 128) > 256) {
+    const auto rounds = [&](int t, int n, int at_once) { return (tiles(t, n) + at_once - 1) / at_once; };
+    const int64_t c256 = 164 * rounds(256, 256, 256), c192 = 137 * rounds(192, 256, 256);
+    const int64_t c160 = 118 * rounds(160, 128, 512), c128 = 100 * rounds(128, 128, 512);
+    const int64_t least = std::min(std::min(c256, c192), std::min(c160, c128));
+    if (c256 == least) return launch_tiles<kType, 256, 256, 2, 4, 2>(P, s);
+    if (c192 == least) return launch_tiles<kType, 192, 256, 4, 2, 2>(P, s);
+    if (c160 == least) return launch_tiles<kType, 160, 128, 2, 2, 2>(P, s);
+    return launch_tiles<kType, 128, 128, 2, 2, 2>(P, s);
+  }
+  if (tiles(128, 128) >= 160) return launch_tiles<kType, 128, 128, 2, 4, 4>(P, s);
+  if (tiles(64, 64) > 256) return launch_tiles<kType, 128, 64, 2, 2, 3>(P, s);
+  return launch_tiles<kType, 64, 64, 2, 2, 4>(P, s);
+}
+
+}  // namespace
+
+extern "C" int tg_project_i8(const tg_project_i8_args *a, void *stream) {
+  if (!a || a->n_tokens < 0 || a->k < 16 || a->k > TG_PROJECT_I8_MAX_K || a->k % 16 || a->n < 1 ||
+      a->n_tokens > kMaxRows || a->n > kMaxRows || !type_ok(a->type))
+    return TG_E_INVAL;
+  if (a->x_stride < a->k || a->w_stride < a->k || a->y_stride < a->n || a->x_stride % 16 ||
+      a->w_stride % 16 || a->x_stride > kMaxStride || a->w_stride > kMaxStride)
+    return TG_E_INVAL;
+  if (a->n_tokens == 0) return TG_OK;
+  if (!a->x || !a->w || !a->y || !a->x_scale || !a->w_scale || !aligned16(a->x) ||
+      !aligned16(a->w))
+    return TG_E_INVAL;
+  ProjectParams P = {};
+  P.x = a->x;
+  P.w = a->w;
+  P.x_scale = a->x_scale;
+  P.w_scale = a->w_scale;
+  P.y = a->y;
+  P.x_stride = a->x_stride;
+  P.w_stride = a->w_stride;
+  P.y_stride = a->y_stride;
+  P.n_tokens = a->n_tokens;
+  P.k = a->k;
+  P.n = a->n;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  return a->type == TG_F16 ? launch<TG_F16>(P, s) : launch<TG_BF16>(P, s);
+}

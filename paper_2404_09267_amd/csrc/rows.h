@@ -1,0 +1,63 @@
+// What the operators that take a row at a time share: a row's values in registers, 8 consecutive
+// ones a chunk, chunk i of thread t at 8 (i R + t) of R threads a row, and sums over a row.
+#pragma once
+
+#include "token_math.h"
+
+namespace tok {
+
+constexpr int kRowThreads = 256;  // of a workgroup, where a row takes no more
+
+template <int R>
+constexpr int kGroupThreads = R < kRowThreads ? kRowThreads : R;
+
+template <int kType>
+using Chunk = typename Num<kType>::V8;
+
+// The chunk at `c`: whole where rows start on 16 bytes and n is a multiple of 8 (kVec), else value
+// by value; zeros past n.
+template <int kType, bool kVec>
+__device__ __forceinline__ Chunk<kType> load_chunk(const typename Num<kType>::E *row, int c, int n,
+                                                   bool stream) {
+  Chunk<kType> v = {};
+  if constexpr (kVec) {
+    const auto *p = reinterpret_cast<const Chunk<kType> *>(row + c);
+    if (c < n) v = stream ? __builtin_nontemporal_load(p) : *p;
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (c + e < n) v[e] = row[c + e];
+  }
+  return v;
+}
+
+template <int kType, bool kVec>
+__device__ __forceinline__ void store_chunk(typename Num<kType>::E *row, int c, int n,
+                                            Chunk<kType> v, bool stream) {
+  if constexpr (kVec) {
+    auto *p = reinterpret_cast<Chunk<kType> *>(row + c);
+    if (c >= n) return;
+    if (stream) __builtin_nontemporal_store(v, p);
+    else *p = v;
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (c + e < n) row[c + e] = v[e];
+  }
+}
+
+// Sum over the R threads of a row, in all of them and in a set order. `turn`: LDS of this sum's own.
+template <int R>
+__device__ __forceinline__ float row_sum(float v, float *turn) {
+  v = wave_sum(v);
+  if constexpr (R > 64) {
+    if ((threadIdx.x & 63) == 0) turn[threadIdx.x >> 6] = v;
+    __syncthreads();
+    v = 0.0f;
+#pragma unroll
+    for (int w = 0; w < R / 64; ++w) v += turn[w];
+  }
+  return v;
+}
+
+}  // namespace tok

@@ -126,10 +126,54 @@ class AttendArgs(ctypes.Structure):
                 ("type", _i32), ("workspace", _vp), ("workspace_bytes", ctypes.c_size_t)]
 
 
+class PagesArgs(ctypes.Structure):
+    _fields_ = [("q_begin", _vp), ("kv_len", _vp), ("kv_len_out", _vp), ("release", _vp),
+                ("table", _vp), ("table_stride", _i64), ("free_pages", _vp), ("n_free", _vp),
+                ("n_free_out", _vp), ("slot", _vp), ("pos", _vp), ("refused", _vp),
+                ("n_seqs", _i32), ("n_tokens", _i32), ("n_pages", _i32), ("page_size", _i32),
+                ("max_pages", _i32), ("workspace", _vp), ("workspace_bytes", ctypes.c_size_t)]
+
+
+class AttendPagesArgs(ctypes.Structure):
+    _fields_ = [("q", _vp), ("k", _vp), ("v", _vp), ("q_stride", _i64), ("q_head_stride", _i64),
+                ("k_stride", _i64), ("k_head_stride", _i64), ("v_stride", _i64),
+                ("v_head_stride", _i64), ("out", _vp), ("out_stride", _i64),
+                ("out_head_stride", _i64), ("table", _vp), ("table_stride", _i64),
+                ("kv_len", _vp), ("slope", _vp), ("scale", _f32), ("cap", _f32),
+                ("window", _i32), ("n_seqs", _i32), ("n_pages", _i32), ("page_size", _i32),
+                ("max_pages", _i32), ("max_kv_len", _i32), ("n_heads", _i32),
+                ("n_kv_heads", _i32), ("d", _i32), ("type", _i32), ("workspace", _vp),
+                ("workspace_bytes", ctypes.c_size_t)]
+
+
+class NormArgs(ctypes.Structure):
+    _fields_ = [("x", _vp), ("x_stride", _i64), ("y", _vp), ("y_stride", _i64), ("y_norm", _i32),
+                ("y_weight", _vp), ("y_bias", _vp), ("gate", _vp), ("gate_stride", _i64),
+                ("gate_row", _vp), ("x_scale", _f32), ("y_scale", _f32), ("x_out", _vp),
+                ("x_out_stride", _i64), ("h", _vp), ("h_stride", _i64), ("norm", _i32),
+                ("weight", _vp), ("bias", _vp), ("eps", _f32), ("n_tokens", _i32), ("n", _i32),
+                ("n_gates", _i32), ("type", _i32)]
+
+
+class QuantizeArgs(ctypes.Structure):
+    _fields_ = [("x", _vp), ("x_stride", _i64), ("q", _vp), ("q_stride", _i64), ("scale", _vp),
+                ("n_rows", _i32), ("k", _i32), ("type", _i32)]
+
+
+class ProjectI8Args(ctypes.Structure):
+    _fields_ = [("x", _vp), ("x_stride", _i64), ("x_scale", _vp), ("w", _vp), ("w_stride", _i64),
+                ("w_scale", _vp), ("y", _vp), ("y_stride", _i64), ("n_tokens", _i32), ("k", _i32),
+                ("n", _i32), ("type", _i32)]
+
+
 GMM_MAX_MIX = 5
 F16, BF16 = 0, 1  # enum tg_type
 PROJECT_MAX_RANK = 64
 ATTEND_MAX_D = 128
+PAGES_MAX_SEQS = 1 << 20
+NORM_NONE, NORM_RMS, NORM_LAYER = 0, 1, 2  # enum tg_norm_kind
+NORM_MAX_N = 32768
+PROJECT_I8_MAX_K = 131056
 
 EXPORTS = ["tg_gmm_plane_stride", "tg_gmm_state_bytes", "tg_gmm_update",
            "tg_mask_rois_workspace_bytes", "tg_mask_rois", "tg_partition_workspace_bytes", "tg_partition", "tg_plan_pack", "tg_batch_count",
@@ -139,6 +183,9 @@ EXPORTS = ["tg_gmm_plane_stride", "tg_gmm_state_bytes", "tg_gmm_update",
            "tg_merge_workspace_bytes", "tg_merge",
            "tg_project_workspace_bytes", "tg_project", "tg_rotate",
            "tg_attend_workspace_bytes", "tg_attend",
+           "tg_pages_workspace_bytes", "tg_pages",
+           "tg_attend_pages_workspace_bytes", "tg_attend_pages",
+           "tg_norm", "tg_quantize", "tg_project_i8",
            "tg_strerror", "tg_abi_version"]
 
 _lib = None
@@ -221,6 +268,20 @@ def lib() -> ctypes.CDLL:
         L.tg_attend_workspace_bytes.restype = ctypes.c_size_t
         L.tg_attend.argtypes = [ctypes.POINTER(AttendArgs), _vp]
         L.tg_attend.restype = ctypes.c_int
+        L.tg_pages_workspace_bytes.argtypes = [_i32] * 2
+        L.tg_pages_workspace_bytes.restype = ctypes.c_size_t
+        L.tg_pages.argtypes = [ctypes.POINTER(PagesArgs), _vp]
+        L.tg_pages.restype = ctypes.c_int
+        L.tg_attend_pages_workspace_bytes.argtypes = [_i32] * 5
+        L.tg_attend_pages_workspace_bytes.restype = ctypes.c_size_t
+        L.tg_attend_pages.argtypes = [ctypes.POINTER(AttendPagesArgs), _vp]
+        L.tg_attend_pages.restype = ctypes.c_int
+        L.tg_norm.argtypes = [ctypes.POINTER(NormArgs), _vp]
+        L.tg_norm.restype = ctypes.c_int
+        L.tg_quantize.argtypes = [ctypes.POINTER(QuantizeArgs), _vp]
+        L.tg_quantize.restype = ctypes.c_int
+        L.tg_project_i8.argtypes = [ctypes.POINTER(ProjectI8Args), _vp]
+        L.tg_project_i8.restype = ctypes.c_int
         L.tg_strerror.argtypes = [ctypes.c_int]
         L.tg_strerror.restype = ctypes.c_char_p
         L.tg_abi_version.argtypes = []
@@ -1024,3 +1085,306 @@ def attend(q, k, v, seqs: Sequences, out, bufs: AttendBuffers, scale: float, cap
                                 k_pos, slope), stream)
     if rc != OK:
         raise TgError("tg_attend", rc)
+
+
+# ---- serving operators: a step of many requests over one paged cache ----------------
+
+def _here(*tensors) -> None:
+    """Checks that tensors are on the current device, whose stream a call is enqueued on."""
+    import torch
+
+    device = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.device.index != device:
+            raise ValueError(f"a tensor is on {t.device}, the current device is {device}")
+
+
+def _row(t):
+    """Pointer and stride of rows; one row's stride may be anything."""
+    return t.data_ptr(), (t.stride(0) if t.shape[0] > 1 else t.shape[1])
+
+
+class Pages:
+    """The pages of a cache on the device: table int32 [sequences, most pages of one], rows of any
+    stride; kv_len int32 [sequences]: rows that each holds; and for tg_pages the stack of free
+    pages, int32 [pages], whose first n_free (int32 [1]) are free."""
+
+    def __init__(self, table, kv_len, page_size: int, free=None, n_free=None):
+        import torch
+
+        _values(table, torch.int32, 2, "table")
+        self.n_seqs, self.max_pages = table.shape
+        _check(kv_len, torch.int32, (self.n_seqs,), "kv_len")
+        if (free is None) != (n_free is None):
+            raise ValueError("free and n_free: both or neither")
+        if free is not None:
+            _check(free, torch.int32, None, "free")
+            _check(n_free, torch.int32, (1,), "n_free")
+            if free.dim() != 1:
+                raise ValueError("free must be [pages]")
+        self.table, self.kv_len, self.page_size = table, kv_len, int(page_size)
+        self.free, self.n_free = free, n_free
+
+    @classmethod
+    def empty(cls, n_seqs: int, max_pages: int, n_pages: int, page_size: int, device="cuda"):
+        """No sequence holds a row, all pages are free; page 0 is taken first."""
+        import torch
+
+        make = dict(dtype=torch.int32, device=device)
+        return cls(torch.full((n_seqs, max_pages), -1, **make), torch.zeros(n_seqs, **make),
+                   page_size, torch.arange(n_pages - 1, -1, -1, **make),
+                   torch.full((1,), n_pages, **make))
+
+
+class PagesBuffers:
+    """Caller-owned results and scratch of tg_pages for n_tokens tokens."""
+
+    def __init__(self, pages: Pages, n_tokens: int, device="cuda"):
+        import torch
+
+        self.slot = torch.empty(n_tokens, dtype=torch.int64, device=device)
+        self.pos = torch.empty((n_tokens, 1), dtype=torch.int32, device=device)
+        self.refused = torch.empty(1, dtype=torch.int32, device=device)
+        ws = int(lib().tg_pages_workspace_bytes(pages.n_seqs, n_tokens))
+        self.workspace = torch.empty(max(ws, 16), dtype=torch.uint8, device=device)
+        self.workspace_bytes = ws
+
+
+def pages_args(pages: Pages, q_begin, bufs: PagesBuffers, release=None,
+               after: Pages | None = None) -> PagesArgs:
+    """q_begin int32 [sequences + 1], release int32 [sequences] or None. The lengths and the count
+    of free pages change in place, or go to those of `after`; table and stack always in place."""
+    import torch
+
+    if pages.free is None:
+        raise ValueError("pages has no stack of free pages")
+    after = pages if after is None else after
+    if (after.n_free is None or after.n_seqs != pages.n_seqs
+            or after.table.data_ptr() != pages.table.data_ptr()
+            or after.free.data_ptr() != pages.free.data_ptr()):
+        raise ValueError("after must have the table and the stack of pages")
+    _check(q_begin, torch.int32, (pages.n_seqs + 1,), "q_begin")
+    if release is not None:
+        _check(release, torch.int32, (pages.n_seqs,), "release")
+    _check(bufs.slot, torch.int64, None, "slot")
+    n_tokens = bufs.slot.shape[0]
+    _check(bufs.pos, torch.int32, (n_tokens, 1), "pos")
+    _check(bufs.refused, torch.int32, (1,), "refused")
+    _here(pages.table, pages.kv_len, pages.free, q_begin, release, bufs.slot, bufs.workspace,
+          after.kv_len, after.n_free)
+    a = PagesArgs()
+    a.q_begin = q_begin.data_ptr()
+    a.kv_len, a.kv_len_out = pages.kv_len.data_ptr(), after.kv_len.data_ptr()
+    a.release = release.data_ptr() if release is not None else None
+    a.table, a.table_stride = _row(pages.table)
+    a.free_pages = pages.free.data_ptr()
+    a.n_free, a.n_free_out = pages.n_free.data_ptr(), after.n_free.data_ptr()
+    a.slot, a.pos, a.refused = (bufs.slot.data_ptr(), bufs.pos.data_ptr(),
+                                bufs.refused.data_ptr())
+    a.n_seqs, a.n_tokens, a.n_pages = pages.n_seqs, n_tokens, pages.free.shape[0]
+    a.page_size, a.max_pages = pages.page_size, pages.max_pages
+    a.workspace, a.workspace_bytes = bufs.workspace.data_ptr(), bufs.workspace_bytes
+    a._keep = (pages, q_begin, bufs, release, after)  # the struct holds raw pointers: keep their owners alive
+    return a
+
+
+def pages_raw(args: PagesArgs, stream=None) -> int:
+    return int(lib().tg_pages(ctypes.byref(args), _stream_handle(stream)))
+
+
+def pages(pages: Pages, q_begin, bufs: PagesBuffers, release=None, after: Pages | None = None,
+          stream=None) -> None:
+    """Enqueue tg_pages: pages given back and taken, and a cache row for every new token, into
+    bufs.slot and bufs.pos."""
+    rc = pages_raw(pages_args(pages, q_begin, bufs, release, after), stream)
+    if rc != OK:
+        raise TgError("tg_pages", rc)
+
+
+class AttendPagesBuffers:
+    """Caller-owned scratch of tg_attend_pages for queries like q [sequences, heads, d] and a cache
+    like k [rows, kv heads, d]; no sequence has more than max_kv keys."""
+
+    def __init__(self, q, k, max_kv: int, device="cuda"):
+        import torch
+
+        self.max_kv = int(max_kv)
+        ws = int(lib().tg_attend_pages_workspace_bytes(q.shape[0], self.max_kv, q.shape[1],
+                                                       k.shape[1], q.shape[2]))
+        self.workspace = torch.empty(max(ws, 16), dtype=torch.uint8, device=device)
+        self.workspace_bytes = ws
+
+
+def attend_pages_args(q, k, v, pages: Pages, out, bufs: AttendPagesBuffers, scale: float,
+                      cap: float = 0.0, window: int = 0, slope=None) -> AttendPagesArgs:
+    """q and out [sequences, heads, d], k and v [cache rows, kv heads, d], any strides; whole pages
+    of cache rows count; slope float32 [heads]."""
+    import torch
+
+    dt = q.dtype
+    type_ = _type_of(dt)
+    _values(q, dt, 3, "q", (pages.n_seqs, *q.shape[1:]))
+    n_seqs, n_heads, d = q.shape
+    _values(k, dt, 3, "k")
+    rows, n_kv, _ = k.shape
+    if k.shape[2] != d:
+        raise ValueError(f"k must have heads of {d}")
+    _values(v, dt, 3, "v", k.shape)
+    _values(out, dt, 3, "out", q.shape)
+    if slope is not None:
+        _check(slope, torch.float32, (n_heads,), "slope")
+    if pages.page_size < 1:
+        raise ValueError("page_size must be positive")
+    _here(q, k, v, pages.table, pages.kv_len, out, bufs.workspace, slope)
+    a = AttendPagesArgs()
+    a.q, a.q_stride, a.q_head_stride = _rows(q)
+    a.k, a.k_stride, a.k_head_stride = _rows(k)
+    a.v, a.v_stride, a.v_head_stride = _rows(v)
+    a.out, a.out_stride, a.out_head_stride = _rows(out)
+    a.table, a.table_stride = _row(pages.table)
+    a.kv_len = pages.kv_len.data_ptr()
+    a.slope = slope.data_ptr() if slope is not None else None
+    a.scale, a.cap, a.window = float(scale), float(cap), int(window)
+    a.n_seqs, a.n_pages, a.page_size = n_seqs, rows // pages.page_size, pages.page_size
+    a.max_pages, a.max_kv_len = pages.max_pages, bufs.max_kv
+    a.n_heads, a.n_kv_heads, a.d, a.type = n_heads, n_kv, d, type_
+    a.workspace, a.workspace_bytes = bufs.workspace.data_ptr(), bufs.workspace_bytes
+    a._keep = (q, k, v, pages, out, bufs, slope)  # the struct holds raw pointers: keep their owners alive
+    return a
+
+
+def attend_pages_raw(args: AttendPagesArgs, stream=None) -> int:
+    return int(lib().tg_attend_pages(ctypes.byref(args), _stream_handle(stream)))
+
+
+def attend_pages(q, k, v, pages: Pages, out, bufs: AttendPagesBuffers, scale: float,
+                 cap: float = 0.0, window: int = 0, slope=None, stream=None) -> None:
+    """Enqueue tg_attend_pages: one query of each sequence over its pages, into out."""
+    rc = attend_pages_raw(attend_pages_args(q, k, v, pages, out, bufs, scale, cap, window, slope),
+                          stream)
+    if rc != OK:
+        raise TgError("tg_attend_pages", rc)
+
+
+def norm_args(x, x_out=None, h=None, y=None, y_norm: int = NORM_NONE, y_weight=None, y_bias=None,
+              gate=None, gate_row=None, x_scale: float = 1.0, y_scale: float = 1.0,
+              norm: int = NORM_RMS, weight=None, bias=None, eps: float = 1e-6) -> NormArgs:
+    """x, y, x_out, h [tokens, n], rows of any stride; weights and biases [n]; gate [gates, n],
+    rows of any stride; gate_row int32 [tokens]."""
+    import torch
+
+    dt = x.dtype
+    type_ = _type_of(dt)
+    _values(x, dt, 2, "x")
+    n_tokens, n = x.shape
+    for t, name in ((y, "y"), (x_out, "x_out"), (h, "h")):
+        if t is not None:
+            _values(t, dt, 2, name, x.shape)
+    for t, name in ((y_weight, "y_weight"), (y_bias, "y_bias"), (weight, "weight"),
+                    (bias, "bias")):
+        if t is not None:
+            _check(t, dt, (n,), name)
+    if gate is not None:
+        _values(gate, dt, 2, "gate", (gate.shape[0], n))
+    if gate_row is not None:
+        _check(gate_row, torch.int32, (n_tokens,), "gate_row")
+    _here(x, y, x_out, h, y_weight, y_bias, weight, bias, gate, gate_row)
+    a = NormArgs()
+    a.x, a.x_stride = _row(x)
+    if y is not None:
+        a.y, a.y_stride = _row(y)
+    if x_out is not None:
+        a.x_out, a.x_out_stride = _row(x_out)
+    if h is not None:
+        a.h, a.h_stride = _row(h)
+    if gate is not None:
+        (a.gate, a.gate_stride), a.n_gates = _row(gate), gate.shape[0]
+    for t, name in ((y_weight, "y_weight"), (y_bias, "y_bias"), (weight, "weight"),
+                    (bias, "bias"), (gate_row, "gate_row")):
+        if t is not None:
+            setattr(a, name, t.data_ptr())
+    a.y_norm, a.norm, a.eps = int(y_norm), int(norm), float(eps)
+    a.x_scale, a.y_scale = float(x_scale), float(y_scale)
+    a.n_tokens, a.n, a.type = n_tokens, n, type_
+    a._keep = (x, x_out, h, y, y_weight, y_bias, gate, gate_row, weight, bias)  # the struct holds raw pointers: keep their owners alive
+    return a
+
+
+def norm_raw(args: NormArgs, stream=None) -> int:
+    return int(lib().tg_norm(ctypes.byref(args), _stream_handle(stream)))
+
+
+def norm(x, x_out=None, h=None, y=None, y_norm: int = NORM_NONE, y_weight=None, y_bias=None,
+         gate=None, gate_row=None, x_scale: float = 1.0, y_scale: float = 1.0,
+         norm: int = NORM_RMS, weight=None, bias=None, eps: float = 1e-6, stream=None) -> None:
+    """Enqueue tg_norm: x_scale x + y_scale gate N_y(y) into x_out, and its norm into h."""
+    rc = norm_raw(norm_args(x, x_out, h, y, y_norm, y_weight, y_bias, gate, gate_row, x_scale,
+                            y_scale, norm, weight, bias, eps), stream)
+    if rc != OK:
+        raise TgError("tg_norm", rc)
+
+
+def quantize_args(x, q, scale) -> QuantizeArgs:
+    """x [rows, k] to q int8 [rows, k] and scale float32 [rows]; rows of any stride."""
+    import torch
+
+    type_ = _type_of(x.dtype)
+    _values(x, x.dtype, 2, "x")
+    _values(q, torch.int8, 2, "q", x.shape)
+    _check(scale, torch.float32, (x.shape[0],), "scale")
+    _here(x, q, scale)
+    a = QuantizeArgs()
+    a.x, a.x_stride = _row(x)
+    a.q, a.q_stride = _row(q)
+    a.scale = scale.data_ptr()
+    a.n_rows, a.k, a.type = x.shape[0], x.shape[1], type_
+    a._keep = (x, q, scale)  # the struct holds raw pointers: keep their owners alive
+    return a
+
+
+def quantize_raw(args: QuantizeArgs, stream=None) -> int:
+    return int(lib().tg_quantize(ctypes.byref(args), _stream_handle(stream)))
+
+
+def quantize(x, q, scale, stream=None) -> None:
+    """Enqueue tg_quantize: rows of x to 8-bit integers and a scale each."""
+    rc = quantize_raw(quantize_args(x, q, scale), stream)
+    if rc != OK:
+        raise TgError("tg_quantize", rc)
+
+
+def project_i8_args(x, x_scale, w, w_scale, y) -> ProjectI8Args:
+    """x int8 [tokens, k], w int8 [outputs, k], y [tokens, outputs], rows of any stride; x_scale
+    float32 [tokens], w_scale float32 [outputs]."""
+    import torch
+
+    _values(x, torch.int8, 2, "x")
+    n_tokens, k = x.shape
+    _values(w, torch.int8, 2, "w")
+    n = w.shape[0]
+    if w.shape[1] != k:
+        raise ValueError(f"w must have {k} columns")
+    type_ = _type_of(y.dtype)
+    _values(y, y.dtype, 2, "y", (n_tokens, n))
+    _check(x_scale, torch.float32, (n_tokens,), "x_scale")
+    _check(w_scale, torch.float32, (n,), "w_scale")
+    _here(x, x_scale, w, w_scale, y)
+    a = ProjectI8Args()
+    a.x, a.x_stride = _row(x)
+    a.w, a.w_stride = _row(w)
+    a.y, a.y_stride = _row(y)
+    a.x_scale, a.w_scale = x_scale.data_ptr(), w_scale.data_ptr()
+    a.n_tokens, a.k, a.n, a.type = n_tokens, k, n, type_
+    a._keep = (x, x_scale, w, w_scale, y)  # the struct holds raw pointers: keep their owners alive
+    return a
+
+
+def project_i8_raw(args: ProjectI8Args, stream=None) -> int:
+    return int(lib().tg_project_i8(ctypes.byref(args), _stream_handle(stream)))
+
+
+def project_i8(x, x_scale, w, w_scale, y, stream=None) -> None:
+    """Enqueue tg_project_i8: x w^T in 8-bit integers times the scales, into y."""
+    rc = project_i8_raw(project_i8_args(x, x_scale, w, w_scale, y), stream)
+    if rc != OK:
+        raise TgError("tg_project_i8", rc)
