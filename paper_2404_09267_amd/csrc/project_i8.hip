@@ -30,6 +30,7 @@ struct ProjectParams {
   int64_t x_stride, w_stride, y_stride;
   int32_t n_tokens, k, n;
   int32_t tiles_t, tiles_n;
+  int32_t whole;  // tiles of 256 x 256 that are taken whole
 };
 
 __device__ __forceinline__ i32x4 mfma(i32x4 a, i32x4 b, i32x4 c) {
@@ -60,48 +61,42 @@ __device__ __forceinline__ void put(const ProjectParams &P, int t, int n, i32x4 
 
 // ------------------------------------------------------------------------------ few tokens
 
+
 constexpr int kFewWaves = 8;
 
-// 16 kTt tokens x 16 outputs a workgroup; a wave takes every kFewWaves-th 256 values of k.
-template <int kType, int kTt>
+// 16 tokens x 16 outputs a workgroup; a wave takes every kFewWaves-th 512 values of k, all of whose
+// loads are under way at once.
+template <int kType>
 __global__ __launch_bounds__(kFewWaves * 64) void few_kernel(const ProjectParams P) {
-  constexpr int kAhead = 4;  // instructions' values of k that are loaded at once
-  __shared__ i32x4 s_sum[kFewWaves][kTt][64];
+  constexpr int kAhead = 8;  // instructions' values of k that are loaded at once
+  __shared__ i32x4 s_sum[kFewWaves][64];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int col = lane & 15, quad = lane >> 4;
   const int id = workgroup();
-  const int n0 = id % P.tiles_n * 16, t0 = id / P.tiles_n * 16 * kTt;
+  const int n0 = id % P.tiles_n * 16, t0 = id / P.tiles_n * 16;
   const int8_t *w = P.w + int64_t(min(n0 + col, P.n - 1)) * P.w_stride;
-  const int8_t *x[kTt];
-#pragma unroll
-  for (int i = 0; i < kTt; ++i) x[i] = P.x + int64_t(min(t0 + 16 * i + col, P.n_tokens - 1)) * P.x_stride;
-  i32x4 acc[kTt] = {};
+  const int8_t *x = P.x + int64_t(min(t0 + col, P.n_tokens - 1)) * P.x_stride;
+  i32x4 acc = {};
   for (int k0 = wave * 64 * kAhead; k0 < P.k; k0 += kFewWaves * 64 * kAhead) {
-    i32x4 wv[kAhead], xv[kAhead][kTt];
+    i32x4 wv[kAhead], xv[kAhead];
 #pragma unroll
     for (int a = 0; a < kAhead; ++a) {
       const int c = k0 + a * 64 + quad * 16;
       const bool in = c < P.k;
       wv[a] = in ? *reinterpret_cast<const i32x4 *>(w + c) : i32x4{};
-#pragma unroll
-      for (int i = 0; i < kTt; ++i)
-        xv[a][i] = in ? *reinterpret_cast<const i32x4 *>(x[i] + c) : i32x4{};
+      xv[a] = in ? *reinterpret_cast<const i32x4 *>(x + c) : i32x4{};
     }
 #pragma unroll
-    for (int a = 0; a < kAhead; ++a)
-#pragma unroll
-      for (int i = 0; i < kTt; ++i) acc[i] = mfma(wv[a], xv[a][i], acc[i]);
+    for (int a = 0; a < kAhead; ++a) acc = mfma(wv[a], xv[a], acc);
   }
-#pragma unroll
-  for (int i = 0; i < kTt; ++i) s_sum[wave][i][lane] = acc[i];
+  s_sum[wave][lane] = acc;
   __syncthreads();
-  for (int i = wave; i < kTt; i += kFewWaves) {
-    i32x4 sum = {};
+  if (wave > 0) return;
+  i32x4 sum = {};
 #pragma unroll
-    for (int v = 0; v < kFewWaves; ++v) sum += s_sum[v][i][lane];
-    put<kType>(P, t0 + 16 * i + col, n0 + 4 * quad, sum);
-  }
+  for (int v = 0; v < kFewWaves; ++v) sum += s_sum[v][lane];
+  put<kType>(P, t0 + col, n0 + 4 * quad, sum);
 }
 
 // ----------------------------------------------------------------------------- many tokens
@@ -112,43 +107,45 @@ __global__ __launch_bounds__(kFewWaves * 64) void few_kernel(const ProjectParams
 // behind the barrier at the end of it, since its operands are in registers by then. Rows of a
 // tile lie in LDS as 8 chunks of 16 bytes, in an order in which one chunk of 16 rows, which is
 // what the operands' reads ask for, falls on all banks.
+// Steps of 64 values with 4 or 5 of them under way are slower (25,600 x 4,096, k 4,096: 453 and 442
+// us for 411), 4 waves of 128 x 128 far slower (589).
 constexpr int kBK = 128;
 __device__ __forceinline__ int place_of(int row, int c) { return c ^ ((row >> 1) & 7); }
 
 // Which tile a workgroup takes: workgroups go round the 8 XCDs, so each XCD gets a run of tiles of
 // its own, in blocks of kGroup token tiles by all output tiles, whose operands its L2 shares.
 constexpr int kXcds = 8, kGroup = 4;
-__device__ __forceinline__ void tile_of(int id, int tiles_t, int tiles_n, int &tt, int &tn) {
-  const int total = tiles_t * tiles_n;
-  const int each = total / kXcds, more = total % kXcds, x = id % kXcds;
-  const int k = x * each + min(x, more) + id / kXcds;
+__device__ __forceinline__ void tile_at(int k, int tiles_t, int tiles_n, int &tt, int &tn) {
   const int per = kGroup * tiles_n, g = k / per, in = k - g * per;
   const int rows = min(kGroup, tiles_t - g * kGroup);
   tt = g * kGroup + in % rows;
   tn = in / rows;
 }
+__device__ __forceinline__ int run_of(int id, int total) {
+  const int each = total / kXcds, more = total % kXcds, x = id % kXcds;
+  return x * each + min(x, more) + id / kXcds;
+}
+
+template <int kT, int kN, int kStages>
+constexpr int kLds = kStages *(kT + kN) * kBK;
 
 template <int kType, int kT, int kN, int kWt, int kWn, int kStages>
-__global__ __launch_bounds__(kWt *kWn * 64, 2) void tile_kernel(const ProjectParams P) {
+__device__ __forceinline__ void tile(const ProjectParams &P, int t0, int n0, int8_t *lds) {
   constexpr int kWaves = kWt * kWn, kFt = kT / kWt / 16, kFn = kN / kWn / 16;
   constexpr int kChunks = kBK / 16, kRows = kT + kN, kPer = 64 / kChunks;  // rows of one load
   constexpr int kLoads = kRows / kPer / kWaves;
   static_assert(kLoads * kPer * kWaves == kRows && kT % kPer == 0, "whole loads");
   static_assert(kWaves * kPer % 16 == 0, "rows of one lane");
-  __shared__ __attribute__((aligned(16))) int8_t tile[kStages][kRows * kBK];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int col = lane & 15, quad = lane >> 4;
-  int tt, tn;
-  tile_of(blockIdx.x, P.tiles_t, P.tiles_n, tt, tn);
-  const int t0 = tt * kT, n0 = tn * kN;
   const int xr = min(kT, P.n_tokens - t0), wr = min(kN, P.n - n0);
   const auto xb =
       buffer(P.x + t0 * P.x_stride, static_cast<uint32_t>((xr - 1) * P.x_stride + P.k));
   const auto wb =
       buffer(P.w + n0 * P.w_stride, static_cast<uint32_t>((wr - 1) * P.w_stride + P.k));
   // load i of a wave covers kPer rows; rows past the tensor are not read. A lane's chunk is the
-  // same in all loads, since their rows are 4 kPer apart or more.
+  // same in all loads, since their rows are a multiple of 16 apart.
   const int chunk = place_of(wave * kPer + lane / kChunks, lane % kChunks);
   uint32_t at[kLoads];
 #pragma unroll
@@ -166,8 +163,8 @@ __global__ __launch_bounds__(kWt *kWn * 64, 2) void tile_kernel(const ProjectPar
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
       const int first = (i * kWaves + wave) * kPer;
-      load_lds(first < kT ? xb : wb, &tile[s % kStages][first * kBK], past ? kNowhere : at[i],
-               static_cast<uint32_t>(k0));
+      load_lds(first < kT ? xb : wb, lds + (s % kStages * kRows + first) * kBK,
+               past ? kNowhere : at[i], static_cast<uint32_t>(k0));
     }
   };
   i32x4 acc[kFn][kFt] = {};
@@ -176,7 +173,7 @@ __global__ __launch_bounds__(kWt *kWn * 64, 2) void tile_kernel(const ProjectPar
     i32x4 x[kFt], w[kFn];
   };
   auto read = [&](Operands &o, int s, int ks) {
-    const int8_t *m = tile[s % kStages];
+    const int8_t *m = lds + s % kStages * kRows * kBK;
 #pragma unroll
     for (int i = 0; i < kFt; ++i) {
       const int row = wt + 16 * i + col;
@@ -228,46 +225,88 @@ __global__ __launch_bounds__(kWt *kWn * 64, 2) void tile_kernel(const ProjectPar
       put<kType>(P, t0 + wt + 16 * i + col, n0 + wn + 16 * j + 4 * quad, acc[j][i]);
 }
 
+template <int kType, int kT, int kN, int kWt, int kWn, int kStages>
+__global__ __launch_bounds__(kWt *kWn * 64, 2) void tile_kernel(const ProjectParams P) {
+  __shared__ __attribute__((aligned(16))) int8_t lds[kLds<kT, kN, kStages>];
+  int tt, tn;
+  tile_at(run_of(blockIdx.x, P.tiles_t * P.tiles_n), P.tiles_t, P.tiles_n, tt, tn);
+  tile<kType, kT, kN, kWt, kWn, kStages>(P, tt * kT, tn * kN, lds);
+}
+
+// Tiles of 256 x 256, one a CU; those past the last whole round of the CUs by quarters, so that a round
+// of few tiles does not take as long as a whole one.
+template <int kType>
+__global__ __launch_bounds__(512, 2) void tile_and_rest_kernel(const ProjectParams P) {
+  __shared__ __attribute__((aligned(16))) int8_t lds[kLds<256, 256, 2>];
+  static_assert(kLds<128, 128, 4> <= kLds<256, 256, 2>, "one LDS for both");
+  int id = blockIdx.x, tt, tn;
+  if (id < P.whole) {
+    tile_at(run_of(id, P.whole), P.tiles_t, P.tiles_n, tt, tn);
+    return tile<kType, 256, 256, 2, 4, 2>(P, tt * 256, tn * 256, lds);
+  }
+  id -= P.whole;  // quarters of one tile on one XCD
+  const int k = P.whole + id % kXcds + id / (4 * kXcds) * kXcds, quarter = id / kXcds % 4;
+  if (k >= P.tiles_t * P.tiles_n) return;
+  tile_at(k, P.tiles_t, P.tiles_n, tt, tn);
+  const int t0 = tt * 256 + quarter % 2 * 128, n0 = tn * 256 + quarter / 2 * 128;
+  if (t0 < P.n_tokens && n0 < P.n) tile<kType, 128, 128, 2, 4, 4>(P, t0, n0, lds);
+}
+
 // ------------------------------------------------------------------------------- the host
+
+constexpr int kCus = 256;
+
+// Tiles of 256 x 256 past the whole rounds, where quarters of them fit the CUs.
+int64_t rest_of(int64_t tiles) {
+  const int64_t rest = tiles % kCus;
+  return tiles > kCus && rest <= kCus / 4 ? rest : 0;
+}
 
 template <int kType, int kT, int kN, int kWt, int kWn, int kStages>
 int launch_tiles(ProjectParams P, hipStream_t s) {
   const int64_t tiles_t = (int64_t(P.n_tokens) + kT - 1) / kT;
   const int64_t tiles_n = (int64_t(P.n) + kN - 1) / kN;
-  const int64_t blocks = tiles_t * tiles_n;
+  int64_t blocks = tiles_t * tiles_n;
+  constexpr bool kRest = kT == 256 && kN == 256;
+  const int64_t rest = kRest ? rest_of(blocks) : 0;
+  P.whole = static_cast<int32_t>(std::min<int64_t>(blocks - rest, INT32_MAX));
+  if (rest > 0) blocks += (rest + kXcds - 1) / kXcds * kXcds * 4 - rest;
   // threads that a launch takes in one direction
   if (blocks * (kWt * kWn * 64) >= int64_t(1) << 32) return TG_E_INVAL;
   P.tiles_t = static_cast<int32_t>(tiles_t);
   P.tiles_n = static_cast<int32_t>(tiles_n);
-  hipLaunchKernelGGL((tile_kernel<kType, kT, kN, kWt, kWn, kStages>),
-                     dim3(static_cast<uint32_t>(blocks)), dim3(kWt * kWn * 64), 0, s, P);
+  const dim3 grid(static_cast<uint32_t>(blocks)), threads(kWt * kWn * 64);
+  if constexpr (kRest)
+    hipLaunchKernelGGL(tile_and_rest_kernel<kType>, grid, threads, 0, s, P);
+  else
+    hipLaunchKernelGGL((tile_kernel<kType, kT, kN, kWt, kWn, kStages>), grid, threads, 0, s, P);
   return hipGetLastError() == hipSuccess ? TG_OK : TG_E_HIP;
 }
 
-template <int kType, int kTt>
+template <int kType>
 int launch_few(ProjectParams P, hipStream_t s) {
-  const int64_t tiles_t = (int64_t(P.n_tokens) + 16 * kTt - 1) / (16 * kTt);
+  const int64_t tiles_t = (int64_t(P.n_tokens) + 15) / 16;
   P.tiles_n = static_cast<int32_t>((int64_t(P.n) + 15) / 16);
   if (tiles_t * P.tiles_n > kMaxWorkgroups) return TG_E_INVAL;
-  hipLaunchKernelGGL((few_kernel<kType, kTt>), grid_of(tiles_t * P.tiles_n, kFewWaves * 64),
+  hipLaunchKernelGGL(few_kernel<kType>, grid_of(tiles_t * P.tiles_n, kFewWaves * 64),
                      dim3(kFewWaves * 64), 0, s, P);
   return hipGetLastError() == hipSuccess ? TG_OK : TG_E_HIP;
 }
 
-constexpr int kFewTokens = 64;
-
 template <int kType>
 int launch(const ProjectParams &P, hipStream_t s) {
-  if (P.n_tokens <= 16) return launch_few<kType, 1>(P, s);
-  if (P.n_tokens <= 32) return launch_few<kType, 2>(P, s);
-  if (P.n_tokens <= kFewTokens) return launch_few<kType, 4>(P, s);
+  const int64_t weights = int64_t(P.n) * P.k;
+  if ((P.n_tokens <= 16 && weights <= 1 << 25) || (P.n_tokens <= 64 && weights <= 1 << 21))
+    return launch_few<kType>(P, s);
   const auto tiles = [&](int t, int n) {
     return ((int64_t(P.n_tokens) + t - 1) / t) * ((int64_t(P.n) + n - 1) / n);
   };
-  if (tiles(128, 128) > 256) {
+  if (tiles(128, 128) > kCus) {
     const auto rounds = [&](int t, int n, int at_once) { return (tiles(t, n) + at_once - 1) / at_once; };
-    const int64_t c256 = 164 * rounds(256, 256, 256), c192 = 137 * rounds(192, 256, 256);
-    const int64_t c160 = 118 * rounds(160, 128, 512), c128 = 100 * rounds(128, 128, 512);
+    const int64_t t256 = tiles(256, 256);
+    const int64_t c256 = 160 * ((t256 - rest_of(t256) + kCus - 1) / kCus) + (rest_of(t256) ? 70 : 0);
+    const int64_t c192 = 128 * rounds(192, 256, kCus);
+    const int64_t c160 = 113 * rounds(160, 128, 2 * kCus), c128 = 100 * rounds(128, 128, 2 * kCus);
     const int64_t least = std::min(std::min(c256, c192), std::min(c160, c128));
     if (c256 == least) return launch_tiles<kType, 256, 256, 2, 4, 2>(P, s);
     if (c192 == least) return launch_tiles<kType, 192, 256, 4, 2, 2>(P, s);
@@ -275,8 +314,9 @@ int launch(const ProjectParams &P, hipStream_t s) {
     return launch_tiles<kType, 128, 128, 2, 2, 2>(P, s);
   }
   if (tiles(128, 128) >= 160) return launch_tiles<kType, 128, 128, 2, 4, 4>(P, s);
-  if (tiles(64, 64) > 256) return launch_tiles<kType, 128, 64, 2, 2, 3>(P, s);
-  return launch_tiles<kType, 64, 64, 2, 2, 4>(P, s);
+  if (tiles(64, 64) > kCus) return launch_tiles<kType, 128, 64, 2, 2, 3>(P, s);
+  if (tiles(64, 64) > kCus / 2) return launch_tiles<kType, 64, 64, 2, 4, 4>(P, s);
+  return launch_tiles<kType, 64, 32, 2, 2, 4>(P, s);
 }
 
 }  // namespace
