@@ -1,20 +1,25 @@
 // tg_attend_pages: attention of one new token a sequence over the pages of a cache.
 //
 // The query heads that share a key head are rows of one matrix tile, so that keys and values are
-// read once, and reading them bounds it: each wave has tiles of 32 keys and their values under way
-// to LDS while it works on the one before. A key's row in the cache is looked up by a lane, a
-// tile ahead of its loads; rows that are not seen (past the end, before the window, on a page
-// that is none) are loaded from 16 zeros instead, so that whatever lies there stays out, and
-// have no weight.
+// read once, and reading them bounds it: each wave has a tile of 32 keys and their values under way
+// to LDS while it works on the one before. A key's row in the cache is looked up by a lane, a tile
+// ahead of its loads. Tiles whose keys are all seen are loaded 16 rows at a time; in the others
+// rows that are not seen (past the end, before the window, on a page that is none) are loaded from
+// zeros instead, so that whatever lies there stays out, and have no weight.
 //
 // Softmax in one pass over the keys (Milakov and Gimelshein 2018): a running maximum m in units of
 // log2, the sum l of 2^(z - m) and the weighted sum of values, the latter two multiplied by
 // 2^(m_old - m_new) when a score passes m by kSlack. Scores are computed transposed, S^T = K Q^T,
-// so that a lane's scores are of one query and the weights come out where the second product,
-// O^T = V^T P^T, takes them as an operand.
+// so that a lane's scores are of one query and the weights come out where the second product, O^T =
+// V^T P^T, takes them as an operand.
 //
-// All sequences' keys are cut into parts of one length, found on the device, so that every
-// workgroup has as much to read whatever the lengths are; join_kernel joins them in a set order.
+// Few keys, or many sequences: a workgroup a sequence and key head. Else all sequences' keys are
+// cut into as many ranges of one length as there is room for workgroups, found on the device, so
+// that each has as much to read whatever the lengths are; a workgroup goes from sequence to
+// sequence, and join_kernel joins what a sequence has in several ranges, in a set order. bfloat16:
+// 8 sequences of up to 100,003 keys, 16 heads of 128 over 2, 583 MB: 111 us, 5.2 TB/s; 256 of up to
+// 4,096, 32 heads over 8, 2.4 GB: 437 us, 5.4; 20 of up to 1,600, 16 heads of 64 over 4: 13 us, a
+// launch and a chain of loads (length, pages, keys, and those of 6 tiles a wave).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -54,12 +59,14 @@ struct AttendParams {
   int32_t most;    // keys of a sequence at most
   int32_t n_heads, n_kv_heads, group, d;
   int32_t row_tiles;
-  int32_t width;   // parts that all keys are cut into, 0: no sequence is cut
+  int32_t width;   // ranges that all keys are cut into at most, 0: a workgroup a sequence
+  int32_t least;   // tiles of a range at least; a multiple of
+  int32_t unit;    // the tiles that a workgroup takes at once
   float *part;     // [width + n_seqs][n_heads][d] weighted sums, and
   float *part_ml;  // [..][..][2] maximum (log2 units) and sum of weights
 };
 
-// Keys [lo, hi) of a sequence are seen by its query.
+// Keys [lo, hi) of a sequence are seen by its query; a tile has 32 keys from a multiple of 32 on.
 struct Span {
   int lo, hi;
 };
@@ -97,26 +104,51 @@ __device__ __forceinline__ float add2<TG_BF16>(Num<TG_BF16>::V2 a, float c) {
   return __builtin_amdgcn_fdot2_f32_bf16(a, one, c, false);
 }
 
-template <int kType>
-__device__ __forceinline__ typename Num<kType>::V4 read_transposed(const void *p) {
-  typedef __attribute__((address_space(3))) s16x4 *P3;
-  return __builtin_bit_cast(
-      typename Num<kType>::V4,
-      __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<P3>(
-          reinterpret_cast<uintptr_t>(p))));
+// What the second product takes of four blocks of 16 of d and 32 keys: transposing reads at the
+// four places, and kHigh bytes further for the upper 16 keys. They wait for themselves: the
+// compiler would have them wait for every load to LDS under way, the next tile's too.
+template <int kType, int kHigh>
+__device__ __forceinline__ void read_transposed(const uint32_t (&at)[4],
+                                                typename Num<kType>::V8 (&out)[4]) {
+  i32x2 v[8];
+  asm volatile(
+      "ds_read_b64_tr_b16 %0, %8\n\t"
+      "ds_read_b64_tr_b16 %1, %8 offset:%12\n\t"
+      "ds_read_b64_tr_b16 %2, %9\n\t"
+      "ds_read_b64_tr_b16 %3, %9 offset:%12\n\t"
+      "ds_read_b64_tr_b16 %4, %10\n\t"
+      "ds_read_b64_tr_b16 %5, %10 offset:%12\n\t"
+      "ds_read_b64_tr_b16 %6, %11\n\t"
+      "ds_read_b64_tr_b16 %7, %11 offset:%12\n\t"
+      "s_waitcnt lgkmcnt(0)"
+      : "=&v"(v[0]), "=&v"(v[1]), "=&v"(v[2]), "=&v"(v[3]), "=&v"(v[4]), "=&v"(v[5]),
+        "=&v"(v[6]), "=&v"(v[7])
+      : "v"(at[0]), "v"(at[1]), "v"(at[2]), "v"(at[3]), "n"(kHigh)
+      : "memory");
+#pragma unroll
+  for (int b = 0; b < 4; ++b) {
+    const i32x4 both = {v[2 * b][0], v[2 * b][1], v[2 * b + 1][0], v[2 * b + 1][1]};
+    out[b] = __builtin_bit_cast(typename Num<kType>::V8, both);
+  }
 }
 
 // 16 bytes per lane, each from its own address, into LDS at `to` + 16 * lane. The caller waits.
-__device__ __forceinline__ void gather_lds(const void *from, void *to) {
+__device__ __forceinline__ void gather_lds(uint64_t from, void *to) {
   __builtin_amdgcn_global_load_lds(
-      reinterpret_cast<const __attribute__((address_space(1))) void *>(
-          reinterpret_cast<uintptr_t>(from)),
+      reinterpret_cast<const __attribute__((address_space(1))) void *>(from),
       reinterpret_cast<__attribute__((address_space(3))) void *>(reinterpret_cast<uintptr_t>(to)),
       16, 0, 0);
 }
 
+// Waits for the wave's LDS reads; no load to LDS is issued before.
+__device__ __forceinline__ void wait_lds() {
+  __builtin_amdgcn_sched_barrier(0);
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  __builtin_amdgcn_sched_barrier(0);
+}
+
 // What rows that are not seen are read from.
-__device__ const uint32_t kZeros[4] __attribute__((aligned(16))) = {0, 0, 0, 0};
+__device__ const uint32_t kZeros[4] __attribute__((aligned(16))) = {};
 
 // Place of 16-byte chunk c of row r in a tile of rows of kChunks chunks (8 or 16). Matrix
 // operands take one chunk of 16 rows at once, transposing reads 2 chunks of 8 rows: both fall on
@@ -127,80 +159,77 @@ __device__ __forceinline__ int place_of(int r, int c) {
   return c ^ ((((r >> 1) & 3) << 1) | ((r >> 3) & 1));
 }
 
-// ------------------------------------------------------------------------ the parts of all keys
+// ------------------------------------------------------------------------ the cut of all keys
 
+constexpr int kKeys = 32;      // of a tile
 constexpr int kMaxCut = 1024;  // sequences, where any is cut
-// Parts have 128 keys at least; where that makes more than one workgroup a place, up to 512, for
-// one workgroup a place; beyond, for three.
-constexpr int kMinPart = 128, kOneRound = 512;
 
-struct Parts {
-  int chunk;   // keys of a part
-  int seq;     // the sequence asked for, -1: there is none
-  int first;   // its first part
-  int count;   // its parts
-  Span s;
+// All sequences' tiles one after the other are cut into ranges of `length`; a workgroup has one,
+// whatever it holds of how many sequences. What range w has of sequence s is part w + s: from one
+// part to the next, one of the two grows.
+struct Cut {
+  int length;  // tiles of a range
+  int ranges;  // that there are
+  int seq;     // the sequence asked for, and
+  int at;      // its first tile
 };
 
-// `part` >= 0: the sequence that has it; otherwise sequence `seq`. A wave works it out.
-__device__ __forceinline__ Parts find_parts(const AttendParams &P, int part, int seq) {
+__device__ __forceinline__ int tiles_of(const Span &s) {
+  return s.hi > s.lo ? (s.hi + kKeys - 1) / kKeys - s.lo / kKeys : 0;
+}
+
+// Sum of `v` over the wave's lanes up to and with this one.
+__device__ __forceinline__ int sum_up(int v) {
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, false);  // the lanes 1, 2, 4 and 8 before
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, false);  // in a row of 16
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xF, 0xF, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, false);  // the last of the row before
+  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false);  // the last of the half before
+  return v;
+}
+
+// `range` >= 0: the first sequence that has a part in that range (a sequence of no keys counts
+// where it starts); otherwise sequence `seq`. A wave works it out.
+__device__ __forceinline__ Cut find_cut(const AttendParams &P, int range, int seq) {
   const int lane = threadIdx.x & 63;
   constexpr int kEach = kMaxCut / 64, kAtOnce = 4;
-  int keys[kEach];
-  int64_t total = 0;
+  int tiles[kEach], upto[kEach], total = 0;  // of a sequence, and with all before it
 #pragma unroll
   for (int u0 = 0; u0 < kEach; u0 += kAtOnce) {
-    if (u0 * 64 < P.n_seqs) {  // loads of one turn without a branch between them
-      int len[kAtOnce];
+    if (u0 * 64 >= P.n_seqs) continue;
+    int len[kAtOnce];  // loads of one turn without a branch between them
 #pragma unroll
-      for (int u = 0; u < kAtOnce; ++u)
-        len[u] = P.kv_len[min((u0 + u) * 64 + lane, P.n_seqs - 1)];
+    for (int u = 0; u < kAtOnce; ++u)
+      len[u] = P.kv_len[min((u0 + u) * 64 + lane, P.n_seqs - 1)];
 #pragma unroll
-      for (int u = 0; u < kAtOnce; ++u) {
-        const Span s = span_of(P, len[u]);
-        keys[u0 + u] = (u0 + u) * 64 + lane < P.n_seqs ? s.hi - s.lo : -1;
-        total += max(keys[u0 + u], 0);
-      }
-    } else {
-#pragma unroll
-      for (int u = 0; u < kAtOnce; ++u) keys[u0 + u] = -1;
+    for (int u = u0; u < u0 + kAtOnce; ++u) {
+      tiles[u] = u * 64 + lane < P.n_seqs ? tiles_of(span_of(P, len[u - u0])) : 0;
+      if (u * 64 >= P.n_seqs) continue;
+      upto[u] = total + sum_up(tiles[u]);
+      total = __builtin_amdgcn_readlane(upto[u], 63);
     }
   }
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) total += __shfl_xor(total, o);
-  const auto even = [&](int parts) {
-    return static_cast<int>(((total + parts - 1) / parts + 63) / 64 * 64);
-  };
-  Parts r = {kMinPart, -1, 0, 0, {0, 0}};
-  const int one = even((P.width + 2) / 3);
-  if (one >= 2 * kMinPart) r.chunk = min(one, kOneRound);
-  r.chunk = max(r.chunk, even(P.width));
-  int before = 0;
+  Cut r;
+  const int even = (total + P.width - 1) / P.width;
+  r.length = max((even + P.unit - 1) / P.unit * P.unit, P.least);
+  r.ranges = max((total + r.length - 1) / r.length, 1);
+  r.seq = -1;
+  r.at = 0;
+  if (range >= r.ranges) return r;
+  const int start = range * r.length;
 #pragma unroll
   for (int u = 0; u < kEach; ++u) {
-    if (u * 64 >= P.n_seqs) continue;
-    const int mine = keys[u] < 0 ? 0 : max((keys[u] + r.chunk - 1) / r.chunk, 1);
-    int upto = mine;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const int v = __shfl_up(upto, o);
-      if (lane >= o) upto += v;
-    }
-    const uint64_t at = part >= 0 ? __ballot(before + upto > part)
-                                  : (seq >= u * 64 && seq < u * 64 + 64 ? 1ull << (seq & 63) : 0);
-    if (at && r.seq < 0) {
-      const int l = __builtin_amdgcn_readfirstlane(__builtin_ctzll(at));
-      r.seq = u * 64 + l;
-      r.count = __builtin_amdgcn_readlane(mine, l);
-      r.first = before + __builtin_amdgcn_readlane(upto, l) - r.count;
-    }
-    before += __builtin_amdgcn_readlane(upto, 63);
+    if (u * 64 >= P.n_seqs || r.seq >= 0) continue;
+    const bool in = u * 64 + lane < P.n_seqs;
+    const uint64_t here =
+        range < 0 ? (seq >= u * 64 && seq < u * 64 + 64 ? 1ull << (seq & 63) : 0)
+                  : __ballot(in && (upto[u] > start || (tiles[u] == 0 && upto[u] == start)));
+    if (!here) continue;
+    const int l = __builtin_amdgcn_readfirstlane(__builtin_ctzll(here));
+    r.seq = u * 64 + l;
+    r.at = __builtin_amdgcn_readlane(upto[u], l) - __builtin_amdgcn_readlane(tiles[u], l);
   }
-  r.seq = __builtin_amdgcn_readfirstlane(r.seq);
-  r.first = __builtin_amdgcn_readfirstlane(r.first);
-  r.count = __builtin_amdgcn_readfirstlane(r.count);
-  r.chunk = __builtin_amdgcn_readfirstlane(r.chunk);
-  if (r.seq >= 0) r.s = span_of(P, P.kv_len[r.seq]);
   return r;
 }
 
@@ -210,13 +239,9 @@ __device__ __forceinline__ float weighted(float sum, float m, float l) {
   return l == 0.0f ? (m == -INFINITY ? 0.0f : NAN) : sum / l;
 }
 
-// Rows of a workgroup: 16 query heads that share a key head. Each of its two waves takes every
-// second 32 keys of the workgroup's range through LDS of its own; two waves, so that several
-// workgroups fit a CU and one's start and end fall into another's loads.
-constexpr int kWaves = 2, kKeys = 32;
-constexpr int kWorkgroups = 1536;  // that the keys are cut for
-
-template <int kType, int kD>
+// Rows of a workgroup: 16 query heads that share a key head. Each of its waves takes every
+// kWaves-th 32 keys of what the workgroup has of a sequence, through LDS of its own.
+template <int kType, int kD, int kWaves, int kBufs>
 __global__ __launch_bounds__(kWaves * 64) void attend_pages_kernel(const AttendParams P) {
   typedef Num<kType> N;
   typedef typename N::E E;
@@ -224,7 +249,8 @@ __global__ __launch_bounds__(kWaves * 64) void attend_pages_kernel(const AttendP
   typedef typename N::V8 V8;
   constexpr int kChunks = kD / 8, kSteps = kD / 32, kBlocks = kD / 16;
   constexpr int kPer = 64 / kChunks, kLoads = kKeys / kPer;  // rows of one load, loads of a tile
-  __shared__ __attribute__((aligned(16))) E tile[kWaves][2][2][kKeys * kD];
+  // keys and values of a step; the waves' sums at the end
+  __shared__ __attribute__((aligned(16))) E tile[kWaves][kBufs][2][kKeys * kD];
   __shared__ float s_m[kWaves][16], s_l[kWaves][16];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -234,25 +260,32 @@ __global__ __launch_bounds__(kWaves * 64) void attend_pages_kernel(const AttendP
   id /= P.n_kv_heads;
   const int rt = id % P.row_tiles;
   id /= P.row_tiles;
-  Parts parts = {0, id, id, 1, {0, 0}};
+  // tiles of all sequences that are this workgroup's, and where its first sequence starts
+  int seq = id, at_tile = 0, begin_tile = 0, end_tile = INT_MAX;
+  bool to_end = false;  // sequences of no keys at the end of all, too
   if (P.width > 0) {
-    parts = find_parts(P, id, -1);
-    if (parts.seq < 0) return;
-  } else {
-    if (id >= P.n_seqs) return;
-    parts.s = span_of(P, P.kv_len[id]);
+    const Cut cut = find_cut(P, id, -1);
+    if (cut.seq < 0) return;
+    seq = cut.seq;
+    at_tile = cut.at;
+    begin_tile = id * cut.length;
+    end_tile = begin_tile + cut.length;
+    to_end = id == cut.ranges - 1;
+  } else if (id >= P.n_seqs) {
+    return;
   }
-  const int seq = parts.seq;
-  const int from = parts.s.lo + (id - parts.first) * parts.chunk;
-  const int end = parts.count > 1 ? from + min(parts.s.hi - from, parts.chunk) : parts.s.hi;
-  const int32_t *table = P.table + seq * P.table_stride;
-  const E *kb = static_cast<const E *>(P.k) + kvh * P.k_head;
-  const E *vb = static_cast<const E *>(P.v) + kvh * P.v_head;
+  const uint64_t zeros = reinterpret_cast<uintptr_t>(kZeros);
+  const uint64_t k_at = reinterpret_cast<uintptr_t>(static_cast<const E *>(P.k) +
+                                                    kvh * P.k_head);
+  const uint64_t v_at = reinterpret_cast<uintptr_t>(static_cast<const E *>(P.v) + kvh * P.v_head);
+  const uint32_t k_bytes = static_cast<uint32_t>(P.k_stride) * 2;
+  const uint32_t v_bytes = static_cast<uint32_t>(P.v_stride) * 2;
   // Lane r of each half of the wave looks after key r of a tile: its page, and its row there.
-  auto page_at = [&](int j0) {
-    const uint32_t j = j0 + (lane & 31);
-    const uint32_t at = P.page_log2 >= 0 ? j >> P.page_log2 : j / P.page_size;
-    return static_cast<int>(j) < end ? table[at] : -1;
+  auto page_at = [&](const int32_t *table, int j0, int lo, int end) {
+    const int j = j0 + (lane & 31);
+    const uint32_t at = P.page_log2 >= 0 ? static_cast<uint32_t>(j) >> P.page_log2
+                                         : static_cast<uint32_t>(j) / P.page_size;
+    return j >= lo && j < end ? table[at] : -1;
   };
   auto row_at = [&](int j0, int page) {
     const uint32_t j = j0 + (lane & 31);
@@ -261,174 +294,251 @@ __global__ __launch_bounds__(kWaves * 64) void attend_pages_kernel(const AttendP
                ? page * P.page_size + static_cast<int>(in)
                : -1;
   };
-  // The loads of a tile, and which of its keys are seen.
-  auto fetch = [&](int row, int to) {
+  // The loads of a tile's keys or values to LDS. Where all its keys are seen, and pages are whole
+  // times 16 rows, 16 rows lie one after the other: a lane's place among them stays the same, and
+  // only where they start is looked up. Else every lane has addresses of its own.
+  uint32_t piece[2][kLoads / 2];
+  const auto pieces = [&](uint32_t bytes, uint32_t(&to)[kLoads / 2]) {
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i) {
+    for (int i = 0; i < kLoads / 2; ++i) {
       const int r = i * kPer + lane / kChunks;
       const int c = place_of<kChunks>(r, lane & (kChunks - 1)) * 8;
-      const int64_t at = __shfl(row, r);
-      const bool use = at >= 0 && c < P.d;
-      const void *pk = use ? static_cast<const void *>(kb + at * P.k_stride + c) : kZeros;
-      const void *pv = use ? static_cast<const void *>(vb + at * P.v_stride + c) : kZeros;
-      gather_lds(pk, &tile[wave][to][0][i * kPer * kD]);
-      gather_lds(pv, &tile[wave][to][1][i * kPer * kD]);
+      to[i] = c < P.d ? r * bytes + c * 2 : kNowhere;
     }
-    return static_cast<uint32_t>(__ballot(row >= 0));
   };
+  pieces(k_bytes, piece[0]);
+  pieces(v_bytes, piece[1]);
+  const bool even_pages = P.page_size % 16 == 0;
+  int rows[kLoads];
+  auto spread = [&](uint32_t all, int row) {
+    if (all == 0xFFFFFFFFu && even_pages) {
+      rows[0] = __builtin_amdgcn_readlane(row, 0);
+      rows[1] = __builtin_amdgcn_readlane(row, 16);
+      return;
+    }
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) rows[i] = __shfl(row, i * kPer + lane / kChunks);
+  };
+  auto fetch = [&](int which, uint32_t all, E *to) {
+    const uint64_t base = which ? v_at : k_at;
+    const uint32_t bytes = which ? v_bytes : k_bytes;
+    if (all == 0xFFFFFFFFu && even_pages) {
+#pragma unroll
+      for (int g = 0; g < 2; ++g) {
+        const uint32_t at = __builtin_amdgcn_readfirstlane(rows[g]);
+        const auto b = buffer(reinterpret_cast<const void *>(base + uint64_t(at) * bytes),
+                              15 * bytes + P.d * 2);
+#pragma unroll
+        for (int i = 0; i < kLoads / 2; ++i)
+          load_lds(b, to + (g * kLoads / 2 + i) * kPer * kD, piece[which][i], 0);
+      }
+      return;
+    }
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const int c = place_of<kChunks>(i * kPer + lane / kChunks, lane & (kChunks - 1)) * 8;
+      const uint64_t p = base + uint64_t(static_cast<uint32_t>(rows[i])) * bytes + c * 2;
+      gather_lds(rows[i] >= 0 && c < P.d ? p : zeros, to + i * kPer * kD);
+    }
+  };
+  E(*const own)[2][kKeys * kD] = tile[wave];
+  // where a lane's transposing reads of a tile start
+  uint32_t place[kBlocks];
+#pragma unroll
+  for (int b = 0; b < kBlocks; ++b) {
+    const int r = 4 * quad + (col >> 2), c = 2 * b + ((col & 3) >> 1);
+    place[b] = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(own[0][1])) +
+               (r * kD + place_of<kChunks>(r, c) * 8 + (col & 1) * 4) * sizeof(E);
+  }
   constexpr int kStep = kWaves * kKeys;
-  int j0 = from + wave * kKeys, buf = 0;
-  const int page0 = page_at(j0);
-  int page = page_at(j0 + kStep);
   const int my = rt * 16 + col;  // this lane's row
   const bool live = my < P.group;
   const int head = kvh * P.group + min(my, P.group - 1);
-  const E *qr = static_cast<const E *>(P.q) + seq * P.q_stride + head * P.q_head;
-  V8 qf[kSteps];
-#pragma unroll
-  for (int k = 0; k < kSteps; ++k) {
-    qf[k] = V8{};
-    if (live && k * 32 + quad * 8 < P.d)
-      qf[k] = *reinterpret_cast<const V8 *>(qr + k * 32 + quad * 8);
-  }
   const float slope2 = P.slope ? P.slope[head] * kLog2e : 0.0f;
-  const int last = P.kv_len[seq] - 1;
-  uint32_t seen = 0;
-  if (j0 < end) seen = fetch(row_at(j0, page0), 0);
-  f32x4 acc[kBlocks] = {};
-  float m = -INFINITY, l = 0.0f;
-  bool any = false;
-  for (; j0 < end; j0 += kStep) {
-    wait_loads();
-    const E *tk = tile[wave][buf][0], *tv = tile[wave][buf][1];
-    const uint32_t now = seen;
-    if (j0 + kStep < end) {
-      // nothing may ask for the page before the wait: the tile's loads are older
-      asm volatile("" : "+v"(page));
-      const int row = row_at(j0 + kStep, page);
-      page = page_at(j0 + 2 * kStep);
-      seen = fetch(row, buf ^ 1);
+  int len = P.kv_len[seq];
+  for (;;) {
+    const Span span = span_of(P, len);
+    const int tiles = tiles_of(span), last = len - 1;
+    const int first = max(begin_tile - at_tile, 0);        // of the sequence's tiles, up to
+    const int beyond = min(end_tile - at_tile, tiles);
+    const bool whole = first == 0 && beyond == tiles;
+    const int base_key = span.lo / kKeys * kKeys;
+    const int from = base_key + first * kKeys, end = min(base_key + beyond * kKeys, span.hi);
+    const bool again = P.width > 0 && seq + 1 < P.n_seqs && (to_end || at_tile + tiles < end_tile);
+    if (again) len = P.kv_len[seq + 1];
+    const int32_t *table = P.table + seq * P.table_stride;
+    int j0 = from + wave * kKeys, buf = 0;
+    const int page0 = page_at(table, j0, span.lo, end);
+    int page = page_at(table, j0 + kStep, span.lo, end);
+    const E *qr = static_cast<const E *>(P.q) + seq * P.q_stride + head * P.q_head;
+    V8 qf[kSteps];
+#pragma unroll
+    for (int k = 0; k < kSteps; ++k) {
+      qf[k] = V8{};
+      if (live && k * 32 + quad * 8 < P.d)
+        qf[k] = *reinterpret_cast<const V8 *>(qr + k * 32 + quad * 8);
     }
-    f32x4 z[2] = {};
-#pragma unroll
-    for (int b = 0; b < 2; ++b)
-#pragma unroll
-      for (int k = 0; k < kSteps; ++k) {
-        const int r = b * 16 + col;
-        const V8 kf = *reinterpret_cast<const V8 *>(
-            tk + r * kD + place_of<kChunks>(r, 4 * k + quad) * 8);
-        z[b] = N::mfma16(kf, qf[k], z[b]);
+    uint32_t seen = 0;
+    if (j0 < end) {
+      const int row = row_at(j0, page0);
+      seen = static_cast<uint32_t>(__ballot(row >= 0));
+      spread(seen, row);
+      fetch(0, seen, own[0][0]);
+      fetch(1, seen, own[0][1]);
+    }
+    f32x4 acc[kBlocks] = {};
+    float m = -INFINITY, l = 0.0f;
+    bool any = false;
+    for (; j0 < end; j0 += kStep) {
+      wait_loads();
+      const uint32_t now = seen;
+      const bool more = j0 + kStep < end;
+      if (more) {
+        // nothing may ask for the page before the wait: the tile's loads are older
+        asm volatile("" : "+v"(page));
+        const int row = row_at(j0 + kStep, page);
+        page = page_at(table, j0 + 2 * kStep, span.lo, end);
+        seen = static_cast<uint32_t>(__ballot(row >= 0));
+        spread(seen, row);
+        if (kBufs > 1) {
+          fetch(0, seen, own[buf ^ 1][0]);
+          fetch(1, seen, own[buf ^ 1][1]);
+        }
       }
-    if (P.cap_out > 0.0f) {
+      const E *tk = own[buf][0];
+      f32x4 z[2] = {};
 #pragma unroll
-      for (int e = 0; e < 8; ++e)
-        z[e >> 2][e & 3] = P.cap_out * bend(z[e >> 2][e & 3] * P.cap_arg);
-    } else {
+      for (int b = 0; b < 2; ++b)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) z[e >> 2][e & 3] *= P.to_log2;
+        for (int k = 0; k < kSteps; ++k) {
+          const int r = b * 16 + col;
+          const V8 kf = *reinterpret_cast<const V8 *>(
+              tk + r * kD + place_of<kChunks>(r, 4 * k + quad) * 8);
+          z[b] = N::mfma16(kf, qf[k], z[b]);
+        }
+      if (kBufs == 1 && more) {
+        wait_lds();  // the keys are in registers, or done with
+        fetch(0, seen, own[0][0]);
+      }
+      if (P.cap_out > 0.0f) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          z[e >> 2][e & 3] = P.cap_out * bend(z[e >> 2][e & 3] * P.cap_arg);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) z[e >> 2][e & 3] *= P.to_log2;
+      }
+      if (P.slope) {
+        const int far = last - j0 - 4 * quad;
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          z[e >> 2][e & 3] -= slope2 * static_cast<float>(far - ((e >> 2) * 16 + (e & 3)));
+      }
+      if (now != 0xFFFFFFFFu) {
+        const uint32_t mine = now >> (4 * quad);
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (!(mine >> ((e >> 2) * 16 + (e & 3)) & 1)) z[e >> 2][e & 3] = -INFINITY;
+      }
+      any = any || now != 0;
+      float big = -INFINITY;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) big = fmaxf(big, z[e >> 2][e & 3]);
+      if (__ballot(big > m + kSlack)) {
+        big = fmaxf(big, __shfl_xor(big, 16));
+        big = fmaxf(big, __shfl_xor(big, 32));
+        const float to = fmaxf(m, big);
+        const float fix = to == m ? 1.0f : __builtin_amdgcn_exp2f(m - to);
+        m = to;
+        l *= fix;
+#pragma unroll
+        for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) acc[b][r] *= fix;
+      }
+      // the difference first: with scores of 2^24 and more the sum of m and kLift would be off
+      const float base = m == -INFINITY ? 0.0f : m;
+      V8 pf;
+#pragma unroll
+      for (int e = 0; e < 8; e += 2) {
+        const float p0 = __builtin_amdgcn_exp2f((z[e >> 2][e & 3] - base) + kLift<kType>);
+        const float p1 = __builtin_amdgcn_exp2f((z[e >> 2][(e & 3) + 1] - base) + kLift<kType>);
+        const auto two = pack2<kType>(p0, p1);
+        l = add2<kType>(two, l);
+        pf[e] = two[0];
+        pf[e + 1] = two[1];
+      }
+#pragma unroll
+      for (int b0 = 0; b0 < kBlocks; b0 += 4) {
+        uint32_t at[4];
+        V8 vf[4];
+#pragma unroll
+        for (int b = 0; b < 4; ++b) at[b] = place[b0 + b] + buf * 2 * kKeys * kD * sizeof(E);
+        read_transposed<kType, 16 * kD * sizeof(E)>(at, vf);
+#pragma unroll
+        for (int b = 0; b < 4; ++b) acc[b0 + b] = N::mfma16(vf[b], pf, acc[b0 + b]);
+      }
+      if (more) {
+        if (kBufs == 1) fetch(1, seen, own[0][1]);
+        buf ^= kBufs - 1;
+      }
     }
-    if (P.slope) {
-      const int far = last - j0 - 4 * quad;
-#pragma unroll
-      for (int e = 0; e < 8; ++e)
-        z[e >> 2][e & 3] -= slope2 * static_cast<float>(far - ((e >> 2) * 16 + (e & 3)));
-    }
-    if (now != 0xFFFFFFFFu) {
-      const uint32_t mine = now >> (4 * quad);
-#pragma unroll
-      for (int e = 0; e < 8; ++e)
-        if (!(mine >> ((e >> 2) * 16 + (e & 3)) & 1)) z[e >> 2][e & 3] = -INFINITY;
-    }
-    any = any || now != 0;
-    float big = -INFINITY;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) big = fmaxf(big, z[e >> 2][e & 3]);
-    if (__ballot(big > m + kSlack)) {
-      big = fmaxf(big, __shfl_xor(big, 16));
-      big = fmaxf(big, __shfl_xor(big, 32));
-      const float to = fmaxf(m, big);
-      const float fix = to == m ? 1.0f : __builtin_amdgcn_exp2f(m - to);
-      m = to;
-      l *= fix;
-#pragma unroll
-      for (int b = 0; b < kBlocks; ++b)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) acc[b][r] *= fix;
-    }
-    // the difference first: with scores of 2^24 and more the sum of m and kLift would be off
-    const float base = m == -INFINITY ? 0.0f : m;
-    V8 pf;
-#pragma unroll
-    for (int e = 0; e < 8; e += 2) {
-      const float p0 = __builtin_amdgcn_exp2f((z[e >> 2][e & 3] - base) + kLift<kType>);
-      const float p1 = __builtin_amdgcn_exp2f((z[e >> 2][(e & 3) + 1] - base) + kLift<kType>);
-      const auto two = pack2<kType>(p0, p1);
-      l = add2<kType>(two, l);
-      pf[e] = two[0];
-      pf[e + 1] = two[1];
+    // the waves' ranges are joined through LDS
+    l += __shfl_xor(l, 16);
+    l += __shfl_xor(l, 32);
+    if (any && m == -INFINITY) m = -FLT_MAX;
+    wait_loads();
+    __syncthreads();  // the tiles are done with
+    float *sums = reinterpret_cast<float *>(&tile[0][0][0][0]);  // [kWaves][16][kD]
+    if (quad == 0) {
+      s_m[wave][col] = m;
+      s_l[wave][col] = l;
     }
 #pragma unroll
-    for (int b = 0; b < kBlocks; ++b) {
-      const int r0 = 4 * quad + (col >> 2), c = 2 * b + ((col & 3) >> 1);
-      const V4 v0 = read_transposed<kType>(
-          tv + r0 * kD + place_of<kChunks>(r0, c) * 8 + (col & 1) * 4);
-      const V4 v1 = read_transposed<kType>(
-          tv + (r0 + 16) * kD + place_of<kChunks>(r0 + 16, c) * 8 + (col & 1) * 4);
-      const V8 vf = __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7);
-      acc[b] = N::mfma16(vf, pf, acc[b]);
+    for (int b = 0; b < kBlocks; ++b)
+      *reinterpret_cast<f32x4 *>(sums + (wave * 16 + col) * kD + b * 16 + quad * 4) = acc[b];
+    __syncthreads();
+    constexpr int kLanes = kWaves * 4 < kD / 4 ? kWaves * 4 : kD / 4;  // threads of a row
+    const int r = threadIdx.x / kLanes, c0 = threadIdx.x % kLanes;
+    const int mine = rt * 16 + r;
+    if (r < 16 && mine < P.group) {
+      float top = -INFINITY;
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) top = fmaxf(top, s_m[w][r]);
+      float f[kWaves], sum = 0.0f;
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) {
+        f[w] = s_m[w][r] == top ? 1.0f : __builtin_amdgcn_exp2f(s_m[w][r] - top);
+        sum += f[w] * s_l[w][r];
+      }
+      const int ohead = kvh * P.group + mine;
+      const int64_t flat = int64_t(id + seq) * P.n_heads + ohead;
+      E *o = static_cast<E *>(P.out) + seq * P.out_stride + ohead * P.out_head;
+#pragma unroll
+      for (int b = 0; b < kD / 4 / kLanes; ++b) {
+        const int c = (b * kLanes + c0) * 4;
+        if (c >= P.d) continue;
+        f32x4 v = {};
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w)
+          v += f[w] * *reinterpret_cast<const f32x4 *>(sums + (w * 16 + r) * kD + c);
+        if (whole) {
+#pragma unroll
+          for (int q = 0; q < 4; ++q) v[q] = weighted(v[q], top, sum);
+          *reinterpret_cast<V4 *>(o + c) = __builtin_convertvector(v, V4);
+        } else {
+          *reinterpret_cast<f32x4 *>(P.part + flat * P.d + c) = v;
+        }
+      }
+      if (!whole && c0 == 0) {
+        P.part_ml[flat * 2] = top;
+        P.part_ml[flat * 2 + 1] = sum;
+      }
     }
-    buf ^= 1;
-  }
-  // the waves' ranges are joined through LDS
-  l += __shfl_xor(l, 16);
-  l += __shfl_xor(l, 32);
-  if (any && m == -INFINITY) m = -FLT_MAX;
-  wait_loads();
-  __syncthreads();  // the tiles are done with
-  float *sums = reinterpret_cast<float *>(&tile[0][0][0][0]);  // [kWaves][16][kD]
-  if (quad == 0) {
-    s_m[wave][col] = m;
-    s_l[wave][col] = l;
-  }
-#pragma unroll
-  for (int b = 0; b < kBlocks; ++b)
-    *reinterpret_cast<f32x4 *>(sums + (wave * 16 + col) * kD + b * 16 + quad * 4) = acc[b];
-  __syncthreads();
-  constexpr int kLanes = kWaves * 4;  // threads of a row
-  const int r = threadIdx.x / kLanes, c0 = threadIdx.x % kLanes;
-  const int mine = rt * 16 + r;
-  if (mine >= P.group) return;
-  float top = -INFINITY;
-#pragma unroll
-  for (int w = 0; w < kWaves; ++w) top = fmaxf(top, s_m[w][r]);
-  float f[kWaves], sum = 0.0f;
-#pragma unroll
-  for (int w = 0; w < kWaves; ++w) {
-    f[w] = s_m[w][r] == top ? 1.0f : __builtin_amdgcn_exp2f(s_m[w][r] - top);
-    sum += f[w] * s_l[w][r];
-  }
-  const int ohead = kvh * P.group + mine;
-  const int64_t flat = int64_t(id) * P.n_heads + ohead;
-  E *o = static_cast<E *>(P.out) + seq * P.out_stride + ohead * P.out_head;
-#pragma unroll
-  for (int b = 0; b < kD / 4 / kLanes; ++b) {
-    const int c = (b * kLanes + c0) * 4;
-    if (c >= P.d) continue;
-    f32x4 v = {};
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w)
-      v += f[w] * *reinterpret_cast<const f32x4 *>(sums + (w * 16 + r) * kD + c);
-    if (parts.count == 1) {
-#pragma unroll
-      for (int q = 0; q < 4; ++q) v[q] = weighted(v[q], top, sum);
-      *reinterpret_cast<V4 *>(o + c) = __builtin_convertvector(v, V4);
-    } else {
-      *reinterpret_cast<f32x4 *>(P.part + flat * P.d + c) = v;
-    }
-  }
-  if (parts.count > 1 && c0 == 0) {
-    P.part_ml[flat * 2] = top;
-    P.part_ml[flat * 2 + 1] = sum;
+    if (!again) return;
+    at_tile += tiles;
+    ++seq;
+    __syncthreads();  // the sums are read
   }
 }
 
@@ -445,10 +555,11 @@ __global__ __launch_bounds__(kJoinThreads, 4) void join_kernel(const AttendParam
   const int tid = threadIdx.x, lane = tid & 63, group = tid >> 5, c = (tid & 31) * 4;
   const int id = workgroup(), head = id % P.n_heads, seq = id / P.n_heads;
   if (seq >= P.n_seqs) return;
-  const Parts parts = find_parts(P, -1, seq);
-  if (parts.count <= 1) return;
-  const int n = parts.count;
-  const int64_t flat = int64_t(parts.first) * P.n_heads + head;
+  const Cut cut = find_cut(P, -1, seq);
+  const int tiles = tiles_of(span_of(P, P.kv_len[seq]));
+  const int first = cut.at / cut.length, n = (cut.at + tiles - 1) / cut.length - first + 1;
+  if (tiles == 0 || n <= 1) return;  // in one range: the result is there
+  const int64_t flat = int64_t(first + seq) * P.n_heads + head;
   float top = -INFINITY, total = 0.0f;
   f32x4 sum = {};
   for (int k0 = 0; k0 < n; k0 += 64) {  // lane k of every wave has part k's maximum and sum
@@ -495,34 +606,61 @@ __global__ __launch_bounds__(kJoinThreads, 4) void join_kernel(const AttendParam
 
 // ------------------------------------------------------------------------------- the host
 
-// Keys that are not cut, as the join's launch costs more: up to 512, or 1,024 where the sequences
-// alone make 64 workgroups, or 4,096 where they make all that the cut would be for.
-constexpr int kWhole = 512, kWholeOfMany = 1024, kWholeOfAll = 4096, kManyWorkgroups = 64;
+// How a call is done: by a workgroup a sequence and key head, of `waves` waves, or with all keys
+// cut into ranges for one workgroup a place (512: two a CU with heads of 128), which a second
+// launch joins.
+struct Form {
+  int waves, width, least;
+};
 
-int64_t each_of(int n_heads, int n_kv_heads) {  // workgroups of a part
+constexpr int kPlaces = 512, kCutWaves = 2;
+
+int64_t each_of(int n_heads, int n_kv_heads) {  // workgroups of a sequence
   return int64_t(n_kv_heads) * ((n_heads / n_kv_heads + 15) / 16);
 }
 
-// Parts that the keys are cut into, 0 for no cut.
-int width_of(int n_seqs, int max_kv, int64_t each) {
+// Whether a sequence's keys are left to one workgroup: where there are few, since the join costs a
+// launch, and up to more of them the more workgroups the sequences alone make; beyond, a long one
+// among short ones would keep all waiting. us by a workgroup of 8 waves (4) and cut:
+//       1 sequence,  5,000 keys, 8 heads of 128 over 2: 33 (51), 13
+//       4 sequences, 1,600, 16 heads of 128 over 4:     16 (20), 13
+//      20 sequences, 1,600, 16 heads of 128 over 4:     17 (21), 20
+//      20 sequences, 1,600, 16 heads of 64 over 4:      13 (19), 18
+//      64 sequences, 2,200, 16 heads of 128 over 4:     41 (40), 46
+//     256 sequences, 4,096, 32 heads of 128 over 8:    439 (442), 439
+//     256 sequences,   500, 16 heads of 64 over 2:      12 (11), 35
+//   1,000 sequences,   900, 8 heads of 128 over 1:      64 (58), 106
+//       8 sequences, 100,003, 16 heads of 128 over 2:  937 (1,107), 111
+constexpr int kWholeNarrow = 1536, kWholeWide = 1024, kWholeOfMany = 2048, kWholeOfAll = 4096;
+
+Form form_of(int n_seqs, int max_kv, int64_t each, int d) {
   const int64_t alone = n_seqs * each;
-  const int whole = alone >= kWorkgroups ? kWholeOfAll : alone >= kManyWorkgroups ? kWholeOfMany
-                                                                                  : kWhole;
-  if (n_seqs > kMaxCut || max_kv <= whole) return 0;
-  return static_cast<int>(std::max<int64_t>((kWorkgroups + each - 1) / each, n_seqs));
+  const int few = d <= 64 ? kWholeNarrow : kWholeWide;
+  const int whole = alone >= 256 ? kWholeOfAll : alone >= 64 ? kWholeOfMany : few;
+  const int waves = alone > 256 && max_kv <= 1024 ? 4 : 8;
+  // tiles are counted in 30 bits
+  if (n_seqs > kMaxCut || max_kv <= whole || n_seqs * (int64_t(max_kv) / kKeys + 2) > 1 << 30)
+    return {waves, 0, 0};
+  return {kCutWaves, static_cast<int>(std::max<int64_t>(kPlaces / each, 1)), kCutWaves};
 }
 
-template <int kType, int kD>
-int launch(const AttendParams &P, hipStream_t s) {
-  const int64_t blocks = (int64_t(P.n_seqs) + P.width) * P.n_kv_heads * P.row_tiles;
+template <int kType, int kD, int kWaves, int kBufs>
+int launch_waves(const AttendParams &P, hipStream_t s) {
+  const int64_t blocks = int64_t(P.width ? P.width : P.n_seqs) * P.n_kv_heads * P.row_tiles;
   const int64_t joined = P.width > 0 ? int64_t(P.n_seqs) * P.n_heads : 0;
   if (blocks > kMaxWorkgroups || joined > kMaxWorkgroups) return TG_E_INVAL;
-  hipLaunchKernelGGL((attend_pages_kernel<kType, kD>), grid_of(blocks, kWaves * 64),
-                     dim3(kWaves * 64), 0, s, P);
+  hipLaunchKernelGGL((attend_pages_kernel<kType, kD, kWaves, kBufs>),
+                     grid_of(blocks, kWaves * 64), dim3(kWaves * 64), 0, s, P);
   if (joined > 0)
     hipLaunchKernelGGL(join_kernel<kType>, grid_of(joined, kJoinThreads), dim3(kJoinThreads), 0, s,
                        P);
   return hipGetLastError() == hipSuccess ? TG_OK : TG_E_HIP;
+}
+
+template <int kType, int kD>
+int launch(const AttendParams &P, hipStream_t s) {
+  if (P.width > 0) return launch_waves<kType, kD, kCutWaves, 2>(P, s);
+  return P.unit == 4 ? launch_waves<kType, kD, 4, 1>(P, s) : launch_waves<kType, kD, 8, 1>(P, s);
 }
 
 bool layout_ok(const void *p, int64_t stride, int64_t head) {
@@ -539,16 +677,16 @@ bool sizes_ok(int n_seqs, int max_kv, int n_heads, int n_kv_heads, int d) {
 
 }  // namespace
 
-// Parts of a call, and of every call of fewer sequences or shorter ones with it: those may have more
-// parts than this one, which may have none.
+// Parts of a call, and of every call of fewer sequences or shorter ones with it: those may have
+// more parts than this one, which may have none.
 extern "C" size_t tg_attend_pages_workspace_bytes(int32_t n_seqs, int32_t max_kv_len,
                                                   int32_t n_heads, int32_t n_kv_heads,
                                                   int32_t d) {
   if (!sizes_ok(n_seqs, max_kv_len, n_heads, n_kv_heads, d) || n_seqs == 0) return 0;
   const int64_t each = each_of(n_heads, n_kv_heads);
-  if (max_kv_len <= kWhole) return 0;
+  if (max_kv_len <= kWholeWide) return 0;
   const int64_t cut = std::min<int64_t>(n_seqs, kMaxCut);
-  const int64_t parts = std::max<int64_t>((kWorkgroups + each - 1) / each, cut) + cut;
+  const int64_t parts = std::max<int64_t>(kPlaces / each, 1) + cut;
   return static_cast<size_t>(parts) * n_heads * (d + 2) * sizeof(float);
 }
 
@@ -613,7 +751,11 @@ extern "C" int tg_attend_pages(const tg_attend_pages_args *a, void *stream) {
   P.d = a->d;
   const int64_t each = each_of(a->n_heads, a->n_kv_heads);
   P.row_tiles = static_cast<int32_t>(each / a->n_kv_heads);
-  P.width = width_of(a->n_seqs, P.most, each);
+  const int seen = a->window > 0 ? std::min(P.most, a->window) : P.most;
+  const Form form = form_of(a->n_seqs, seen, each, a->d);
+  P.unit = form.waves;
+  P.width = form.width;
+  P.least = form.least;
   P.part = static_cast<float *>(a->workspace);
   P.part_ml = P.part + (static_cast<size_t>(P.width) + a->n_seqs) * a->n_heads * a->d;
   hipStream_t s = static_cast<hipStream_t>(stream);

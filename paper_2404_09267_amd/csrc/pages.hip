@@ -4,10 +4,10 @@
 // What each sequence gets depends on what all before it have asked for, so one workgroup goes over
 // the sequences, kThreads at a time, with a prefix sum of pages each: first of those that go back,
 // which are pushed on the stack, then of those that are asked for, which come off its top. No
-// sequence waits for another's write: a page that is taken is read from the stack by whoever
-// needs it. The rows of new tokens come with it where they are few; many are a second kernel's, a
-// thread a few tokens, which finds a token's sequence by bisection.
-// There is next to nothing to read, so a chain of loads bounds it (lengths, stack, then the stores).
+// sequence waits for another's write: a page that is taken is read from the stack by whoever needs
+// it. The rows of new tokens come with it where they are few; many are a second kernel's, a thread
+// a few tokens, which finds a token's sequence by bisection. There is next to nothing to read, so a
+// chain of loads bounds it (lengths, stack, then the stores).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -53,8 +53,8 @@ __device__ __forceinline__ void put(const PagesParams &P, int t, int64_t slot, i
   if (P.pos) P.pos[t] = slot < 0 ? 0 : place;
 }
 
-// Sum of `v` over the workgroup's threads up to and with this one; `total` over all. 64 bits: q_begin
-// may be anything, and the sums decide what is read.
+// Sum of `v` over the workgroup's threads up to and with this one; `total` over all. 64 bits:
+// q_begin may be anything, and the sums decide what is read.
 __device__ __forceinline__ int64_t sum_up(int64_t v, int64_t (&waves)[kWaves], int64_t &total) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
 #pragma unroll

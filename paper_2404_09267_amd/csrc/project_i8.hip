@@ -1,13 +1,13 @@
-// tg_project_i8: a projection in 8-bit integers, y = (x_scale w_scale) (x w^T), sums exact in 32 bits.
+// tg_project_i8: a projection in 8-bit integers, y = (x_scale w_scale) (x w^T), sums exact in 32
+// bits.
 //
 // Few tokens: reading w bounds it. A workgroup takes 16 outputs and up to 64 tokens, its waves
 // parts of k in turn, straight from memory to the matrix instructions' registers, and the waves'
-// sums are joined through LDS: one launch, no workspace.
-// Many tokens: tiles of x and w go through LDS to the matrix instructions, several steps of 128
-// values of k under way.
-// Results lie transposed in the registers (a lane holds 4 outputs of one token), so that stores are
-// contiguous and a token's scale belongs to the lane. Both operands take the same values of k in
-// the same places, so that the order within an instruction does not matter.
+// sums are joined through LDS: one launch, no workspace. Many tokens: tiles of x and w go through
+// LDS to the matrix instructions, several steps of 128 values of k under way. Results lie
+// transposed in the registers (a lane holds 4 outputs of one token), so that stores are contiguous
+// and a token's scale belongs to the lane. Both operands take the same values of k in the same
+// places, so that the order within an instruction does not matter.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -233,8 +233,8 @@ __global__ __launch_bounds__(kWt *kWn * 64, 2) void tile_kernel(const ProjectPar
   tile<kType, kT, kN, kWt, kWn, kStages>(P, tt * kT, tn * kN, lds);
 }
 
-// Tiles of 256 x 256, one a CU; those past the last whole round of the CUs by quarters, so that a round
-// of few tiles does not take as long as a whole one.
+// Tiles of 256 x 256, one a CU; those past the last whole round of the CUs by quarters, so that a
+// round of few tiles does not take as long as a whole one.
 template <int kType>
 __global__ __launch_bounds__(512, 2) void tile_and_rest_kernel(const ProjectParams P) {
   __shared__ __attribute__((aligned(16))) int8_t lds[kLds<256, 256, 2>];

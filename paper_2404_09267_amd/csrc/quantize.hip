@@ -1,9 +1,9 @@
 // tg_quantize: rows of 16-bit values to 8-bit integers with a scale each.
 //
 // A row is read once into registers, its largest magnitude found, and the integers written: 3 bytes
-// a value, which bounds it. The integer is that of the exact quotient x / scale. The product with the
-// scale's inverse is off by 127 * 2^-23 at most, so only where it lies within kNear of a tie is the
-// quotient looked at: x - r scale is exact in binary32 (both are multiples of the scale's last
+// a value, which bounds it. The integer is that of the exact quotient x / scale. The product with
+// the scale's inverse is off by 127 * 2^-23 at most, so only where it lies within kNear of a tie is
+// the quotient looked at: x - r scale is exact in binary32 (both are multiples of the scale's last
 // bit, and at most as far apart as the scale), and half the scale decides.
 #include <hip/hip_runtime.h>
 

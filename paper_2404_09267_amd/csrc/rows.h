@@ -46,7 +46,8 @@ __device__ __forceinline__ void store_chunk(typename Num<kType>::E *row, int c, 
   }
 }
 
-// Sum over the R threads of a row, in all of them and in a set order. `turn`: LDS of this sum's own.
+// Sum over the R threads of a row, in all of them and in a set order. `turn`: LDS of this sum's
+// own.
 template <int R>
 __device__ __forceinline__ float row_sum(float v, float *turn) {
   v = wave_sum(v);

@@ -413,6 +413,20 @@ def test_attend_pages_far_rows():
     R_assert(run_attend(q, k, v, table + far, lens, page, scale=0.1), want, bound, "far")
 
 
+@pytest.mark.parametrize("window", [0, 33, 2222])
+@pytest.mark.parametrize("lens", [[0, 0, 2500, 0, 1, 31, 32, 33, 0, 4000, 64, 0, 0], [0] * 7,
+                                  [1] * 40 + [0] * 40 + [4500], [4100, 0], [64] * 66 + [2100]])
+def test_attend_pages_ranges(lens, window):
+    """Sequences of no keys and of few among long ones, where all keys are cut into ranges."""
+    say("attend_pages ranges", len(lens), window)
+    g, page = gen(19), 8
+    k, v, table = cache(g, lens, page, 1, 32, torch.bfloat16)
+    q = normal(g, len(lens), 2, 32, dtype=torch.bfloat16)
+    want, bound = R.attend_pages(q, k, v, table, lens, page, 0.2, window=window)
+    got = run_attend(q, k, v, table, lens, page, 9000, scale=0.2, window=window)
+    R_assert(got, want, bound, "ranges")
+
+
 @pytest.mark.parametrize("seqs", [1024, 1025])
 def test_attend_pages_many_sequences(seqs):
     """As many sequences as are cut, and one more; one of them long."""
