@@ -757,7 +757,7 @@ typedef struct {
   int32_t *refused;        /* device out [1]: sequences whose tokens got no rows */
   int32_t n_seqs, n_tokens, n_pages;
   int32_t page_size;       /* >= 1; n_pages * page_size < 2^31 */
-  int32_t max_pages;       /* pages that a sequence may hold, >= 1 */
+  int32_t max_pages;       /* pages that a sequence may hold, 1 .. 2^20 */
   void *workspace;         /* device scratch, 16-byte aligned, >= tg_pages_workspace_bytes(...) */
   size_t workspace_bytes;
 } tg_pages_args;
@@ -781,8 +781,8 @@ size_t tg_pages_workspace_bytes(int32_t n_seqs, int32_t n_tokens);
  * before it begins has no tokens. A table entry outside [0, n_pages) gives its tokens no row. A
  * page belongs to one sequence: nothing counts who shares it.
  * Enqueued on `stream`; the library allocates nothing. Returns TG_E_INVAL (null pointer, negative
- * count, n_seqs > TG_PAGES_MAX_SEQS, page_size or max_pages < 1, n_pages * page_size >= 2^31, a
- * stride below max_pages), TG_E_WORKSPACE, TG_E_HIP. n_seqs == 0 and n_tokens == 0 enqueues
+ * count, n_seqs > TG_PAGES_MAX_SEQS, page_size < 1, max_pages outside [1, 2^20], n_pages * page_size
+ * >= 2^31, a stride below max_pages), TG_E_WORKSPACE, TG_E_HIP. n_seqs == 0 and n_tokens == 0 enqueues
  * nothing, n_seqs == 0 alone gives slot, pos, n_free_out and refused.
  */
 int tg_pages(const tg_pages_args *args, void *stream);

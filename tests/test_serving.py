@@ -61,6 +61,7 @@ def project(**change):
 @pytest.mark.parametrize("change", [
     dict(n_seqs=-1), dict(n_seqs=(1 << 20) + 1), dict(n_tokens=-1), dict(n_pages=-1),
     dict(page_size=0), dict(max_pages=0), dict(table_stride=8), dict(table_stride=-9),
+    dict(max_pages=(1 << 20) + 1, table_stride=1 << 21),
     dict(n_pages=1 << 20, page_size=1 << 11), dict(q_begin=None), dict(kv_len=None),
     dict(kv_len_out=None), dict(table=None), dict(free_pages=None), dict(n_free=None),
     dict(n_free_out=None), dict(slot=None), dict(refused=None)])
