@@ -85,8 +85,7 @@ __device__ __forceinline__ uint32_t low_bytes(float a, float b, float c, float d
 // Largest over the R threads of a row.
 template <int R>
 __device__ __forceinline__ uint32_t row_max(uint32_t v, uint32_t *turn) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v = max(v, static_cast<uint32_t>(__shfl_xor(static_cast<int>(v), o)));
+  v = lanes_max(v);
   if constexpr (R > 64) {
     if ((threadIdx.x & 63) == 0) turn[threadIdx.x >> 6] = v;
     __syncthreads();

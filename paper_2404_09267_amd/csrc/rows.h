@@ -46,11 +46,42 @@ __device__ __forceinline__ void store_chunk(typename Num<kType>::E *row, int c, 
   }
 }
 
+// v of the lane that kCtrl says (1, 2, 4 or 8 before in a row of 16, or the last of the row or of
+// the half before), 0 where there is none.
+template <int kCtrl, int kRows>
+__device__ __forceinline__ uint32_t before(uint32_t v) {
+  return __builtin_amdgcn_update_dpp(0u, v, kCtrl, kRows, 0xF, false);
+}
+
+// Sum over the wave, in all lanes and in a set order; without LDS, whose six round trips a row
+// of few values would wait for.
+__device__ __forceinline__ float lanes_sum(float v) {
+  const auto bits = [](float x) { return __builtin_bit_cast(uint32_t, x); };
+  const auto value = [](uint32_t x) { return __builtin_bit_cast(float, x); };
+  v += value(before<0x111, 0xF>(bits(v)));
+  v += value(before<0x112, 0xF>(bits(v)));
+  v += value(before<0x114, 0xF>(bits(v)));
+  v += value(before<0x118, 0xF>(bits(v)));
+  v += value(before<0x142, 0xA>(bits(v)));
+  v += value(before<0x143, 0xC>(bits(v)));
+  return value(__builtin_amdgcn_readlane(bits(v), 63));
+}
+
+__device__ __forceinline__ uint32_t lanes_max(uint32_t v) {
+  v = max(v, before<0x111, 0xF>(v));
+  v = max(v, before<0x112, 0xF>(v));
+  v = max(v, before<0x114, 0xF>(v));
+  v = max(v, before<0x118, 0xF>(v));
+  v = max(v, before<0x142, 0xA>(v));
+  v = max(v, before<0x143, 0xC>(v));
+  return __builtin_amdgcn_readlane(v, 63);
+}
+
 // Sum over the R threads of a row, in all of them and in a set order. `turn`: LDS of this sum's
 // own.
 template <int R>
 __device__ __forceinline__ float row_sum(float v, float *turn) {
-  v = wave_sum(v);
+  v = lanes_sum(v);
   if constexpr (R > 64) {
     if ((threadIdx.x & 63) == 0) turn[threadIdx.x >> 6] = v;
     __syncthreads();
