@@ -1,48 +1,60 @@
-// What the operators that take a row at a time share: a row's values in registers, 8 consecutive
-// ones a chunk, chunk i of thread t at 8 (i R + t) of R threads a row, and sums over a row.
+// What the operators that take a row at a time share: a row's values in registers, 8 a chunk, of R
+// threads a row, and sums over a row.
 #pragma once
 
 #include "token_math.h"
 
 namespace tok {
 
-constexpr int kRowThreads = 256;  // of a workgroup, where a row takes no more
-
+// Threads of a workgroup: four rows of a wave each, or one row.
 template <int R>
-constexpr int kGroupThreads = R < kRowThreads ? kRowThreads : R;
+constexpr int kGroupThreads = R == 64 ? 256 : R;
 
 template <int kType>
 using Chunk = typename Num<kType>::V8;
 
-// The chunk at `c`: whole where rows start on 16 bytes and n is a multiple of 8 (kVec), else value
-// by value; zeros past n.
-template <int kType, bool kVec>
-__device__ __forceinline__ Chunk<kType> load_chunk(const typename Num<kType>::E *row, int c, int n,
+// Place in the row of value e of this thread's chunk i: 8 that follow each other where rows start on
+// 16 bytes and n is a multiple of 8 (kVec), else what the row's threads have follows each other.
+template <int R, bool kVec>
+__device__ __forceinline__ int place_in_row(int i, int e) {
+  const int t = threadIdx.x % R;
+  return kVec ? (i * R + t) * 8 + e : (i * 8 + e) * R + t;
+}
+
+// Chunk i of a row; zeros past n.
+template <int kType, int R, bool kVec>
+__device__ __forceinline__ Chunk<kType> load_chunk(const typename Num<kType>::E *row, int i, int n,
                                                    bool stream) {
   Chunk<kType> v = {};
   if constexpr (kVec) {
+    const int c = place_in_row<R, kVec>(i, 0);
     const auto *p = reinterpret_cast<const Chunk<kType> *>(row + c);
     if (c < n) v = stream ? __builtin_nontemporal_load(p) : *p;
   } else {
 #pragma unroll
-    for (int e = 0; e < 8; ++e)
-      if (c + e < n) v[e] = row[c + e];
+    for (int e = 0; e < 8; ++e) {
+      const int c = place_in_row<R, kVec>(i, e);
+      if (c < n) v[e] = row[c];
+    }
   }
   return v;
 }
 
-template <int kType, bool kVec>
-__device__ __forceinline__ void store_chunk(typename Num<kType>::E *row, int c, int n,
+template <int kType, int R, bool kVec>
+__device__ __forceinline__ void store_chunk(typename Num<kType>::E *row, int i, int n,
                                             Chunk<kType> v, bool stream) {
   if constexpr (kVec) {
+    const int c = place_in_row<R, kVec>(i, 0);
     auto *p = reinterpret_cast<Chunk<kType> *>(row + c);
     if (c >= n) return;
     if (stream) __builtin_nontemporal_store(v, p);
     else *p = v;
   } else {
 #pragma unroll
-    for (int e = 0; e < 8; ++e)
-      if (c + e < n) row[c + e] = v[e];
+    for (int e = 0; e < 8; ++e) {
+      const int c = place_in_row<R, kVec>(i, e);
+      if (c < n) row[c] = v[e];
+    }
   }
 }
 
