@@ -788,9 +788,8 @@ size_t tg_pages_workspace_bytes(int32_t n_seqs, int32_t n_tokens);
 int tg_pages(const tg_pages_args *args, void *stream);
 
 typedef struct {
-  /* Value c of head h of sequence s's query is q[s * q_stride + h * q_head_stride + c], c < d;
-   * k and v alike by cache row, with n_kv_heads heads: query head h reads key head
-   * h / (n_heads / n_kv_heads). */
+  /* Value c of head h of row r is q[r * q_stride + h * q_head_stride + c], c < d; k and v alike by
+   * cache row, with n_kv_heads heads: query head h reads key head h / (n_heads / n_kv_heads). */
   const void *q, *k, *v;
   int64_t q_stride, q_head_stride, k_stride, k_head_stride, v_stride, v_head_stride;
   void *out;                 /* device out, rows and heads of q */
@@ -799,11 +798,15 @@ typedef struct {
   int64_t table_stride;      /* >= max_pages */
   const int32_t *kv_len;     /* device [n_seqs]: keys of each sequence; its query stands at the
                                 last */
+  const int32_t *q_begin;    /* device [n_seqs + 1] or NULL: as for tg_pages; a sequence's query is
+                                the row of its last token, and one without tokens, or with that
+                                row outside [0, n_q_rows), has none. NULL: row s for each */
   const float *slope;        /* device [n_heads] or NULL: bias per unit of distance, of any sign */
   float scale;               /* finite */
   float cap;                 /* > 0: scores are capped; 0: not */
   int32_t window;            /* > 0: a query sees that many of the last keys; 0: all */
   int32_t n_seqs, n_pages, page_size, max_pages;
+  int32_t n_q_rows;          /* rows of q and out, with q_begin */
   int32_t max_kv_len;        /* bound on kv_len; keys from there on are left out */
   int32_t n_heads, n_kv_heads, d;
   int32_t type;              /* enum tg_type of q, k, v and out */
@@ -823,8 +826,8 @@ size_t tg_attend_pages_workspace_bytes(int32_t n_seqs, int32_t max_kv_len, int32
  *   with slope z -= slope[h] * (n - 1 - j);
  * and the query sees keys j < min(n, max_kv_len, max_pages * page_size) with window == 0 or
  * j >= n - window, but none on a page outside [0, n_pages). The output is the softmax-weighted sum
- * of the v_j it sees, 0 if it sees none (kv_len <= 0 among them; such rows are written), NaN if all
- * its scores are minus infinity. Rows that it does not see are not read. Weights are rounded to
+ * of the v_j it sees, 0 if it sees none (kv_len <= 0 among them; such rows are written, but no row that
+ * is no sequence's query), NaN if all its scores are minus infinity. Rows that it does not see are not read. Weights are rounded to
  * the type before the product with v, in binary16 as 2^7 times their share of the largest or more;
  * their sum is of the rounded ones. An infinite value whose weight rounds to 0 makes NaN. Distances
  * up to 2^24 are exact.
@@ -833,7 +836,7 @@ size_t tg_attend_pages_workspace_bytes(int32_t n_seqs, int32_t max_kv_len, int32
  * TG_ATTEND_MAX_D] or not a multiple of 8, heads that n_kv_heads does not divide, a negative
  * window, page_size or max_pages < 1, n_pages * page_size >= 2^31, a bad type, scale or cap, a table_stride below max_pages, q, k, v or out not
  * 16-byte aligned, another stride that is negative, not a multiple of 8 or, of rows, over 2^22),
- * TG_E_WORKSPACE, TG_E_HIP. n_seqs == 0 enqueues nothing.
+ * TG_E_WORKSPACE, TG_E_HIP. n_seqs == 0, or n_q_rows == 0 with q_begin, enqueues nothing.
  */
 int tg_attend_pages(const tg_attend_pages_args *args, void *stream);
 

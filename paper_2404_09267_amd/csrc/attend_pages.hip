@@ -49,12 +49,12 @@ struct AttendParams {
   void *out;
   int64_t q_stride, q_head, k_stride, k_head, v_stride, v_head, out_stride, out_head;
   int64_t table_stride;
-  const int32_t *table, *kv_len;
+  const int32_t *table, *kv_len, *q_begin;
   const float *slope;
   float to_log2;   // scale * log2(e): a raw score's factor
   float cap_arg;   // scale / cap
   float cap_out;   // cap * log2(e), 0: no cap
-  int32_t window, n_seqs, n_pages, page_size;
+  int32_t window, n_seqs, n_q_rows, n_pages, page_size;
   int32_t page_log2;  // of page_size, -1: it is no power of two
   int32_t most;    // keys of a sequence at most
   int32_t n_heads, n_kv_heads, group, d;
@@ -65,6 +65,21 @@ struct AttendParams {
   float *part;     // [width + n_seqs][n_heads][d] weighted sums, and
   float *part_ml;  // [..][..][2] maximum (log2 units) and sum of weights
 };
+
+// A sequence's query and its keys; no row, no keys where it has no query.
+struct Query {
+  int row, keys;
+};
+
+__device__ __forceinline__ Query query_of(const AttendParams &P, int s) {
+  Query r = {s, P.kv_len[s]};
+  if (P.q_begin) {
+    const int begin = P.q_begin[s], end = P.q_begin[s + 1];
+    r.row = end > begin && end > 0 && end <= P.n_q_rows ? end - 1 : -1;
+  }
+  r.keys = r.row < 0 ? 0 : max(r.keys, 0);
+  return r;
+}
 
 // Keys [lo, hi) of a sequence are seen by its query; a tile has 32 keys from a multiple of 32 on.
 struct Span {
@@ -201,7 +216,7 @@ __device__ __forceinline__ Cut find_cut(const AttendParams &P, int range, int se
     int len[kAtOnce];  // loads of one turn without a branch between them
 #pragma unroll
     for (int u = 0; u < kAtOnce; ++u)
-      len[u] = P.kv_len[min((u0 + u) * 64 + lane, P.n_seqs - 1)];
+      len[u] = query_of(P, min((u0 + u) * 64 + lane, P.n_seqs - 1)).keys;
 #pragma unroll
     for (int u = u0; u < u0 + kAtOnce; ++u) {
       tiles[u] = u * 64 + lane < P.n_seqs ? tiles_of(span_of(P, len[u - u0])) : 0;
@@ -355,22 +370,22 @@ __global__ __launch_bounds__(kWaves * 64) void attend_pages_kernel(const AttendP
   const bool live = my < P.group;
   const int head = kvh * P.group + min(my, P.group - 1);
   const float slope2 = P.slope ? P.slope[head] * kLog2e : 0.0f;
-  int len = P.kv_len[seq];
+  Query query = query_of(P, seq);
   for (;;) {
-    const Span span = span_of(P, len);
-    const int tiles = tiles_of(span), last = len - 1;
+    const Span span = span_of(P, query.keys);
+    const int tiles = tiles_of(span), last = query.keys - 1, q_row = query.row;
     const int first = max(begin_tile - at_tile, 0);        // of the sequence's tiles, up to
     const int beyond = min(end_tile - at_tile, tiles);
     const bool whole = first == 0 && beyond == tiles;
     const int base_key = span.lo / kKeys * kKeys;
     const int from = base_key + first * kKeys, end = min(base_key + beyond * kKeys, span.hi);
     const bool again = P.width > 0 && seq + 1 < P.n_seqs && (to_end || at_tile + tiles < end_tile);
-    if (again) len = P.kv_len[seq + 1];
+    if (again) query = query_of(P, seq + 1);
     const int32_t *table = P.table + seq * P.table_stride;
     int j0 = from + wave * kKeys, buf = 0;
     const int page0 = page_at(table, j0, span.lo, end);
     int page = page_at(table, j0 + kStep, span.lo, end);
-    const E *qr = static_cast<const E *>(P.q) + seq * P.q_stride + head * P.q_head;
+    const E *qr = static_cast<const E *>(P.q) + max(q_row, 0) * P.q_stride + head * P.q_head;
     V8 qf[kSteps];
 #pragma unroll
     for (int k = 0; k < kSteps; ++k) {
@@ -501,7 +516,7 @@ __global__ __launch_bounds__(kWaves * 64) void attend_pages_kernel(const AttendP
     constexpr int kLanes = kWaves * 4 < kD / 4 ? kWaves * 4 : kD / 4;  // threads of a row
     const int r = threadIdx.x / kLanes, c0 = threadIdx.x % kLanes;
     const int mine = rt * 16 + r;
-    if (r < 16 && mine < P.group) {
+    if (r < 16 && mine < P.group && q_row >= 0) {
       float top = -INFINITY;
 #pragma unroll
       for (int w = 0; w < kWaves; ++w) top = fmaxf(top, s_m[w][r]);
@@ -513,7 +528,7 @@ __global__ __launch_bounds__(kWaves * 64) void attend_pages_kernel(const AttendP
       }
       const int ohead = kvh * P.group + mine;
       const int64_t flat = int64_t(id + seq) * P.n_heads + ohead;
-      E *o = static_cast<E *>(P.out) + seq * P.out_stride + ohead * P.out_head;
+      E *o = static_cast<E *>(P.out) + q_row * P.out_stride + ohead * P.out_head;
 #pragma unroll
       for (int b = 0; b < kD / 4 / kLanes; ++b) {
         const int c = (b * kLanes + c0) * 4;
@@ -556,7 +571,8 @@ __global__ __launch_bounds__(kJoinThreads, 4) void join_kernel(const AttendParam
   const int id = workgroup(), head = id % P.n_heads, seq = id / P.n_heads;
   if (seq >= P.n_seqs) return;
   const Cut cut = find_cut(P, -1, seq);
-  const int tiles = tiles_of(span_of(P, P.kv_len[seq]));
+  const Query query = query_of(P, seq);
+  const int tiles = tiles_of(span_of(P, query.keys));
   const int first = cut.at / cut.length, n = (cut.at + tiles - 1) / cut.length - first + 1;
   if (tiles == 0 || n <= 1) return;  // in one range: the result is there
   const int64_t flat = int64_t(first + seq) * P.n_heads + head;
@@ -599,7 +615,7 @@ __global__ __launch_bounds__(kJoinThreads, 4) void join_kernel(const AttendParam
     for (int g = 1; g < kAtOnce; ++g) sum += s_sum[g][tid];
 #pragma unroll
     for (int q = 0; q < 4; ++q) sum[q] = weighted(sum[q], top, total);
-    E *o = static_cast<E *>(P.out) + seq * P.out_stride + head * P.out_head;
+    E *o = static_cast<E *>(P.out) + query.row * P.out_stride + head * P.out_head;
     *reinterpret_cast<V4 *>(o + c) = __builtin_convertvector(sum, V4);
   }
 }
@@ -693,11 +709,11 @@ extern "C" size_t tg_attend_pages_workspace_bytes(int32_t n_seqs, int32_t max_kv
 extern "C" int tg_attend_pages(const tg_attend_pages_args *a, void *stream) {
   if (!a || !type_ok(a->type) ||
       !sizes_ok(a->n_seqs, a->max_kv_len, a->n_heads, a->n_kv_heads, a->d) || a->n_pages < 0 ||
-      a->page_size < 1 || a->max_pages < 1 || a->window < 0 ||
+      (a->q_begin && a->n_q_rows < 0) || a->page_size < 1 || a->max_pages < 1 || a->window < 0 ||
       int64_t(a->n_pages) * a->page_size > INT32_MAX || a->table_stride < a->max_pages ||
       !std::isfinite(a->scale) || !std::isfinite(a->cap) || a->cap < 0.0f)
     return TG_E_INVAL;
-  if (a->n_seqs == 0) return TG_OK;
+  if (a->n_seqs == 0 || (a->q_begin && a->n_q_rows == 0)) return TG_OK;
   if (!a->table || !a->kv_len || !layout_ok(a->q, a->q_stride, a->q_head_stride) ||
       !layout_ok(a->out, a->out_stride, a->out_head_stride))
     return TG_E_INVAL;
@@ -724,6 +740,8 @@ extern "C" int tg_attend_pages(const tg_attend_pages_args *a, void *stream) {
   P.table = a->table;
   P.table_stride = a->table_stride;
   P.kv_len = a->kv_len;
+  P.q_begin = a->q_begin;
+  P.n_q_rows = a->n_q_rows;
   P.slope = a->slope;
   // factors at the ends of binary32 are its largest numbers
   const auto factor = [](double v) {

@@ -139,9 +139,9 @@ class AttendPagesArgs(ctypes.Structure):
                 ("k_stride", _i64), ("k_head_stride", _i64), ("v_stride", _i64),
                 ("v_head_stride", _i64), ("out", _vp), ("out_stride", _i64),
                 ("out_head_stride", _i64), ("table", _vp), ("table_stride", _i64),
-                ("kv_len", _vp), ("slope", _vp), ("scale", _f32), ("cap", _f32),
-                ("window", _i32), ("n_seqs", _i32), ("n_pages", _i32), ("page_size", _i32),
-                ("max_pages", _i32), ("max_kv_len", _i32), ("n_heads", _i32),
+                ("kv_len", _vp), ("q_begin", _vp), ("slope", _vp), ("scale", _f32),
+                ("cap", _f32), ("window", _i32), ("n_seqs", _i32), ("n_pages", _i32),
+                ("page_size", _i32), ("max_pages", _i32), ("n_q_rows", _i32), ("max_kv_len", _i32), ("n_heads", _i32),
                 ("n_kv_heads", _i32), ("d", _i32), ("type", _i32), ("workspace", _vp),
                 ("workspace_bytes", ctypes.c_size_t)]
 
@@ -1202,29 +1202,33 @@ def pages(pages: Pages, q_begin, bufs: PagesBuffers, release=None, after: Pages 
 
 
 class AttendPagesBuffers:
-    """Caller-owned scratch of tg_attend_pages for queries like q [sequences, heads, d] and a cache
-    like k [rows, kv heads, d]; no sequence has more than max_kv keys."""
+    """Caller-owned scratch of tg_attend_pages for queries like q [rows, heads, d], of n_seqs
+    sequences (by default as many), and a cache like k [rows, kv heads, d]; no sequence has more
+    than max_kv keys."""
 
-    def __init__(self, q, k, max_kv: int, device="cuda"):
+    def __init__(self, q, k, max_kv: int, n_seqs: int | None = None, device="cuda"):
         import torch
 
         self.max_kv = int(max_kv)
-        ws = int(lib().tg_attend_pages_workspace_bytes(q.shape[0], self.max_kv, q.shape[1],
+        n_seqs = q.shape[0] if n_seqs is None else n_seqs
+        ws = int(lib().tg_attend_pages_workspace_bytes(n_seqs, self.max_kv, q.shape[1],
                                                        k.shape[1], q.shape[2]))
         self.workspace = torch.empty(max(ws, 16), dtype=torch.uint8, device=device)
         self.workspace_bytes = ws
 
 
 def attend_pages_args(q, k, v, pages: Pages, out, bufs: AttendPagesBuffers, scale: float,
-                      cap: float = 0.0, window: int = 0, slope=None) -> AttendPagesArgs:
-    """q and out [sequences, heads, d], k and v [cache rows, kv heads, d], any strides; whole pages
-    of cache rows count; slope float32 [heads]."""
+                      cap: float = 0.0, window: int = 0, slope=None,
+                      q_begin=None) -> AttendPagesArgs:
+    """q and out [sequences, heads, d], or with q_begin (int32 [sequences + 1], as for tg_pages)
+    [tokens, heads, d]; k and v [cache rows, kv heads, d], any strides; whole pages of cache rows
+    count; slope float32 [heads]."""
     import torch
 
     dt = q.dtype
     type_ = _type_of(dt)
-    _values(q, dt, 3, "q", (pages.n_seqs, *q.shape[1:]))
-    n_seqs, n_heads, d = q.shape
+    _values(q, dt, 3, "q", None if q_begin is not None else (pages.n_seqs, *q.shape[1:]))
+    n_rows, n_heads, d = q.shape
     _values(k, dt, 3, "k")
     rows, n_kv, _ = k.shape
     if k.shape[2] != d:
@@ -1233,9 +1237,11 @@ def attend_pages_args(q, k, v, pages: Pages, out, bufs: AttendPagesBuffers, scal
     _values(out, dt, 3, "out", q.shape)
     if slope is not None:
         _check(slope, torch.float32, (n_heads,), "slope")
+    if q_begin is not None:
+        _check(q_begin, torch.int32, (pages.n_seqs + 1,), "q_begin")
     if pages.page_size < 1:
         raise ValueError("page_size must be positive")
-    _here(q, k, v, pages.table, pages.kv_len, out, bufs.workspace, slope)
+    _here(q, k, v, pages.table, pages.kv_len, out, bufs.workspace, slope, q_begin)
     a = AttendPagesArgs()
     a.q, a.q_stride, a.q_head_stride = _rows(q)
     a.k, a.k_stride, a.k_head_stride = _rows(k)
@@ -1245,11 +1251,14 @@ def attend_pages_args(q, k, v, pages: Pages, out, bufs: AttendPagesBuffers, scal
     a.kv_len = pages.kv_len.data_ptr()
     a.slope = slope.data_ptr() if slope is not None else None
     a.scale, a.cap, a.window = float(scale), float(cap), int(window)
-    a.n_seqs, a.n_pages, a.page_size = n_seqs, rows // pages.page_size, pages.page_size
+    if q_begin is not None:
+        a.q_begin, a.n_q_rows = q_begin.data_ptr(), n_rows
+    a.n_seqs, a.n_pages = pages.n_seqs, rows // pages.page_size
+    a.page_size = pages.page_size
     a.max_pages, a.max_kv_len = pages.max_pages, bufs.max_kv
     a.n_heads, a.n_kv_heads, a.d, a.type = n_heads, n_kv, d, type_
     a.workspace, a.workspace_bytes = bufs.workspace.data_ptr(), bufs.workspace_bytes
-    a._keep = (q, k, v, pages, out, bufs, slope)  # the struct holds raw pointers: keep their owners alive
+    a._keep = (q, k, v, pages, out, bufs, slope, q_begin)  # the struct holds raw pointers: keep their owners alive
     return a
 
 
@@ -1258,10 +1267,10 @@ def attend_pages_raw(args: AttendPagesArgs, stream=None) -> int:
 
 
 def attend_pages(q, k, v, pages: Pages, out, bufs: AttendPagesBuffers, scale: float,
-                 cap: float = 0.0, window: int = 0, slope=None, stream=None) -> None:
+                 cap: float = 0.0, window: int = 0, slope=None, q_begin=None, stream=None) -> None:
     """Enqueue tg_attend_pages: one query of each sequence over its pages, into out."""
-    rc = attend_pages_raw(attend_pages_args(q, k, v, pages, out, bufs, scale, cap, window, slope),
-                          stream)
+    rc = attend_pages_raw(attend_pages_args(q, k, v, pages, out, bufs, scale, cap, window, slope,
+                                            q_begin), stream)
     if rc != OK:
         raise TgError("tg_attend_pages", rc)
 

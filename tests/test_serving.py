@@ -104,6 +104,8 @@ def test_attend_pages_workspace():
     assert attend(workspace=P + 4) == tg.E_WORKSPACE
     assert attend(workspace_bytes=need - 1) == tg.E_WORKSPACE
     assert attend(n_seqs=0) == tg.OK
+    assert attend(q_begin=P, n_q_rows=0) == tg.OK
+    assert attend(q_begin=P, n_q_rows=-1) == tg.E_INVAL
     for heads, kv, d in ((4, 2, 64), (16, 16, 128), (40, 1, 80), (4000, 2000, 8)):
         last = 0
         for seqs in (1, 2, 60, 400, 1024, 1025, 9000, 1 << 20):

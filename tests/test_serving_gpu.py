@@ -427,6 +427,31 @@ def test_attend_pages_ranges(lens, window):
     R_assert(got, want, bound, "ranges")
 
 
+@pytest.mark.parametrize("longest", [300, 3000])
+def test_attend_pages_rows_of_tokens(longest):
+    """Queries are the last tokens of sequences; those without tokens have none, and no other row
+    is written."""
+    say("attend_pages rows", longest)
+    g, page, lens = gen(20), 16, [40, 7, longest, 0, 90, 64, 33]
+    k, v, table = cache(g, lens, page, 2, 64, torch.float16)
+    begin = [2, 3, 3, 8, 9, 9, 10, 14]  # the last one's row is outside
+    q = normal(g, 12, 4, 64, dtype=torch.float16)
+    has, rows = [0, 2, 3, 5], [2, 7, 8, 9]
+    want, bound = R.attend_pages(q[rows], k, v, table[has], [lens[i] for i in has], page, 0.2)
+    pages = tg.Pages(table.cuda(), ints(lens), page)
+    out = torch.full(q.shape, 5.0, dtype=q.dtype, device="cuda")
+    bufs = tg.AttendPagesBuffers(q, k, longest, n_seqs=len(lens))
+    tg.attend_pages(q.cuda(), k.cuda(), v.cuda(), pages, out, bufs, 0.2, q_begin=ints(begin))
+    out = out.cpu()
+    R_assert(out[rows], want, bound, "rows")
+    out[rows] = 5.0
+    assert bool((out == 5.0).all())
+    begin = [-5, -1, 0, 0, 1 << 30, 3, 99, -(1 << 31)]
+    bad = torch.full(q.shape, 5.0, dtype=q.dtype, device="cuda")
+    tg.attend_pages(q.cuda(), k.cuda(), v.cuda(), pages, bad, bufs, 0.2, q_begin=ints(begin))
+    assert bool((bad == 5.0).all())
+
+
 @pytest.mark.parametrize("seqs", [1024, 1025])
 def test_attend_pages_many_sequences(seqs):
     """As many sequences as are cut, and one more; one of them long."""
