@@ -744,3 +744,131 @@ def test_quantized_rows_through_the_product():
     off = (s[fine].double()[:, None] / 2) * w.double().abs().sum(1) + (
         ws.double() / 2) * (x[fine].double().abs().sum(1)[:, None] + 320 * s[fine].double()[:, None] / 2)
     assert bool(((want - plain).abs() <= off).all())
+
+
+# --------------------------------------------------------------- sizes, streams and graphs
+
+def test_rows_past_32_bits():
+    """Arrays of more than 2^31 values: the last rows are where they belong."""
+    say("far rows")
+    g, n, rows = gen(61), 32768, 70000
+    x = torch.zeros((rows, n), dtype=torch.bfloat16, device="cuda")
+    some = normal(g, 3, n, dtype=torch.bfloat16)
+    at = torch.tensor([0, rows // 2 + 3, rows - 1])
+    x[at.cuda()] = some.cuda()
+    h = torch.full_like(x, 3.0)
+    tg.norm(x, None, h, norm=tg.NORM_RMS)
+    _, (want, bound) = R.norm(some, kind=1)
+    R_assert(h[at.cuda()].cpu(), want, bound, "norm")
+    q = torch.full((rows, n), 7, dtype=torch.int8, device="cuda")
+    s = torch.empty(rows, device="cuda")
+    tg.quantize(x, q, s)
+    wq, ws = R.quantize(some)
+    assert torch.equal(q[at.cuda()].cpu(), wq) and torch.equal(s[at.cuda()].cpu(), ws)
+    assert int(q[1].abs().max()) == 0 and int(q[rows - 2].abs().max()) == 0
+    del x, h
+    w, scale = signed(g, 40, n), torch.full((40,), 1e-3)
+    y = torch.full((rows, 40), NAN, dtype=torch.bfloat16, device="cuda")
+    tg.project_i8(q, s, w.cuda(), scale.cuda(), y)
+    torch.cuda.synchronize()
+    want, bound = R.project_i8(wq, ws, w, scale, torch.bfloat16)
+    R_assert(y[at.cuda()].cpu(), want, bound, "project_i8")
+    assert int((y != 0).any(1).sum()) == 3
+
+
+def operators(seed):
+    """A call of each operator as (outputs, function of a stream), on inputs of its own."""
+    g, dt = gen(seed), torch.bfloat16
+    x, y = normal(g, 70, 1024, dtype=dt).cuda(), normal(g, 70, 1024, dtype=dt).cuda()
+    xo, h = torch.empty_like(x), torch.empty_like(x)
+    q8, s8 = torch.empty((70, 1024), dtype=torch.int8, device="cuda"), torch.empty(70, device="cuda")
+    w8, sw = signed(g, 300, 1024).cuda(), torch.rand(300, generator=g).cuda()
+    y8 = torch.empty((70, 300), dtype=dt, device="cuda")
+    lens, page = [3000, 5, 0, 640, 1777], 16
+    k, v, table = cache(g, lens, page, 2, 64, dt)
+    pages = tg.Pages(table.cuda(), ints(lens), page)
+    q = normal(g, 5, 8, 64, dtype=dt).cuda()
+    k, v, out = k.cuda(), v.cuda(), torch.empty_like(q)
+    bufs = tg.AttendPagesBuffers(q, k, 3000)
+    free = tg.Pages.empty(40, 300, 9000, 16)
+    after = tg.Pages(free.table, torch.empty_like(free.kv_len), 16, free.free,
+                     torch.empty_like(free.n_free))
+    begin = torch.cat([torch.zeros(1), torch.randint(0, 400, (40,), generator=g).cumsum(0)]).int()
+    rows = tg.PagesBuffers(free, int(begin[-1]))
+    begin = begin.cuda()
+    return [
+        ([xo, h], lambda s: tg.norm(x, xo, h, y=y, y_norm=tg.NORM_LAYER, stream=s)),
+        ([q8, s8], lambda s: tg.quantize(x, q8, s8, stream=s)),
+        ([y8], lambda s: tg.project_i8(q8, s8, w8, sw, y8, stream=s)),
+        ([out], lambda s: tg.attend_pages(q, k, v, pages, out, bufs, 0.1, stream=s)),
+        ([rows.slot, rows.pos, rows.refused, after.kv_len, after.n_free],  # the table: in and out
+         lambda s: tg.pages(free, begin, rows, after=after, stream=s))]
+
+
+def test_streams():
+    """Two sets of calls at once on two streams give what each gives alone on the current one."""
+    say("streams")
+    sets = [operators(71), operators(72)]
+    want = []
+    for calls in sets:
+        for outs, call in calls:
+            call(None)
+        want.append([[t.clone() for t in outs] for outs, _ in calls])
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in sets]
+    for turn in range(4):
+        for calls in sets:
+            for outs, _ in calls:
+                for t in outs:
+                    t.zero_()
+        torch.cuda.synchronize()
+        for i in range(len(sets[0])):
+            for calls, s in zip(sets, streams):
+                calls[i][1](s)
+        torch.cuda.synchronize()
+        for calls, exp in zip(sets, want):
+            for (outs, _), ref in zip(calls, exp):
+                assert all(torch.equal(a, b) for a, b in zip(outs, ref))
+
+
+def test_graphs():
+    """Captured calls, replayed with eager work between, of two graphs that share workspaces."""
+    say("graphs")
+    calls = operators(73)
+    want = []
+    for outs, call in calls:
+        call(None)
+        want.append([t.clone() for t in outs])
+    torch.cuda.synchronize()
+    graphs = []
+    for _ in range(2):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            for _, call in calls:
+                call(None)
+        graphs.append(graph)
+    for turn in range(6):
+        for outs, _ in calls:
+            for t in outs:
+                t.zero_()
+        graphs[turn % 2].replay()
+        if turn % 3 == 2:
+            torch.cuda.synchronize()
+            for _, call in calls:
+                call(None)
+        torch.cuda.synchronize()
+        for (outs, _), ref in zip(calls, want):
+            assert all(torch.equal(a, b) for a, b in zip(outs, ref))
+
+
+def test_the_same_call_gives_the_same_bits():
+    say("repeat")
+    calls = operators(74)
+    first = None
+    for _ in range(5):
+        for _, call in calls:
+            call(None)
+        torch.cuda.synchronize()
+        got = [t.clone() for outs, _ in calls for t in outs]
+        first = first or got
+        assert all(torch.equal(a, b) for a, b in zip(got, first))
