@@ -155,6 +155,12 @@ __device__ __forceinline__ void gather_lds(uint64_t from, void *to) {
       16, 0, 0);
 }
 
+// Waits for the wave's loads; LDS is not read before.
+__device__ __forceinline__ void wait_tile() {
+  wait_loads();
+  asm volatile("" ::: "memory");
+}
+
 // Waits for the wave's LDS reads; no load to LDS is issued before.
 __device__ __forceinline__ void wait_lds() {
   __builtin_amdgcn_sched_barrier(0);
@@ -405,7 +411,7 @@ __global__ __launch_bounds__(kWaves * 64) void attend_pages_kernel(const AttendP
     float m = -INFINITY, l = 0.0f;
     bool any = false;
     for (; j0 < end; j0 += kStep) {
-      wait_loads();
+      wait_tile();
       const uint32_t now = seen;
       const bool more = j0 + kStep < end;
       if (more) {

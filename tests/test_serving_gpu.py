@@ -129,6 +129,18 @@ def test_pages_many_short_prompts():
     s.step([i % 3 for i in range(5000)], [int(i % 7 == 0) for i in range(5000)])
 
 
+def test_pages_without_tokens():
+    """A step in which requests end and nobody brings a token."""
+    say("pages without tokens")
+    for seqs in (3, 1100):
+        s = Step(seqs, 5, 5 * seqs, 8, seed=6)
+        s.step([i % 39 for i in range(seqs)])
+        s.step([0] * seqs, [i % 2 for i in range(seqs)])
+        s.step([0] * seqs)
+        s.step([0] * seqs, [1] * seqs)
+        assert len(s.free) == 5 * seqs
+
+
 def test_pages_nobody():
     """No sequences: padding alone."""
     say("pages nobody")
@@ -803,6 +815,23 @@ def operators(seed):
         ([out], lambda s: tg.attend_pages(q, k, v, pages, out, bufs, 0.1, stream=s)),
         ([rows.slot, rows.pos, rows.refused, after.kv_len, after.n_free],  # the table: in and out
          lambda s: tg.pages(free, begin, rows, after=after, stream=s))]
+
+
+def test_other_device_is_refused(monkeypatch):
+    """A call goes to the current device's stream: tensors of another are refused."""
+    say("other device")
+    x, p = torch.zeros((2, 64), device="cuda").half(), tg.Pages.empty(2, 3, 4, 16)
+    q8, one = torch.zeros((2, 64), dtype=torch.int8, device="cuda"), torch.zeros(2, device="cuda")
+    bufs, q = tg.PagesBuffers(p, 2), x.view(2, 1, 64)
+    scratch = tg.AttendPagesBuffers(q, q, 40)
+    begin = ints([0, 1, 2])
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 1)
+    for make in (lambda: tg.norm_args(x, x), lambda: tg.quantize_args(x, q8, one),
+                 lambda: tg.project_i8_args(q8, one, q8, one, x[:, :2]),
+                 lambda: tg.pages_args(p, begin, bufs),
+                 lambda: tg.attend_pages_args(q, q, q, p, q, scratch, 1.0)):
+        with pytest.raises(ValueError, match="current device"):
+            make()
 
 
 def test_streams():
