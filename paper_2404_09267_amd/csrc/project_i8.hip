@@ -37,18 +37,28 @@ __device__ __forceinline__ i32x4 mfma(i32x4 a, i32x4 b, i32x4 c) {
   return __builtin_amdgcn_mfma_i32_16x16x64_i8(a, b, c, 0, 0, 0);
 }
 
+// Scales of the tokens and outputs that a lane has results of; of the nearest inside where it has none.
+__device__ __forceinline__ float scale_of(const ProjectParams &P, int t) {
+  return P.x_scale[min(t, P.n_tokens - 1)];
+}
+__device__ __forceinline__ f32x4 scales_of(const ProjectParams &P, int n) {
+  f32x4 v;
+#pragma unroll
+  for (int r = 0; r < 4; ++r) v[r] = P.w_scale[min(n + r, P.n - 1)];
+  return v;
+}
+
 // 4 outputs of one token, from n on.
 template <int kType>
-__device__ __forceinline__ void put(const ProjectParams &P, int t, int n, i32x4 sum) {
+__device__ __forceinline__ void put(const ProjectParams &P, int t, int n, i32x4 sum, float xs,
+                                    f32x4 ws) {
   typedef typename Num<kType>::E E;
   typedef typename Num<kType>::V4 V4;
   if (t >= P.n_tokens || n >= P.n) return;
-  const float xs = P.x_scale[t];
   E *to = static_cast<E *>(P.y) + int64_t(t) * P.y_stride + n;
   f32x4 v;
 #pragma unroll
-  for (int r = 0; r < 4; ++r)
-    v[r] = static_cast<float>(sum[r]) * (xs * P.w_scale[min(n + r, P.n - 1)]);
+  for (int r = 0; r < 4; ++r) v[r] = static_cast<float>(sum[r]) * (xs * ws[r]);
   const V4 out = __builtin_convertvector(v, V4);
   if (n + 3 < P.n) {  // as they lie: rows may start anywhere
     __builtin_memcpy(to, &out, sizeof(out));
@@ -78,6 +88,8 @@ __global__ __launch_bounds__(kFewWaves * 64) void few_kernel(const ProjectParams
   const int8_t *w = P.w + int64_t(min(n0 + col, P.n - 1)) * P.w_stride;
   const int8_t *x = P.x + int64_t(min(t0 + col, P.n_tokens - 1)) * P.x_stride;
   i32x4 acc = {};
+  const float xs = scale_of(P, t0 + col);
+  const f32x4 ws = scales_of(P, n0 + 4 * quad);
   for (int k0 = wave * 64 * kAhead; k0 < P.k; k0 += kFewWaves * 64 * kAhead) {
     i32x4 wv[kAhead], xv[kAhead];
 #pragma unroll
@@ -96,7 +108,7 @@ __global__ __launch_bounds__(kFewWaves * 64) void few_kernel(const ProjectParams
   i32x4 sum = {};
 #pragma unroll
   for (int v = 0; v < kFewWaves; ++v) sum += s_sum[v][lane];
-  put<kType>(P, t0 + col, n0 + 4 * quad, sum);
+  put<kType>(P, t0 + col, n0 + 4 * quad, sum, xs, ws);
 }
 
 // ----------------------------------------------------------------------------- many tokens
@@ -169,6 +181,17 @@ __device__ __forceinline__ void tile(const ProjectParams &P, int t0, int n0, int
   };
   i32x4 acc[kFn][kFt] = {};
   const int wt = (wave % kWt) * (kT / kWt), wn = (wave / kWt) * (kN / kWn);
+  // the scales first where registers allow, so that nothing waits for them at the end
+  constexpr bool kEarly = kFt * kFn <= 16;
+  float xs[kFt];
+  f32x4 ws[kFn];
+  auto scales = [&] {
+#pragma unroll
+    for (int i = 0; i < kFt; ++i) xs[i] = scale_of(P, t0 + wt + 16 * i + col);
+#pragma unroll
+    for (int j = 0; j < kFn; ++j) ws[j] = scales_of(P, n0 + wn + 16 * j + 4 * quad);
+  };
+  if (kEarly) scales();
   struct Operands {  // of 64 values of k
     i32x4 x[kFt], w[kFn];
   };
@@ -218,11 +241,12 @@ __device__ __forceinline__ void tile(const ProjectParams &P, int t0, int n0, int
     interleave(true);
   }
   wait_loads();  // LDS belongs to the next workgroup from here on
+  if (!kEarly) scales();
 #pragma unroll
   for (int i = 0; i < kFt; ++i)
 #pragma unroll
     for (int j = 0; j < kFn; ++j)
-      put<kType>(P, t0 + wt + 16 * i + col, n0 + wn + 16 * j + 4 * quad, acc[j][i]);
+      put<kType>(P, t0 + wt + 16 * i + col, n0 + wn + 16 * j + 4 * quad, acc[j][i], xs[i], ws[j]);
 }
 
 template <int kType, int kT, int kN, int kWt, int kWn, int kStages>
