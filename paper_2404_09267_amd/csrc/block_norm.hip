@@ -91,19 +91,20 @@ __device__ __forceinline__ void normalise(const NormParams &P, float (&u)[kV * 8
 #pragma unroll
   for (int i = 0; i < kV; ++i) {
     if (weight) {
-      const Chunk<kType> w = load_chunk<kType, R, kVec>(static_cast<const E *>(weight), i, n, false);
+      const Chunk<kType> w = load_chunk<kType, R, kVec>(static_cast<const E *>(weight), i, n);
 #pragma unroll
       for (int e = 0; e < 8; ++e) u[i * 8 + e] *= static_cast<float>(w[e]);
     }
     if (bias) {
-      const Chunk<kType> b = load_chunk<kType, R, kVec>(static_cast<const E *>(bias), i, n, false);
+      const Chunk<kType> b = load_chunk<kType, R, kVec>(static_cast<const E *>(bias), i, n);
 #pragma unroll
       for (int e = 0; e < 8; ++e) u[i * 8 + e] += static_cast<float>(b[e]);
     }
   }
 }
 
-template <int kType, int R, int kV, bool kVec>
+// kStream: x, y and the results go past the caches.
+template <int kType, int R, int kV, bool kVec, bool kStream>
 __global__ __launch_bounds__(kGroupThreads<R>) void norm_kernel(const NormParams P) {
   typedef typename Num<kType>::E E;
   constexpr int kRows = kGroupThreads<R> / R;
@@ -111,11 +112,10 @@ __global__ __launch_bounds__(kGroupThreads<R>) void norm_kernel(const NormParams
   const int64_t t = int64_t(workgroup()) * kRows + threadIdx.x / R;
   if (t >= P.n_tokens) return;  // a whole wave, or the workgroup
   const int n = P.n;
-  const bool stream = P.stream != 0;
   Chunk<kType> xv[kV];
   const E *x = static_cast<const E *>(P.x) + t * P.x_stride;
 #pragma unroll
-  for (int i = 0; i < kV; ++i) xv[i] = load_chunk<kType, R, kVec>(x, i, n, stream);
+  for (int i = 0; i < kV; ++i) xv[i] = load_chunk<kType, R, kVec, kStream>(x, i, n);
   int g = P.y ? 0 : -1;
   if (P.gate_row) g = P.gate_row[t];
   if (P.gate && (g < 0 || g >= P.n_gates)) g = -1;
@@ -124,7 +124,7 @@ __global__ __launch_bounds__(kGroupThreads<R>) void norm_kernel(const NormParams
     const E *y = static_cast<const E *>(P.y) + t * P.y_stride;
 #pragma unroll
     for (int i = 0; i < kV; ++i) {
-      const Chunk<kType> v = load_chunk<kType, R, kVec>(y, i, n, stream);
+      const Chunk<kType> v = load_chunk<kType, R, kVec, kStream>(y, i, n);
 #pragma unroll
       for (int e = 0; e < 8; ++e) u[i * 8 + e] = static_cast<float>(v[e]);
     }
@@ -133,7 +133,7 @@ __global__ __launch_bounds__(kGroupThreads<R>) void norm_kernel(const NormParams
 #pragma unroll
     for (int i = 0; i < kV; ++i) {
       if (gate) {
-        const Chunk<kType> v = load_chunk<kType, R, kVec>(gate, i, n, false);
+        const Chunk<kType> v = load_chunk<kType, R, kVec>(gate, i, n);
 #pragma unroll
         for (int e = 0; e < 8; ++e) u[i * 8 + e] *= static_cast<float>(v[e]);
       }
@@ -152,7 +152,7 @@ __global__ __launch_bounds__(kGroupThreads<R>) void norm_kernel(const NormParams
       Chunk<kType> v;
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[e] = static_cast<E>(u[i * 8 + e]);
-      store_chunk<kType, R, kVec>(row, i, n, v, stream);
+      store_chunk<kType, R, kVec, kStream>(row, i, n, v);
     }
   };
   if (P.x_out) put(P.x_out, P.x_out_stride);
@@ -167,8 +167,12 @@ int launch_rows(const NormParams &P, bool vec, hipStream_t s) {
   const int64_t blocks = (int64_t(P.n_tokens) + kRows - 1) / kRows;
   if (blocks > kMaxWorkgroups) return TG_E_INVAL;
   const dim3 grid = grid_of(blocks, kThreads), threads(kThreads);
-  if (vec) hipLaunchKernelGGL((norm_kernel<kType, R, kV, true>), grid, threads, 0, s, P);
-  else hipLaunchKernelGGL((norm_kernel<kType, R, kV, false>), grid, threads, 0, s, P);
+  if (vec && P.stream)
+    hipLaunchKernelGGL((norm_kernel<kType, R, kV, true, true>), grid, threads, 0, s, P);
+  else if (vec)
+    hipLaunchKernelGGL((norm_kernel<kType, R, kV, true, false>), grid, threads, 0, s, P);
+  else
+    hipLaunchKernelGGL((norm_kernel<kType, R, kV, false, false>), grid, threads, 0, s, P);
   return hipGetLastError() == hipSuccess ? TG_OK : TG_E_HIP;
 }
 

@@ -99,7 +99,7 @@ __device__ __forceinline__ uint32_t row_max(uint32_t v, uint32_t *turn) {
 }
 
 // k a multiple of 8, rows of x on 16 bytes, of q on 8.
-template <int kType, int R, int kV>
+template <int kType, int R, int kV, bool kStream>
 __global__ __launch_bounds__(kGroupThreads<R>) void quantize_kernel(const QuantizeParams P) {
   typedef typename Num<kType>::E E;
   constexpr int kRows = kGroupThreads<R> / R;
@@ -111,7 +111,7 @@ __global__ __launch_bounds__(kGroupThreads<R>) void quantize_kernel(const Quanti
   Chunk<kType> v[kV];
 #pragma unroll
   for (int i = 0; i < kV; ++i)
-    v[i] = load_chunk<kType, R, true>(x, i, P.k, P.stream != 0);
+    v[i] = load_chunk<kType, R, true, kStream>(x, i, P.k);
   typedef uint16_t u16x8 __attribute__((ext_vector_type(8)));
   u16x8 most = {};
 #pragma unroll
@@ -144,7 +144,7 @@ __global__ __launch_bounds__(kGroupThreads<R>) void quantize_kernel(const Quanti
     const u32x2 out = {low_bytes(r[0], r[1], r[2], r[3]), low_bytes(r[4], r[5], r[6], r[7])};
     u32x2 *to = reinterpret_cast<u32x2 *>(q + c);
     if (c < P.k) {
-      if (P.stream) __builtin_nontemporal_store(out, to);
+      if constexpr (kStream) __builtin_nontemporal_store(out, to);
       else *to = out;
     }
   }
@@ -183,6 +183,12 @@ int launch_rows(const QuantizeParams &P, Kernel kernel, hipStream_t s) {
   return hipGetLastError() == hipSuccess ? TG_OK : TG_E_HIP;
 }
 
+template <int kType, int R, int kV>
+int launch_vec(const QuantizeParams &P, hipStream_t s) {
+  return P.stream ? launch_rows<R>(P, quantize_kernel<kType, R, kV, true>, s)
+                  : launch_rows<R>(P, quantize_kernel<kType, R, kV, false>, s);
+}
+
 constexpr int kLongest = 32768;  // of a row that is kept in registers
 
 template <int kType>
@@ -191,13 +197,13 @@ int launch(const QuantizeParams &P, bool vec, hipStream_t s) {
     if (P.k <= 4096) return launch_rows<64>(P, quantize_any_kernel<kType, 64>, s);
     return launch_rows<1024>(P, quantize_any_kernel<kType, 1024>, s);
   }
-  if (P.k <= 512) return launch_rows<64>(P, quantize_kernel<kType, 64, 1>, s);
-  if (P.k <= 1024) return launch_rows<64>(P, quantize_kernel<kType, 64, 2>, s);
-  if (P.k <= 2048) return launch_rows<256>(P, quantize_kernel<kType, 256, 1>, s);
-  if (P.k <= 4096) return launch_rows<256>(P, quantize_kernel<kType, 256, 2>, s);
-  if (P.k <= 8192) return launch_rows<256>(P, quantize_kernel<kType, 256, 4>, s);
-  if (P.k <= 16384) return launch_rows<1024>(P, quantize_kernel<kType, 1024, 2>, s);
-  return launch_rows<1024>(P, quantize_kernel<kType, 1024, 4>, s);
+  if (P.k <= 512) return launch_vec<kType, 64, 1>(P, s);
+  if (P.k <= 1024) return launch_vec<kType, 64, 2>(P, s);
+  if (P.k <= 2048) return launch_vec<kType, 256, 1>(P, s);
+  if (P.k <= 4096) return launch_vec<kType, 256, 2>(P, s);
+  if (P.k <= 8192) return launch_vec<kType, 256, 4>(P, s);
+  if (P.k <= 16384) return launch_vec<kType, 1024, 2>(P, s);
+  return launch_vec<kType, 1024, 4>(P, s);
 }
 
 }  // namespace

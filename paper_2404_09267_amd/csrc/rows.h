@@ -21,15 +21,15 @@ __device__ __forceinline__ int place_in_row(int i, int e) {
   return kVec ? (i * R + t) * 8 + e : (i * 8 + e) * R + t;
 }
 
-// Chunk i of a row; zeros past n.
-template <int kType, int R, bool kVec>
-__device__ __forceinline__ Chunk<kType> load_chunk(const typename Num<kType>::E *row, int i, int n,
-                                                   bool stream) {
+// Chunk i of a row; zeros past n. kStream: past the caches.
+template <int kType, int R, bool kVec, bool kStream = false>
+__device__ __forceinline__ Chunk<kType> load_chunk(const typename Num<kType>::E *row, int i,
+                                                   int n) {
   Chunk<kType> v = {};
   if constexpr (kVec) {
     const int c = place_in_row<R, kVec>(i, 0);
     const auto *p = reinterpret_cast<const Chunk<kType> *>(row + c);
-    if (c < n) v = stream ? __builtin_nontemporal_load(p) : *p;
+    if (c < n) v = kStream ? __builtin_nontemporal_load(p) : *p;
   } else {
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
@@ -40,14 +40,14 @@ __device__ __forceinline__ Chunk<kType> load_chunk(const typename Num<kType>::E 
   return v;
 }
 
-template <int kType, int R, bool kVec>
+template <int kType, int R, bool kVec, bool kStream = false>
 __device__ __forceinline__ void store_chunk(typename Num<kType>::E *row, int i, int n,
-                                            Chunk<kType> v, bool stream) {
+                                            Chunk<kType> v) {
   if constexpr (kVec) {
     const int c = place_in_row<R, kVec>(i, 0);
     auto *p = reinterpret_cast<Chunk<kType> *>(row + c);
     if (c >= n) return;
-    if (stream) __builtin_nontemporal_store(v, p);
+    if constexpr (kStream) __builtin_nontemporal_store(v, p);
     else *p = v;
   } else {
 #pragma unroll
