@@ -35,7 +35,7 @@ struct NormParams {
 constexpr float kFar = 0x1p80f, kTiny = 0x1p-80f, kHides = 0x1p-60f;
 
 // u of a row to weight * (u [- mean]) / sqrt(mean square + eps) + bias. `turns`: LDS of 6 sums.
-template <int kType, int R, int kV, bool kVec>
+template <int kType, int R, int kV, int W>
 __device__ __forceinline__ void normalise(const NormParams &P, float (&u)[kV * 8], int kind,
                                           const void *weight, const void *bias,
                                           float (*turns)[16]) {
@@ -50,7 +50,7 @@ __device__ __forceinline__ void normalise(const NormParams &P, float (&u)[kV * 8
       for (int i = 0; i < kV; ++i)
 #pragma unroll
         for (int e = 0; e < 8; ++e)
-          if (place_in_row<R, kVec>(i, e) < n) v += u[i * 8 + e] * up;
+          if (place_in_row<R, W>(i, e) < n) v += u[i * 8 + e] * up;
       return row_sum<R>(v, turn) * share;
     };
     // Of the differences from a mean, which is rounded: their mean (what that rounding left), and
@@ -61,7 +61,7 @@ __device__ __forceinline__ void normalise(const NormParams &P, float (&u)[kV * 8
       for (int i = 0; i < kV; ++i)
 #pragma unroll
         for (int e = 0; e < 8; ++e)
-          if (place_in_row<R, kVec>(i, e) < n) {
+          if (place_in_row<R, W>(i, e) < n) {
             const float d = from(u[i * 8 + e]);
             v += d;
             w += d * d;
@@ -91,12 +91,12 @@ __device__ __forceinline__ void normalise(const NormParams &P, float (&u)[kV * 8
 #pragma unroll
   for (int i = 0; i < kV; ++i) {
     if (weight) {
-      const Chunk<kType> w = load_chunk<kType, R, kVec>(static_cast<const E *>(weight), i, n);
+      const Chunk<kType> w = load_chunk<kType, R, W>(static_cast<const E *>(weight), i, n);
 #pragma unroll
       for (int e = 0; e < 8; ++e) u[i * 8 + e] *= static_cast<float>(w[e]);
     }
     if (bias) {
-      const Chunk<kType> b = load_chunk<kType, R, kVec>(static_cast<const E *>(bias), i, n);
+      const Chunk<kType> b = load_chunk<kType, R, W>(static_cast<const E *>(bias), i, n);
 #pragma unroll
       for (int e = 0; e < 8; ++e) u[i * 8 + e] += static_cast<float>(b[e]);
     }
@@ -104,7 +104,7 @@ __device__ __forceinline__ void normalise(const NormParams &P, float (&u)[kV * 8
 }
 
 // kStream: x, y and the results go past the caches.
-template <int kType, int R, int kV, bool kVec, bool kStream>
+template <int kType, int R, int kV, int W, bool kStream>
 __global__ __launch_bounds__(kGroupThreads<R>) void norm_kernel(const NormParams P) {
   typedef typename Num<kType>::E E;
   constexpr int kRows = kGroupThreads<R> / R;
@@ -115,7 +115,7 @@ __global__ __launch_bounds__(kGroupThreads<R>) void norm_kernel(const NormParams
   Chunk<kType> xv[kV];
   const E *x = static_cast<const E *>(P.x) + t * P.x_stride;
 #pragma unroll
-  for (int i = 0; i < kV; ++i) xv[i] = load_chunk<kType, R, kVec, kStream>(x, i, n);
+  for (int i = 0; i < kV; ++i) xv[i] = load_chunk<kType, R, W, kStream>(x, i, n);
   int g = P.y ? 0 : -1;
   if (P.gate_row) g = P.gate_row[t];
   if (P.gate && (g < 0 || g >= P.n_gates)) g = -1;
@@ -124,16 +124,16 @@ __global__ __launch_bounds__(kGroupThreads<R>) void norm_kernel(const NormParams
     const E *y = static_cast<const E *>(P.y) + t * P.y_stride;
 #pragma unroll
     for (int i = 0; i < kV; ++i) {
-      const Chunk<kType> v = load_chunk<kType, R, kVec, kStream>(y, i, n);
+      const Chunk<kType> v = load_chunk<kType, R, W, kStream>(y, i, n);
 #pragma unroll
       for (int e = 0; e < 8; ++e) u[i * 8 + e] = static_cast<float>(v[e]);
     }
-    normalise<kType, R, kV, kVec>(P, u, P.y_norm, P.y_weight, P.y_bias, s_turns);
+    normalise<kType, R, kV, W>(P, u, P.y_norm, P.y_weight, P.y_bias, s_turns);
     const E *gate = P.gate ? static_cast<const E *>(P.gate) + g * P.gate_stride : nullptr;
 #pragma unroll
     for (int i = 0; i < kV; ++i) {
       if (gate) {
-        const Chunk<kType> v = load_chunk<kType, R, kVec>(gate, i, n);
+        const Chunk<kType> v = load_chunk<kType, R, W>(gate, i, n);
 #pragma unroll
         for (int e = 0; e < 8; ++e) u[i * 8 + e] *= static_cast<float>(v[e]);
       }
@@ -152,44 +152,46 @@ __global__ __launch_bounds__(kGroupThreads<R>) void norm_kernel(const NormParams
       Chunk<kType> v;
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[e] = static_cast<E>(u[i * 8 + e]);
-      store_chunk<kType, R, kVec, kStream>(row, i, n, v);
+      store_chunk<kType, R, W, kStream>(row, i, n, v);
     }
   };
   if (P.x_out) put(P.x_out, P.x_out_stride);
   if (!P.h) return;
-  normalise<kType, R, kV, kVec>(P, u, P.norm, P.weight, P.bias, s_turns + (R > 64 ? 6 : 0));
+  normalise<kType, R, kV, W>(P, u, P.norm, P.weight, P.bias, s_turns + (R > 64 ? 6 : 0));
   put(P.h, P.h_stride);
 }
 
 template <int kType, int R, int kV>
-int launch_rows(const NormParams &P, bool vec, hipStream_t s) {
+int launch_rows(const NormParams &P, int piece, hipStream_t s) {
   constexpr int kThreads = kGroupThreads<R>, kRows = kThreads / R;
   const int64_t blocks = (int64_t(P.n_tokens) + kRows - 1) / kRows;
   if (blocks > kMaxWorkgroups) return TG_E_INVAL;
   const dim3 grid = grid_of(blocks, kThreads), threads(kThreads);
-  if (vec && P.stream)
-    hipLaunchKernelGGL((norm_kernel<kType, R, kV, true, true>), grid, threads, 0, s, P);
-  else if (vec)
-    hipLaunchKernelGGL((norm_kernel<kType, R, kV, true, false>), grid, threads, 0, s, P);
+  if (piece == 8 && P.stream)
+    hipLaunchKernelGGL((norm_kernel<kType, R, kV, 8, true>), grid, threads, 0, s, P);
+  else if (piece == 8)
+    hipLaunchKernelGGL((norm_kernel<kType, R, kV, 8, false>), grid, threads, 0, s, P);
+  else if (piece == 4)
+    hipLaunchKernelGGL((norm_kernel<kType, R, kV, 4, false>), grid, threads, 0, s, P);
   else
-    hipLaunchKernelGGL((norm_kernel<kType, R, kV, false, false>), grid, threads, 0, s, P);
+    hipLaunchKernelGGL((norm_kernel<kType, R, kV, 1, false>), grid, threads, 0, s, P);
   return hipGetLastError() == hipSuccess ? TG_OK : TG_E_HIP;
 }
 
 template <int kType>
-int launch(const NormParams &P, bool vec, hipStream_t s) {
+int launch(const NormParams &P, int piece, hipStream_t s) {
   // Up to 16 values a thread, as far as that goes, and no more threads than that takes. Layer
   // norms, us with 8, 16 and 32 values a thread:
   //   300 x 1,024:      4.8, 5.7        25,600 x 1,024:  53, 50
   //   25,600 x 2,048: 100, 94, 109      12,800 x 4,096: 105, 95, 116
   //   12,800 x 8,192: 187, 212 (16, 32)
-  if (P.n <= 512) return launch_rows<kType, 64, 1>(P, vec, s);
-  if (P.n <= 1024) return launch_rows<kType, 128, 1>(P, vec, s);
-  if (P.n <= 2048) return launch_rows<kType, 128, 2>(P, vec, s);
-  if (P.n <= 4096) return launch_rows<kType, 256, 2>(P, vec, s);
-  if (P.n <= 8192) return launch_rows<kType, 512, 2>(P, vec, s);
-  if (P.n <= 16384) return launch_rows<kType, 1024, 2>(P, vec, s);
-  return launch_rows<kType, 1024, 4>(P, vec, s);
+  if (P.n <= 512) return launch_rows<kType, 64, 1>(P, piece, s);
+  if (P.n <= 1024) return launch_rows<kType, 128, 1>(P, piece, s);
+  if (P.n <= 2048) return launch_rows<kType, 128, 2>(P, piece, s);
+  if (P.n <= 4096) return launch_rows<kType, 256, 2>(P, piece, s);
+  if (P.n <= 8192) return launch_rows<kType, 512, 2>(P, piece, s);
+  if (P.n <= 16384) return launch_rows<kType, 1024, 2>(P, piece, s);
+  return launch_rows<kType, 1024, 4>(P, piece, s);
 }
 
 bool kind_ok(int32_t k) { return k >= TG_NORM_NONE && k <= TG_NORM_LAYER; }
@@ -204,8 +206,9 @@ extern "C" int tg_norm(const tg_norm_args *a, void *stream) {
   if ((a->gate && (!a->y || a->n_gates < 1)) || (a->gate_row && !a->gate)) return TG_E_INVAL;
   if (a->n_tokens == 0) return TG_OK;
   if (!a->x || (!a->x_out && !a->h)) return TG_E_INVAL;
-  bool vec = a->n % 8 == 0 && aligned16(a->y_weight) && aligned16(a->y_bias) &&
-             aligned16(a->weight) && aligned16(a->bias);
+  int piece = piece_of(8, nullptr, a->n, 2);
+  for (const void *v : {a->y_weight, a->y_bias, a->weight, a->bias})
+    piece = piece_of(piece, v, 0, 2);
   const void *rows[5] = {a->x, a->y, a->gate, a->x_out, a->h};
   const int64_t strides[5] = {a->x_stride, a->y_stride, a->gate_stride, a->x_out_stride,
                               a->h_stride};
@@ -213,7 +216,7 @@ extern "C" int tg_norm(const tg_norm_args *a, void *stream) {
   for (int i = 0; i < 5; ++i) {
     if (!rows[i]) continue;
     if (strides[i] < a->n) return TG_E_INVAL;
-    vec = vec && aligned16(rows[i]) && strides[i] % 8 == 0;
+    piece = piece_of(piece, rows[i], strides[i], 2);
     arrays += i != 2;
   }
   NormParams P = {};
@@ -243,5 +246,5 @@ extern "C" int tg_norm(const tg_norm_args *a, void *stream) {
   // against the 256 MB that the last cache holds
   P.stream = arrays * a->n_tokens * a->n * 2 > (int64_t(256) << 20);
   hipStream_t s = static_cast<hipStream_t>(stream);
-  return a->type == TG_F16 ? launch<TG_F16>(P, vec, s) : launch<TG_BF16>(P, vec, s);
+  return a->type == TG_F16 ? launch<TG_F16>(P, piece, s) : launch<TG_BF16>(P, piece, s);
 }

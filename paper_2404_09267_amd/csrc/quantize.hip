@@ -98,20 +98,18 @@ __device__ __forceinline__ uint32_t row_max(uint32_t v, uint32_t *turn) {
   return v;
 }
 
-// k a multiple of 8, rows of x on 16 bytes, of q on 8.
-template <int kType, int R, int kV, bool kStream>
+template <int kType, int R, int kV, int W, bool kStream>
 __global__ __launch_bounds__(kGroupThreads<R>) void quantize_kernel(const QuantizeParams P) {
   typedef typename Num<kType>::E E;
   constexpr int kRows = kGroupThreads<R> / R;
   __shared__ uint32_t s_turn[16];
   const int64_t t = int64_t(workgroup()) * kRows + threadIdx.x / R;
   if (t >= P.n_rows) return;  // a whole wave, or the workgroup
-  const int first = threadIdx.x % R * 8;
   const E *x = static_cast<const E *>(P.x) + t * P.x_stride;
   Chunk<kType> v[kV];
 #pragma unroll
   for (int i = 0; i < kV; ++i)
-    v[i] = load_chunk<kType, R, true, kStream>(x, i, P.k);
+    v[i] = load_chunk<kType, R, W, kStream>(x, i, P.k);
   typedef uint16_t u16x8 __attribute__((ext_vector_type(8)));
   u16x8 most = {};
 #pragma unroll
@@ -124,11 +122,10 @@ __global__ __launch_bounds__(kGroupThreads<R>) void quantize_kernel(const Quanti
   for (int e = 0; e < 8; ++e) top = max(top, static_cast<uint32_t>(most[e]));
   float scale;
   const Scale s = scale_of<kType>(row_max<R>(top, s_turn), scale);
-  if (first == 0) P.scale[t] = scale;
+  if (threadIdx.x % R == 0) P.scale[t] = scale;
   int8_t *q = P.q + t * P.q_stride;
 #pragma unroll
   for (int i = 0; i < kV; ++i) {
-    const int c = first + i * R * 8;
     float r[8];
     bool near = false;
 #pragma unroll
@@ -142,17 +139,26 @@ __global__ __launch_bounds__(kGroupThreads<R>) void quantize_kernel(const Quanti
       }
     }
     const u32x2 out = {low_bytes(r[0], r[1], r[2], r[3]), low_bytes(r[4], r[5], r[6], r[7])};
-    u32x2 *to = reinterpret_cast<u32x2 *>(q + c);
-    if (c < P.k) {
-      if constexpr (kStream) __builtin_nontemporal_store(out, to);
-      else *to = out;
+    typedef int8_t Bytes __attribute__((ext_vector_type(8)));
+    typedef int8_t Piece __attribute__((ext_vector_type(W)));
+    const Bytes all = __builtin_bit_cast(Bytes, out);
+#pragma unroll
+    for (int e = 0; e < 8; e += W) {
+      const int c = place_in_row<R, W>(i, e);
+      Piece piece;
+#pragma unroll
+      for (int f = 0; f < W; ++f) piece[f] = all[e + f];
+      Piece *to = reinterpret_cast<Piece *>(q + c);
+      if (c >= P.k) continue;
+      if constexpr (kStream) __builtin_nontemporal_store(piece, to);
+      else *to = piece;
     }
   }
 }
 
-// Any length and alignment, value by value; the row is read twice.
+// Rows longer than registers hold, value by value; the row is read twice.
 template <int kType, int R>
-__global__ __launch_bounds__(kGroupThreads<R>) void quantize_any_kernel(const QuantizeParams P) {
+__global__ __launch_bounds__(kGroupThreads<R>) void quantize_long_kernel(const QuantizeParams P) {
   typedef typename Num<kType>::E E;
   constexpr int kRows = kGroupThreads<R> / R;
   __shared__ uint32_t s_turn[16];
@@ -184,26 +190,25 @@ int launch_rows(const QuantizeParams &P, Kernel kernel, hipStream_t s) {
 }
 
 template <int kType, int R, int kV>
-int launch_vec(const QuantizeParams &P, hipStream_t s) {
-  return P.stream ? launch_rows<R>(P, quantize_kernel<kType, R, kV, true>, s)
-                  : launch_rows<R>(P, quantize_kernel<kType, R, kV, false>, s);
+int launch_pieces(const QuantizeParams &P, int piece, hipStream_t s) {
+  if (piece == 8 && P.stream) return launch_rows<R>(P, quantize_kernel<kType, R, kV, 8, true>, s);
+  if (piece == 8) return launch_rows<R>(P, quantize_kernel<kType, R, kV, 8, false>, s);
+  if (piece == 4) return launch_rows<R>(P, quantize_kernel<kType, R, kV, 4, false>, s);
+  return launch_rows<R>(P, quantize_kernel<kType, R, kV, 1, false>, s);
 }
 
 constexpr int kLongest = 32768;  // of a row that is kept in registers
 
 template <int kType>
-int launch(const QuantizeParams &P, bool vec, hipStream_t s) {
-  if (!vec || P.k > kLongest) {
-    if (P.k <= 4096) return launch_rows<64>(P, quantize_any_kernel<kType, 64>, s);
-    return launch_rows<1024>(P, quantize_any_kernel<kType, 1024>, s);
-  }
-  if (P.k <= 512) return launch_vec<kType, 64, 1>(P, s);
-  if (P.k <= 1024) return launch_vec<kType, 64, 2>(P, s);
-  if (P.k <= 2048) return launch_vec<kType, 256, 1>(P, s);
-  if (P.k <= 4096) return launch_vec<kType, 256, 2>(P, s);
-  if (P.k <= 8192) return launch_vec<kType, 256, 4>(P, s);
-  if (P.k <= 16384) return launch_vec<kType, 1024, 2>(P, s);
-  return launch_vec<kType, 1024, 4>(P, s);
+int launch(const QuantizeParams &P, int piece, hipStream_t s) {
+  if (P.k > kLongest) return launch_rows<1024>(P, quantize_long_kernel<kType, 1024>, s);
+  if (P.k <= 512) return launch_pieces<kType, 64, 1>(P, piece, s);
+  if (P.k <= 1024) return launch_pieces<kType, 64, 2>(P, piece, s);
+  if (P.k <= 2048) return launch_pieces<kType, 256, 1>(P, piece, s);
+  if (P.k <= 4096) return launch_pieces<kType, 256, 2>(P, piece, s);
+  if (P.k <= 8192) return launch_pieces<kType, 256, 4>(P, piece, s);
+  if (P.k <= 16384) return launch_pieces<kType, 1024, 2>(P, piece, s);
+  return launch_pieces<kType, 1024, 4>(P, piece, s);
 }
 
 }  // namespace
@@ -224,8 +229,8 @@ extern "C" int tg_quantize(const tg_quantize_args *a, void *stream) {
   P.k = a->k;
   // against the 256 MB that the last cache holds
   P.stream = int64_t(a->n_rows) * a->k * 3 > (int64_t(256) << 20);
-  const bool vec = a->k % 8 == 0 && aligned16(a->x) && a->x_stride % 8 == 0 &&
-                   reinterpret_cast<uintptr_t>(a->q) % 8 == 0 && a->q_stride % 8 == 0;
+  const int piece = piece_of(piece_of(piece_of(8, nullptr, a->k, 2), a->x, a->x_stride, 2), a->q,
+                             a->q_stride, 1);
   hipStream_t s = static_cast<hipStream_t>(stream);
-  return a->type == TG_F16 ? launch<TG_F16>(P, vec, s) : launch<TG_BF16>(P, vec, s);
+  return a->type == TG_F16 ? launch<TG_F16>(P, piece, s) : launch<TG_BF16>(P, piece, s);
 }
