@@ -767,22 +767,22 @@ typedef struct {
 size_t tg_pages_workspace_bytes(int32_t n_seqs, int32_t n_tokens);
 
 /*
- * Page tables and cache rows of a step, from lengths. In this order: every sequence with `release`
- * pushes its pages on the stack (sequences in order, their pages in order) and holds no rows; a
- * sequence whose new tokens end inside its pages takes none; the others ask for pages, and as long
- * as the sum of what has been asked for, up to and with the sequence, does not pass the stack, it
- * gets them, from the top. A sequence that does not, or would pass max_pages or 2^31 - 1 rows, is
- * refused: its tokens get no rows, and it keeps what it holds. Tokens before q_begin[0] and
- * from q_begin[n_seqs] on belong to nobody and get no rows, so that a batch can be padded.
- * Nothing but the order of sequences decides, so two runs give the same. With kv_len_out and
- * n_free_out apart from the inputs, and no sequence that is both released and given tokens, the
- * call can be repeated. Lengths outside [0, max_pages * page_size] count as the nearest inside,
- * n_free outside [0, n_pages] alike; q_begin outside [0, n_tokens] alike, and a sequence that ends
- * before it begins has no tokens. A table entry outside [0, n_pages) gives its tokens no row. A
- * page belongs to one sequence: nothing counts who shares it.
- * Enqueued on `stream`; the library allocates nothing. Returns TG_E_INVAL (null pointer, negative
- * count, n_seqs > TG_PAGES_MAX_SEQS, page_size < 1, max_pages outside [1, 2^20], n_pages * page_size
- * >= 2^31, a stride below max_pages), TG_E_WORKSPACE, TG_E_HIP. n_seqs == 0 and n_tokens == 0 enqueues
+ * Page tables and cache rows of a step, from lengths. In this order: every sequence with
+ * `release` pushes its pages on the stack (sequences in order, their pages in order) and holds no
+ * rows; a sequence whose new tokens end inside its pages takes none; the others ask for pages,
+ * and as long as the sum of what has been asked for, up to and with the sequence, does not pass
+ * the stack, it gets them, from the top. A sequence that does not, or would pass max_pages or
+ * 2^31 - 1 rows, is refused: its tokens get no rows, and it keeps what it holds. Tokens before
+ * q_begin[0] and from q_begin[n_seqs] on belong to nobody and get no rows, so that a batch can be
+ * padded. Nothing but the order of sequences decides, so two runs give the same. With kv_len_out
+ * and n_free_out apart from the inputs, and no sequence that is both released and given tokens,
+ * the call can be repeated. Lengths outside [0, max_pages * page_size] count as the nearest
+ * inside, n_free outside [0, n_pages] alike; q_begin outside [0, n_tokens] alike, and a sequence
+ * that ends before it begins has no tokens. A table entry outside [0, n_pages) gives its tokens
+ * no row. A page belongs to one sequence: nothing counts who shares it. Enqueued on `stream`; the
+ * library allocates nothing. Returns TG_E_INVAL (null pointer, negative count, n_seqs >
+ * TG_PAGES_MAX_SEQS, page_size < 1, max_pages outside [1, 2^20], n_pages * page_size >= 2^31, a
+ * stride below max_pages), TG_E_WORKSPACE, TG_E_HIP. n_seqs == 0 and n_tokens == 0 enqueues
  * nothing, n_seqs == 0 alone gives slot, pos, n_free_out and refused.
  */
 int tg_pages(const tg_pages_args *args, void *stream);
@@ -824,19 +824,20 @@ size_t tg_attend_pages_workspace_bytes(int32_t n_seqs, int32_t max_kv_len, int32
  * Attention of one new token a sequence over its pages. With n = kv_len[s], the score with key j is
  *   z = scale * (q . k_j);  with cap z = cap * tanh(z / cap);
  *   with slope z -= slope[h] * (n - 1 - j);
- * and the query sees keys j < min(n, max_kv_len, max_pages * page_size) with window == 0 or
- * j >= n - window, but none on a page outside [0, n_pages). The output is the softmax-weighted sum
- * of the v_j it sees, 0 if it sees none (kv_len <= 0 among them; such rows are written, but no row that
- * is no sequence's query), NaN if all its scores are minus infinity. Rows that it does not see are not read. Weights are rounded to
- * the type before the product with v, in binary16 as 2^7 times their share of the largest or more;
- * their sum is of the rounded ones. An infinite value whose weight rounds to 0 makes NaN. Distances
- * up to 2^24 are exact.
- * out must not overlap an input. Enqueued on `stream`; allocates nothing. Returns TG_E_INVAL (null
- * pointer, negative count, n_seqs > TG_PAGES_MAX_SEQS, max_kv_len > 2^30, d outside [8,
- * TG_ATTEND_MAX_D] or not a multiple of 8, heads that n_kv_heads does not divide, a negative
- * window, page_size or max_pages < 1, n_pages * page_size >= 2^31, a bad type, scale or cap, a table_stride below max_pages, q, k, v or out not
- * 16-byte aligned, another stride that is negative, not a multiple of 8 or, of rows, over 2^22),
- * TG_E_WORKSPACE, TG_E_HIP. n_seqs == 0, or n_q_rows == 0 with q_begin, enqueues nothing.
+ * and the query sees keys j < min(n, max_kv_len, max_pages * page_size) with window == 0 or j >=
+ * n - window, but none on a page outside [0, n_pages). The output is the softmax-weighted sum of
+ * the v_j it sees, 0 if it sees none (kv_len <= 0 among them; such rows are written, but no row
+ * that is no sequence's query), NaN if all its scores are minus infinity. Rows that it does not
+ * see are not read. Weights are rounded to the type before the product with v, in binary16 as 2^7
+ * times their share of the largest or more; their sum is of the rounded ones. An infinite value
+ * whose weight rounds to 0 makes NaN. Distances up to 2^24 are exact. out must not overlap an
+ * input. Enqueued on `stream`; allocates nothing. Returns TG_E_INVAL (null pointer, negative
+ * count, n_seqs > TG_PAGES_MAX_SEQS, max_kv_len > 2^30, d outside [8, TG_ATTEND_MAX_D] or not a
+ * multiple of 8, heads that n_kv_heads does not divide, a negative window, page_size or max_pages
+ * < 1, n_pages * page_size >= 2^31, a bad type, scale or cap, a table_stride below max_pages, q,
+ * k, v or out not 16-byte aligned, another stride that is negative, not a multiple of 8 or, of
+ * rows, over 2^22), TG_E_WORKSPACE, TG_E_HIP. n_seqs == 0, or n_q_rows == 0 with q_begin,
+ * enqueues nothing.
  */
 int tg_attend_pages(const tg_attend_pages_args *args, void *stream);
 
@@ -879,12 +880,11 @@ typedef struct {
  *   r[t] = x_scale * x[t] + y_scale * gate[gate_row[t]] * N_y(y[t]),
  *   x_out[t] = r[t],  h[t] = N(r[t]).
  * r is kept in binary32 between the two, and each output rounded once. Sums of squares that leave
- * binary32 are formed again from scaled values. A weight or bias without its norm is applied all the
- * same.
- * x_out and h must not overlap each other, nor an input but as above. Enqueued on `stream`;
- * allocates nothing. Returns TG_E_INVAL (x NULL, x_out and h both NULL, negative count, n outside
- * [1, TG_NORM_MAX_N], a bad kind, type, eps, scale or stride, y NULL with a gate, gate_row without
- * gate, gate with n_gates < 1), TG_E_HIP. n_tokens == 0 enqueues nothing.
+ * binary32 are formed again from scaled values. A weight or bias without its norm is applied all
+ * the same. x_out and h must not overlap each other, nor an input but as above. Enqueued on
+ * `stream`; allocates nothing. Returns TG_E_INVAL (x NULL, x_out and h both NULL, negative count,
+ * n outside [1, TG_NORM_MAX_N], a bad kind, type, eps, scale or stride, y NULL with a gate,
+ * gate_row without gate, gate with n_gates < 1), TG_E_HIP. n_tokens == 0 enqueues nothing.
  */
 int tg_norm(const tg_norm_args *args, void *stream);
 
@@ -901,11 +901,11 @@ typedef struct {
 /*
  * Rows (tokens, or a weight's outputs) to 8-bit integers with a scale each:
  *   scale[t] = max_i |x[t][i]| / 127, rounded to binary32;  q[t][i] = x[t][i] / scale[t], the
- * exact quotient rounded to the nearest integer, ties to even, at most 127 either way. A row of zeros
- * has scale 0 and integers 0. A row with an infinity or NaN has no such integers: its scale is NaN
- * and they are 0, so that its products are NaN, and those of no other row.
- * q must not overlap x. Enqueued on `stream`; allocates nothing. Returns TG_E_INVAL (null pointer,
- * negative count, k < 1, a bad type or stride), TG_E_HIP. n_rows == 0 enqueues nothing.
+ * exact quotient rounded to the nearest integer, ties to even, at most 127 either way. A row of
+ * zeros has scale 0 and integers 0. A row with an infinity or NaN has no such integers: its scale
+ * is NaN and they are 0, so that its products are NaN, and those of no other row. q must not
+ * overlap x. Enqueued on `stream`; allocates nothing. Returns TG_E_INVAL (null pointer, negative
+ * count, k < 1, a bad type or stride), TG_E_HIP. n_rows == 0 enqueues nothing.
  */
 int tg_quantize(const tg_quantize_args *args, void *stream);
 
@@ -932,7 +932,8 @@ typedef struct {
  * binary32, and the result once to the type. All 256 integers may occur. y must not overlap an
  * input. Enqueued on `stream`; allocates nothing and needs no workspace. Returns TG_E_INVAL (null
  * pointer, negative count, k outside [16, TG_PROJECT_I8_MAX_K] or not a multiple of 16, n < 1,
- * n_tokens or n over 2^30, a bad type or stride, x or w not 16-byte aligned), TG_E_HIP. n_tokens == 0 enqueues nothing.
+ * n_tokens or n over 2^30, a bad type or stride, x or w not 16-byte aligned), TG_E_HIP. n_tokens
+ * == 0 enqueues nothing.
  */
 int tg_project_i8(const tg_project_i8_args *args, void *stream);
 

@@ -571,8 +571,8 @@ __global__ __launch_bounds__(kWaves * 64) void attend_pages_kernel(const AttendP
   }
 }
 
-// Joins the parts of a query head: a workgroup each, 32 lanes a part with 4 values each. Up to 64 parts
-// have all their loads under way at once; of more, the weights are found first (1 sequence of
+// Joins the parts of a query head: a workgroup each, 32 lanes a part with 4 values each. Up to 64
+// parts have all their loads under way at once; of more, the weights are found first (1 sequence of
 // 100,003 keys, 4 heads over one, 391 parts: 28 -> 22 us in all).
 constexpr int kPlaces = 512;  // ranges at most
 constexpr int kJoinThreads = 256;
@@ -828,8 +828,8 @@ extern "C" int tg_attend_pages(const tg_attend_pages_args *a, void *stream) {
   P.least = form.least;
   // Heads that share lines of 128 bytes, or more than 16 query heads that share a key head, would
   // have them read once for each XCD; with few sequences all XCDs are wanted. us without and with:
-  // 8 sequences of 100,003 keys, 16 heads of 96 over 2: 95, 86; 8 of 60,000, 32 heads of 128 over 1:
-  // 68, 51; 64 of 900, 16 heads of 80 over 4: 17.2, 14.8.
+  // 8 sequences of 100,003 keys, 16 heads of 96 over 2: 95, 86; 8 of 60,000, 32 heads of 128 over
+  // 1: 68, 51; 64 of 900, 16 heads of 80 over 4: 17.2, 14.8.
   const bool share = P.row_tiles > 1 ||
                      (a->n_kv_heads > 1 && (a->k_head_stride % 64 || a->v_head_stride % 64));
   P.near = share && (P.width > 0 ? P.width : P.n_seqs) >= kNear;

@@ -296,7 +296,8 @@ extern "C" size_t tg_pages_workspace_bytes(int32_t n_seqs, int32_t n_tokens) {
 
 extern "C" int tg_pages(const tg_pages_args *a, void *stream) {
   if (!a || a->n_seqs < 0 || a->n_seqs > TG_PAGES_MAX_SEQS || a->n_tokens < 0 || a->n_pages < 0 ||
-      a->page_size < 1 || a->max_pages < 1 || a->max_pages > kMaxPages || a->table_stride < a->max_pages ||
+      a->page_size < 1 || a->max_pages < 1 || a->max_pages > kMaxPages ||
+      a->table_stride < a->max_pages ||
       int64_t(a->n_pages) * a->page_size > INT32_MAX)
     return TG_E_INVAL;
   if (a->n_seqs == 0 && a->n_tokens == 0) return TG_OK;
@@ -331,7 +332,8 @@ extern "C" int tg_pages(const tg_pages_args *a, void *stream) {
   hipStream_t s = static_cast<hipStream_t>(stream);
   hipLaunchKernelGGL(pages_kernel, dim3(1), dim3(kThreads), 0, s, P);
   if (P.start) {
-    const int64_t blocks = (int64_t(P.n_tokens) + kSlotThreads * kEach - 1) / (kSlotThreads * kEach);
+    const int64_t each = kSlotThreads * kEach;
+    const int64_t blocks = (P.n_tokens + each - 1) / each;
     hipLaunchKernelGGL(slots_kernel, grid_of(blocks, kSlotThreads), dim3(kSlotThreads), 0, s, P);
   }
   return hipGetLastError() == hipSuccess ? TG_OK : TG_E_HIP;

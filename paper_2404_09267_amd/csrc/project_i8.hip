@@ -1,13 +1,19 @@
 // tg_project_i8: a projection in 8-bit integers, y = (x_scale w_scale) (x w^T), sums exact in 32
 // bits.
 //
-// Few tokens: reading w bounds it. A workgroup takes 16 outputs and up to 64 tokens, its waves
-// parts of k in turn, straight from memory to the matrix instructions' registers, and the waves'
-// sums are joined through LDS: one launch, no workspace. Many tokens: tiles of x and w go through
-// LDS to the matrix instructions, several steps of 128 values of k under way. Results lie
-// transposed in the registers (a lane holds 4 outputs of one token), so that stores are contiguous
-// and a token's scale belongs to the lane. Both operands take the same values of k in the same
-// places, so that the order within an instruction does not matter.
+// Few tokens: reading w bounds it. A workgroup takes 16 outputs and 16 tokens, its waves parts of k
+// in turn, straight from memory to the matrix instructions' registers, and the waves' sums are
+// joined through LDS: one launch, no workspace.
+//
+// Many tokens: tiles of x and w go through LDS to the matrix instructions, several steps of 128
+// values of k under way; how fast they get there bounds it (13 to 17 bytes a cycle and CU, the
+// matrix units at work 54 % of the time). bfloat16: 25,600 x 4,096, k 4,096: 352 us, 2.44 POPS (a
+// library's product, which gives sums of 32 bits, 420; its best at any size 2.5 POPS); 8,192 x
+// 8,192, k 8,192: 414, 2.66; 8 x 1,536, k 1,024: 3.5, a launch.
+//
+// Results lie transposed in the registers (a lane holds 4 outputs of one token), so that stores are
+// contiguous and a token's scale belongs to the lane. Both operands take the same values of k in
+// the same places, so that the order within an instruction does not matter.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -38,7 +44,8 @@ __device__ __forceinline__ i32x4 mfma(i32x4 a, i32x4 b, i32x4 c) {
   return __builtin_amdgcn_mfma_i32_16x16x64_i8(a, b, c, 0, 0, 0);
 }
 
-// Scales of the tokens and outputs that a lane has results of; of the nearest inside where it has none.
+// Scales of the tokens and outputs that a lane has results of; of the nearest inside where it has
+// none.
 __device__ __forceinline__ float scale_of(const ProjectParams &P, int t) {
   return P.x_scale[min(t, P.n_tokens - 1)];
 }
@@ -70,15 +77,15 @@ __device__ __forceinline__ void put(const ProjectParams &P, int t, int n, i32x4 
   }
 }
 
-// The same of two blocks of 16 outputs where rows of y start on 16 bytes, 8 outputs a lane: lanes of
-// odd rows of 16 give the first block's for the second's of the row before, so that a token's 64
-// bytes are stored at once (25,600 x 4,096, k 4,096: 368 -> 355 us), and where those are whole lines'
-// halves past the caches (6,400 x 1,536, k 1,024: 18.0 -> 14.5, through the caches 16.8; but 4,000 x
-// 1,000, whose rows start elsewhere, 9.7 for 8.6). Unaligned stores of 16 bytes are slower than those
-// of 8 (1,777 x 2,051, k 1,168: 13.1 for 12.7).
+// The same of two blocks of 16 outputs where rows of y start on 16 bytes, 8 outputs a lane: lanes
+// of odd rows of 16 give the first block's for the second's of the row before, so that a token's 64
+// bytes are stored at once (25,600 x 4,096, k 4,096: 368 -> 355 us), and where those are whole
+// lines' halves past the caches (6,400 x 1,536, k 1,024: 18.0 -> 14.5, through the caches 16.8; but
+// 4,000 x 1,000, whose rows start elsewhere, 9.7 for 8.6). Unaligned stores of 16 bytes are slower
+// than those of 8 (1,777 x 2,051, k 1,168: 13.1 for 12.7).
 template <int kType>
-__device__ __forceinline__ void put_pair(const ProjectParams &P, int t, int n0, i32x4 one, i32x4 two,
-                                         float xs, f32x4 ws_one, f32x4 ws_two) {
+__device__ __forceinline__ void put_pair(const ProjectParams &P, int t, int n0, i32x4 one,
+                                         i32x4 two, float xs, f32x4 ws_one, f32x4 ws_two) {
   typedef typename Num<kType>::E E;
   typedef typename Num<kType>::V4 V4;
   typedef typename Num<kType>::V8 V8;
@@ -370,6 +377,9 @@ int launch_few(ProjectParams P, hipStream_t s) {
   return hipGetLastError() == hipSuccess ? TG_OK : TG_E_HIP;
 }
 
+// Few tokens go without LDS as long as their rows, which every 16 outputs read again, are less than
+// the weights are worth: 16 x 4,096, k 4,096 5.5 us for 8.0 with tiles of 64 x 32, 64 x 1,536, k
+// 1,024 3.9 for 4.4, but 32 x 4,096, k 4,096 10.2 for 8.3 and 16 x 8,192, k 8,192 16.7 for 13.4.
 template <int kType>
 int launch(const ProjectParams &P, hipStream_t s) {
   const int64_t weights = int64_t(P.n) * P.k;
@@ -378,15 +388,34 @@ int launch(const ProjectParams &P, hipStream_t s) {
   const auto tiles = [&](int t, int n) {
     return ((int64_t(P.n_tokens) + t - 1) / t) * ((int64_t(P.n) + n - 1) / n);
   };
+  // Large problems take the tile with the least time for its rounds of workgroups, one or two a CU;
+  // a round of 192 x 128, 160 x 128, 192 x 256 and 256 x 256 takes 0.75, 1.13, 1.28 and 1.60 times
+  // one of 128 x 128, the quarters that are left of 256 x 256 0.70. Fewer tiles than CUs: one a CU,
+  // by 8 waves with more steps under way, and smaller ones where few even of those would be busy.
+  // Measured (bfloat16, us) with tiles of 256 x 256, 192 x 256, 160 x 128, 128 x 128, 192 x 128,
+  // and one a CU 128 x 128, 128 x 64, 64 x 64, 64 x 32:
+  //   25,600 x 4,096, k 4,096: 411, 439, 449, 476
+  //    8,192 x 8,192, k 4,096: 253,  -,   -,  338, 292
+  //    6,400 x 1,536, k 1,024:  27,  23,  21,  26,   -,  27, 25, 27
+  //    5,000 x 1,536, k 4,096:  53,   -,  41,  37,  50,  38, 42
+  //    3,202 x 1,560, k 3,232:  48,   -,  37,  36,  27,  40, 37
+  //    2,917 x 1,320, k 1,600:  30,   -,  19,  17,  16,  13, 15
+  //    1,777 x 2,051, k 1,168:   -,  27,  19,   -,  18,  14, 15, 17, 21
+  //      512 x 4,096, k 4,096:   -,  40,  28,   -,   -,  19, 15, 17, 22
+  //    1,000 x 1,024, k 2,048:   -,  26,  19,   -,   -,  12, 10,  7,  8
+  //      300 x   300, k 4,096:   -,  39,  25,   -,   -,  17, 13, 10,  8
   if (tiles(128, 128) > kCus) {
-    const auto rounds = [&](int t, int n, int at_once) { return (tiles(t, n) + at_once - 1) / at_once; };
-    const int64_t t256 = tiles(256, 256);
-    const int64_t c256 = 160 * ((t256 - rest_of(t256) + kCus - 1) / kCus) + (rest_of(t256) ? 70 : 0);
-    const int64_t c192 = 128 * rounds(192, 256, kCus);
+    const auto rounds = [&](int t, int n, int at_once) {
+      return (tiles(t, n) + at_once - 1) / at_once;
+    };
+    const int64_t t256 = tiles(256, 256), rest = rest_of(t256);
+    const int64_t c256 = 160 * ((t256 - rest + kCus - 1) / kCus) + (rest ? 70 : 0);
+    const int64_t c192 = 128 * rounds(192, 256, kCus), half = 75 * rounds(192, 128, kCus);
     const int64_t c160 = 113 * rounds(160, 128, 2 * kCus), c128 = 100 * rounds(128, 128, 2 * kCus);
-    const int64_t least = std::min(std::min(c256, c192), std::min(c160, c128));
+    const int64_t least = std::min({c256, c192, half, c160, c128});
     if (c256 == least) return launch_tiles<kType, 256, 256, 2, 4, 2>(P, s);
     if (c192 == least) return launch_tiles<kType, 192, 256, 4, 2, 2>(P, s);
+    if (half == least) return launch_tiles<kType, 192, 128, 4, 2, 3>(P, s);
     if (c160 == least) return launch_tiles<kType, 160, 128, 2, 2, 2>(P, s);
     return launch_tiles<kType, 128, 128, 2, 2, 2>(P, s);
   }

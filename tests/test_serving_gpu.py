@@ -682,7 +682,8 @@ def test_quantize_ties(dtype):
 PROJECT = [(1, 16, 1), (1, 64, 300), (7, 1024, 130), (8, 1024, 1536), (16, 80, 17), (17, 112, 129),
            (33, 512, 64), (64, 208, 96), (64, 4096, 33), (65, 144, 257), (129, 320, 200),
            (300, 192, 384), (513, 96, 515), (700, 1024, 1000), (2048, 128, 2048), (3000, 272, 1500),
-           (5000, 64, 1111), (2500, 64, 4100)]
+           (5000, 64, 1111), (2500, 64, 4100), (2100, 144, 2100), (4352, 64, 4096), (6400, 64, 1536),
+           (3500, 80, 2048), (1500, 96, 1000)]
 
 
 def signed(g, *shape):
