@@ -2,8 +2,8 @@
 //
 // x and y are read once and the residual and its norm written once, 8 bytes a value, and everything
 // between is kept in registers: that is what bounds it (25,600 x 4,096 in bfloat16, gates of 20
-// cameras, a layer norm of y and a norm of the result: 177 us, 4.7 TB/s where a large copy reaches
-// 4.9; 20 x 1,024: 4 us, a launch and two loads in a row). A row is a wave's or a workgroup's, of
+// cameras, a layer norm of y and a norm of the result: 157 us, 5.3 TB/s where a large copy reaches
+// 4.9; 20 x 1,024: 3.7 us, a launch and two loads in a row). A row is a wave's or a workgroup's, of
 // 128 to 1,024 threads, so that a thread has 8 to 32 values. The variance is of the differences
 // from the mean, which costs a second sum over the row but no digits, where sum and sum of squares
 // at once would cancel; and what rounding the mean has left is taken off with it, as a row that
@@ -44,31 +44,42 @@ __device__ __forceinline__ void normalise(const NormParams &P, float (&u)[kV * 8
   const float share = 1.0f / static_cast<float>(n);
   if (kind != TG_NORM_NONE) {
     const bool layer = kind == TG_NORM_LAYER;
-    const auto mean_of = [&](float up, float *turn) {
-      float v = 0.0f;
+    // what each value of the row, and nothing past it, is given to
+    const auto each = [&](auto &&take) {
 #pragma unroll
-      for (int i = 0; i < kV; ++i)
+      for (int i = 0; i < kV; ++i) {
+        if (W == 8 && place_in_row<R, W>(i, 0) >= n) continue;
 #pragma unroll
         for (int e = 0; e < 8; ++e)
-          if (place_in_row<R, W>(i, e) < n) v += u[i * 8 + e] * up;
+          if (W == 8 || place_in_row<R, W>(i, e) < n) take(u[i * 8 + e]);
+      }
+    };
+    const auto mean_of = [&](float up, float *turn) {
+      float v = 0.0f;
+      each([&](float x) { v += x * up; });
       return row_sum<R>(v, turn) * share;
     };
     // Of the differences from a mean, which is rounded: their mean (what that rounding left), and
     // their mean square less its square.
     const auto spread = [&](auto &&from, float &left, float *turn) {
       float v = 0.0f, w = 0.0f;
-#pragma unroll
-      for (int i = 0; i < kV; ++i)
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-          if (place_in_row<R, W>(i, e) < n) {
-            const float d = from(u[i * 8 + e]);
-            v += d;
-            w += d * d;
-          }
+      left = 0.0f;
+      if (!layer) {
+        each([&](float x) {
+          const float d = from(x);
+          w += d * d;
+        });
+        return row_sum<R>(w, turn) * share;
+      }
+      each([&](float x) {
+        const float d = from(x);
+        v += d;
+        w += d * d;
+      });
       w = row_sum<R>(w, turn) * share;
-      left = layer ? row_sum<R>(v, turn + 16) * share : 0.0f;
-      return layer ? fmaxf(w - left * left, 0.0f) : w;  // of NaN, `left` is NaN
+      left = row_sum<R>(v, turn + 16) * share;
+      // fused: `left` squared may pass binary32 where w does, and inf - inf would come out as 0
+      return fmaxf(__builtin_fmaf(-left, left, w), 0.0f);  // of NaN, `left` is NaN
     };
     float left, mean = layer ? mean_of(1.0f, turns[0]) : 0.0f;
     float square = spread([&](float v) { return v - mean; }, left, turns[1]);
@@ -178,15 +189,24 @@ int launch_rows(const NormParams &P, int piece, hipStream_t s) {
   return hipGetLastError() == hipSuccess ? TG_OK : TG_E_HIP;
 }
 
+constexpr int64_t kFew = int64_t(1) << 22;
+
 template <int kType>
 int launch(const NormParams &P, int piece, hipStream_t s) {
-  // Up to 16 values a thread, as far as that goes, and no more threads than that takes. Layer
-  // norms, us with 8, 16 and 32 values a thread:
-  //   300 x 1,024:      4.8, 5.7        25,600 x 1,024:  53, 50
-  //   25,600 x 2,048: 100, 94, 109      12,800 x 4,096: 105, 95, 116
-  //   12,800 x 8,192: 187, 212 (16, 32)
+  // 8 values a thread where there is little to do and latency counts, 16 where there is more, as
+  // far as that goes, and no more threads than that takes. Two layer norms, us with 8, 16 and 32
+  // values a thread:
+  //   20 x 1,024:      4.6,  5.4        64 x 8,192:      5.9,  6.6
+  //   3,200 x 1,024:   9.2,  9.7        1,600 x 2,048:   9.8, 10.2
+  //   6,400 x 1,024:  14.6, 13.4, 17.6  1,600 x 4,096:  15.5, 14.4
+  //   25,600 x 2,048: 91.9, 81.2, 82.7  25,600 x 4,096: 186, 161, 172
+  const bool few = int64_t(P.n_tokens) * P.n <= kFew;
   if (P.n <= 512) return launch_rows<kType, 64, 1>(P, piece, s);
-  if (P.n <= 1024) return launch_rows<kType, 128, 1>(P, piece, s);
+  if (few && P.n <= 1024) return launch_rows<kType, 128, 1>(P, piece, s);
+  if (few && P.n <= 2048) return launch_rows<kType, 256, 1>(P, piece, s);
+  if (few && P.n <= 4096) return launch_rows<kType, 512, 1>(P, piece, s);
+  if (few && P.n <= 8192) return launch_rows<kType, 1024, 1>(P, piece, s);
+  if (P.n <= 1024) return launch_rows<kType, 64, 2>(P, piece, s);
   if (P.n <= 2048) return launch_rows<kType, 128, 2>(P, piece, s);
   if (P.n <= 4096) return launch_rows<kType, 256, 2>(P, piece, s);
   if (P.n <= 8192) return launch_rows<kType, 512, 2>(P, piece, s);

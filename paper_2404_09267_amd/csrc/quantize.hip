@@ -5,8 +5,8 @@
 // the scale's inverse is off by 127 * 2^-23 at most, so only where it lies within kNear of a tie is
 // the quotient looked at: x - r scale is exact in binary32 (both are multiples of the scale's last
 // bit, and at most as far apart as the scale), and half the scale decides.
-// bfloat16, 25,600 x 4,096: 55 us, 5.7 TB/s, as part of it stays in the last cache; 1,777 x 1,160:
-// 3.8 us, a launch.
+// bfloat16, 25,600 x 4,096: 50 us, 6.3 TB/s, as part of it stays in the last cache; 1,777 x 1,160:
+// 3.7 us, a launch.
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
@@ -57,13 +57,6 @@ __device__ __forceinline__ Scale scale_of(uint32_t bits, float &out) {
   return {up, out * up, 1.0f / (out * up)};
 }
 
-// The integer of a value, as a float whose low byte it is.
-__device__ __forceinline__ float whole(float t, bool &near) {
-  const float with = t + kRound;
-  near = near || fabsf(t - (with - kRound)) > 0.5f - kNear;
-  return with;
-}
-
 __device__ __forceinline__ float decided(float x, float t, const Scale &s) {
   float r = (t + kRound) - kRound;
   const float left = __builtin_fmaf(-r, s.scale, x), half = 0.5f * s.scale;
@@ -75,6 +68,28 @@ __device__ __forceinline__ float decided(float x, float t, const Scale &s) {
 // NaN and infinity times 0 are left out: such rows have integers 0.
 __device__ __forceinline__ float lifted(float x, const Scale &s) {
   return s.up == 0.0f ? 0.0f : x * s.up;
+}
+
+// The integers of 8 values, each as a float whose low byte it is.
+template <int kType>
+__device__ __forceinline__ void integers(const Chunk<kType> &v, const Scale &s, float (&r)[8]) {
+  float far = 1.0f;  // rows of zeros, and those that are lifted, are not for the short way
+  if (s.up == 1.0f) {
+    far = 0.0f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const float x = static_cast<float>(v[e]);
+      r[e] = __builtin_fmaf(x, s.inverse, kRound);
+      far = fmaxf(far, fabsf(__builtin_fmaf(x, s.inverse, -(r[e] - kRound))));
+    }
+  }
+  if (__ballot(far > 0.5f - kNear)) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const float a = lifted(static_cast<float>(v[e]), s);
+      r[e] = decided(a, a * s.inverse, s);
+    }
+  }
 }
 
 __device__ __forceinline__ uint32_t low_bytes(float a, float b, float c, float d) {
@@ -127,17 +142,7 @@ __global__ __launch_bounds__(kGroupThreads<R>) void quantize_kernel(const Quanti
 #pragma unroll
   for (int i = 0; i < kV; ++i) {
     float r[8];
-    bool near = false;
-#pragma unroll
-    for (int e = 0; e < 8; ++e)
-      r[e] = whole(lifted(static_cast<float>(v[i][e]), s) * s.inverse, near);
-    if (__ballot(near)) {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const float a = lifted(static_cast<float>(v[i][e]), s);
-        r[e] = decided(a, a * s.inverse, s);
-      }
-    }
+    integers<kType>(v[i], s, r);
     const u32x2 out = {low_bytes(r[0], r[1], r[2], r[3]), low_bytes(r[4], r[5], r[6], r[7])};
     typedef int8_t Bytes __attribute__((ext_vector_type(8)));
     typedef int8_t Piece __attribute__((ext_vector_type(W)));
@@ -202,11 +207,15 @@ constexpr int kLongest = 32768;  // of a row that is kept in registers
 template <int kType>
 int launch(const QuantizeParams &P, int piece, hipStream_t s) {
   if (P.k > kLongest) return launch_rows<1024>(P, quantize_long_kernel<kType, 1024>, s);
+  // 16 values a thread, as far as that goes. us with 8, 16 and 32:
+  //   20 x 8,192:      3.5,  3.3,  4.1  1,600 x 2,048:  3.9,  4.1,  4.8
+  //   25,600 x 1,024: 14.9, 13.7, 15.6  25,600 x 2,048: 31.5, 28.9, 29.4
+  //   25,600 x 4,096: 58.7, 49.6, 49.9  25,600 x 8,192:  119, 95.9, 98.6
   if (P.k <= 512) return launch_pieces<kType, 64, 1>(P, piece, s);
   if (P.k <= 1024) return launch_pieces<kType, 64, 2>(P, piece, s);
-  if (P.k <= 2048) return launch_pieces<kType, 256, 1>(P, piece, s);
+  if (P.k <= 2048) return launch_pieces<kType, 128, 2>(P, piece, s);
   if (P.k <= 4096) return launch_pieces<kType, 256, 2>(P, piece, s);
-  if (P.k <= 8192) return launch_pieces<kType, 256, 4>(P, piece, s);
+  if (P.k <= 8192) return launch_pieces<kType, 512, 2>(P, piece, s);
   if (P.k <= 16384) return launch_pieces<kType, 1024, 2>(P, piece, s);
   return launch_pieces<kType, 1024, 4>(P, piece, s);
 }

@@ -586,6 +586,22 @@ def test_norm_far_from_one(n, kind):
     assert bool(((ho - int(kind == 1)).abs() <= 2.0 ** -7).all())
 
 
+@pytest.mark.parametrize("n", [520, 1024, 1999, 2040, 4092, 4096, 8184, 8191])
+def test_norm_many(n):
+    """Rows of more than 2^22 values together, some of them with squares past binary32."""
+    say("norm many", n)
+    tokens = (1 << 22) // n + 3
+    g, dt = gen(n), torch.bfloat16
+    for kind in (1, 2):
+        x, y, yw, yb, gate, row, w, b = norm_inputs(g, tokens, n, dt, 3)
+        x[5], x[tokens - 1] = x[5] * 1e30, x[tokens - 1] * 1e30
+        more = dict(y_norm=kind, y_weight=yw, gate=gate, gate_row=row, weight=w, bias=b, eps=1e-5)
+        (r, er), (h, eh) = R.norm(x, y, kind=kind, **more)
+        xo, ho = run_norm(x, y, norm=kind, **more)
+        R_assert(xo.cpu(), r, er, "x_out")
+        R_assert(ho.cpu(), h, eh, "h")
+
+
 def test_norm_large_offset():
     """A mean far larger than the spread: variance from differences, not from sums of squares."""
     say("norm offset")
