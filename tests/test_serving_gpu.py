@@ -807,6 +807,27 @@ def test_rows_past_32_bits():
     assert int((y != 0).any(1).sum()) == 3
 
 
+@pytest.mark.parametrize("n", [512, 1024, 2048, 4096, 8192, 16384, 32768])
+def test_rows_past_the_caches(n):
+    """Results that pass the caches are those of the same rows in calls that do not."""
+    say("past the caches", n)
+    rows, part = (96 << 20) // n + 1, (20 << 20) // n  # of 2^22 values or more, each
+    g = torch.Generator("cuda").manual_seed(n)
+    x, y = (torch.randn((rows, n), generator=g, device="cuda").bfloat16() for _ in range(2))
+    xo, h = torch.full_like(x, NAN), torch.full_like(x, NAN)
+    q = torch.full((rows, n), 77, dtype=torch.int8, device="cuda")
+    s = torch.full((rows,), -1.0, device="cuda")
+    more = dict(y_norm=tg.NORM_LAYER, norm=tg.NORM_RMS)
+    tg.norm(x, xo, h, y=y, **more)
+    tg.quantize(x, q, s)
+    for t in range(0, rows, part):
+        xs, hs, qs, ss = (torch.empty_like(a[t:t + part]) for a in (xo, h, q, s))
+        tg.norm(x[t:t + part], xs, hs, y=y[t:t + part], **more)
+        tg.quantize(x[t:t + part], qs, ss)
+        for got, want in ((xo, xs), (h, hs), (q, qs), (s, ss)):
+            assert torch.equal(got[t:t + part], want)
+
+
 def operators(seed):
     """A call of each operator as (outputs, function of a stream), on inputs of its own."""
     g, dt = gen(seed), torch.bfloat16
