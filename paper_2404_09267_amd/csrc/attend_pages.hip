@@ -17,8 +17,8 @@
 // cut into as many ranges of one length as there is room for workgroups, found on the device, so
 // that each has as much to read whatever the lengths are; a workgroup goes from sequence to
 // sequence, and join_kernel joins what a sequence has in several ranges, in a set order. bfloat16:
-// 8 sequences of up to 100,003 keys, 16 heads of 128 over 2, 583 MB: 111 us, 5.2 TB/s; 256 of up to
-// 4,096, 32 heads over 8, 2.4 GB: 437 us, 5.4; 20 of up to 1,600, 16 heads of 64 over 4: 13 us, a
+// 8 sequences of up to 100,003 keys, 16 heads of 128 over 2, 583 MB: 111 us, 5.3 TB/s; 256 of up to
+// 4,096, 32 heads over 8, 2.4 GB: 440 us, 5.4; 20 of up to 1,600, 16 heads of 64 over 4: 13 us, a
 // launch and a chain of loads (length, pages, keys, and those of 6 tiles a wave).
 #include <hip/hip_runtime.h>
 
@@ -697,6 +697,8 @@ int64_t each_of(int n_heads, int n_kv_heads) {  // workgroups of a sequence
 //     256 sequences,   500, 16 heads of 64 over 2:      12 (11), 35
 //   1,000 sequences,   900, 8 heads of 128 over 1:      64 (58), 106
 //       8 sequences, 100,003, 16 heads of 128 over 2:  937 (1,107), 111
+// 16 waves, of heads of 64: 13.3 for 13.1 where 20 have 1,600 keys, 73.8 for 65.8 where 256 have
+// 2,000.
 constexpr int kWholeNarrow = 1536, kWholeWide = 1024, kWholeOfMany = 2048, kWholeOfAll = 4096;
 
 Form form_of(int n_seqs, int max_kv, int64_t each, int d) {

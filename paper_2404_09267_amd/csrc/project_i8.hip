@@ -6,10 +6,10 @@
 // joined through LDS: one launch, no workspace.
 //
 // Many tokens: tiles of x and w go through LDS to the matrix instructions, several steps of 128
-// values of k under way; how fast they get there bounds it (13 to 17 bytes a cycle and CU, the
-// matrix units at work 54 % of the time). bfloat16: 25,600 x 4,096, k 4,096: 352 us, 2.44 POPS (a
+// values of k under way; how fast they get there bounds it (the matrix units are at work 64 % of
+// the time). bfloat16: 25,600 x 4,096, k 4,096: 346 to 363 us by card, 2.37 to 2.48 POPS (a
 // library's product, which gives sums of 32 bits, 420; its best at any size 2.5 POPS); 8,192 x
-// 8,192, k 8,192: 414, 2.66; 8 x 1,536, k 1,024: 3.5, a launch.
+// 8,192, k 8,192: 414 to 423, 2.6; 8 x 1,536, k 1,024: 3.5, a launch.
 //
 // Results lie transposed in the registers (a lane holds 4 outputs of one token), so that stores are
 // contiguous and a token's scale belongs to the lane. Both operands take the same values of k in
@@ -392,8 +392,9 @@ int launch(const ProjectParams &P, hipStream_t s) {
   // a round of 192 x 128, 160 x 128, 192 x 256 and 256 x 256 takes 0.75, 1.13, 1.28 and 1.60 times
   // one of 128 x 128, the quarters that are left of 256 x 256 0.70. Fewer tiles than CUs: one a CU,
   // by 8 waves with more steps under way, and smaller ones where few even of those would be busy.
-  // Measured (bfloat16, us) with tiles of 256 x 256, 192 x 256, 160 x 128, 128 x 128, 192 x 128,
-  // and one a CU 128 x 128, 128 x 64, 64 x 64, 64 x 32:
+  // Measured (bfloat16, us; with results through the caches, 4 to 18 % more than now) with tiles of
+  // 256 x 256, 192 x 256, 160 x 128, 128 x 128, 192 x 128, and one a CU 128 x 128, 128 x 64, 64 x 64,
+  // 64 x 32:
   //   25,600 x 4,096, k 4,096: 411, 439, 449, 476
   //    8,192 x 8,192, k 4,096: 253,  -,   -,  338, 292
   //    6,400 x 1,536, k 1,024:  27,  23,  21,  26,   -,  27, 25, 27
