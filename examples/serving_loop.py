@@ -71,7 +71,8 @@ class Server:
     def __init__(self, cameras=6, places=8, n_layers=2, heads=8, kv_heads=2, d=64, page=16,
                  n_pages=96, most=512, seed=0):
         g = torch.Generator(device="cuda").manual_seed(seed)
-        self.heads, self.kv_heads, self.d, self.width, self.most = heads, kv_heads, d, heads * d, most
+        self.heads, self.kv_heads, self.d = heads, kv_heads, d
+        self.width, self.most = heads * d, most
         self.layers = [Layer(cameras, heads, kv_heads, d, g) for _ in range(n_layers)]
         self.pages = tg.Pages.empty(places, most // page, n_pages, page)
         self.cache = [torch.zeros((2, n_pages * page, kv_heads, d), dtype=DTYPE, device="cuda")

@@ -123,7 +123,6 @@ __device__ __forceinline__ void put_pair(const ProjectParams &P, int t, int n0, 
 
 // ------------------------------------------------------------------------------ few tokens
 
-
 constexpr int kFewWaves = 8;
 
 // 16 tokens x 16 outputs a workgroup; a wave takes every kFewWaves-th 512 values of k, all of whose
@@ -393,8 +392,8 @@ int launch(const ProjectParams &P, hipStream_t s) {
   // one of 128 x 128, the quarters that are left of 256 x 256 0.70. Fewer tiles than CUs: one a CU,
   // by 8 waves with more steps under way, and smaller ones where few even of those would be busy.
   // Measured (bfloat16, us; with results through the caches, 4 to 18 % more than now) with tiles of
-  // 256 x 256, 192 x 256, 160 x 128, 128 x 128, 192 x 128, and one a CU 128 x 128, 128 x 64, 64 x 64,
-  // 64 x 32:
+  // 256 x 256, 192 x 256, 160 x 128, 128 x 128, 192 x 128, and one a CU 128 x 128, 128 x 64, 64 x
+  // 64, 64 x 32:
   //   25,600 x 4,096, k 4,096: 411, 439, 449, 476
   //    8,192 x 8,192, k 4,096: 253,  -,   -,  338, 292
   //    6,400 x 1,536, k 1,024:  27,  23,  21,  26,   -,  27, 25, 27

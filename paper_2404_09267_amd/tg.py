@@ -141,9 +141,9 @@ class AttendPagesArgs(ctypes.Structure):
                 ("out_head_stride", _i64), ("table", _vp), ("table_stride", _i64),
                 ("kv_len", _vp), ("q_begin", _vp), ("slope", _vp), ("scale", _f32),
                 ("cap", _f32), ("window", _i32), ("n_seqs", _i32), ("n_pages", _i32),
-                ("page_size", _i32), ("max_pages", _i32), ("n_q_rows", _i32), ("max_kv_len", _i32), ("n_heads", _i32),
-                ("n_kv_heads", _i32), ("d", _i32), ("type", _i32), ("workspace", _vp),
-                ("workspace_bytes", ctypes.c_size_t)]
+                ("page_size", _i32), ("max_pages", _i32), ("n_q_rows", _i32),
+                ("max_kv_len", _i32), ("n_heads", _i32), ("n_kv_heads", _i32), ("d", _i32),
+                ("type", _i32), ("workspace", _vp), ("workspace_bytes", ctypes.c_size_t)]
 
 
 class NormArgs(ctypes.Structure):
@@ -1170,8 +1170,8 @@ def pages_args(pages: Pages, q_begin, bufs: PagesBuffers, release=None,
     n_tokens = bufs.slot.shape[0]
     _check(bufs.pos, torch.int32, (n_tokens, 1), "pos")
     _check(bufs.refused, torch.int32, (1,), "refused")
-    _here(pages.table, pages.kv_len, pages.free, q_begin, release, bufs.slot, bufs.workspace,
-          after.kv_len, after.n_free)
+    _here(pages.table, pages.kv_len, pages.free, pages.n_free, q_begin, release, bufs.slot,
+          bufs.pos, bufs.refused, bufs.workspace, after.kv_len, after.n_free)
     a = PagesArgs()
     a.q_begin = q_begin.data_ptr()
     a.kv_len, a.kv_len_out = pages.kv_len.data_ptr(), after.kv_len.data_ptr()

@@ -872,6 +872,14 @@ def test_other_device_is_refused(monkeypatch):
                  lambda: tg.attend_pages_args(q, q, q, p, q, scratch, 1.0)):
         with pytest.raises(ValueError, match="current device"):
             make()
+    seen = []
+    monkeypatch.setattr(tg, "_here", lambda *tensors: seen.extend(tensors))
+    after = tg.Pages(p.table, p.kv_len.clone(), 16, p.free, p.n_free.clone())
+    ends = ints([0, 1])
+    tg.pages_args(p, begin, bufs, ends, after)
+    for t in (p.table, p.kv_len, p.free, p.n_free, begin, ends, bufs.slot, bufs.pos, bufs.refused,
+              bufs.workspace, after.kv_len, after.n_free):
+        assert any(t is u for u in seen)
 
 
 def test_streams():
