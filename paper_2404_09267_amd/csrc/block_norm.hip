@@ -3,8 +3,8 @@
 // x and y are read once and the residual and its norm written once, 8 bytes a value, and everything
 // between is kept in registers: that is what bounds it (25,600 x 4,096 in bfloat16, gates of 20
 // cameras, a layer norm of y and a norm of the result: 157 us, 5.3 TB/s where a large copy reaches
-// 4.9; 20 x 1,024: 3.7 us, a launch and two loads in a row). A row is a wave's or a workgroup's, of
-// 128 to 1,024 threads, so that a thread has 8 to 32 values. The variance is of the differences
+// 4.9; 20 x 1,024: 3.7 us, a launch and two loads in a row). A row is 16 lanes', a wave's or a
+// workgroup's, of 128 to 1,024 threads, so that a thread has 8 to 32 values. The variance is of the differences
 // from the mean, which costs a second sum over the row but no digits, where sum and sum of squares
 // at once would cancel; and what rounding the mean has left is taken off with it, as a row that
 // hardly varies would show it (all 1,000: 0.06 for 0).
@@ -121,7 +121,7 @@ __global__ __launch_bounds__(kGroupThreads<R>) void norm_kernel(const NormParams
   constexpr int kRows = kGroupThreads<R> / R;
   __shared__ float s_turns[R > 64 ? 12 : 1][16];
   const int64_t t = int64_t(workgroup()) * kRows + threadIdx.x / R;
-  if (t >= P.n_tokens) return;  // a whole wave, or the workgroup
+  if (t >= P.n_tokens) return;  // 16 lanes, a whole wave, or the workgroup
   const int n = P.n;
   Chunk<kType> xv[kV];
   const E *x = static_cast<const E *>(P.x) + t * P.x_stride;
@@ -190,6 +190,7 @@ int launch_rows(const NormParams &P, int piece, hipStream_t s) {
 }
 
 constexpr int64_t kFew = int64_t(1) << 22;
+constexpr int kNarrow = 128;
 
 template <int kType>
 int launch(const NormParams &P, int piece, hipStream_t s) {
@@ -200,7 +201,11 @@ int launch(const NormParams &P, int piece, hipStream_t s) {
   //   3,200 x 1,024:   9.2,  9.7        1,600 x 2,048:   9.8, 10.2
   //   6,400 x 1,024:  14.6, 13.4, 17.6  1,600 x 4,096:  15.5, 14.4
   //   25,600 x 2,048: 91.9, 81.2, 82.7  25,600 x 4,096: 186, 161, 172
+  // Up to 256 values 16 lanes a row: 409,600 x 128 89 us, 261 with a wave a row, 14,768 x 19 5.5 for
+  // 11.5; with 32 values a lane up to 512, 6,400 x 512 13.3 for 9.2, 102,400 x 512 83 for 89.
   const bool few = int64_t(P.n_tokens) * P.n <= kFew;
+  if (P.n <= kNarrow) return launch_rows<kType, 16, 1>(P, piece, s);
+  if (P.n <= 2 * kNarrow) return launch_rows<kType, 16, 2>(P, piece, s);
   if (P.n <= 512) return launch_rows<kType, 64, 1>(P, piece, s);
   if (few && P.n <= 1024) return launch_rows<kType, 128, 1>(P, piece, s);
   if (few && P.n <= 2048) return launch_rows<kType, 256, 1>(P, piece, s);

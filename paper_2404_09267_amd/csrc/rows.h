@@ -6,9 +6,9 @@
 
 namespace tok {
 
-// Threads of a workgroup: four rows of a wave each, or one row.
+// Threads of a workgroup: rows of 16 lanes or a wave each, or one row.
 template <int R>
-constexpr int kGroupThreads = R == 64 ? 256 : R;
+constexpr int kGroupThreads = R <= 64 ? 256 : R;
 
 template <int kType>
 using Chunk = typename Num<kType>::V8;
@@ -95,10 +95,37 @@ __device__ __forceinline__ uint32_t lanes_max(uint32_t v) {
   return __builtin_amdgcn_readlane(v, 63);
 }
 
+// v of the lane 1 or 2 away, or of the mirrored lane among 8 or 16: the four of them together go
+// over 16 lanes, in an order that is the same for all.
+template <int kStep>
+__device__ __forceinline__ uint32_t across(uint32_t v) {
+  constexpr int kCtrl[4] = {0xB1, 0x4E, 0x141, 0x140};
+  return __builtin_amdgcn_update_dpp(0u, v, kCtrl[kStep], 0xF, 0xF, false);
+}
+
+// Sum and largest over 16 lanes, in all of them.
+__device__ __forceinline__ float sum16(float v) {
+  const auto bits = [](float x) { return __builtin_bit_cast(uint32_t, x); };
+  const auto value = [](uint32_t x) { return __builtin_bit_cast(float, x); };
+  v += value(across<0>(bits(v)));
+  v += value(across<1>(bits(v)));
+  v += value(across<2>(bits(v)));
+  v += value(across<3>(bits(v)));
+  return v;
+}
+
+__device__ __forceinline__ uint32_t max16(uint32_t v) {
+  v = max(v, across<0>(v));
+  v = max(v, across<1>(v));
+  v = max(v, across<2>(v));
+  return max(v, across<3>(v));
+}
+
 // Sum over the R threads of a row, in all of them and in a set order. `turn`: LDS of this sum's
 // own.
 template <int R>
 __device__ __forceinline__ float row_sum(float v, float *turn) {
+  if constexpr (R == 16) return sum16(v);
   v = lanes_sum(v);
   if constexpr (R > 64) {
     if ((threadIdx.x & 63) == 0) turn[threadIdx.x >> 6] = v;

@@ -586,6 +586,27 @@ def test_norm_far_from_one(n, kind):
     assert bool(((ho - int(kind == 1)).abs() <= 2.0 ** -7).all())
 
 
+@pytest.mark.parametrize("n", [1, 9, 60, 64, 100, 128, 129, 132, 200, 255, 256, 257])
+def test_norm_narrow(n):
+    """Many short rows, of which neighbours share a wave: far, flat, broken and without a gate."""
+    say("norm narrow", n)
+    g, dt, tokens = gen(n), torch.bfloat16, 1003
+    for kind in (1, 2):
+        x, y, yw, yb, gate, row, w, b = norm_inputs(g, tokens, n, dt, 3)
+        gain = torch.tensor([1.0, 1e30, 1e-3, 0.0, 1.0, 1e25, 1.0])[torch.arange(tokens) % 7]
+        x = (x.float() * gain[:, None]).to(dt)
+        more = dict(y_norm=kind, y_weight=yw, gate=gate, gate_row=row, weight=w, bias=b, eps=1e-5)
+        if n == 1 and kind == 2:  # all of a row is its mean
+            more.update(y_norm=0)
+        (r, er), (h, eh) = R.norm(x, y, kind=kind, **more)
+        broken = torch.arange(tokens) % 11 == 5
+        x[broken, n - 1] = NAN
+        xo, ho = run_norm(x, y, norm=kind, **more)
+        R_assert(xo.cpu()[~broken], r[~broken], er[~broken], "x_out")
+        R_assert(ho.cpu()[~broken], h[~broken], eh[~broken], "h")
+        assert bool(torch.isnan(ho.cpu()[broken]).all())
+
+
 @pytest.mark.parametrize("n", [520, 1024, 1999, 2040, 4092, 4096, 8184, 8191])
 def test_norm_many(n):
     """Rows of more than 2^22 values together, some of them with squares past binary32."""
@@ -658,6 +679,19 @@ def test_quantize(rows, k, dtype):
     q, whole = apart(torch.zeros(x.shape, dtype=torch.int8))
     same_rows(run_quantize(wide, q), R.quantize(x))
     assert untouched(q, whole)
+
+
+@pytest.mark.parametrize("k", [1, 9, 60, 64, 100, 128, 129, 132, 200, 255, 256, 257])
+def test_quantize_narrow(k):
+    """Many short rows, of which neighbours share a wave: far, of zeros and broken."""
+    say("quantize narrow", k)
+    for dt in (torch.float16, torch.bfloat16):
+        x = normal(gen(k), 1003, k, dtype=torch.float32)
+        gain = torch.tensor([1.0, 1e4, 1e-6, 0.0, 1.0, 1e-37])[torch.arange(1003) % 6]
+        x = (x * gain[:, None]).to(dt)
+        x[torch.arange(1003) % 11 == 5, k - 1] = NAN
+        x[torch.arange(1003) % 13 == 7, 0] = INF
+        same_rows(run_quantize(x), R.quantize(x))
 
 
 @pytest.mark.parametrize("dtype", ["f16", "bf16"])
@@ -807,7 +841,7 @@ def test_rows_past_32_bits():
     assert int((y != 0).any(1).sum()) == 3
 
 
-@pytest.mark.parametrize("n", [512, 1024, 2048, 4096, 8192, 16384, 32768])
+@pytest.mark.parametrize("n", [8, 128, 256, 512, 1024, 2048, 4096, 8192, 16384, 32768])
 def test_rows_past_the_caches(n):
     """Results that pass the caches are those of the same rows in calls that do not."""
     say("past the caches", n)
