@@ -688,23 +688,36 @@ int64_t each_of(int n_heads, int n_kv_heads) {  // workgroups of a sequence
 // Whether a sequence's keys are left to one workgroup: where there are few, since the join costs a
 // launch, and up to more of them the more workgroups the sequences alone make; beyond, a long one
 // among short ones would keep all waiting. us by a workgroup of 8 waves (4) and cut:
-//       1 sequence,  5,000 keys, 8 heads of 128 over 2: 33 (51), 13
-//       4 sequences, 1,600, 16 heads of 128 over 4:     16 (20), 13
-//      20 sequences, 1,600, 16 heads of 128 over 4:     17 (21), 20
-//      20 sequences, 1,600, 16 heads of 64 over 4:      13 (19), 18
-//      64 sequences, 2,200, 16 heads of 128 over 4:     41 (40), 46
-//     256 sequences, 4,096, 32 heads of 128 over 8:    439 (442), 439
-//     256 sequences,   500, 16 heads of 64 over 2:      12 (11), 35
-//   1,000 sequences,   900, 8 heads of 128 over 1:      64 (58), 106
-//       8 sequences, 100,003, 16 heads of 128 over 2:  937 (1,107), 111
+//       1 sequence,    900 keys, 16 heads of 128 over 4: 12.3, 12.0;   2,048: 16, 12
+//       4 sequences, 1,200, 16 heads of 128 over 4:      13.9, 12.3;   2,048: 19, 16
+//       8 sequences, 1,600, 16 heads of 128 over 4:      17.0, 17.3;   2,048: 20, 18
+//      14 sequences, 2,048, 16 heads of 128 over 4:      20.3, 20.8;   2,560: 23, 21
+//      30 sequences, 2,048, 16 heads of 128 over 4:      22.2, 25.3;   3,500: 49, 37
+//       1 sequence,  1,600, 16 heads of 64 over 4:        9.8, 10.7;   2,048: 11.4, 10.7
+//       4 sequences, 2,560, 16 heads of 64 over 4:       13.9, 14.1;   3,500: 19, 14
+//       8 sequences, 2,560, 16 heads of 64 over 4:       14.9, 15.6;   3,500: 19, 16
+//      20 sequences, 1,600, 16 heads of 64 over 4:         13 (19), 18
+//      30 sequences, 3,500, 16 heads of 64 over 4:       19.9, 23.1
+//      64 sequences, 2,200, 16 heads of 128 over 4:        41 (40), 46
+//     256 sequences, 4,096, 32 heads of 128 over 8:       439 (442), 439
+//     256 sequences,   500, 16 heads of 64 over 2:         12 (11), 35
+//   1,000 sequences,   900, 8 heads of 128 over 1:         64 (58), 106
+//       8 sequences, 100,003, 16 heads of 128 over 2:     937 (1,107), 111
 // 16 waves, of heads of 64: 13.3 for 13.1 where 20 have 1,600 keys, 73.8 for 65.8 where 256 have
 // 2,000.
-constexpr int kWholeNarrow = 1536, kWholeWide = 1024, kWholeOfMany = 2048, kWholeOfAll = 4096;
+struct Whole {
+  int alone;         // from so many workgroups on
+  int narrow, wide;  // keys of heads up to 64, and of wider ones
+};
+constexpr int kWholeLeast = 768;
+constexpr Whole kWhole[] = {{256, 4096, 4096}, {64, 3584, 2048}, {32, 2816, 1664},
+                            {16, 2560, 1408},  {8, 2048, 1024},  {0, 1792, kWholeLeast}};
 
 Form form_of(int n_seqs, int max_kv, int64_t each, int d) {
   const int64_t alone = n_seqs * each;
-  const int few = d <= 64 ? kWholeNarrow : kWholeWide;
-  const int whole = alone >= 256 ? kWholeOfAll : alone >= 64 ? kWholeOfMany : few;
+  const Whole *limit = kWhole;
+  while (alone < limit->alone) ++limit;
+  const int whole = d <= 64 ? limit->narrow : limit->wide;
   const int waves = max_kv <= (alone > 256 ? 1024 : 512) ? 4 : 8;
   // tiles are counted in 30 bits
   if (n_seqs > kMaxCut || max_kv <= whole || n_seqs * (int64_t(max_kv) / kKeys + 2) > 1 << 30)
@@ -754,7 +767,7 @@ extern "C" size_t tg_attend_pages_workspace_bytes(int32_t n_seqs, int32_t max_kv
                                                   int32_t d) {
   if (!sizes_ok(n_seqs, max_kv_len, n_heads, n_kv_heads, d) || n_seqs == 0) return 0;
   const int64_t each = each_of(n_heads, n_kv_heads);
-  if (max_kv_len <= kWholeWide) return 0;
+  if (max_kv_len <= kWholeLeast) return 0;
   const int64_t cut = std::min<int64_t>(n_seqs, kMaxCut);
   const int64_t parts = std::max<int64_t>(kPlaces / each, 1) + cut;
   return static_cast<size_t>(parts) * n_heads * (d + 2) * sizeof(float);
