@@ -230,6 +230,13 @@ def cache(g, lens, page, kv_heads, d, dtype, spare=3, cols=None):
     return k, v, table
 
 
+def widened(table, page, most):
+    """The table with entries that are no page, up to `most` rows: what a sequence may hold, and
+    not what it holds, decides how a call is done."""
+    more = 0 if most is None else -(-most // page) - table.shape[1]
+    return torch.nn.functional.pad(table, (0, max(more, 0)), value=-1)
+
+
 def run_attend(q, k, v, table, lens, page, max_kv=None, out=None, **more):
     pages = tg.Pages(table.cuda(), ints(list(lens)), page)
     qd, kd, vd = (t if t.is_cuda else t.cuda() for t in (q, k, v))
@@ -257,19 +264,21 @@ ATTEND = [
 ]
 
 
+@pytest.mark.parametrize("most", [None, 20000])  # of the lengths; the larger has keys cut
 @pytest.mark.parametrize("dtype", ["f16", "bf16"])
 @pytest.mark.parametrize("case", range(len(ATTEND)))
-def test_attend_pages(case, dtype):
+def test_attend_pages(case, dtype, most):
     lens, page, heads, kv, d, extra = ATTEND[case]
     say("attend_pages", case, dtype)
     g, dt = gen(case), DT[dtype]
     k, v, table = cache(g, lens, page, kv, d, dt)
+    table = widened(table, page, most)
     q = normal(g, len(lens), heads, d, dtype=dt, gain=2.0)
     more = dict(extra, scale=d ** -0.5)
     if more.get("slope"):
         more["slope"] = torch.linspace(-0.01, 0.3, heads)
     want, bound = R.attend_pages(q, k, v, table, lens, page, **more)
-    got = run_attend(q, k, v, table, lens, page, **more)
+    got = run_attend(q, k, v, table, lens, page, most, **more)
     R_assert(got, want, bound, "attend_pages")
 
 
@@ -300,13 +309,15 @@ def test_attend_pages_bounds(max_kv):
         R_assert(got[3:], want, bound, "past the table")
 
 
+@pytest.mark.parametrize("most", [None, 20000])  # of the lengths; the larger has keys cut
 @pytest.mark.parametrize("length", [60, 1500])
-def test_attend_pages_hides(length):
+def test_attend_pages_hides(length, most):
     """Pages that are none, rows past the end and before the window hold NaN and infinities."""
     say("attend_pages hides", length)
     g, page = gen(12), 16
     lens = [length, length - 5, 20, 17]
     k, v, table = cache(g, lens, page, 2, 64, torch.float16)
+    table = widened(table, page, most)
     q = normal(g, 4, 4, 64, dtype=torch.float16)
     n_pages = k.shape[0] // page
     for s, (at, bad) in enumerate(((1, -1), (0, n_pages), (0, 1 << 30), (1, -(1 << 31)))):
@@ -315,26 +326,30 @@ def test_attend_pages_hides(length):
         k[rows], v[rows] = INF, NAN
         table[s, at] = bad
     want, bound = R.attend_pages(q, k, v, table, lens, page, 0.2)
-    R_assert(run_attend(q, k, v, table, lens, page, scale=0.2), want, bound, "bad pages")
+    R_assert(run_attend(q, k, v, table, lens, page, most, scale=0.2), want, bound, "bad pages")
     table[:] = -1
-    assert bool((run_attend(q, k, v, table, lens, page, scale=0.2) == 0).all())
+    assert bool((run_attend(q, k, v, table, lens, page, most, scale=0.2) == 0).all())
     k, v, table = cache(g, lens, page, 2, 64, torch.float16)
+    table = widened(table, page, most)
     for s, n in enumerate(lens):
         j = torch.arange(n - 9)
         rows = table[s].long()[j // page] * page + j % page
         k[rows], v[rows] = NAN, INF
     want, bound = R.attend_pages(q, k, v, table, lens, page, 0.2, window=9)
-    R_assert(run_attend(q, k, v, table, lens, page, scale=0.2, window=9), want, bound, "window")
+    got = run_attend(q, k, v, table, lens, page, most, scale=0.2, window=9)
+    R_assert(got, want, bound, "window")
 
 
+@pytest.mark.parametrize("most", [None, 20000])  # of the lengths; the larger has keys cut
 @pytest.mark.parametrize("length", [40, 1500])
-def test_attend_pages_broken_values(length):
+def test_attend_pages_broken_values(length, most):
     """NaN that a query sees is its result, an infinite value its column's; scores that are all
     minus infinity leave no weights. Other sequences and heads do not see it."""
     say("attend_pages broken", length)
     g, page, d = gen(13), 16, 32
     lens = [length] * 5
     k, v, table = cache(g, lens, page, 2, d, torch.bfloat16)
+    table = widened(table, page, most)
     k, v = torch.nan_to_num(k, nan=1.0), torch.nan_to_num(v, nan=1.0)
     q = normal(g, 5, 4, d, dtype=torch.bfloat16).abs() + 0.1
     row = lambda s, j: int(table[s, j // page]) * page + j % page
@@ -344,7 +359,7 @@ def test_attend_pages_broken_values(length):
     for j in range(length):
         k[row(3, j), 1, :] = -INF
     k[row(4, 7), 0, :] = -INF  # one score of minus infinity: no weight
-    got = run_attend(q, k, v, table, lens, page, scale=0.1)
+    got = run_attend(q, k, v, table, lens, page, most, scale=0.1)
     assert bool(torch.isnan(got[1, :2]).all()) and bool((got[2, 2:, 5] == INF).all())
     assert bool(torch.isnan(got[3, 2:]).all())
     want4, bound4 = R.attend_pages(q[4:], torch.nan_to_num(k, nan=0, neginf=-3e38), v, table[4:],
@@ -355,17 +370,19 @@ def test_attend_pages_broken_values(length):
     R_assert(got[fine], clean[fine], bound[fine], "others")
 
 
+@pytest.mark.parametrize("most", [None, 20000])  # of the lengths; the larger has keys cut
 @pytest.mark.parametrize("length", [45, 1300])
 @pytest.mark.parametrize("dtype", ["f16", "bf16"])
-def test_attend_pages_large_scores(length, dtype):
+def test_attend_pages_large_scores(length, dtype, most):
     """Scores of 2^24 and more: the largest takes all, none is lost to rounding; factors at the
     ends of binary32; a factor of 0 and below 0."""
     say("attend_pages large", length, dtype)
     g, page, d, dt = gen(14), 16, 64, DT[dtype]
     k, v, table = cache(g, [length], page, 1, d, dt)
+    table = widened(table, page, most)
     q = normal(g, 1, 3, d, dtype=dt)
     for scale in (0.0, -0.3, 3e7, 1e30):
-        got = run_attend(q, k, v, table, [length], page, scale=scale).double()
+        got = run_attend(q, k, v, table, [length], page, most, scale=scale).double()
         j = torch.arange(length)
         rows = table[0].long()[j // page] * page + j % page
         if abs(scale) < 1:
@@ -377,22 +394,26 @@ def test_attend_pages_large_scores(length, dtype):
             assert torch.equal(got[0, h], v[rows[best], 0].double()), (scale, h)
 
 
+@pytest.mark.parametrize("most", [None, 20000])  # of the lengths; the larger has keys cut
 @pytest.mark.parametrize("cap", [1e-3, 5.0, 1e4, 1e30])
-def test_attend_pages_caps(cap):
+def test_attend_pages_caps(cap, most):
     say("attend_pages cap", cap)
     g, page, d, lens = gen(15), 16, 64, [50, 1100]
     k, v, table = cache(g, lens, page, 1, d, torch.float16)
+    table = widened(table, page, most)
     q = normal(g, 2, 5, d, dtype=torch.float16, gain=3.0)
     # tanh does nothing to scores under 1e30, and the bound is then that of the plain score
     want, bound = R.attend_pages(q, k, v, table, lens, page, 0.2, cap=cap if cap < 1e15 else 0.0)
-    R_assert(run_attend(q, k, v, table, lens, page, scale=0.2, cap=cap), want, bound, "cap")
+    R_assert(run_attend(q, k, v, table, lens, page, most, scale=0.2, cap=cap), want, bound, "cap")
 
 
-def test_attend_pages_strides():
+@pytest.mark.parametrize("most", [None, 20000])  # of the lengths; the larger has keys cut
+def test_attend_pages_strides(most):
     """Heads and rows apart, inside wider tensors; nothing but the result is written."""
     say("attend_pages strides")
     g, page, lens = gen(16), 24, [70, 1200, 0]
     k, v, table = cache(g, lens, page, 2, 72, torch.bfloat16)
+    table = widened(table, page, most)
     q = normal(g, 3, 6, 72, dtype=torch.bfloat16)
     want, bound = R.attend_pages(q, k, v, table, lens, page, 0.1)
     # k and v of one tensor, heads outside rows
@@ -405,7 +426,7 @@ def test_attend_pages_strides():
     wide = torch.full((3, table.shape[1] + 5), 0, dtype=torch.int32, device="cuda")
     wide[:, 2:-3] = table.cuda()
     pages = tg.Pages(wide[:, 2:-3], ints(lens), page)
-    tg.attend_pages(qd, kd, vd, pages, out, tg.AttendPagesBuffers(qd, kd, 1200), 0.1)
+    tg.attend_pages(qd, kd, vd, pages, out, tg.AttendPagesBuffers(qd, kd, most or 1200), 0.1)
     torch.cuda.synchronize()
     R_assert(out.cpu(), want, bound, "strides")
     assert untouched(out, whole)
