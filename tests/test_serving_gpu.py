@@ -754,7 +754,9 @@ PROJECT = [(1, 16, 1), (1, 64, 300), (7, 1024, 130), (8, 1024, 1536), (16, 80, 1
            (33, 512, 64), (64, 208, 96), (64, 4096, 33), (65, 144, 257), (129, 320, 200),
            (300, 192, 384), (513, 96, 515), (700, 1024, 1000), (2048, 128, 2048), (3000, 272, 1500),
            (5000, 64, 1111), (2500, 64, 4100), (2100, 144, 2100), (4352, 64, 4096), (6400, 64, 1536),
-           (3500, 80, 2048), (1500, 96, 1000)]
+           (3500, 80, 2048), (1500, 96, 1000),
+           # several tiles of 256 x 256 a workgroup, of 2, 3 and 4 steps
+           (6300, 144, 4200), (6400, 272, 4096), (6350, 400, 4099), (13200, 144, 4096)]
 
 
 def signed(g, *shape):
