@@ -7,9 +7,9 @@
 //
 // Many tokens: tiles of x and w go through LDS to the matrix instructions, several steps of 128
 // values of k under way; how fast they get there bounds it (the matrix units are at work 64 % of
-// the time). bfloat16: 25,600 x 4,096, k 4,096: 346 to 363 us by card, 2.37 to 2.48 POPS (a
+// the time). bfloat16: 25,600 x 4,096, k 4,096: 346 to 367 us by card, 2.34 to 2.48 POPS (a
 // library's product, which gives sums of 32 bits, 420; its best at any size 2.5 POPS); 8,192 x
-// 8,192, k 8,192: 414 to 423, 2.6; 8 x 1,536, k 1,024: 3.5, a launch.
+// 8,192, k 8,192: 414 to 425, 2.6; 8 x 1,536, k 1,024: 3.5, a launch.
 //
 // Results lie transposed in the registers (a lane holds 4 outputs of one token), so that stores are
 // contiguous and a token's scale belongs to the lane. Both operands take the same values of k in
