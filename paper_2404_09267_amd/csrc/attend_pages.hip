@@ -3,7 +3,7 @@
 // The query heads that share a key head are rows of one matrix tile, so that keys and values are
 // read once, and reading them bounds it: each wave has a tile of 32 keys and their values under way
 // to LDS while it works on the one before. A key's row in the cache is looked up by a lane, a tile
-// ahead of its loads. Tiles whose keys are all seen are loaded 16 rows at a time; in the others
+// ahead of its loads. Tiles whose keys are all seen are loaded by runs of rows; in the others
 // rows that are not seen (past the end, before the window, on a page that is none) are loaded from
 // zeros instead, so that whatever lies there stays out, and have no weight.
 //
@@ -324,25 +324,28 @@ __global__ __launch_bounds__(kWaves * 64) void attend_pages_kernel(const AttendP
                : -1;
   };
   // The loads of a tile's keys or values to LDS. Where all its keys are seen, and pages are whole
-  // times 16 rows, 16 rows lie one after the other: a lane's place among them stays the same, and
-  // only where they start is looked up. Else every lane has addresses of its own.
+  // times kRun rows, that many rows lie one after the other: a lane's place among them stays the
+  // same, and only where they start is looked up. Else every lane has addresses of its own. Runs of
+  // 8 cost wide heads nothing (33 sequences of 3,001, pages of 24: 17.4 -> 15.5 us), those of 64 5 %
+  // where pages are of 16 (20 of 1,600: 13.7 for 13.0).
+  constexpr int kRun = kD > 64 ? 8 : 16, kRuns = kKeys / kRun;
   uint32_t piece[2][kLoads / 2];
   const auto pieces = [&](uint32_t bytes, uint32_t(&to)[kLoads / 2]) {
 #pragma unroll
     for (int i = 0; i < kLoads / 2; ++i) {
-      const int r = i * kPer + lane / kChunks;
+      const int r = i * kPer + lane / kChunks;  // of 16
       const int c = place_of<kChunks>(r, lane & (kChunks - 1)) * 8;
-      to[i] = c < P.d ? r * bytes + c * 2 : kNowhere;
+      to[i] = c < P.d ? r % kRun * bytes + c * 2 : kNowhere;
     }
   };
   pieces(k_bytes, piece[0]);
   pieces(v_bytes, piece[1]);
-  const bool even_pages = P.page_size % 16 == 0;
+  const bool even_pages = P.page_size % kRun == 0;
   int rows[kLoads];
   auto spread = [&](uint32_t all, int row) {
     if (all == 0xFFFFFFFFu && even_pages) {
-      rows[0] = __builtin_amdgcn_readlane(row, 0);
-      rows[1] = __builtin_amdgcn_readlane(row, 16);
+#pragma unroll
+      for (int g = 0; g < kRuns; ++g) rows[g] = __builtin_amdgcn_readlane(row, kRun * g);
       return;
     }
 #pragma unroll
@@ -353,13 +356,13 @@ __global__ __launch_bounds__(kWaves * 64) void attend_pages_kernel(const AttendP
     const uint32_t bytes = which ? v_bytes : k_bytes;
     if (all == 0xFFFFFFFFu && even_pages) {
 #pragma unroll
-      for (int g = 0; g < 2; ++g) {
+      for (int g = 0; g < kRuns; ++g) {
         const uint32_t at = __builtin_amdgcn_readfirstlane(rows[g]);
         const auto b = buffer(reinterpret_cast<const void *>(base + uint64_t(at) * bytes),
-                              15 * bytes + P.d * 2);
+                              (kRun - 1) * bytes + P.d * 2);
 #pragma unroll
-        for (int i = 0; i < kLoads / 2; ++i)
-          load_lds(b, to + (g * kLoads / 2 + i) * kPer * kD, piece[which][i], 0);
+        for (int i = g * kLoads / kRuns; i < (g + 1) * kLoads / kRuns; ++i)
+          load_lds(b, to + i * kPer * kD, piece[which][i % (kLoads / 2)], 0);
       }
       return;
     }

@@ -260,6 +260,7 @@ ATTEND = [
                                                         dict(window=64, slope=True)),
     ([1500, 1501, 1502], 32, 6, 2, 128, dict(window=1100, cap=50.0)),
     ([3000] + [3] * 70, 16, 8, 4, 64, {}), ([90] * 260, 16, 2, 1, 16, {}),
+    ([90, 33, 64], 8, 6, 2, 128, {}), ([400, 39], 40, 5, 1, 72, {}),
     ([90, 5, 0] * 13, 16, 6, 2, 72, {}), ([64, 33, 100] * 11, 32, 36, 1, 40, dict(slope=True)),
 ]
 
