@@ -828,10 +828,10 @@ size_t tg_attend_pages_workspace_bytes(int32_t n_seqs, int32_t max_kv_len, int32
  * n - window, but none on a page outside [0, n_pages). The output is the softmax-weighted sum of
  * the v_j it sees, 0 if it sees none (kv_len <= 0 among them; such rows are written, but no row
  * that is no sequence's query), NaN if all its scores are minus infinity. Rows that it does not
- * see are not read. Weights are rounded to the type before the product with v, in binary16 as 2^7
- * times their share of the largest or more; their sum is of the rounded ones. An infinite value
- * whose weight rounds to 0 makes NaN. Distances up to 2^24 are exact. out must not overlap an
- * input. Enqueued on `stream`; allocates nothing. Returns TG_E_INVAL (null pointer, negative
+ * see are not read. Weights go into the product with v as two values of the type, a rounding and
+ * what that leaves (16 bits of bfloat16, 22 of binary16, there as 2^7 times their share of the
+ * largest or more); their sum is of the same. An infinite value whose weight rounds to 0 makes
+ * NaN. Distances up to 2^24 are exact. out must not overlap an input. Enqueued on `stream`; allocates nothing. Returns TG_E_INVAL (null pointer, negative
  * count, n_seqs > TG_PAGES_MAX_SEQS, max_kv_len > 2^30, d outside [8, TG_ATTEND_MAX_D] or not a
  * multiple of 8, heads that n_kv_heads does not divide, a negative window, page_size or max_pages
  * < 1, n_pages * page_size >= 2^31, a bad type, scale or cap, a table_stride below max_pages, q,

@@ -11,7 +11,13 @@
 // log2, the sum l of 2^(z - m) and the weighted sum of values, the latter two multiplied by
 // 2^(m_old - m_new) when a score passes m by kSlack. Scores are computed transposed, S^T = K Q^T,
 // so that a lane's scores are of one query and the weights come out where the second product, O^T =
-// V^T P^T, takes them as an operand.
+// V^T P^T, takes them as an operand. That product takes 16-bit operands; where values of both signs
+// cancel, weights of 8 or 11 bits would show long before the result's own rounding does, so they
+// go in as two parts, a rounding and, rounded too, what that leaves. Up to 8 query heads a key head
+// leave half the tile's columns free, and those take the second part of the same heads (20 sequences
+// of 1,600, 16 heads of 64 over 4: 12.6 -> 13.2 us for it, 8 of 100,003 the same 107); more heads
+// take a second product (8 of 60,000, 32 heads of 128 over 1: 39 -> 44; the paired columns would
+// read keys once for every 8).
 //
 // Few keys, or many sequences: a workgroup a sequence and key head. Else all sequences' keys are
 // cut into as many ranges of one length as there is room for workgroups, found on the device, so
@@ -38,7 +44,7 @@ using namespace tok;
 constexpr int kMaxStride = 1 << 22, kMaxKeys = 1 << 30;
 constexpr float kSlack = 8.0f;
 // Weights are kept times 2^kLift: binary16's smallest number is 2^-24, and what lies below 2^-25 of
-// the largest weight would be lost, however many such keys there are. With kSlack they reach
+// the largest weight, of a second part too, would be lost, however many such keys there are. With kSlack they reach
 // 2^15, which binary16 holds.
 template <int kType>
 constexpr float kLift = kType == TG_F16 ? 7.0f : 0.0f;
@@ -261,18 +267,32 @@ __device__ __forceinline__ float weighted(float sum, float m, float l) {
   return l == 0.0f ? (m == -INFINITY ? 0.0f : NAN) : sum / l;
 }
 
+// v of the lane 8 on in a row of 16 lanes, which goes round.
+__device__ __forceinline__ float eight_on(float v) {
+  const int bits = __builtin_bit_cast(int, v);
+  return __builtin_bit_cast(float,
+                            __builtin_amdgcn_update_dpp(bits, bits, 0x128, 0xF, 0xF, false));
+}
+
 constexpr int kXcds = 8;  // that workgroups go round
 
+// Waves of a SIMD that registers are to have room for: as many as LDS has where keys are not cut. Heads
+// of 64 get 4 with 3 asked for (126 registers); asked for 4, more than 8 a key head spill two.
+constexpr int per_simd(int d, int bufs) { return bufs > 1 ? 1 : d == 64 ? 3 : 2; }
+
 // Rows of a workgroup: 16 query heads that share a key head. Each of its waves takes every
-// kWaves-th 32 keys of what the workgroup has of a sequence, through LDS of its own.
-template <int kType, int kD, int kWaves, int kBufs>
-__global__ __launch_bounds__(kWaves * 64) void attend_pages_kernel(const AttendParams P) {
+// kWaves-th 32 keys of what the workgroup has of a sequence, through LDS of its own. kPair: 8 heads
+// at most, which columns 8 to 15 are once more: they take what the weights' roundings leave.
+template <int kType, int kD, int kWaves, int kBufs, bool kPair>
+__global__ __launch_bounds__(kWaves * 64, per_simd(kD, kBufs)) void attend_pages_kernel(
+    const AttendParams P) {
   typedef Num<kType> N;
   typedef typename N::E E;
   typedef typename N::V4 V4;
   typedef typename N::V8 V8;
   constexpr int kChunks = kD / 8, kSteps = kD / 32, kBlocks = kD / 16;
   constexpr int kPer = 64 / kChunks, kLoads = kKeys / kPer;  // rows of one load, loads of a tile
+  constexpr int kRows = kPair ? 8 : 16;
   // keys and values of a step; the waves' sums at the end
   __shared__ __attribute__((aligned(16))) E tile[kWaves][kBufs][2][kKeys * kD];
   __shared__ float s_m[kWaves][16], s_l[kWaves][16];
@@ -383,7 +403,8 @@ __global__ __launch_bounds__(kWaves * 64) void attend_pages_kernel(const AttendP
                (r * kD + place_of<kChunks>(r, c) * 8 + (col & 1) * 4) * sizeof(E);
   }
   constexpr int kStep = kWaves * kKeys;
-  const int my = rt * 16 + col;  // this lane's row
+  const int my = kPair ? col & 7 : rt * 16 + col;  // this lane's row
+  const float less = kPair && col < 8 ? 0.0f : -1.0f;  // times a weight's rounding: its second part
   const bool live = my < P.group;
   const int head = kvh * P.group + min(my, P.group - 1);
   const float slope2 = P.slope ? P.slope[head] * kLog2e : 0.0f;
@@ -418,7 +439,7 @@ __global__ __launch_bounds__(kWaves * 64) void attend_pages_kernel(const AttendP
       fetch(0, seen, own[0][0]);
       fetch(1, seen, own[0][1]);
     }
-    f32x4 acc[kBlocks] = {};
+    f32x4 acc[kBlocks] = {}, low[kPair ? 1 : kBlocks] = {};
     float m = -INFINITY, l = 0.0f;
     bool any = false;
     for (; j0 < end; j0 += kStep) {
@@ -486,19 +507,29 @@ __global__ __launch_bounds__(kWaves * 64) void attend_pages_kernel(const AttendP
 #pragma unroll
         for (int b = 0; b < kBlocks; ++b)
 #pragma unroll
-          for (int r = 0; r < 4; ++r) acc[b][r] *= fix;
+          for (int r = 0; r < 4; ++r) {
+            acc[b][r] *= fix;
+            if (!kPair) low[b][r] *= fix;
+          }
       }
       // the difference first: with scores of 2^24 and more the sum of m and kLift would be off
       const float base = m == -INFINITY ? 0.0f : m;
-      V8 pf;
+      V8 pf, pl;  // weights, first and second parts; kPair: the one that this column takes
 #pragma unroll
       for (int e = 0; e < 8; e += 2) {
         const float p0 = __builtin_amdgcn_exp2f((z[e >> 2][e & 3] - base) + kLift<kType>);
         const float p1 = __builtin_amdgcn_exp2f((z[e >> 2][(e & 3) + 1] - base) + kLift<kType>);
-        const auto two = pack2<kType>(p0, p1);
+        auto two = pack2<kType>(p0, p1);
+        const auto left = pack2<kType>(__builtin_fmaf(static_cast<float>(two[0]), less, p0),
+                                       __builtin_fmaf(static_cast<float>(two[1]), less, p1));
+        if (kPair) two = left;
         l = add2<kType>(two, l);
         pf[e] = two[0];
         pf[e + 1] = two[1];
+        if (kPair) continue;
+        l = add2<kType>(left, l);
+        pl[e] = left[0];
+        pl[e + 1] = left[1];
       }
 #pragma unroll
       for (int b0 = 0; b0 < kBlocks; b0 += 4) {
@@ -508,7 +539,10 @@ __global__ __launch_bounds__(kWaves * 64) void attend_pages_kernel(const AttendP
         for (int b = 0; b < 4; ++b) at[b] = place[b0 + b] + buf * 2 * kKeys * kD * sizeof(E);
         read_transposed<kType, 16 * kD * sizeof(E)>(at, vf);
 #pragma unroll
-        for (int b = 0; b < 4; ++b) acc[b0 + b] = N::mfma16(vf[b], pf, acc[b0 + b]);
+        for (int b = 0; b < 4; ++b) {
+          acc[b0 + b] = N::mfma16(vf[b], pf, acc[b0 + b]);
+          if (!kPair) low[b0 + b] = N::mfma16(vf[b], pl, low[b0 + b]);
+        }
       }
       if (more) {
         if (kBufs == 1) fetch(1, seen, own[0][1]);
@@ -518,22 +552,36 @@ __global__ __launch_bounds__(kWaves * 64) void attend_pages_kernel(const AttendP
     // the waves' ranges are joined through LDS
     l += __shfl_xor(l, 16);
     l += __shfl_xor(l, 32);
+    if (kPair) l += eight_on(l);
+#pragma unroll
+    for (int b = 0; b < kBlocks; ++b) {
+      f32x4 more = kPair ? acc[b] : low[b];
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        if (kPair) more[r] = eight_on(more[r]);
+        // may be an infinite value times 0, and such a value goes by its weight's rounding alone
+        if (fabsf(acc[b][r]) < INFINITY) acc[b][r] += more[r];
+      }
+    }
     if (any && m == -INFINITY) m = -FLT_MAX;
     wait_loads();
     __syncthreads();  // the tiles are done with
-    float *sums = reinterpret_cast<float *>(&tile[0][0][0][0]);  // [kWaves][16][kD]
+    float *sums = reinterpret_cast<float *>(&tile[0][0][0][0]);  // [kWaves][kRows][kD]
     if (quad == 0) {
       s_m[wave][col] = m;
       s_l[wave][col] = l;
     }
+    if (col < kRows) {
 #pragma unroll
-    for (int b = 0; b < kBlocks; ++b)
-      *reinterpret_cast<f32x4 *>(sums + (wave * 16 + col) * kD + b * 16 + quad * 4) = acc[b];
+      for (int b = 0; b < kBlocks; ++b)
+        *reinterpret_cast<f32x4 *>(sums + (wave * kRows + col) * kD + b * 16 + quad * 4) = acc[b];
+    }
     __syncthreads();
-    constexpr int kLanes = kWaves * 4 < kD / 4 ? kWaves * 4 : kD / 4;  // threads of a row
+    constexpr int kMost = kWaves * 64 / kRows;
+    constexpr int kLanes = kMost < kD / 4 ? kMost : kD / 4;  // threads of a row
     const int r = threadIdx.x / kLanes, c0 = threadIdx.x % kLanes;
     const int mine = rt * 16 + r;
-    if (r < 16 && mine < P.group && q_row >= 0) {
+    if (r < kRows && mine < P.group && q_row >= 0) {
       float top = -INFINITY;
 #pragma unroll
       for (int w = 0; w < kWaves; ++w) top = fmaxf(top, s_m[w][r]);
@@ -553,7 +601,7 @@ __global__ __launch_bounds__(kWaves * 64) void attend_pages_kernel(const AttendP
         f32x4 v = {};
 #pragma unroll
         for (int w = 0; w < kWaves; ++w)
-          v += f[w] * *reinterpret_cast<const f32x4 *>(sums + (w * 16 + r) * kD + c);
+          v += f[w] * *reinterpret_cast<const f32x4 *>(sums + (w * kRows + r) * kD + c);
         if (whole) {
 #pragma unroll
           for (int q = 0; q < 4; ++q) v[q] = weighted(v[q], top, sum);
@@ -690,7 +738,8 @@ int64_t each_of(int n_heads, int n_kv_heads) {  // workgroups of a sequence
 
 // Whether a sequence's keys are left to one workgroup: where there are few, since the join costs a
 // launch, and up to more of them the more workgroups the sequences alone make; beyond, a long one
-// among short ones would keep all waiting. us by a workgroup of 8 waves (4) and cut:
+// among short ones would keep all waiting. us by a workgroup of 8 waves (4) and cut, with weights in
+// one part (the second adds up to 5 % to either):
 //       1 sequence,    900 keys, 16 heads of 128 over 4: 12.3, 12.0;   2,048: 16, 12
 //       4 sequences, 1,200, 16 heads of 128 over 4:      13.9, 12.3;   2,048: 19, 16
 //       8 sequences, 1,600, 16 heads of 128 over 4:      17.0, 17.3;   2,048: 20, 18
@@ -728,14 +777,14 @@ Form form_of(int n_seqs, int max_kv, int64_t each, int d) {
   return {kCutWaves, static_cast<int>(std::max<int64_t>(kPlaces / each, 1)), kCutWaves};
 }
 
-template <int kType, int kD, int kWaves, int kBufs>
+template <int kType, int kD, int kWaves, int kBufs, bool kPair>
 int launch_waves(const AttendParams &P, hipStream_t s) {
   int64_t blocks = P.width ? P.width : P.n_seqs;
   if (P.near) blocks = (blocks + kXcds - 1) / kXcds * kXcds;
   blocks *= int64_t(P.n_kv_heads) * P.row_tiles;
   const int64_t joined = P.width > 0 ? int64_t(P.n_seqs) * P.n_heads : 0;
   if (blocks > kMaxWorkgroups || joined > kMaxWorkgroups) return TG_E_INVAL;
-  hipLaunchKernelGGL((attend_pages_kernel<kType, kD, kWaves, kBufs>),
+  hipLaunchKernelGGL((attend_pages_kernel<kType, kD, kWaves, kBufs, kPair>),
                      grid_of(blocks, kWaves * 64), dim3(kWaves * 64), 0, s, P);
   if (joined > 0)
     hipLaunchKernelGGL(join_kernel<kType>, grid_of(joined, kJoinThreads), dim3(kJoinThreads), 0, s,
@@ -743,10 +792,16 @@ int launch_waves(const AttendParams &P, hipStream_t s) {
   return hipGetLastError() == hipSuccess ? TG_OK : TG_E_HIP;
 }
 
+template <int kType, int kD, bool kPair>
+int launch_form(const AttendParams &P, hipStream_t s) {
+  if (P.width > 0) return launch_waves<kType, kD, kCutWaves, 2, kPair>(P, s);
+  return P.unit == 4 ? launch_waves<kType, kD, 4, 1, kPair>(P, s)
+                     : launch_waves<kType, kD, 8, 1, kPair>(P, s);
+}
+
 template <int kType, int kD>
 int launch(const AttendParams &P, hipStream_t s) {
-  if (P.width > 0) return launch_waves<kType, kD, kCutWaves, 2>(P, s);
-  return P.unit == 4 ? launch_waves<kType, kD, 4, 1>(P, s) : launch_waves<kType, kD, 8, 1>(P, s);
+  return P.group <= 8 ? launch_form<kType, kD, true>(P, s) : launch_form<kType, kD, false>(P, s);
 }
 
 bool layout_ok(const void *p, int64_t stride, int64_t head) {
