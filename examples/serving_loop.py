@@ -80,6 +80,7 @@ class Server:
         angle = (torch.arange(most, device="cuda")[:, None].double()
                  * 1000.0 ** (-torch.arange(d // 2, device="cuda").double() / (d // 2)))
         self.table = torch.stack([angle.cos(), angle.sin()], -1).float().contiguous()
+        self.refused = ints([0])  # of the last step: requests whose tokens found no pages
         self.graph = None
 
     def project(self, x, w):
@@ -105,6 +106,7 @@ class Server:
     def forward(self, x, camera, begin, release, prompts=None):
         """New tokens x [tokens, width] of the requests, request by request; their results."""
         bufs = tg.PagesBuffers(self.pages, x.shape[0])
+        bufs.refused = self.refused
         tg.pages(self.pages, begin, bufs, release=release)
         h, g, d = self.heads, self.kv_heads, self.d
         y = None  # what the layer before has made of x
@@ -124,7 +126,7 @@ class Server:
             y = self.project(n, layer.mix)
         out = torch.empty_like(x)
         tg.norm(x, None, out, y=y, weight=e)
-        return out, bufs.refused
+        return out
 
     def capture(self):
         """The step of single tokens as a graph over buffers of its own."""
@@ -140,11 +142,12 @@ class Server:
         torch.cuda.current_stream().wait_stream(side)
         self.graph = torch.cuda.CUDAGraph()
         with torch.cuda.graph(self.graph):
-            self.y, _ = self.forward(self.x, self.camera, self.begin, self.release)
+            self.y = self.forward(self.x, self.camera, self.begin, self.release)
 
     def step(self, tokens, cameras, ended, replay=True):
         """One step: tokens[p] is the list of place p's new tokens ([width] each), None or empty for
-        none; ended: places whose requests have ended before it. Returns, by place, the results."""
+        none; ended: places whose requests have ended before it. Returns, by place, the results;
+        raises where a request found no pages for its tokens."""
         new = [t if t is not None else [] for t in tokens]
         begin = np.concatenate([[0], np.cumsum([len(t) for t in new])])
         flat = [row for t in new for row in t]
@@ -165,9 +168,10 @@ class Server:
             prompts = (ints(first.tolist(), torch.int64), ints(np.diff(begin).tolist()))
             if all(len(t) <= 1 for t in new):
                 prompts = None
-            y, refused = self.forward(torch.stack(flat), ints(camera), ints(begin.tolist()),
-                                      ints(release), prompts)
-            assert int(refused) == 0, "the cache is full"
+            y = self.forward(torch.stack(flat), ints(camera), ints(begin.tolist()),
+                             ints(release), prompts)
+        if int(self.refused):  # their tokens are nowhere, and no results
+            raise RuntimeError("the cache is full")
         return [y[begin[p]:begin[p + 1]] for p in range(len(new))]
 
 

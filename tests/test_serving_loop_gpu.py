@@ -58,3 +58,22 @@ def test_two_graphs_share_a_cache():
         got = first.step(tokens, [t[0] for t in todo], set(), replay=turn % 3 < 2)
         want = servers[1].step(tokens, [t[0] for t in todo], set(), replay=False)
         assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+@pytest.mark.parametrize("replay", [True, False])
+def test_a_full_cache_is_said(replay):
+    """A token that finds no page raises, in a replayed step as in an eager one; those who found
+    theirs have moved on, and it goes on once somebody has ended."""
+    example = load()
+    server = example.Server(places=3, n_pages=3, page=16, most=64, seed=6)
+    row = lambda: torch.ones(server.width, dtype=example.DTYPE, device="cuda")
+    prompt = lambda n: [row() for _ in range(n)]
+    server.step([prompt(15), prompt(16), prompt(9)], [0, 1, 2], set())
+    server.step([[row()], None, None], [0, 1, 2], set(), replay)
+    for _ in range(2):
+        with pytest.raises(RuntimeError, match="cache is full"):
+            server.step([None, [row()], [row()]], [0, 1, 2], set(), replay)
+    assert server.pages.kv_len.tolist() == [16, 16, 11]
+    server.step([None, [row()], None], [0, 1, 2], {0}, replay)
+    assert server.pages.kv_len.tolist() == [0, 17, 11]
+    assert int(server.pages.n_free) == 0
