@@ -754,7 +754,7 @@ typedef struct {
   int64_t *slot;           /* device out [n_tokens]: the cache row of each token, -1: none */
   int32_t *pos;            /* device out [n_tokens] or NULL: its place in its sequence, 0 where it
                               has no row */
-  int32_t *refused;        /* device out [1]: sequences whose tokens got no rows */
+  int32_t *refused;        /* device out [1]: sequences that were refused */
   int32_t n_seqs, n_tokens, n_pages;
   int32_t page_size;       /* >= 1; n_pages * page_size < 2^31 */
   int32_t max_pages;       /* pages that a sequence may hold, 1 .. 2^20 */
@@ -768,19 +768,21 @@ size_t tg_pages_workspace_bytes(int32_t n_seqs, int32_t n_tokens);
 
 /*
  * Page tables and cache rows of a step, from lengths. In this order: every sequence with
- * `release` pushes its pages on the stack (sequences in order, their pages in order) and holds no
- * rows; a sequence whose new tokens end inside its pages takes none; the others ask for pages,
- * and as long as the sum of what has been asked for, up to and with the sequence, does not pass
- * the stack, it gets them, from the top. A sequence that does not, or would pass max_pages or
- * 2^31 - 1 rows, is refused: its tokens get no rows, and it keeps what it holds. Tokens before
- * q_begin[0] and from q_begin[n_seqs] on belong to nobody and get no rows, so that a batch can be
- * padded. Nothing but the order of sequences decides, so two runs give the same. With kv_len_out
- * and n_free_out apart from the inputs, and no sequence that is both released and given tokens,
- * the call can be repeated. Lengths outside [0, max_pages * page_size] count as the nearest
- * inside, n_free outside [0, n_pages] alike; q_begin outside [0, n_tokens] alike, and a sequence
- * that ends before it begins has no tokens. A table entry outside [0, n_pages) gives its tokens
- * no row. A page belongs to one sequence: nothing counts who shares it. Enqueued on `stream`; the
- * library allocates nothing. Returns TG_E_INVAL (null pointer, negative count, n_seqs >
+ * `release` pushes its pages on the stack (sequences in order, their pages in order, entries outside
+ * [0, n_pages) left out, and no more than n_pages in all) and holds no rows; a sequence whose new
+ * tokens end inside its pages takes none; the others ask for pages, and as long as the sum of what
+ * has been asked for, up to and with the sequence, does not pass the stack, it gets them, from the
+ * top. A sequence that does not, or would pass max_pages or 2^31 - 1 rows, is refused: its tokens
+ * get no rows, and it keeps what it holds. Tokens before q_begin[0] and from q_begin[n_seqs] on
+ * belong to nobody and get no rows, so that a batch can be padded. Nothing but the order of
+ * sequences decides, so two runs give the same. With kv_len_out and n_free_out apart from the
+ * inputs, and no sequence that is both released and given tokens, the call can be repeated.
+ * Lengths outside [0, max_pages * page_size] count as the nearest inside, n_free outside [0,
+ * n_pages] alike; q_begin outside [0, n_tokens] alike, and a sequence that ends before it begins
+ * has no tokens. A table entry outside [0, n_pages) gives its tokens no row; one that comes off
+ * the caller's stack goes into the table as it is, and its sequence does not count as refused. A
+ * page belongs to one sequence: nothing counts who shares it. Enqueued on `stream`; the library
+ * allocates nothing. Returns TG_E_INVAL (null pointer, negative count, n_seqs >
  * TG_PAGES_MAX_SEQS, page_size < 1, max_pages outside [1, 2^20], n_pages * page_size >= 2^31, a
  * stride below max_pages), TG_E_WORKSPACE, TG_E_HIP. n_seqs == 0 and n_tokens == 0 enqueues
  * nothing, n_seqs == 0 alone gives slot, pos, n_free_out and refused.

@@ -1,10 +1,14 @@
-"""Serving operators where their other tests do not reach: the digits of attention weights."""
+"""Serving operators where their other tests do not reach: the digits of attention weights, and
+pages that are none on their way back to the stack."""
+import random
+
 import pytest
 import torch
 
 from gpu_helpers import say
+from paper_2404_09267_amd import tg
 import serving_reference as R
-from test_serving_gpu import DT, R_assert, cache, gen, normal, run_attend, widened
+from test_serving_gpu import DT, R_assert, cache, gen, ints, normal, run_attend, widened
 from token_reference import UNIT
 
 pytestmark = pytest.mark.gpu
@@ -48,3 +52,70 @@ def test_attend_pages_keeps_the_weights_digits(lens, page, heads, kv, d, extra, 
     want, bound = attend_bound(q, k, v, table, lens, page, **more)
     got = run_attend(q, k, v, table, lens, page, most, **more)
     R_assert(got, want, bound, "digits")
+
+
+# --------------------------------------------------------------------------------- pages
+
+def same(got, want, name):
+    off = (got.cpu() != torch.tensor(want, dtype=got.dtype)).sum()
+    assert int(off) == 0, f"{name}: {int(off)} differ"
+
+
+def freed(table, lens, release, page, n_pages):
+    """Pages that go back, in order: what is no page is left out."""
+    back = [p for row, n, r in zip(table, lens, release) if r for p in row[:-(-n // page)]]
+    return [p for p in back if 0 <= p < n_pages]
+
+
+@pytest.mark.parametrize("seqs,cols", [(3, 3), (40, 100), (1500, 4), (2100, 2)])
+def test_pages_that_are_none_do_not_go_back(seqs, cols):
+    """A sequence that ends with entries that are no page gives back the others: nobody else is
+    given what is none, and the count of free pages is of pages."""
+    say("pages none", seqs, cols)
+    r, page = random.Random(seqs), 4
+    n_pages = seqs * cols
+    order = list(range(n_pages))
+    r.shuffle(order)
+    lens = [r.randint(0, cols * page) for _ in range(seqs)]
+    table = [[-1] * cols for _ in range(seqs)]
+    for row, n in zip(table, lens):
+        for i in range(-(-n // page)):
+            row[i] = order.pop()
+    release = [int(r.random() < 0.6) for _ in range(seqs)]
+    release[0], lens[0] = 1, cols * page
+    for row, ends in zip(table, release):
+        for i in range(cols):
+            if ends and r.random() < 0.2:
+                row[i] = r.choice([-1, n_pages, -(1 << 31), (1 << 31) - 1])
+    table[0][1] = n_pages
+    free = order[:1]  # next to nothing but what goes back
+    new = [r.choice([0, 1, 1, 2, page + 1]) for _ in range(seqs)]
+    begin = [0]
+    for n in new:
+        begin.append(begin[-1] + n)
+    stack = free + freed(table, lens, release, page, n_pages)
+    want = R.pages(begin, [0 if e else n for e, n in zip(release, lens)], table, stack, len(stack),
+                   page, n_pages, begin[-1])
+    dev = tg.Pages(ints(table), ints(lens), page, ints(free + [-5] * (n_pages - len(free))),
+                   ints([len(free)]))
+    bufs = tg.PagesBuffers(dev, begin[-1])
+    tg.pages(dev, ints(begin), bufs, release=ints(release))
+    torch.cuda.synchronize()
+    assert int(dev.n_free) == len(want["free"]) and int(bufs.refused) == want["refused"]
+    same(dev.free[:len(want["free"])], want["free"], "free")
+    same(dev.table, want["table"], "table")
+    same(dev.kv_len, want["kv_len"], "kv_len")
+    same(bufs.slot, want["slot"], "slot")
+    same(bufs.pos[:, 0], want["pos"], "pos")
+
+
+def test_pages_more_than_there_are_go_back():
+    """Rows that name pages twice, and none among them: the stack holds as many as there are."""
+    say("pages too many")
+    table = [[i % 7 if i % 3 else 1 << 20 for i in range(s, s + 1200)] for s in range(5)]
+    dev = tg.Pages(ints(table), ints([1200] * 5), 1, ints([3] * 2 + [-5] * 1998), ints([2]))
+    bufs = tg.PagesBuffers(dev, 0)
+    tg.pages(dev, ints([0] * 6), bufs, release=ints([1] * 5))
+    torch.cuda.synchronize()
+    assert int(dev.n_free) == 2000
+    same(dev.free, ([3, 3] + freed(table, [1200] * 5, [1] * 5, 1, 2000))[:2000], "free")
