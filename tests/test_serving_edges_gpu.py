@@ -1,5 +1,6 @@
-"""Serving operators where their other tests do not reach: the digits of attention weights, and
-pages that are none on their way back to the stack."""
+"""Serving operators where their other tests do not reach: the digits of attention weights,
+lengths past every bound where keys are cut, and pages that are none on their way back to the
+stack."""
 import random
 
 import pytest
@@ -52,6 +53,26 @@ def test_attend_pages_keeps_the_weights_digits(lens, page, heads, kv, d, extra, 
     want, bound = attend_bound(q, k, v, table, lens, page, **more)
     got = run_attend(q, k, v, table, lens, page, most, **more)
     R_assert(got, want, bound, "digits")
+
+
+@pytest.mark.parametrize("window", [0, 50])
+@pytest.mark.parametrize("max_kv", [5000, 20000, 1 << 30])
+def test_attend_pages_lengths_past_the_bound(max_kv, window):
+    """Lengths below 0 and up to 2^31 - 1 where keys are cut into ranges: the query stands at the
+    last key that is claimed, and sees those that there are."""
+    say("attend_pages lengths", max_kv, window)
+    g, lens, page = gen(11), [700, 64, 0, 33], 16
+    k, v, table = cache(g, lens, page, 2, 64, torch.bfloat16)
+    table = widened(table, page, 20000)
+    k, v = torch.nan_to_num(k, nan=0.5), torch.nan_to_num(v, nan=0.25)
+    q = normal(g, 4, 8, 64, dtype=torch.bfloat16)
+    claimed = [700, 64, -5, (1 << 31) - 1]
+    got = run_attend(q, k, v, table, claimed, page, max_kv, scale=0.1, window=window)
+    seen = 3 if window else 4
+    want, bound = R.attend_pages(q[:seen], k, v, table[:seen], claimed[:seen], page, 0.1,
+                                 window=window, max_kv=max_kv)
+    R_assert(got[:seen], want, bound, "claimed")
+    assert bool((got[seen:] == 0).all())  # the last 50 of what is claimed are not there
 
 
 # --------------------------------------------------------------------------------- pages
