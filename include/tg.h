@@ -838,8 +838,8 @@ size_t tg_attend_pages_workspace_bytes(int32_t n_seqs, int32_t max_kv_len, int32
  * multiple of 8, heads that n_kv_heads does not divide, a negative window, page_size or max_pages
  * < 1, n_pages * page_size >= 2^31, a bad type, scale or cap, a table_stride below max_pages, q,
  * k, v or out not 16-byte aligned, another stride that is negative, not a multiple of 8 or, of
- * rows, over 2^22), TG_E_WORKSPACE, TG_E_HIP. n_seqs == 0, or n_q_rows == 0 with q_begin,
- * enqueues nothing.
+ * rows, over 2^22, more than 2^31 - 2^20 workgroups of a sequence, a key head and up to 16 query
+ * heads), TG_E_WORKSPACE, TG_E_HIP. n_seqs == 0, or n_q_rows == 0 with q_begin, enqueues nothing.
  */
 int tg_attend_pages(const tg_attend_pages_args *args, void *stream);
 
@@ -886,7 +886,8 @@ typedef struct {
  * the same. x_out and h must not overlap each other, nor an input but as above. Enqueued on
  * `stream`; allocates nothing. Returns TG_E_INVAL (x NULL, x_out and h both NULL, negative count,
  * n outside [1, TG_NORM_MAX_N], a bad kind, type, eps, scale or stride, y NULL with a gate,
- * gate_row without gate, gate with n_gates < 1), TG_E_HIP. n_tokens == 0 enqueues nothing.
+ * gate_row without gate, gate with n_gates < 1, more than 2^31 - 2^20 rows of over 1,024 values),
+ * TG_E_HIP. n_tokens == 0 enqueues nothing.
  */
 int tg_norm(const tg_norm_args *args, void *stream);
 
@@ -907,7 +908,8 @@ typedef struct {
  * zeros has scale 0 and integers 0. A row with an infinity or NaN has no such integers: its scale
  * is NaN and they are 0, so that its products are NaN, and those of no other row. q must not
  * overlap x. Enqueued on `stream`; allocates nothing. Returns TG_E_INVAL (null pointer, negative
- * count, k < 1, a bad type or stride), TG_E_HIP. n_rows == 0 enqueues nothing.
+ * count, k < 1, a bad type or stride, more than 2^31 - 2^20 rows of over 1,024 values), TG_E_HIP.
+ * n_rows == 0 enqueues nothing.
  */
 int tg_quantize(const tg_quantize_args *args, void *stream);
 
@@ -934,8 +936,8 @@ typedef struct {
  * binary32, and the result once to the type. All 256 integers may occur. y must not overlap an
  * input. Enqueued on `stream`; allocates nothing and needs no workspace. Returns TG_E_INVAL (null
  * pointer, negative count, k outside [16, TG_PROJECT_I8_MAX_K] or not a multiple of 16, n < 1,
- * n_tokens or n over 2^30, a bad type or stride, x or w not 16-byte aligned), TG_E_HIP. n_tokens
- * == 0 enqueues nothing.
+ * n_tokens or n over 2^30, a bad type or stride, x or w not 16-byte aligned, more results than a
+ * launch has workgroups for: over 2^37), TG_E_HIP. n_tokens == 0 enqueues nothing.
  */
 int tg_project_i8(const tg_project_i8_args *args, void *stream);
 

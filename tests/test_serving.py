@@ -146,6 +146,18 @@ def test_project_i8_refuses(change):
     assert project(**change) == tg.E_INVAL
 
 
+def test_more_than_a_launch_holds():
+    """Sizes within every other limit that no grid holds; no card holds their arrays either."""
+    most = (1 << 31) - 1
+    assert attend(n_seqs=1 << 20, n_heads=2048, n_kv_heads=2048, max_kv_len=500) == tg.E_INVAL
+    assert norm(n_tokens=most, n=1100, x_stride=1100, y_stride=1100, gate_stride=1100,
+                x_out_stride=1100, h_stride=1100) == tg.E_INVAL
+    assert quantize(n_rows=most, k=1100, x_stride=1100, q_stride=1100) == tg.E_INVAL
+    assert quantize(n_rows=most, k=40000, x_stride=40000, q_stride=40000) == tg.E_INVAL
+    for tokens, n in ((1 << 30, 1 << 10), (1 << 20, 1 << 20), (300, 1 << 30), (1 << 30, 400)):
+        assert project(n_tokens=tokens, n=n, y_stride=n) == tg.E_INVAL, (tokens, n)
+
+
 def test_nothing():
     assert norm(n_tokens=0) == quantize(n_rows=0) == project(n_tokens=0) == tg.OK
     L = tg.lib()
