@@ -55,6 +55,30 @@ def test_attend_pages_keeps_the_weights_digits(lens, page, heads, kv, d, extra, 
     R_assert(got, want, bound, "digits")
 
 
+@pytest.mark.parametrize("most", [None, 20000])  # of the lengths; the larger has keys cut
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("group", [1, 8, 9, 20])  # a weight's parts beside each other, or not
+@pytest.mark.parametrize("even", [True, False])  # weights that are all 1, with nothing left, or not
+def test_attend_pages_infinite_values(even, group, dtype, most):
+    """An infinite value that has a weight is its column's result, whatever sign the weight's second
+    part has, and NaN makes NaN; other columns do not see them."""
+    say("attend_pages infinite", even, group, dtype, most)
+    g, page, d, n, dt = gen(21), 16, 40, 170, DT[dtype]
+    k, v, table = cache(g, [n], page, 1, d, dt)
+    table = widened(table, page, most)
+    q = normal(g, 1, group, d, dtype=dt, gain=0.0 if even else 1.0)
+    row = lambda j: int(table[0, j // page]) * page + j % page
+    want, bound = R.attend_pages(q, k, v, table, [n], page, 0.1)
+    inf, nan = float("inf"), float("nan")
+    for j, c, bad in ((3, 5, inf), (n - 1, 7, -inf), (77, 9, nan), (40, 11, inf), (41, 11, -inf)):
+        v[row(j), 0, c] = bad
+    got = run_attend(q, k, v, table, [n], page, most, scale=0.1)
+    assert bool((got[0, :, 5] == inf).all()) and bool((got[0, :, 7] == -inf).all())
+    assert bool(torch.isnan(got[0, :, [9, 11]]).all())
+    fine = [c for c in range(d) if c not in (5, 7, 9, 11)]
+    R_assert(got[:, :, fine], want[:, :, fine], bound[:, :, fine], "others")
+
+
 @pytest.mark.parametrize("window", [0, 50])
 @pytest.mark.parametrize("max_kv", [5000, 20000, 1 << 30])
 def test_attend_pages_lengths_past_the_bound(max_kv, window):
