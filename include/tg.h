@@ -833,13 +833,17 @@ size_t tg_attend_pages_workspace_bytes(int32_t n_seqs, int32_t max_kv_len, int32
  * see are not read. Weights go into the product with v as two values of the type, a rounding and
  * what that leaves (16 bits of bfloat16, 22 of binary16, there as 2^7 times their share of the
  * largest or more); their sum is of the same. An infinite value whose weight rounds to 0 makes
- * NaN. Distances up to 2^24 are exact. out must not overlap an input. Enqueued on `stream`; allocates nothing. Returns TG_E_INVAL (null pointer, negative
- * count, n_seqs > TG_PAGES_MAX_SEQS, max_kv_len > 2^30, d outside [8, TG_ATTEND_MAX_D] or not a
- * multiple of 8, heads that n_kv_heads does not divide, a negative window, page_size or max_pages
- * < 1, n_pages * page_size >= 2^31, a bad type, scale or cap, a table_stride below max_pages, q,
- * k, v or out not 16-byte aligned, another stride that is negative, not a multiple of 8 or, of
- * rows, over 2^22, more than 2^31 - 2^20 workgroups of a sequence, a key head and up to 16 query
- * heads), TG_E_WORKSPACE, TG_E_HIP. n_seqs == 0, or n_q_rows == 0 with q_begin, enqueues nothing.
+ * NaN. Distances up to 2^24 are exact. One query a sequence: a prompt's other new tokens are not
+ * attended here. Of up to 1,024 sequences with many keys, all keys are cut into equal shares; of
+ * more, a sequence's stay with one workgroup for each key head, so that a long one among short ones
+ * is better given in a call of its own. out must not overlap an input. Enqueued on `stream`;
+ * allocates nothing. Returns TG_E_INVAL (null pointer, negative count, n_seqs > TG_PAGES_MAX_SEQS,
+ * max_kv_len > 2^30, d outside [8, TG_ATTEND_MAX_D] or not a multiple of 8, heads that n_kv_heads
+ * does not divide, a negative window, page_size or max_pages < 1, n_pages * page_size >= 2^31, a
+ * bad type, scale or cap, a table_stride below max_pages, q, k, v or out not 16-byte aligned,
+ * another stride that is negative, not a multiple of 8 or, of rows, over 2^22, more than 2^31 - 2^20
+ * workgroups of a sequence, a key head and up to 16 query heads), TG_E_WORKSPACE, TG_E_HIP. n_seqs
+ * == 0, or n_q_rows == 0 with q_begin, enqueues nothing.
  */
 int tg_attend_pages(const tg_attend_pages_args *args, void *stream);
 
@@ -933,11 +937,12 @@ typedef struct {
  * A projection in 8-bit integers with a scale for each token and output:
  *   y[t][j] = (x_scale[t] * w_scale[j]) * sum_i x[t][i] w[j][i].
  * The sum is exact, in 32 bits; it, the scales' product and the result are rounded once each in
- * binary32, and the result once to the type. All 256 integers may occur. y must not overlap an
- * input. Enqueued on `stream`; allocates nothing and needs no workspace. Returns TG_E_INVAL (null
- * pointer, negative count, k outside [16, TG_PROJECT_I8_MAX_K] or not a multiple of 16, n < 1,
- * n_tokens or n over 2^30, a bad type or stride, x or w not 16-byte aligned, more results than a
- * launch has workgroups for: over 2^37), TG_E_HIP. n_tokens == 0 enqueues nothing.
+ * binary32, and the result once to the type. All 256 integers may occur. y on 64 bytes with a
+ * stride that is a multiple of 32 is the quickest, whatever n is. y must not overlap an input.
+ * Enqueued on `stream`; allocates nothing and needs no workspace. Returns TG_E_INVAL (null pointer,
+ * negative count, k outside [16, TG_PROJECT_I8_MAX_K] or not a multiple of 16, n < 1, n_tokens or n
+ * over 2^30, a bad type or stride, x or w not 16-byte aligned, more results than a launch has
+ * workgroups for: over 2^37), TG_E_HIP. n_tokens == 0 enqueues nothing.
  */
 int tg_project_i8(const tg_project_i8_args *args, void *stream);
 

@@ -23,9 +23,10 @@
 // cut into as many ranges of one length as there is room for workgroups, found on the device, so
 // that each has as much to read whatever the lengths are; a workgroup goes from sequence to
 // sequence, and join_kernel joins what a sequence has in several ranges, in a set order. bfloat16:
-// 8 sequences of up to 100,003 keys, 16 heads of 128 over 2, 583 MB: 111 us, 5.3 TB/s; 256 of up to
-// 4,096, 32 heads over 8, 2.4 GB: 440 us, 5.4; 20 of up to 1,600, 16 heads of 64 over 4: 13 us, a
-// launch and a chain of loads (length, pages, keys, and those of 6 tiles a wave).
+// 8 sequences of up to 100,003 keys, 16 heads of 128 over 2, 583 MB: 107 to 111 us, 5.3 TB/s; 256 of
+// up to 4,096, 32 heads over 8, 2.4 GB: 440 to 467 us by card, 5.1 to 5.4; 20 of up to 1,600, 16 heads
+// of 64 over 4: 13.4 us with a cap and 10.6 without, a launch and a chain of loads (length, pages,
+// keys, and those of 6 tiles a wave) and of what each tile is put through.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -192,7 +193,10 @@ __device__ __forceinline__ int place_of(int r, int c) {
 // ------------------------------------------------------------------------ the cut of all keys
 
 constexpr int kKeys = 32;      // of a tile
-constexpr int kMaxCut = 1024;  // sequences, where any is cut
+// Sequences, where any is cut: a wave has them in registers. Of more, a long one among short ones
+// is one workgroup's for each key head (one of 100,003 keys, 16 heads of 128 over 2, among 1,024: 150
+// us, among 1,025: 544).
+constexpr int kMaxCut = 1024;
 
 // All sequences' tiles one after the other are cut into ranges of `length`; a workgroup has one,
 // whatever it holds of how many sequences. What range w has of sequence s is part w + s: from one
@@ -349,7 +353,8 @@ __global__ __launch_bounds__(kWaves * 64, per_simd(kD, kBufs)) void attend_pages
   // times kRun rows, that many rows lie one after the other: a lane's place among them stays the
   // same, and only where they start is looked up. Else every lane has addresses of its own. Runs of
   // 8 cost wide heads nothing (33 sequences of 3,001, pages of 24: 17.4 -> 15.5 us), those of 64 5 %
-  // where pages are of 16 (20 of 1,600: 13.7 for 13.0).
+  // where pages are of 16 (20 of 1,600: 13.7 for 13.0), which is why pages of 8 and 24 go row by row
+  // there (20 of 1,600 without a cap: 12.0 and 12.3, pages of 16 to 64 10.6 to 10.4).
   constexpr int kRun = kD > 64 ? 8 : 16, kRuns = kKeys / kRun;
   uint32_t piece[2][kLoads / 2];
   const auto pieces = [&](uint32_t bytes, uint32_t(&to)[kLoads / 2]) {

@@ -203,6 +203,8 @@ int launch(const NormParams &P, int piece, hipStream_t s) {
   //   25,600 x 2,048: 91.9, 81.2, 82.7  25,600 x 4,096: 186, 161, 172
   // Up to 256 values 16 lanes a row: 409,600 x 128 89 us, 261 with a wave a row, 14,768 x 19 5.5 for
   // 11.5; with 32 values a lane up to 512, 6,400 x 512 13.3 for 9.2, 102,400 x 512 83 for 89.
+  // Over 16,384 values off 16 bytes, 15 to 28 registers go to scratch: a norm alone of 2,000 x 32,768
+  // takes 46 us, by 4 values 51, of 32,767 one at a time 61.
   const bool few = int64_t(P.n_tokens) * P.n <= kFew;
   if (P.n <= kNarrow) return launch_rows<kType, 16, 1>(P, piece, s);
   if (P.n <= 2 * kNarrow) return launch_rows<kType, 16, 2>(P, piece, s);

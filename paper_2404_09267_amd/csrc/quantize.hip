@@ -162,7 +162,9 @@ __global__ __launch_bounds__(kGroupThreads<R>) void quantize_kernel(const Quanti
   }
 }
 
-// Rows longer than registers hold, value by value; the row is read twice.
+// Rows longer than registers hold, value by value; the row is read twice. Left simple, as no layer
+// here has such rows: 2,000 x 40,000 118 us, 2.4 times what its bytes take at a copy's rate, 200 x
+// 100,003 66, 5.4 times (2,000 x 32,768, from registers, 37, 0.93 times).
 template <int kType, int R>
 __global__ __launch_bounds__(kGroupThreads<R>) void quantize_long_kernel(const QuantizeParams P) {
   typedef typename Num<kType>::E E;
