@@ -841,9 +841,9 @@ size_t tg_attend_pages_workspace_bytes(int32_t n_seqs, int32_t max_kv_len, int32
  * max_kv_len > 2^30, d outside [8, TG_ATTEND_MAX_D] or not a multiple of 8, heads that n_kv_heads
  * does not divide, a negative window, page_size or max_pages < 1, n_pages * page_size >= 2^31, a
  * bad type, scale or cap, a table_stride below max_pages, q, k, v or out not 16-byte aligned,
- * another stride that is negative, not a multiple of 8 or, of rows, over 2^22, more than 2^31 - 2^20
- * workgroups of a sequence, a key head and up to 16 query heads), TG_E_WORKSPACE, TG_E_HIP. n_seqs
- * == 0, or n_q_rows == 0 with q_begin, enqueues nothing.
+ * another stride that is negative, not a multiple of 8 or, of rows, over 2^22, more than 2^31 -
+ * 2^20 workgroups of a sequence, a key head and up to 16 query heads), TG_E_WORKSPACE, TG_E_HIP.
+ * n_seqs == 0, or n_q_rows == 0 with q_begin, enqueues nothing.
  */
 int tg_attend_pages(const tg_attend_pages_args *args, void *stream);
 

@@ -23,10 +23,10 @@
 // cut into as many ranges of one length as there is room for workgroups, found on the device, so
 // that each has as much to read whatever the lengths are; a workgroup goes from sequence to
 // sequence, and join_kernel joins what a sequence has in several ranges, in a set order. bfloat16:
-// 8 sequences of up to 100,003 keys, 16 heads of 128 over 2, 583 MB: 107 to 111 us, 5.3 TB/s; 256 of
-// up to 4,096, 32 heads over 8, 2.4 GB: 440 to 467 us by card, 5.1 to 5.4; 20 of up to 1,600, 16 heads
-// of 64 over 4: 13.4 us with a cap and 10.6 without, a launch and a chain of loads (length, pages,
-// keys, and those of 6 tiles a wave) and of what each tile is put through.
+// 8 sequences of up to 100,003 keys, 16 heads of 128 over 2, 583 MB: 107 to 111 us, 5.3 TB/s; 256
+// of up to 4,096, 32 heads over 8, 2.4 GB: 440 to 467 us by card, 5.1 to 5.4; 20 of up to 1,600, 16
+// heads of 64 over 4: 13.4 us with a cap and 10.6 without, a launch and a chain of loads (length,
+// pages, keys, and those of 6 tiles a wave) and of what each tile is put through.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -282,8 +282,9 @@ __device__ __forceinline__ float eight_on(float v) {
 
 constexpr int kXcds = 8;  // that workgroups go round
 
-// Waves of a SIMD that registers are to have room for: as many as LDS has where keys are not cut. Heads
-// of 64 get 4 with 3 asked for (126 registers); asked for 4, more than 8 a key head spill two.
+// Waves of a SIMD that registers are to have room for: as many as LDS has where keys are not cut.
+// Heads of 64 get 4 with 3 asked for (126 registers); asked for 4, more than 8 a key head spill
+// two.
 constexpr int per_simd(int d, int bufs) { return bufs > 1 ? 1 : d == 64 ? 3 : 2; }
 
 // Rows of a workgroup: 16 query heads that share a key head. Each of its waves takes every
@@ -352,9 +353,9 @@ __global__ __launch_bounds__(kWaves * 64, per_simd(kD, kBufs)) void attend_pages
   // The loads of a tile's keys or values to LDS. Where all its keys are seen, and pages are whole
   // times kRun rows, that many rows lie one after the other: a lane's place among them stays the
   // same, and only where they start is looked up. Else every lane has addresses of its own. Runs of
-  // 8 cost wide heads nothing (33 sequences of 3,001, pages of 24: 17.4 -> 15.5 us), those of 64 5 %
-  // where pages are of 16 (20 of 1,600: 13.7 for 13.0), which is why pages of 8 and 24 go row by row
-  // there (20 of 1,600 without a cap: 12.0 and 12.3, pages of 16 to 64 10.6 to 10.4).
+  // 8 cost wide heads nothing (33 sequences of 3,001, pages of 24: 17.4 -> 15.5 us), those of 64 5
+  // % where pages are of 16 (20 of 1,600: 13.7 for 13.0), which is why pages of 8 and 24 go row by
+  // row there (20 of 1,600 without a cap: 12.0 and 12.3, pages of 16 to 64 10.6 to 10.4).
   constexpr int kRun = kD > 64 ? 8 : 16, kRuns = kKeys / kRun;
   uint32_t piece[2][kLoads / 2];
   const auto pieces = [&](uint32_t bytes, uint32_t(&to)[kLoads / 2]) {

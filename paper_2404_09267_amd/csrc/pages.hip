@@ -128,8 +128,8 @@ __device__ __forceinline__ int owner_of(const Dealt &d, int i) {
 }
 
 // Pushes the pages of all sequences that have ended on the stack, whose `top` it moves; `q`: this
-// thread's sequence of the first turn. True in some threads if an entry is no page. kSift: those are
-// left out, which takes a prefix sum for every kThreads entries.
+// thread's sequence of the first turn. True in some threads if an entry is no page. kSift: those
+// are left out, which takes a prefix sum for every kThreads entries.
 template <bool kSift>
 __device__ __forceinline__ bool give_back(const PagesParams &P, Seq q, int64_t &top, Dealt &dealt,
                                           int (&waves)[kWaves]) {

@@ -10,9 +10,9 @@
 // the time). bfloat16: 25,600 x 4,096, k 4,096: 346 to 369 us by card, 2.33 to 2.48 POPS (a
 // library's product, which gives sums of 32 bits, 420; its best at any size 2.5 POPS); 8,192 x
 // 8,192, k 8,192: 414 to 425, 2.6; 8 x 1,536, k 1,024: 3.5 to 3.9, a launch. Between them one round
-// of small tiles hardly fills the pipeline: 3,500 x 2,048, k 2,048 20, 1.5; 512 x 4,096, k 4,096 14, 1.2.
-// Rows of y that do not start on 16 bytes take stores of 8 that straddle lines: 22,333 x 2,565, k 144
-// 58, 40 where they are 2,592 apart.
+// of small tiles hardly fills the pipeline: 3,500 x 2,048, k 2,048 20, 1.5; 512 x 4,096, k 4,096
+// 14, 1.2. Rows of y that do not start on 16 bytes take stores of 8 that straddle lines: 22,333 x
+// 2,565, k 144 58, 40 where they are 2,592 apart.
 //
 // Results lie transposed in the registers (a lane holds 4 outputs of one token), so that stores are
 // contiguous and a token's scale belongs to the lane. Both operands take the same values of k in
@@ -360,8 +360,8 @@ __global__ __launch_bounds__(kWt *kWn * 64, 2) void tile_kernel(const ProjectPar
 }
 
 // Tiles of 256 x 256, one a CU; those past the last whole round of the CUs by quarters, so that a
-// round of few tiles does not take as long as a whole one. All 256 registers are in use, and 8 bytes
-// a lane go to scratch.
+// round of few tiles does not take as long as a whole one. All 256 registers are in use, and 8
+// bytes a lane go to scratch.
 template <int kType>
 __global__ __launch_bounds__(512, 2) void tile_and_rest_kernel(const ProjectParams P) {
   __shared__ __attribute__((aligned(16))) int8_t lds[kLds<256, 256, 2>];
